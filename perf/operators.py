@@ -66,9 +66,9 @@ def draw(rng):
     """Another case of the same ranges: one token to long caches, small and odd batches, every type and layout."""
     op = rng.choice(["diff_step", "diff_step", "diff_prompt", "weights", "weights", "select", "compact"])
     if op == "select":
-        N, groups = _log(rng, 64, 65536), rng.choice([1, 2, 4, 8])
+        N, groups = _log(rng, 128, 65536), rng.choice([1, 2, 4, 8])
         B = _log(rng, 1, max(1, min(48, 8 * 32768 * 48 // (N * groups))))
-        budget = _log(rng, max(1, N // 16), N)
+        budget = _log(rng, N // 16, 3 * N // 4)
         first, last = rng.choice([0, 4]), rng.choice([1, 16, 64])
         return dict(op=op, B=B, groups=groups, N=N, budget=max(budget, first + last), first=first, last=last, ragged=rng.random() < 0.5)
     page = rng.choice([0, 0, 16, 64])
@@ -104,7 +104,7 @@ def draw(rng):
     case = _attn(op, "drawn", B=B, L=L, Hq=Hkv * G, Hkv=Hkv, d=d, w=rng.choice([16, 64, 200]), N=N, page=page, q_len=q_len, dtype=dtype, ragged=rng.random() < 0.5)
     if op == "diff_step":
         return case | dict(norm=rng.random() < 0.7, lambda_heads=rng.choice([1, Hkv * G]))
-    return case | dict(group=rng.choice([1, 1, 2 if Hkv > 1 else 1, Hkv]), maps=maps, gate=rng.random() < 0.5, decay=rng.choice([0.0, 0.5, 1.0]))
+    return case | dict(group=rng.choice([1, 1, 2 if Hkv > 1 else 1, Hkv]), maps=maps, gate=rng.random() < 0.5, decay=rng.choice([0.0, 0.5, 1.0]) if N > 8 else 1.0)
 
 
 # ---- inputs -------------------------------------------------------------------------------------------------------
