@@ -90,6 +90,7 @@ def draw(rng):
                      lambda_heads=rng.choice([1, Hkv * G])) | {"name": "drawn"}
     dtype = rng.choice(["bf16", "bf16", "bf16", "e4m3", "f32"])
     d = 128 if dtype == "e4m3" else rng.choice([64, 128, 128])
+    page = 32 if dtype == "e4m3" and page == 16 else page       # the attention on 8-bit caches takes pages of 32 tokens up
     L = rng.choice([1, 1, 2, 3])
     maps = 2 if op == "diff_step" else rng.choice([1, 1, 2])
     q_len = rng.choice([1, 1, 1, 2, 3]) if dtype != "f32" else 1
