@@ -27,6 +27,9 @@ EXPORTS = (
     "plt_decode_attn_step",
     "plt_seq_attn_create", "plt_seq_attn_run", "plt_seq_attn_check", "plt_seq_attn_destroy", "plt_seq_attn_last_error",
 )
+DIFF_EXPORTS = tuple(f"plt_diff_attn_{n}" for n in ("create", "run", "step", "check", "destroy", "last_error",
+                                                  "workspace_bytes")) + \
+    tuple(f"plt_diff_seq_attn_{n}" for n in ("create", "run", "check", "destroy", "last_error"))
 PLT_NO_ALLOC_SCRATCH_BYTES = 16 << 20
 
 
@@ -87,6 +90,29 @@ class SeqArgs(ctypes.Structure):
     ]
 
 
+class DiffConfig(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("max_batch", ctypes.c_int32),
+        ("L", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("max_seq_len", ctypes.c_int32), ("w", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("sm_scale", ctypes.c_float), ("device", ctypes.c_int32), ("loop_offset", ctypes.POINTER(ctypes.c_int32)),
+        ("kernel_path", ctypes.c_int32), ("kv_dtype", ctypes.c_int32), ("q_len", ctypes.c_int32),
+        ("typical_seq_len", ctypes.c_int32), ("lambda_init", ctypes.c_float), ("norm_eps", ctypes.c_float),
+    ]
+
+
+class DiffSeqConfig(ctypes.Structure):
+    _fields_ = SeqConfig._fields_ + [("lambda_init", ctypes.c_float), ("norm_eps", ctypes.c_float)]
+
+
+class DiffWeights(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("lambda_heads", ctypes.c_int32), ("lambda_q1", ctypes.c_void_p),
+        ("lambda_k1", ctypes.c_void_p), ("lambda_q2", ctypes.c_void_p), ("lambda_k2", ctypes.c_void_p),
+        ("norm_gain", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -117,7 +143,19 @@ def load_library() -> ctypes.CDLL:
         lib.plt_seq_attn_destroy.argtypes = [h]
         lib.plt_seq_attn_last_error.argtypes = [h]
         lib.plt_seq_attn_last_error.restype = ctypes.c_char_p
-        for name in EXPORTS:
+        lib.plt_diff_attn_create.argtypes = [ctypes.POINTER(DiffConfig), ctypes.POINTER(h)]
+        lib.plt_diff_attn_workspace_bytes.argtypes = [ctypes.POINTER(DiffConfig), ctypes.POINTER(ctypes.c_size_t)]
+        lib.plt_diff_attn_run.argtypes = [h, ctypes.POINTER(Args), ctypes.POINTER(DiffWeights), ctypes.c_void_p]
+        lib.plt_diff_attn_step.argtypes = [h, ctypes.POINTER(Args), ctypes.POINTER(StepArgs),
+                                           ctypes.POINTER(DiffWeights), ctypes.c_void_p]
+        lib.plt_diff_seq_attn_create.argtypes = [ctypes.POINTER(DiffSeqConfig), ctypes.POINTER(h)]
+        lib.plt_diff_seq_attn_run.argtypes = [h, ctypes.POINTER(SeqArgs), ctypes.POINTER(DiffWeights), ctypes.c_void_p]
+        for prefix in ("plt_diff_attn", "plt_diff_seq_attn"):
+            getattr(lib, prefix + "_check").argtypes = [h, ctypes.c_void_p, ctypes.POINTER(ctypes.c_uint32)]
+            getattr(lib, prefix + "_destroy").argtypes = [h]
+            getattr(lib, prefix + "_last_error").argtypes = [h]
+            getattr(lib, prefix + "_last_error").restype = ctypes.c_char_p
+        for name in EXPORTS + DIFF_EXPORTS:
             if not name.endswith("_last_error"):
                 getattr(lib, name).restype = ctypes.c_int
         _lib = lib
@@ -319,3 +357,128 @@ def plt_seq_attn_check(handle, stream: int = 0) -> int:
 
 def plt_seq_attn_destroy(handle) -> None:
     load_library().plt_seq_attn_destroy(handle)
+
+
+# ---- differential attention (plt_diff_attn.h) ---------------------------------------------------------------------
+def _offsets(c, loop_offset: Optional[Sequence[int]]) -> None:
+    if loop_offset is not None:
+        arr = (ctypes.c_int32 * len(loop_offset))(*[int(x) for x in loop_offset])
+        c._keep = arr
+        c.loop_offset = ctypes.cast(arr, ctypes.POINTER(ctypes.c_int32))
+
+
+def _call(name: str, handle, *args) -> None:
+    """Calls the entry point `name`; `name`'s family (all but its last word) has the message of a failure."""
+    lib = load_library()
+    st = getattr(lib, name)(handle, *args)
+    if st != PLT_OK:
+        msg = getattr(lib, name.rpartition("_")[0] + "_last_error")(handle)
+        raise PltError(st, msg.decode() if msg else "")
+
+
+def _create(family: str, config) -> ctypes.c_void_p:
+    lib, handle = load_library(), ctypes.c_void_p()
+    st = getattr(lib, family + "_create")(ctypes.byref(config), ctypes.byref(handle))
+    if st != PLT_OK:
+        msg = getattr(lib, family + "_last_error")(None)
+        raise PltError(st, msg.decode() if msg else "")
+    return handle
+
+
+def _check(family: str, handle, stream: int) -> int:
+    lib, bits = load_library(), ctypes.c_uint32()
+    st = getattr(lib, family + "_check")(handle, ctypes.c_void_p(stream), ctypes.byref(bits))
+    if st not in (PLT_OK, PLT_ERR_DEVICE_CHECK):
+        msg = getattr(lib, family + "_last_error")(handle)
+        raise PltError(st, msg.decode() if msg else "")
+    return int(bits.value)
+
+
+def _workspace_bytes(family: str, config) -> int:
+    lib, out = load_library(), ctypes.c_size_t()
+    st = getattr(lib, family + "_workspace_bytes")(ctypes.byref(config), ctypes.byref(out))
+    if st != PLT_OK:
+        msg = getattr(lib, family + "_last_error")(None)
+        raise PltError(st, msg.decode() if msg else "")
+    return int(out.value)
+
+
+def make_diff_config(dtype, max_batch: int, L: int, Hq: int, Hkv: int, d: int, max_seq_len: int, w: int,
+                     page_size: int = 0, sm_scale: float = 0.0, device: int = 0,
+                     loop_offset: Optional[Sequence[int]] = None, kernel_path: int = 0, kv_dtype=0, q_len: int = 0,
+                     typical_seq_len: int = 0, lambda_init: float = 0.8, norm_eps: float = 1e-5) -> DiffConfig:
+    c = DiffConfig()
+    c.struct_size = ctypes.sizeof(DiffConfig)
+    c.dtype = {"f32": PLT_F32, "bf16": PLT_BF16}.get(dtype, dtype)
+    c.max_batch, c.L, c.Hq, c.Hkv, c.d = max_batch, L, Hq, Hkv, d
+    c.max_seq_len, c.w, c.page_size, c.sm_scale, c.device = max_seq_len, w, page_size, sm_scale, device
+    c.kernel_path, c.kv_dtype = kernel_path, {"": PLT_KV_SAME, "e4m3": PLT_KV_E4M3}.get(kv_dtype, kv_dtype)
+    c.q_len, c.typical_seq_len, c.lambda_init, c.norm_eps = q_len, typical_seq_len, lambda_init, norm_eps
+    _offsets(c, loop_offset)
+    return c
+
+
+def make_diff_seq_config(max_batch: int, L: int, Hq: int, Hkv: int, d: int, max_seq_len: int, w: int,
+                         sm_scale: float = 0.0, device: int = 0, loop_offset: Optional[Sequence[int]] = None,
+                         lambda_init: float = 0.8, norm_eps: float = 1e-5) -> DiffSeqConfig:
+    c = DiffSeqConfig()
+    c.struct_size = ctypes.sizeof(DiffSeqConfig)
+    c.max_batch, c.L, c.Hq, c.Hkv, c.d, c.max_seq_len, c.w = max_batch, L, Hq, Hkv, d, max_seq_len, w
+    c.sm_scale, c.device, c.lambda_init, c.norm_eps = sm_scale, device, lambda_init, norm_eps
+    _offsets(c, loop_offset)
+    return c
+
+
+def make_diff_weights(lambda_q1, lambda_k1, lambda_q2, lambda_k2, norm_gain=None,
+                      lambda_heads: Optional[int] = None) -> DiffWeights:
+    """The learned parameters (fp32 device tensors); lambda_heads: rows of the four vectors (their shape's, if they have one)."""
+    w = DiffWeights()
+    w.struct_size = ctypes.sizeof(DiffWeights)
+    if lambda_heads is None:
+        lambda_heads = lambda_q1.shape[0] if len(lambda_q1.shape) > 1 else 1
+    w.lambda_heads = lambda_heads
+    w.lambda_q1, w.lambda_k1, w.lambda_q2, w.lambda_k2 = (_ptr(x) for x in (lambda_q1, lambda_k1, lambda_q2, lambda_k2))
+    w.norm_gain = _ptr(norm_gain)
+    w._keep = (lambda_q1, lambda_k1, lambda_q2, lambda_k2, norm_gain)
+    return w
+
+
+def plt_diff_attn_create(config: DiffConfig) -> ctypes.c_void_p:
+    return _create("plt_diff_attn", config)
+
+
+def plt_diff_attn_workspace_bytes(config: DiffConfig) -> int:
+    return _workspace_bytes("plt_diff_attn", config)
+
+
+def plt_diff_attn_run(handle, args: Args, weights: DiffWeights, stream: int = 0) -> None:
+    _call("plt_diff_attn_run", handle, ctypes.byref(args), ctypes.byref(weights), ctypes.c_void_p(stream))
+
+
+def plt_diff_attn_step(handle, args: Args, step: StepArgs, weights: DiffWeights, stream: int = 0) -> None:
+    _call("plt_diff_attn_step", handle, ctypes.byref(args), ctypes.byref(step), ctypes.byref(weights),
+          ctypes.c_void_p(stream))
+
+
+def plt_diff_attn_check(handle, stream: int = 0) -> int:
+    return _check("plt_diff_attn", handle, stream)
+
+
+def plt_diff_attn_destroy(handle) -> None:
+    load_library().plt_diff_attn_destroy(handle)
+
+
+def plt_diff_seq_attn_create(config: DiffSeqConfig) -> ctypes.c_void_p:
+    return _create("plt_diff_seq_attn", config)
+
+
+def plt_diff_seq_attn_run(handle, args: SeqArgs, weights: DiffWeights, stream: int = 0) -> None:
+    _call("plt_diff_seq_attn_run", handle, ctypes.byref(args), ctypes.byref(weights), ctypes.c_void_p(stream))
+
+
+def plt_diff_seq_attn_check(handle, stream: int = 0) -> int:
+    return _check("plt_diff_seq_attn", handle, stream)
+
+
+def plt_diff_seq_attn_destroy(handle) -> None:
+    load_library().plt_diff_seq_attn_destroy(handle)

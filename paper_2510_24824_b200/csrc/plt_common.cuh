@@ -45,6 +45,9 @@ struct Params {
     int32_t tile_keys;         // keys per plan tile
     int32_t num_ctas;          // persistent grid size of the main kernel
     int32_t piece_cost;        // what starting and finishing an item costs a block, in tiles (balances the plan)
+    int32_t qsplit;            // 1: differential heads. Every head of q contributes two packed rows, one per half of its d
+                               // elements (the other half read as zero); Hq and G then count those rows, so the head of
+                               // packed row i is i >> 1 and its half i & 1
     float scale_log2;          // sm_scale * log2(e)
     int32_t delta[kMaxLoops];  // per-loop causal offset
 };

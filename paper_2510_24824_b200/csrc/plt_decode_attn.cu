@@ -43,6 +43,7 @@ struct plt_decode_attn {
     plt_decode_attn_config cfg;
     int32_t delta[kMaxLoops];
     int G, R, Qn = 1;
+    int qsplit = 0;       // 1: differential heads (G and cfg.Hq count two packed rows for each head of q)
     bool bf16;
     int sm_count;
     MainVariant var;      // bf16: full variant; fp32: only grid/smem used
@@ -444,7 +445,11 @@ PLT_API plt_status plt_decode_attn_workspace_bytes(const plt_decode_attn_config*
     return PLT_OK;
 }
 
-PLT_API plt_status plt_decode_attn_create(const plt_decode_attn_config* config, plt_decode_attn_t* out_handle) {
+}  // extern "C"
+
+namespace plt {
+
+plt_status decode_create(const plt_decode_attn_config* config, int qsplit, plt_decode_attn_t* out_handle) {
     if (!out_handle) return fail(nullptr, PLT_ERR_INVALID_ARG, "out_handle is NULL");
     *out_handle = nullptr;
     Geometry g;
@@ -468,6 +473,7 @@ PLT_API plt_status plt_decode_attn_create(const plt_decode_attn_config* config, 
     h->G = g.G;
     h->R = g.R;
     h->Qn = g.Qn;
+    h->qsplit = qsplit;
     h->bf16 = config->dtype == PLT_BF16;
     h->sm_count = prop.multiProcessorCount;
     const float scale = config->sm_scale > 0.f ? config->sm_scale : 1.0f / sqrtf((float)config->d);
@@ -493,18 +499,22 @@ PLT_API plt_status plt_decode_attn_create(const plt_decode_attn_config* config, 
     return PLT_OK;
 }
 
+}  // namespace plt
+
 namespace {
 plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cuda_stream,
-                    const plt_decode_attn_step_args* step);
+                    const plt_decode_attn_step_args* step, const DiffTail* tail);
 plt_decode_attn* no_alloc_handle_of_current_device();
 }
 
-PLT_API plt_status plt_decode_attn_run(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cuda_stream) {
-    return run_impl(h, a, cuda_stream, nullptr);
+namespace plt {
+
+plt_status decode_run(plt_decode_attn_t h, const plt_decode_attn_args* a, const DiffTail* tail, void* cuda_stream) {
+    return run_impl(h, a, cuda_stream, nullptr, tail);
 }
 
-PLT_API plt_status plt_decode_attn_step(plt_decode_attn_t h, const plt_decode_attn_args* a,
-                                        const plt_decode_attn_step_args* step, void* cuda_stream) {
+plt_status decode_step(plt_decode_attn_t h, const plt_decode_attn_args* a, const plt_decode_attn_step_args* step,
+                       const DiffTail* tail, void* cuda_stream) {
     if (!h) return fail(nullptr, PLT_ERR_INVALID_ARG, "handle is NULL");
     if (!a) return fail(h, PLT_ERR_INVALID_ARG, "args is NULL");
     if (!step) return fail(h, PLT_ERR_INVALID_ARG, "step is NULL");
@@ -521,12 +531,34 @@ PLT_API plt_status plt_decode_attn_step(plt_decode_attn_t h, const plt_decode_at
     if (h->Qn > 1) return fail(h, PLT_ERR_UNSUPPORTED, "plt_decode_attn_step takes one query token per loop (q_len <= 1)");
     plt_decode_attn_args a2 = *a;
     a2.gate_logits = step->gate_logits;
-    return run_impl(h, &a2, cuda_stream, step);
+    return run_impl(h, &a2, cuda_stream, step, tail);
 }
+
+plt_status decode_error(plt_decode_attn_t h, plt_status code, const char* what) { return fail(h, code, "%s", what); }
+int decode_device(plt_decode_attn_t h) { return h->cfg.device; }
+
+}  // namespace plt
+
+extern "C" {
+
+PLT_API plt_status plt_decode_attn_create(const plt_decode_attn_config* config, plt_decode_attn_t* out_handle) {
+    return decode_create(config, /*qsplit=*/0, out_handle);
+}
+
+PLT_API plt_status plt_decode_attn_run(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cuda_stream) {
+    return decode_run(h, a, nullptr, cuda_stream);
+}
+
+PLT_API plt_status plt_decode_attn_step(plt_decode_attn_t h, const plt_decode_attn_args* a,
+                                        const plt_decode_attn_step_args* step, void* cuda_stream) {
+    return decode_step(h, a, step, nullptr, cuda_stream);
+}
+
+}  // extern "C"
 
 namespace {
 plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cuda_stream,
-                    const plt_decode_attn_step_args* step) {
+                    const plt_decode_attn_step_args* step, const DiffTail* tail) {
     if (!h) return fail(nullptr, PLT_ERR_INVALID_ARG, "handle is NULL");
     if (!a) return fail(h, PLT_ERR_INVALID_ARG, "args is NULL");
     if (a->struct_size != sizeof(plt_decode_attn_args))
@@ -576,6 +608,7 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
     p.kv_stride_b = sb; p.kv_stride_n = sn; p.kv_stride_h = sh;
     p.B = a->batch; p.L = c.L; p.Hq = c.Hq; p.Hkv = c.Hkv; p.G = h->G; p.R = h->R; p.d = c.d; p.w = c.w;
     p.Qn = h->Qn;
+    p.qsplit = h->qsplit;
     p.max_seq_len = c.max_seq_len; p.page_size = c.page_size; p.max_pages = a->max_pages;
     p.num_pool_pages = a->num_pool_pages;
     p.hpc = h->var.HPC;
@@ -588,7 +621,9 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     cudaError_t e;
     if (step) {
-        e = launch_prestep(p, h->bf16, step->k_new, step->v_new, step->w_gate, step->b_gate, step->gate_logits, stream);
+        Params pre = p;
+        pre.Hq >>= h->qsplit;   // the gate linear takes a head's whole row
+        e = launch_prestep(pre, h->bf16, step->k_new, step->v_new, step->w_gate, step->b_gate, step->gate_logits, stream);
         if (e != cudaSuccess) return cuda_fail(h, "launching the pre-step kernel", e);
     }
     if (h->bf16) {
@@ -638,11 +673,14 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
     if (e != cudaSuccess) return cuda_fail(h, "launching the main kernel", e);
     if (h->ev_end) cudaEventRecord(h->ev_end, stream);
     // The merge kernel may set up while the main kernel drains, unless an event sits between the two launches.
-    e = launch_reduce(p, h->bf16, /*overlap=*/h->ev_end == nullptr, stream);
+    e = tail ? launch_reduce_diff(p, *tail, h->bf16, /*overlap=*/h->ev_end == nullptr, stream)
+             : launch_reduce(p, h->bf16, /*overlap=*/h->ev_end == nullptr, stream);
     if (e != cudaSuccess) return cuda_fail(h, "launching the merge kernel", e);
     return PLT_OK;
 }
 }  // namespace
+
+extern "C" {
 
 static plt_status stage_in(plt_decode_attn_t h, int idx, const void* host, size_t bytes, cudaStream_t stream,
                            const void** dev) {

@@ -5,6 +5,8 @@
 #include <stddef.h>
 
 #include "plt_common.cuh"
+#include "plt_decode_attn.h"
+#include "plt_seq_attn.h"
 
 namespace plt {
 
@@ -81,5 +83,41 @@ cudaError_t launch_prestep(const Params& p, bool bf16, const void* k_new, const 
                            const float* b_gate, float* gate_out, cudaStream_t stream);
 
 cudaError_t launch_reduce(const Params& p, bool bf16, bool overlap, cudaStream_t stream);
+
+// The merge of differential heads (Params::qsplit): the two maps of a head, their difference and the norm.
+struct DiffTail {
+    const float *lq1, *lk1, *lq2, *lk2;   // [lambda_heads, d / 2]
+    const float* gain;                    // [d] or null: no norm
+    int32_t lambda_heads;                 // 1 (shared by the heads) or Hq
+    float lambda_init, eps;
+};
+cudaError_t launch_reduce_diff(const Params& p, const DiffTail& tail, bool bf16, bool overlap, cudaStream_t stream);
+
+// Handles behind the public entry points. qsplit = 1 / diff = true: differential heads; `config->Hq` of decode_create
+// then counts two rows for each head of q, and runs take the tail.
+plt_status decode_create(const plt_decode_attn_config* config, int qsplit, plt_decode_attn_t* out_handle);
+plt_status decode_run(plt_decode_attn_t h, const plt_decode_attn_args* a, const DiffTail* tail, void* cuda_stream);
+plt_status decode_step(plt_decode_attn_t h, const plt_decode_attn_args* a, const plt_decode_attn_step_args* step,
+                       const DiffTail* tail, void* cuda_stream);
+plt_status decode_error(plt_decode_attn_t h, plt_status code, const char* what);   // sets the message, returns the code
+int decode_device(plt_decode_attn_t h);
+plt_status seq_create(const plt_seq_attn_config* config, bool diff, plt_seq_attn_t* out_handle);
+plt_status seq_run(plt_seq_attn_t h, const plt_seq_attn_args* a, const DiffTail* tail, void* cuda_stream);
+plt_status seq_error(plt_seq_attn_t h, plt_status code, const char* what);
+int seq_device(plt_seq_attn_t h);
+
+// Makes a handle's device current for the length of a call and puts the caller's back.
+struct DeviceScope {
+    int before = -1;
+    cudaError_t err;
+    explicit DeviceScope(int device) {
+        err = cudaGetDevice(&before);
+        if (err == cudaSuccess && before != device) err = cudaSetDevice(device);
+        else if (err == cudaSuccess) before = -1;
+    }
+    ~DeviceScope() {
+        if (before >= 0) (void)cudaSetDevice(before);
+    }
+};
 
 }  // namespace plt

@@ -514,13 +514,15 @@ plt_decode_main_bf16(const __grid_constant__ CUtensorMap tmK, const __grid_const
                     const int r = rb + nt * 8 + grp;
                     const bool v = r < p.R;
                     const int lq = v ? r / p.G : 0;       // loop * Qn + token: q is [B, L, Qn, Hq, d]
-                    const int64_t qrow = (((int64_t)pc.b * p.L * p.Qn + lq) * p.Hq + kvh * p.G + (r - lq * p.G)) * D;
+                    const int64_t head_row = ((int64_t)pc.b * p.L * p.Qn + lq) * p.Hq + kvh * p.G + (r - lq * p.G);
+                    const int64_t qrow = (head_row >> p.qsplit) * D;
+                    const int zero_half = p.qsplit ? 1 - (int)(head_row & 1) : -1;   // the half this row leaves out
                     if constexpr (FP8) {
                         // contraction order of process_keys_fp8: k-step ks takes d = 16 ks + 4 tq .. + 3; bf16 -> f16
 #pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks) {
                             uint2 u = make_uint2(0u, 0u);
-                            if (v) u = *(const uint2*)(qg + qrow + ks * 16 + 4 * tq);
+                            if (v && ks / (D / 32) != zero_half) u = *(const uint2*)(qg + qrow + ks * 16 + 4 * tq);
                             qb[ks][nt][0] = pack_f16x2(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u));
                             qb[ks][nt][1] = pack_f16x2(__uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
                         }
@@ -528,8 +530,9 @@ plt_decode_main_bf16(const __grid_constant__ CUtensorMap tmK, const __grid_const
                         const int64_t q0 = qrow + 2 * tq;
 #pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks) {
-                            qb[ks][nt][0] = v ? *(const uint32_t*)(qg + q0 + ks * 16) : 0u;
-                            qb[ks][nt][1] = v ? *(const uint32_t*)(qg + q0 + ks * 16 + 8) : 0u;
+                            const bool use = v && ks / (D / 32) != zero_half;
+                            qb[ks][nt][0] = use ? *(const uint32_t*)(qg + q0 + ks * 16) : 0u;
+                            qb[ks][nt][1] = use ? *(const uint32_t*)(qg + q0 + ks * 16 + 8) : 0u;
                         }
                     }
                 }

@@ -64,7 +64,9 @@ __global__ void __launch_bounds__(NT) plt_decode_main_f32(const __grid_constant_
         for (int i = tid; i < R * D; i += NT) {
             const int r = i / D, c = i - r * D;
             const int l = r / p.G, g = r - l * p.G;
-            sQ[i] = ((const float*)p.q)[(((int64_t)pc.b * p.L + l) * p.Hq + kvh * p.G + g) * D + c];
+            const int64_t head_row = ((int64_t)pc.b * p.L + l) * p.Hq + kvh * p.G + g;
+            const bool other_half = p.qsplit && c / (D / 2) != (int)(head_row & 1);
+            sQ[i] = other_half ? 0.f : ((const float*)p.q)[(head_row >> p.qsplit) * D + c];
         }
         for (int r = tid; r < R; r += NT) {
             sM[r] = -INFINITY;

@@ -314,8 +314,11 @@ plt_decode_main_umma(const __grid_constant__ CUtensorMap tmK, const __grid_const
                 for (int id = lane; id < p.R * 16; id += 32) {
                     const int r = id >> 4, c = id & 15;
                     const int l = s_rowloop[r], g = r - l * p.G;
-                    const __nv_bfloat16* src = qg + (((int64_t)q_pc.b * p.L + l) * p.Hq + q_pc.hg * p.G + g) * UD + c * 8;
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(dst + c * C::QLBO + r * 16), "l"(src) : "memory");
+                    const int64_t head_row = ((int64_t)q_pc.b * p.L + l) * p.Hq + q_pc.hg * p.G + g;
+                    const __nv_bfloat16* src = qg + (head_row >> p.qsplit) * UD + c * 8;
+                    const int bytes = p.qsplit && (c >> 3) != (int)(head_row & 1) ? 0 : 16;   // the rest of the chunk is zero
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;"
+                                 ::"r"(dst + c * C::QLBO + r * 16), "l"(src), "r"(bytes) : "memory");
                 }
             };
             bool ok = true;

@@ -100,8 +100,13 @@ __global__ void __launch_bounds__(RP * 8) plt_decode_pack_q_e4m3(const Params p,
     float mx = 0.f;
     if (r < p.R) {
         const int l = r / p.G, g = r - l * p.G;
-        const __nv_bfloat16* src = (const __nv_bfloat16*)p.q + (((int64_t)b * p.L + l) * p.Hq + hg * p.G + g) * UD + c * 16;
-        uint4 raw[2] = {*(const uint4*)src, *(const uint4*)(src + 8)};
+        const int64_t head_row = ((int64_t)b * p.L + l) * p.Hq + hg * p.G + g;
+        const __nv_bfloat16* src = (const __nv_bfloat16*)p.q + (head_row >> p.qsplit) * UD + c * 16;
+        uint4 raw[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+        if (!p.qsplit || (c >> 2) == (int)(head_row & 1)) {
+            raw[0] = *(const uint4*)src;
+            raw[1] = *(const uint4*)(src + 8);
+        }
         const __nv_bfloat162* h2 = (const __nv_bfloat162*)raw;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {

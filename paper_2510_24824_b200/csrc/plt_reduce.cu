@@ -212,6 +212,160 @@ cudaError_t launch_one(const Params& p, unsigned grid, int chunks, bool overlap,
     return cudaLaunchKernelEx(&cfg, plt_decode_reduce<D, BF16>, p, chunks);
 }
 
+// ---- differential heads ---------------------------------------------------------------------------------------
+// The packed rows come in pairs, one per softmax map of a query head; each map is merged and gate-mixed like a row of
+// the plain attention, then
+//   x = y_1 - lambda_h y_2,  lambda_h = exp(lq1 . lk1) - exp(lq2 . lk2) + lambda_init
+// and, with a gain, x / sqrt(mean(x^2) + eps) * gain * (1 - lambda_init) over the head's D elements. One warp per query
+// head; both maps' partials are loaded together. Everything up to the store is fp32: the difference of two nearly equal
+// results is taken before the one rounding to the output type. Launch-latency bound like the kernel above: it reads twice
+// its partials, and the four vectors of the factor (a few KB, the same for every sequence) before the main kernel ends.
+
+// What is loaded of one map of a head: its shared-cache and its window partial when each was left by one block.
+template <int D>
+struct MapPart {
+    Vec<D> g, l;
+    float2 mg, ml;
+};
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kReduceWarps * 32) plt_decode_reduce_diff(const __grid_constant__ Params p,
+                                                                            const __grid_constant__ DiffTail tail,
+                                                                            const int chunks) {
+    grid_launch_dependents();
+    constexpr int N = Vec<D>::N;
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int HG = p.Hkv / p.hpc;
+    const int chunk = (int)(blockIdx.x % chunks);
+    const int hg = (int)((blockIdx.x / chunks) % HG);
+    const int b = (int)(blockIdx.x / (chunks * HG));
+    const int pair = chunk * kReduceWarps + wid;      // query head of this head group: hl * (R / 2) + pair of rows
+    if (pair >= p.hpc * (p.R >> 1)) return;
+    const int hl = pair / (p.R >> 1), r = (pair - hl * (p.R >> 1)) * 2;   // first row of the pair
+    const int lq = r / p.G;
+    const int l = lq / p.Qn, newer = p.Qn - 1 - lq % p.Qn;
+    const int hq = (((hg * p.hpc + hl) * p.G) + (r - lq * p.G)) >> 1;    // query head
+    const int Hq = p.Hq >> 1;
+
+    uint32_t flags = 0;
+    const int32_t n = seq_len_clamped(p, b, flags);
+    int cut_loop = n - p.delta[l];
+    cut_loop = cut_loop > 0 ? cut_loop : 0;
+    int cut = cut_loop - newer;
+    cut = cut > 0 ? cut : 0;
+    int wl = 0;
+    float gate = 0.f;
+    if (l > 0) {
+        wl = cut_loop < p.w ? cut_loop : p.w;
+        if (p.win_lens != nullptr && cut_loop > 0) {
+            wl = p.win_lens[b * (p.L - 1) + (l - 1)];
+            wl = wl < 0 ? 0 : (wl > p.w ? p.w : wl);
+        }
+        const float x = p.gate_logits[(((int64_t)b * (p.L - 1) + (l - 1)) * p.Qn + (lq - l * p.Qn)) * Hq + hq];
+        gate = 1.f / (1.f + expf(-x));
+    }
+    // the learned factor of this head
+    float d1 = 0.f, d2 = 0.f;
+    const int64_t lrow = tail.lambda_heads > 1 ? (int64_t)hq * (D / 2) : 0;
+#pragma unroll
+    for (int i = lane; i < D / 2; i += 32) {
+        d1 = fmaf(tail.lq1[lrow + i], tail.lk1[lrow + i], d1);
+        d2 = fmaf(tail.lq2[lrow + i], tail.lk2[lrow + i], d2);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        d1 += __shfl_xor_sync(0xffffffffu, d1, o);
+        d2 += __shfl_xor_sync(0xffffffffu, d2, o);
+    }
+    const float lambda = expf(d1) - expf(d2) + tail.lambda_init;
+    float gain[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) gain[i] = tail.gain != nullptr ? tail.gain[lane * N + i] * (1.f - tail.lambda_init) : 1.f;
+    const int item_g = item_index(p, b, hg, 0), item_l = item_index(p, b, hg, 1);
+
+    grid_dependency_wait();
+    int2 rg = make_int2(0, -1), rl = make_int2(0, -1);
+    if (cut > 0) rg = *(const int2*)(p.item_blocks + 2 * item_g);
+    if (wl > 0) rl = *(const int2*)(p.item_blocks + 2 * item_l);
+
+    float x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = 0.f;
+    if (cut > 0) {
+        if (rg.x == rg.y && rl.x >= rl.y) {
+            // The usual case: each item was done by one block (or the window is empty); both maps' loads go out together.
+            const int64_t row_g = (slot_of(item_g, rg.x) * p.hpc + hl) * p.R + r;
+            const int64_t row_l = (slot_of(item_l, rl.x) * p.hpc + hl) * p.R + r;
+            const bool has_l = rl.x == rl.y;
+            MapPart<D> a[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                a[m].mg = *(const float2*)(p.part_ml + (row_g + m) * 2);
+                load_vec<D>(p.part_acc + (row_g + m) * D + lane * N, a[m].g);
+                a[m].ml = make_float2(-INFINITY, 0.f);
+                if (has_l) {
+                    a[m].ml = *(const float2*)(p.part_ml + (row_l + m) * 2);
+                    load_vec<D>(p.part_acc + (row_l + m) * D + lane * N, a[m].l);
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const float ig = (a[m].mg.x != -INFINITY && a[m].mg.y > 0.f) ? (1.f - gate) / a[m].mg.y : 0.f;
+                const float il = (a[m].ml.x != -INFINITY && a[m].ml.y > 0.f) ? gate / a[m].ml.y : 0.f;
+                const float f = m == 0 ? 1.f : -lambda;
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = fmaf(f, a[m].g.v[i] * ig + (has_l ? a[m].l.v[i] * il : 0.f), x[i]);
+            }
+        } else {
+#pragma unroll 1
+            for (int m = 0; m < 2; ++m) {
+                Vec<D> yg, yl;
+                const float dg = merge_item<D>(p, item_g, hl, r + m, rg.x, rg.y, lane, yg);
+                const float dl = merge_item<D>(p, item_l, hl, r + m, rl.x, rl.y, lane, yl);
+                const float ig = dg > 0.f ? (1.f - gate) / dg : 0.f, il = dl > 0.f ? gate / dl : 0.f;
+                const float f = m == 0 ? 1.f : -lambda;
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = fmaf(f, yg.v[i] * ig + yl.v[i] * il, x[i]);
+            }
+        }
+        if (tail.gain != nullptr) {
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) ss = fmaf(x[i], x[i], ss);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            const float inv = 1.f / sqrtf(ss * (1.f / D) + tail.eps);
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] *= inv * gain[i];
+        }
+    }
+    const int64_t o = (((int64_t)b * p.L * p.Qn + lq) * Hq + hq) * D + lane * N;
+    if (BF16) {
+        __nv_bfloat16* dst = (__nv_bfloat16*)p.out + o;
+#pragma unroll
+        for (int i = 0; i < N; i += 2) *(__nv_bfloat162*)(dst + i) = __floats2bfloat162_rn(x[i], x[i + 1]);
+    } else {
+        float* dst = (float*)p.out + o;
+#pragma unroll
+        for (int i = 0; i < N; i += 2) *(float2*)(dst + i) = make_float2(x[i], x[i + 1]);
+    }
+}
+
+template <int D, bool BF16>
+cudaError_t launch_diff(const Params& p, const DiffTail& tail, unsigned grid, int chunks, bool overlap, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kReduceWarps * 32);
+    cfg.dynamicSmemBytes = 0;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = overlap ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, plt_decode_reduce_diff<D, BF16>, p, tail, chunks);
+}
+
 }  // namespace
 
 // `overlap`: launch with programmatic stream serialisation, so that the blocks of this kernel are
@@ -227,6 +381,18 @@ cudaError_t launch_reduce(const Params& p, bool bf16, bool overlap, cudaStream_t
                                 : launch_one<128, false>(p, grid, chunks, overlap, stream);
     return bf16 ? launch_one<64, true>(p, grid, chunks, overlap, stream)
                 : launch_one<64, false>(p, grid, chunks, overlap, stream);
+}
+
+cudaError_t launch_reduce_diff(const Params& p, const DiffTail& tail, bool bf16, bool overlap, cudaStream_t stream) {
+    const int pairs = p.hpc * (p.R >> 1);
+    const int chunks = (pairs + kReduceWarps - 1) / kReduceWarps;
+    const int64_t blocks = (int64_t)p.B * (p.Hkv / p.hpc) * chunks;
+    if (blocks == 0) return cudaSuccess;
+    const unsigned grid = (unsigned)blocks;
+    if (p.d == 128) return bf16 ? launch_diff<128, true>(p, tail, grid, chunks, overlap, stream)
+                                : launch_diff<128, false>(p, tail, grid, chunks, overlap, stream);
+    return bf16 ? launch_diff<64, true>(p, tail, grid, chunks, overlap, stream)
+                : launch_diff<64, false>(p, tail, grid, chunks, overlap, stream);
 }
 
 }  // namespace plt

@@ -23,6 +23,13 @@
 // and denominator, and a pass whose probabilities are already normalised and gated, g * p / l_local, and accumulate into
 // the same O, which the softmax threads have scaled to (1 - g) * y_global in between. Eq. 2 thus costs no second
 // accumulator. Every wait on an mbarrier is bounded and reports through the status word.
+//
+// DIFF = true is the kernel of differential heads: tiles A and B are the two softmax maps of ONE query head on the same
+// 128 rows. Map x multiplies half x of the query and key rows (64 of the 128 elements: one 128-byte swizzled half of the
+// tiles as TMA wrote them, so nothing is copied or padded), both maps multiply the same V tile, and the block owns both
+// results of a row: the epilogue reads the two accumulators, takes y_1 - lambda y_2 in fp32 and normalises the head
+// without either map reaching memory. Per key tile the products cost three quarters of two plain tiles (the scores
+// contract 64 elements instead of 128) and the exponentials the same.
 #include "../../include/plt_seq_attn.h"
 
 #include <cuda.h>
@@ -73,6 +80,7 @@ struct SeqParams {
     int32_t pair_heads, heads_per_grid;      // tiles of a block = two heads of one KV group; grid entries per (row block, loop)
     float scale_log2;
     int32_t delta[kSeqMaxLoops];
+    DiffTail tail;              // DIFF only
 };
 
 // The steps of one block: nG tiles of the shared K/V (tile A takes part in the first ntA of them), then for loops
@@ -331,6 +339,71 @@ __device__ __forceinline__ void scale_o_row(uint32_t tO, float f) {
     tmem_wait_st();
 }
 
+// Epilogue of a differential head. Thread (x, row) holds the factor f that makes accumulator x of its row a finished
+// result (1 / denominator, or 1 where Eq. 2 has been applied already) and writes the columns [64 x, 64 x + 64) of the row:
+// x = y_1 - lambda y_2 and the norm over the row's 128 elements, in fp32. `xch`: 4 x 128 floats of shared memory (the half
+// of the query buffer that the two maps do not need). All 256 softmax threads call it, whatever became of their waits.
+__device__ __forceinline__ void diff_epilogue(const SeqParams& p, float* xch, uint32_t t_lane, int x, int row, int b, int l, int h,
+                                              const RowCtx& rc, bool have_o, float f) {
+    const int lane = threadIdx.x & 31;
+    float d1 = 0.f, d2 = 0.f;   // the learned factor of this head
+    const int lrow = p.tail.lambda_heads > 1 ? h * (SD / 2) : 0;
+#pragma unroll
+    for (int i = lane; i < SD / 2; i += 32) {
+        d1 = fmaf(p.tail.lq1[lrow + i], p.tail.lk1[lrow + i], d1);
+        d2 = fmaf(p.tail.lq2[lrow + i], p.tail.lk2[lrow + i], d2);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        d1 += __shfl_xor_sync(0xffffffffu, d1, o);
+        d2 += __shfl_xor_sync(0xffffffffu, d2, o);
+    }
+    const float lambda = expf(d1) - expf(d2) + p.tail.lambda_init;
+    xch[x * SQ + row] = f;
+    named_barrier_sync(1, 256);
+    const float f1 = xch[row], f2 = -lambda * xch[SQ + row];
+    float y[SD / 2];
+    float ss = 0.f;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        uint32_t r1[32], r2[32];
+        if (have_o) {   // warp-uniform: the loads are collective
+            tmem_ld32(t_lane + 256 + x * 64 + c * 32, r1);
+            tmem_ld32(t_lane + 384 + x * 64 + c * 32, r2);
+            tmem_wait_ld();
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float v = have_o && rc.live ? fmaf(f2, __uint_as_float(r2[i]), f1 * __uint_as_float(r1[i])) : 0.f;
+            y[c * 32 + i] = v;
+            ss = fmaf(v, v, ss);
+        }
+    }
+    float inv = 1.f;
+    if (p.tail.gain != nullptr) {
+        xch[2 * SQ + x * SQ + row] = ss;
+        named_barrier_sync(1, 256);
+        ss += xch[2 * SQ + (1 - x) * SQ + row];
+        inv = (1.f - p.tail.lambda_init) / sqrtf(ss * (1.f / SD) + p.tail.eps);
+    }
+    if (rc.t < p.T) {
+        __nv_bfloat16* dst = p.out + ((((int64_t)b * p.L + l) * p.T + rc.t) * p.Hq + h) * SD + x * 64;
+#pragma unroll
+        for (int i = 0; i < SD / 2; i += 8) {
+            float g[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] = inv * (p.tail.gain != nullptr ? p.tail.gain[x * 64 + i + j] : 1.f);
+            uint4 v;
+            v.x = pack_bf16x2(y[i] * g[0], y[i + 1] * g[1]);
+            v.y = pack_bf16x2(y[i + 2] * g[2], y[i + 3] * g[3]);
+            v.z = pack_bf16x2(y[i + 4] * g[4], y[i + 5] * g[5]);
+            v.w = pack_bf16x2(y[i + 6] * g[6], y[i + 7] * g[7]);
+            *(uint4*)(dst + i) = v;
+        }
+    }
+}
+
+template <bool DIFF>
 __global__ void __launch_bounds__(kSeqThreads, 1)
 plt_seq_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmKl,
@@ -356,7 +429,7 @@ plt_seq_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const int l = item % p.L; item /= p.L;
     const int b = item % p.B; item /= p.B;
     const int qb = p.nqb - 1 - item;
-    const int hA = p.pair_heads ? 2 * hh : hh, hB = p.pair_heads ? 2 * hh + 1 : hh;
+    const int hA = !DIFF && p.pair_heads ? 2 * hh : hh, hB = !DIFF && p.pair_heads ? 2 * hh + 1 : hh;
     uint32_t flags = 0;
     int n = p.seq_lens[b];
     if (n < 0 || n > p.T) {
@@ -434,8 +507,8 @@ plt_seq_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             tma_prefetch_desc(&tmV);
             const uint64_t keep = l2_evict_first_policy();   // K/V tiles are re-read by the other heads and loops from L2;
             // the policy only orders evictions among streamed data
-            mbar_expect_tx(&bars[SB_QFULL], (activeA ? kTileBytes : 0) + (activeB ? kTileBytes : 0));
-            for (int x = 0; x < 2; ++x) {
+            mbar_expect_tx(&bars[SB_QFULL], (activeA ? kTileBytes : 0) + (activeB && !DIFF ? kTileBytes : 0));
+            for (int x = 0; x < (DIFF ? 1 : 2); ++x) {   // the two maps of a head share one query tile
                 if (!(x == 0 ? activeA : activeB)) continue;
                 const int r0 = x == 0 ? r0A : r0B;
                 for (int hf = 0; hf < 2; ++hf)
@@ -495,9 +568,11 @@ plt_seq_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 if (!ok) return;
                 tc_fence_after_sync();
                 if (lane == 0) {
-                    const uint32_t ka = ring_a + (uint32_t)slot * kTileBytes, qa = q_a + (uint32_t)x * kTileBytes;
+                    // DIFF: map x contracts half x of the rows only
+                    const uint32_t ka = ring_a + (uint32_t)slot * kTileBytes + (DIFF ? (uint32_t)x * kHalf : 0u);
+                    const uint32_t qa = q_a + (uint32_t)x * (DIFF ? kHalf : kTileBytes);
 #pragma unroll
-                    for (int kk = 0; kk < SD / 16; ++kk)
+                    for (int kk = 0; kk < (DIFF ? SD / 32 : SD / 16); ++kk)
                         umma_bf16(tmem_base + x * 128, seq_smem_desc(qa + (kk >> 2) * kHalf + (kk & 3) * 32, 16, 1024),
                                   seq_smem_desc(ka + (kk >> 2) * kHalf + (kk & 3) * 32, 16, 1024), idesc_qk, kk == 0 ? 0u : 1u);
                     umma_commit(&bars[SB_SFULL + x]);
@@ -665,10 +740,14 @@ plt_seq_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             }
             // ---- epilogue: O_x out of tensor memory ---------------------------------------------------------
             if (ok) ok = seq_wait(&bars[SB_ODONE + x], 0, abort_flag);
+            if (DIFF && ok) ok = seq_wait(&bars[SB_ODONE + 1 - x], 0, abort_flag);   // the other map's result is read too
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after_sync();
         }
-        {
+        if constexpr (DIFF) {
+            diff_epilogue(p, (float*)(q_smem + kTileBytes), tmem_base + lane_off, x, wq * 32 + lane, b, l, h, rc, active && ok,
+                          l == 0 ? (lg > 0.f ? 1.f / lg : 0.f) : 1.f);
+        } else {
             // Every lane of the warp runs the loads (they are collective); only rows inside the tensor are stored.
             const bool in_tensor = rc.t < p.T;
             __nv_bfloat16* dst = p.out + ((((int64_t)b * p.L + l) * p.T + (in_tensor ? rc.t : 0)) * p.Hq + h) * SD;
@@ -742,6 +821,7 @@ struct plt_seq_attn {
     plt_seq_attn_config cfg;
     int32_t delta[kSeqMaxLoops];
     float scale_log2;
+    bool diff = false;      // differential heads
     uint32_t* status = nullptr;
     SeqEncodeFn encode = nullptr;
     CUtensorMap maps[5];
@@ -784,10 +864,9 @@ bool seq_aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 }  // namespace
 
-#define PLT_API __attribute__((visibility("default")))
-extern "C" {
+namespace plt {
 
-PLT_API plt_status plt_seq_attn_create(const plt_seq_attn_config* c, plt_seq_attn_t* out_handle) {
+plt_status seq_create(const plt_seq_attn_config* c, bool diff, plt_seq_attn_t* out_handle) {
     if (!out_handle) return seq_fail(nullptr, PLT_ERR_INVALID_ARG, "out_handle is NULL");
     *out_handle = nullptr;
     if (!c) return seq_fail(nullptr, PLT_ERR_INVALID_ARG, "config is NULL");
@@ -803,7 +882,7 @@ PLT_API plt_status plt_seq_attn_create(const plt_seq_attn_config* c, plt_seq_att
         for (int l = 0; l < c->L; ++l)
             if (c->loop_offset[l] < 0) return seq_fail(nullptr, PLT_ERR_INVALID_ARG, "loop_offset[%d] < 0", l);
     const int64_t nqb = (c->max_seq_len + 2 * SQ - 1) / (2 * SQ);
-    if ((double)nqb * c->max_batch * c->L * c->Hq >= 2147483647.0)
+    if ((double)nqb * c->max_batch * c->L * c->Hq * (diff ? 2 : 1) >= 2147483647.0)
         return seq_fail(nullptr, PLT_ERR_UNSUPPORTED, "max_batch * L * Hq * max_seq_len too large for one grid");
     cudaError_t e = cudaSetDevice(c->device);
     if (e != cudaSuccess) return seq_fail(nullptr, PLT_ERR_CUDA, "cudaSetDevice: %s", cudaGetErrorString(e));
@@ -817,8 +896,9 @@ PLT_API plt_status plt_seq_attn_create(const plt_seq_attn_config* c, plt_seq_att
     if (!h) return seq_fail(nullptr, PLT_ERR_OUT_OF_MEMORY, "host allocation failed");
     h->cfg = *c;
     h->cfg.loop_offset = nullptr;
+    h->diff = diff;
     for (int l = 0; l < kSeqMaxLoops; ++l) h->delta[l] = c->loop_offset && l < c->L ? c->loop_offset[l] : l;
-    const float scale = c->sm_scale > 0.f ? c->sm_scale : 1.0f / sqrtf((float)c->d);
+    const float scale = c->sm_scale > 0.f ? c->sm_scale : 1.0f / sqrtf((float)(diff ? c->d / 2 : c->d));
     h->scale_log2 = scale * 1.4426950408889634f;
     h->err[0] = 0;
     void* fn = nullptr;
@@ -829,7 +909,7 @@ PLT_API plt_status plt_seq_attn_create(const plt_seq_attn_config* c, plt_seq_att
         return seq_fail(nullptr, PLT_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
     }
     h->encode = (SeqEncodeFn)fn;
-    e = allow_max_dynamic_smem((const void*)plt_seq_attn_kernel);
+    e = allow_max_dynamic_smem(diff ? (const void*)plt_seq_attn_kernel<true> : (const void*)plt_seq_attn_kernel<false>);
     if (e != cudaSuccess) {
         delete h;
         return seq_fail(nullptr, PLT_ERR_CUDA, "preparing the kernel: %s", cudaGetErrorString(e));
@@ -850,7 +930,7 @@ PLT_API plt_status plt_seq_attn_create(const plt_seq_attn_config* c, plt_seq_att
     return PLT_OK;
 }
 
-PLT_API plt_status plt_seq_attn_run(plt_seq_attn_t h, const plt_seq_attn_args* a, void* cuda_stream) {
+plt_status seq_run(plt_seq_attn_t h, const plt_seq_attn_args* a, const DiffTail* tail, void* cuda_stream) {
     if (!h) return seq_fail(nullptr, PLT_ERR_INVALID_ARG, "handle is NULL");
     if (!a) return seq_fail(h, PLT_ERR_INVALID_ARG, "args is NULL");
     if (a->struct_size != sizeof(plt_seq_attn_args))
@@ -884,17 +964,38 @@ PLT_API plt_status plt_seq_attn_run(plt_seq_attn_t h, const plt_seq_attn_args* a
     p.out = (__nv_bfloat16*)a->out;
     p.status = h->status;
     p.B = a->batch; p.L = c.L; p.T = T; p.Hq = c.Hq; p.Hkv = c.Hkv; p.G = c.Hq / c.Hkv; p.w = c.w;
-    p.pair_heads = (p.G % 2 == 0) ? 1 : 0;
-    p.heads_per_grid = p.pair_heads ? p.Hq / 2 : p.Hq;
+    p.pair_heads = (h->diff || p.G % 2 == 0) ? 1 : 0;     // both tiles of a block take the same rows
+    p.heads_per_grid = p.pair_heads && !h->diff ? p.Hq / 2 : p.Hq;
+    if (tail) p.tail = *tail;
     p.nqb = p.pair_heads ? (T + SQ - 1) / SQ : (T + 2 * SQ - 1) / (2 * SQ);
     p.scale_log2 = h->scale_log2;
     for (int l = 0; l < kSeqMaxLoops; ++l) p.delta[l] = h->delta[l];
     const unsigned grid = (unsigned)((int64_t)p.nqb * p.B * p.L * p.heads_per_grid);
-    plt_seq_attn_kernel<<<grid, kSeqThreads, kSeqSmem, (cudaStream_t)cuda_stream>>>(h->maps[0], h->maps[1], h->maps[2],
-                                                                                    h->maps[3], h->maps[4], p);
+    if (h->diff)
+        plt_seq_attn_kernel<true><<<grid, kSeqThreads, kSeqSmem, (cudaStream_t)cuda_stream>>>(h->maps[0], h->maps[1], h->maps[2],
+                                                                                              h->maps[3], h->maps[4], p);
+    else
+        plt_seq_attn_kernel<false><<<grid, kSeqThreads, kSeqSmem, (cudaStream_t)cuda_stream>>>(h->maps[0], h->maps[1], h->maps[2],
+                                                                                               h->maps[3], h->maps[4], p);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return seq_fail(h, PLT_ERR_CUDA, "launching the kernel: %s", cudaGetErrorString(e));
     return PLT_OK;
+}
+
+plt_status seq_error(plt_seq_attn_t h, plt_status code, const char* what) { return seq_fail(h, code, "%s", what); }
+int seq_device(plt_seq_attn_t h) { return h->cfg.device; }
+
+}  // namespace plt
+
+#define PLT_API __attribute__((visibility("default")))
+extern "C" {
+
+PLT_API plt_status plt_seq_attn_create(const plt_seq_attn_config* c, plt_seq_attn_t* out_handle) {
+    return seq_create(c, /*diff=*/false, out_handle);
+}
+
+PLT_API plt_status plt_seq_attn_run(plt_seq_attn_t h, const plt_seq_attn_args* a, void* cuda_stream) {
+    return seq_run(h, a, nullptr, cuda_stream);
 }
 
 PLT_API plt_status plt_seq_attn_check(plt_seq_attn_t h, void* cuda_stream, uint32_t* out_bits) {

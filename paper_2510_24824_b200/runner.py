@@ -166,6 +166,106 @@ class SeqAttn:
         self.close()
 
 
+def _learned(lambdas, norm_gain, device):
+    """The learned parameters of differential heads (numpy or torch, fp32) as the binding's struct; it keeps its tensors."""
+    dev = lambda x: None if x is None else torch.as_tensor(x, dtype=torch.float32).to(device).contiguous()
+    return B.make_diff_weights(*[dev(x) for x in lambdas], norm_gain=dev(norm_gain))
+
+
+class DiffAttn(DecodeAttn):
+    """Owns one plt_diff_attn handle sized for a problem, with the learned parameters of a layer (`lambdas`: the four vectors
+    [1 or Hq, d / 2]; `norm_gain`: [d] or None)."""
+
+    def __init__(self, p, lambdas, norm_gain=None, lambda_init: float = 0.8, norm_eps: float = 1e-5, device="cuda:0",
+                 device_index: int = 0, max_batch: Optional[int] = None, **config):
+        self.handle = None
+        self.config = B.make_diff_config(
+            p.dtype, max_batch or max(p.B, 1), p.L, p.Hq, p.Hkv, p.d, p.max_seq_len, p.w, page_size=p.page_size,
+            sm_scale=p.sm_scale, device=device_index,
+            loop_offset=None if p.loop_offset is None else [int(x) for x in p.loop_offset], kv_dtype=p.kv_dtype,
+            lambda_init=lambda_init, norm_eps=norm_eps, **config)
+        self.weights = _learned(lambdas, norm_gain, device)
+        self.handle = B.plt_diff_attn_create(self.config)
+
+    def run(self, dp: DeviceProblem, stream: Optional[int] = None, out=None):
+        if stream is None:
+            stream = torch.cuda.current_stream().cuda_stream
+        B.plt_diff_attn_run(self.handle, dp.args(out), self.weights, stream)
+        return dp.out if out is None else out
+
+    def step(self, dp: DeviceProblem, k_new, v_new, w_gate=None, b_gate=None, stream: Optional[int] = None):
+        if stream is None:
+            stream = torch.cuda.current_stream().cuda_stream
+        st = B.make_step_args(k_new, v_new, w_gate, b_gate, dp.gate_logits if dp.problem.L > 1 else None)
+        B.plt_diff_attn_step(self.handle, dp.args(), st, self.weights, stream)
+        return dp.out
+
+    def run_host(self, hp, stream=None):
+        raise NotImplementedError("plt_diff_attn has no entry point for host buffers")
+
+    def check(self, stream: Optional[int] = None) -> int:
+        if stream is None:
+            stream = torch.cuda.current_stream().cuda_stream
+        return B.plt_diff_attn_check(self.handle, stream)
+
+    def close(self):
+        if self.handle is not None:
+            B.plt_diff_attn_destroy(self.handle)
+            self.handle = None
+
+
+class DiffSeqAttn:
+    """One plt_diff_seq_attn handle, the device tensors of a sequence problem and the learned parameters of a layer."""
+
+    def __init__(self, p, lambdas, norm_gain=None, lambda_init: float = 0.8, norm_eps: float = 1e-5, device="cuda:0",
+                 device_index: int = 0):
+        self.handle = None
+        self.problem = p
+        for f in SeqAttn.FIELDS:
+            setattr(self, f, to_torch(getattr(p, f), "bf16", device))
+        self.gate_logits = to_torch(p.gate_logits, "", device)
+        self.seq_lens = to_torch(p.seq_lens, "", device)
+        self.out = torch.empty((p.B, p.L, p.T, p.Hq, p.d), dtype=torch.bfloat16, device=device)
+        self.config = B.make_diff_seq_config(
+            max(p.B, 1), p.L, p.Hq, p.Hkv, p.d, p.T, p.w, sm_scale=p.sm_scale, device=device_index,
+            loop_offset=None if p.loop_offset is None else [int(x) for x in p.loop_offset], lambda_init=lambda_init,
+            norm_eps=norm_eps)
+        self.weights = _learned(lambdas, norm_gain, device)
+        self.handle = B.plt_diff_seq_attn_create(self.config)
+        many = p.L > 1
+        self.args = B.make_seq_args(p.B, self.q, self.k_share, self.v_share, self.seq_lens, self.out,
+                                    k_loc=self.k_loc if many else None, v_loc=self.v_loc if many else None,
+                                    gate_logits=self.gate_logits if many else None)
+
+    def run(self, stream: Optional[int] = None):
+        if stream is None:
+            stream = torch.cuda.current_stream().cuda_stream
+        B.plt_diff_seq_attn_run(self.handle, self.args, self.weights, stream)
+        return self.out
+
+    def check(self, stream: Optional[int] = None) -> int:
+        if stream is None:
+            stream = torch.cuda.current_stream().cuda_stream
+        return B.plt_diff_seq_attn_check(self.handle, stream)
+
+    def close(self):
+        if self.handle is not None:
+            B.plt_diff_seq_attn_destroy(self.handle)
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 class LoopOrderAblation:
     """The ablation rows of Table 1 at kernel level, on the tensors of a device problem: the same loop-queries served
 
