@@ -19,6 +19,7 @@ PLT_F32, PLT_BF16 = 0, 1
 PLT_PATH_AUTO, PLT_PATH_WARP_MMA, PLT_PATH_TCGEN05 = 0, 1, 2
 PLT_KV_SAME, PLT_KV_E4M3 = 0, 1
 PLT_DEV_SEQ_LEN_CLAMPED, PLT_DEV_PAGE_ID_CLAMPED, PLT_DEV_WAIT_TIMEOUT, PLT_DEV_WIN_LEN_CLAMPED = 1, 2, 4, 8
+PLT_DEV_KEEP_CLAMPED = 16
 
 EXPORTS = (
     "plt_decode_attn_create", "plt_decode_attn_run", "plt_decode_attn_run_host", "plt_decode_attn_check",
@@ -30,6 +31,8 @@ EXPORTS = (
 DIFF_EXPORTS = tuple(f"plt_diff_attn_{n}" for n in ("create", "run", "step", "check", "destroy", "last_error",
                                                   "workspace_bytes")) + \
     tuple(f"plt_diff_seq_attn_{n}" for n in ("create", "run", "check", "destroy", "last_error"))
+EVICT_EXPORTS = tuple(f"plt_cache_evict_{n}" for n in ("create", "weights", "select", "compact", "check", "destroy",
+                                                      "last_error", "workspace_bytes"))
 PLT_NO_ALLOC_SCRATCH_BYTES = 16 << 20
 
 
@@ -113,6 +116,47 @@ class DiffWeights(ctypes.Structure):
     ]
 
 
+class EvictConfig(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("kv_dtype", ctypes.c_int32),
+        ("max_batch", ctypes.c_int32), ("L", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+        ("d", ctypes.c_int32), ("max_seq_len", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("sm_scale", ctypes.c_float), ("device", ctypes.c_int32), ("loop_offset", ctypes.POINTER(ctypes.c_int32)),
+        ("q_len", ctypes.c_int32), ("maps", ctypes.c_int32), ("heads_per_group", ctypes.c_int32),
+    ]
+
+
+class EvictWeightsArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("batch", ctypes.c_int32), ("q", ctypes.c_void_p),
+        ("k_cache", ctypes.c_void_p), ("kv_stride_b", ctypes.c_int64), ("kv_stride_n", ctypes.c_int64),
+        ("kv_stride_h", ctypes.c_int64), ("seq_lens", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+        ("max_pages", ctypes.c_int32), ("num_pool_pages", ctypes.c_int32), ("k_scale", ctypes.c_void_p),
+        ("gate_logits", ctypes.c_void_p), ("weights", ctypes.c_void_p), ("weights_stride", ctypes.c_int64),
+        ("decay", ctypes.c_float),
+    ]
+
+
+class EvictSelectArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("batch", ctypes.c_int32), ("weights", ctypes.c_void_p),
+        ("weights_stride", ctypes.c_int64), ("seq_lens", ctypes.c_void_p), ("budget", ctypes.c_int32),
+        ("keep_first", ctypes.c_int32), ("keep_last", ctypes.c_int32), ("keep", ctypes.c_void_p),
+        ("new_lens", ctypes.c_void_p),
+    ]
+
+
+class EvictCompactArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("batch", ctypes.c_int32), ("k_cache", ctypes.c_void_p),
+        ("v_cache", ctypes.c_void_p), ("kv_stride_b", ctypes.c_int64), ("kv_stride_n", ctypes.c_int64),
+        ("kv_stride_h", ctypes.c_int64), ("page_table", ctypes.c_void_p), ("max_pages", ctypes.c_int32),
+        ("num_pool_pages", ctypes.c_int32), ("seq_lens", ctypes.c_void_p), ("keep", ctypes.c_void_p),
+        ("keep_stride", ctypes.c_int32), ("new_lens", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+        ("weights_stride", ctypes.c_int64),
+    ]
+
+
 _lib = None
 
 
@@ -150,12 +194,17 @@ def load_library() -> ctypes.CDLL:
                                            ctypes.POINTER(DiffWeights), ctypes.c_void_p]
         lib.plt_diff_seq_attn_create.argtypes = [ctypes.POINTER(DiffSeqConfig), ctypes.POINTER(h)]
         lib.plt_diff_seq_attn_run.argtypes = [h, ctypes.POINTER(SeqArgs), ctypes.POINTER(DiffWeights), ctypes.c_void_p]
-        for prefix in ("plt_diff_attn", "plt_diff_seq_attn"):
+        lib.plt_cache_evict_create.argtypes = [ctypes.POINTER(EvictConfig), ctypes.POINTER(h)]
+        lib.plt_cache_evict_workspace_bytes.argtypes = [ctypes.POINTER(EvictConfig), ctypes.POINTER(ctypes.c_size_t)]
+        lib.plt_cache_evict_weights.argtypes = [h, ctypes.POINTER(EvictWeightsArgs), ctypes.c_void_p]
+        lib.plt_cache_evict_select.argtypes = [h, ctypes.POINTER(EvictSelectArgs), ctypes.c_void_p]
+        lib.plt_cache_evict_compact.argtypes = [h, ctypes.POINTER(EvictCompactArgs), ctypes.c_void_p]
+        for prefix in ("plt_diff_attn", "plt_diff_seq_attn", "plt_cache_evict"):
             getattr(lib, prefix + "_check").argtypes = [h, ctypes.c_void_p, ctypes.POINTER(ctypes.c_uint32)]
             getattr(lib, prefix + "_destroy").argtypes = [h]
             getattr(lib, prefix + "_last_error").argtypes = [h]
             getattr(lib, prefix + "_last_error").restype = ctypes.c_char_p
-        for name in EXPORTS + DIFF_EXPORTS:
+        for name in EXPORTS + DIFF_EXPORTS + EVICT_EXPORTS:
             if not name.endswith("_last_error"):
                 getattr(lib, name).restype = ctypes.c_int
         _lib = lib
@@ -482,3 +531,86 @@ def plt_diff_seq_attn_check(handle, stream: int = 0) -> int:
 
 def plt_diff_seq_attn_destroy(handle) -> None:
     load_library().plt_diff_seq_attn_destroy(handle)
+
+
+# ---- eviction from the shared cache (plt_cache_evict.h) -------------------------------------------------------------
+def make_evict_config(dtype, max_batch: int, L: int, Hq: int, Hkv: int, d: int, max_seq_len: int, page_size: int = 0,
+                      sm_scale: float = 0.0, device: int = 0, loop_offset: Optional[Sequence[int]] = None, kv_dtype=0,
+                      q_len: int = 0, maps: int = 1, heads_per_group: int = 1) -> EvictConfig:
+    c = EvictConfig()
+    c.struct_size = ctypes.sizeof(EvictConfig)
+    c.dtype = {"f32": PLT_F32, "bf16": PLT_BF16}.get(dtype, dtype)
+    c.kv_dtype = {"": PLT_KV_SAME, "e4m3": PLT_KV_E4M3}.get(kv_dtype, kv_dtype)
+    c.max_batch, c.L, c.Hq, c.Hkv, c.d, c.max_seq_len, c.page_size = max_batch, L, Hq, Hkv, d, max_seq_len, page_size
+    c.sm_scale, c.device, c.q_len, c.maps, c.heads_per_group = sm_scale, device, q_len, maps, heads_per_group
+    _offsets(c, loop_offset)
+    return c
+
+
+def _fill(a, batch: int, tensors: dict, numbers: dict):
+    """Sets an argument struct's fields and keeps the tensors alive with it."""
+    a.struct_size, a.batch = ctypes.sizeof(type(a)), batch
+    for name, t in tensors.items():
+        setattr(a, name, _ptr(t))
+    for name, x in numbers.items():
+        setattr(a, name, x)
+    a._keep = tuple(tensors.values())
+    return a
+
+
+def _strides(kv_strides) -> dict:
+    return dict(zip(("kv_stride_b", "kv_stride_n", "kv_stride_h"), (int(s) for s in kv_strides)))
+
+
+def make_evict_weights_args(batch: int, q, k_cache, seq_lens, weights, gate_logits=None, decay: float = 1.0, page_table=None,
+                            max_pages: int = 0, num_pool_pages: int = 0, k_scale=None, kv_strides=(0, 0, 0),
+                            weights_stride: int = 0) -> EvictWeightsArgs:
+    return _fill(EvictWeightsArgs(), batch,
+                 dict(q=q, k_cache=k_cache, seq_lens=seq_lens, weights=weights, gate_logits=gate_logits,
+                      page_table=page_table, k_scale=k_scale),
+                 dict(_strides(kv_strides), max_pages=max_pages, num_pool_pages=num_pool_pages, decay=decay,
+                      weights_stride=weights_stride))
+
+
+def make_evict_select_args(batch: int, weights, seq_lens, keep, new_lens, budget: int, keep_first: int = 0,
+                           keep_last: int = 0, weights_stride: int = 0) -> EvictSelectArgs:
+    return _fill(EvictSelectArgs(), batch, dict(weights=weights, seq_lens=seq_lens, keep=keep, new_lens=new_lens),
+                 dict(budget=budget, keep_first=keep_first, keep_last=keep_last, weights_stride=weights_stride))
+
+
+def make_evict_compact_args(batch: int, k_cache, v_cache, seq_lens, keep, new_lens, keep_stride: int, weights=None,
+                            page_table=None, max_pages: int = 0, num_pool_pages: int = 0, kv_strides=(0, 0, 0),
+                            weights_stride: int = 0) -> EvictCompactArgs:
+    return _fill(EvictCompactArgs(), batch,
+                 dict(k_cache=k_cache, v_cache=v_cache, seq_lens=seq_lens, keep=keep, new_lens=new_lens, weights=weights,
+                      page_table=page_table),
+                 dict(_strides(kv_strides), max_pages=max_pages, num_pool_pages=num_pool_pages, keep_stride=keep_stride,
+                      weights_stride=weights_stride))
+
+
+def plt_cache_evict_create(config: EvictConfig) -> ctypes.c_void_p:
+    return _create("plt_cache_evict", config)
+
+
+def plt_cache_evict_workspace_bytes(config: EvictConfig) -> int:
+    return _workspace_bytes("plt_cache_evict", config)
+
+
+def plt_cache_evict_weights(handle, args: EvictWeightsArgs, stream: int = 0) -> None:
+    _call("plt_cache_evict_weights", handle, ctypes.byref(args), ctypes.c_void_p(stream))
+
+
+def plt_cache_evict_select(handle, args: EvictSelectArgs, stream: int = 0) -> None:
+    _call("plt_cache_evict_select", handle, ctypes.byref(args), ctypes.c_void_p(stream))
+
+
+def plt_cache_evict_compact(handle, args: EvictCompactArgs, stream: int = 0) -> None:
+    _call("plt_cache_evict_compact", handle, ctypes.byref(args), ctypes.c_void_p(stream))
+
+
+def plt_cache_evict_check(handle, stream: int = 0) -> int:
+    return _check("plt_cache_evict", handle, stream)
+
+
+def plt_cache_evict_destroy(handle) -> None:
+    load_library().plt_cache_evict_destroy(handle)

@@ -16,6 +16,7 @@ constexpr uint32_t kDevSeqLenClamped = 1u;
 constexpr uint32_t kDevPageIdClamped = 2u;
 constexpr uint32_t kDevWaitTimeout = 4u;
 constexpr uint32_t kDevWinLenClamped = 8u;
+constexpr uint32_t kDevKeepClamped = 16u;
 
 // Everything a kernel needs besides its TMA descriptors. Passed by value.
 struct Params {

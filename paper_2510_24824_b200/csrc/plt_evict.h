@@ -1,0 +1,80 @@
+// Host-side interface between the C ABI of cache eviction and its kernels.
+#pragma once
+#include "plt_host.h"
+
+namespace plt {
+
+// ---- attention weights ------------------------------------------------------------------------------------------
+// The work of plt_cache_evict_weights is two kernels over one batch of sequences:
+//   scores  streams K once: scores of all packed rows (log2 units) into a scratch array, and for every row the maximum and
+//           the sum of exponentials over the block's piece of the keys
+//   add     joins the pieces' statistics and adds 2^(score - max) * rho / sum over the rows of a head group to the totals
+struct EvictWeights {
+    Params p;                  // plan, query rows, lengths, pages; w = 0, hpc and tile_keys of the scores kernel
+    Params pa;                 // plan of the add kernel: one loop without offset (all positions below the length), hpc = heads of a
+                               // group, its own tile
+    int32_t b0;                // first sequence of this launch (pointers in p and pa are shifted already, K's tensor map is not)
+    int32_t kw;                // warps along the keys of a tile of the scores kernel (each leaves statistics of its own)
+    int32_t kbox;              // keys per TMA box
+    int32_t row_pitch;         // floats between the scores of consecutive keys: rows rounded up to even
+    float* scores;             // [tile of p's line][head of the tile][key][row_pitch]
+    float* ml;                 // [slot of p's plan][head][kw][R][2]
+    float* weights;            // [B][Hkv / pa.hpc] rows, weights_stride apart
+    int64_t weights_stride;
+    const float* gate;         // [B, L-1, Qn, Hq] or null
+    float decay;
+};
+
+constexpr int kEvictAddKeys = 256;     // keys per tile of the add kernel (one thread each)
+constexpr int kEvictF32Keys = 32;      // keys per tile of the fp32 scores kernel
+
+// Blocks of a plan of T tiles: at least `least` tiles each.
+__host__ __device__ inline int evict_ctas(int64_t T, int launched, int least) {
+    int64_t c = T / least;
+    if (c < 1) c = 1;
+    return c < launched ? (int)c : launched;
+}
+constexpr int kEvictScoreTiles = 2;    // least tiles per block of the scores kernel
+
+struct ScoreVariant {
+    int D, NT, HPC;        // head dim (elements), 8-row groups, KV heads per block
+    bool fp8;
+    int KW, KS, tile_keys; // derived: HPC * KW = 4 consumer warps, KS 16-key slices each
+    int stages;
+    size_t smem;
+};
+ScoreVariant score_variant(int D, int R, int Hkv, bool fp8, int max_batch);
+cudaError_t scores_prepare(const ScoreVariant& v, int* blocks_per_sm);
+cudaError_t launch_scores(const ScoreVariant& v, const CUtensorMap& mapK, const EvictWeights& e, int grid, cudaStream_t stream);
+size_t scores_f32_smem(int D, int R, int max_batch);
+cudaError_t scores_f32_prepare(int D, int R, int max_batch, int* blocks_per_sm);
+cudaError_t launch_scores_f32(const EvictWeights& e, int grid, size_t smem, cudaStream_t stream);
+size_t evict_add_smem(int rows, int max_batch);
+cudaError_t evict_add_prepare(size_t smem, int* blocks_per_sm);
+cudaError_t launch_evict_add(const EvictWeights& e, int grid, size_t smem, cudaStream_t stream);
+
+// ---- selection ----------------------------------------------------------------------------------------------------
+struct SelectParams {
+    const float* weights;
+    int64_t weights_stride;
+    const int32_t* seq_lens;
+    int32_t* keep;
+    int32_t* new_lens;
+    uint32_t* status;
+    int32_t groups, max_seq_len, budget, keep_first, keep_last;
+};
+cudaError_t launch_select(const SelectParams& p, int batch, cudaStream_t stream);
+
+// ---- compaction ---------------------------------------------------------------------------------------------------
+struct CompactParams {
+    char *k, *v;                       // bytes
+    int64_t stride_b, stride_n, stride_h;   // bytes
+    const int32_t *page_table, *seq_lens, *keep, *new_lens;
+    float* weights;
+    int64_t weights_stride;
+    uint32_t* status;
+    int32_t Hkv, hpg, row_bytes, max_seq_len, page_size, max_pages, num_pool_pages, keep_stride;
+};
+cudaError_t launch_compact(const CompactParams& p, int batch, int sm_count, cudaStream_t stream);
+
+}  // namespace plt

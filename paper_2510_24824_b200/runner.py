@@ -266,6 +266,78 @@ class DiffSeqAttn:
             pass
 
 
+class CacheEvict:
+    """Owns one plt_cache_evict handle sized for a problem: totals of attention weight, selection and compaction on the shared
+    cache of a DeviceProblem (the caller holds the totals [B, groups, >= max_seq_len], `keep` and `new_lens`)."""
+
+    def __init__(self, p, device_index: int = 0, max_batch: Optional[int] = None, q_len: int = 1, maps: int = 1,
+                 heads_per_group: int = 1):
+        self.handle = None
+        self.config = B.make_evict_config(
+            p.dtype, max_batch or max(p.B, 1), p.L, p.Hq, p.Hkv, p.d, p.max_seq_len, page_size=p.page_size,
+            sm_scale=p.sm_scale, device=device_index,
+            loop_offset=None if p.loop_offset is None else [int(x) for x in p.loop_offset], kv_dtype=p.kv_dtype,
+            q_len=q_len, maps=maps, heads_per_group=heads_per_group)
+        self.handle = B.plt_cache_evict_create(self.config)
+
+    @staticmethod
+    def _pages(dp: DeviceProblem) -> dict:
+        p = dp.problem
+        return dict(page_table=dp.page_table, max_pages=p.max_pages, num_pool_pages=p.num_pool_pages)
+
+    def weights_args(self, dp: DeviceProblem, q, weights, gate_logits=None, decay: float = 1.0, kv_strides=(0, 0, 0)):
+        return B.make_evict_weights_args(dp.problem.B, q, dp.k_cache, dp.seq_lens, weights, gate_logits=gate_logits,
+                                         decay=decay, k_scale=dp.k_scale, kv_strides=kv_strides,
+                                         weights_stride=weights.shape[-1], **self._pages(dp))
+
+    def select_args(self, dp: DeviceProblem, weights, keep, new_lens, budget: int, keep_first: int, keep_last: int):
+        return B.make_evict_select_args(dp.problem.B, weights, dp.seq_lens, keep, new_lens, budget, keep_first, keep_last,
+                                        weights_stride=weights.shape[-1])
+
+    def compact_args(self, dp: DeviceProblem, keep, new_lens, weights=None, kv_strides=(0, 0, 0)):
+        return B.make_evict_compact_args(dp.problem.B, dp.k_cache, dp.v_cache, dp.seq_lens, keep, new_lens, keep.shape[-1],
+                                         weights=weights, kv_strides=kv_strides,
+                                         weights_stride=0 if weights is None else weights.shape[-1], **self._pages(dp))
+
+    def weights(self, dp: DeviceProblem, q, weights, gate_logits=None, decay: float = 1.0, kv_strides=(0, 0, 0),
+                stream: Optional[int] = None):
+        """Adds the weights that the queries q [B, L, q_len, Hq, d] give each cached position to the totals, in place."""
+        B.plt_cache_evict_weights(self.handle, self.weights_args(dp, q, weights, gate_logits, decay, kv_strides),
+                                  torch.cuda.current_stream().cuda_stream if stream is None else stream)
+        return weights
+
+    def select(self, dp: DeviceProblem, weights, keep, new_lens, budget: int, keep_first: int = 0, keep_last: int = 0,
+               stream: Optional[int] = None):
+        B.plt_cache_evict_select(self.handle, self.select_args(dp, weights, keep, new_lens, budget, keep_first, keep_last),
+                                 torch.cuda.current_stream().cuda_stream if stream is None else stream)
+        return keep, new_lens
+
+    def compact(self, dp: DeviceProblem, keep, new_lens, weights=None, kv_strides=(0, 0, 0), stream: Optional[int] = None):
+        """Moves the kept rows of dp's shared cache to the front, in place; dp.seq_lens still holds the lengths before."""
+        B.plt_cache_evict_compact(self.handle, self.compact_args(dp, keep, new_lens, weights, kv_strides),
+                                  torch.cuda.current_stream().cuda_stream if stream is None else stream)
+
+    def check(self, stream: Optional[int] = None) -> int:
+        return B.plt_cache_evict_check(self.handle, torch.cuda.current_stream().cuda_stream if stream is None else stream)
+
+    def close(self):
+        if self.handle is not None:
+            B.plt_cache_evict_destroy(self.handle)
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 class LoopOrderAblation:
     """The ablation rows of Table 1 at kernel level, on the tensors of a device problem: the same loop-queries served
 

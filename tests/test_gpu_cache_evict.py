@@ -1,0 +1,392 @@
+"""GPU parity of cache eviction (plt_cache_evict_* through the C ABI) against the fp64 oracle, and a run of its three calls
+with the attention that reads the cache."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import plt_cache_evict as oracle_evict
+from paper_2510_24824_b200 import binding as B
+from paper_2510_24824_b200.inputs import f32_to_bf16_bits, make_problem
+from paper_2510_24824_b200.runner import CacheEvict, DecodeAttn, DeviceProblem, DiffAttn, to_torch
+
+from diff_util import EPS, LAMBDA_INIT, assert_close, largest, learned, map_error, stored
+from gpu_util import assert_parity
+
+pytestmark = pytest.mark.gpu
+
+BASE = dict(name="evict", dtype="bf16", B=3, L=2, Hq=8, Hkv=4, d=128, w=16, lens=("list", [300, 77, 2]), seed=21)
+
+
+def problem(**kw):
+    tail = kw.pop("tail_fill", None)
+    return make_problem(dict(BASE, **kw), tail_fill=tail)
+
+
+def values(p, name):
+    """A shared cache as float64 [B, capacity, Hkv, d] (pages gathered, codes with their scales)."""
+    a = getattr(p, name)
+    if p.page_size:
+        a = a[p.page_table].reshape(p.B, -1, p.Hkv, p.d)
+    if p.kv_dtype == "e4m3":
+        x = torch.from_numpy(np.ascontiguousarray(a)).view(torch.float8_e4m3fn).to(torch.float64).numpy()
+        return x * getattr(p, name[0] + "_scale").astype(np.float64)[:, None]
+    return stored(a)
+
+
+def check_weights(p, q_len=1, maps=1, group=1, decay=1.0, gated=True, stride=0, seed=3, held=None):
+    rng = np.random.default_rng(seed)
+    q = rng.standard_normal((p.B, p.L, q_len, p.Hq, p.d)).astype(np.float32) * 1.5
+    q = f32_to_bf16_bits(q) if p.dtype == "bf16" else q
+    gate = rng.standard_normal((p.B, p.L - 1, q_len, p.Hq)).astype(np.float32) if gated and p.L > 1 else None
+    pitch = stride or p.max_seq_len
+    if held is None:
+        held = rng.random((p.B, p.Hkv // group, pitch)).astype(np.float32)
+    dp = DeviceProblem(p, "cuda:0")
+    dq, dg, dw = to_torch(q, p.dtype, "cuda:0"), to_torch(gate, "", "cuda:0"), to_torch(held, "", "cuda:0")
+    with CacheEvict(p, q_len=q_len, maps=maps, heads_per_group=group) as op:
+        op.weights(dp, dq, dw, gate_logits=dg, decay=decay)
+        assert op.check() == 0
+        first = dw.clone()
+        dw.copy_(torch.from_numpy(held))
+        op.weights(dp, dq, dw, gate_logits=dg, decay=decay)
+        assert op.check() == 0
+        assert torch.equal(first.view(torch.int32), dw.view(torch.int32)), "two calls on the same inputs differ"
+    got = first.cpu().numpy()
+    k = np.nan_to_num(values(p, "k_cache"))
+    n = k.shape[1]
+    want, terms = oracle_evict.weights(stored(q), k, p.seq_lens, held[:, :, :n], group, maps, decay, gate, p.sm_scale, p.loop_offset)
+    # a score is a sum of d products, each add off by at most 2^-23 of the running sum <= sum |q k|; a weight's exponent and
+    # its denominator's by twice that; exp2, the sums over rows and pieces and the store add some 2^-19
+    new = want - np.where(np.arange(n) < p.seq_lens[:, None, None], decay * held[:, :, :n].astype(np.float64), held[:, :, :n]) if decay else want
+    bound = (2.0 * p.d * 2.0 ** -23 * terms + 2.0 ** -19) * np.abs(new) + 2.0 ** -21 * np.abs(want) + 1e-30
+    err = np.abs(got[:, :, :n] - want)
+    live = np.arange(n) < p.seq_lens[:, None, None]
+    live = np.broadcast_to(live, err.shape)
+    assert (err[live] <= bound[live]).all(), f"worst {np.max(err[live] / bound[live]):.2f} of its bound"
+    same = got.view(np.int32) == held.view(np.int32)
+    assert same[:, :, :n][~live].all() and same[:, :, n:].all(), "totals behind a sequence's length were written"
+
+
+@pytest.mark.parametrize("dtype,d,kv", [("bf16", 128, ""), ("bf16", 64, ""), ("f32", 128, ""), ("f32", 64, ""), ("bf16", 128, "e4m3")])
+@pytest.mark.parametrize("L", [1, 3])
+def test_weights_types_and_loops(dtype, d, kv, L):
+    check_weights(problem(dtype=dtype, d=d, kv_dtype=kv, L=L, tail_fill=None if kv else float("nan")))
+
+
+@pytest.mark.parametrize("lens", [[0, 1, 2], [1, 1, 1], [31, 32, 33], [127, 128, 129], [255, 256, 257], [1500, 3, 700]])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weights_lengths(lens, dtype):
+    check_weights(problem(lens=("list", lens), L=3, dtype=dtype))
+
+
+@pytest.mark.parametrize("Hq,Hkv,L,q_len,maps", [(1, 1, 1, 1, 1), (3, 1, 1, 1, 1), (5, 1, 1, 1, 2), (12, 2, 2, 1, 1), (8, 2, 2, 1, 2),
+                                                (16, 4, 2, 3, 1), (16, 4, 1, 5, 2), (12, 4, 3, 2, 2), (6, 3, 2, 1, 1), (64, 1, 1, 1, 1)])
+@pytest.mark.parametrize("kv", ["", "e4m3"])
+def test_weights_rows_and_heads(Hq, Hkv, L, q_len, maps, kv):
+    check_weights(problem(Hq=Hq, Hkv=Hkv, L=L, kv_dtype=kv, lens=("list", [200, 40, 3])), q_len=q_len, maps=maps)
+
+
+@pytest.mark.parametrize("Hq,L,q_len,maps", [(5, 1, 1, 1), (4, 2, 2, 2), (32, 2, 1, 1)])
+def test_weights_rows_fp32(Hq, L, q_len, maps):
+    check_weights(problem(Hq=Hq, Hkv=1, L=L, dtype="f32", lens=("list", [200, 40, 3])), q_len=q_len, maps=maps)
+
+
+@pytest.mark.parametrize("group", [1, 2, 4])
+@pytest.mark.parametrize("decay", [0.0, 0.5, 1.0])
+def test_weights_groups_and_decay(group, decay):
+    p = problem()
+    held = None
+    if decay == 0.0:
+        held = np.full((p.B, p.Hkv // group, p.max_seq_len), np.nan, np.float32)      # not read
+    check_weights(p, group=group, decay=decay, held=held)
+
+
+@pytest.mark.parametrize("page", [16, 32, 48, 64, 256])
+@pytest.mark.parametrize("dtype,kv,Hkv", [("bf16", "", 4), ("bf16", "e4m3", 1), ("bf16", "", 1), ("f32", "", 2)])
+def test_weights_pages(page, dtype, kv, Hkv):
+    check_weights(problem(page_size=page, dtype=dtype, kv_dtype=kv, Hkv=Hkv, Hq=2 * Hkv, lens=("list", [300, 77, 1])))
+
+
+def test_weights_without_gate_with_offsets_and_wide_rows():
+    check_weights(problem(loop_offset=[1, 5]), gated=False, stride=333)
+    check_weights(problem(loop_offset=[0, 0]), stride=301)
+
+
+def test_weights_gates_at_their_ends():
+    p = problem(lens=("list", [100, 50, 2]))
+    q = f32_to_bf16_bits(np.random.default_rng(0).standard_normal((p.B, p.L, 1, p.Hq, p.d)).astype(np.float32))
+    dp, dq = DeviceProblem(p, "cuda:0"), to_torch(q, "bf16", "cuda:0")
+    with CacheEvict(p) as op:
+        for end, rows in ((float("inf"), 1.0), (float("-inf"), 2.0)):
+            w = torch.zeros(p.B, p.Hkv, p.max_seq_len, device="cuda")
+            op.weights(dp, dq, w, gate_logits=torch.full((p.B, p.L - 1, 1, p.Hq), end, device="cuda"))
+            assert op.check() == 0
+            assert torch.allclose(w.sum(-1), torch.full((p.B, p.Hkv), 2.0 * rows, device="cuda"), atol=1e-4)
+
+
+def test_weights_split_over_the_whole_grid_and_in_parts_of_the_batch():
+    """One long sequence; and a batch whose scores do not fit the scratch, which runs in several pairs of launches."""
+    check_weights(problem(B=1, lens=("list", [20011]), Hq=4, Hkv=1, L=1))
+    lens = [300, 77, 0, 5, 300, 1, 222]
+    for kw in (dict(Hq=128, Hkv=4, max_seq_len=40000), dict(Hq=16, Hkv=4, max_seq_len=524288, page_size=64)):
+        p = problem(B=7, L=2, lens=("list", lens), **kw)
+        rows = p.L * p.Hq // p.Hkv
+        whole = p.B * p.max_seq_len * p.Hkv * rows * 4
+        assert B.plt_cache_evict_workspace_bytes(B.make_evict_config("bf16", p.B, p.L, p.Hq, p.Hkv, p.d, p.max_seq_len, p.page_size)) < whole
+        check_weights(p)
+
+
+def test_weights_strided_cache():
+    p = problem()
+    rng = np.random.default_rng(2)
+    q = f32_to_bf16_bits(rng.standard_normal((p.B, p.L, 1, p.Hq, p.d)).astype(np.float32))
+    dp, dq = DeviceProblem(p, "cuda:0"), to_torch(q, "bf16", "cuda:0")
+    with CacheEvict(p) as op:
+        dense, strided = (torch.zeros(p.B, p.Hkv, p.max_seq_len, device="cuda") for _ in range(2))
+        op.weights(dp, dq, dense)
+        heads_first = dp.k_cache.permute(0, 2, 1, 3).contiguous()
+        dp.k_cache = heads_first
+        op.weights(dp, dq, strided, kv_strides=(p.Hkv * p.max_seq_len * p.d, p.d, p.max_seq_len * p.d))
+        assert op.check() == 0
+    assert torch.equal(dense, strided)
+
+
+# ---- select -------------------------------------------------------------------------------------------------------
+def check_select(w, lens, budget, first=0, last=1, stride=0):
+    Bn, groups, N = w.shape
+    store = np.zeros((Bn, groups, stride or N), np.float32)
+    store[:, :, :N] = w
+    keep = torch.full((Bn, groups, budget), 77, dtype=torch.int32, device="cuda")
+    new = torch.full((Bn,), -5, dtype=torch.int32, device="cuda")
+    h = B.plt_cache_evict_create(B.make_evict_config("bf16", Bn, 1, groups, groups, 128, N))
+    try:
+        dw, dl = to_torch(store, "", "cuda:0"), to_torch(np.asarray(lens, np.int32), "", "cuda:0")
+        a = B.make_evict_select_args(Bn, dw, dl, keep, new, budget, first, last, weights_stride=stride)
+        B.plt_cache_evict_select(h, a, torch.cuda.current_stream().cuda_stream)
+        assert B.plt_cache_evict_check(h, torch.cuda.current_stream().cuda_stream) == 0
+    finally:
+        B.plt_cache_evict_destroy(h)
+    want, lengths = oracle_evict.select(store[:, :, :N], lens, budget, first, last)
+    assert np.array_equal(new.cpu().numpy(), lengths)
+    got = keep.cpu().numpy()
+    assert np.array_equal(got, want), f"{(got != want).sum()} positions differ"
+
+
+@pytest.mark.parametrize("N,budget", [(1, 1), (2, 1), (33, 32), (1024, 100), (4096, 1), (4097, 4096), (5000, 1024), (9001, 700)])
+def test_select_sizes(N, budget):
+    rng = np.random.default_rng(N)
+    check_select(np.exp(1.5 * rng.standard_normal((2, 3, N))).astype(np.float32), [N, max(1, N // 2)], budget, 0, min(1, budget))
+
+
+@pytest.mark.parametrize("first,last", [(0, 0), (4, 64), (0, 300), (300, 0), (100, 200)])
+def test_select_protected_positions(first, last):
+    rng = np.random.default_rng(7)
+    check_select(rng.random((2, 2, 2000)).astype(np.float32), [2000, 1999], 300, first, last)
+
+
+def test_select_ties_and_special_values():
+    rng = np.random.default_rng(8)
+    w = rng.integers(0, 4, (4, 3, 6000)).astype(np.float32)      # long runs of equal totals
+    w[1] = 0.0                                                    # all equal
+    w[2] = -w[2]
+    w[2, :, ::7] = -0.0
+    w[3, :, ::3] = np.nan
+    w[3, :, 1::50] = np.inf
+    w[3, :, 2::50] = -np.inf
+    check_select(w, [6000, 6000, 5999, 6000], 1500, 3, 17)
+    check_select(w, [0, 1, 1500, 1501], 1500, 3, 17)
+    check_select(w[3:], [6000], 5000, 3, 17)                      # some of the NaN are kept
+
+
+def test_select_long_rows_on_several_blocks_each():
+    rng = np.random.default_rng(9)
+    w = np.exp(2.0 * rng.standard_normal((2, 2, 70001))).astype(np.float32)
+    w[0, 1] = np.round(w[0, 1])
+    check_select(w, [70001, 4099], 3001, 4, 64, stride=70003)
+    check_select(w[:1, :1], [65536], 60000, 0, 1, stride=70001)
+
+
+# ---- compact ------------------------------------------------------------------------------------------------------
+def check_compact(p, group=1, budget=64, first=2, last=5, with_totals=True, stride=0, seed=4):
+    rng = np.random.default_rng(seed)
+    groups, pitch = p.Hkv // group, stride or p.max_seq_len
+    keep, new = oracle_evict.select(rng.random((p.B, groups, p.max_seq_len)).astype(np.float32), p.seq_lens, budget, first, last)
+    totals = rng.random((p.B, groups, pitch)).astype(np.float32)
+    dp = DeviceProblem(p, "cuda:0")
+    dk, dn, dw = (to_torch(x, "", "cuda:0") for x in (keep, new, totals))
+    with CacheEvict(p, heads_per_group=group) as op:
+        op.compact(dp, dk, dn, weights=dw if with_totals else None)
+        assert op.check() == 0
+    for name in ("k_cache", "v_cache"):
+        before = getattr(p, name)
+        want = before.copy()
+        if p.page_size:
+            moved = oracle_evict.compact(before[p.page_table].reshape(p.B, -1, p.Hkv, p.d), keep, new, group)
+            for b in range(p.B):
+                for i in range(int(new[b])):
+                    want[p.page_table[b, i // p.page_size], i % p.page_size] = moved[b, i]
+        else:
+            want = oracle_evict.compact(before, keep, new, group)
+        got = getattr(dp, name).cpu()
+        got = got.view(torch.uint8).numpy() if got.dtype != torch.float32 else got.numpy().view(np.uint8)
+        assert np.array_equal(got, np.ascontiguousarray(want).view(np.uint8)), f"{name} differs"
+    if with_totals:
+        want = totals.copy()
+        for b in range(p.B):
+            for g in range(groups):
+                want[b, g, : new[b]] = totals[b, g, keep[b, g, : new[b]]]
+                want[b, g, new[b]: p.seq_lens[b]] = 0.0
+        assert np.array_equal(dw.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("dtype,d,kv", [("bf16", 128, ""), ("bf16", 64, ""), ("f32", 128, ""), ("f32", 64, ""), ("bf16", 128, "e4m3")])
+@pytest.mark.parametrize("page", [0, 16])
+def test_compact_types(dtype, d, kv, page):
+    check_compact(problem(dtype=dtype, d=d, kv_dtype=kv, page_size=page, tail_fill=None if kv else float("nan")))
+
+
+@pytest.mark.parametrize("lens", [[0, 1, 2], [64, 65, 66], [2000, 1, 700], [5000, 4999, 3]])
+@pytest.mark.parametrize("budget", [7, 64, 1900])
+def test_compact_lengths(lens, budget):
+    check_compact(problem(lens=("list", lens)), budget=min(budget, max(7, max(lens))) if max(lens) >= 7 else 2, first=0 if max(lens) < 7 else 2,
+                  last=1 if max(lens) < 7 else 5)
+
+
+@pytest.mark.parametrize("group", [1, 2, 4])
+@pytest.mark.parametrize("page", [0, 64])
+def test_compact_groups_and_pages(group, page):
+    check_compact(problem(lens=("list", [900, 300, 65]), page_size=page), group=group, budget=256)
+
+
+def test_compact_without_totals_wide_rows_and_a_large_batch():
+    check_compact(problem(), with_totals=False)
+    check_compact(problem(lens=("list", [3000, 200, 2900])), stride=3333, budget=1000)
+    check_compact(problem(B=40, Hkv=8, lens=("uniform", 1, 400)), budget=100)
+
+
+def test_compact_clamps_and_flags_what_is_out_of_range():
+    p = problem(lens=("list", [100, 50, 20]))
+    keep, new = oracle_evict.select(np.random.default_rng(0).random((3, 4, 100)).astype(np.float32), p.seq_lens, 40, 1, 1)
+    wild = keep.copy()
+    wild[0, 0, 3], wild[0, 1, 4] = -9, 10 ** 8
+    dp = DeviceProblem(p, "cuda:0")
+    with CacheEvict(p) as op:
+        op.compact(dp, to_torch(wild, "", "cuda:0"), to_torch(new, "", "cuda:0"))
+        assert op.check() == B.PLT_DEV_KEEP_CLAMPED
+        fixed = keep.copy()
+        fixed[0, 0, 3], fixed[0, 1, 4] = 3, 99
+        want = oracle_evict.compact(p.k_cache, fixed, new)
+        assert np.array_equal(dp.k_cache.cpu().view(torch.uint8).numpy(), want.view(np.uint8))
+        dp = DeviceProblem(p, "cuda:0")
+        op.compact(dp, to_torch(keep, "", "cuda:0"), to_torch(np.array([-3, 1000, 20], np.int32), "", "cuda:0"))
+        assert op.check() == B.PLT_DEV_KEEP_CLAMPED
+        assert np.array_equal(dp.k_cache[0].cpu().view(torch.uint8).numpy(), p.k_cache[0].view(np.uint8))
+
+
+def test_refusals_of_calls():
+    p = problem(page_size=16, lens=("list", [60, 50, 20]))
+    dp = DeviceProblem(p, "cuda:0")
+    w = torch.zeros(p.B, p.Hkv, p.max_seq_len, device="cuda")
+    keep, new = torch.zeros(p.B, p.Hkv, 32, dtype=torch.int32, device="cuda"), torch.zeros(p.B, dtype=torch.int32, device="cuda")
+    q = torch.zeros(p.B, p.L, 1, p.Hq, p.d, dtype=torch.bfloat16, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    with CacheEvict(p) as op:
+        make = {"weights": lambda: op.weights_args(dp, q, w), "select": lambda: op.select_args(dp, w, keep, new, 32, 1, 4),
+                "compact": lambda: op.compact_args(dp, keep, new, w)}
+        bad = [("weights", "q", None), ("weights", "q", q.data_ptr() + 2), ("weights", "weights", None), ("weights", "weights", w.data_ptr() + 2),
+               ("weights", "decay", -1.0), ("weights", "decay", float("nan")), ("weights", "weights_stride", 5), ("weights", "kv_stride_n", 3),
+               ("weights", "page_table", None), ("weights", "num_pool_pages", 0), ("weights", "struct_size", 3), ("weights", "seq_lens", None),
+               ("select", "budget", 0), ("select", "budget", p.max_seq_len + 1), ("select", "keep_first", -1), ("select", "keep_first", 29),
+               ("select", "keep_last", 0), ("select", "new_lens", dp.seq_lens.data_ptr()), ("select", "keep", None), ("select", "struct_size", 1),
+               ("compact", "keep", None), ("compact", "keep_stride", 0), ("compact", "keep_stride", p.max_seq_len + 1),
+               ("compact", "v_cache", dp.k_cache.data_ptr()), ("compact", "new_lens", dp.seq_lens.data_ptr()), ("compact", "k_cache", dp.k_cache.data_ptr() + 2),
+               ("compact", "page_table", None), ("compact", "struct_size", 1), ("compact", "batch", -1)]
+        for name, field, value in bad:
+            a = make[name]()
+            setattr(a, field, value)
+            with pytest.raises(B.PltError) as e:
+                getattr(B, f"plt_cache_evict_{name}")(op.handle, a, stream)
+            assert e.value.status == B.PLT_ERR_INVALID_ARG and e.value.message, (name, field)
+        for name, field, value in (("weights", "batch", 4), ("compact", "max_pages", 1)):
+            a = make[name]()
+            setattr(a, field, value)
+            with pytest.raises(B.PltError) as e:
+                getattr(B, f"plt_cache_evict_{name}")(op.handle, a, stream)
+            assert e.value.status == B.PLT_ERR_CAPACITY, (name, field)
+        assert op.check() == 0
+
+
+# ---- together -----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("page,kv", [(0, ""), (32, ""), (32, "e4m3")])
+@pytest.mark.parametrize("diff", [False, True])
+def test_a_cache_held_to_its_budget_between_steps(page, kv, diff):
+    """Attention, totals, selection and compaction in one captured graph, then attention on the smaller cache: every stage
+    against its oracle on what the stage before left."""
+    p = problem(page_size=page, kv_dtype=kv, lens=("list", [400, 150, 30]), max_seq_len=448)
+    budget, first, last = 100, 4, 16
+    lambdas, gain = learned(p.d, 1)
+    dp = DeviceProblem(p, "cuda:0")
+    w = torch.rand(p.B, p.Hkv, p.max_seq_len, device="cuda") * 0.01
+    held = w.cpu().numpy()
+    keep, new = torch.empty(p.B, p.Hkv, budget, dtype=torch.int32, device="cuda"), torch.empty(p.B, dtype=torch.int32, device="cuda")
+    q = dp.q.view(p.B, p.L, 1, p.Hq, p.d)
+    attn = DiffAttn(p, lambdas, gain, LAMBDA_INIT, EPS) if diff else DecodeAttn(p)
+    out2 = torch.full_like(dp.out, float("nan"))
+    side = torch.cuda.Stream()
+    with attn, CacheEvict(p, maps=2 if diff else 1) as op:
+        def step():
+            attn.run(dp)
+            op.weights(dp, q, w, gate_logits=dp.gate_logits.view(p.B, p.L - 1, 1, p.Hq), decay=0.5)
+            op.select(dp, w, keep, new, budget, first, last)
+            op.compact(dp, keep, new, weights=w)
+            lens, dp.seq_lens = dp.seq_lens, new
+            attn.run(dp, out=out2)
+            dp.seq_lens = lens
+        saved = [t.clone() for t in (dp.k_cache, dp.v_cache, w)]
+        with torch.cuda.stream(side):
+            step()                                    # outside a capture first: tensor maps are encoded
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                step()
+        for t, s in zip((dp.k_cache, dp.v_cache, w), saved):
+            t.copy_(s)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert attn.check() == 0 and op.check() == 0
+    want_w, _ = oracle_evict.weights(stored(p.q)[:, :, None], values(p, "k_cache"), p.seq_lens, held[:, :, : values(p, "k_cache").shape[1]], 1,
+                                     2 if diff else 1, 0.5, p.gate_logits[:, :, None])
+    got_keep, got_new = keep.cpu().numpy(), new.cpu().numpy()
+    assert np.array_equal(got_new, np.minimum(p.seq_lens, budget))
+    # the kept totals are those of the exact ranking up to the totals' own error
+    for b in range(p.B):
+        n, m = int(p.seq_lens[b]), int(got_new[b])
+        for g in range(p.Hkv):
+            at = got_keep[b, g, :m]
+            assert (np.diff(at) > 0).all() and at[0] >= 0 and at[-1] == n - 1 and (at[: min(first, m)] == np.arange(min(first, m))).all()
+            dropped = np.setdiff1d(np.arange(n), at)
+            inner = at[(at >= first) & (at < n - last)]
+            if len(dropped) and len(inner):
+                assert want_w[b, g, inner].min() >= want_w[b, g, dropped].max() - 1e-4 * want_w[b, g].max()
+            assert np.allclose(w[b, g, :m].cpu().numpy(), want_w[b, g, at], rtol=1e-3, atol=1e-7)
+            assert not w[b, g, m:n].any()
+    # the attention on the smaller cache: the problem with the moved rows
+    after = p.with_(seq_lens=got_new, k_cache=_numpy(dp.k_cache, p), v_cache=_numpy(dp.v_cache, p))
+    moved = oracle_evict.compact(values(p, "k_cache"), got_keep, got_new)
+    for b in range(p.B):
+        assert np.array_equal(values(after, "k_cache")[b, : got_new[b]], moved[b, : got_new[b]])
+    got = out2.float().cpu().numpy().astype(np.float64)
+    if diff:
+        fp8 = p.kv_dtype == "e4m3"
+        e = map_error("bf16", max(largest(a, p.v_scale if fp8 else None) for a in (p.v_cache, p.v_win)), p.d, largest(p.q),
+                      max(largest(a, p.k_scale if fp8 else None) for a in (p.k_cache, p.k_win)))
+        assert_close(got, oracle.diff_maps(after), lambdas, gain, "bf16", e, "after")
+    else:
+        assert_parity(got, oracle.decode_attn(after), "bf16", "after")
+
+
+def _numpy(t, p):
+    t = t.cpu()
+    return t.view(torch.int16).numpy().view(np.uint16) if t.dtype == torch.bfloat16 else t.numpy()
