@@ -414,8 +414,11 @@ PLT_API plt_status plt_cache_evict_compact(plt_cache_evict_t h, const plt_cache_
     if (s != PLT_OK) return s;
     DeviceScope scope(c.device);
     if (scope.err != cudaSuccess) return cuda_fail(h, "cudaSetDevice", scope.err);
+    int shift = -1;
+    if (c.page_size > 0 && (c.page_size & (c.page_size - 1)) == 0)
+        while ((1 << ++shift) < c.page_size) {}
     const CompactParams p = {(char*)a->k_cache, (char*)a->v_cache, sb * es, sn * es, sh * es, a->page_table, a->seq_lens, a->keep,
-                             a->new_lens, a->weights, ws, h->status, c.Hkv, h->g.hpg, c.d * es, c.max_seq_len, c.page_size,
+                             a->new_lens, a->weights, ws, h->status, c.Hkv, h->g.hpg, c.d * es, c.max_seq_len, c.page_size, shift,
                              a->max_pages, a->num_pool_pages, a->keep_stride};
     const cudaError_t err = launch_compact(p, a->batch, h->sm_count, (cudaStream_t)cuda_stream);
     if (err != cudaSuccess) return cuda_fail(h, "launching the compaction kernel", err);

@@ -73,7 +73,8 @@ struct CompactParams {
     float* weights;
     int64_t weights_stride;
     uint32_t* status;
-    int32_t Hkv, hpg, row_bytes, max_seq_len, page_size, max_pages, num_pool_pages, keep_stride;
+    int32_t Hkv, hpg, row_bytes, max_seq_len, page_size, page_shift /* log2 of a page that is a power of two, else -1 */;
+    int32_t max_pages, num_pool_pages, keep_stride;
 };
 cudaError_t launch_compact(const CompactParams& p, int batch, int sm_count, cudaStream_t stream);
 

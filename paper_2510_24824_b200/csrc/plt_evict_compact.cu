@@ -2,12 +2,14 @@
 //
 // Slot i of a head takes row keep[i] >= i. Reading is safe as long as the slot has not been overwritten, i.e. before slot
 // keep[i] itself is written, and since keep[i] >= i that is never before slot i is: a block that walks the slots in order,
-// reading a chunk of rows, waiting for all its threads' reads, then writing the chunk, always reads old values, and may read
-// ahead as far as it likes. So no scratch copy of the cache is needed and every row moves once: 2 x its bytes, the floor.
-// The order binds the slots of one head only; heads, K and V, and the 16-byte columns of a row are independent, which is
-// where the blocks come from: one per (sequence, head, K or V, piece of the row). Rows are cut into pieces of down to 64
-// bytes only while that is needed to give every SM a block. Two chunks of loads are in flight per block, the next chunk's
-// page ids and positions included. Bound: HBM on batches, the chain position -> page id -> row for one sequence.
+// reading a chunk of rows, waiting for all its threads' reads, then writing the chunk, always reads old values. So no scratch
+// copy of the cache is needed and every row moves once: 2 x its bytes, the floor. The order binds the slots of one head only,
+// and only within the same bytes of the rows: heads, K and V, and the 16-byte columns of a row are independent. A block owns
+// a 64-byte piece of the rows of one (sequence, head, K or V). The chain position -> page id -> row is taken apart: one thread
+// per row works out the next chunk's addresses into shared memory while the rows of the current one are under way, from
+// positions it fetched a chunk earlier. (Every thread working out the addresses of the rows it moves, 4 lanes to a row, took
+// 2.1x the time on pages of 64 tokens: integer divisions.) Blocks of 256 threads move 512 rows a chunk; where the batch has
+// no more blocks than SMs, blocks of 1024 threads move 1024 (one sequence: 1024 kept rows in a single chunk).
 #include "plt_common.cuh"
 #include "plt_evict.h"
 #include "plt_ptx.cuh"
@@ -15,9 +17,6 @@
 namespace plt {
 
 namespace {
-
-constexpr int kCmpThreads = 256;
-constexpr int kCmpUnroll = 8;         // rows in flight per thread and chunk
 
 struct Slots {                        // the slots of one (sequence, group)
     const int32_t* keep;
@@ -41,29 +40,37 @@ __device__ __forceinline__ Slots read_slots(const CompactParams& p, int b, int g
     return s;
 }
 
-__device__ __forceinline__ int source_of(const Slots& s, int i, uint32_t& flags) {
-    int k = s.keep[i];
-    if (k < i || k >= s.n) {
-        flags |= kDevKeepClamped;
-        k = k < i ? i : s.n - 1;
-    }
-    return k;
+// Clamped position that slot i < m takes.
+__device__ __forceinline__ int clamp_source(const Slots& s, int i, int k, uint32_t& flags) {
+    if (k >= i && k < s.n) return k;
+    flags |= kDevKeepClamped;
+    return k < i ? i : s.n - 1;
 }
 
-// Byte offset of a position's row of KV head 0.
-__device__ __forceinline__ int64_t cell(const CompactParams& p, const int32_t* pages, int b, int pos, uint32_t& flags) {
+__device__ __forceinline__ int clamp_page(const CompactParams& p, int page, uint32_t& flags) {
+    if (page >= 0 && page < p.num_pool_pages) return page;
+    flags |= kDevPageIdClamped;
+    return page < 0 ? 0 : p.num_pool_pages - 1;
+}
+
+constexpr int kColumns = 4;           // 16-byte columns of a block's piece of a row
+
+// Byte offsets of a row's source and destination, from the head's first row; to = -1: the row stays.
+struct Move {
+    int64_t from, to;
+};
+
+__device__ __forceinline__ int64_t row_offset(const CompactParams& p, const int32_t* pages, int b, int pos, uint32_t& flags) {
     if (p.page_size == 0) return (int64_t)b * p.stride_b + (int64_t)pos * p.stride_n;
-    int page = pages[pos / p.page_size];
-    if (page < 0 || page >= p.num_pool_pages) {
-        flags |= kDevPageIdClamped;
-        page = page < 0 ? 0 : p.num_pool_pages - 1;
-    }
-    return (int64_t)page * p.stride_b + (int64_t)(pos % p.page_size) * p.stride_n;
+    const int page = p.page_shift >= 0 ? pos >> p.page_shift : pos / p.page_size;
+    return (int64_t)clamp_page(p, pages[page], flags) * p.stride_b + (int64_t)(pos - page * p.page_size) * p.stride_n;
 }
 
-// `lanes`: 16-byte columns of a block's piece of a row (a power of two, at most 32); `pieces`: pieces of a row.
-__global__ void __launch_bounds__(kCmpThreads) plt_evict_compact_kernel(const __grid_constant__ CompactParams p, const int lanes,
-                                                                        const int pieces, const int row_blocks) {
+template <int THREADS, int U>
+__global__ void __launch_bounds__(THREADS) plt_evict_compact_kernel(const __grid_constant__ CompactParams p, const int pieces,
+                                                                    const int row_blocks) {
+    constexpr int STEP = THREADS / kColumns, CHUNK = STEP * U, MINE = CHUNK / THREADS;   // rows: per step, per chunk, planned per thread
+    __shared__ Move moves[3][CHUNK];     // a buffer is rewritten two barriers after its last use
     uint32_t flags = 0;
     const int tid = threadIdx.x;
     if ((int)blockIdx.x < row_blocks) {
@@ -73,66 +80,78 @@ __global__ void __launch_bounds__(kCmpThreads) plt_evict_compact_kernel(const __
         const int h = id % p.Hkv, b = id / p.Hkv;
         const Slots s = read_slots(p, b, h / p.hpg, flags);
         const int32_t* pages = p.page_table + (int64_t)b * p.max_pages;
-        char* base = (which ? p.v : p.k) + (int64_t)h * p.stride_h + (piece * lanes + tid % lanes) * 16;
-        const int per = kCmpThreads / lanes;             // rows per step
-        const int chunk = per * kCmpUnroll, row0 = tid / lanes;
-        uint4 x[kCmpUnroll];
-        int64_t to[kCmpUnroll];                          // where the row goes; -1: it stays (or there is none)
-        auto load = [&](int c0, uint4 (&v)[kCmpUnroll], int64_t (&dst)[kCmpUnroll]) {
-            int64_t from[kCmpUnroll];
+        char* base = (which ? p.v : p.k) + (int64_t)h * p.stride_h + (piece * kColumns + tid % kColumns) * 16;
+        int k[MINE];                     // positions of the chunk that is planned next
+        auto fetch = [&](int c0) {
 #pragma unroll
-            for (int u = 0; u < kCmpUnroll; ++u) {
-                const int i = c0 + u * per + row0;
-                dst[u] = -1;
-                from[u] = 0;
+            for (int j = 0; j < MINE; ++j) k[j] = c0 + j * THREADS + tid < s.m ? s.keep[c0 + j * THREADS + tid] : 0;
+        };
+        auto plan = [&](int c0, Move* to) {
+#pragma unroll
+            for (int j = 0; j < MINE; ++j) {
+                const int i = c0 + j * THREADS + tid;
+                Move m{0, -1};
                 if (i < s.m) {
-                    const int k = source_of(s, i, flags);
-                    if (k != i) {
-                        from[u] = cell(p, pages, b, k, flags);
-                        dst[u] = cell(p, pages, b, i, flags);
+                    const int from = clamp_source(s, i, k[j], flags);
+                    if (from != i) {
+                        m.from = row_offset(p, pages, b, from, flags);
+                        m.to = row_offset(p, pages, b, i, flags);
                     }
                 }
+                to[j * THREADS + tid] = m;
             }
-#pragma unroll
-            for (int u = 0; u < kCmpUnroll; ++u)
-                if (dst[u] >= 0) v[u] = *(const uint4*)(base + from[u]);
         };
-        load(0, x, to);
-        for (int c0 = 0; c0 < s.m; c0 += chunk) {
-            uint4 y[kCmpUnroll];
-            int64_t to2[kCmpUnroll];
-            load(c0 + chunk, y, to2);
-            __syncthreads();                             // every row of this chunk (and of the next) has been read
+        fetch(0);
+        plan(0, moves[0]);
+        fetch(CHUNK);
+        __syncthreads();
+        int buf = 0;
+        for (int c0 = 0; c0 < s.m; c0 += CHUNK) {
+            const Move* now = moves[buf] + tid / kColumns;
+            uint4 x[U];
 #pragma unroll
-            for (int u = 0; u < kCmpUnroll; ++u)
-                if (to[u] >= 0) *(uint4*)(base + to[u]) = x[u];
+            for (int u = 0; u < U; ++u) {
+                const Move m = now[u * STEP];
+                if (m.to >= 0) x[u] = *(const uint4*)(base + m.from);
+            }
+            buf = buf == 2 ? 0 : buf + 1;
+            plan(c0 + CHUNK, moves[buf]);
+            fetch(c0 + 2 * CHUNK);
+            __syncthreads();             // every row of the chunk has been read, the next one's addresses are in place
 #pragma unroll
-            for (int u = 0; u < kCmpUnroll; ++u) {
-                x[u] = y[u];
-                to[u] = to2[u];
+            for (int u = 0; u < U; ++u) {
+                const int64_t to = now[u * STEP].to;
+                if (to >= 0) *(uint4*)(base + to) = x[u];
             }
         }
     } else {
         // the totals of one (sequence, group): the same walk on single elements, then zeros up to the old length
+        constexpr int V = 8;
         const int groups = p.Hkv / p.hpg, id = blockIdx.x - row_blocks, b = id / groups, g = id - b * groups;
         const Slots s = read_slots(p, b, g, flags);
         float* w = p.weights + (int64_t)id * p.weights_stride;
-        for (int c0 = 0; c0 < s.m; c0 += kCmpThreads * kCmpUnroll) {
-            float x[kCmpUnroll];
+        for (int c0 = 0; c0 < s.m; c0 += THREADS * V) {
+            int k[V];
+            float x[V];
 #pragma unroll
-            for (int u = 0; u < kCmpUnroll; ++u) {
-                const int i = c0 + u * kCmpThreads + tid;
-                x[u] = i < s.m ? w[source_of(s, i, flags)] : 0.f;
+            for (int u = 0; u < V; ++u) {
+                const int i = c0 + u * THREADS + tid;
+                k[u] = i < s.m ? s.keep[i] : 0;
+            }
+#pragma unroll
+            for (int u = 0; u < V; ++u) {
+                const int i = c0 + u * THREADS + tid;
+                x[u] = i < s.m ? w[clamp_source(s, i, k[u], flags)] : 0.f;
             }
             __syncthreads();
 #pragma unroll
-            for (int u = 0; u < kCmpUnroll; ++u) {
-                const int i = c0 + u * kCmpThreads + tid;
+            for (int u = 0; u < V; ++u) {
+                const int i = c0 + u * THREADS + tid;
                 if (i < s.m) w[i] = x[u];
             }
         }
         __syncthreads();
-        for (int i = s.m + tid; i < s.n; i += kCmpThreads) w[i] = 0.f;
+        for (int i = s.m + tid; i < s.n; i += THREADS) w[i] = 0.f;
     }
     if (flags) atomicOr(p.status, flags);
 }
@@ -140,14 +159,11 @@ __global__ void __launch_bounds__(kCmpThreads) plt_evict_compact_kernel(const __
 }  // namespace
 
 cudaError_t launch_compact(const CompactParams& p, int batch, int sm_count, cudaStream_t stream) {
-    int pieces = 1, lanes = p.row_bytes / 16;
-    while (lanes > 4 && (int64_t)batch * p.Hkv * 2 * pieces < sm_count) {
-        lanes /= 2;
-        pieces *= 2;
-    }
+    const int pieces = p.row_bytes / (16 * kColumns);
     const int row_blocks = batch * p.Hkv * 2 * pieces;
-    const int blocks = row_blocks + (p.weights ? batch * (p.Hkv / p.hpg) : 0);
-    plt_evict_compact_kernel<<<(unsigned)blocks, kCmpThreads, 0, stream>>>(p, lanes, pieces, row_blocks);
+    const unsigned grid = (unsigned)(row_blocks + (p.weights ? batch * (p.Hkv / p.hpg) : 0));
+    if (row_blocks <= sm_count) plt_evict_compact_kernel<1024, 4><<<grid, 1024, 0, stream>>>(p, pieces, row_blocks);
+    else plt_evict_compact_kernel<256, 8><<<grid, 256, 0, stream>>>(p, pieces, row_blocks);
     return cudaGetLastError();
 }
 

@@ -3,13 +3,15 @@
 // Per (sequence, head group) the `budget` largest of N totals, ties to the lowest position, in ascending order. A total maps
 // to a 32-bit key that orders like it (protected positions above everything, NaN below); three radix passes (11, 11, 10
 // bits, from the top) find the key T of the budget-th largest, each a histogram of the next digit of the keys that share the
-// digits found so far; a last pass walks the positions in order and writes those above T and as many equal to T as are left.
-// After the first pass few keys take part in the histograms, so the passes are reads (the later ones from L1 / L2) and a few
-// block-wide scans: bound by latency for one sequence and by the SM's load path for long rows.
+// digits found so far; then every warp counts the keys of its run that are above T and equal to T, one scan over the warps
+// gives each its place in the output, and the runs are written without further synchronisation.
 //
-// One block of 1024 threads per row, or a cluster of up to 8 on long rows when the batch leaves SMs idle: each block then
-// holds a run of the row, histograms are summed over the cluster through distributed shared memory, and every block takes
-// the same decisions on the same sums.
+// A block of 1024 threads takes a row, or a cluster of up to 8 blocks where rows are long and few: each block then holds a
+// part of the row, histograms are summed over the cluster through distributed shared memory, and every block takes the same
+// decisions on the same sums. A block's keys are read from memory once and stay with it, in registers (up to 8 per thread)
+// or shared memory (up to 48 K keys), by the capacity, which bounds the length; longer parts are read again by every pass.
+// The floor is one read of the totals; what bounds it is the chain of passes (histogram, scan, pick) and, on long rows, the histogram's
+// shared-memory atomics.
 #include <cooperative_groups.h>
 
 #include "plt_common.cuh"
@@ -25,8 +27,6 @@ namespace cg = cooperative_groups;
 constexpr int kSelThreads = 1024;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelBins = 2048;
-constexpr int kSelRun = 4;                              // 32-element pieces a warp takes per step of the last pass
-constexpr int kSelTile = kSelThreads * kSelRun;
 
 // Orders like the value: NaN 0, then from -inf up; -0 and 0 alike. All ones is left for protected positions.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -38,7 +38,8 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 struct Row {
     const float* w;
     int n, first, last0;                                // [0, first) and [last0, n) are protected
-    __device__ __forceinline__ uint32_t key(int i) const { return i < first || i >= last0 ? 0xffffffffu : order_key(w[i]); }
+    __device__ __forceinline__ uint32_t key(int i, float x) const { return i < first || i >= last0 ? 0xffffffffu : order_key(x); }
+    __device__ __forceinline__ uint32_t key(int i) const { return key(i, w[i]); }
 };
 
 // Inclusive sum over the block; total: the block's. `warp_sums`: 32 words of shared memory.
@@ -63,11 +64,16 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums, 
     return v + (wid > 0 ? before : 0u);
 }
 
-template <bool CLUSTER>
+// Where a block's keys stay between the passes.
+enum Home { kMemory, kRegisters, kShared };
+constexpr int kRegKeys = 8;                             // per thread
+constexpr int kSharedKeys = 48 * 1024;                  // per block
+
+template <int HOME, bool CLUSTER>
 __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __grid_constant__ SelectParams p, const int csize) {
     __shared__ uint32_t hist[kSelBins];                 // this block's counts (read by the whole cluster)
     __shared__ uint32_t warp_sums[32];
-    __shared__ uint32_t s_pick[3];                      // digit picked, keys above it (cluster), keys above it (this block)
+    __shared__ uint32_t s_pick[4];                      // digit picked; keys above it: in the cluster, in this block; equal: in this block
     __shared__ uint32_t s_mine[2];                      // keys above T and equal to T in this block (read by the cluster)
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const int row = CLUSTER ? (int)(blockIdx.x / csize) : (int)blockIdx.x, rank = CLUSTER ? (int)(blockIdx.x % csize) : 0;
@@ -85,10 +91,50 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
         return;
     }
     const Row r{p.weights + (int64_t)row * p.weights_stride, n, p.keep_first, n - p.keep_last};
-    // this block's run of the row: whole tiles
-    const int tiles = (n + kSelTile - 1) / kSelTile;
-    const int i0 = min(n, (int)((int64_t)tiles * rank / csize) * kSelTile);
-    const int i1 = min(n, (int)((int64_t)tiles * (rank + 1) / csize) * kSelTile);
+    // Warp w of the csize * 32 warps of the row has the run [w0, w1): `steps` pieces of 32 positions.
+    const int steps = (n + csize * kSelThreads - 1) / (csize * kSelThreads);
+    const int w0 = min(n, (rank * kSelWarps + wid) * steps * 32), w1 = min(n, w0 + steps * 32);
+    constexpr int IPT = HOME == kRegisters ? kRegKeys : 1;
+    uint32_t held[IPT];
+    extern __shared__ uint32_t s_keys[];
+    uint32_t* run = s_keys + wid * steps * 32;          // kShared: this warp's keys; no other warp reads them
+    if constexpr (HOME == kRegisters) {
+#pragma unroll
+        for (int j = 0; j < IPT; ++j) {
+            const int i = w0 + j * 32 + lane;
+            held[j] = j < steps && i < w1 ? r.key(i) : 0u;
+        }
+    } else if constexpr (HOME == kShared) {
+        // the totals as they are, all on their way at once; the first pass turns them into keys
+        for (int j = 0; j < steps; ++j) {
+            const int i = w0 + j * 32 + lane;
+            if (i < w1)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(run + j * 32 + lane)), "l"(r.w + i) : "memory");
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    }
+    // Calls f(piece, key, whether the position exists) for every piece of the warp's run; `fresh`: the first call. A lane
+    // reads back its own keys.
+    auto walk = [&](bool fresh, auto&& f) {
+        if constexpr (HOME == kRegisters) {
+#pragma unroll
+            for (int j = 0; j < IPT; ++j)
+                if (j < steps) f(j, held[j], w0 + j * 32 + lane < w1);
+        } else {
+#pragma unroll 4
+            for (int j = 0; j < steps; ++j) {
+                const int i = w0 + j * 32 + lane;
+                uint32_t k = 0u;
+                if constexpr (HOME == kShared) {
+                    k = run[j * 32 + lane];
+                    if (fresh) run[j * 32 + lane] = k = r.key(i, __uint_as_float(k));
+                } else {
+                    if (i < w1) k = r.key(i);
+                }
+                f(j, k, i < w1);
+            }
+        }
+    };
 
     uint32_t prefix = 0, left = (uint32_t)kept;         // digits found so far; how many of the keys that share them are kept
     uint32_t above_mine = 0, equal_mine = 0;            // in this block: keys above T, keys equal to T
@@ -96,33 +142,17 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
         const int bits = pass < 2 ? 11 : 10;
-        const int bins = 1 << bits, prev = shift;
+        const uint32_t digits = (1u << bits) - 1u;
+        const int prev = shift;
         shift -= bits;
         for (int i = tid; i < kSelBins; i += kSelThreads) hist[i] = 0;
         __syncthreads();
-        for (int base = i0; base < i1; base += kSelThreads * 4) {
-            uint32_t k[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int i = base + u * kSelThreads + tid;
-                k[u] = i < i1 ? r.key(i) : 0u;
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int i = base + u * kSelThreads + tid;
-                const bool in = i < i1 && (pass == 0 || (k[u] >> prev) == prefix);
-                const uint32_t mask = __ballot_sync(0xffffffffu, in);
-                if (mask == 0) continue;
-                const uint32_t digit = (k[u] >> shift) & (uint32_t)(bins - 1);
-                // lanes that agree on the digit (long runs of equal totals) add once
-                const uint32_t lead = __shfl_sync(0xffffffffu, digit, __ffs(mask) - 1);
-                if (__all_sync(0xffffffffu, !in || digit == lead)) {
-                    if (lane == 0) atomicAdd(&hist[lead], (uint32_t)__popc(mask));
-                } else if (in) {
-                    atomicAdd(&hist[digit], 1u);
-                }
-            }
-        }
+        if (pass == 0) walk(true, [&](int, uint32_t k, bool exists) {
+            if (exists) atomicAdd(&hist[k >> shift], 1u);
+        });
+        else walk(false, [&](int, uint32_t k, bool exists) {
+            if (exists && (k >> prev) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1u);
+        });
         if constexpr (CLUSTER) cg::this_cluster().sync(); else __syncthreads();
         // thread t has bins 2 t and 2 t + 1 counted from the top; the picked one is where the running count reaches `left`
         uint32_t c[2], mine[2];
@@ -133,17 +163,15 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
             if constexpr (CLUSTER)
                 for (int q = 1; q < csize; ++q) c[u] += *cg::this_cluster().map_shared_rank(&hist[bin], (rank + q) % csize);
         }
-        uint32_t total, total_mine;
-        const uint32_t upto = block_scan(c[0] + c[1], warp_sums, total);
-        const uint32_t upto_mine = block_scan(mine[0] + mine[1], warp_sums, total_mine);
-        uint32_t before = upto - c[0] - c[1], before_mine = upto_mine - mine[0] - mine[1];
+        uint32_t total, before = block_scan(c[0] + c[1], warp_sums, total) - c[0] - c[1], before_mine = before;
+        if constexpr (CLUSTER) before_mine = block_scan(mine[0] + mine[1], warp_sums, total) - mine[0] - mine[1];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             if (before < left && before + c[u] >= left) {
                 s_pick[0] = (uint32_t)(kSelBins - 1 - (2 * tid + u));
                 s_pick[1] = before;
                 s_pick[2] = before_mine;
-                s_mine[1] = mine[u];
+                s_pick[3] = mine[u];
             }
             before += c[u];
             before_mine += mine[u];
@@ -152,11 +180,11 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
         prefix = (prefix << bits) | s_pick[0];
         left -= s_pick[1];
         above_mine += s_pick[2];
-        equal_mine = s_mine[1];
-        if constexpr (CLUSTER) cg::this_cluster().sync(); else __syncthreads();   // counts and picks have been read
+        equal_mine = s_pick[3];
+        if constexpr (CLUSTER) cg::this_cluster().sync();   // the other blocks have read this one's counts
     }
     // T = prefix; `left` of the keys equal to it are kept, the lowest positions first
-    uint32_t above = 0, equal = 0;                      // before this block's run
+    uint32_t above = 0, equal = 0;                      // before this block's part
     if constexpr (CLUSTER) {
         if (tid == 0) {
             s_mine[0] = above_mine;
@@ -170,61 +198,74 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
         }
         cg::this_cluster().sync();                      // no block ends while another reads its counts
     }
-    for (int base = i0; base < i1; base += kSelTile) {
-        uint32_t mg[kSelRun], me[kSelRun], ng = 0, ne = 0;
-#pragma unroll
-        for (int u = 0; u < kSelRun; ++u) {
-            const int i = base + (wid * kSelRun + u) * 32 + lane;
-            const uint32_t k = i < i1 ? r.key(i) : 0u;
-            mg[u] = __ballot_sync(0xffffffffu, i < i1 && k > prefix);
-            me[u] = __ballot_sync(0xffffffffu, i < i1 && k == prefix);
-            ng += __popc(mg[u]);
-            ne += __popc(me[u]);
+    uint32_t ng = 0, ne = 0;                            // in this warp's run
+    walk(false, [&](int, uint32_t k, bool exists) {
+        ng += __popc(__ballot_sync(0xffffffffu, exists && k > prefix));
+        ne += __popc(__ballot_sync(0xffffffffu, exists && k == prefix));
+    });
+    uint32_t total;
+    const uint32_t ig = block_scan(lane == 31 ? ng : 0u, warp_sums, total), ie = block_scan(lane == 31 ? ne : 0u, warp_sums, total);
+    above += __shfl_sync(0xffffffffu, ig, 31) - ng;
+    equal += __shfl_sync(0xffffffffu, ie, 31) - ne;
+    const uint32_t below = (1u << lane) - 1u;
+    int32_t* to = out + above + min(equal, left);       // the warp's next place
+    walk(false, [&](int j, uint32_t k, bool exists) {
+        const int at = w0 + j * 32 + lane;
+        bool take = exists && k > prefix;
+        const bool tie = exists && k == prefix;
+        if (__any_sync(0xffffffffu, tie)) {             // rare
+            const uint32_t me = __ballot_sync(0xffffffffu, tie);
+            take = take || (tie && equal + __popc(me & below) < left);
+            equal += __popc(me);
         }
-        // both counts of a tile fit 16 bits: one scan over the warps' sums (kept by lane 31 of each)
-        uint32_t total;
-        const uint32_t mine = ng | (ne << 16);
-        const uint32_t incl = block_scan(lane == 31 ? mine : 0u, warp_sums, total);
-        const uint32_t mine_before = __shfl_sync(0xffffffffu, incl, 31) - mine;
-        uint32_t ag = above + (mine_before & 0xffffu), ae = equal + (mine_before >> 16);
-        const uint32_t below = (1u << lane) - 1u;
-#pragma unroll
-        for (int u = 0; u < kSelRun; ++u) {
-            const int i = base + (wid * kSelRun + u) * 32 + lane;
-            const uint32_t g0 = ag + __popc(mg[u] & below), e0 = ae + __popc(me[u] & below);
-            if ((mg[u] >> lane) & 1u) out[g0 + min(e0, left)] = i;
-            else if (((me[u] >> lane) & 1u) && e0 < left) out[g0 + e0] = i;
-            ag += __popc(mg[u]);
-            ae += __popc(me[u]);
-        }
-        above += total & 0xffffu;
-        equal += total >> 16;
-    }
+        const uint32_t mask = __ballot_sync(0xffffffffu, take);
+        if (take) to[__popc(mask & below)] = at;
+        to += __popc(mask);
+    });
 }
 
-// Blocks per row: as many as leave each 4096 positions of a full row and the grid within what two blocks per SM take. A row
-// of 65536 among 8 took ... us with one block and ... us with eight; batches that fill the SMs gain nothing from it.
+// Blocks per row: as few as can hold a full row, and more while the grid leaves SMs idle and every block keeps 4096
+// positions.
 int select_cluster(const SelectParams& p, int batch) {
     int c = 1;
-    while (c < 8 && (int64_t)batch * p.groups * c * 2 <= 296 && p.max_seq_len / (2 * c) >= kSelTile) c *= 2;
+    while (c < 8 && p.max_seq_len / c >= 2 * 4096 && ((int64_t)batch * p.groups * c * 2 <= 148 || p.max_seq_len > c * kSharedKeys)) c *= 2;
     return c;
+}
+
+template <int HOME, bool CLUSTER>
+cudaError_t launch_home(const SelectParams& p, int batch, int c, cudaStream_t stream) {
+    auto fn = plt_evict_select_kernel<HOME, CLUSTER>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(batch * p.groups * c));
+    cfg.blockDim = dim3(kSelThreads);
+    cfg.stream = stream;
+    if (HOME == kShared) {
+        const int steps = (p.max_seq_len + c * kSelThreads - 1) / (c * kSelThreads);   // of the longest row
+        cfg.dynamicSmemBytes = (size_t)steps * kSelThreads * 4;
+        const cudaError_t e = allow_max_dynamic_smem((const void*)fn);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)c;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CLUSTER ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, fn, p, c);
+}
+
+template <int HOME>
+cudaError_t launch_cluster(const SelectParams& p, int batch, int c, cudaStream_t stream) {
+    return c > 1 ? launch_home<HOME, true>(p, batch, c, stream) : launch_home<HOME, false>(p, batch, c, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_select(const SelectParams& p, int batch, cudaStream_t stream) {
     const int c = select_cluster(p, batch);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(batch * p.groups * c));
-    cfg.blockDim = dim3(kSelThreads);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)c;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = c > 1 ? 1 : 0;
-    return c > 1 ? cudaLaunchKernelEx(&cfg, plt_evict_select_kernel<true>, p, c) : cudaLaunchKernelEx(&cfg, plt_evict_select_kernel<false>, p, 1);
+    if (p.max_seq_len <= c * kRegKeys * kSelThreads) return launch_cluster<kRegisters>(p, batch, c, stream);
+    if (p.max_seq_len <= c * kSharedKeys) return launch_cluster<kShared>(p, batch, c, stream);
+    return launch_cluster<kMemory>(p, batch, c, stream);
 }
 
 }  // namespace plt

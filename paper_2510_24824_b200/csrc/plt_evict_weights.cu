@@ -154,6 +154,33 @@ __global__ void __launch_bounds__(kFThreads) plt_evict_scores_f32(const __grid_c
 // lie side by side, so the reads are whole sectors; the sum's order is the rows' order. Bound: L2 / HBM on the scores, and
 // the exponentials (one per row and key).
 constexpr int kAddThreads = kEvictAddKeys;
+constexpr int kAddTiles = 4;
+
+// Adds the weights of R rows of one head to the accumulators of kAddTiles keys; W rows per load.
+template <int W>
+__device__ __forceinline__ void add_rows(const float* s, const int64_t (&at)[kAddTiles], const float2* mc, int R, float (&acc)[kAddTiles]) {
+    for (int r = 0; r < R; r += W) {
+        float v[kAddTiles][W];
+#pragma unroll
+        for (int u = 0; u < kAddTiles; ++u) {
+            if constexpr (W == 4) {
+                const float4 x = *(const float4*)(s + at[u] + r);
+                v[u][0] = x.x; v[u][1] = x.y; v[u][2] = x.z; v[u][3] = x.w;
+            } else {
+                const float2 x = *(const float2*)(s + at[u] + r);
+                v[u][0] = x.x; v[u][1] = x.y;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            if (r + j < R) {                               // the pitch may hold one row more than there are
+                const float2 c = mc[r + j];
+#pragma unroll
+                for (int u = 0; u < kAddTiles; ++u) acc[u] = fmaf(fast_exp2(v[u][j] - c.x), c.y, acc[u]);
+            }
+        }
+    }
+}
 
 __global__ void __launch_bounds__(kAddThreads) plt_evict_add(const __grid_constant__ EvictWeights e) {
     const Params &p = e.p, &pa = e.pa;
@@ -217,28 +244,39 @@ __global__ void __launch_bounds__(kAddThreads) plt_evict_add(const __grid_consta
         const int n = pc.sp.cmax;                          // the length
         const int scored = sp.gt * p.tile_keys;            // keys that have scores (beyond a row's cutoff: -inf)
         float* w = e.weights + ((int64_t)pc.b * (p.Hkv / pa.hpc) + pc.hg) * e.weights_stride;
-        for (int t = pc.t0; t < pc.t1; ++t) {
-            const int key = t * kEvictAddKeys + tid;
-            if (key >= n) break;
-            float acc = 0.f;
-            if (key < scored) {
-                const int tile = key / p.tile_keys, in = key - tile * p.tile_keys;
+        for (int t = pc.t0; t < pc.t1; t += kAddTiles) {
+            // kAddTiles keys of a thread, a tile apart: their loads are in flight together
+            float acc[kAddTiles], old[kAddTiles];
+            int key[kAddTiles];
+            int64_t at[kAddTiles];                         // first score of the key for KV head 0 of the item's head line
+#pragma unroll
+            for (int u = 0; u < kAddTiles; ++u) {
+                key[u] = (t + u) * kEvictAddKeys + tid;
+                if (t + u >= pc.t1 || key[u] >= n) key[u] = -1;
+                acc[u] = 0.f;
+                old[u] = e.decay != 0.f && key[u] >= 0 ? w[key[u]] : 0.f;
+                const int kk = key[u] >= 0 && key[u] < scored ? key[u] : 0;
+                const int tile = kk / p.tile_keys;
+                at[u] = ((int64_t)tile * p.hpc * p.tile_keys + (kk - tile * p.tile_keys)) * e.row_pitch;
+            }
+            if (scored > 0) {
                 for (int hh = 0; hh < pa.hpc; ++hh) {
                     const int h = pc.hg * pa.hpc + hh, hg = h / p.hpc, hl = h - hg * p.hpc;
-                    const float2* s = (const float2*)(e.scores + ((((int64_t)s_tiles[pc.b] + (int64_t)hg * sp.gt + tile) * p.hpc + hl) *
-                                                                      p.tile_keys + in) * e.row_pitch);
+                    const float* s = e.scores + (((int64_t)s_tiles[pc.b] + (int64_t)hg * sp.gt) * p.hpc + hl) * p.tile_keys * e.row_pitch;
                     const float2* mc = s_mc + hh * p.R;
-                    int r = 0;
-#pragma unroll 4
-                    for (; r + 1 < p.R; r += 2) {
-                        const float2 v = s[r >> 1];
-                        acc = fmaf(fast_exp2(v.x - mc[r].x), mc[r].y, acc);
-                        acc = fmaf(fast_exp2(v.y - mc[r + 1].x), mc[r + 1].y, acc);
+                    if ((e.row_pitch & 3) == 0) {
+                        add_rows<4>(s, at, mc, p.R, acc);
+                    } else {
+                        add_rows<2>(s, at, mc, p.R, acc);
                     }
-                    if (r < p.R) acc = fmaf(fast_exp2(s[r >> 1].x - mc[r].x), mc[r].y, acc);
                 }
             }
-            w[key] = e.decay != 0.f ? fmaf(e.decay, w[key], acc) : acc;
+#pragma unroll
+            for (int u = 0; u < kAddTiles; ++u)
+                if (key[u] >= 0) {
+                    const float x = key[u] < scored ? acc[u] : 0.f;
+                    w[key[u]] = e.decay != 0.f ? fmaf(e.decay, old[u], x) : x;
+                }
         }
     }
     if (flags) atomicOr(p.status, flags);
