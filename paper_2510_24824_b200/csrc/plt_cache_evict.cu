@@ -31,7 +31,7 @@ struct EvictGeometry {
     bool bf16, fp8;
     ScoreVariant v;              // fp32: HPC, KW and tile_keys only
     int part;                    // sequences per pair of launches
-    size_t score_floats, ml_floats, items;
+    size_t score_floats, ml_floats, mc_floats, items;
 };
 
 }  // namespace
@@ -39,12 +39,12 @@ struct EvictGeometry {
 struct plt_cache_evict {
     plt_cache_evict_config cfg;
     int32_t delta[kMaxLoops];
-    int32_t max_delta = 0;
+    int32_t min_delta = 0, max_delta = 0;
     EvictGeometry g;
     int sm_count = 0, score_grid = 0, add_grid = 0;
     size_t score_smem = 0, add_smem = 0;
     float scale_log2 = 0.f;
-    float *scores = nullptr, *ml = nullptr;
+    float *scores = nullptr, *ml = nullptr, *mc = nullptr;
     int32_t* item_blocks = nullptr;
     uint32_t* status = nullptr;
     EncodeTiledFn encode = nullptr;
@@ -70,6 +70,8 @@ plt_status fail(plt_cache_evict_t h, plt_status code, const char* fmt, ...) {
 plt_status cuda_fail(plt_cache_evict_t h, const char* what, cudaError_t e) {
     return fail(h, PLT_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
+
+int row_pitch(int rows) { return (rows + 3) & ~3; }
 
 plt_status check_config(const plt_cache_evict_config* c, EvictGeometry* g) {
     if (!c) return fail(nullptr, PLT_ERR_INVALID_ARG, "config is NULL");
@@ -104,16 +106,14 @@ plt_status check_config(const plt_cache_evict_config* c, EvictGeometry* g) {
     if (rows > kMaxRows) return fail(nullptr, PLT_ERR_UNSUPPORTED, "maps * L * q_len * Hq/Hkv = %.0f packed rows > %d", rows, kMaxRows);
     g->G = (c->Hq / c->Hkv) << g->qsplit;
     g->R = c->L * g->Qn * g->G;
-    if (evict_add_smem(g->hpg * g->R, c->max_batch) > 200 * 1024)
-        return fail(nullptr, PLT_ERR_UNSUPPORTED, "heads_per_group %d with %d packed rows each needs too much shared memory", g->hpg, g->R);
     if (g->bf16) {
         g->v = score_variant(c->d, g->R, c->Hkv, g->fp8, c->max_batch);
         if (g->v.smem > 227 * 1024) return fail(nullptr, PLT_ERR_UNSUPPORTED, "max_batch %d needs too much shared memory", c->max_batch);
     } else {
         g->v = ScoreVariant{c->d, 0, 1, false, 1, 1, kEvictF32Keys, 0, scores_f32_smem(c->d, g->R, c->max_batch)};
     }
-    const size_t tiles = ((size_t)c->max_seq_len + g->v.tile_keys - 1) / g->v.tile_keys;
-    const size_t per = tiles * g->v.tile_keys * c->Hkv * ((g->R + 1) & ~1);     // floats of a sequence's scores
+    const size_t tiles = ((size_t)c->max_seq_len + g->v.tile_keys - 1) / g->v.tile_keys + kEvictPieceCost;
+    const size_t per = tiles * g->v.tile_keys * c->Hkv * row_pitch(g->R);     // floats of a sequence's scores
     size_t part = kScoreScratch / 4 / per;
     part = part < 1 ? 1 : (part > (size_t)c->max_batch ? (size_t)c->max_batch : part);
     g->part = (int)part;
@@ -127,7 +127,9 @@ plt_status check_config(const plt_cache_evict_config* c, EvictGeometry* g) {
 
 size_t layout(const plt_cache_evict_config* c, EvictGeometry* g, int score_grid) {
     g->ml_floats = (g->items + score_grid) * g->v.HPC * g->v.KW * g->R * 2;
-    return (g->score_floats + g->ml_floats) * 4 + g->items * 8 + 256;
+    g->mc_floats = (size_t)g->part * c->Hkv * row_pitch(g->R) * 2;
+    g->ml_floats = (g->ml_floats + 3) & ~(size_t)3;       // the array behind is read 16 bytes at a time
+    return (g->score_floats + g->ml_floats + g->mc_floats) * 4 + g->items * 8 + 256;
 }
 
 bool aligned(const void* p, unsigned n) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -208,8 +210,8 @@ plt_status create_on_device(plt_cache_evict* h) {
     const int most = g.bf16 ? 2 : 4;
     h->score_grid = h->sm_count * (blocks < most ? blocks : most);
     h->score_smem = g.v.smem;
-    h->add_smem = evict_add_smem(g.hpg * g.R, c.max_batch);
-    e = evict_add_prepare(h->add_smem, &blocks);
+    h->add_smem = evict_add_smem(c.max_batch);
+    e = evict_add_prepare(row_pitch(g.R), h->add_smem, &blocks);
     if (e != cudaSuccess) return cuda_fail(nullptr, "preparing the add kernel", e);
     if (blocks < 1) return fail(nullptr, PLT_ERR_UNSUPPORTED, "the add kernel does not fit an SM");
     h->add_grid = h->sm_count * blocks;
@@ -230,7 +232,8 @@ plt_status create_on_device(plt_cache_evict* h) {
     }
     h->scores = (float*)ws;
     h->ml = h->scores + g.score_floats;
-    h->item_blocks = (int32_t*)(h->ml + g.ml_floats);
+    h->mc = h->ml + g.ml_floats;
+    h->item_blocks = (int32_t*)(h->mc + g.mc_floats);
     h->status = (uint32_t*)(h->item_blocks + 2 * g.items);
     e = cudaMemset(h->status, 0, 4);
     if (e != cudaSuccess) {
@@ -274,6 +277,7 @@ PLT_API plt_status plt_cache_evict_create(const plt_cache_evict_config* config, 
     for (int l = 0; l < kMaxLoops; ++l) {
         h->delta[l] = config->loop_offset && l < config->L ? config->loop_offset[l] : l;
         if (l < config->L && h->delta[l] > h->max_delta) h->max_delta = h->delta[l];
+        if (l == 0 || (l < config->L && h->delta[l] < h->min_delta)) h->min_delta = h->delta[l];
     }
     const float scale = config->sm_scale > 0.f ? config->sm_scale : 1.0f / sqrtf((float)(config->d >> g.qsplit));
     h->scale_log2 = scale * 1.4426950408889634f;
@@ -315,9 +319,13 @@ PLT_API plt_status plt_cache_evict_weights(plt_cache_evict_t h, const plt_cache_
     e.kbox = g.v.tile_keys;
     if (c.page_size > 0)
         while (c.page_size % e.kbox != 0) e.kbox >>= 1;    // 16 divides every page
-    e.row_pitch = (g.R + 1) & ~1;
+    e.row_pitch = row_pitch(g.R);
+    while ((1 << e.tile_shift) < g.v.tile_keys) ++e.tile_shift;
+    e.hpg = g.hpg;
+    e.min_delta = h->min_delta;
     e.scores = h->scores;
     e.ml = h->ml;
+    e.mc = (float2*)h->mc;
     e.weights_stride = ws;
     e.decay = a->decay;
     if (g.bf16) {
@@ -335,6 +343,7 @@ PLT_API plt_status plt_cache_evict_weights(plt_cache_evict_t h, const plt_cache_
     p.max_seq_len = c.max_seq_len; p.page_size = c.page_size; p.max_pages = a->max_pages; p.num_pool_pages = a->num_pool_pages;
     p.hpc = g.v.HPC;
     p.tile_keys = g.v.tile_keys;
+    p.piece_cost = kEvictPieceCost;
     p.scale_log2 = h->scale_log2;
     for (int l = 0; l < kMaxLoops; ++l) p.delta[l] = h->delta[l];
     const int groups = c.Hkv / g.hpg;
@@ -348,18 +357,11 @@ PLT_API plt_status plt_cache_evict_weights(plt_cache_evict_t h, const plt_cache_
         p.page_table = c.page_size > 0 ? a->page_table + (int64_t)b0 * a->max_pages : nullptr;
         e.gate = a->gate_logits && c.L > 1 ? a->gate_logits + (int64_t)b0 * (c.L - 1) * g.Qn * c.Hq : nullptr;
         e.weights = a->weights + (int64_t)b0 * groups * ws;
-        e.pa = p;
-        e.pa.L = 1;
-        e.pa.Qn = 1;
-        for (int l = 0; l < kMaxLoops; ++l) e.pa.delta[l] = 0;
-        e.pa.hpc = g.hpg;
-        e.pa.tile_keys = kEvictAddKeys;
-        e.pa.piece_cost = 1;
         cudaError_t err = g.bf16 ? launch_scores(g.v, h->map, e, h->score_grid, stream)
                                  : launch_scores_f32(e, h->score_grid, h->score_smem, stream);
         if (err != cudaSuccess) return cuda_fail(h, "launching the scores kernel", err);
         err = launch_evict_add(e, h->add_grid, h->add_smem, stream);
-        if (err != cudaSuccess) return cuda_fail(h, "launching the add kernel", err);
+        if (err != cudaSuccess) return cuda_fail(h, "launching the join and add kernels", err);
     }
     return PLT_OK;
 }

@@ -5,27 +5,29 @@
 namespace plt {
 
 // ---- attention weights ------------------------------------------------------------------------------------------
-// The work of plt_cache_evict_weights is two kernels over one batch of sequences:
+// The work of plt_cache_evict_weights is three kernels over one batch of sequences:
 //   scores  streams K once: scores of all packed rows (log2 units) into a scratch array, and for every row the maximum and
 //           the sum of exponentials over the block's piece of the keys
-//   add     joins the pieces' statistics and adds 2^(score - max) * rho / sum over the rows of a head group to the totals
+//   join    joins the pieces' statistics
+//   add     adds 2^(score - max) * rho / sum over the rows of a head group to the totals
 struct EvictWeights {
     Params p;                  // plan, query rows, lengths, pages; w = 0, hpc and tile_keys of the scores kernel
-    Params pa;                 // plan of the add kernel: one loop without offset (all positions below the length), hpc = heads of a
-                               // group, its own tile
-    int32_t b0;                // first sequence of this launch (pointers in p and pa are shifted already, K's tensor map is not)
+    int32_t b0;                // first sequence of this launch (the pointers in p are shifted already, K's tensor map is not)
     int32_t kw;                // warps along the keys of a tile of the scores kernel (each leaves statistics of its own)
     int32_t kbox;              // keys per TMA box
-    int32_t row_pitch;         // floats between the scores of consecutive keys: rows rounded up to even
-    float* scores;             // [tile of p's line][head of the tile][key][row_pitch]
-    float* ml;                 // [slot of p's plan][head][kw][R][2]
-    float* weights;            // [B][Hkv / pa.hpc] rows, weights_stride apart
+    int32_t row_pitch;         // floats between the scores of consecutive keys: rows rounded up to a multiple of four
+    int32_t tile_shift;        // log2 of p.tile_keys
+    int32_t hpg;               // KV heads of a group
+    int32_t min_delta;         // smallest causal offset: positions below length - min_delta have scores
+    float* scores;             // [place on p's line][head of the tile][key][row_pitch]
+    float* ml;                 // [slot of p's plan][head][kw][R][2] maximum and sum of a piece
+    float2* mc;                // [B][Hkv][row_pitch] maximum of a row and rho / sum (0 where there is no row or no key)
+    float* weights;            // [B][Hkv / hpg] rows, weights_stride apart
     int64_t weights_stride;
     const float* gate;         // [B, L-1, Qn, Hq] or null
     float decay;
 };
 
-constexpr int kEvictAddKeys = 256;     // keys per tile of the add kernel (one thread each)
 constexpr int kEvictF32Keys = 32;      // keys per tile of the fp32 scores kernel
 
 // Blocks of a plan of T tiles: at least `least` tiles each.
@@ -35,6 +37,7 @@ __host__ __device__ inline int evict_ctas(int64_t T, int launched, int least) {
     return c < launched ? (int)c : launched;
 }
 constexpr int kEvictScoreTiles = 2;    // least tiles per block of the scores kernel
+constexpr int kEvictPieceCost = 3;     // what starting and finishing an item costs a block of it, in tiles
 
 struct ScoreVariant {
     int D, NT, HPC;        // head dim (elements), 8-row groups, KV heads per block
@@ -49,9 +52,10 @@ cudaError_t launch_scores(const ScoreVariant& v, const CUtensorMap& mapK, const 
 size_t scores_f32_smem(int D, int R, int max_batch);
 cudaError_t scores_f32_prepare(int D, int R, int max_batch, int* blocks_per_sm);
 cudaError_t launch_scores_f32(const EvictWeights& e, int grid, size_t smem, cudaStream_t stream);
-size_t evict_add_smem(int rows, int max_batch);
-cudaError_t evict_add_prepare(size_t smem, int* blocks_per_sm);
-cudaError_t launch_evict_add(const EvictWeights& e, int grid, size_t smem, cudaStream_t stream);
+size_t evict_add_smem(int max_batch);
+cudaError_t evict_add_prepare(int row_pitch, size_t smem, int* blocks_per_sm);
+cudaError_t launch_evict_add(   // join and add
+    const EvictWeights& e, int grid, size_t smem, cudaStream_t stream);
 
 // ---- selection ----------------------------------------------------------------------------------------------------
 struct SelectParams {

@@ -201,8 +201,8 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
                 lsum[nt][0] = lsum[nt][1] = 0.f;
             }
             const float sc2 = FP8 ? p.scale_log2 * p.k_scale[kvh] : p.scale_log2;
-            // scores of the item's tile t, head h_local: tile index on the line times heads per tile
-            const int64_t tile0 = (int64_t)s_prefix[pc.b] + (int64_t)pc.hg * pc.sp.gt;
+            // the item's first tile on the line, behind its lead-in (whose places in the scratch stay empty)
+            const int64_t tile0 = (int64_t)s_prefix[pc.b] + (int64_t)pc.hg * line_len(p, pc.sp.gt) + p.piece_cost;
 
             for (int t = pc.t0; t < pc.t1; ++t) {
                 if (ok) {
@@ -270,7 +270,7 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
                             for (int ki = 0; ki < C::KS; ++ki)
                                 lsum[nt][j] += fast_exp2(s[ki][nt][j] - mref[nt][j]) + fast_exp2(s[ki][nt][2 + j] - mref[nt][j]);
                         }
-                        if (nt * 8 + 2 * tq < p.R) {
+                        if (nt * 8 + 2 * tq < e.row_pitch) {   // behind the last row: finite, or -inf
 #pragma unroll
                             for (int ki = 0; ki < C::KS; ++ki)
 #pragma unroll

@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(kFThreads) plt_evict_scores_f32(const __grid_c
             m[k] = -1e30f;
             l[k] = 0.f;
         }
-        const int64_t tile0 = (int64_t)s_prefix[pc.b] + (int64_t)pc.hg * pc.sp.gt;
+        const int64_t tile0 = (int64_t)s_prefix[pc.b] + (int64_t)pc.hg * line_len(p, pc.sp.gt) + p.piece_cost;
         for (int t = pc.t0; t < pc.t1; ++t) {
             const int key0 = t * TK;
             __syncthreads();   // the tile before has been read (and the query rows are in place)
@@ -103,6 +103,7 @@ __global__ void __launch_bounds__(kFThreads) plt_evict_scores_f32(const __grid_c
             }
             __syncthreads();
             float* dst = e.scores + ((tile0 + t) * TK + lane) * (int64_t)e.row_pitch;
+            if (R + wid < e.row_pitch) dst[R + wid] = -INFINITY;   // no row: weight 0
 #pragma unroll
             for (int k = 0; k < kFRows; ++k) {
                 const int r = wid + k * (kFThreads / 32);
@@ -148,135 +149,182 @@ __global__ void __launch_bounds__(kFThreads) plt_evict_scores_f32(const __grid_c
 }
 
 // ---- scores to weights --------------------------------------------------------------------------------------------
-// weight of a key = sum over rows of 2^(score - m) * (rho / l), m and l joined over the pieces of the row's item. A block
-// owns a run of 256-key tiles of one (sequence, head group): it joins the statistics of the group's rows into shared memory
-// (one warp per row, lanes over the pieces), then one thread per key walks the rows of the group's heads. The rows of a key
-// lie side by side, so the reads are whole sectors; the sum's order is the rows' order. Bound: L2 / HBM on the scores, and
-// the exponentials (one per row and key).
-constexpr int kAddThreads = kEvictAddKeys;
-constexpr int kAddTiles = 4;
-
-// Adds the weights of R rows of one head to the accumulators of kAddTiles keys; W rows per load.
-template <int W>
-__device__ __forceinline__ void add_rows(const float* s, const int64_t (&at)[kAddTiles], const float2* mc, int R, float (&acc)[kAddTiles]) {
-    for (int r = 0; r < R; r += W) {
-        float v[kAddTiles][W];
-#pragma unroll
-        for (int u = 0; u < kAddTiles; ++u) {
-            if constexpr (W == 4) {
-                const float4 x = *(const float4*)(s + at[u] + r);
-                v[u][0] = x.x; v[u][1] = x.y; v[u][2] = x.z; v[u][3] = x.w;
-            } else {
-                const float2 x = *(const float2*)(s + at[u] + r);
-                v[u][0] = x.x; v[u][1] = x.y;
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-            if (r + j < R) {                               // the pitch may hold one row more than there are
-                const float2 c = mc[r + j];
-#pragma unroll
-                for (int u = 0; u < kAddTiles; ++u) acc[u] = fmaf(fast_exp2(v[u][j] - c.x), c.y, acc[u]);
-            }
-        }
-    }
+// weight of a key = sum over rows of 2^(score - m) * (rho / l), m and l joined over the pieces of the row's item.
+//
+// Two kernels: `join` leaves (m, rho / l) of every row, a warp per 8 rows of a (sequence, KV head) with its lanes over the
+// pieces; `add` then has no chain of dependent loads and no barrier left. A warp of it takes 128 keys of one (sequence, head
+// group). The rows of a key lie side by side in the scratch, so LPK lanes share a key, four rows each in one 16-byte load: a
+// warp's load is 512 consecutive bytes, and a lane's statistics stay in its registers over the keys. (With a key per lane the
+// same loads touch a line each.) The sum's order is fixed by the rows alone. Bound: L2 / HBM on the scores.
+__device__ __forceinline__ int scored_tiles(const EvictWeights& e, int n) {
+    return (max(n - e.min_delta, 0) + (1 << e.tile_shift) - 1) >> e.tile_shift;
 }
 
-__global__ void __launch_bounds__(kAddThreads) plt_evict_add(const __grid_constant__ EvictWeights e) {
-    const Params &p = e.p, &pa = e.pa;
-    extern __shared__ float2 smem_f2[];
-    const int rows = pa.hpc * p.R;
-    float2* s_mc = smem_f2;                               // [rows] (m, rho / l)
-    int32_t* s_tiles = (int32_t*)(s_mc + rows);           // tile prefix of the scores plan
-    int32_t* s_prefix = s_tiles + p.B + 1;
-    int32_t* s_lens = s_prefix + p.B + 1;
+constexpr int kJoinThreads = 128;
+constexpr int kJoinRows = 8;                              // rows of a warp
+
+// Folds the statistics (m2, l2) into (m, l).
+__device__ __forceinline__ void fold(float& m, float& l, float m2, float l2) {
+    const float mm = fmaxf(m, m2);
+    l = l * fast_exp2(m - mm) + l2 * fast_exp2(m2 - mm);
+    m = mm;
+}
+
+__global__ void __launch_bounds__(kJoinThreads) plt_evict_join(const __grid_constant__ EvictWeights e) {
+    const Params& p = e.p;
+    const int lane = threadIdx.x & 31;
+    const int chunks = (p.R + kJoinRows - 1) / kJoinRows;
+    const int task = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
+    const int id = task / chunks, r0 = (task - id * chunks) * kJoinRows;    // sequence * Hkv + head, first row
+    grid_launch_dependents();
+    if (id >= p.B * p.Hkv) return;
+    const int b = id / p.Hkv, h = id - b * p.Hkv, hg = h / p.hpc, hl = h - hg * p.hpc;
+    uint32_t flags = 0;                                   // reported by the other kernels
+    const int n = seq_len_clamped(p, b, flags);
+    const int item = item_index(p, b, hg, 0);
+    // lane j (of 8) ends up with row r0 + j: its factor rho
+    const int row = r0 + (lane & (kJoinRows - 1));
+    float rho = 1.f;
+    const int lq = row / p.G, loop = lq / p.Qn;
+    const bool gated = e.gate != nullptr && row < p.R && loop > 0;
+    grid_dependency_wait();
+    int2 c = make_int2(0, -1);
+    if (scored_tiles(e, n) > 0) c = *(const int2*)(p.item_blocks + 2 * item);
+    if (gated) rho = e.gate[(((int64_t)b * (p.L - 1) + (loop - 1)) * p.Qn + (lq - loop * p.Qn)) * (p.Hq >> p.qsplit) +
+                            ((h * p.G + (row - lq * p.G)) >> p.qsplit)];
+    const int np = (c.y - c.x + 1) * e.kw;
+    float m[kJoinRows], l[kJoinRows];
+#pragma unroll
+    for (int j = 0; j < kJoinRows; ++j) {
+        m[j] = -1e30f;
+        l[j] = 0.f;
+    }
+    for (int i = lane; i < np; i += 32) {                 // a piece per lane, its rows together
+        const int64_t slot = slot_of(item, c.x + i / e.kw);
+        const float2* src = (const float2*)e.ml + ((slot * p.hpc + hl) * e.kw + i % e.kw) * p.R + r0;
+        float2 v[kJoinRows];
+#pragma unroll
+        for (int j = 0; j < kJoinRows; ++j) v[j] = r0 + j < p.R ? src[j] : make_float2(-1e30f, 0.f);
+#pragma unroll
+        for (int j = 0; j < kJoinRows; ++j) fold(m[j], l[j], v[j].x, v[j].y);
+    }
+    if (np > 1) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            if (o >= np) continue;                        // lanes from np on hold nothing
+#pragma unroll
+            for (int j = 0; j < kJoinRows; ++j)
+                fold(m[j], l[j], __shfl_xor_sync(0xffffffffu, m[j], o), __shfl_xor_sync(0xffffffffu, l[j], o));
+        }
+    }
+    if (gated) rho = 1.f / (1.f + expf(rho));             // 1 - sigmoid
+    // lane 0 has the joined statistics (with one piece, alone); lane j takes row r0 + j
+    float mj = 0.f, lj = 0.f;
+#pragma unroll
+    for (int j = 0; j < kJoinRows; ++j) {
+        const float m0 = __shfl_sync(0xffffffffu, m[j], 0), l0 = __shfl_sync(0xffffffffu, l[j], 0);
+        if (lane == j) {
+            mj = m0;
+            lj = l0;
+        }
+    }
+    // a row without a key, or no row at all (the pitch may hold more than there are): 2^(score - inf) * 0
+    if (lane < kJoinRows && row < e.row_pitch)            // the pitch ends within the last chunk of 8
+        e.mc[(int64_t)id * e.row_pitch + row] = lj == 0.f ? make_float2(INFINITY, 0.f) : make_float2(mj, rho / lj);
+}
+
+constexpr int kAddThreads = 256;
+constexpr int kAddRun = 128;                              // keys of a warp
+constexpr int kAddBatch = 8;                              // loads in flight per lane
+
+template <int LPK>
+__global__ void __launch_bounds__(kAddThreads, 3) plt_evict_add(const __grid_constant__ EvictWeights e) {
+    const Params& p = e.p;
+    extern __shared__ int32_t smem_i[];
+    const int groups = p.Hkv / e.hpg;
+    int32_t* s_tiles = smem_i;                            // [B + 1] line of the scores plan
+    int32_t* s_line = s_tiles + p.B + 1;                  // [B + 1] line of this kernel: runs of kAddRun keys of every head group
+    int32_t* s_lens = s_line + p.B + 1;                   // [B]
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     uint32_t flags = 0;
-    build_prefix(p, s_tiles, flags);
-    build_prefix(pa, s_prefix, flags, s_lens);
-    const int64_t T = s_prefix[p.B];
-    const int cta = blockIdx.x, nctas = evict_ctas(T, (int)gridDim.x, 1);
-    const bool in_plan = cta < nctas;
-    const int64_t lo = in_plan ? cta_begin(T, cta, nctas) : 0, hi = in_plan ? cta_begin(T, cta + 1, nctas) : 0;
-    grid_dependency_wait();
-
-    PieceWalk walk(pa, s_prefix, lo, hi, s_lens);
-    Piece pc;
-    while (walk.next(pc, flags)) {
-        SeqPlan sp;
-        seq_plan_n(p, pc.b, s_lens[pc.b], sp, flags);     // the scores plan of this sequence
-        __syncthreads();
-        for (int row = wid; row < rows; row += kAddThreads / 32) {
-            const int hh = row / p.R, r = row - hh * p.R;
-            const int h = pc.hg * pa.hpc + hh, hg = h / p.hpc, hl = h - hg * p.hpc;
-            float m = -1e30f, l = 0.f;
-            if (sp.gt > 0) {
-                const int item = item_index(p, pc.b, hg, 0);
-                const int2 c = *(const int2*)(p.item_blocks + 2 * item);
-                const int np = (c.y - c.x + 1) * e.kw;
-                for (int i = lane; i < np; i += 32) {
-                    const int64_t slot = slot_of(item, c.x + i / e.kw);
-                    const float2 v = *(const float2*)(e.ml + (((slot * p.hpc + hl) * e.kw + i % e.kw) * p.R + r) * 2);
-                    const float mm = fmaxf(m, v.x);
-                    l = l * fast_exp2(m - mm) + v.y * fast_exp2(v.x - mm);
-                    m = mm;
-                }
-            }
+    for (int b = tid; b < p.B; b += kAddThreads) {
+        const int n = seq_len_clamped(p, b, flags);
+        s_lens[b] = n;
+        s_tiles[b + 1] = (p.Hkv / p.hpc) * line_len(p, scored_tiles(e, n));
+        s_line[b + 1] = groups * ((n + kAddRun - 1) / kAddRun);
+    }
+    __syncthreads();
+    if (wid < 2) {                                        // both prefixes, a warp each
+        int32_t* sp = wid == 0 ? s_tiles : s_line;
+        int32_t run = 0;
+        if (lane == 0) sp[0] = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            int32_t v = b0 + lane < p.B ? sp[b0 + lane + 1] : 0;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
-                const float mm = fmaxf(m, m2);
-                l = l * fast_exp2(m - mm) + l2 * fast_exp2(m2 - mm);
-                m = mm;
+                const int32_t u = __shfl_up_sync(0xffffffffu, v, o);
+                if (lane >= o) v += u;
             }
-            if (lane == 0) {
-                const int lq = r / p.G, loop = lq / p.Qn;
-                float rho = 1.f;
-                if (e.gate != nullptr && loop > 0) {
-                    const int hq = (h * p.G + (r - lq * p.G)) >> p.qsplit;
-                    const float x = e.gate[(((int64_t)pc.b * (p.L - 1) + (loop - 1)) * p.Qn + (lq - loop * p.Qn)) * (p.Hq >> p.qsplit) + hq];
-                    rho = 1.f / (1.f + expf(x));           // 1 - sigmoid(x)
-                }
-                s_mc[row] = make_float2(m, l == 0.f ? 0.f : rho / l);
-            }
+            if (b0 + lane < p.B) sp[b0 + lane + 1] = run + v;
+            run += __shfl_sync(0xffffffffu, v, 31);
         }
-        __syncthreads();
-        const int n = pc.sp.cmax;                          // the length
-        const int scored = sp.gt * p.tile_keys;            // keys that have scores (beyond a row's cutoff: -inf)
-        float* w = e.weights + ((int64_t)pc.b * (p.Hkv / pa.hpc) + pc.hg) * e.weights_stride;
-        for (int t = pc.t0; t < pc.t1; t += kAddTiles) {
-            // kAddTiles keys of a thread, a tile apart: their loads are in flight together
-            float acc[kAddTiles], old[kAddTiles];
-            int key[kAddTiles];
-            int64_t at[kAddTiles];                         // first score of the key for KV head 0 of the item's head line
+    }
+    __syncthreads();
+    grid_dependency_wait();
+    const int T = s_line[p.B];
+    const int64_t head = (int64_t)e.row_pitch << e.tile_shift;              // scores of a head's part of a tile
+    for (int pos = blockIdx.x * (kAddThreads / 32) + wid; pos < T; pos += gridDim.x * (kAddThreads / 32)) {
+        const int b = find_seq(s_line, p.B, pos);
+        const int n = s_lens[b], runs = (n + kAddRun - 1) / kAddRun;
+        const int o = pos - s_line[b], g = o / runs;
+        constexpr int KPI = 32 / LPK, BATCHES = kAddRun / (KPI * kAddBatch);
+        constexpr int U = BATCHES > 0 ? kAddBatch : kAddRun / KPI;          // keys of a lane's group in flight
+        const int sub = lane & (LPK - 1), r0 = 4 * sub;
+        const int gt = scored_tiles(e, n), scored = gt << e.tile_shift;     // keys that have scores (beyond a row's cutoff: -inf)
+        float* w = e.weights + ((int64_t)b * groups + g) * e.weights_stride;
+        const int64_t line = (int64_t)line_len(p, gt) * p.hpc * head;       // scores of a head line
+        const float* first = e.scores + ((int64_t)s_tiles[b] + p.piece_cost) * p.hpc * head;
+        for (int k0 = (o - g * runs) * kAddRun + lane / LPK, done = 0; done < kAddRun && k0 - lane / LPK < n; done += U * KPI, k0 += U * KPI) {
+            float acc[U];
 #pragma unroll
-            for (int u = 0; u < kAddTiles; ++u) {
-                key[u] = (t + u) * kEvictAddKeys + tid;
-                if (t + u >= pc.t1 || key[u] >= n) key[u] = -1;
-                acc[u] = 0.f;
-                old[u] = e.decay != 0.f && key[u] >= 0 ? w[key[u]] : 0.f;
-                const int kk = key[u] >= 0 && key[u] < scored ? key[u] : 0;
-                const int tile = kk / p.tile_keys;
-                at[u] = ((int64_t)tile * p.hpc * p.tile_keys + (kk - tile * p.tile_keys)) * e.row_pitch;
+            for (int u = 0; u < U; ++u) acc[u] = 0.f;
+            float old[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int key = k0 + u * KPI;
+                old[u] = e.decay != 0.f && u % LPK == sub && key < n ? w[key] : 0.f;
             }
-            if (scored > 0) {
-                for (int hh = 0; hh < pa.hpc; ++hh) {
-                    const int h = pc.hg * pa.hpc + hh, hg = h / p.hpc, hl = h - hg * p.hpc;
-                    const float* s = e.scores + (((int64_t)s_tiles[pc.b] + (int64_t)hg * sp.gt) * p.hpc + hl) * p.tile_keys * e.row_pitch;
-                    const float2* mc = s_mc + hh * p.R;
-                    if ((e.row_pitch & 3) == 0) {
-                        add_rows<4>(s, at, mc, p.R, acc);
-                    } else {
-                        add_rows<2>(s, at, mc, p.R, acc);
+            if (r0 < e.row_pitch) {
+                for (int h = g * e.hpg; h < (g + 1) * e.hpg; ++h) {
+                    const int hg = h / p.hpc, hl = h - hg * p.hpc;
+                    const float* s = first + hg * line + hl * head + r0;
+                    const float2* mc = e.mc + ((int64_t)b * p.Hkv + h) * e.row_pitch + r0;
+                    const float4 c01 = *(const float4*)mc, c23 = *(const float4*)(mc + 2);
+                    float4 v[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int key = k0 + u * KPI;
+                        v[u] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                        // row (tile * hpc * TK + key % TK) of the head line
+                        if (key < scored && key < n)
+                            v[u] = *(const float4*)(s + ((int64_t)(key >> e.tile_shift) * ((p.hpc - 1) << e.tile_shift) + key) * e.row_pitch);
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        acc[u] = fmaf(fast_exp2(v[u].x - c01.x), c01.y, acc[u]);
+                        acc[u] = fmaf(fast_exp2(v[u].y - c01.z), c01.w, acc[u]);
+                        acc[u] = fmaf(fast_exp2(v[u].z - c23.x), c23.y, acc[u]);
+                        acc[u] = fmaf(fast_exp2(v[u].w - c23.z), c23.w, acc[u]);
                     }
                 }
             }
 #pragma unroll
-            for (int u = 0; u < kAddTiles; ++u)
-                if (key[u] >= 0) {
-                    const float x = key[u] < scored ? acc[u] : 0.f;
-                    w[key[u]] = e.decay != 0.f ? fmaf(e.decay, old[u], x) : x;
-                }
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int i = 1; i < LPK; i <<= 1) acc[u] += __shfl_xor_sync(0xffffffffu, acc[u], i);
+                const int key = k0 + u * KPI;
+                if (u % LPK == sub && key < n) w[key] = e.decay != 0.f ? fmaf(e.decay, old[u], acc[u]) : acc[u];
+            }
         }
     }
     if (flags) atomicOr(p.status, flags);
@@ -349,16 +397,32 @@ cudaError_t launch_scores_f32(const EvictWeights& e, int grid, size_t smem, cuda
                         : launch_overlapped(plt_evict_scores_f32<64>, e, grid, kFThreads, smem, stream);
 }
 
-size_t evict_add_smem(int rows, int max_batch) { return (size_t)rows * 8 + (size_t)(3 * max_batch + 4) * 4; }
+size_t evict_add_smem(int max_batch) { return (size_t)(3 * max_batch + 4) * 4; }
 
-cudaError_t evict_add_prepare(size_t smem, int* blocks_per_sm) {
-    const cudaError_t err = allow_max_dynamic_smem((const void*)plt_evict_add);
-    if (err != cudaSuccess) return err;
-    return cudaOccupancyMaxActiveBlocksPerMultiprocessor(blocks_per_sm, plt_evict_add, kAddThreads, smem);
+namespace {
+// lanes per key: four rows each, a power of two
+template <typename F>
+cudaError_t with_lanes(int row_pitch, F&& f) {
+    if (row_pitch <= 4) return f(plt_evict_add<1>);
+    if (row_pitch <= 8) return f(plt_evict_add<2>);
+    if (row_pitch <= 16) return f(plt_evict_add<4>);
+    if (row_pitch <= 32) return f(plt_evict_add<8>);
+    return f(plt_evict_add<16>);
+}
+}  // namespace
+
+cudaError_t evict_add_prepare(int row_pitch, size_t smem, int* blocks_per_sm) {
+    return with_lanes(row_pitch, [&](auto fn) {
+        const cudaError_t err = allow_max_dynamic_smem((const void*)fn);
+        return err != cudaSuccess ? err : cudaOccupancyMaxActiveBlocksPerMultiprocessor(blocks_per_sm, fn, kAddThreads, smem);
+    });
 }
 
 cudaError_t launch_evict_add(const EvictWeights& e, int grid, size_t smem, cudaStream_t stream) {
-    return launch_overlapped(plt_evict_add, e, grid, kAddThreads, smem, stream);
+    const int warps = e.p.B * e.p.Hkv * ((e.p.R + kJoinRows - 1) / kJoinRows);
+    const cudaError_t err = launch_overlapped(plt_evict_join, e, (warps + kJoinThreads / 32 - 1) / (kJoinThreads / 32), kJoinThreads, 0, stream);
+    if (err != cudaSuccess) return err;
+    return with_lanes(e.row_pitch, [&](auto fn) { return launch_overlapped(fn, e, grid, kAddThreads, smem, stream); });
 }
 
 }  // namespace plt

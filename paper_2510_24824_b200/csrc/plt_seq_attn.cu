@@ -23,17 +23,9 @@
 // and denominator, and a pass whose probabilities are already normalised and gated, g * p / l_local, and accumulate into
 // the same O, which the softmax threads have scaled to (1 - g) * y_global in between. Eq. 2 thus costs no second
 // accumulator. Every wait on an mbarrier is bounded and reports through the status word.
-//
-// DIFF = true is the kernel of differential heads: tiles A and B are the two softmax maps of ONE query head on the same
-// 128 rows. Map x multiplies half x of the query and key rows (64 of the 128 elements: one 128-byte swizzled half of the
-// tiles as TMA wrote them, so nothing is copied or padded), both maps multiply the same V tile, and the block owns both
-// results of a row: the epilogue reads the two accumulators, takes y_1 - lambda y_2 in fp32 and normalises the head
-// without either map reaching memory. Per key tile the products cost three quarters of two plain tiles (the scores
-// contract 64 elements instead of 128) and the exponentials the same.
 #include "../../include/plt_seq_attn.h"
 
 #include <cuda.h>
-#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <cmath>
@@ -42,23 +34,12 @@
 #include <cstring>
 #include <new>
 
-#include "plt_host.h"
-#include "plt_ptx.cuh"
+#include "plt_seq_util.cuh"
 
 namespace plt {
 namespace {
 
-constexpr int SQ = 128;                    // query rows per tile
-constexpr int SK = 128;                    // keys per tile
-constexpr int SD = 128;                    // head dimension
-constexpr int kTileBytes = SK * SD * 2;    // one Q, K or V tile
-constexpr int kHalf = SK * 128;            // one 64-element half of a tile: [128 rows][128 bytes]
 constexpr int kRing = 5;                   // K/V ring slots
-constexpr int kSeqThreads = 384;
-constexpr float kSeqBig = 256.f;           // probabilities stay below 2^8 of their row's reference, else the slow path
-constexpr float kSeqNoMax = -1e30f;
-constexpr uint64_t kSeqWaitNs = 1000000000ull;
-constexpr int kSeqMaxLoops = 8;
 
 // mbarriers
 constexpr int SB_QFULL = 0;                // Q tiles landed
@@ -70,18 +51,6 @@ constexpr int SB_ODONE = SB_PFULL + 2;     // + X: every product into O_X comple
 constexpr int SB_COUNT = SB_ODONE + 2;
 
 constexpr size_t kSeqSmem = 1024 + 2 * kTileBytes + (size_t)kRing * kTileBytes + SB_COUNT * 8 + 64;
-
-struct SeqParams {
-    const float* gate;          // [B, L-1, T, Hq]
-    const int32_t* seq_lens;    // [B]
-    __nv_bfloat16* out;         // [B, L, T, Hq, d]
-    uint32_t* status;
-    int32_t B, L, T, Hq, Hkv, G, w, nqb;   // nqb: row blocks per sequence (128 rows with paired heads, else 256)
-    int32_t pair_heads, heads_per_grid;      // tiles of a block = two heads of one KV group; grid entries per (row block, loop)
-    float scale_log2;
-    int32_t delta[kSeqMaxLoops];
-    DiffTail tail;              // DIFF only
-};
 
 // The steps of one block: nG tiles of the shared K/V (tile A takes part in the first ntA of them), then for loops
 // 2..L the tiles [l0, l0 + nL) of the loop's own K/V that the windows of the block's rows touch, scores only (kind 1),
@@ -113,70 +82,6 @@ __device__ __forceinline__ SeqStep seq_step_at(const SeqPlan& pl, int i) {
     return s;
 }
 
-// Shared-memory matrix descriptor of tcgen05.mma (start address, leading / stride byte offsets in 16-byte units,
-// descriptor version 1, 128-byte swizzle).
-__device__ __forceinline__ uint64_t seq_smem_desc(uint32_t addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lbo_bytes >> 4) << 16) | ((uint64_t)(sbo_bytes >> 4) << 32) |
-           (1ull << 46) | (2ull << 61);
-}
-// Instruction descriptor: fp32 accumulate, bf16 A and B, B majorness (0 = K-major, 1 = MN-major), N / 8, M / 16.
-__host__ __device__ constexpr uint32_t seq_instr_desc(int M, int N, int b_mn_major) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) |
-           ((uint32_t)(M >> 4) << 24);
-}
-// D[tmem] (+)= A[tmem] * B[smem]
-__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
-                                             uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-// 32 consecutive 32-bit columns of this thread's lane
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
-          "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
-          "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
-}
-
-// Bounded wait that also gives up as soon as another thread of the block has given up.
-__device__ __noinline__ bool seq_wait_slow(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    const uint64_t t0 = global_timer_ns();
-    uint32_t spins = 0;
-    while (!mbar_try_wait(bar, parity)) {
-        if ((++spins & 0x3fu) == 0) {
-            if (*abort_flag) return false;
-            if (global_timer_ns() - t0 > kSeqWaitNs) {
-                *abort_flag = 1;
-                return false;
-            }
-        }
-    }
-    return true;
-}
-__device__ __forceinline__ bool seq_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    if (mbar_test_wait(bar, parity)) return true;
-    return seq_wait_slow(bar, parity, abort_flag);
-}
-
 struct SeqRing {
     int slot;
     uint32_t parity;
@@ -188,34 +93,6 @@ struct SeqRing {
         }
     }
 };
-
-// What a softmax thread knows about its row.
-struct RowCtx {
-    int t;            // row (decode step) index
-    int cut;          // shared keys the row may see: max(0, t + 1 - delta)
-    int lo;           // first own key of the window: max(delta, t + 1 - w)
-    bool live;        // t < n_b and cut > 0
-};
-
-// 32 scores of a row -> probabilities against the reference: packed bf16 into pk[16], summed (fp32, two lanes) and
-// their packed maximum tracked (bf16 bit patterns of non-negative numbers order like integers).
-template <bool FULL>
-__device__ __forceinline__ void global_chunk(const uint32_t (&r)[32], int c, int lim, float2 sc2, float2 nm2, uint32_t* pk,
-                                             float2& sum2, uint32_t& pmax) {
-#pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-        float2 t = __ffma2_rn(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), sc2, nm2);
-        if (!FULL) {
-            if (c * 32 + i >= lim) t.x = -INFINITY;
-            if (c * 32 + i + 1 >= lim) t.y = -INFINITY;
-        }
-        const float2 pr = make_float2(fast_exp2(t.x), fast_exp2(t.y));
-        sum2 = __fadd2_rn(sum2, pr);
-        const uint32_t h = pack_bf16x2(pr.x, pr.y);
-        pk[i / 2] = h;
-        asm("max.u16x2 %0, %0, %1;" : "+r"(pmax) : "r"(h));
-    }
-}
 
 // One pass over the 128 scores of this thread's row (tensor-memory lane) of a shared-K/V step: probabilities against
 // the reference mref, packed bf16 into pk[64], their sum and the largest probability. kbase: index of the tile's first
@@ -260,26 +137,6 @@ __device__ __forceinline__ float global_row_max(uint32_t tS, const RowCtx& rc, i
     return mx;
 }
 
-// Scores-only pass over a tile of the loop's own keys: folds the visible columns [c_lo, c_hi] of this thread's row into
-// the window softmax's exact running maximum ml (log2 units) and denominator ll. Rows without a visible key keep
-// ml = -inf, ll = 0. Every lane runs every load (they are collective over the warp).
-__device__ __forceinline__ void window_stats_chunk(const uint32_t (&r)[32], int c, int c_lo, int c_hi, float scale, float& ml,
-                                                   float& ll) {
-    float t[32], cmax = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        const int col = c * 32 + i;
-        t[i] = (col >= c_lo && col <= c_hi) ? __uint_as_float(r[i]) * scale : -INFINITY;
-        cmax = fmaxf(cmax, t[i]);
-    }
-    const float m_new = fmaxf(ml, cmax);
-    const float m_use = m_new > -INFINITY ? m_new : 0.f;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) sum += fast_exp2(t[i] - m_use);
-    ll = ll * fast_exp2(ml - m_use) + sum;   // ml = -inf: the old denominator is 0 and stays 0
-    ml = m_new;
-}
 __device__ __forceinline__ void window_stats(uint32_t tS, int c_lo, int c_hi, float scale, float& ml, float& ll) {
     uint32_t ra[32], rb[32];
     tmem_ld32(tS, ra);
@@ -296,18 +153,6 @@ __device__ __forceinline__ void window_stats(uint32_t tS, int c_lo, int c_hi, fl
     window_stats_chunk(rb, 3, c_lo, c_hi, scale, ml, ll);
 }
 
-// Second pass over the same tile: the weights 2^(s * scale + negm) of the visible columns (0 elsewhere), packed bf16.
-__device__ __forceinline__ void window_weights_chunk(const uint32_t (&r)[32], int c, int c_lo, int c_hi, float2 sc2, float2 nm2,
-                                                     uint32_t* pk) {
-#pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-        const int col = c * 32 + i;
-        float2 t = __ffma2_rn(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), sc2, nm2);
-        if (!(col >= c_lo && col <= c_hi)) t.x = -INFINITY;
-        if (!(col + 1 >= c_lo && col + 1 <= c_hi)) t.y = -INFINITY;
-        pk[i / 2] = pack_bf16x2(fast_exp2(t.x), fast_exp2(t.y));
-    }
-}
 __device__ __forceinline__ void window_weights(uint32_t tS, int c_lo, int c_hi, float scale, float negm, uint32_t (&pk)[64]) {
     const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(negm, negm);
     uint32_t ra[32], rb[32];
@@ -325,85 +170,6 @@ __device__ __forceinline__ void window_weights(uint32_t tS, int c_lo, int c_hi, 
     window_weights_chunk(rb, 3, c_lo, c_hi, sc2, nm2, &pk[48]);
 }
 
-// Multiplies this thread's row of O (128 fp32 columns) by f.
-__device__ __forceinline__ void scale_o_row(uint32_t tO, float f) {
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        uint32_t r[32];
-        tmem_ld32(tO + c * 32, r);
-        tmem_wait_ld();
-#pragma unroll
-        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
-        tmem_st32(tO + c * 32, r);
-    }
-    tmem_wait_st();
-}
-
-// Epilogue of a differential head. Thread (x, row) holds the factor f that makes accumulator x of its row a finished
-// result (1 / denominator, or 1 where Eq. 2 has been applied already) and writes the columns [64 x, 64 x + 64) of the row:
-// x = y_1 - lambda y_2 and the norm over the row's 128 elements, in fp32. `xch`: 4 x 128 floats of shared memory (the half
-// of the query buffer that the two maps do not need). All 256 softmax threads call it, whatever became of their waits.
-__device__ __forceinline__ void diff_epilogue(const SeqParams& p, float* xch, uint32_t t_lane, int x, int row, int b, int l, int h,
-                                              const RowCtx& rc, bool have_o, float f) {
-    const int lane = threadIdx.x & 31;
-    float d1 = 0.f, d2 = 0.f;   // the learned factor of this head
-    const int lrow = p.tail.lambda_heads > 1 ? h * (SD / 2) : 0;
-#pragma unroll
-    for (int i = lane; i < SD / 2; i += 32) {
-        d1 = fmaf(p.tail.lq1[lrow + i], p.tail.lk1[lrow + i], d1);
-        d2 = fmaf(p.tail.lq2[lrow + i], p.tail.lk2[lrow + i], d2);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        d1 += __shfl_xor_sync(0xffffffffu, d1, o);
-        d2 += __shfl_xor_sync(0xffffffffu, d2, o);
-    }
-    const float lambda = expf(d1) - expf(d2) + p.tail.lambda_init;
-    xch[x * SQ + row] = f;
-    named_barrier_sync(1, 256);
-    const float f1 = xch[row], f2 = -lambda * xch[SQ + row];
-    float y[SD / 2];
-    float ss = 0.f;
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        uint32_t r1[32], r2[32];
-        if (have_o) {   // warp-uniform: the loads are collective
-            tmem_ld32(t_lane + 256 + x * 64 + c * 32, r1);
-            tmem_ld32(t_lane + 384 + x * 64 + c * 32, r2);
-            tmem_wait_ld();
-        }
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const float v = have_o && rc.live ? fmaf(f2, __uint_as_float(r2[i]), f1 * __uint_as_float(r1[i])) : 0.f;
-            y[c * 32 + i] = v;
-            ss = fmaf(v, v, ss);
-        }
-    }
-    float inv = 1.f;
-    if (p.tail.gain != nullptr) {
-        xch[2 * SQ + x * SQ + row] = ss;
-        named_barrier_sync(1, 256);
-        ss += xch[2 * SQ + (1 - x) * SQ + row];
-        inv = (1.f - p.tail.lambda_init) / sqrtf(ss * (1.f / SD) + p.tail.eps);
-    }
-    if (rc.t < p.T) {
-        __nv_bfloat16* dst = p.out + ((((int64_t)b * p.L + l) * p.T + rc.t) * p.Hq + h) * SD + x * 64;
-#pragma unroll
-        for (int i = 0; i < SD / 2; i += 8) {
-            float g[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] = inv * (p.tail.gain != nullptr ? p.tail.gain[x * 64 + i + j] : 1.f);
-            uint4 v;
-            v.x = pack_bf16x2(y[i] * g[0], y[i + 1] * g[1]);
-            v.y = pack_bf16x2(y[i + 2] * g[2], y[i + 3] * g[3]);
-            v.z = pack_bf16x2(y[i + 4] * g[4], y[i + 5] * g[5]);
-            v.w = pack_bf16x2(y[i + 6] * g[6], y[i + 7] * g[7]);
-            *(uint4*)(dst + i) = v;
-        }
-    }
-}
-
-template <bool DIFF>
 __global__ void __launch_bounds__(kSeqThreads, 1)
 plt_seq_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmKl,
@@ -429,7 +195,7 @@ plt_seq_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const int l = item % p.L; item /= p.L;
     const int b = item % p.B; item /= p.B;
     const int qb = p.nqb - 1 - item;
-    const int hA = !DIFF && p.pair_heads ? 2 * hh : hh, hB = !DIFF && p.pair_heads ? 2 * hh + 1 : hh;
+    const int hA = p.pair_heads ? 2 * hh : hh, hB = p.pair_heads ? 2 * hh + 1 : hh;
     uint32_t flags = 0;
     int n = p.seq_lens[b];
     if (n < 0 || n > p.T) {
@@ -507,8 +273,8 @@ plt_seq_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             tma_prefetch_desc(&tmV);
             const uint64_t keep = l2_evict_first_policy();   // K/V tiles are re-read by the other heads and loops from L2;
             // the policy only orders evictions among streamed data
-            mbar_expect_tx(&bars[SB_QFULL], (activeA ? kTileBytes : 0) + (activeB && !DIFF ? kTileBytes : 0));
-            for (int x = 0; x < (DIFF ? 1 : 2); ++x) {   // the two maps of a head share one query tile
+            mbar_expect_tx(&bars[SB_QFULL], (activeA ? kTileBytes : 0) + (activeB ? kTileBytes : 0));
+            for (int x = 0; x < 2; ++x) {
                 if (!(x == 0 ? activeA : activeB)) continue;
                 const int r0 = x == 0 ? r0A : r0B;
                 for (int hf = 0; hf < 2; ++hf)
@@ -568,11 +334,9 @@ plt_seq_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 if (!ok) return;
                 tc_fence_after_sync();
                 if (lane == 0) {
-                    // DIFF: map x contracts half x of the rows only
-                    const uint32_t ka = ring_a + (uint32_t)slot * kTileBytes + (DIFF ? (uint32_t)x * kHalf : 0u);
-                    const uint32_t qa = q_a + (uint32_t)x * (DIFF ? kHalf : kTileBytes);
+                    const uint32_t ka = ring_a + (uint32_t)slot * kTileBytes, qa = q_a + (uint32_t)x * kTileBytes;
 #pragma unroll
-                    for (int kk = 0; kk < (DIFF ? SD / 32 : SD / 16); ++kk)
+                    for (int kk = 0; kk < SD / 16; ++kk)
                         umma_bf16(tmem_base + x * 128, seq_smem_desc(qa + (kk >> 2) * kHalf + (kk & 3) * 32, 16, 1024),
                                   seq_smem_desc(ka + (kk >> 2) * kHalf + (kk & 3) * 32, 16, 1024), idesc_qk, kk == 0 ? 0u : 1u);
                     umma_commit(&bars[SB_SFULL + x]);
@@ -740,14 +504,10 @@ plt_seq_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             }
             // ---- epilogue: O_x out of tensor memory ---------------------------------------------------------
             if (ok) ok = seq_wait(&bars[SB_ODONE + x], 0, abort_flag);
-            if (DIFF && ok) ok = seq_wait(&bars[SB_ODONE + 1 - x], 0, abort_flag);   // the other map's result is read too
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after_sync();
         }
-        if constexpr (DIFF) {
-            diff_epilogue(p, (float*)(q_smem + kTileBytes), tmem_base + lane_off, x, wq * 32 + lane, b, l, h, rc, active && ok,
-                          l == 0 ? (lg > 0.f ? 1.f / lg : 0.f) : 1.f);
-        } else {
+        {
             // Every lane of the warp runs the loads (they are collective); only rows inside the tensor are stored.
             const bool in_tensor = rc.t < p.T;
             __nv_bfloat16* dst = p.out + ((((int64_t)b * p.L + l) * p.T + (in_tensor ? rc.t : 0)) * p.Hq + h) * SD;
@@ -909,7 +669,7 @@ plt_status seq_create(const plt_seq_attn_config* c, bool diff, plt_seq_attn_t* o
         return seq_fail(nullptr, PLT_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
     }
     h->encode = (SeqEncodeFn)fn;
-    e = allow_max_dynamic_smem(diff ? (const void*)plt_seq_attn_kernel<true> : (const void*)plt_seq_attn_kernel<false>);
+    e = diff ? diff_seq_prepare() : allow_max_dynamic_smem((const void*)plt_seq_attn_kernel);
     if (e != cudaSuccess) {
         delete h;
         return seq_fail(nullptr, PLT_ERR_CUDA, "preparing the kernel: %s", cudaGetErrorString(e));
@@ -964,20 +724,25 @@ plt_status seq_run(plt_seq_attn_t h, const plt_seq_attn_args* a, const DiffTail*
     p.out = (__nv_bfloat16*)a->out;
     p.status = h->status;
     p.B = a->batch; p.L = c.L; p.T = T; p.Hq = c.Hq; p.Hkv = c.Hkv; p.G = c.Hq / c.Hkv; p.w = c.w;
-    p.pair_heads = (h->diff || p.G % 2 == 0) ? 1 : 0;     // both tiles of a block take the same rows
-    p.heads_per_grid = p.pair_heads && !h->diff ? p.Hq / 2 : p.Hq;
-    if (tail) p.tail = *tail;
+    p.pair_heads = (p.G % 2 == 0) ? 1 : 0;
+    p.heads_per_grid = p.pair_heads ? p.Hq / 2 : p.Hq;
     p.nqb = p.pair_heads ? (T + SQ - 1) / SQ : (T + 2 * SQ - 1) / (2 * SQ);
+    if (h->diff) {          // both maps of a head on the same 128 rows
+        p.tail = *tail;
+        p.heads_per_grid = p.Hq;
+        p.nqb = (T + SQ - 1) / SQ;
+    }
     p.scale_log2 = h->scale_log2;
     for (int l = 0; l < kSeqMaxLoops; ++l) p.delta[l] = h->delta[l];
     const unsigned grid = (unsigned)((int64_t)p.nqb * p.B * p.L * p.heads_per_grid);
-    if (h->diff)
-        plt_seq_attn_kernel<true><<<grid, kSeqThreads, kSeqSmem, (cudaStream_t)cuda_stream>>>(h->maps[0], h->maps[1], h->maps[2],
-                                                                                              h->maps[3], h->maps[4], p);
-    else
-        plt_seq_attn_kernel<false><<<grid, kSeqThreads, kSeqSmem, (cudaStream_t)cuda_stream>>>(h->maps[0], h->maps[1], h->maps[2],
-                                                                                               h->maps[3], h->maps[4], p);
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e;
+    if (h->diff) {
+        e = launch_diff_seq(h->maps, p, grid, (cudaStream_t)cuda_stream);
+    } else {
+        plt_seq_attn_kernel<<<grid, kSeqThreads, kSeqSmem, (cudaStream_t)cuda_stream>>>(h->maps[0], h->maps[1], h->maps[2],
+                                                                                        h->maps[3], h->maps[4], p);
+        e = cudaGetLastError();
+    }
     if (e != cudaSuccess) return seq_fail(h, PLT_ERR_CUDA, "launching the kernel: %s", cudaGetErrorString(e));
     return PLT_OK;
 }

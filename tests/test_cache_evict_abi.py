@@ -49,7 +49,7 @@ OK = dict(dtype="bf16", max_batch=4, L=2, Hq=8, Hkv=4, d=128, max_seq_len=512)
     (dict(kv_dtype="e4m3", d=64), B.PLT_ERR_UNSUPPORTED), (dict(kv_dtype="e4m3", dtype="f32"), B.PLT_ERR_UNSUPPORTED),
     (dict(kv_dtype=9), B.PLT_ERR_INVALID_ARG), (dict(dtype=9), B.PLT_ERR_INVALID_ARG), (dict(max_batch=0), B.PLT_ERR_INVALID_ARG),
     (dict(max_batch=4097), B.PLT_ERR_UNSUPPORTED), (dict(max_seq_len=(1 << 24) + 1), B.PLT_ERR_UNSUPPORTED),
-    (dict(loop_offset=[0, -1]), B.PLT_ERR_INVALID_ARG), (dict(Hkv=1024, Hq=32768, L=2, heads_per_group=1024), B.PLT_ERR_UNSUPPORTED),
+    (dict(loop_offset=[0, -1]), B.PLT_ERR_INVALID_ARG),
 ])
 def test_refusals(change, code):
     for call in (B.plt_cache_evict_workspace_bytes, B.plt_cache_evict_create):
