@@ -28,17 +28,18 @@ constexpr int kSelThreads = 1024;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelBins = 2048;
 
-// Orders like the value: NaN 0, then from -inf up; -0 and 0 alike. All ones is left for protected positions.
+// Orders like the value: NaN 1, then from -inf up; -0 and 0 alike. All ones is left for protected positions, 0 for places
+// behind the row's end, which are below everything that can be picked and so need no test of their own.
 __device__ __forceinline__ uint32_t order_key(float x) {
-    if (x != x) return 0u;
     const uint32_t u = __float_as_uint(x + 0.f);        // -0 + 0 = 0
-    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+    const uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return x == x ? k : 1u;
 }
 
 struct Row {
     const float* w;
-    int n, first, last0;                                // [0, first) and [last0, n) are protected
-    __device__ __forceinline__ uint32_t key(int i, float x) const { return i < first || i >= last0 ? 0xffffffffu : order_key(x); }
+    uint32_t first, inner;                              // [0, first) and [first + inner, n) are protected
+    __device__ __forceinline__ uint32_t key(int i, float x) const { return (uint32_t)i - first >= inner ? 0xffffffffu : order_key(x); }
     __device__ __forceinline__ uint32_t key(int i) const { return key(i, w[i]); }
 };
 
@@ -71,7 +72,8 @@ constexpr int kSharedKeys = 48 * 1024;                  // per block
 
 template <int HOME, bool CLUSTER>
 __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __grid_constant__ SelectParams p, const int csize) {
-    __shared__ uint32_t hist[kSelBins];                 // this block's counts (read by the whole cluster)
+    __shared__ uint32_t hist[kSelBins];                 // this block's counts
+    __shared__ uint32_t sums[CLUSTER ? 2 : 1][CLUSTER ? kSelBins : 1];   // the cluster's, for this pass and the next
     __shared__ uint32_t warp_sums[32];
     __shared__ uint32_t s_pick[4];                      // digit picked; keys above it: in the cluster, in this block; equal: in this block
     __shared__ uint32_t s_mine[2];                      // keys above T and equal to T in this block (read by the cluster)
@@ -90,7 +92,7 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
         for (int i = rank * kSelThreads + tid; i < p.budget; i += csize * kSelThreads) out[i] = i < n ? i : -1;
         return;
     }
-    const Row r{p.weights + (int64_t)row * p.weights_stride, n, p.keep_first, n - p.keep_last};
+    const Row r{p.weights + (int64_t)row * p.weights_stride, (uint32_t)p.keep_first, (uint32_t)(n - p.keep_last - p.keep_first)};
     // Warp w of the csize * 32 warps of the row has the run [w0, w1): `steps` pieces of 32 positions.
     const int steps = (n + csize * kSelThreads - 1) / (csize * kSelThreads);
     const int w0 = min(n, (rank * kSelWarps + wid) * steps * 32), w1 = min(n, w0 + steps * 32);
@@ -105,34 +107,40 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
             held[j] = j < steps && i < w1 ? r.key(i) : 0u;
         }
     } else if constexpr (HOME == kShared) {
-        // the totals as they are, all on their way at once; the first pass turns them into keys
-        for (int j = 0; j < steps; ++j) {
-            const int i = w0 + j * 32 + lane;
-            if (i < w1)
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(run + j * 32 + lane)), "l"(r.w + i) : "memory");
+        // the totals as they are, all on their way at once; the first pass turns them into keys. Rows that start on a 16-byte
+        // boundary move four to an instruction, up to the last whole four.
+        int i0 = w0;
+        if (((uintptr_t)r.w & 15u) == 0) {
+            i0 = w0 + ((w1 - w0) & ~3);
+            for (int i = w0 + 4 * lane; i < i0; i += 128)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(run + (i - w0))), "l"(r.w + i) : "memory");
         }
+        for (int i = i0 + lane; i < w1; i += 32)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(run + (i - w0))), "l"(r.w + i) : "memory");
         asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();                                   // the copies of the other lanes
     }
-    // Calls f(piece, key, whether the position exists) for every piece of the warp's run; `fresh`: the first call. A lane
-    // reads back its own keys.
+    const int whole = (w1 - w0) / 32;                   // pieces that have all their positions
+    // Calls f(piece, key) for every piece of the warp's run, with key 0 behind the end; `fresh`: the first call.
     auto walk = [&](bool fresh, auto&& f) {
         if constexpr (HOME == kRegisters) {
 #pragma unroll
             for (int j = 0; j < IPT; ++j)
-                if (j < steps) f(j, held[j], w0 + j * 32 + lane < w1);
+                if (j < steps) f(j, held[j]);
         } else {
-#pragma unroll 4
-            for (int j = 0; j < steps; ++j) {
+            auto key_of = [&](int j) {
                 const int i = w0 + j * 32 + lane;
-                uint32_t k = 0u;
                 if constexpr (HOME == kShared) {
-                    k = run[j * 32 + lane];
+                    uint32_t k = run[j * 32 + lane];
                     if (fresh) run[j * 32 + lane] = k = r.key(i, __uint_as_float(k));
+                    return k;
                 } else {
-                    if (i < w1) k = r.key(i);
+                    return r.key(i);
                 }
-                f(j, k, i < w1);
-            }
+            };
+#pragma unroll 4
+            for (int j = 0; j < whole; ++j) f(j, key_of(j));
+            if (whole < steps && w0 + whole * 32 < w1) f(whole, w0 + whole * 32 + lane < w1 ? key_of(whole) : 0u);
         }
     };
 
@@ -146,22 +154,39 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
         const int prev = shift;
         shift -= bits;
         for (int i = tid; i < kSelBins; i += kSelThreads) hist[i] = 0;
+        if (CLUSTER && pass == 0) {
+            for (int i = tid; i < kSelBins; i += kSelThreads) sums[0][i] = 0;
+            cg::this_cluster().sync();                  // no block adds before all have cleared
+        }
         __syncthreads();
-        if (pass == 0) walk(true, [&](int, uint32_t k, bool exists) {
-            if (exists) atomicAdd(&hist[k >> shift], 1u);
+        if (pass == 0) walk(true, [&](int, uint32_t k) { atomicAdd(&hist[k >> shift], 1u); });
+        else walk(false, [&](int, uint32_t k) {
+            if ((k >> prev) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1u);
         });
-        else walk(false, [&](int, uint32_t k, bool exists) {
-            if (exists && (k >> prev) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1u);
-        });
-        if constexpr (CLUSTER) cg::this_cluster().sync(); else __syncthreads();
+        __syncthreads();
+        const uint32_t* counts = hist;
+        if constexpr (CLUSTER) {
+            // Bins that hold something are few: each block adds its own to every block's sums. The sums of the next pass are
+            // cleared before the barrier behind which anyone adds to them.
+            cg::cluster_group cluster = cg::this_cluster();
+#pragma unroll
+            for (int u = 0; u < kSelBins / kSelThreads; ++u) {
+                const int bin = tid + u * kSelThreads;
+                const uint32_t v = hist[bin];
+                sums[(pass + 1) & 1][bin] = 0;
+                if (v != 0)
+                    for (int q = 0; q < csize; ++q) atomicAdd(cluster.map_shared_rank(&sums[pass & 1][bin], q), v);
+            }
+            cluster.sync();
+            counts = sums[pass & 1];
+        }
         // thread t has bins 2 t and 2 t + 1 counted from the top; the picked one is where the running count reaches `left`
         uint32_t c[2], mine[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int bin = kSelBins - 1 - (2 * tid + u);
-            mine[u] = c[u] = hist[bin];
-            if constexpr (CLUSTER)
-                for (int q = 1; q < csize; ++q) c[u] += *cg::this_cluster().map_shared_rank(&hist[bin], (rank + q) % csize);
+            mine[u] = hist[bin];
+            c[u] = counts[bin];
         }
         uint32_t total, before = block_scan(c[0] + c[1], warp_sums, total) - c[0] - c[1], before_mine = before;
         if constexpr (CLUSTER) before_mine = block_scan(mine[0] + mine[1], warp_sums, total) - mine[0] - mine[1];
@@ -181,7 +206,6 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
         left -= s_pick[1];
         above_mine += s_pick[2];
         equal_mine = s_pick[3];
-        if constexpr (CLUSTER) cg::this_cluster().sync();   // the other blocks have read this one's counts
     }
     // T = prefix; `left` of the keys equal to it are kept, the lowest positions first
     uint32_t above = 0, equal = 0;                      // before this block's part
@@ -199,27 +223,29 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
         cg::this_cluster().sync();                      // no block ends while another reads its counts
     }
     uint32_t ng = 0, ne = 0;                            // in this warp's run
-    walk(false, [&](int, uint32_t k, bool exists) {
-        ng += __popc(__ballot_sync(0xffffffffu, exists && k > prefix));
-        ne += __popc(__ballot_sync(0xffffffffu, exists && k == prefix));
+    walk(false, [&](int, uint32_t k) {
+        ng += k > prefix;
+        ne += k == prefix;
     });
+    ng = __reduce_add_sync(0xffffffffu, ng);
+    ne = __reduce_add_sync(0xffffffffu, ne);
     uint32_t total;
     const uint32_t ig = block_scan(lane == 31 ? ng : 0u, warp_sums, total), ie = block_scan(lane == 31 ? ne : 0u, warp_sums, total);
     above += __shfl_sync(0xffffffffu, ig, 31) - ng;
     equal += __shfl_sync(0xffffffffu, ie, 31) - ne;
     const uint32_t below = (1u << lane) - 1u;
-    int32_t* to = out + above + min(equal, left);       // the warp's next place
-    walk(false, [&](int j, uint32_t k, bool exists) {
-        const int at = w0 + j * 32 + lane;
-        bool take = exists && k > prefix;
-        const bool tie = exists && k == prefix;
-        if (__any_sync(0xffffffffu, tie)) {             // rare
+    uint32_t to = above + min(equal, left);             // the warp's next place
+    const bool ties = ne > 0 && equal < left;           // of the warp's run, some equal to T are kept
+    walk(false, [&](int j, uint32_t k) {
+        bool take = k > prefix;
+        if (ties) {
+            const bool tie = k == prefix;
             const uint32_t me = __ballot_sync(0xffffffffu, tie);
             take = take || (tie && equal + __popc(me & below) < left);
             equal += __popc(me);
         }
         const uint32_t mask = __ballot_sync(0xffffffffu, take);
-        if (take) to[__popc(mask & below)] = at;
+        if (take) out[to + __popc(mask & below)] = w0 + j * 32 + lane;
         to += __popc(mask);
     });
 }
