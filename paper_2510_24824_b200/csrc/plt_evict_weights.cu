@@ -273,7 +273,9 @@ __global__ void __launch_bounds__(kAddThreads, 3) plt_evict_add(const __grid_con
     grid_dependency_wait();
     const int T = s_line[p.B];
     const int64_t head = (int64_t)e.row_pitch << e.tile_shift;              // scores of a head's part of a tile
-    for (int pos = blockIdx.x * (kAddThreads / 32) + wid; pos < T; pos += gridDim.x * (kAddThreads / 32)) {
+    // from the line's end: part of what the scores kernel wrote last is still in L2 (8 sequences of 32768 codes, 16 rows: 91
+    // instead of 104 MB of the 134 read from HBM, the call 104 instead of 108 us)
+    for (int pos = T - 1 - (int)(blockIdx.x * (kAddThreads / 32) + wid); pos >= 0; pos -= gridDim.x * (kAddThreads / 32)) {
         const int b = find_seq(s_line, p.B, pos);
         const int n = s_lens[b], runs = (n + kAddRun - 1) / kAddRun;
         const int o = pos - s_line[b], g = o / runs;
