@@ -19,7 +19,9 @@
  * All tensor pointers are DEVICE pointers owned by the caller unless a comment says "host".  No exception crosses this
  * boundary; errors are plt_status codes.  There is no CPU fallback.  The device of a handle is made current for the length
  * of each call; the stream must belong to it.  Calls on the same handle must be stream-ordered (they share the workspace);
- * none of them allocates or synchronises, and all can be captured in a CUDA graph.
+ * none of them allocates or synchronises, and all can be captured in a CUDA graph (a call that a capture replays has fixed
+ * addresses; lengths, positions and totals are read on the device).  plt_cache_evict_weights reads seq_lens while the kernel
+ * before it in the stream finishes, under the terms that plt_decode_attn_run states; the other two are ordinary launches.
  */
 #ifndef PLT_CACHE_EVICT_H
 #define PLT_CACHE_EVICT_H
@@ -66,7 +68,8 @@ typedef struct {
  *
  * with the cutoffs of plt_decode_attn_run (cut = max(0, N_b - delta_l - (q_len - 1 - token)); a position that a row does not
  * see gets nothing from it).  rho = 1, or, where gate_logits is given, 1 - sigmoid(gate) for the rows of loops 2..L: the
- * share that Eq. 2 gives the shared cache.  Scores, softmax and totals are fp32.  The sums' order depends on nothing but the
+ * share that Eq. 2 gives the shared cache.  Scores, softmax and totals are fp32 (with E4M3 caches the products take the
+ * queries in f16, which holds bf16 values exactly between 2^-14 and 65504).  The sums' order depends on nothing but the
  * configuration and the lengths, so results repeat bit for bit.
  */
 typedef struct {

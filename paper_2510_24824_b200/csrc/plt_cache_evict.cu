@@ -236,6 +236,7 @@ plt_status create_on_device(plt_cache_evict* h) {
     h->item_blocks = (int32_t*)(h->mc + g.mc_floats);
     h->status = (uint32_t*)(h->item_blocks + 2 * g.items);
     e = cudaMemset(h->status, 0, 4);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);   // before a call on a stream that does not wait for the default one
     if (e != cudaSuccess) {
         cudaFree(ws);
         return cuda_fail(nullptr, "cudaMemset", e);

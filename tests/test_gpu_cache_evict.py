@@ -317,6 +317,52 @@ def test_refusals_of_calls():
         assert op.check() == 0
 
 
+def test_a_handle_for_a_larger_batch_and_other_buffers_between_calls():
+    """max_batch above the batch; the same handle on other addresses, another length and another stream in turn."""
+    big = problem(lens=("list", [300, 77, 2]))
+    small = problem(B=2, lens=("list", [200, 300]), max_seq_len=300, seed=8)
+    side = torch.cuda.Stream()
+    with CacheEvict(big, max_batch=9) as op:
+        for p in (big, small, big):
+            q = f32_to_bf16_bits(np.random.default_rng(p.B).standard_normal((p.B, p.L, 1, p.Hq, p.d)).astype(np.float32))
+            dp, dq = DeviceProblem(p, "cuda:0"), to_torch(q, "bf16", "cuda:0")
+            w = torch.zeros(p.B + 1, p.Hkv, p.max_seq_len, device="cuda")
+            w[p.B] = 3.0
+            torch.cuda.synchronize()
+            with torch.cuda.stream(side):
+                op.weights(dp, dq, w)
+                assert op.check() == 0
+            want, _ = oracle_evict.weights(stored(q), values(p, "k_cache"), p.seq_lens, np.zeros((p.B, p.Hkv, p.max_seq_len)))
+            assert np.allclose(w[: p.B].cpu().numpy(), want, rtol=1e-3, atol=1e-7)
+            assert bool((w[p.B] == 3.0).all()), "rows behind the batch were written"
+
+
+def test_compact_caches_that_share_one_buffer_and_repeated_positions():
+    """K and V as the two halves of one tensor (strides), and a position that is kept twice."""
+    p = problem(lens=("list", [300, 120, 40]))
+    dp = DeviceProblem(p, "cuda:0")
+    both = torch.stack([dp.k_cache, dp.v_cache], dim=3).contiguous()          # [B, N, Hkv, 2, d]
+    dp.k_cache, dp.v_cache = both[:, :, :, 0], both[:, :, :, 1]
+    n, h, d = p.max_seq_len, p.Hkv, p.d
+    keep, new = oracle_evict.select(np.random.default_rng(3).random((p.B, h, n)).astype(np.float32), p.seq_lens, 50, 2, 5)
+    keep[:, :, 10] = keep[:, :, 11]
+    with CacheEvict(p) as op:
+        op.compact(dp, to_torch(keep, "", "cuda:0"), to_torch(new, "", "cuda:0"), kv_strides=(n * h * 2 * d, h * 2 * d, 2 * d))
+        assert op.check() == 0
+    for i, name in enumerate(("k_cache", "v_cache")):
+        want = oracle_evict.compact(getattr(p, name), keep, new)
+        assert np.array_equal(both[:, :, :, i].contiguous().cpu().view(torch.int16).numpy().view(np.uint16), want)
+
+
+def test_infinite_and_huge_scores():
+    """Keys that drive scores far apart, and a cache row of the largest values: weights stay finite and sum to their rows."""
+    p = problem(L=1, Hq=4, Hkv=4, lens=("list", [300, 77, 2]))
+    k = stored(p.k_cache) * 40.0
+    k[:, 1] *= 8.0
+    p = p.with_(k_cache=f32_to_bf16_bits(k.astype(np.float32)))
+    check_weights(p, decay=0.0)
+
+
 # ---- together -----------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("page,kv", [(0, ""), (32, ""), (32, "e4m3")])
 @pytest.mark.parametrize("diff", [False, True])

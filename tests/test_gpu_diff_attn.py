@@ -173,6 +173,31 @@ def test_bad_lengths_and_pages_are_clamped_and_flagged():
         assert op.check() == B.PLT_DEV_PAGE_ID_CLAMPED
 
 
+def test_a_handle_for_a_larger_batch():
+    p = make_problem(spec(lens=("list", [300, 77, 2])))
+    lambdas, gain = learned(p.d, 1)
+    dp = DeviceProblem(p, "cuda:0")
+    out = torch.full((p.B + 1, p.L, p.Hq, p.d), 5.0, dtype=torch.bfloat16, device="cuda")
+    with DiffAttn(p, lambdas, gain, LAMBDA_INIT, EPS, max_batch=70) as op:
+        op.run(dp, out=out)
+        assert op.check() == 0
+    assert_close(out[: p.B].float().cpu().numpy().astype(np.float64), oracle.diff_maps(p), lambdas, gain, "bf16", e_map(p), "max_batch 70")
+    assert bool((out[p.B] == 5.0).all()), "rows behind the batch were written"
+
+
+def test_strided_head_major_cache():
+    p = make_problem(spec(lens=("list", [320, 100, 7])))
+    lambdas, gain = learned(p.d, p.Hq)
+    dp = DeviceProblem(p, "cuda:0")
+    dp.k_cache, dp.v_cache = (t.permute(0, 2, 1, 3).contiguous() for t in (dp.k_cache, dp.v_cache))
+    with DiffAttn(p, lambdas, gain, LAMBDA_INIT, EPS) as op:
+        a = dp.args()
+        a.kv_stride_b, a.kv_stride_h, a.kv_stride_n = p.Hkv * 320 * p.d, 320 * p.d, p.d
+        B.plt_diff_attn_run(op.handle, a, op.weights, torch.cuda.current_stream().cuda_stream)
+        assert op.check() == 0
+    assert_close(dp.out.float().cpu().numpy().astype(np.float64), oracle.diff_maps(p), lambdas, gain, "bf16", e_map(p), "HND strides")
+
+
 def test_refusals_of_a_call():
     p = make_problem(spec())
     lambdas, gain = learned(p.d, 1)
@@ -260,6 +285,33 @@ def test_prompt_with_sharp_rows():
     p = make_seq_problem(B=1, L=2, T=400, Hq=2, Hkv=2, d=128, w=50, seed=7)
     big = f32_to_bf16_bits((np.random.default_rng(1).standard_normal(p.q.shape) * 6.0).astype(np.float32))
     run_seq(p.with_(q=big))
+
+
+def test_prompt_graph_replay_with_new_lengths():
+    p = make_seq_problem(B=2, L=2, T=300, Hq=2, Hkv=1, d=128, w=64, seed=12)
+    lambdas, gain = learned(128, 1)
+    side = torch.cuda.Stream()
+    with DiffSeqAttn(p, lambdas, gain, LAMBDA_INIT, EPS) as op:
+        with torch.cuda.stream(side):
+            op.run()
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                op.run()
+        for lens in ([300, 129], [0, 1]):
+            op.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+            op.out.fill_(float("nan"))
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            q = p.with_(seq_lens=np.array(lens, np.int32))
+            e = map_error("bf16", max(largest(p.v_share), largest(p.v_loc)), 128, largest(p.q), max(largest(p.k_share), largest(p.k_loc)))
+            assert_close(op.out.float().cpu().numpy().astype(np.float64), oracle.diff_seq_maps(q), lambdas, gain, "bf16", e, f"{lens}")
+        assert op.check() == 0
+        bad = torch.tensor([-1, 10 ** 6], dtype=torch.int32)
+        op.seq_lens.copy_(bad)
+        op.run()
+        assert op.check() == B.PLT_DEV_SEQ_LEN_CLAMPED
 
 
 def test_prompt_rows_are_decode_steps():
