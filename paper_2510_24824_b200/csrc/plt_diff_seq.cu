@@ -138,6 +138,12 @@ plt_diff_seq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         pl.total = pl.nG + 2 * pl.nL;
     }
 
+    if (pl.total == 0) {   // no row has a token: zeros, without tensor memory or barriers
+        for (int i = tid; i < (min(r0 + SQ, p.T) - r0) * (SD / 8); i += kSeqThreads)
+            *(uint4*)(p.out + ((((int64_t)b * p.L + l) * p.T + r0 + i / (SD / 8)) * p.Hq + h) * SD + i % (SD / 8) * 8) = make_uint4(0, 0, 0, 0);
+        if (flags && tid == 0) atomicOr(p.status, flags);
+        return;
+    }
     if (tid == 0) {
         s_ctl[0] = 0;
         s_ctl[2] = 0;
