@@ -83,10 +83,13 @@ __global__ void __launch_bounds__(THREADS) plt_evict_compact_kernel(const __grid
         // A sequence that keeps all it has moves nothing: seen in one sweep without barriers (in a batch of ragged lengths these
         // are many, and chunk by chunk they held up the blocks with work: 97 -> 92 us)
         if (s.m == s.n) {
-            bool moves = false;
+            bool moved = false;
 #pragma unroll 4
-            for (int i = tid; i < s.m; i += THREADS) moves |= s.keep[i] != i;
-            if (!__syncthreads_or(moves)) return;
+            for (int i = tid; i < s.m; i += THREADS) moved |= s.keep[i] != i;
+            if (!__syncthreads_or(moved)) {
+                if (flags) atomicOr(p.status, flags);     // a length may have been clamped
+                return;
+            }
         }
         char* base = (which ? p.v : p.k) + (int64_t)h * p.stride_h + (piece * kColumns + tid % kColumns) * 16;
         int k[MINE];                     // positions of the chunk that is planned next

@@ -363,6 +363,74 @@ def test_infinite_and_huge_scores():
     check_weights(p, decay=0.0)
 
 
+def test_compact_flags_clamped_lengths_where_nothing_moves():
+    """Every kept position is its own slot and there are no totals: the lengths out of range still show."""
+    p = problem(lens=("list", [100, 50, 20]))
+    keep = np.tile(np.arange(100, dtype=np.int32), (3, 4, 1))
+    for lens, new, bits in (([100, 50, 20], [100, 50, 20], 0), ([10 ** 6, 50, 20], [100, 50, 20], B.PLT_DEV_SEQ_LEN_CLAMPED),
+                            ([100, -4, 20], [100, 0, 20], B.PLT_DEV_SEQ_LEN_CLAMPED), ([100, 50, 20], [100, 50, 21], B.PLT_DEV_KEEP_CLAMPED)):
+        dp = DeviceProblem(p, "cuda:0")
+        dp.seq_lens = to_torch(np.array(lens, np.int32), "", "cuda:0")
+        with CacheEvict(p) as op:
+            op.compact(dp, to_torch(keep, "", "cuda:0"), to_torch(np.array(new, np.int32), "", "cuda:0"))
+            assert op.check() == bits, (lens, new)
+        assert np.array_equal(dp.k_cache.cpu().view(torch.int16).numpy().view(np.uint16), p.k_cache)
+
+
+@pytest.mark.parametrize("page", [0, 64])
+def test_offsets_beyond_32_bits(page):
+    """The same cache in a few MB and spread over more than 2^32 bytes: totals, attention and compaction agree bit for bit."""
+    p = problem(B=1, lens=("list", [2300]), page_size=page)
+    lambdas, gain = learned(p.d, 1)
+    row, budget = p.Hkv * p.d, 700
+    near, far = DeviceProblem(p, "cuda:0"), DeviceProblem(p, "cuda:0")
+    if page:
+        pages = (1 << 33) // (page * row * 2) // 2 + 200                 # 2^32 bytes and some
+        pools = []
+        for name in ("k_cache", "v_cache"):
+            pool = torch.empty(pages, page, p.Hkv, p.d, dtype=torch.bfloat16, device="cuda")
+            pool[pages - p.num_pool_pages:] = getattr(near, name).flip(0)
+            pools.append(pool)
+        far.k_cache, far.v_cache = pools
+        far.page_table = (pages - 1 - near.page_table).to(torch.int32)
+        strides, count = (0, 0, 0), pages
+        rows = [lambda t, which: getattr(near, which)[near.page_table[0].long()].view(-1, row)[:t],
+                lambda t, which: getattr(far, which)[far.page_table[0].long()].view(-1, row)[:t]]
+    else:
+        wide = 1 << 20                                                   # elements between rows: 4.8 GB
+        both = torch.empty(p.max_seq_len, wide, dtype=torch.bfloat16, device="cuda")
+        far.k_cache, far.v_cache = both, both[:, wide // 2:]
+        both[:, :row], both[:, wide // 2:wide // 2 + row] = near.k_cache.view(-1, row), near.v_cache.view(-1, row)
+        strides, count = (p.max_seq_len * wide, wide, p.d), 0
+        rows = [lambda t, which: getattr(near, which).view(-1, row)[:t],
+                lambda t, which: getattr(far, which)[:t, :row]]
+    q = near.q.view(p.B, p.L, 1, p.Hq, p.d)
+    results = []
+    with DiffAttn(p, lambdas, gain, LAMBDA_INIT, EPS) as attn, CacheEvict(p, maps=2) as op:
+        for dp, (sb, sn, sh), n in ((near, (0, 0, 0), p.num_pool_pages), (far, strides, count)):
+            stream = torch.cuda.current_stream().cuda_stream
+            a = dp.args()
+            a.kv_stride_b, a.kv_stride_n, a.kv_stride_h, a.num_pool_pages = sb, sn, sh, n
+            B.plt_diff_attn_run(attn.handle, a, attn.weights, stream)
+            w = torch.zeros(p.B, p.Hkv, p.max_seq_len, device="cuda")
+            a = op.weights_args(dp, q, w, kv_strides=(sb, sn, sh))
+            a.num_pool_pages = n
+            B.plt_cache_evict_weights(op.handle, a, stream)
+            keep, new = torch.empty(p.B, p.Hkv, budget, dtype=torch.int32, device="cuda"), torch.empty(p.B, dtype=torch.int32, device="cuda")
+            op.select(dp, w, keep, new, budget, 4, 16)
+            a = op.compact_args(dp, keep, new, w, kv_strides=(sb, sn, sh))
+            a.num_pool_pages = n
+            B.plt_cache_evict_compact(op.handle, a, stream)
+            assert attn.check() == 0 and op.check() == 0
+            results.append((dp.out.clone(), w, keep))
+    for one, other in zip(*results):
+        assert torch.equal(one, other)
+    for which in ("k_cache", "v_cache"):
+        assert torch.equal(rows[0](p.max_seq_len, which), rows[1](p.max_seq_len, which)), which
+    moved = oracle_evict.compact(values(p, "k_cache"), results[0][2].cpu().numpy(), np.array([budget]))
+    assert np.array_equal(rows[0](budget, "k_cache").float().cpu().numpy(), moved.reshape(-1, row)[:budget].astype(np.float32))
+
+
 # ---- together -----------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("page,kv", [(0, ""), (32, ""), (32, "e4m3")])
 @pytest.mark.parametrize("diff", [False, True])
