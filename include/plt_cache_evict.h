@@ -55,8 +55,8 @@ typedef struct {
     int32_t device;
     const int32_t* loop_offset; /* host, L entries delta_l >= 0; NULL: delta_l = l-1.  Copied at create. */
     int32_t q_len;            /* query tokens per loop of one plt_cache_evict_weights call; 0 or 1: one */
-    int32_t maps;             /* 0 or 1: one softmax for each head; 2: differential heads (plt_diff_attn.h), the weights of
-                                 both maps count */
+    int32_t maps;             /* 0 or 1: one softmax for each head; 2: differential heads (plt_diff_attn.h, with what it says
+                                 of K's values), the weights of both maps count */
     int32_t heads_per_group;  /* KV heads that share totals and positions; 0 or 1: none; divides Hkv */
 } plt_cache_evict_config;
 

@@ -16,6 +16,9 @@
  * h / (Hq / Hkv).  With loops 2..L each map is mixed by the gate first (Eq. 2 is linear, so y_m = g * y_m,local +
  * (1 - g) * y_m,global), then the difference is taken.  Rows whose loop has no token yet are written as zeros.
  *
+ * The K rows that a query row sees have to be finite in both halves (the decode step multiplies the half of the other map
+ * by zero).
+ *
  * Softmax statistics, both results, the factor, the difference and the norm are held in fp32; the output is rounded once.
  * All tensor pointers are DEVICE pointers owned by the caller.  No exception crosses this boundary; errors are plt_status
  * codes.  There is no CPU fallback.  The device of a handle is made current for the length of each call; the stream must

@@ -22,15 +22,16 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Scratch for scores: a batch whose scores at full length exceed this runs in several pairs of launches over parts of the
-// batch. At 8 packed rows of d = 128 it holds the scores of 2 GB of keys.
+// Scratch for scores: a batch whose scores at full length exceed this runs in several rounds of the three launches, each over a
+// part of the batch. At 8 packed rows of d = 128 it holds the scores of 2 GB of keys. (Smaller parts, whose scores would stay in
+// L2, cost more than they save: 8 sequences of 32768 codes, 16 rows, 104 us in one round, 122 us in parts of 72 MB, 145 us of 36.)
 constexpr size_t kScoreScratch = (size_t)256 << 20;
 
 struct EvictGeometry {
     int G, R, Qn, qsplit, hpg;   // packed rows per loop and token of a KV head (both maps), all packed rows
     bool bf16, fp8;
     ScoreVariant v;              // fp32: HPC, KW and tile_keys only
-    int part;                    // sequences per pair of launches
+    int part;                    // sequences per round of launches
     size_t score_floats, ml_floats, mc_floats, items;
 };
 
@@ -48,11 +49,6 @@ struct plt_cache_evict {
     int32_t* item_blocks = nullptr;
     uint32_t* status = nullptr;
     EncodeTiledFn encode = nullptr;
-    CUtensorMap map;
-    struct {
-        const void* base;
-        int64_t sb, sn, sh, outer;
-    } key = {nullptr, 0, 0, 0, 0};
     char err[512];
 };
 
@@ -175,21 +171,17 @@ plt_status check_totals(plt_cache_evict_t h, const void* weights, int64_t& strid
     return PLT_OK;
 }
 
-plt_status encode_keys(plt_cache_evict_t h, const void* base, int64_t sb, int64_t sn, int64_t sh, int es, int64_t outer, int kbox) {
-    if (h->key.base == base && h->key.sb == sb && h->key.sn == sn && h->key.sh == sh && h->key.outer == outer) return PLT_OK;
+plt_status encode_keys(plt_cache_evict_t h, CUtensorMap* map, const void* base, int64_t sb, int64_t sn, int64_t sh, int es, int64_t outer,
+                       int kbox) {
     const plt_cache_evict_config& c = h->cfg;
     cuuint64_t dims[4] = {(cuuint64_t)c.d, (cuuint64_t)(c.page_size > 0 ? c.page_size : c.max_seq_len), (cuuint64_t)c.Hkv, (cuuint64_t)outer};
     cuuint64_t strides[3] = {(cuuint64_t)(sn * es), (cuuint64_t)(sh * es), (cuuint64_t)(sb * es)};
     cuuint32_t box[4] = {(cuuint32_t)(128 / es), (cuuint32_t)kbox, (cuuint32_t)h->g.v.HPC, 1u};
     cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
-    const CUresult r = h->encode(&h->map, es == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+    const CUresult r = h->encode(map, es == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
                                  const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        h->key.base = nullptr;
-        return fail(h, PLT_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d for the keys", (int)r);
-    }
-    h->key = {base, sb, sn, sh, outer};
+    if (r != CUDA_SUCCESS) return fail(h, PLT_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d for the keys", (int)r);
     return PLT_OK;
 }
 
@@ -329,8 +321,9 @@ PLT_API plt_status plt_cache_evict_weights(plt_cache_evict_t h, const plt_cache_
     e.mc = (float2*)h->mc;
     e.weights_stride = ws;
     e.decay = a->decay;
+    CUtensorMap map;
     if (g.bf16) {
-        s = encode_keys(h, a->k_cache, sb, sn, sh, es, c.page_size > 0 ? a->num_pool_pages : a->batch, e.kbox);
+        s = encode_keys(h, &map, a->k_cache, sb, sn, sh, es, c.page_size > 0 ? a->num_pool_pages : a->batch, e.kbox);
         if (s != PLT_OK) return s;
     }
     Params& p = e.p;
@@ -358,7 +351,7 @@ PLT_API plt_status plt_cache_evict_weights(plt_cache_evict_t h, const plt_cache_
         p.page_table = c.page_size > 0 ? a->page_table + (int64_t)b0 * a->max_pages : nullptr;
         e.gate = a->gate_logits && c.L > 1 ? a->gate_logits + (int64_t)b0 * (c.L - 1) * g.Qn * c.Hq : nullptr;
         e.weights = a->weights + (int64_t)b0 * groups * ws;
-        cudaError_t err = g.bf16 ? launch_scores(g.v, h->map, e, h->score_grid, stream)
+        cudaError_t err = g.bf16 ? launch_scores(g.v, map, e, h->score_grid, stream)
                                  : launch_scores_f32(e, h->score_grid, h->score_smem, stream);
         if (err != cudaSuccess) return cuda_fail(h, "launching the scores kernel", err);
         err = launch_evict_add(e, h->add_grid, h->add_smem, stream);
@@ -379,9 +372,10 @@ PLT_API plt_status plt_cache_evict_select(plt_cache_evict_t h, const plt_cache_e
     if (a->new_lens == a->seq_lens) return fail(h, PLT_ERR_INVALID_ARG, "new_lens and seq_lens must be different buffers");
     if (a->budget < 1 || a->budget > c.max_seq_len)
         return fail(h, PLT_ERR_INVALID_ARG, "budget %d outside [1, max_seq_len %d]", a->budget, c.max_seq_len);
-    if (a->keep_first < 0 || a->keep_last < h->max_delta + h->g.Qn - 1 || (int64_t)a->keep_first + a->keep_last > a->budget)
-        return fail(h, PLT_ERR_INVALID_ARG, "keep_first %d, keep_last %d: not negative, keep_last >= %d, together <= budget %d", a->keep_first,
-                    a->keep_last, h->max_delta + h->g.Qn - 1, a->budget);
+    const int64_t least = (int64_t)h->max_delta + h->g.Qn - 1;   // positions that a row's cutoff counts from the end
+    if (a->keep_first < 0 || a->keep_last < least || (int64_t)a->keep_first + a->keep_last > a->budget)
+        return fail(h, PLT_ERR_INVALID_ARG, "keep_first %d, keep_last %d: not negative, keep_last >= %lld, together <= budget %d", a->keep_first,
+                    a->keep_last, (long long)least, a->budget);
     int64_t ws = a->weights_stride;
     s = check_totals(h, a->weights, ws);
     if (s != PLT_OK) return s;

@@ -1,7 +1,7 @@
-// C ABI of differential attention: one decode step and whole prompts. Both run on the kernels of the plain attention, which
-// take a query head as two packed rows (decode step: the halves of the row, the other half zero, so that one pass over a
-// cache row serves both maps) or as the two tiles of a block (prompt); what differs lies in their last step, where the two
-// maps of a head are joined (plt_reduce.cu, plt_seq_attn.cu). Here: argument checks and the parameters' struct.
+// C ABI of differential attention: one decode step and whole prompts. The decode step runs on the main kernels of the plain
+// attention, which take a query head as two packed rows (the halves of the row, the other half zero, so that one pass over a
+// cache row serves both maps), with a merge kernel of its own that joins the maps (plt_reduce.cu); prompts have a kernel of
+// their own (plt_diff_seq.cu). Here: argument checks and the parameters' struct.
 #include "../../include/plt_diff_attn.h"
 
 #include <cmath>

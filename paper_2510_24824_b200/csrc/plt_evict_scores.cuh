@@ -206,7 +206,7 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
 
             for (int t = pc.t0; t < pc.t1; ++t) {
                 if (ok) {
-                    ok = mbar_wait_bounded(&full_bar[stage], use & 1, kScoreWaitNs);
+                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&full_bar[stage], use & 1, kScoreWaitNs));   // what follows is the whole warp's
                     if (!ok) flags |= kDevWaitTimeout;
                 }
                 if (ok) {

@@ -32,11 +32,11 @@ def largest(a, scale=None):
 def map_error(dtype, max_v, d, max_q=0.0, max_k=0.0, e4m3_terms=False):
     """How far one map's result can be from the exact one. Weights p' = p (1 + delta), |delta| <= u, move the weighted mean
     of values of magnitude max_v by at most 2 u max_v (numerator and denominator one u each).
-    bf16: u = 2^-9 from rounding the weights; codes held as two E4M3 terms: 2^-8, to which the terms below the format's
-    smallest steps add less than as much again. The fp32 side: a dot product of d terms is off by at most
+    bf16: u = 2^-8 from rounding the weights, half a step; weights as two E4M3 terms: each leaves at most 2^-4 of what it holds,
+    2^-8 together, to which the terms below the format's smallest steps add less than as much again. The fp32 side: a dot product of d terms is off by at most
     d 2^-24 sum|q k| <= d 2^-24 d max|q| max|k|, scaled by 1/sqrt(d/2); its exponential by that much relatively, and
     exp2, the sums and the merge by some 2^-20."""
-    u = {"bf16": 2.0 ** -9, "f32": 0.0}[dtype] * (4.0 if e4m3_terms else 1.0)
+    u = {"bf16": 2.0 ** -8, "f32": 0.0}[dtype] * (2.0 if e4m3_terms else 1.0)
     u += d * 2.0 ** -24 * d * max_q * max_k / np.sqrt(d / 2.0) + 2.0 ** -20
     return 2.0 * u * max_v
 
