@@ -69,7 +69,7 @@ typedef struct {
  * with the cutoffs of plt_decode_attn_run (cut = max(0, N_b - delta_l - (q_len - 1 - token)); a position that a row does not
  * see gets nothing from it).  rho = 1, or, where gate_logits is given, 1 - sigmoid(gate) for the rows of loops 2..L: the
  * share that Eq. 2 gives the shared cache.  Scores, softmax and totals are fp32 (with E4M3 caches the products take the
- * queries in f16, which holds bf16 values exactly between 2^-14 and 65504).  The sums' order depends on nothing but the
+ * queries in f16, which holds bf16 values exactly between 2^-14 and 65504).  K rows that a query row sees have to be finite.  The sums' order depends on nothing but the
  * configuration and the lengths, so results repeat bit for bit.
  */
 typedef struct {

@@ -22,7 +22,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Scratch for scores: a batch whose scores at full length exceed this runs in several rounds of the three launches, each over a
+// Scratch for scores: a batch whose scores at full length exceed this runs in several rounds of launches, each over a
 // part of the batch. At 8 packed rows of d = 128 it holds the scores of 2 GB of keys. (Smaller parts, whose scores would stay in
 // L2, cost more than they save: 8 sequences of 32768 codes, 16 rows, 104 us in one round, 122 us in parts of 72 MB, 145 us of 36.)
 constexpr size_t kScoreScratch = (size_t)256 << 20;
@@ -68,6 +68,7 @@ plt_status cuda_fail(plt_cache_evict_t h, const char* what, cudaError_t e) {
 }
 
 int row_pitch(int rows) { return (rows + 3) & ~3; }
+int key_pitch(const EvictGeometry& g) { return g.v.twice ? g.v.RS : row_pitch(g.R); }
 
 plt_status check_config(const plt_cache_evict_config* c, EvictGeometry* g) {
     if (!c) return fail(nullptr, PLT_ERR_INVALID_ARG, "config is NULL");
@@ -106,10 +107,10 @@ plt_status check_config(const plt_cache_evict_config* c, EvictGeometry* g) {
         g->v = score_variant(c->d, g->R, c->Hkv, g->fp8, c->max_batch);
         if (g->v.smem > 227 * 1024) return fail(nullptr, PLT_ERR_UNSUPPORTED, "max_batch %d needs too much shared memory", c->max_batch);
     } else {
-        g->v = ScoreVariant{c->d, 0, 1, false, 1, 1, kEvictF32Keys, 0, scores_f32_smem(c->d, g->R, c->max_batch)};
+        g->v = ScoreVariant{c->d, 0, 1, 1, false, false, 1, 1, kEvictF32Keys, 0, scores_f32_smem(c->d, g->R, c->max_batch)};
     }
     const size_t tiles = ((size_t)c->max_seq_len + g->v.tile_keys - 1) / g->v.tile_keys + kEvictPieceCost;
-    const size_t per = tiles * g->v.tile_keys * c->Hkv * row_pitch(g->R);     // floats of a sequence's scores
+    const size_t per = tiles * g->v.tile_keys * c->Hkv * key_pitch(*g);       // floats of a sequence's scores or sums
     size_t part = kScoreScratch / 4 / per;
     part = part < 1 ? 1 : (part > (size_t)c->max_batch ? (size_t)c->max_batch : part);
     g->part = (int)part;
@@ -203,7 +204,7 @@ plt_status create_on_device(plt_cache_evict* h) {
     h->score_grid = h->sm_count * (blocks < most ? blocks : most);
     h->score_smem = g.v.smem;
     h->add_smem = evict_add_smem(c.max_batch);
-    e = evict_add_prepare(row_pitch(g.R), h->add_smem, &blocks);
+    e = evict_add_prepare(g.v.twice, key_pitch(g), h->add_smem, &blocks);
     if (e != cudaSuccess) return cuda_fail(nullptr, "preparing the add kernel", e);
     if (blocks < 1) return fail(nullptr, PLT_ERR_UNSUPPORTED, "the add kernel does not fit an SM");
     h->add_grid = h->sm_count * blocks;
@@ -313,6 +314,7 @@ PLT_API plt_status plt_cache_evict_weights(plt_cache_evict_t h, const plt_cache_
     if (c.page_size > 0)
         while (c.page_size % e.kbox != 0) e.kbox >>= 1;    // 16 divides every page
     e.row_pitch = row_pitch(g.R);
+    e.key_pitch = key_pitch(g);
     while ((1 << e.tile_shift) < g.v.tile_keys) ++e.tile_shift;
     e.hpg = g.hpg;
     e.min_delta = h->min_delta;
@@ -354,8 +356,12 @@ PLT_API plt_status plt_cache_evict_weights(plt_cache_evict_t h, const plt_cache_
         cudaError_t err = g.bf16 ? launch_scores(g.v, map, e, h->score_grid, stream)
                                  : launch_scores_f32(e, h->score_grid, h->score_smem, stream);
         if (err != cudaSuccess) return cuda_fail(h, "launching the scores kernel", err);
-        err = launch_evict_add(e, h->add_grid, h->add_smem, stream);
-        if (err != cudaSuccess) return cuda_fail(h, "launching the join and add kernels", err);
+        err = launch_evict_join(e, stream);
+        if (err != cudaSuccess) return cuda_fail(h, "launching the join kernel", err);
+        if (g.v.twice) err = launch_sums(g.v, map, e, h->score_grid, stream);
+        if (err != cudaSuccess) return cuda_fail(h, "launching the sums kernel", err);
+        err = launch_evict_add(e, g.v.twice, h->add_grid, h->add_smem, stream);
+        if (err != cudaSuccess) return cuda_fail(h, "launching the add kernel", err);
     }
     return PLT_OK;
 }

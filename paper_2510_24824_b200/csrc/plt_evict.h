@@ -5,21 +5,24 @@
 namespace plt {
 
 // ---- attention weights ------------------------------------------------------------------------------------------
-// The work of plt_cache_evict_weights is three kernels over one batch of sequences:
-//   scores  streams K once: scores of all packed rows (log2 units) into a scratch array, and for every row the maximum and
-//           the sum of exponentials over the block's piece of the keys
+// The work of plt_cache_evict_weights is three or four kernels over one batch of sequences:
+//   scores  streams K: for every packed row the maximum (log2 units) and the sum of exponentials over the block's piece of
+//           the keys; up to 16 rows also all scores into a scratch array
 //   join    joins the pieces' statistics
-//   add     adds 2^(score - max) * rho / sum over the rows of a head group to the totals
+//   sums    above 16 rows: streams K again and leaves 2^(score - max) * rho / sum added up over the rows in the scratch array
+//   add     up to 16 rows: adds 2^(score - max) * rho / sum over the rows of a head group to the totals; fold, above: adds
+//           up the sums of a head group
 struct EvictWeights {
     Params p;                  // plan, query rows, lengths, pages; w = 0, hpc and tile_keys of the scores kernel
     int32_t b0;                // first sequence of this launch (the pointers in p are shifted already, K's tensor map is not)
     int32_t kw;                // warps along the keys of a tile of the scores kernel (each leaves statistics of its own)
     int32_t kbox;              // keys per TMA box
-    int32_t row_pitch;         // floats between the scores of consecutive keys: rows rounded up to a multiple of four
+    int32_t row_pitch;         // rows rounded up to a multiple of four
+    int32_t key_pitch;         // floats of a key in the scratch: row_pitch scores, or (twice) sums over each share of the rows
     int32_t tile_shift;        // log2 of p.tile_keys
     int32_t hpg;               // KV heads of a group
     int32_t min_delta;         // smallest causal offset: positions below length - min_delta have scores
-    float* scores;             // [place on p's line][head of the tile][key][row_pitch]
+    float* scores;             // [place on p's line][head of the tile][key][key_pitch]
     float* ml;                 // [slot of p's plan][head][kw][R][2] maximum and sum of a piece
     float2* mc;                // [B][Hkv][row_pitch] maximum of a row and rho / sum (0 where there is no row or no key)
     float* weights;            // [B][Hkv / hpg] rows, weights_stride apart
@@ -40,22 +43,24 @@ constexpr int kEvictScoreTiles = 2;    // least tiles per block of the scores ke
 constexpr int kEvictPieceCost = 3;     // what starting and finishing an item costs a block of it, in tiles
 
 struct ScoreVariant {
-    int D, NT, HPC;        // head dim (elements), 8-row groups, KV heads per block
+    int D, NT, RS, HPC;    // head dim (elements), 8-row groups of a warp, warps that share the rows, KV heads per block
     bool fp8;
-    int KW, KS, tile_keys; // derived: HPC * KW = 4 consumer warps, KS 16-key slices each
+    bool twice;            // K is streamed twice (statistics, then sums) instead of leaving its scores in the scratch
+    int KW, KS, tile_keys; // derived: HPC * KW = 4 consumer warps for each share of the rows, KS 16-key slices each
     int stages;
     size_t smem;
 };
 ScoreVariant score_variant(int D, int R, int Hkv, bool fp8, int max_batch);
 cudaError_t scores_prepare(const ScoreVariant& v, int* blocks_per_sm);
 cudaError_t launch_scores(const ScoreVariant& v, const CUtensorMap& mapK, const EvictWeights& e, int grid, cudaStream_t stream);
+cudaError_t launch_sums(const ScoreVariant& v, const CUtensorMap& mapK, const EvictWeights& e, int grid, cudaStream_t stream);
 size_t scores_f32_smem(int D, int R, int max_batch);
 cudaError_t scores_f32_prepare(int D, int R, int max_batch, int* blocks_per_sm);
 cudaError_t launch_scores_f32(const EvictWeights& e, int grid, size_t smem, cudaStream_t stream);
+cudaError_t launch_evict_join(const EvictWeights& e, cudaStream_t stream);
 size_t evict_add_smem(int max_batch);
-cudaError_t evict_add_prepare(int row_pitch, size_t smem, int* blocks_per_sm);
-cudaError_t launch_evict_add(   // join and add
-    const EvictWeights& e, int grid, size_t smem, cudaStream_t stream);
+cudaError_t evict_add_prepare(bool twice, int key_pitch, size_t smem, int* blocks_per_sm);
+cudaError_t launch_evict_add(const EvictWeights& e, bool twice, int grid, size_t smem, cudaStream_t stream);
 
 // ---- selection ----------------------------------------------------------------------------------------------------
 struct SelectParams {

@@ -1,15 +1,20 @@
 // Scores kernel of the attention-weight totals (plt_cache_evict_weights), caches of bf16 values or E4M3 codes.
 //
-// The total of a key needs every row's softmax denominator over the whole cache before its first weight is known, so K
-// would be streamed twice: once for the denominators, once for the weights. A row's score of a key is 4 bytes where the
-// key's row of K is 2 d: with R packed rows the scores are 4 R / (2 d) of K (an eighth at 8 rows of d = 128). So this
-// kernel streams K once, by TMA into a shared-memory ring like the decode step's main kernel, and leaves the scores in a
-// scratch array that the second kernel reads back, for the most part from L2. Bound: HBM (K once) and L2.
+// The total of a key needs every row's softmax denominator over the whole cache before its first weight is known. Up to 16
+// packed rows this kernel streams K once, by TMA into a shared-memory ring like the decode step's main kernel, and leaves every
+// score in a scratch array (kScoreDump), from which the add kernel makes the weights, once the pieces' statistics are joined:
+// a row's score of a key is 4 bytes where the key's row of K is 2 d. With more rows the scratch would cost more than K, so K is
+// streamed twice, first for the statistics (kScoreStats), then for the sums of the weights over the rows (kScoreSums: one float
+// a key and share of the rows); the rule stands at score_variant. Bound: HBM (K); with E4M3 codes above 16 rows the
+// conversions of the codes, which every share of the rows repeats.
+// Measured: 8 rows, 64 ragged sequences of up to 8192 keys, 8 KV heads of 128 bf16 (284 MB of K): 52 us for this kernel, 65
+// for the call; 32 rows there: 110 us, 64 rows 165. 16 rows, 8 x 32768 E4M3 codes in pages of 64: 67 us, the call 104.
 //
-// One producer warp; HPC * KW = 4 consumer warps, each with KS 16-key slices of a tile for one KV head and all packed rows:
-// S^T [16 keys x 8 NT] = K_slice . Q^T with the keys as the M dimension of mma.sync, K fragments by ldmatrix from the
-// swizzled tile, query rows in registers. Row statistics are kept by each thread for its own keys (an online softmax with a
-// reference that moves only when a score exceeds it by more than 2^8, no shuffles) and joined once per piece.
+// One producer warp; consumer warps in RS shares of the rows of four warps each. HPC * KW = 4 warps, each with KS 16-key slices
+// of a tile for one KV head and the share's packed rows: S^T [16 keys x 8 NT] = K_slice . Q^T with the keys as the M dimension
+// of mma.sync, K fragments by ldmatrix from the swizzled tile, query rows in registers. Row statistics are kept by each thread
+// for its own keys (an online softmax with a reference that moves only when a score exceeds it by more than 2^8, no shuffles)
+// and joined once per piece.
 #pragma once
 #include <cuda_bf16.h>
 
@@ -23,14 +28,19 @@ constexpr uint64_t kScoreWaitNs = 2000000000ull;
 constexpr float kScoreSlack = 8.f;
 constexpr float kScoreNoMax = -1e30f;
 
-template <int D, int NT, int HPC, bool FP8>
+// What a pass over K leaves: every score and the row statistics; the statistics alone; or, with the joined statistics at
+// hand, the weights of every key summed over the rows.
+enum ScoreMode { kScoreDump, kScoreStats, kScoreSums };
+
+template <int D, int NT, int RS, int HPC, bool FP8>
 struct ScoreCfg {
     static constexpr int ES = FP8 ? 1 : 2;
     static constexpr int NH = D * ES / 128;            // 128-byte pieces of a head row
     static constexpr int KW = 4 / HPC;                 // warps along the keys
-    static constexpr int KS = NT <= 4 ? 2 : 1;         // 16-key slices per warp; above 32 rows one, for registers
+    static constexpr int KS = 2;                       // 16-key slices per warp
     static constexpr int TK = 16 * KW * KS;
-    static constexpr int NTHREADS = 5 * 32;
+    static constexpr int CONSUMERS = 4 * RS;           // warps
+    static constexpr int NTHREADS = (CONSUMERS + 1) * 32;
     static constexpr int PIECE_BYTES = 128 * TK * HPC; // one 128-byte piece of all rows of a tile
     static constexpr int STAGE_BYTES = NH * PIECE_BYTES;
     static constexpr int kMaxStages = 8;
@@ -39,10 +49,10 @@ struct ScoreCfg {
     }
 };
 
-template <int D, int NT, int HPC, bool FP8>
-__global__ void __launch_bounds__(ScoreCfg<D, NT, HPC, FP8>::NTHREADS, NT <= 4 ? 2 : 1)   // above 32 rows the query fragments take the registers
+template <int D, int NT, int RS, int HPC, bool FP8, int MODE>
+__global__ void __launch_bounds__(ScoreCfg<D, NT, RS, HPC, FP8>::NTHREADS, NT * RS <= 4 ? 2 : 1)
 plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ EvictWeights e, const int stages) {
-    using C = ScoreCfg<D, NT, HPC, FP8>;
+    using C = ScoreCfg<D, NT, RS, HPC, FP8>;
     const Params& p = e.p;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -60,7 +70,7 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         s_ctl[1] = 0;
         for (int s = 0; s < stages; ++s) {
             mbar_init(&full_bar[s], 1);
-            mbar_init(&empty_bar[s], 4);
+            mbar_init(&empty_bar[s], C::CONSUMERS);
         }
         mbar_fence_init();
     }
@@ -73,7 +83,7 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     const bool in_plan = cta < nctas;
     const int64_t lo = in_plan ? cta_begin(T, cta, nctas) : 0, hi = in_plan ? cta_begin(T, cta + 1, nctas) : 0;
 
-    if (wid == 4) {
+    if (wid == C::CONSUMERS) {
         // =========================== producer warp (one lane issues) ==============================
         if (lane == 0 && lo < hi) {
             tma_prefetch_desc(&tmK);
@@ -122,7 +132,8 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         }
     } else {
         // ================================= consumer warps =========================================
-        const int h_local = wid / C::KW, kw = wid % C::KW;
+        const int slot4 = wid & 3, h_local = slot4 / C::KW, kw = slot4 % C::KW;
+        const int rs = wid >> 2, rb = rs * NT * 8;   // this warp's rows: rb .. rb + 8 NT
         const int grp = lane >> 2, tq = lane & 3;
         const __nv_bfloat16* qg = (const __nv_bfloat16*)p.q;
         int lc[NT][2];   // loop of the row in the low byte (kMaxLoops: no row), newer tokens of the step above it
@@ -130,7 +141,7 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int r = nt * 8 + 2 * tq + j;
+                const int r = rb + nt * 8 + 2 * tq + j;
                 const int lq = r / p.G;
                 lc[nt][j] = r < p.R ? (lq / p.Qn) | ((p.Qn - 1 - lq % p.Qn) << 8) : kMaxLoops;
             }
@@ -157,7 +168,7 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
                 q_hg = pc.hg;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const int r = nt * 8 + grp;
+                    const int r = rb + nt * 8 + grp;
                     const bool v = r < p.R;
                     const int lq = v ? r / p.G : 0;
                     const int64_t head_row = ((int64_t)pc.b * p.L * p.Qn + lq) * p.Hq + kvh * p.G + (v ? r - lq * p.G : 0);
@@ -180,6 +191,24 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
                     }
                 }
             }
+            float mref[NT][2], lsum[NT][2];   // reference and sum of the rows; kScoreSums: what the join left
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                mref[nt][0] = mref[nt][1] = kScoreNoMax;
+                lsum[nt][0] = lsum[nt][1] = 0.f;
+            }
+            if constexpr (MODE == kScoreSums) {   // rows of the joined statistics lie as far apart as there are, rounded up to four
+                const float2* mc = e.mc + ((int64_t)pc.b * p.Hkv + kvh) * e.row_pitch;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int r = rb + nt * 8 + 2 * tq + j;
+                        const float2 c = r < p.R ? mc[r] : make_float2(INFINITY, 0.f);
+                        mref[nt][j] = c.x;
+                        lsum[nt][j] = c.y;
+                    }
+            }
             int cutr[NT][2], cmin = 0x7fffffff;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) cutr[nt][0] = cutr[nt][1] = 0;
@@ -194,12 +223,6 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
                         for (int j = 0; j < 2; ++j)
                             if ((lc[nt][j] & 0xff) == l) cutr[nt][j] = max(c - (lc[nt][j] >> 8), 0);
                 }
-            float mref[NT][2], lsum[NT][2];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                mref[nt][0] = mref[nt][1] = kScoreNoMax;
-                lsum[nt][0] = lsum[nt][1] = 0.f;
-            }
             const float sc2 = FP8 ? p.scale_log2 * p.k_scale[kvh] : p.scale_log2;
             // the item's first tile on the line, behind its lead-in (whose places in the scratch stay empty)
             const int64_t tile0 = (int64_t)s_prefix[pc.b] + (int64_t)pc.hg * line_len(p, pc.sp.gt) + p.piece_cost;
@@ -247,7 +270,10 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
                     if (lane == 0) mbar_arrive(&empty_bar[stage]);   // the tile is in registers: the slot may be refilled
                     const int key0 = t * C::TK + kw * C::KS * 16 + grp;   // this thread's keys: key0 + 16 ki (+ 8)
                     const bool masked = t * C::TK + C::TK > cmin;
-                    float* dst = e.scores + (((tile0 + t) * HPC + h_local) * C::TK + kw * C::KS * 16 + grp) * (int64_t)e.row_pitch + 2 * tq;
+                    float* dst = e.scores + (((tile0 + t) * HPC + h_local) * C::TK + kw * C::KS * 16 + grp) * (int64_t)e.key_pitch + (MODE == kScoreSums ? rs : rb + 2 * tq);
+                    float total[C::KS][2];
+#pragma unroll
+                    for (int ki = 0; ki < C::KS; ++ki) total[ki][0] = total[ki][1] = 0.f;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -262,22 +288,41 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
                                     s[ki][nt][2 * u + j] = x;
                                     mx = fmaxf(mx, x);
                                 }
-                            if (mx - mref[nt][j] > kScoreSlack) {
-                                lsum[nt][j] *= fast_exp2(mref[nt][j] - mx);
-                                mref[nt][j] = mx;
-                            }
+                            if constexpr (MODE == kScoreSums) {
 #pragma unroll
-                            for (int ki = 0; ki < C::KS; ++ki)
-                                lsum[nt][j] += fast_exp2(s[ki][nt][j] - mref[nt][j]) + fast_exp2(s[ki][nt][2 + j] - mref[nt][j]);
+                                for (int ki = 0; ki < C::KS; ++ki)
+#pragma unroll
+                                    for (int u = 0; u < 2; ++u)
+                                        total[ki][u] = fmaf(fast_exp2(s[ki][nt][2 * u + j] - mref[nt][j]), lsum[nt][j], total[ki][u]);
+                            } else {
+                                if (mx - mref[nt][j] > kScoreSlack) {
+                                    lsum[nt][j] *= fast_exp2(mref[nt][j] - mx);
+                                    mref[nt][j] = mx;
+                                }
+#pragma unroll
+                                for (int ki = 0; ki < C::KS; ++ki)
+                                    lsum[nt][j] += fast_exp2(s[ki][nt][j] - mref[nt][j]) + fast_exp2(s[ki][nt][2 + j] - mref[nt][j]);
+                            }
                         }
-                        if (nt * 8 + 2 * tq < e.row_pitch) {   // behind the last row: finite, or -inf
+                        if (MODE == kScoreDump && rb + nt * 8 + 2 * tq < e.key_pitch) {   // behind the last row: finite, or -inf
 #pragma unroll
                             for (int ki = 0; ki < C::KS; ++ki)
 #pragma unroll
                                 for (int u = 0; u < 2; ++u)
-                                    *(float2*)(dst + (int64_t)(16 * ki + 8 * u) * e.row_pitch + nt * 8) =
+                                    *(float2*)(dst + (int64_t)(16 * ki + 8 * u) * e.key_pitch + nt * 8) =
                                         make_float2(s[ki][nt][2 * u], s[ki][nt][2 * u + 1]);
                         }
+                    }
+                    if constexpr (MODE == kScoreSums) {   // the four threads that share a key
+#pragma unroll
+                        for (int ki = 0; ki < C::KS; ++ki)
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                float x = total[ki][u];
+                                x += __shfl_xor_sync(0xffffffffu, x, 1);
+                                x += __shfl_xor_sync(0xffffffffu, x, 2);
+                                if (tq == ((2 * ki + u) & 3)) dst[(16 * ki + 8 * u) * RS] = x;
+                            }
                     }
                 } else {
                     __syncwarp();
@@ -288,6 +333,7 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
                     ++use;
                 }
             }
+            if constexpr (MODE == kScoreSums) continue;
             // ---- end of piece: the eight threads that share a row join their statistics --------------
             const int64_t slot = slot_of(item_index(p, pc.b, pc.hg, 0), cta);
             if (tid == 0) note_piece(p, pc, cta);
@@ -304,7 +350,7 @@ plt_evict_scores(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
                         m = mm;
                     }
                     if (grp == 0 && lc[nt][j] != kMaxLoops) {
-                        const int64_t row = ((slot * HPC + h_local) * C::KW + kw) * p.R + nt * 8 + 2 * tq + j;
+                        const int64_t row = ((slot * HPC + h_local) * C::KW + kw) * p.R + rb + nt * 8 + 2 * tq + j;
                         *(float2*)(e.ml + row * 2) = make_float2(m, l);
                     }
                 }

@@ -1,21 +1,22 @@
 // The rest of plt_cache_evict_weights: choice of the scores kernel's variant, the scores kernel for fp32 caches, and the
-// kernel that turns scores into weights and adds them up.
+// kernels that join the pieces' statistics, turn scores into weights and add them up.
 #include "plt_common.cuh"
 #include "plt_evict.h"
+#include "plt_evict_scores.cuh"
 #include "plt_ptx.cuh"
 
 namespace plt {
 
-cudaError_t scores_bf16_d128(int op, const ScoreVariant&, const CUtensorMap*, const EvictWeights*, int, cudaStream_t, int*);
-cudaError_t scores_bf16_d64(int op, const ScoreVariant&, const CUtensorMap*, const EvictWeights*, int, cudaStream_t, int*);
-cudaError_t scores_e4m3(int op, const ScoreVariant&, const CUtensorMap*, const EvictWeights*, int, cudaStream_t, int*);
+cudaError_t scores_bf16_d128(int op, int mode, const ScoreVariant&, const CUtensorMap*, const EvictWeights*, int, cudaStream_t, int*);
+cudaError_t scores_bf16_d64(int op, int mode, const ScoreVariant&, const CUtensorMap*, const EvictWeights*, int, cudaStream_t, int*);
+cudaError_t scores_e4m3(int op, int mode, const ScoreVariant&, const CUtensorMap*, const EvictWeights*, int, cudaStream_t, int*);
 
 namespace {
 
-cudaError_t score_dispatch(int op, const ScoreVariant& v, const CUtensorMap* map, const EvictWeights* e, int grid, cudaStream_t stream,
-                           int* out) {
-    if (v.fp8) return scores_e4m3(op, v, map, e, grid, stream, out);
-    return v.D == 128 ? scores_bf16_d128(op, v, map, e, grid, stream, out) : scores_bf16_d64(op, v, map, e, grid, stream, out);
+cudaError_t score_dispatch(int op, int mode, const ScoreVariant& v, const CUtensorMap* map, const EvictWeights* e, int grid,
+                           cudaStream_t stream, int* out) {
+    if (v.fp8) return scores_e4m3(op, mode, v, map, e, grid, stream, out);
+    return v.D == 128 ? scores_bf16_d128(op, mode, v, map, e, grid, stream, out) : scores_bf16_d64(op, mode, v, map, e, grid, stream, out);
 }
 
 // ---- fp32 caches --------------------------------------------------------------------------------------------------
@@ -237,16 +238,12 @@ constexpr int kAddThreads = 256;
 constexpr int kAddRun = 128;                              // keys of a warp
 constexpr int kAddBatch = 8;                              // loads in flight per lane
 
-template <int LPK>
-__global__ void __launch_bounds__(kAddThreads, 3) plt_evict_add(const __grid_constant__ EvictWeights e) {
+// Lengths, the line of the scores plan and this kernel's own line (runs of kAddRun keys of every head group) into shared
+// memory; the latter's length. Waits for the kernel before. `tiles`: [B + 1], behind it `line` [B + 1] and `lens` [B].
+__device__ __forceinline__ int add_plan(const EvictWeights& e, int32_t* s_tiles, uint32_t& flags) {
     const Params& p = e.p;
-    extern __shared__ int32_t smem_i[];
-    const int groups = p.Hkv / e.hpg;
-    int32_t* s_tiles = smem_i;                            // [B + 1] line of the scores plan
-    int32_t* s_line = s_tiles + p.B + 1;                  // [B + 1] line of this kernel: runs of kAddRun keys of every head group
-    int32_t* s_lens = s_line + p.B + 1;                   // [B]
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    uint32_t flags = 0;
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, groups = p.Hkv / e.hpg;
+    int32_t *s_line = s_tiles + p.B + 1, *s_lens = s_line + p.B + 1;
     for (int b = tid; b < p.B; b += kAddThreads) {
         const int n = seq_len_clamped(p, b, flags);
         s_lens[b] = n;
@@ -271,8 +268,18 @@ __global__ void __launch_bounds__(kAddThreads, 3) plt_evict_add(const __grid_con
     }
     __syncthreads();
     grid_dependency_wait();
-    const int T = s_line[p.B];
-    const int64_t head = (int64_t)e.row_pitch << e.tile_shift;              // scores of a head's part of a tile
+    return s_line[p.B];
+}
+
+template <int LPK>
+__global__ void __launch_bounds__(kAddThreads, 3) plt_evict_add(const __grid_constant__ EvictWeights e) {
+    const Params& p = e.p;
+    extern __shared__ int32_t smem_i[];
+    const int groups = p.Hkv / e.hpg, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int32_t *s_tiles = smem_i, *s_line = s_tiles + p.B + 1, *s_lens = s_line + p.B + 1;
+    uint32_t flags = 0;
+    const int T = add_plan(e, smem_i, flags);
+    const int64_t head = (int64_t)e.key_pitch << e.tile_shift;              // scores of a head's part of a tile
     // from the line's end: part of what the scores kernel wrote last is still in L2 (8 sequences of 32768 codes, 16 rows: 91
     // instead of 104 MB of the 134 read from HBM, the call 104 instead of 108 us)
     for (int pos = T - 1 - (int)(blockIdx.x * (kAddThreads / 32) + wid); pos >= 0; pos -= gridDim.x * (kAddThreads / 32)) {
@@ -332,39 +339,108 @@ __global__ void __launch_bounds__(kAddThreads, 3) plt_evict_add(const __grid_con
     if (flags) atomicOr(p.status, flags);
 }
 
+// After two passes over K: the sums over the rows are there for every KV head and key, and only the heads of a group and the
+// old totals are left to add.
+__global__ void __launch_bounds__(kAddThreads) plt_evict_fold(const __grid_constant__ EvictWeights e) {
+    const Params& p = e.p;
+    extern __shared__ int32_t smem_i[];
+    const int groups = p.Hkv / e.hpg, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int32_t *s_tiles = smem_i, *s_line = s_tiles + p.B + 1, *s_lens = s_line + p.B + 1;
+    uint32_t flags = 0;
+    const int T = add_plan(e, smem_i, flags);
+    constexpr int U = kAddRun / 32;
+    for (int pos = blockIdx.x * (kAddThreads / 32) + wid; pos < T; pos += gridDim.x * (kAddThreads / 32)) {
+        const int b = find_seq(s_line, p.B, pos);
+        const int n = s_lens[b], runs = (n + kAddRun - 1) / kAddRun;
+        const int o = pos - s_line[b], g = o / runs, k0 = (o - g * runs) * kAddRun + lane;
+        const int gt = scored_tiles(e, n), scored = gt << e.tile_shift;
+        float* w = e.weights + ((int64_t)b * groups + g) * e.weights_stride;
+        const int64_t head = (int64_t)e.key_pitch << e.tile_shift, line = (int64_t)line_len(p, gt) * p.hpc * head;
+        const float* first = e.scores + ((int64_t)s_tiles[b] + p.piece_cost) * p.hpc * head;
+        float acc[U], old[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int key = k0 + 32 * u;
+            acc[u] = 0.f;
+            old[u] = e.decay != 0.f && key < n ? w[key] : 0.f;
+        }
+        for (int h = g * e.hpg; h < (g + 1) * e.hpg; ++h) {
+            const int hg = h / p.hpc, hl = h - hg * p.hpc;
+            const float* s = first + hg * line + hl * head;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int key = k0 + 32 * u;
+                if (key >= scored || key >= n) continue;
+                const float* parts = s + ((int64_t)(key >> e.tile_shift) * ((p.hpc - 1) << e.tile_shift) + key) * e.key_pitch;
+                if (e.key_pitch == 1) acc[u] += parts[0];
+                else if (e.key_pitch == 2) {
+                    const float2 v = *(const float2*)parts;
+                    acc[u] += v.x + v.y;
+                } else {
+                    const float4 v = *(const float4*)parts;
+                    acc[u] += (v.x + v.y) + (v.z + v.w);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int key = k0 + 32 * u;
+            if (key < n) w[key] = e.decay != 0.f ? fmaf(e.decay, old[u], acc[u]) : acc[u];
+        }
+    }
+    if (flags) atomicOr(p.status, flags);
+}
+
 }  // namespace
 
 ScoreVariant score_variant(int D, int R, int Hkv, bool fp8, int max_batch) {
     ScoreVariant v;
     v.D = D;
     v.fp8 = fp8;
-    const int nt = (R + 7) / 8;
-    v.NT = nt <= 2 ? nt : (nt <= 4 ? 4 : 8);
+    // Above 16 rows K is streamed twice: the scores' way through the scratch (4 R bytes a key, written and read) costs more than
+    // K's rows again. Once / twice, bf16, 64 ragged sequences: 8 rows 65 / 100 us, 16 rows 97 / 103, 24 rows 120 / 109, 32 rows
+    // 157 / 110; E4M3, 8 x 32768: 16 rows 103 / 99, 20 rows 153 / 163, 28 rows 177 / 164, 32 rows 203 / 164. 64 rows, once with
+    // 64 rows in a warp / twice with 16: bf16 423 / 165, E4M3 519 / 287.
+    v.twice = R > 16;
+    // At most 16 rows in a warp, so that 8 or 16 warps of an SM hold their queries in registers (64 rows, 32 / 16 in a warp: bf16
+    // 180 / 165 us, E4M3 318 / 287).
+    v.NT = R <= 8 ? 1 : 2;
+    v.RS = R <= 16 ? 1 : (R <= 32 ? 2 : 4);
     v.HPC = Hkv % 4 == 0 ? 4 : (Hkv % 2 == 0 ? 2 : 1);
     v.KW = 4 / v.HPC;
-    v.KS = v.NT <= 4 ? 2 : 1;
+    v.KS = 2;
     v.tile_keys = 16 * v.KW * v.KS;
     // two blocks per SM, at most 64 KB of loads in flight each (more only delays the first data)
     v.stages = 8;
     for (; v.stages > 2; --v.stages) {
         int bytes = 0;
-        score_dispatch(0, v, nullptr, nullptr, max_batch, nullptr, &bytes);
+        score_dispatch(0, v.twice ? kScoreStats : kScoreDump, v, nullptr, nullptr, max_batch, nullptr, &bytes);
         v.smem = (size_t)bytes;
         const size_t ring = (size_t)v.stages * v.HPC * v.tile_keys * D * (fp8 ? 1 : 2);
         if (ring <= 64 * 1024 && v.smem <= 110 * 1024) return v;
     }
     int bytes = 0;
-    score_dispatch(0, v, nullptr, nullptr, max_batch, nullptr, &bytes);
+    score_dispatch(0, v.twice ? kScoreStats : kScoreDump, v, nullptr, nullptr, max_batch, nullptr, &bytes);
     v.smem = (size_t)bytes;
     return v;
 }
 
 cudaError_t scores_prepare(const ScoreVariant& v, int* blocks_per_sm) {
-    return score_dispatch(1, v, nullptr, nullptr, 0, nullptr, blocks_per_sm);
+    if (!v.twice) return score_dispatch(1, kScoreDump, v, nullptr, nullptr, 0, nullptr, blocks_per_sm);
+    int stats = 0;
+    const cudaError_t err = score_dispatch(1, kScoreStats, v, nullptr, nullptr, 0, nullptr, &stats);
+    if (err != cudaSuccess) return err;
+    const cudaError_t err2 = score_dispatch(1, kScoreSums, v, nullptr, nullptr, 0, nullptr, blocks_per_sm);
+    if (stats < *blocks_per_sm) *blocks_per_sm = stats;
+    return err2;
 }
 
 cudaError_t launch_scores(const ScoreVariant& v, const CUtensorMap& mapK, const EvictWeights& e, int grid, cudaStream_t stream) {
-    return score_dispatch(2, v, &mapK, &e, grid, stream, nullptr);
+    return score_dispatch(2, v.twice ? kScoreStats : kScoreDump, v, &mapK, &e, grid, stream, nullptr);
+}
+
+cudaError_t launch_sums(const ScoreVariant& v, const CUtensorMap& mapK, const EvictWeights& e, int grid, cudaStream_t stream) {
+    return score_dispatch(2, kScoreSums, v, &mapK, &e, grid, stream, nullptr);
 }
 
 size_t scores_f32_smem(int D, int R, int max_batch) {
@@ -404,27 +480,30 @@ size_t evict_add_smem(int max_batch) { return (size_t)(3 * max_batch + 4) * 4; }
 namespace {
 // lanes per key: four rows each, a power of two
 template <typename F>
-cudaError_t with_lanes(int row_pitch, F&& f) {
-    if (row_pitch <= 4) return f(plt_evict_add<1>);
-    if (row_pitch <= 8) return f(plt_evict_add<2>);
-    if (row_pitch <= 16) return f(plt_evict_add<4>);
-    if (row_pitch <= 32) return f(plt_evict_add<8>);
+cudaError_t with_lanes(bool twice, int key_pitch, F&& f) {
+    if (twice) return f(plt_evict_fold);
+    if (key_pitch <= 4) return f(plt_evict_add<1>);
+    if (key_pitch <= 8) return f(plt_evict_add<2>);
+    if (key_pitch <= 16) return f(plt_evict_add<4>);
+    if (key_pitch <= 32) return f(plt_evict_add<8>);
     return f(plt_evict_add<16>);
 }
 }  // namespace
 
-cudaError_t evict_add_prepare(int row_pitch, size_t smem, int* blocks_per_sm) {
-    return with_lanes(row_pitch, [&](auto fn) {
+cudaError_t evict_add_prepare(bool twice, int key_pitch, size_t smem, int* blocks_per_sm) {
+    return with_lanes(twice, key_pitch, [&](auto fn) {
         const cudaError_t err = allow_max_dynamic_smem((const void*)fn);
         return err != cudaSuccess ? err : cudaOccupancyMaxActiveBlocksPerMultiprocessor(blocks_per_sm, fn, kAddThreads, smem);
     });
 }
 
-cudaError_t launch_evict_add(const EvictWeights& e, int grid, size_t smem, cudaStream_t stream) {
+cudaError_t launch_evict_join(const EvictWeights& e, cudaStream_t stream) {
     const int warps = e.p.B * e.p.Hkv * ((e.p.R + kJoinRows - 1) / kJoinRows);
-    const cudaError_t err = launch_overlapped(plt_evict_join, e, (warps + kJoinThreads / 32 - 1) / (kJoinThreads / 32), kJoinThreads, 0, stream);
-    if (err != cudaSuccess) return err;
-    return with_lanes(e.row_pitch, [&](auto fn) { return launch_overlapped(fn, e, grid, kAddThreads, smem, stream); });
+    return launch_overlapped(plt_evict_join, e, (warps + kJoinThreads / 32 - 1) / (kJoinThreads / 32), kJoinThreads, 0, stream);
+}
+
+cudaError_t launch_evict_add(const EvictWeights& e, bool twice, int grid, size_t smem, cudaStream_t stream) {
+    return with_lanes(twice, e.key_pitch, [&](auto fn) { return launch_overlapped(fn, e, grid, kAddThreads, smem, stream); });
 }
 
 }  // namespace plt

@@ -152,6 +152,47 @@ def test_weights_strided_cache():
     assert torch.equal(dense, strided)
 
 
+def test_weights_of_many_rows_in_parts_of_the_batch():
+    """64 rows a head: a handle whose capacity makes it take the batch in parts, against one that takes it whole."""
+    p = problem(B=7, Hq=128, Hkv=4, page_size=64, lens=("list", [300, 77, 0, 5, 300, 1, 222]))
+    cap = 1 << 21
+    config = B.make_evict_config("bf16", p.B, p.L, p.Hq, p.Hkv, p.d, cap, p.page_size)
+    assert B.plt_cache_evict_workspace_bytes(config) < p.B * cap * p.Hkv * 4 * 4
+    q = f32_to_bf16_bits(np.random.default_rng(6).standard_normal((p.B, p.L, 1, p.Hq, p.d)).astype(np.float32))
+    dp, dq = DeviceProblem(p, "cuda:0"), to_torch(q, "bf16", "cuda:0")
+    gate = dp.gate_logits.view(p.B, p.L - 1, 1, p.Hq)
+    whole, parts = torch.zeros(p.B, p.Hkv, p.max_seq_len, device="cuda"), torch.zeros(p.B, p.Hkv, cap, device="cuda")
+    with CacheEvict(p) as op:
+        op.weights(dp, dq, whole, gate_logits=gate)
+        assert op.check() == 0
+    table = torch.zeros(p.B, cap // p.page_size, dtype=torch.int32, device="cuda")
+    table[:, : p.max_pages] = dp.page_table
+    h = B.plt_cache_evict_create(config)
+    try:
+        a = B.make_evict_weights_args(p.B, dq, dp.k_cache, dp.seq_lens, parts, gate_logits=gate, page_table=table, max_pages=table.shape[1],
+                                      num_pool_pages=p.num_pool_pages, weights_stride=cap)
+        stream = torch.cuda.current_stream().cuda_stream
+        B.plt_cache_evict_weights(h, a, stream)
+        assert B.plt_cache_evict_check(h, stream) == 0
+    finally:
+        B.plt_cache_evict_destroy(h)
+    n = p.max_seq_len
+    assert not parts[:, :, n:].any() and torch.allclose(parts[:, :, :n], whole, rtol=2e-5, atol=1e-8)
+    # a row's weights add up to its share of the gate
+    live = (dp.seq_lens > 1).float()
+    rho = (1 - torch.sigmoid(gate.double())).view(p.B, p.Hkv, -1).sum(-1) + p.Hq // p.Hkv
+    assert torch.allclose(whole.double().sum(-1)[live > 0], rho[live > 0], rtol=1e-5)
+
+
+@pytest.mark.parametrize("Hq,L,q_len,maps", [(17, 1, 1, 1), (12, 2, 1, 1), (8, 2, 2, 1), (33, 1, 1, 1), (24, 2, 1, 1), (8, 2, 2, 2), (64, 1, 1, 1)])
+@pytest.mark.parametrize("kv,d", [("", 64), ("", 128), ("e4m3", 128)])
+@pytest.mark.parametrize("heads,group,page", [(1, 1, 0), (2, 2, 64), (8, 1, 32), (8, 8, 0)])
+def test_weights_above_sixteen_rows(Hq, L, q_len, maps, kv, d, heads, group, page):
+    """Every share of the rows full, begun and empty, and heads of a group in one block and in several."""
+    check_weights(problem(Hq=Hq * heads, Hkv=heads, L=L, d=d, kv_dtype=kv, page_size=page, lens=("list", [700, 33, 2])), q_len=q_len, maps=maps,
+                  group=group, decay=0.5)
+
+
 # ---- select -------------------------------------------------------------------------------------------------------
 def check_select(w, lens, budget, first=0, last=1, stride=0):
     Bn, groups, N = w.shape
