@@ -423,7 +423,7 @@ PLT_API plt_status plt_cache_evict_compact(plt_cache_evict_t h, const plt_cache_
     const CompactParams p = {(char*)a->k_cache, (char*)a->v_cache, sb * es, sn * es, sh * es, a->page_table, a->seq_lens, a->keep,
                              a->new_lens, a->weights, ws, h->status, c.Hkv, h->g.hpg, c.d * es, c.max_seq_len, c.page_size, shift,
                              a->max_pages, a->num_pool_pages, a->keep_stride};
-    const cudaError_t err = launch_compact(p, a->batch, h->sm_count, (cudaStream_t)cuda_stream);
+    const cudaError_t err = launch_compact(p, a->batch, (cudaStream_t)cuda_stream);
     if (err != cudaSuccess) return cuda_fail(h, "launching the compaction kernel", err);
     return PLT_OK;
 }

@@ -85,6 +85,6 @@ struct CompactParams {
     int32_t Hkv, hpg, row_bytes, max_seq_len, page_size, page_shift /* log2 of a page that is a power of two, else -1 */;
     int32_t max_pages, num_pool_pages, keep_stride;
 };
-cudaError_t launch_compact(const CompactParams& p, int batch, int sm_count, cudaStream_t stream);
+cudaError_t launch_compact(const CompactParams& p, int batch, cudaStream_t stream);
 
 }  // namespace plt

@@ -8,8 +8,11 @@
 // a 64-byte piece of the rows of one (sequence, head, K or V). The chain position -> page id -> row is taken apart: one thread
 // per row works out the next chunk's addresses into shared memory while the rows of the current one are under way, from
 // positions it fetched a chunk earlier. (Every thread working out the addresses of the rows it moves, 4 lanes to a row, took
-// 2.1x the time on pages of 64 tokens: integer divisions.) Blocks of 256 threads move 512 rows a chunk; where the batch has
-// no more blocks than SMs, blocks of 1024 threads move 1024 (one sequence: 1024 kept rows in a single chunk).
+// 2.1x the time on pages of 64 tokens: integer divisions.) A chunk is 512 rows.
+//
+// Bound: HBM, reads and writes mixed: 64 sequences of 8192, 4096 kept, 8 heads of 128 bf16: 390 us, 0.87 of the copy rate; ragged
+// lengths, half of which keep everything: 82 us, 0.70. One sequence of 5000, 1024 kept: 8.3 us, the chain lengths -> positions ->
+// pages -> rows. (Blocks of 1024 threads with 1024 rows a chunk: 8.6 there, 468 us on the full batch.)
 #include "plt_common.cuh"
 #include "plt_evict.h"
 #include "plt_ptx.cuh"
@@ -66,9 +69,11 @@ __device__ __forceinline__ int64_t row_offset(const CompactParams& p, const int3
     return (int64_t)clamp_page(p, pages[page], flags) * p.stride_b + (int64_t)(pos - page * p.page_size) * p.stride_n;
 }
 
-template <int THREADS, int U>
-__global__ void __launch_bounds__(THREADS) plt_evict_compact_kernel(const __grid_constant__ CompactParams p, const int pieces,
-                                                                    const int row_blocks) {
+constexpr int kMoveThreads = 256;
+
+__global__ void __launch_bounds__(kMoveThreads) plt_evict_compact_kernel(const __grid_constant__ CompactParams p, const int pieces,
+                                                                         const int row_blocks) {
+    constexpr int THREADS = kMoveThreads, U = 8;                                         // U: rows of a thread in flight
     constexpr int STEP = THREADS / kColumns, CHUNK = STEP * U, MINE = CHUNK / THREADS;   // rows: per step, per chunk, planned per thread
     __shared__ Move moves[3][CHUNK];     // a buffer is rewritten two barriers after its last use
     uint32_t flags = 0;
@@ -175,12 +180,11 @@ __global__ void __launch_bounds__(THREADS) plt_evict_compact_kernel(const __grid
 
 }  // namespace
 
-cudaError_t launch_compact(const CompactParams& p, int batch, int sm_count, cudaStream_t stream) {
+cudaError_t launch_compact(const CompactParams& p, int batch, cudaStream_t stream) {
     const int pieces = p.row_bytes / (16 * kColumns);
     const int row_blocks = batch * p.Hkv * 2 * pieces;
     const unsigned grid = (unsigned)(row_blocks + (p.weights ? batch * (p.Hkv / p.hpg) : 0));
-    if (row_blocks <= sm_count) plt_evict_compact_kernel<1024, 4><<<grid, 1024, 0, stream>>>(p, pieces, row_blocks);
-    else plt_evict_compact_kernel<256, 8><<<grid, 256, 0, stream>>>(p, pieces, row_blocks);
+    plt_evict_compact_kernel<<<grid, kMoveThreads, 0, stream>>>(p, pieces, row_blocks);
     return cudaGetLastError();
 }
 

@@ -6,7 +6,8 @@
 // a row's score of a key is 4 bytes where the key's row of K is 2 d. With more rows the scratch would cost more than K, so K is
 // streamed twice, first for the statistics (kScoreStats), then for the sums of the weights over the rows (kScoreSums: one float
 // a key and share of the rows); the rule stands at score_variant. Bound: HBM (K); with E4M3 codes above 16 rows the
-// conversions of the codes, which every share of the rows repeats.
+// instructions of 16 warps an SM (32 rows: issue slots 56 %, tensor pipe 41 %, DRAM 39 % busy), of which the conversion of the
+// codes, repeated by every share of the rows, is the larger part.
 // Measured: 8 rows, 64 ragged sequences of up to 8192 keys, 8 KV heads of 128 bf16 (284 MB of K): 52 us for this kernel, 65
 // for the call; 32 rows there: 110 us, 64 rows 165. 16 rows, 8 x 32768 E4M3 codes in pages of 64: 67 us, the call 104.
 //
