@@ -220,7 +220,7 @@ cudaError_t launch_one(const Params& p, unsigned grid, int chunks, bool overlap,
 // head; both maps' partials are loaded together. Everything up to the store is fp32: the difference of two nearly equal
 // results is taken before the one rounding to the output type. Launch-latency bound like the kernel above: it reads twice
 // its partials, and the four vectors of the factor (a few KB, the same for every sequence) before the main kernel ends. The whole step, 64 sequences
-// of 4096 keys, two loops, 32 heads on 8 of 128 bf16: 175 us, 0.96 of the copy rate on its 1.09 GB; one sequence of 700: 12.2 us.
+// of 4096 keys, two loops, 32 heads on 8 of 128 bf16: 175 us, 0.96 of the copy rate on its 1.09 GB; one sequence of 300: 12.2 us.
 
 // What is loaded of one map of a head: its shared-cache and its window partial when each was left by one block.
 template <int D>
