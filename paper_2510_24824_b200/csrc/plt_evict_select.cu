@@ -3,16 +3,17 @@
 // Per (sequence, head group) the `budget` largest of N totals, ties to the lowest position, in ascending order. A total maps
 // to a 32-bit key that orders like it (protected positions above everything, NaN below); three radix passes (11, 11, 10
 // bits, from the top) find the key T of the budget-th largest, each a histogram of the next digit of the keys that share the
-// digits found so far; then every warp counts the keys of its run that are above T and equal to T, one scan over the warps
-// gives each its place in the output, and the runs are written without further synchronisation.
+// digits found so far. Every warp then knows the keys of its run that are above T and equal to T (the third pass counts those
+// that the first two digits tell apart, and only a warp with others counts once more), one scan over the warps gives each its
+// place in the output, and the runs are written without further synchronisation.
 //
 // A block of 1024 threads takes a row, or a cluster of up to 8 blocks where rows are long and few: each block then holds a
 // part of the row, histograms are summed over the cluster through distributed shared memory, and every block takes the same
 // decisions on the same sums. A block's keys are read from memory once and stay with it, in registers (up to 8 per thread)
 // or shared memory (up to 48 K keys), by the capacity, which bounds the length; longer parts are read again by every pass.
 // The floor is one read of the totals; what bounds it is the chain of passes (histogram, scan, pick) and, on long rows, the
-// histogram's shared-memory atomics. A row of 32768, alone on its SM: load 2.4 us, passes 3.2 / 2.1 / 1.7, picks 0.65 each,
-// count 1.6, positions out 5.6. 384 rows of up to 32768: 26.6 us (18.6 MB at 680 GB/s); 8 rows of 5000: 10.2.
+// histogram's shared-memory atomics. A row of 32768, alone on its SM, 18 us: load 2.4, passes 3.2 / 2.1 / 1.9, picks 0.65 each,
+// scan, positions out and the end 6. 384 rows of up to 32768: 25.9 us (18 MB at 700 GB/s); 8 rows of 5000: 9.4.
 #include <cooperative_groups.h>
 
 #include "plt_common.cuh"
@@ -147,6 +148,8 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
 
     uint32_t prefix = 0, left = (uint32_t)kept;         // digits found so far; how many of the keys that share them are kept
     uint32_t above_mine = 0, equal_mine = 0;            // in this block: keys above T, keys equal to T
+    uint32_t ng = 0, ne = 0;                            // in this warp's run: keys above T, keys equal to T
+    bool near = false;                                  // a key of the run shares T's first two digits
     int shift = 32;
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
@@ -161,8 +164,15 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
         }
         __syncthreads();
         if (pass == 0) walk(true, [&](int, uint32_t k) { atomicAdd(&hist[k >> shift], 1u); });
-        else walk(false, [&](int, uint32_t k) {
+        else if (pass == 1) walk(false, [&](int, uint32_t k) {
             if ((k >> prev) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1u);
+        });
+        else walk(false, [&](int, uint32_t k) {
+            ng += (k >> prev) > prefix;
+            if ((k >> prev) == prefix) {
+                atomicAdd(&hist[k & digits], 1u);
+                near = true;
+            }
         });
         __syncthreads();
         const uint32_t* counts = hist;
@@ -223,11 +233,13 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
         }
         cg::this_cluster().sync();                      // no block ends while another reads its counts
     }
-    uint32_t ng = 0, ne = 0;                            // in this warp's run
-    walk(false, [&](int, uint32_t k) {
-        ng += k > prefix;
-        ne += k == prefix;
-    });
+    if (__any_sync(0xffffffffu, near)) {                // the last pass counted what the first two digits tell
+        ng = 0;
+        walk(false, [&](int, uint32_t k) {
+            ng += k > prefix;
+            ne += k == prefix;
+        });
+    }
     ng = __reduce_add_sync(0xffffffffu, ng);
     ne = __reduce_add_sync(0xffffffffu, ne);
     uint32_t total;
@@ -237,14 +249,22 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
     const uint32_t below = (1u << lane) - 1u;
     uint32_t to = above + min(equal, left);             // the warp's next place
     const bool ties = ne > 0 && equal < left;           // of the warp's run, some equal to T are kept
+    if (!ties) {
+        int32_t* dst = out + to;
+        int at = w0 + lane;
+        walk(false, [&](int j, uint32_t k) {
+            const bool take = k > prefix;
+            const uint32_t mask = __ballot_sync(0xffffffffu, take);
+            if (take) dst[__popc(mask & below)] = at + j * 32;
+            dst += __popc(mask);
+        });
+        return;
+    }
     walk(false, [&](int j, uint32_t k) {
-        bool take = k > prefix;
-        if (ties) {
-            const bool tie = k == prefix;
-            const uint32_t me = __ballot_sync(0xffffffffu, tie);
-            take = take || (tie && equal + __popc(me & below) < left);
-            equal += __popc(me);
-        }
+        const bool tie = k == prefix;
+        const uint32_t me = __ballot_sync(0xffffffffu, tie);
+        const bool take = k > prefix || (tie && equal + __popc(me & below) < left);
+        equal += __popc(me);
         const uint32_t mask = __ballot_sync(0xffffffffu, take);
         if (take) out[to + __popc(mask & below)] = w0 + j * 32 + lane;
         to += __popc(mask);
