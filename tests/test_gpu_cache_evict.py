@@ -472,6 +472,57 @@ def test_offsets_beyond_32_bits(page):
     assert np.array_equal(rows[0](budget, "k_cache").float().cpu().numpy(), moved.reshape(-1, row)[:budget].astype(np.float32))
 
 
+def test_two_handles_at_once_on_two_streams():
+    """Handles own their workspaces: calls of two of them that overlap on the device give what each gives alone."""
+    problems = [problem(B=24, Hq=16, Hkv=4, lens=("uniform", 1, 1500), seed=31), problem(B=20, Hq=40, Hkv=4, lens=("uniform", 1, 1700), seed=32)]
+    lambdas, gain = learned(128, 1)
+    alone, budget = [], 200
+    jobs = []
+    for p in problems:                        # 8 and 20 packed rows (16 and 40 with both maps): K once, K twice
+        dp = DeviceProblem(p, "cuda:0")
+        q = dp.q.view(p.B, p.L, 1, p.Hq, p.d)
+        w = torch.zeros(p.B, p.Hkv, p.max_seq_len, device="cuda")
+        keep, new = torch.empty(p.B, p.Hkv, budget, dtype=torch.int32, device="cuda"), torch.empty(p.B, dtype=torch.int32, device="cuda")
+        jobs.append((p, dp, q, w, keep, new, DiffAttn(p, lambdas, gain, LAMBDA_INIT, EPS), CacheEvict(p), torch.cuda.Stream()))
+
+    def work(job):
+        p, dp, q, w, keep, new, attn, op, _ = job
+        attn.run(dp)
+        op.weights(dp, q, w, decay=0.0)
+        op.select(dp, w, keep, new, budget, 2, 8)
+        return dp.out, w, keep, new
+    for job in jobs:
+        alone.append([t.clone() for t in work(job)])
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for job in jobs:
+            with torch.cuda.stream(job[-1]):
+                work(job)
+    torch.cuda.synchronize()
+    for job, want in zip(jobs, alone):
+        assert job[6].check() == 0 and job[7].check() == 0
+        for got, t in zip((job[1].out, job[3], job[4], job[5]), want):
+            live = t == t if t.is_floating_point() else slice(None)
+            assert torch.equal(got[live], t[live])
+        job[6].close()
+        job[7].close()
+
+
+def test_a_batch_of_none_does_nothing():
+    p = problem()
+    dp = DeviceProblem(p, "cuda:0")
+    w = torch.full((p.B, p.Hkv, p.max_seq_len), 7.0, device="cuda")
+    keep, new = torch.full((p.B, p.Hkv, 32), 5, dtype=torch.int32, device="cuda"), torch.full((p.B,), 5, dtype=torch.int32, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    with CacheEvict(p) as op:
+        for name, a in (("weights", op.weights_args(dp, dp.q.view(p.B, p.L, 1, p.Hq, p.d), w)), ("select", op.select_args(dp, w, keep, new, 32, 1, 4)),
+                        ("compact", op.compact_args(dp, keep, new, w))):
+            a.batch = 0
+            getattr(B, f"plt_cache_evict_{name}")(op.handle, a, stream)
+        assert op.check() == 0
+    assert bool((w == 7.0).all()) and bool((keep == 5).all()) and bool((new == 5).all())
+
+
 # ---- together -----------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("page,kv", [(0, ""), (32, ""), (32, "e4m3")])
 @pytest.mark.parametrize("diff", [False, True])
