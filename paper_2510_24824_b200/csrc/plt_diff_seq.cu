@@ -7,6 +7,9 @@
 //   S_x [128 rows x 64 keys] = Q_x [128 x 64] . K_x^T [64 x 64 keys]       x = 1, 2, for each half h of a 128-key tile
 //   O_x [128 rows x 128]    += P_x [128 x 64] . V_half [64 x 128]          P in tensor memory (bf16, over S)
 //
+// The weights are rounded to bf16 for the second product, the operand type of its V; the denominators add them unrounded. That
+// puts a map's result off by at most 2^-8 of the largest value it averages, as much as the output's own rounding.
+//
 // Tensor memory holds both accumulators (256 columns) and, for each map, the scores of two 64-key halves (256 columns). A
 // softmax warp works on one half while the products on the other half of the same map run: the P of a half is consumed and
 // the next tile's scores of that half are written behind it in the tensor core's own order. With whole 128-key score tiles
