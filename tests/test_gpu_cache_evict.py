@@ -193,6 +193,31 @@ def test_weights_above_sixteen_rows(Hq, L, q_len, maps, kv, d, heads, group, pag
                   group=group, decay=0.5)
 
 
+@pytest.mark.parametrize("Hq,dtype", [(16, "bf16"), (80, "bf16"), (16, "f32")])
+def test_weights_replayed_with_other_lengths_queries_and_keys(Hq, dtype):
+    p = problem(Hq=Hq, dtype=dtype, lens=("list", [2100, 900, 40]))
+    dp, other = DeviceProblem(p, "cuda:0"), DeviceProblem(problem(Hq=Hq, dtype=dtype, lens=("list", [17, 2100, 0]), max_seq_len=2100, seed=77), "cuda:0")
+    q, w = dp.q.view(p.B, p.L, 1, p.Hq, p.d), torch.zeros(p.B, p.Hkv, p.max_seq_len, device="cuda")
+    side = torch.cuda.Stream()
+    with CacheEvict(p) as op:
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            op.weights(dp, q, w, decay=0.25)          # the first call of the handle
+        for t in ("q", "k_cache", "seq_lens"):
+            getattr(dp, t).copy_(getattr(other, t))
+        w.fill_(0.5)
+        want = w.clone()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            graph.replay()
+            op.weights(other, other.q.view(p.B, p.L, 1, p.Hq, p.d), want, decay=0.25)
+        torch.cuda.synchronize()
+        assert op.check() == 0
+    assert torch.equal(w, want)
+    assert bool((w[2] == 0.5).all()) and bool((w[0, :, 17:] == 0.5).all())
+
+
 # ---- select -------------------------------------------------------------------------------------------------------
 def check_select(w, lens, budget, first=0, last=1, stride=0):
     Bn, groups, N = w.shape
