@@ -421,15 +421,13 @@ plt_diff_seq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             if (kind != 1) ++pv;
         }
         // ---- epilogue: both accumulators out of tensor memory ------------------------------------------------
-        if (pl.total > 0) {
-            // the other map has handed over as many halves: all four products of the last step with V
-            for (int s = 0; s < 4; ++s)
-                if (ok && pv > 0) ok = seq_wait(&bars[DB_PVD + s], (pv - 1) & 1u, abort_flag);
-            ok = __all_sync(0xffffffffu, ok);
-            tc_fence_after_sync();
-        }
+        // Each map waits for its own last products only: a barrier's parity tells a phase from the one before it, and nothing
+        // keeps the maps that close (the ring leaves them up to two steps apart). The block barrier then stands for both, and
+        // for every product that reads the query tile, which the exchange buffer overwrites.
+        if (pl.total > 0) wait_products(false);
         const bool have_o = pl.total > 0 && ok;            // warp-uniform
-        float* xch = (float*)q_smem;                       // [4][128]; every product that reads the query tile has completed
+        named_barrier_sync(1, 256);
+        float* xch = (float*)q_smem;                       // [4][128]
         xch[x * SQ + row] = l == 0 ? (lg > 0.f ? 1.f / lg : 0.f) : 1.f;   // makes accumulator x of the row a finished result
         named_barrier_sync(1, 256);
         const float f1 = xch[row], f2 = -lambda * xch[SQ + row];
