@@ -426,7 +426,9 @@ plt_diff_seq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         // for every product that reads the query tile, which the exchange buffer overwrites.
         if (pl.total > 0) wait_products(false);
         const bool have_o = pl.total > 0 && ok;            // warp-uniform
-        named_barrier_sync(1, 256);
+        tc_fence_before_sync();                            // the other map's accumulator is read behind the barrier: its products,
+        named_barrier_sync(1, 256);                        // and what its softmax warps stored to it, come before those loads
+        tc_fence_after_sync();
         float* xch = (float*)q_smem;                       // [4][128]
         xch[x * SQ + row] = l == 0 ? (lg > 0.f ? 1.f / lg : 0.f) : 1.f;   // makes accumulator x of the row a finished result
         named_barrier_sync(1, 256);
