@@ -173,7 +173,7 @@ plt_diff_seq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 
     if (wid == 0) {
         // =========================== TMA producer (one lane) ==============================================
-        if (lane == 0 && pl.total > 0) {
+        if (lane == 0) {
             tma_prefetch_desc(&tmQ);
             tma_prefetch_desc(&tmK);
             tma_prefetch_desc(&tmV);
@@ -208,100 +208,98 @@ plt_diff_seq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         // One lane's instruction stream is what bounds the issue (about 95 cycles a product with its descriptors and commits,
         // against 32 to 64 cycles of the tensor core), so each map has an issuer of its own.
         const int x = wid - 1;
-        if (pl.total > 0) {
-            constexpr uint32_t idesc_qk = seq_instr_desc(SQ, HK, 0);
-            constexpr uint32_t idesc_pv = seq_instr_desc(SQ, SD, 1);
-            // descriptors of the first byte; a byte offset adds offset / 16 to the address field
-            const uint64_t q_desc = seq_smem_desc(smem_u32(q_smem) + x * kHalf, 16, 1024);
-            const uint64_t k_desc = seq_smem_desc(smem_u32(ring) + x * kHalf, 16, 1024);
-            const uint64_t v_desc = seq_smem_desc(smem_u32(ring), kHalf, 1024);
-            const uint32_t tS = tmem_base + x * 128, tO = tmem_base + 256 + x * 128;
-            // waits as a warp; false once any wait of the block has run out
-            auto wait = [&](int bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, seq_wait(&bars[bar], parity, abort_flag)); };
-            auto issue_s = [&](int slot, int hh) {   // scores of half hh on the K tile in `slot`
-                if (lane == 0) {
-                    const uint64_t kd = k_desc + (uint64_t)(slot * (kTileBytes / 16) + hh * (HK * 128 / 16));
+        constexpr uint32_t idesc_qk = seq_instr_desc(SQ, HK, 0);
+        constexpr uint32_t idesc_pv = seq_instr_desc(SQ, SD, 1);
+        // descriptors of the first byte; a byte offset adds offset / 16 to the address field
+        const uint64_t q_desc = seq_smem_desc(smem_u32(q_smem) + x * kHalf, 16, 1024);
+        const uint64_t k_desc = seq_smem_desc(smem_u32(ring) + x * kHalf, 16, 1024);
+        const uint64_t v_desc = seq_smem_desc(smem_u32(ring), kHalf, 1024);
+        const uint32_t tS = tmem_base + x * 128, tO = tmem_base + 256 + x * 128;
+        // waits as a warp; false once any wait of the block has run out
+        auto wait = [&](int bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, seq_wait(&bars[bar], parity, abort_flag)); };
+        auto issue_s = [&](int slot, int hh) {   // scores of half hh on the K tile in `slot`
+            if (lane == 0) {
+                const uint64_t kd = k_desc + (uint64_t)(slot * (kTileBytes / 16) + hh * (HK * 128 / 16));
 #pragma unroll
-                    for (int kk = 0; kk < SD / 32; ++kk) mma_ss(tS + hh * HK, q_desc + kk * 2, kd + kk * 2, idesc_qk, kk > 0);
-                    umma_commit(&bars[DB_SFULL + 2 * x + hh]);
+                for (int kk = 0; kk < SD / 32; ++kk) mma_ss(tS + hh * HK, q_desc + kk * 2, kd + kk * 2, idesc_qk, kk > 0);
+                umma_commit(&bars[DB_SFULL + 2 * x + hh]);
+            }
+            __syncwarp();
+        };
+        int slot = 0;                            // ring position of the next load to be used
+        uint32_t parity = 0;
+        auto advance = [&]() {
+            if (++slot == kDRing) {
+                slot = 0;
+                parity ^= 1u;
+            }
+        };
+        bool ok = wait(DB_QFULL, 0) && wait(DB_FULL + 0, 0);
+        if (ok) {
+            tc_fence_after_sync();
+            issue_s(0, 0);
+            issue_s(0, 1);
+            if (lane == 0) umma_commit(&bars[DB_EMPTY + 0]);
+            __syncwarp();
+            advance();
+        }
+        bool o_started = false;
+        for (int i = 0; i < pl.total && ok; ++i) {
+            int kind, tile;
+            pl.step(i, kind, tile);
+            const int v_slot = slot;
+            if (kind != 1) {
+                ok = wait(DB_FULL + slot, parity);
+                if (!ok) break;
+                advance();
+                // Rows of the V tile at or beyond the sequence's length may hold anything: zero them, so that a weight
+                // of 0 times garbage cannot produce NaN (both issuers write the same zeros before their own products).
+                const int vrow0 = max(n - tile * SK, 0);
+                if (vrow0 < SK) {
+                    uint8_t* v = ring + (size_t)v_slot * kTileBytes;
+                    for (int idx = lane; idx < (SK - vrow0) * 16; idx += 32) {
+                        const int row = vrow0 + idx / 16, ch = idx % 16;
+                        *(uint4*)(v + (ch >> 3) * kHalf + row * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
                 }
-                __syncwarp();
-            };
-            int slot = 0;                            // ring position of the next load to be used
-            uint32_t parity = 0;
-            auto advance = [&]() {
-                if (++slot == kDRing) {
-                    slot = 0;
-                    parity ^= 1u;
-                }
-            };
-            bool ok = wait(DB_QFULL, 0) && wait(DB_FULL + 0, 0);
-            if (ok) {
-                tc_fence_after_sync();
-                issue_s(0, 0);
-                issue_s(0, 1);
-                if (lane == 0) umma_commit(&bars[DB_EMPTY + 0]);
-                __syncwarp();
+            }
+            const bool next = i + 1 < pl.total;
+            const int k_slot = slot;
+            if (next) {
+                ok = wait(DB_FULL + slot, parity);   // there since the step before, as a rule: the ring is six deep
+                if (!ok) break;
                 advance();
             }
-            bool o_started = false;
-            for (int i = 0; i < pl.total && ok; ++i) {
-                int kind, tile;
-                pl.step(i, kind, tile);
-                const int v_slot = slot;
-                if (kind != 1) {
-                    ok = wait(DB_FULL + slot, parity);
-                    if (!ok) break;
-                    advance();
-                    // Rows of the V tile at or beyond the sequence's length may hold anything: zero them, so that a weight
-                    // of 0 times garbage cannot produce NaN (both issuers write the same zeros before their own products).
-                    const int vrow0 = max(n - tile * SK, 0);
-                    if (vrow0 < SK) {
-                        uint8_t* v = ring + (size_t)v_slot * kTileBytes;
-                        for (int idx = lane; idx < (SK - vrow0) * 16; idx += 32) {
-                            const int row = vrow0 + idx / 16, ch = idx % 16;
-                            *(uint4*)(v + (ch >> 3) * kHalf + row * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                if (ok) ok = wait(DB_PFULL + 2 * x + hh, (uint32_t)i & 1u);
+                if (ok) {
+                    tc_fence_after_sync();
+                    if (kind != 1) {
+                        if (lane == 0) {
+                            const uint64_t vd = v_desc + (uint64_t)(v_slot * (kTileBytes / 16) + hh * (HK * 128 / 16));
+#pragma unroll
+                            for (int kk = 0; kk < HK / 16; ++kk) {
+                                if (hh == 0 && kk == 0 && !o_started) mma_ts(tO, tS, vd, idesc_pv, false);
+                                else mma_ts(tO, tS + hh * HK + kk * 8, vd + kk * (2048 / 16), idesc_pv, true);
+                            }
+                            umma_commit(&bars[DB_PVD + 2 * x + hh]);
                         }
-                        fence_proxy_async_smem();
                         __syncwarp();
                     }
+                    // the next tile's scores of this half: behind the product that reads its weights, in order
+                    if (next) issue_s(k_slot, hh);
                 }
-                const bool next = i + 1 < pl.total;
-                const int k_slot = slot;
-                if (next) {
-                    ok = wait(DB_FULL + slot, parity);   // there since the step before, as a rule: the ring is six deep
-                    if (!ok) break;
-                    advance();
-                }
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    if (ok) ok = wait(DB_PFULL + 2 * x + hh, (uint32_t)i & 1u);
-                    if (ok) {
-                        tc_fence_after_sync();
-                        if (kind != 1) {
-                            if (lane == 0) {
-                                const uint64_t vd = v_desc + (uint64_t)(v_slot * (kTileBytes / 16) + hh * (HK * 128 / 16));
-#pragma unroll
-                                for (int kk = 0; kk < HK / 16; ++kk) {
-                                    if (hh == 0 && kk == 0 && !o_started) mma_ts(tO, tS, vd, idesc_pv, false);
-                                    else mma_ts(tO, tS + hh * HK + kk * 8, vd + kk * (2048 / 16), idesc_pv, true);
-                                }
-                                umma_commit(&bars[DB_PVD + 2 * x + hh]);
-                            }
-                            __syncwarp();
-                        }
-                        // the next tile's scores of this half: behind the product that reads its weights, in order
-                        if (next) issue_s(k_slot, hh);
-                    }
-                }
-                if (!ok) break;
-                if (kind != 1) o_started = true;
-                if (lane == 0) {
-                    if (kind != 1) umma_commit(&bars[DB_EMPTY + v_slot]);
-                    if (next) umma_commit(&bars[DB_EMPTY + k_slot]);
-                }
-                __syncwarp();
             }
+            if (!ok) break;
+            if (kind != 1) o_started = true;
+            if (lane == 0) {
+                if (kind != 1) umma_commit(&bars[DB_EMPTY + v_slot]);
+                if (next) umma_commit(&bars[DB_EMPTY + k_slot]);
+            }
+            __syncwarp();
         }
     } else if (wid >= 4) {
         // =========================== softmax and epilogue ================================================
@@ -332,7 +330,7 @@ plt_diff_seq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         }
         const float lambda = expf(d1) - expf(d2) + p.tail.lambda_init;
         float gate = 0.f;
-        if (pl.total > 0 && l > 0 && rc.t < p.T) {
+        if (l > 0 && rc.t < p.T) {
             const float z = p.gate[(((int64_t)b * (p.L - 1) + (l - 1)) * p.T + rc.t) * p.Hq + h];
             gate = 1.f / (1.f + __expf(-z));
         }
@@ -424,8 +422,7 @@ plt_diff_seq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         // Each map waits for its own last products only: a barrier's parity tells a phase from the one before it, and nothing
         // keeps the maps that close (the ring leaves them up to two steps apart). The block barrier then stands for both, and
         // for every product that reads the query tile, which the exchange buffer overwrites.
-        if (pl.total > 0) wait_products(false);
-        const bool have_o = pl.total > 0 && ok;            // warp-uniform
+        wait_products(false);
         tc_fence_before_sync();                            // the other map's accumulator is read behind the barrier: its products,
         named_barrier_sync(1, 256);                        // and what its softmax warps stored to it, come before those loads
         tc_fence_after_sync();
@@ -438,14 +435,14 @@ plt_diff_seq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             uint32_t ra[32], rb[32];
-            if (have_o) {
+            if (ok) {
                 tmem_ld32(t_lane + 256 + x * 64 + c * 32, ra);
                 tmem_ld32(t_lane + 384 + x * 64 + c * 32, rb);
                 tmem_wait_ld();
             }
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-                const float v = have_o && rc.live ? fmaf(f2, __uint_as_float(rb[i]), f1 * __uint_as_float(ra[i])) : 0.f;
+                const float v = ok && rc.live ? fmaf(f2, __uint_as_float(rb[i]), f1 * __uint_as_float(ra[i])) : 0.f;
                 y[c * 32 + i] = v;
                 ss = fmaf(v, v, ss);
             }
@@ -485,7 +482,7 @@ plt_diff_seq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const uint32_t cnt = issued - 1 - k;
             mbar_wait_bounded(&bars[DB_FULL + cnt % kDRing], (cnt / kDRing) & 1u, kSeqWaitNs);
         }
-        if (pl.total > 0) mbar_wait_bounded(&bars[DB_QFULL], 0, kSeqWaitNs);
+        mbar_wait_bounded(&bars[DB_QFULL], 0, kSeqWaitNs);
     }
     __syncthreads();
     if (wid == 1) {
