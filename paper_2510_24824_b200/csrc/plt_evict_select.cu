@@ -313,7 +313,7 @@ cudaError_t launch_select(const SelectParams& p, int batch, cudaStream_t stream)
     const int c = select_cluster(p, batch);
     if (p.max_seq_len <= c * kRegKeys * kSelThreads) return launch_cluster<kRegisters>(p, batch, c, stream);
     if (p.max_seq_len <= c * kSharedKeys) return launch_cluster<kShared>(p, batch, c, stream);
-    return launch_cluster<kMemory>(p, batch, c, stream);
+    return launch_home<kMemory, true>(p, batch, c, stream);      // select_cluster gives rows this long eight blocks
 }
 
 }  // namespace plt
