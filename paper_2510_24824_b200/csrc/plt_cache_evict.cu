@@ -388,7 +388,7 @@ PLT_API plt_status plt_cache_evict_select(plt_cache_evict_t h, const plt_cache_e
     DeviceScope scope(c.device);
     if (scope.err != cudaSuccess) return cuda_fail(h, "cudaSetDevice", scope.err);
     const SelectParams p = {a->weights, ws, a->seq_lens, a->keep, a->new_lens, h->status, c.Hkv / h->g.hpg, c.max_seq_len, a->budget,
-                            a->keep_first, a->keep_last};
+                            a->keep_first, a->keep_last, h->sm_count};
     const cudaError_t err = launch_select(p, a->batch, (cudaStream_t)cuda_stream);
     if (err != cudaSuccess) return cuda_fail(h, "launching the selection kernel", err);
     return PLT_OK;

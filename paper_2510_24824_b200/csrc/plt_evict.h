@@ -71,6 +71,7 @@ struct SelectParams {
     int32_t* new_lens;
     uint32_t* status;
     int32_t groups, max_seq_len, budget, keep_first, keep_last;
+    int32_t sm_count;
 };
 cudaError_t launch_select(const SelectParams& p, int batch, cudaStream_t stream);
 

@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
 // of up to 32768, which fill the device: one 26.8, two 38.4; 8 rows of 5000: one 11.2, two 12.5).
 int select_cluster(const SelectParams& p, int batch) {
     int c = 1;
-    while (c < 8 && p.max_seq_len / c >= 2 * 4096 && ((int64_t)batch * p.groups * c * 2 <= 148 || p.max_seq_len > c * kSharedKeys)) c *= 2;
+    while (c < 8 && p.max_seq_len / c >= 2 * 4096 && ((int64_t)batch * p.groups * c * 2 <= p.sm_count || p.max_seq_len > c * kSharedKeys)) c *= 2;
     return c;
 }
 
