@@ -266,9 +266,19 @@ class DiffSeqAttn:
             pass
 
 
+def _dense(name: str, t, dtype, B: int, per: int):
+    """Refuses a tensor whose first B entries are not `per` elements of `dtype` each, one behind the other."""
+    if t.dtype != dtype or t.dim() < 1 or not t.is_contiguous() or t.shape[0] < B or t.numel() != t.shape[0] * per:
+        raise ValueError(f"{name}: {B} x {per} dense elements of {dtype} are needed, not {tuple(t.shape)} of {t.dtype} with "
+                         f"strides {t.stride()}")
+    return t
+
+
 class CacheEvict:
     """Owns one plt_cache_evict handle sized for a problem: totals of attention weight, selection and compaction on the shared
-    cache of a DeviceProblem (the caller holds the totals [B, groups, >= max_seq_len], `keep` and `new_lens`)."""
+    cache of a DeviceProblem.  The caller holds the totals [B, groups, >= max_seq_len] (fp32, rows equally far apart, so a
+    view of wider rows will do), `keep` [B, groups, budget] and `new_lens` [B] (int32, dense); what a kernel would read
+    otherwise than torch does is refused with ValueError."""
 
     def __init__(self, p, device_index: int = 0, max_batch: Optional[int] = None, q_len: int = 1, maps: int = 1,
                  heads_per_group: int = 1):
@@ -285,19 +295,46 @@ class CacheEvict:
         p = dp.problem
         return dict(page_table=dp.page_table, max_pages=p.max_pages, num_pool_pages=p.num_pool_pages)
 
+    def _groups(self) -> int:
+        return self.config.Hkv // max(1, self.config.heads_per_group)
+
+    def _row_pitch(self, dp: DeviceProblem, weights) -> int:
+        """Elements between the rows of the totals, of which one (sequence, group) follows the other."""
+        n, groups, least = dp.problem.B, self._groups(), self.config.max_seq_len
+        ok = weights.dtype == torch.float32 and weights.dim() == 3 and weights.shape[0] >= n and weights.shape[1] == groups and \
+            weights.shape[2] >= least
+        if ok:
+            pitch = weights.stride(1) if groups > 1 else weights.stride(0) if n > 1 else weights.shape[2]
+            ok = pitch >= least and (weights.stride(2) == 1 or least == 1) and (n <= 1 or weights.stride(0) == groups * pitch)
+        if not ok:
+            raise ValueError(f"totals: {n} x {groups} fp32 rows of at least {least} elements, equally far apart, are needed, not "
+                             f"{tuple(weights.shape)} of {weights.dtype} with strides {weights.stride()}")
+        return pitch
+
     def weights_args(self, dp: DeviceProblem, q, weights, gate_logits=None, decay: float = 1.0, kv_strides=(0, 0, 0)):
-        return B.make_evict_weights_args(dp.problem.B, q, dp.k_cache, dp.seq_lens, weights, gate_logits=gate_logits,
+        p, c = dp.problem, self.config
+        rows = max(1, c.q_len) * c.Hq
+        _dense("q", q, torch.bfloat16 if c.dtype == B.PLT_BF16 else torch.float32, p.B, c.L * rows * c.d)
+        if gate_logits is not None and c.L > 1:
+            _dense("gate_logits", gate_logits, torch.float32, p.B, (c.L - 1) * rows)
+        return B.make_evict_weights_args(p.B, q, dp.k_cache, dp.seq_lens, weights, gate_logits=gate_logits,
                                          decay=decay, k_scale=dp.k_scale, kv_strides=kv_strides,
-                                         weights_stride=weights.shape[-1], **self._pages(dp))
+                                         weights_stride=self._row_pitch(dp, weights), **self._pages(dp))
 
     def select_args(self, dp: DeviceProblem, weights, keep, new_lens, budget: int, keep_first: int, keep_last: int):
-        return B.make_evict_select_args(dp.problem.B, weights, dp.seq_lens, keep, new_lens, budget, keep_first, keep_last,
-                                        weights_stride=weights.shape[-1])
+        n = dp.problem.B
+        _dense("keep", keep, torch.int32, n, self._groups() * budget)
+        _dense("new_lens", new_lens, torch.int32, n, 1)
+        return B.make_evict_select_args(n, weights, dp.seq_lens, keep, new_lens, budget, keep_first, keep_last,
+                                        weights_stride=self._row_pitch(dp, weights))
 
     def compact_args(self, dp: DeviceProblem, keep, new_lens, weights=None, kv_strides=(0, 0, 0)):
-        return B.make_evict_compact_args(dp.problem.B, dp.k_cache, dp.v_cache, dp.seq_lens, keep, new_lens, keep.shape[-1],
+        n = dp.problem.B
+        _dense("keep", keep, torch.int32, n, self._groups() * keep.shape[-1])
+        _dense("new_lens", new_lens, torch.int32, n, 1)
+        return B.make_evict_compact_args(n, dp.k_cache, dp.v_cache, dp.seq_lens, keep, new_lens, keep.shape[-1],
                                          weights=weights, kv_strides=kv_strides,
-                                         weights_stride=0 if weights is None else weights.shape[-1], **self._pages(dp))
+                                         weights_stride=0 if weights is None else self._row_pitch(dp, weights), **self._pages(dp))
 
     def weights(self, dp: DeviceProblem, q, weights, gate_logits=None, decay: float = 1.0, kv_strides=(0, 0, 0),
                 stream: Optional[int] = None):

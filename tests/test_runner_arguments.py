@@ -1,0 +1,83 @@
+"""CPU checks of what the runner makes of the caller's tensors (no compute call is made)."""
+import pytest
+import torch
+
+from paper_2510_24824_b200 import binding as B
+from paper_2510_24824_b200.inputs import make_problem
+from paper_2510_24824_b200.runner import CacheEvict, DeviceProblem
+
+P = make_problem(dict(name="args", dtype="bf16", B=3, L=2, Hq=8, Hkv=4, d=128, w=16, lens=("list", [40, 7, 2]), seed=1))
+N = P.max_seq_len
+
+
+def op(p=P, group=1, q_len=1):
+    """A CacheEvict without its library handle."""
+    o = CacheEvict.__new__(CacheEvict)
+    o.handle = None
+    o.config = B.make_evict_config(p.dtype, p.B, p.L, p.Hq, p.Hkv, p.d, p.max_seq_len, q_len=q_len, heads_per_group=group)
+    return o
+
+
+def tensors(p=P, group=1, budget=16, q_len=1):
+    groups = p.Hkv // group
+    return dict(dp=DeviceProblem(p, "cpu"), q=torch.zeros(p.B, p.L, q_len, p.Hq, p.d, dtype=torch.bfloat16),
+                weights=torch.zeros(p.B, groups, p.max_seq_len), keep=torch.zeros(p.B, groups, budget, dtype=torch.int32),
+                new_lens=torch.zeros(p.B, dtype=torch.int32))
+
+
+def all_args(o, t, budget=16, gate=None):
+    return (o.weights_args(t["dp"], t["q"], t["weights"], gate), o.select_args(t["dp"], t["weights"], t["keep"], t["new_lens"], budget, 1, 4),
+            o.compact_args(t["dp"], t["keep"], t["new_lens"], t["weights"]))
+
+
+@pytest.mark.parametrize("group", [1, 2, 4])
+def test_totals_that_are_a_view_of_wider_rows(group):
+    t = tensors(group=group)
+    for wide in (torch.zeros(P.B, P.Hkv // group, N + 24)[..., :N], torch.zeros(P.B + 2, P.Hkv // group, N + 3)[1:-1, :, 2:N + 2]):
+        t["weights"] = wide
+        for a in all_args(op(group=group), t):
+            assert a.weights_stride == wide.stride(0 if group == P.Hkv else 1)
+
+
+def test_one_row_of_totals():
+    p = make_problem(dict(name="args", dtype="bf16", B=1, L=1, Hq=4, Hkv=1, d=128, w=0, lens=("list", [40]), seed=1))
+    t = tensors(p)
+    t["weights"] = torch.zeros(64, 1, N).transpose(0, 1)[:, 3:4]            # strides that no row uses
+    assert all(a.weights_stride >= N for a in all_args(op(p), t))
+
+
+@pytest.mark.parametrize("name,bad", [
+    ("weights", lambda t: t[:, :, : N - 1]),                                # rows shorter than the capacity
+    ("weights", lambda t: t.double()), ("weights", lambda t: t[:2]), ("weights", lambda t: t[:, :3]), ("weights", lambda t: t[0]),
+    ("weights", lambda t: torch.zeros(P.B, P.Hkv, 2 * N)[:, :, ::2]),       # elements apart
+    ("weights", lambda t: torch.zeros(P.Hkv, P.B, N).transpose(0, 1)),      # rows in another order
+    ("weights", lambda t: torch.zeros(P.B, 2 * P.Hkv, N)[:, : P.Hkv]),      # a gap between sequences
+    ("keep", lambda t: t.long()), ("keep", lambda t: torch.zeros(P.B, P.Hkv, 32, dtype=torch.int32)[..., :16]),
+    ("keep", lambda t: t[:2]), ("keep", lambda t: t[:, :3].contiguous()), ("keep", lambda t: t[0]),
+    ("new_lens", lambda t: t.long()), ("new_lens", lambda t: t[:2]), ("new_lens", lambda t: torch.zeros(2 * P.B, dtype=torch.int32)[::2]),
+    ("q", lambda t: t.float()), ("q", lambda t: t[:, :1]), ("q", lambda t: torch.zeros(P.L, P.B, 1, P.Hq, P.d, dtype=torch.bfloat16).transpose(0, 1)),
+])
+def test_tensors_that_a_kernel_would_misread(name, bad):
+    t = tensors()
+    all_args(op(), t)
+    t[name] = bad(t[name])
+    with pytest.raises(ValueError):
+        all_args(op(), t)
+
+
+def test_a_budget_that_is_not_the_width_of_keep_and_gates_of_another_shape():
+    t = tensors()
+    with pytest.raises(ValueError):
+        all_args(op(), t, budget=15)
+    good = torch.zeros(P.B, P.L - 1, 1, P.Hq)
+    all_args(op(), t, gate=good)
+    for bad in (good.double(), good[:2], torch.zeros(P.B, P.L - 1, 1, 2 * P.Hq)[..., ::2]):
+        with pytest.raises(ValueError):
+            all_args(op(), t, gate=bad)
+
+
+def test_larger_buffers_and_several_tokens_are_taken():
+    t = tensors(q_len=2)
+    t["weights"], t["new_lens"] = torch.zeros(P.B + 1, P.Hkv, N), torch.zeros(P.B + 4, dtype=torch.int32)
+    t["keep"] = torch.zeros(P.B + 1, P.Hkv, 16, dtype=torch.int32)
+    all_args(op(q_len=2), t)
