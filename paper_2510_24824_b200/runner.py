@@ -166,10 +166,16 @@ class SeqAttn:
         self.close()
 
 
-def _learned(lambdas, norm_gain, device):
+def _learned(lambdas, norm_gain, device, Hq: int, d: int):
     """The learned parameters of differential heads (numpy or torch, fp32) as the binding's struct; it keeps its tensors."""
     dev = lambda x: None if x is None else torch.as_tensor(x, dtype=torch.float32).to(device).contiguous()
-    return B.make_diff_weights(*[dev(x) for x in lambdas], norm_gain=dev(norm_gain))
+    vectors, gain = [dev(x) for x in lambdas], dev(norm_gain)
+    shapes = [tuple(x.shape) for x in vectors]
+    if len(shapes) != 4 or len(set(shapes)) != 1 or shapes[0] not in ((d // 2,), (1, d // 2), (Hq, d // 2)):
+        raise ValueError(f"lambdas: four vectors [1 or {Hq}, {d // 2}], all alike, are needed, not {shapes}")
+    if gain is not None and tuple(gain.shape) != (d,):
+        raise ValueError(f"norm_gain: [{d}] is needed, not {tuple(gain.shape)}")
+    return B.make_diff_weights(*vectors, norm_gain=gain)
 
 
 class DiffAttn(DecodeAttn):
@@ -184,7 +190,7 @@ class DiffAttn(DecodeAttn):
             sm_scale=p.sm_scale, device=device_index,
             loop_offset=None if p.loop_offset is None else [int(x) for x in p.loop_offset], kv_dtype=p.kv_dtype,
             lambda_init=lambda_init, norm_eps=norm_eps, **config)
-        self.weights = _learned(lambdas, norm_gain, device)
+        self.weights = _learned(lambdas, norm_gain, device, p.Hq, p.d)
         self.handle = B.plt_diff_attn_create(self.config)
 
     def run(self, dp: DeviceProblem, stream: Optional[int] = None, out=None):
@@ -230,7 +236,7 @@ class DiffSeqAttn:
             max(p.B, 1), p.L, p.Hq, p.Hkv, p.d, p.T, p.w, sm_scale=p.sm_scale, device=device_index,
             loop_offset=None if p.loop_offset is None else [int(x) for x in p.loop_offset], lambda_init=lambda_init,
             norm_eps=norm_eps)
-        self.weights = _learned(lambdas, norm_gain, device)
+        self.weights = _learned(lambdas, norm_gain, device, p.Hq, p.d)
         self.handle = B.plt_diff_seq_attn_create(self.config)
         many = p.L > 1
         self.args = B.make_seq_args(p.B, self.q, self.k_share, self.v_share, self.seq_lens, self.out,

@@ -4,7 +4,7 @@ import torch
 
 from paper_2510_24824_b200 import binding as B
 from paper_2510_24824_b200.inputs import make_problem
-from paper_2510_24824_b200.runner import CacheEvict, DeviceProblem
+from paper_2510_24824_b200.runner import CacheEvict, DeviceProblem, _learned
 
 P = make_problem(dict(name="args", dtype="bf16", B=3, L=2, Hq=8, Hkv=4, d=128, w=16, lens=("list", [40, 7, 2]), seed=1))
 N = P.max_seq_len
@@ -81,3 +81,22 @@ def test_larger_buffers_and_several_tokens_are_taken():
     t["weights"], t["new_lens"] = torch.zeros(P.B + 1, P.Hkv, N), torch.zeros(P.B + 4, dtype=torch.int32)
     t["keep"] = torch.zeros(P.B + 1, P.Hkv, 16, dtype=torch.int32)
     all_args(op(q_len=2), t)
+
+
+# ---- learned parameters of differential heads ------------------------------------------------------------------------
+def learned(q1=(1, 64), k1=(1, 64), q2=(1, 64), k2=(1, 64), gain=(128,)):
+    return _learned([torch.zeros(s) for s in (q1, k1, q2, k2)], None if gain is None else torch.ones(gain), "cpu", 8, 128)
+
+
+def test_learned_parameters_of_every_allowed_shape():
+    for rows in ((64,), (1, 64), (8, 64)):
+        w = learned(rows, rows, rows, rows)
+        assert w.lambda_heads == (8 if rows == (8, 64) else 1) and w.norm_gain
+    assert not learned(gain=None).norm_gain
+
+
+@pytest.mark.parametrize("bad", [dict(q1=(8, 64)), dict(k2=(8, 64)), dict(k1=(64, 8)), dict(q2=(1, 32)), dict(gain=(64,)), dict(gain=(2, 64)),
+                                 dict(q1=(4, 64), k1=(4, 64), q2=(4, 64), k2=(4, 64)), dict(q1=(8, 8, 64))])
+def test_learned_parameters_that_a_kernel_would_read_beyond(bad):
+    with pytest.raises(ValueError):
+        learned(**bad)
