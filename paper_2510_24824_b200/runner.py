@@ -180,11 +180,12 @@ def _learned(lambdas, norm_gain, device, Hq: int, d: int):
 
 class DiffAttn(DecodeAttn):
     """Owns one plt_diff_attn handle sized for a problem, with the learned parameters of a layer (`lambdas`: the four vectors
-    [1 or Hq, d / 2]; `norm_gain`: [d] or None)."""
+    [1 or Hq, d / 2]; `norm_gain`: [d] or None; put on `device`, by default that of device_index)."""
 
-    def __init__(self, p, lambdas, norm_gain=None, lambda_init: float = 0.8, norm_eps: float = 1e-5, device="cuda:0",
+    def __init__(self, p, lambdas, norm_gain=None, lambda_init: float = 0.8, norm_eps: float = 1e-5, device=None,
                  device_index: int = 0, max_batch: Optional[int] = None, **config):
         self.handle = None
+        device = f"cuda:{device_index}" if device is None else device
         self.config = B.make_diff_config(
             p.dtype, max_batch or max(p.B, 1), p.L, p.Hq, p.Hkv, p.d, p.max_seq_len, p.w, page_size=p.page_size,
             sm_scale=p.sm_scale, device=device_index,
@@ -221,11 +222,13 @@ class DiffAttn(DecodeAttn):
 
 
 class DiffSeqAttn:
-    """One plt_diff_seq_attn handle, the device tensors of a sequence problem and the learned parameters of a layer."""
+    """One plt_diff_seq_attn handle, the device tensors of a sequence problem and the learned parameters of a layer (on
+    `device`, by default that of device_index)."""
 
-    def __init__(self, p, lambdas, norm_gain=None, lambda_init: float = 0.8, norm_eps: float = 1e-5, device="cuda:0",
+    def __init__(self, p, lambdas, norm_gain=None, lambda_init: float = 0.8, norm_eps: float = 1e-5, device=None,
                  device_index: int = 0):
         self.handle = None
+        device = f"cuda:{device_index}" if device is None else device
         self.problem = p
         for f in SeqAttn.FIELDS:
             setattr(self, f, to_torch(getattr(p, f), "bf16", device))

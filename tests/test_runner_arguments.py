@@ -3,7 +3,8 @@ import pytest
 import torch
 
 from paper_2510_24824_b200 import binding as B
-from paper_2510_24824_b200.inputs import make_problem
+from paper_2510_24824_b200 import runner
+from paper_2510_24824_b200.inputs import make_problem, make_seq_problem
 from paper_2510_24824_b200.runner import CacheEvict, DeviceProblem, _learned
 
 P = make_problem(dict(name="args", dtype="bf16", B=3, L=2, Hq=8, Hkv=4, d=128, w=16, lens=("list", [40, 7, 2]), seed=1))
@@ -100,3 +101,17 @@ def test_learned_parameters_of_every_allowed_shape():
 def test_learned_parameters_that_a_kernel_would_read_beyond(bad):
     with pytest.raises(ValueError):
         learned(**bad)
+
+
+def test_learned_parameters_go_to_the_handles_device(monkeypatch):
+    """Without a device of their own they follow device_index (nothing is created here)."""
+    seen = []
+    monkeypatch.setattr(runner, "_learned", lambda lambdas, gain, device, Hq, d: seen.append(str(device)))
+    monkeypatch.setattr(runner, "to_torch", lambda a, dtype, device, pin=False: seen.append(str(device)))
+    monkeypatch.setattr(runner.torch, "empty", lambda *a, device=None, **k: seen.append(str(device)))
+    for name in ("plt_diff_attn_create", "plt_diff_seq_attn_create"):
+        monkeypatch.setattr(B, name, lambda config: None)
+    monkeypatch.setattr(B, "make_seq_args", lambda *a, **k: None)
+    runner.DiffAttn(P, None, device_index=3)
+    runner.DiffSeqAttn(make_seq_problem(B=1, L=1, T=2, Hq=1, Hkv=1, d=128, w=0), None, device_index=3)
+    assert set(seen) == {"cuda:3"}
