@@ -101,6 +101,11 @@ plt_status check_config(const plt_cache_evict_config* c, EvictGeometry* g) {
         return fail(nullptr, PLT_ERR_INVALID_ARG, "heads_per_group %d does not divide Hkv %d", g->hpg, c->Hkv);
     const double rows = (double)c->L * g->Qn * (c->Hq / c->Hkv) * (1 + g->qsplit);
     if (rows > kMaxRows) return fail(nullptr, PLT_ERR_UNSUPPORTED, "maps * L * q_len * Hq/Hkv = %.0f packed rows > %d", rows, kMaxRows);
+    // grids count blocks in 31 bits: compaction takes one for each sequence, head, cache and 64 bytes of a row and one more for
+    // each group's totals, selection up to eight for each sequence and group
+    const double pieces = c->d * (g->fp8 ? 1 : (g->bf16 ? 2 : 4)) / 64;
+    if ((double)c->max_batch * c->Hkv * (2 * pieces + 8) >= 2147483647.0)
+        return fail(nullptr, PLT_ERR_UNSUPPORTED, "max_batch %d * Hkv %d is more than a launch can count", c->max_batch, c->Hkv);
     g->G = (c->Hq / c->Hkv) << g->qsplit;
     g->R = c->L * g->Qn * g->G;
     if (g->bf16) {
