@@ -113,7 +113,7 @@ typedef struct {
  * all from the values before the call; weights[b, g, new_lens[b] .. seq_lens[b]) = 0 (the next tokens start there).  K and V
  * rows from new_lens[b] on stay as they are.  Positions have to be ascending (as plt_cache_evict_select writes them): one
  * below its slot or not below seq_lens[b] is clamped and flagged.  No page may belong to two sequences, and the rows of the
- * cache must not overlap.
+ * cache must not overlap.  Rows in front of the first dropped position stay where they are, all kept ones behind it move.
  */
 typedef struct {
     uint32_t struct_size;
@@ -131,7 +131,8 @@ typedef struct {
     int64_t weights_stride;
 } plt_cache_evict_compact_args;
 
-/* Validates the configuration and allocates the handle's workspace on config->device (the only call that allocates). */
+/* Validates the configuration and allocates the handle's workspace on config->device (the only call that allocates): at most
+ * about 256 MB, or what one sequence of max_seq_len tokens needs where that is more; select and compact use the status word alone. */
 plt_status plt_cache_evict_create(const plt_cache_evict_config* config, plt_cache_evict_t* out_handle);
 
 /* Device bytes plt_cache_evict_create would allocate for this configuration (no device needed; 148 SMs are assumed then). */

@@ -14,8 +14,8 @@
 // softmax warp works on one half while the products on the other half of the same map run: the P of a half is consumed and
 // the next tile's scores of that half are written behind it in the tensor core's own order. With whole 128-key score tiles
 // the chain scores -> softmax -> P V -> next scores of a map was open at every link, and the two maps' chains alone filled
-// 40 % of the exponential unit's time (5000 rows, 32 heads: 534 us; in this order, with an issuer for each map, 418 us,
-// 735 TFLOP/s over the visible keys).
+// 40 % of the exponential unit's time (5000 rows, 32 heads: 534 us; in this order, with an issuer for each map, 394 to 428 us by
+// box, 718 to 779 TFLOP/s over the visible keys).
 //
 // The block owns both results of a row, so the epilogue takes y_1 - lambda y_2 and the norm over the head's 128 elements in
 // fp32 from the two accumulators, and neither map reaches memory. Steps, masks and windows of loops 2..L are those of
@@ -24,7 +24,8 @@
 //
 // Warp roles: warp 0 streams K and V tiles by TMA into a ring of 32 KB slots, warps 1 and 2 issue the products of map 1 and 2
 // (one lane each; warp 1 owns tensor memory), warps 4-7 are the softmax of map 1, warps 8-11 of map 2 (thread = row =
-// tensor-memory lane). Every wait on an mbarrier is bounded and reports through the status word. Bound: the exponentials, 2 x
+// tensor-memory lane). The maps share nothing but the ring and may run two steps apart; they meet once, before the epilogue. Every
+// wait on an mbarrier is bounded and reports through the status word. Bound: the exponentials, 2 x
 // 128 x 128 per tile and block at 16 per cycle and SM (2048 cycles; the products take 1536). A tile takes 3440: a softmax warp is
 // busy for 1436 of every half's 1720, 155 of the rest are waits for scores.
 #include "plt_seq_util.cuh"

@@ -13,7 +13,8 @@
 // or shared memory (up to 48 K keys), by the capacity, which bounds the length; longer parts are read again by every pass.
 // The floor is one read of the totals; what bounds it is the chain of passes (histogram, scan, pick) and, on long rows, the
 // histogram's shared-memory atomics. A row of 32768, alone on its SM, 18 us: load 2.4, passes 3.2 / 2.1 / 1.9, picks 0.65 each,
-// scan, positions out and the end 6. 384 rows of up to 32768: 25.9 us (18 MB at 700 GB/s); 8 rows of 5000: 9.4.
+// scan, positions out and the end 6. 384 rows of up to 32768: 25.6 us (18 MB at 700 GB/s), all of 32768: 60, and with all totals equal,
+// where one bin of each histogram takes every addition: 65; 8 rows of 5000: 9.2, of 65536: 16.6.
 #include <cooperative_groups.h>
 
 #include "plt_common.cuh"
@@ -272,8 +273,9 @@ __global__ void __launch_bounds__(kSelThreads) plt_evict_select_kernel(const __g
 }
 
 // Blocks per row: as few as can hold a full row, and more while the grid leaves SMs idle and every block keeps 4096
-// positions (blocks per row, 8 rows of 65536: two 24.7 us, four or eight 18.5; 8 rows of 32768: one 20.6, four 16.5; 384 rows
-// of up to 32768, which fill the device: one 26.8, two 38.4; 8 rows of 5000: one 11.2, two 12.5).
+// positions (blocks per row, 8 rows of 65536: two 26.1 us, four 20.7, eight 16.6; 8 rows of 32768: one 20.7, two 19.4, four 16.6,
+// eight 14.6; 384 rows of up to 32768, which fill the device: one 25.6, two 40.0; 8 rows of 5000: one 9.2, two 12.5). The rule
+// knows the capacity, not the lengths: a row that is short in a long capacity is spread over as many blocks.
 int select_cluster(const SelectParams& p, int batch) {
     int c = 1;
     while (c < 8 && p.max_seq_len / c >= 2 * 4096 && ((int64_t)batch * p.groups * c * 2 <= p.sm_count || p.max_seq_len > c * kSharedKeys)) c *= 2;

@@ -21,7 +21,9 @@ cudaError_t score_dispatch(int op, int mode, const ScoreVariant& v, const CUtens
 
 // ---- fp32 caches --------------------------------------------------------------------------------------------------
 // Plain fp32 FMA (tensor-core formats would round the products). A tile of 32 keys in shared memory; warp = packed rows
-// wid, wid + 8, ..; lane = key, so a row's statistics stay with the lane until the end of the piece.
+// wid, wid + 8, ..; lane = key, so a row's statistics stay with the lane until the end of the piece. Not tuned: a tile is loaded,
+// then multiplied, with nothing in flight meanwhile. 8 rows, 64 ragged sequences of up to 8192 keys, 8 KV heads of 128: the call
+// takes 387 us, 4.4 times its floor; one sequence of 700: 15.8.
 constexpr int kFThreads = 256;
 constexpr int kFRows = kMaxRows / (kFThreads / 32);   // rows per warp at most
 
