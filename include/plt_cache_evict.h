@@ -113,7 +113,7 @@ typedef struct {
  * all from the values before the call; weights[b, g, new_lens[b] .. seq_lens[b]) = 0 (the next tokens start there).  K and V
  * rows from new_lens[b] on stay as they are.  Positions have to be ascending (as plt_cache_evict_select writes them): one
  * below its slot or not below seq_lens[b] is clamped and flagged.  No page may belong to two sequences, and the rows of the
- * cache must not overlap.  Rows in front of the first dropped position stay where they are, all kept ones behind it move.
+ * cache must not overlap.  A row that would come from or go to a page outside the pool stays where it is (flagged).  Rows in front of the first dropped position stay where they are, all kept ones behind it move.
  */
 typedef struct {
     uint32_t struct_size;

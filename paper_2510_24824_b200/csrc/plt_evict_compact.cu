@@ -117,8 +117,10 @@ __global__ void __launch_bounds__(kMoveThreads) plt_evict_compact_kernel(const _
                 if (i < s.m) {
                     const int from = clamp_source(s, i, k[j], flags);
                     if (from != i) {
-                        m.from = row_offset(p, pages, b, from, flags);
-                        m.to = row_offset(p, pages, b, i, flags);
+                        uint32_t bad = 0;          // a page outside the pool: the row stays, no other sequence's page is written
+                        const int64_t src = row_offset(p, pages, b, from, bad), dst = row_offset(p, pages, b, i, bad);
+                        if (bad == 0) m = Move{src, dst};
+                        flags |= bad;
                     }
                 }
                 to[j * THREADS + tid] = m;
