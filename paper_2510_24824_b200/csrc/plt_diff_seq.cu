@@ -14,8 +14,8 @@
 // softmax warp works on one half while the products on the other half of the same map run: the P of a half is consumed and
 // the next tile's scores of that half are written behind it in the tensor core's own order. With whole 128-key score tiles
 // the chain scores -> softmax -> P V -> next scores of a map was open at every link, and the two maps' chains alone filled
-// 40 % of the exponential unit's time (5000 rows, 32 heads: 534 us; in this order, with an issuer for each map, 394 to 428 us by
-// box, 718 to 779 TFLOP/s over the visible keys).
+// 40 % of the exponential unit's time (5000 rows, 32 heads: 534 us; in this order, with an issuer for each map, 394 to 428 us on
+// different devices, 718 to 779 TFLOP/s over the visible keys).
 //
 // The block owns both results of a row, so the epilogue takes y_1 - lambda y_2 and the norm over the head's 128 elements in
 // fp32 from the two accumulators, and neither map reaches memory. Steps, masks and windows of loops 2..L are those of

@@ -11,8 +11,8 @@
 // 2.1x the time on pages of 64 tokens: integer divisions.) A chunk is 512 rows.
 //
 // Bound: HBM, reads and writes mixed: 64 sequences of 8192, 4096 kept, 8 heads of 128 bf16: 370 us, 0.91 of the copy rate, in pages
-// of 64 tokens 392, 0.86; ragged lengths, half of which keep everything: 85 us, 0.68. One sequence of 5000, 1024 kept: 8.3 to 10.7
-// us by box, the chain lengths -> positions -> pages -> rows. What moves is what lies behind the first dropped position: a cache one
+// of 64 tokens 392, 0.86; ragged lengths, half of which keep everything: 85 us, 0.68. One sequence of 5000, 1024 kept: 8.3 to 8.6
+// us, the chain lengths -> positions -> pages -> rows. What moves is what lies behind the first dropped position: a cache one
 // position over its budget moves half of its rows on average (64 sequences of 4097, 4096 kept: 249 us). (Blocks of 1024 threads with 1024 rows a chunk: 8.6 there, 468 us on the full batch.)
 #include "plt_common.cuh"
 #include "plt_evict.h"
