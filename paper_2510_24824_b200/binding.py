@@ -20,6 +20,7 @@ PLT_PATH_AUTO, PLT_PATH_WARP_MMA, PLT_PATH_TCGEN05 = 0, 1, 2
 PLT_KV_SAME, PLT_KV_E4M3 = 0, 1
 PLT_DEV_SEQ_LEN_CLAMPED, PLT_DEV_PAGE_ID_CLAMPED, PLT_DEV_WAIT_TIMEOUT, PLT_DEV_WIN_LEN_CLAMPED = 1, 2, 4, 8
 PLT_DEV_KEEP_CLAMPED = 16
+PLT_DEV_TOKEN_OUT_OF_RANGE, PLT_DEV_NO_PROBABILITY = 32, 64
 
 EXPORTS = (
     "plt_decode_attn_create", "plt_decode_attn_run", "plt_decode_attn_run_host", "plt_decode_attn_check",
@@ -33,6 +34,7 @@ DIFF_EXPORTS = tuple(f"plt_diff_attn_{n}" for n in ("create", "run", "step", "ch
     tuple(f"plt_diff_seq_attn_{n}" for n in ("create", "run", "check", "destroy", "last_error"))
 EVICT_EXPORTS = tuple(f"plt_cache_evict_{n}" for n in ("create", "weights", "select", "compact", "check", "destroy",
                                                       "last_error", "workspace_bytes"))
+VERIFY_EXPORTS = tuple(f"plt_draft_verify_{n}" for n in ("create", "run", "check", "destroy", "last_error", "workspace_bytes"))
 PLT_NO_ALLOC_SCRATCH_BYTES = 16 << 20
 
 
@@ -157,6 +159,24 @@ class EvictCompactArgs(ctypes.Structure):
     ]
 
 
+class VerifyConfig(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("max_batch", ctypes.c_int32),
+        ("max_drafts", ctypes.c_int32), ("vocab", ctypes.c_int32), ("device", ctypes.c_int32),
+    ]
+
+
+class VerifyArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("batch", ctypes.c_int32), ("target_probs", ctypes.c_void_p),
+        ("target_stride_b", ctypes.c_int64), ("target_stride_j", ctypes.c_int64), ("draft_probs", ctypes.c_void_p),
+        ("draft_stride_b", ctypes.c_int64), ("draft_stride_j", ctypes.c_int64), ("draft_tokens", ctypes.c_void_p),
+        ("draft_lens", ctypes.c_void_p), ("accept_u", ctypes.c_void_p), ("sample_u", ctypes.c_void_p),
+        ("tokens", ctypes.c_void_p), ("num_accepted", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+        ("new_lens", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -194,17 +214,20 @@ def load_library() -> ctypes.CDLL:
                                            ctypes.POINTER(DiffWeights), ctypes.c_void_p]
         lib.plt_diff_seq_attn_create.argtypes = [ctypes.POINTER(DiffSeqConfig), ctypes.POINTER(h)]
         lib.plt_diff_seq_attn_run.argtypes = [h, ctypes.POINTER(SeqArgs), ctypes.POINTER(DiffWeights), ctypes.c_void_p]
+        lib.plt_draft_verify_create.argtypes = [ctypes.POINTER(VerifyConfig), ctypes.POINTER(h)]
+        lib.plt_draft_verify_workspace_bytes.argtypes = [ctypes.POINTER(VerifyConfig), ctypes.POINTER(ctypes.c_size_t)]
+        lib.plt_draft_verify_run.argtypes = [h, ctypes.POINTER(VerifyArgs), ctypes.c_void_p]
         lib.plt_cache_evict_create.argtypes = [ctypes.POINTER(EvictConfig), ctypes.POINTER(h)]
         lib.plt_cache_evict_workspace_bytes.argtypes = [ctypes.POINTER(EvictConfig), ctypes.POINTER(ctypes.c_size_t)]
         lib.plt_cache_evict_weights.argtypes = [h, ctypes.POINTER(EvictWeightsArgs), ctypes.c_void_p]
         lib.plt_cache_evict_select.argtypes = [h, ctypes.POINTER(EvictSelectArgs), ctypes.c_void_p]
         lib.plt_cache_evict_compact.argtypes = [h, ctypes.POINTER(EvictCompactArgs), ctypes.c_void_p]
-        for prefix in ("plt_diff_attn", "plt_diff_seq_attn", "plt_cache_evict"):
+        for prefix in ("plt_diff_attn", "plt_diff_seq_attn", "plt_cache_evict", "plt_draft_verify"):
             getattr(lib, prefix + "_check").argtypes = [h, ctypes.c_void_p, ctypes.POINTER(ctypes.c_uint32)]
             getattr(lib, prefix + "_destroy").argtypes = [h]
             getattr(lib, prefix + "_last_error").argtypes = [h]
             getattr(lib, prefix + "_last_error").restype = ctypes.c_char_p
-        for name in EXPORTS + DIFF_EXPORTS + EVICT_EXPORTS:
+        for name in EXPORTS + DIFF_EXPORTS + EVICT_EXPORTS + VERIFY_EXPORTS:
             if not name.endswith("_last_error"):
                 getattr(lib, name).restype = ctypes.c_int
         _lib = lib
@@ -614,3 +637,44 @@ def plt_cache_evict_check(handle, stream: int = 0) -> int:
 
 def plt_cache_evict_destroy(handle) -> None:
     load_library().plt_cache_evict_destroy(handle)
+
+
+# ---- draft verification (plt_draft_verify.h) -------------------------------------------------------------------------
+def make_verify_config(dtype, max_batch: int, max_drafts: int, vocab: int, device: int = 0) -> VerifyConfig:
+    c = VerifyConfig()
+    c.struct_size = ctypes.sizeof(VerifyConfig)
+    c.dtype = {"f32": PLT_F32, "bf16": PLT_BF16}.get(dtype, dtype)
+    c.max_batch, c.max_drafts, c.vocab, c.device = max_batch, max_drafts, vocab, device
+    return c
+
+
+def make_verify_args(batch: int, target_probs, draft_tokens, accept_u, sample_u, tokens, num_accepted, draft_probs=None,
+                     draft_lens=None, seq_lens=None, new_lens=None, target_strides=(0, 0),
+                     draft_strides=(0, 0)) -> VerifyArgs:
+    """Strides in elements between sequences and between rows; both 0: dense."""
+    return _fill(VerifyArgs(), batch,
+                 dict(target_probs=target_probs, draft_probs=draft_probs, draft_tokens=draft_tokens, draft_lens=draft_lens,
+                      accept_u=accept_u, sample_u=sample_u, tokens=tokens, num_accepted=num_accepted, seq_lens=seq_lens,
+                      new_lens=new_lens),
+                 dict(target_stride_b=int(target_strides[0]), target_stride_j=int(target_strides[1]),
+                      draft_stride_b=int(draft_strides[0]), draft_stride_j=int(draft_strides[1])))
+
+
+def plt_draft_verify_create(config: VerifyConfig) -> ctypes.c_void_p:
+    return _create("plt_draft_verify", config)
+
+
+def plt_draft_verify_workspace_bytes(config: VerifyConfig) -> int:
+    return _workspace_bytes("plt_draft_verify", config)
+
+
+def plt_draft_verify_run(handle, args: VerifyArgs, stream: int = 0) -> None:
+    _call("plt_draft_verify_run", handle, ctypes.byref(args), ctypes.c_void_p(stream))
+
+
+def plt_draft_verify_check(handle, stream: int = 0) -> int:
+    return _check("plt_draft_verify", handle, stream)
+
+
+def plt_draft_verify_destroy(handle) -> None:
+    load_library().plt_draft_verify_destroy(handle)

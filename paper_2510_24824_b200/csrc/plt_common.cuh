@@ -17,6 +17,9 @@ constexpr uint32_t kDevPageIdClamped = 2u;
 constexpr uint32_t kDevWaitTimeout = 4u;
 constexpr uint32_t kDevWinLenClamped = 8u;
 constexpr uint32_t kDevKeepClamped = 16u;
+constexpr uint32_t kDevTokenRange = 32u;
+constexpr uint32_t kDevNoProbability = 64u;
+constexpr uint32_t kDevGroupClamped = 128u;
 
 // Everything a kernel needs besides its TMA descriptors. Passed by value.
 struct Params {

@@ -384,6 +384,67 @@ class CacheEvict:
             pass
 
 
+class DraftVerify:
+    """Owns one plt_draft_verify handle: which drafted tokens of a multi-token step stand, and the token behind them.
+    Probabilities [B, K + 1, V] and [B, K, V] may be views whose vocabulary is dense; the other tensors are dense."""
+
+    def __init__(self, dtype: str, max_batch: int, max_drafts: int, vocab: int, device_index: int = 0):
+        self.handle = None
+        self.config = B.make_verify_config(dtype, max_batch, max_drafts, vocab, device=device_index)
+        self.handle = B.plt_draft_verify_create(self.config)
+
+    def _strides(self, name: str, t, n: int, rows: int):
+        c = self.config
+        want = torch.bfloat16 if c.dtype == B.PLT_BF16 else torch.float32
+        if t.dtype != want or t.dim() != 3 or t.shape[0] < n or tuple(t.shape[1:]) != (rows, c.vocab) or \
+                (c.vocab > 1 and t.stride(2) != 1) or (rows > 1 and t.stride(1) < c.vocab) or (n > 1 and t.stride(0) < c.vocab):
+            raise ValueError(f"{name}: {n} x {rows} rows of {c.vocab} dense elements of {want} are needed, not {tuple(t.shape)} "
+                             f"of {t.dtype} with strides {t.stride()}")
+        return t.stride(0), t.stride(1) if rows > 1 else max(t.stride(1), c.vocab)
+
+    def args(self, target, draft_tokens, accept_u, sample_u, tokens, num_accepted, draft=None, draft_lens=None, seq_lens=None,
+             new_lens=None):
+        K, n = self.config.max_drafts, draft_tokens.shape[0]
+        for name, t, dtype, per in (("draft_tokens", draft_tokens, torch.int32, K), ("accept_u", accept_u, torch.float32, K),
+                                    ("sample_u", sample_u, torch.float32, 1), ("tokens", tokens, torch.int32, K + 1),
+                                    ("num_accepted", num_accepted, torch.int32, 1), ("draft_lens", draft_lens, torch.int32, 1),
+                                    ("seq_lens", seq_lens, torch.int32, 1), ("new_lens", new_lens, torch.int32, 1)):
+            if t is not None:
+                _dense(name, t, dtype, n, per)
+        return B.make_verify_args(n, target, draft_tokens, accept_u, sample_u, tokens, num_accepted, draft_probs=draft,
+                                  draft_lens=draft_lens, seq_lens=seq_lens, new_lens=new_lens,
+                                  target_strides=self._strides("target", target, n, K + 1),
+                                  draft_strides=(0, 0) if draft is None else self._strides("draft", draft, n, K))
+
+    def run(self, target, draft_tokens, accept_u, sample_u, tokens, num_accepted, draft=None, draft_lens=None, seq_lens=None,
+            new_lens=None, stream: Optional[int] = None):
+        """target [B, K + 1, V], draft [B, K, V] or None -> tokens [B, K + 1], num_accepted [B] (and new_lens [B])."""
+        B.plt_draft_verify_run(self.handle, self.args(target, draft_tokens, accept_u, sample_u, tokens, num_accepted, draft,
+                                                      draft_lens, seq_lens, new_lens),
+                               torch.cuda.current_stream().cuda_stream if stream is None else stream)
+        return tokens, num_accepted
+
+    def check(self, stream: Optional[int] = None) -> int:
+        return B.plt_draft_verify_check(self.handle, torch.cuda.current_stream().cuda_stream if stream is None else stream)
+
+    def close(self):
+        if self.handle is not None:
+            B.plt_draft_verify_destroy(self.handle)
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 class LoopOrderAblation:
     """The ablation rows of Table 1 at kernel level, on the tensors of a device problem: the same loop-queries served
 
