@@ -20,7 +20,9 @@ PLT_PATH_AUTO, PLT_PATH_WARP_MMA, PLT_PATH_TCGEN05 = 0, 1, 2
 PLT_KV_SAME, PLT_KV_E4M3 = 0, 1
 PLT_DEV_SEQ_LEN_CLAMPED, PLT_DEV_PAGE_ID_CLAMPED, PLT_DEV_WAIT_TIMEOUT, PLT_DEV_WIN_LEN_CLAMPED = 1, 2, 4, 8
 PLT_DEV_KEEP_CLAMPED = 16
-PLT_DEV_TOKEN_OUT_OF_RANGE, PLT_DEV_NO_PROBABILITY = 32, 64
+PLT_DEV_TOKEN_OUT_OF_RANGE, PLT_DEV_NO_PROBABILITY, PLT_DEV_GROUP_CLAMPED = 32, 64, 128
+PLT_ROPE_HALF, PLT_ROPE_INTERLEAVED = 0, 1
+PLT_ROPE_PLAIN, PLT_ROPE_LINEAR, PLT_ROPE_BASE, PLT_ROPE_WAVELENGTH, PLT_ROPE_RAMP = range(5)
 
 EXPORTS = (
     "plt_decode_attn_create", "plt_decode_attn_run", "plt_decode_attn_run_host", "plt_decode_attn_check",
@@ -35,6 +37,7 @@ DIFF_EXPORTS = tuple(f"plt_diff_attn_{n}" for n in ("create", "run", "step", "ch
 EVICT_EXPORTS = tuple(f"plt_cache_evict_{n}" for n in ("create", "weights", "select", "compact", "check", "destroy",
                                                       "last_error", "workspace_bytes"))
 VERIFY_EXPORTS = tuple(f"plt_draft_verify_{n}" for n in ("create", "run", "check", "destroy", "last_error", "workspace_bytes"))
+ROPE_EXPORTS = tuple(f"plt_rope_{n}" for n in ("create", "frequencies", "step", "seq", "check", "destroy", "last_error"))
 PLT_NO_ALLOC_SCRATCH_BYTES = 16 << 20
 
 
@@ -177,6 +180,39 @@ class VerifyArgs(ctypes.Structure):
     ]
 
 
+class RopeConfig(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("kv_dtype", ctypes.c_int32),
+        ("max_batch", ctypes.c_int32), ("L", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+        ("d", ctypes.c_int32), ("max_seq_len", ctypes.c_int32), ("w", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("device", ctypes.c_int32), ("loop_offset", ctypes.POINTER(ctypes.c_int32)), ("q_len", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+        ("original_len", ctypes.c_int32), ("norm_eps", ctypes.c_float), ("attn_factor", ctypes.c_float),
+        ("theta", ctypes.c_double), ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+        ("inv_freq", ctypes.POINTER(ctypes.c_double)),
+    ]
+
+
+class RopeStepArgs(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("batch", ctypes.c_int32)] + \
+        [(n, ctypes.c_void_p) for n in ("q", "k_new", "v_new")] + \
+        [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + \
+        [(n, ctypes.c_void_p) for n in ("q_gain", "k_gain", "q_out", "k_cache", "v_cache")] + \
+        [(n, ctypes.c_int64) for n in ("kv_stride_b", "kv_stride_n", "kv_stride_h")] + \
+        [(n, ctypes.c_void_p) for n in ("seq_lens", "prefix_lens", "page_table")] + \
+        [(n, ctypes.c_int32) for n in ("max_pages", "num_pool_pages")] + \
+        [(n, ctypes.c_void_p) for n in ("k_win", "v_win", "k_scale", "v_scale", "w_gate", "b_gate", "gate_logits")]
+
+
+class RopeSeqArgs(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("batch", ctypes.c_int32), ("rows", ctypes.c_int32)] + \
+        [(n, ctypes.c_void_p) for n in ("q", "k_share", "v_share", "k_loc", "q_out", "k_share_out", "k_loc_out", "q_gain",
+                                        "k_gain", "seq_lens", "start", "prefix_lens", "k_cache", "v_cache")] + \
+        [(n, ctypes.c_int64) for n in ("kv_stride_b", "kv_stride_n", "kv_stride_h")] + \
+        [("page_table", ctypes.c_void_p), ("max_pages", ctypes.c_int32), ("num_pool_pages", ctypes.c_int32)] + \
+        [(n, ctypes.c_void_p) for n in ("k_scale", "v_scale")]
+
+
 _lib = None
 
 
@@ -214,6 +250,10 @@ def load_library() -> ctypes.CDLL:
                                            ctypes.POINTER(DiffWeights), ctypes.c_void_p]
         lib.plt_diff_seq_attn_create.argtypes = [ctypes.POINTER(DiffSeqConfig), ctypes.POINTER(h)]
         lib.plt_diff_seq_attn_run.argtypes = [h, ctypes.POINTER(SeqArgs), ctypes.POINTER(DiffWeights), ctypes.c_void_p]
+        lib.plt_rope_create.argtypes = [ctypes.POINTER(RopeConfig), ctypes.POINTER(h)]
+        lib.plt_rope_frequencies.argtypes = [ctypes.POINTER(RopeConfig), ctypes.POINTER(ctypes.c_double)]
+        lib.plt_rope_step.argtypes = [h, ctypes.POINTER(RopeStepArgs), ctypes.c_void_p]
+        lib.plt_rope_seq.argtypes = [h, ctypes.POINTER(RopeSeqArgs), ctypes.c_void_p]
         lib.plt_draft_verify_create.argtypes = [ctypes.POINTER(VerifyConfig), ctypes.POINTER(h)]
         lib.plt_draft_verify_workspace_bytes.argtypes = [ctypes.POINTER(VerifyConfig), ctypes.POINTER(ctypes.c_size_t)]
         lib.plt_draft_verify_run.argtypes = [h, ctypes.POINTER(VerifyArgs), ctypes.c_void_p]
@@ -222,12 +262,12 @@ def load_library() -> ctypes.CDLL:
         lib.plt_cache_evict_weights.argtypes = [h, ctypes.POINTER(EvictWeightsArgs), ctypes.c_void_p]
         lib.plt_cache_evict_select.argtypes = [h, ctypes.POINTER(EvictSelectArgs), ctypes.c_void_p]
         lib.plt_cache_evict_compact.argtypes = [h, ctypes.POINTER(EvictCompactArgs), ctypes.c_void_p]
-        for prefix in ("plt_diff_attn", "plt_diff_seq_attn", "plt_cache_evict", "plt_draft_verify"):
+        for prefix in ("plt_diff_attn", "plt_diff_seq_attn", "plt_cache_evict", "plt_draft_verify", "plt_rope"):
             getattr(lib, prefix + "_check").argtypes = [h, ctypes.c_void_p, ctypes.POINTER(ctypes.c_uint32)]
             getattr(lib, prefix + "_destroy").argtypes = [h]
             getattr(lib, prefix + "_last_error").argtypes = [h]
             getattr(lib, prefix + "_last_error").restype = ctypes.c_char_p
-        for name in EXPORTS + DIFF_EXPORTS + EVICT_EXPORTS + VERIFY_EXPORTS:
+        for name in EXPORTS + DIFF_EXPORTS + EVICT_EXPORTS + VERIFY_EXPORTS + ROPE_EXPORTS:
             if not name.endswith("_last_error"):
                 getattr(lib, name).restype = ctypes.c_int
         _lib = lib
@@ -678,3 +718,85 @@ def plt_draft_verify_check(handle, stream: int = 0) -> int:
 
 def plt_draft_verify_destroy(handle) -> None:
     load_library().plt_draft_verify_destroy(handle)
+
+
+# ---- norm and rotation of queries and keys (plt_rope.h) ---------------------------------------------------------------
+_SCALINGS = {"none": PLT_ROPE_PLAIN, "linear": PLT_ROPE_LINEAR, "base": PLT_ROPE_BASE, "wavelength": PLT_ROPE_WAVELENGTH,
+             "ramp": PLT_ROPE_RAMP}
+
+
+def make_rope_config(dtype, max_batch: int, L: int, Hq: int, Hkv: int, d: int, max_seq_len: int, w: int, page_size: int = 0,
+                     device: int = 0, loop_offset: Optional[Sequence[int]] = None, kv_dtype=0, q_len: int = 0,
+                     rotary_dim: int = 0, layout="half", theta: float = 10000.0, scaling="none", factor: float = 1.0,
+                     low: float = 1.0, high: float = 4.0, original_len: int = 0, attn_factor: float = 0.0,
+                     norm_eps: float = 1e-6, inv_freq: Optional[Sequence[float]] = None) -> RopeConfig:
+    c = RopeConfig()
+    c.struct_size = ctypes.sizeof(RopeConfig)
+    c.dtype = {"f32": PLT_F32, "bf16": PLT_BF16}.get(dtype, dtype)
+    c.kv_dtype = {"": PLT_KV_SAME, "e4m3": PLT_KV_E4M3}.get(kv_dtype, kv_dtype)
+    c.max_batch, c.L, c.Hq, c.Hkv, c.d, c.max_seq_len, c.w = max_batch, L, Hq, Hkv, d, max_seq_len, w
+    c.page_size, c.device, c.q_len, c.rotary_dim = page_size, device, q_len, rotary_dim
+    c.layout = {"half": PLT_ROPE_HALF, "interleaved": PLT_ROPE_INTERLEAVED}.get(layout, layout)
+    c.scaling = _SCALINGS.get(scaling, scaling)
+    c.original_len, c.norm_eps, c.attn_factor = original_len, norm_eps, attn_factor
+    c.theta, c.factor, c.low, c.high = theta, factor, low, high
+    _offsets(c, loop_offset)
+    if inv_freq is not None:
+        c._keep_freq = (ctypes.c_double * len(inv_freq))(*[float(x) for x in inv_freq])
+        c.inv_freq = ctypes.cast(c._keep_freq, ctypes.POINTER(ctypes.c_double))
+    return c
+
+
+def make_rope_step_args(batch: int, q, k_new, v_new, q_out, k_cache, v_cache, seq_lens, prefix_lens=None, q_gain=None,
+                        k_gain=None, page_table=None, max_pages: int = 0, num_pool_pages: int = 0, k_win=None, v_win=None,
+                        k_scale=None, v_scale=None, w_gate=None, b_gate=None, gate_logits=None, row_strides=(0, 0, 0),
+                        kv_strides=(0, 0, 0)) -> RopeStepArgs:
+    """row_strides: elements between the rows (b, l, token) of q, k_new and v_new; 0: dense."""
+    return _fill(RopeStepArgs(), batch,
+                 dict(q=q, k_new=k_new, v_new=v_new, q_out=q_out, k_cache=k_cache, v_cache=v_cache, seq_lens=seq_lens,
+                      prefix_lens=prefix_lens, q_gain=q_gain, k_gain=k_gain, page_table=page_table, k_win=k_win, v_win=v_win,
+                      k_scale=k_scale, v_scale=v_scale, w_gate=w_gate, b_gate=b_gate, gate_logits=gate_logits),
+                 dict(_strides(kv_strides), q_stride=int(row_strides[0]), k_stride=int(row_strides[1]),
+                      v_stride=int(row_strides[2]), max_pages=max_pages, num_pool_pages=num_pool_pages))
+
+
+def make_rope_seq_args(batch: int, rows: int, q, k_share, seq_lens, q_out, k_share_out=None, k_loc=None, k_loc_out=None,
+                       q_gain=None, k_gain=None, start=None, prefix_lens=None, v_share=None, k_cache=None, v_cache=None,
+                       page_table=None, max_pages: int = 0, num_pool_pages: int = 0, k_scale=None, v_scale=None,
+                       kv_strides=(0, 0, 0)) -> RopeSeqArgs:
+    return _fill(RopeSeqArgs(), batch,
+                 dict(q=q, k_share=k_share, v_share=v_share, k_loc=k_loc, q_out=q_out, k_share_out=k_share_out,
+                      k_loc_out=k_loc_out, q_gain=q_gain, k_gain=k_gain, seq_lens=seq_lens, start=start,
+                      prefix_lens=prefix_lens, k_cache=k_cache, v_cache=v_cache, page_table=page_table, k_scale=k_scale,
+                      v_scale=v_scale),
+                 dict(_strides(kv_strides), rows=rows, max_pages=max_pages, num_pool_pages=num_pool_pages))
+
+
+def plt_rope_create(config: RopeConfig) -> ctypes.c_void_p:
+    return _create("plt_rope", config)
+
+
+def plt_rope_frequencies(config: RopeConfig) -> list:
+    """Radians a position of each pair that turns."""
+    lib, out = load_library(), (ctypes.c_double * 64)()
+    st = lib.plt_rope_frequencies(ctypes.byref(config), out)
+    if st != PLT_OK:
+        msg = lib.plt_rope_last_error(None)
+        raise PltError(st, msg.decode() if msg else "")
+    return list(out[: (config.rotary_dim or config.d) // 2])
+
+
+def plt_rope_step(handle, args: RopeStepArgs, stream: int = 0) -> None:
+    _call("plt_rope_step", handle, ctypes.byref(args), ctypes.c_void_p(stream))
+
+
+def plt_rope_seq(handle, args: RopeSeqArgs, stream: int = 0) -> None:
+    _call("plt_rope_seq", handle, ctypes.byref(args), ctypes.c_void_p(stream))
+
+
+def plt_rope_check(handle, stream: int = 0) -> int:
+    return _check("plt_rope", handle, stream)
+
+
+def plt_rope_destroy(handle) -> None:
+    load_library().plt_rope_destroy(handle)

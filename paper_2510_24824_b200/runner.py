@@ -384,6 +384,112 @@ class CacheEvict:
             pass
 
 
+class Rope:
+    """Owns one plt_rope handle sized for a problem: norm and rotation of queries and keys, with the caches of a DeviceProblem.
+    `rotation`: what make_rope_config takes of rotary_dim, layout, theta, scaling, factor, low, high, original_len, attn_factor,
+    norm_eps and inv_freq.  Gains are fp32 [d] or None; a tensor that a kernel would read otherwise than torch does is refused
+    with ValueError."""
+
+    def __init__(self, p, device_index: int = 0, max_batch: Optional[int] = None, q_len: int = 1, **rotation):
+        self.handle = None
+        self.config = B.make_rope_config(
+            p.dtype, max_batch or max(p.B, 1), p.L, p.Hq, p.Hkv, p.d, p.max_seq_len, p.w, page_size=p.page_size, device=device_index,
+            loop_offset=None if p.loop_offset is None else [int(x) for x in p.loop_offset], kv_dtype=p.kv_dtype, q_len=q_len,
+            **rotation)
+        self.handle = B.plt_rope_create(self.config)
+
+    def _act(self):
+        return torch.bfloat16 if self.config.dtype == B.PLT_BF16 else torch.float32
+
+    def _rows(self, name: str, t, n: int, heads: int) -> int:
+        """Elements between the rows (b, l, token) of t [B, L, q_len, heads, d], each row dense."""
+        c = self.config
+        rows, lead = (c.L, max(1, c.q_len)), t.shape[1:3] if t.dim() == 5 else ()
+        if t.dim() == 4 and c.q_len <= 1:
+            t, lead = t.unsqueeze(2), (t.shape[1], 1)
+        ok = t.dtype == self._act() and t.dim() == 5 and t.shape[0] >= n and tuple(lead) == rows and tuple(t.shape[3:]) == (heads, c.d) and \
+            (t.stride(4) == 1 and (heads == 1 or t.stride(3) == c.d))
+        if ok:
+            per = t.stride(2) if rows[1] > 1 else t.stride(1) if rows[0] > 1 else t.stride(0) if n > 1 else heads * c.d
+            ok = (rows[1] <= 1 or rows[0] <= 1 or t.stride(1) == rows[1] * per) and (n <= 1 or t.stride(0) == rows[0] * rows[1] * per)
+        if not ok:
+            raise ValueError(f"{name}: rows of {heads} x {c.d} dense elements of {self._act()}, equally far apart, are needed, not "
+                             f"{tuple(t.shape)} of {t.dtype} with strides {t.stride()}")
+        return per
+
+    def _small(self, n: int, **tensors):
+        c = self.config
+        want = dict(q_gain=(torch.float32, 1, c.d), k_gain=(torch.float32, 1, c.d), w_gate=(torch.float32, c.Hq, c.d),
+                    b_gate=(torch.float32, c.Hq, 1), gate_logits=(torch.float32, n, (c.L - 1) * c.Hq), prefix_lens=(torch.int32, n, 1),
+                    seq_lens=(torch.int32, n, 1), start=(torch.int32, n, 1))
+        for name, t in tensors.items():
+            if t is not None:
+                dtype, lead, per = want[name]
+                _dense(name, t.view(1, -1) if name.endswith("gain") and t.is_contiguous() else t, dtype, lead, per)
+
+    def step_args(self, dp: DeviceProblem, q, k_new, v_new, q_out=None, q_gain=None, k_gain=None, prefix_lens=None, w_gate=None,
+                  b_gate=None, gate_logits=None, kv_strides=(0, 0, 0)):
+        p, c = dp.problem, self.config
+        q_out = dp.q if q_out is None else q_out
+        strides = [self._rows(name, t, p.B, h) for name, t, h in (("q", q, c.Hq), ("k_new", k_new, c.Hkv), ("v_new", v_new, c.Hkv))]
+        _dense("q_out", q_out, self._act(), p.B, c.L * max(1, c.q_len) * c.Hq * c.d)
+        if w_gate is not None and gate_logits is None:
+            gate_logits = dp.gate_logits
+        self._small(p.B, q_gain=q_gain, k_gain=k_gain, w_gate=w_gate, b_gate=b_gate, prefix_lens=prefix_lens,
+                    gate_logits=gate_logits if c.L > 1 else None)
+        return B.make_rope_step_args(p.B, q, k_new, v_new, q_out, dp.k_cache, dp.v_cache, dp.seq_lens, prefix_lens=prefix_lens, q_gain=q_gain,
+                                     k_gain=k_gain, page_table=dp.page_table, max_pages=p.max_pages, num_pool_pages=p.num_pool_pages,
+                                     k_win=dp.k_win if c.L > 1 else None, v_win=dp.v_win if c.L > 1 else None, k_scale=dp.k_scale,
+                                     v_scale=dp.v_scale, w_gate=w_gate, b_gate=b_gate, gate_logits=gate_logits if w_gate is not None else None,
+                                     row_strides=strides, kv_strides=kv_strides)
+
+    def step(self, dp: DeviceProblem, q, k_new, v_new, stream: Optional[int] = None, **more):
+        """Norms and turns q [B, L(, q_len), Hq, d] into dp.q (or q_out), and k_new, with v_new, into dp's caches and windows;
+        w_gate, b_gate: also the gates, into dp.gate_logits.  dp.seq_lens counts the tokens of this step."""
+        args = self.step_args(dp, q, k_new, v_new, **more)
+        B.plt_rope_step(self.handle, args, torch.cuda.current_stream().cuda_stream if stream is None else stream)
+        return dp.q if more.get("q_out") is None else more["q_out"]
+
+    def seq(self, q, k_share, seq_lens, q_out, k_share_out=None, k_loc=None, k_loc_out=None, q_gain=None, k_gain=None, start=None,
+            prefix_lens=None, v_share=None, dp: Optional[DeviceProblem] = None, kv_strides=(0, 0, 0), stream: Optional[int] = None):
+        """Norms and turns the rows of prompts, q [B, L, T, Hq, d] and k_share [B, T, Hkv, d]; with dp and v_share they also go
+        into its shared cache."""
+        c, n, rows = self.config, q.shape[0], q.shape[2]
+        for name, t, per in (("q", q, c.L * rows * c.Hq * c.d), ("q_out", q_out, c.L * rows * c.Hq * c.d), ("k_share", k_share, rows * c.Hkv * c.d),
+                             ("k_share_out", k_share_out, rows * c.Hkv * c.d), ("v_share", v_share, rows * c.Hkv * c.d),
+                             ("k_loc", k_loc, (c.L - 1) * rows * c.Hkv * c.d), ("k_loc_out", k_loc_out, (c.L - 1) * rows * c.Hkv * c.d)):
+            if t is not None:
+                _dense(name, t, self._act(), n, per)
+        self._small(n, q_gain=q_gain, k_gain=k_gain, seq_lens=seq_lens, start=start, prefix_lens=prefix_lens)
+        cache = {} if dp is None else dict(
+            k_cache=dp.k_cache, v_cache=dp.v_cache, page_table=dp.page_table, max_pages=dp.problem.max_pages,
+            num_pool_pages=dp.problem.num_pool_pages, k_scale=dp.k_scale, v_scale=dp.v_scale, kv_strides=kv_strides)
+        args = B.make_rope_seq_args(n, rows, q, k_share, seq_lens, q_out, k_share_out=k_share_out, k_loc=k_loc, k_loc_out=k_loc_out,
+                                    q_gain=q_gain, k_gain=k_gain, start=start, prefix_lens=prefix_lens, v_share=v_share, **cache)
+        B.plt_rope_seq(self.handle, args, torch.cuda.current_stream().cuda_stream if stream is None else stream)
+        return q_out
+
+    def check(self, stream: Optional[int] = None) -> int:
+        return B.plt_rope_check(self.handle, torch.cuda.current_stream().cuda_stream if stream is None else stream)
+
+    def close(self):
+        if self.handle is not None:
+            B.plt_rope_destroy(self.handle)
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 class DraftVerify:
     """Owns one plt_draft_verify handle: which drafted tokens of a multi-token step stand, and the token behind them.
     Probabilities [B, K + 1, V] and [B, K, V] may be views whose vocabulary is dense; the other tensors are dense."""
