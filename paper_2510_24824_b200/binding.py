@@ -38,6 +38,7 @@ EVICT_EXPORTS = tuple(f"plt_cache_evict_{n}" for n in ("create", "weights", "sel
                                                       "last_error", "workspace_bytes"))
 VERIFY_EXPORTS = tuple(f"plt_draft_verify_{n}" for n in ("create", "run", "check", "destroy", "last_error", "workspace_bytes"))
 ROPE_EXPORTS = tuple(f"plt_rope_{n}" for n in ("create", "frequencies", "step", "seq", "check", "destroy", "last_error"))
+PREFIX_EXPORTS = tuple(f"plt_prefix_attn_{n}" for n in ("create", "run", "check", "destroy", "last_error", "workspace_bytes"))
 PLT_NO_ALLOC_SCRATCH_BYTES = 16 << 20
 
 
@@ -180,6 +181,26 @@ class VerifyArgs(ctypes.Structure):
     ]
 
 
+class PrefixConfig(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("max_batch", ctypes.c_int32),
+        ("L", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("max_seq_len", ctypes.c_int32), ("w", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("sm_scale", ctypes.c_float), ("device", ctypes.c_int32), ("loop_offset", ctypes.POINTER(ctypes.c_int32)),
+        ("kernel_path", ctypes.c_int32), ("kv_dtype", ctypes.c_int32), ("q_len", ctypes.c_int32),
+        ("typical_seq_len", ctypes.c_int32), ("max_prefix_len", ctypes.c_int32), ("max_groups", ctypes.c_int32),
+    ]
+
+
+class PrefixArgs(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("num_groups", ctypes.c_int32), ("group_begin", ctypes.c_void_p),
+        ("prefix_lens", ctypes.c_void_p), ("k_prefix", ctypes.c_void_p), ("v_prefix", ctypes.c_void_p),
+        ("stride_g", ctypes.c_int64), ("stride_n", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+        ("page_table", ctypes.c_void_p), ("max_pages", ctypes.c_int32),
+    ]
+
+
 class RopeConfig(ctypes.Structure):
     _fields_ = [
         ("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("kv_dtype", ctypes.c_int32),
@@ -250,6 +271,9 @@ def load_library() -> ctypes.CDLL:
                                            ctypes.POINTER(DiffWeights), ctypes.c_void_p]
         lib.plt_diff_seq_attn_create.argtypes = [ctypes.POINTER(DiffSeqConfig), ctypes.POINTER(h)]
         lib.plt_diff_seq_attn_run.argtypes = [h, ctypes.POINTER(SeqArgs), ctypes.POINTER(DiffWeights), ctypes.c_void_p]
+        lib.plt_prefix_attn_create.argtypes = [ctypes.POINTER(PrefixConfig), ctypes.POINTER(h)]
+        lib.plt_prefix_attn_workspace_bytes.argtypes = [ctypes.POINTER(PrefixConfig), ctypes.POINTER(ctypes.c_size_t)]
+        lib.plt_prefix_attn_run.argtypes = [h, ctypes.POINTER(Args), ctypes.POINTER(PrefixArgs), ctypes.c_void_p]
         lib.plt_rope_create.argtypes = [ctypes.POINTER(RopeConfig), ctypes.POINTER(h)]
         lib.plt_rope_frequencies.argtypes = [ctypes.POINTER(RopeConfig), ctypes.POINTER(ctypes.c_double)]
         lib.plt_rope_step.argtypes = [h, ctypes.POINTER(RopeStepArgs), ctypes.c_void_p]
@@ -262,12 +286,13 @@ def load_library() -> ctypes.CDLL:
         lib.plt_cache_evict_weights.argtypes = [h, ctypes.POINTER(EvictWeightsArgs), ctypes.c_void_p]
         lib.plt_cache_evict_select.argtypes = [h, ctypes.POINTER(EvictSelectArgs), ctypes.c_void_p]
         lib.plt_cache_evict_compact.argtypes = [h, ctypes.POINTER(EvictCompactArgs), ctypes.c_void_p]
-        for prefix in ("plt_diff_attn", "plt_diff_seq_attn", "plt_cache_evict", "plt_draft_verify", "plt_rope"):
+        for prefix in ("plt_diff_attn", "plt_diff_seq_attn", "plt_cache_evict", "plt_draft_verify", "plt_rope",
+                       "plt_prefix_attn"):
             getattr(lib, prefix + "_check").argtypes = [h, ctypes.c_void_p, ctypes.POINTER(ctypes.c_uint32)]
             getattr(lib, prefix + "_destroy").argtypes = [h]
             getattr(lib, prefix + "_last_error").argtypes = [h]
             getattr(lib, prefix + "_last_error").restype = ctypes.c_char_p
-        for name in EXPORTS + DIFF_EXPORTS + EVICT_EXPORTS + VERIFY_EXPORTS + ROPE_EXPORTS:
+        for name in EXPORTS + DIFF_EXPORTS + EVICT_EXPORTS + VERIFY_EXPORTS + ROPE_EXPORTS + PREFIX_EXPORTS:
             if not name.endswith("_last_error"):
                 getattr(lib, name).restype = ctypes.c_int
         _lib = lib
@@ -800,3 +825,51 @@ def plt_rope_check(handle, stream: int = 0) -> int:
 
 def plt_rope_destroy(handle) -> None:
     load_library().plt_rope_destroy(handle)
+
+
+# ---- shared prefixes (plt_prefix_attn.h) -------------------------------------------------------------------------------
+def make_prefix_config(dtype, max_batch: int, L: int, Hq: int, Hkv: int, d: int, max_seq_len: int, w: int,
+                       max_prefix_len: int, max_groups: int = 1, page_size: int = 0, sm_scale: float = 0.0, device: int = 0,
+                       loop_offset: Optional[Sequence[int]] = None, kernel_path: int = 0, kv_dtype=0, q_len: int = 0,
+                       typical_seq_len: int = 0) -> PrefixConfig:
+    c = PrefixConfig()
+    c.struct_size = ctypes.sizeof(PrefixConfig)
+    c.dtype = {"f32": PLT_F32, "bf16": PLT_BF16}.get(dtype, dtype)
+    c.max_batch, c.L, c.Hq, c.Hkv, c.d = max_batch, L, Hq, Hkv, d
+    c.max_seq_len, c.w, c.page_size, c.sm_scale, c.device = max_seq_len, w, page_size, sm_scale, device
+    c.kernel_path, c.kv_dtype = kernel_path, {"": PLT_KV_SAME, "e4m3": PLT_KV_E4M3}.get(kv_dtype, kv_dtype)
+    c.q_len, c.typical_seq_len, c.max_prefix_len, c.max_groups = q_len, typical_seq_len, max_prefix_len, max_groups
+    _offsets(c, loop_offset)
+    return c
+
+
+def make_prefix_args(num_groups: int, group_begin, prefix_lens, k_prefix=None, v_prefix=None, page_table=None,
+                     max_pages: int = 0, strides=(0, 0, 0)) -> PrefixArgs:
+    """strides: elements between prefixes, tokens and heads of contiguous prefixes; all 0: dense."""
+    a = PrefixArgs()
+    a.struct_size, a.num_groups, a.max_pages = ctypes.sizeof(PrefixArgs), num_groups, max_pages
+    a.group_begin, a.prefix_lens, a.k_prefix, a.v_prefix, a.page_table = (
+        _ptr(x) for x in (group_begin, prefix_lens, k_prefix, v_prefix, page_table))
+    a.stride_g, a.stride_n, a.stride_h = (int(s) for s in strides)
+    a._keep = (group_begin, prefix_lens, k_prefix, v_prefix, page_table)
+    return a
+
+
+def plt_prefix_attn_create(config: PrefixConfig) -> ctypes.c_void_p:
+    return _create("plt_prefix_attn", config)
+
+
+def plt_prefix_attn_workspace_bytes(config: PrefixConfig) -> int:
+    return _workspace_bytes("plt_prefix_attn", config)
+
+
+def plt_prefix_attn_run(handle, args: Args, prefix: PrefixArgs, stream: int = 0) -> None:
+    _call("plt_prefix_attn_run", handle, ctypes.byref(args), ctypes.byref(prefix), ctypes.c_void_p(stream))
+
+
+def plt_prefix_attn_check(handle, stream: int = 0) -> int:
+    return _check("plt_prefix_attn", handle, stream)
+
+
+def plt_prefix_attn_destroy(handle) -> None:
+    load_library().plt_prefix_attn_destroy(handle)

@@ -52,6 +52,8 @@ struct Params {
     int32_t qsplit;            // 1: differential heads. Every head of q contributes two packed rows, one per half of its d
                                // elements (the other half read as zero); Hq and G then count those rows, so the head of
                                // packed row i is i >> 1 and its half i & 1
+    int32_t win_free;          // 1: win_lens holds for loops that see no key of the shared cache too (the keys in front of it
+                               // lie in a prefix of their own)
     float scale_log2;          // sm_scale * log2(e)
     int32_t delta[kMaxLoops];  // per-loop causal offset
 };
@@ -91,7 +93,7 @@ __device__ __forceinline__ void seq_plan_step(const Params& p, int b, int32_t n,
         s.cmax = c > s.cmax ? c : s.cmax;
         if (l >= 1) {
             int32_t wl = c < p.w ? c : p.w;
-            if (p.win_lens != nullptr && c > 0) {
+            if (p.win_lens != nullptr && (c > 0 || p.win_free)) {
                 wl = p.win_lens[b * (p.L - 1) + (l - 1)];
                 if (wl < 0 || wl > p.w) {
                     flags |= kDevWinLenClamped;

@@ -12,6 +12,7 @@
 #include <new>
 
 #include "plt_host.h"
+#include "plt_prefix.h"
 
 using namespace plt;
 
@@ -231,21 +232,27 @@ void place_workspace(plt_decode_attn* h, const plt_decode_attn_config* c, void* 
     }
 }
 
-plt_status encode_map(plt_decode_attn_t h, int idx, const void* base, int es, int D, int64_t d1, int64_t d2, int64_t d3,
-                      int64_t s1, int64_t s2, int64_t s3, int box_keys, int box_heads) {
-    MapKey key{base, s1, s2, s3, d1, d2, d3};
-    if (h->map_valid[idx] && h->keys[idx] == key) return PLT_OK;
+// Map of rows of D elements, [d3][d2][d1][D] with strides s3, s2, s1 in elements, boxes of 128-byte wide rows.
+plt_status encode_rows(plt_decode_attn_t h, CUtensorMap* map, const void* base, int es, int D, int64_t d1, int64_t d2, int64_t d3,
+                       int64_t s1, int64_t s2, int64_t s3, int box_keys, int box_heads) {
     cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)d1, (cuuint64_t)d2, (cuuint64_t)d3};
     cuuint64_t strides[3] = {(cuuint64_t)(s1 * es), (cuuint64_t)(s2 * es), (cuuint64_t)(s3 * es)};
     cuuint32_t box[4] = {(cuuint32_t)(128 / es), (cuuint32_t)box_keys, (cuuint32_t)box_heads, 1u};   // 128-byte rows
     cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
-    CUresult r = h->encode(&h->maps[idx], es == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box,
+    CUresult r = h->encode(map, es == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box,
                            estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        h->map_valid[idx] = false;
-        return fail(h, PLT_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d for tensor %d", (int)r, idx);
-    }
+    if (r != CUDA_SUCCESS) return fail(h, PLT_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+    return PLT_OK;
+}
+
+plt_status encode_map(plt_decode_attn_t h, int idx, const void* base, int es, int D, int64_t d1, int64_t d2, int64_t d3,
+                      int64_t s1, int64_t s2, int64_t s3, int box_keys, int box_heads) {
+    MapKey key{base, s1, s2, s3, d1, d2, d3};
+    if (h->map_valid[idx] && h->keys[idx] == key) return PLT_OK;
+    h->map_valid[idx] = false;
+    const plt_status s = encode_rows(h, &h->maps[idx], base, es, D, d1, d2, d3, s1, s2, s3, box_keys, box_heads);
+    if (s != PLT_OK) return s;
     h->keys[idx] = key;
     h->map_valid[idx] = true;
     return PLT_OK;
@@ -503,7 +510,7 @@ plt_status decode_create(const plt_decode_attn_config* config, int qsplit, plt_d
 
 namespace {
 plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cuda_stream,
-                    const plt_decode_attn_step_args* step, const DiffTail* tail);
+                    const plt_decode_attn_step_args* step, const DiffTail* tail, PrefixRun* prefix = nullptr);
 plt_decode_attn* no_alloc_handle_of_current_device();
 }
 
@@ -534,6 +541,15 @@ plt_status decode_step(plt_decode_attn_t h, const plt_decode_attn_args* a, const
     return run_impl(h, &a2, cuda_stream, step, tail);
 }
 
+plt_status decode_run_prefix(plt_decode_attn_t h, const plt_decode_attn_args* a, PrefixRun* prefix, void* cuda_stream) {
+    return run_impl(h, a, cuda_stream, nullptr, nullptr, prefix);
+}
+
+plt_status decode_encode_rows(plt_decode_attn_t h, CUtensorMap* map, const void* base, int es, int d, int64_t keys, int64_t heads,
+                              int64_t outer, int64_t sn, int64_t sh, int64_t so, int box_keys) {
+    return encode_rows(h, map, base, es, d, keys, heads, outer, sn, sh, so, box_keys, 1);
+}
+
 plt_status decode_error(plt_decode_attn_t h, plt_status code, const char* what) { return fail(h, code, "%s", what); }
 int decode_device(plt_decode_attn_t h) { return h->cfg.device; }
 
@@ -558,7 +574,7 @@ PLT_API plt_status plt_decode_attn_step(plt_decode_attn_t h, const plt_decode_at
 
 namespace {
 plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cuda_stream,
-                    const plt_decode_attn_step_args* step, const DiffTail* tail) {
+                    const plt_decode_attn_step_args* step, const DiffTail* tail, PrefixRun* prefix) {
     if (!h) return fail(nullptr, PLT_ERR_INVALID_ARG, "handle is NULL");
     if (!a) return fail(h, PLT_ERR_INVALID_ARG, "args is NULL");
     if (a->struct_size != sizeof(plt_decode_attn_args))
@@ -620,6 +636,31 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
 
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     cudaError_t e;
+    if (prefix) {
+        // The prefixes first; the kernels below then take the lengths that each sequence holds itself, and the windows'.
+        PrefixParams& pp = prefix->pp;
+        pp.q = a->q; pp.seq_lens = a->seq_lens; pp.win_lens = c.L > 1 ? a->win_lens : nullptr;
+        pp.k_scale = p.k_scale; pp.v_scale = p.v_scale;
+        pp.B = p.B; pp.L = p.L; pp.Qn = p.Qn; pp.Hq = p.Hq; pp.Hkv = p.Hkv; pp.G = p.G; pp.R = p.R; pp.d = p.d; pp.w = p.w;
+        pp.max_seq_len = p.max_seq_len; pp.page_size = p.page_size; pp.num_pool_pages = p.num_pool_pages;
+        pp.scale_log2 = p.scale_log2;
+        for (int l = 0; l < kMaxLoops; ++l) pp.delta[l] = p.delta[l];
+        if (c.page_size > 0 && pp.groups > 0) {
+            plt_status s = encode_rows(h, &prefix->maps[0], a->k_cache, es, c.d, c.page_size, c.Hkv, a->num_pool_pages, sn, sh, sb, pp.kbox, 1);
+            if (s == PLT_OK)
+                s = encode_rows(h, &prefix->maps[1], a->v_cache, es, c.d, c.page_size, c.Hkv, a->num_pool_pages, sn, sh, sb, pp.kbox, 1);
+            if (s != PLT_OK) return s;
+        }
+        e = launch_prefix_plan(pp, stream);
+        if (e != cudaSuccess) return cuda_fail(h, "launching the plan kernel", e);
+        if (pp.groups > 0) {
+            e = launch_prefix_main(prefix->maps, pp, prefix->fp8, stream);
+            if (e != cudaSuccess) return cuda_fail(h, "launching the prefix kernel", e);
+        }
+        p.seq_lens = pp.plan.own_lens;
+        p.win_lens = pp.plan.win_lens;
+        p.win_free = 1;
+    }
     if (step) {
         Params pre = p;
         pre.Hq >>= h->qsplit;   // the gate linear takes a head's whole row
@@ -665,7 +706,8 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
             e = launch_main_umma(h->maps, p, h->var.grid, h->var.smem, h->var.stages, h->kbox, h->wbox,
                                  c.loads_in_flight > 0 ? c.loads_in_flight : 2, stream);
         else
-            e = launch_main_bf16(h->var, h->maps, p, /*overlap=*/true, stream);
+            // without a prefix kernel in between, this one may not look at the plan's lengths before the plan kernel has ended
+            e = launch_main_bf16(h->var, h->maps, p, /*overlap=*/!prefix || prefix->pp.groups > 0, stream);
     } else {
         if (h->ev_begin) cudaEventRecord(h->ev_begin, stream);
         e = launch_main_f32(p, h->var.grid, h->var.smem, stream);
@@ -673,8 +715,9 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
     if (e != cudaSuccess) return cuda_fail(h, "launching the main kernel", e);
     if (h->ev_end) cudaEventRecord(h->ev_end, stream);
     // The merge kernel may set up while the main kernel drains, unless an event sits between the two launches.
-    e = tail ? launch_reduce_diff(p, *tail, h->bf16, /*overlap=*/h->ev_end == nullptr, stream)
-             : launch_reduce(p, h->bf16, /*overlap=*/h->ev_end == nullptr, stream);
+    if (prefix) e = launch_prefix_merge(p, prefix->pp, /*overlap=*/true, stream);
+    else e = tail ? launch_reduce_diff(p, *tail, h->bf16, /*overlap=*/h->ev_end == nullptr, stream)
+                  : launch_reduce(p, h->bf16, /*overlap=*/h->ev_end == nullptr, stream);
     if (e != cudaSuccess) return cuda_fail(h, "launching the merge kernel", e);
     return PLT_OK;
 }

@@ -167,7 +167,7 @@ __device__ __forceinline__ int e_cut(const Params& p, int n, int l) {
 __device__ __forceinline__ int e_wl(const Params& p, int b, int n, int l, uint32_t& flags) {
     const int c = e_cut(p, n, l);
     int wl = c < p.w ? c : p.w;
-    if (p.win_lens != nullptr && c > 0) {
+    if (p.win_lens != nullptr && (c > 0 || p.win_free)) {
         wl = p.win_lens[b * (p.L - 1) + (l - 1)];
         if (wl < 0 || wl > p.w) {
             flags |= kDevWinLenClamped;

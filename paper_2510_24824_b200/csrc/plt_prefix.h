@@ -1,0 +1,71 @@
+// Shared prefixes: what the host layer and the kernels of the prefix pass have in common.
+#pragma once
+#include "plt_host.h"
+
+namespace plt {
+
+constexpr int kMaxGroups = 1024;
+constexpr int kPrefixRows = 256;      // packed query rows of a unit: two tiles of 128
+constexpr int kPrefixTile = 128;      // keys of a tile
+constexpr int kPrefixLead = 2;        // line positions that stand for starting and finishing a unit's piece, in tiles
+
+// The plan that the plan kernel leaves for the others. A unit is (group, KV head, 256 packed rows); the units of a group lie
+// one after the other on a line of key tiles, each preceded by kPrefixLead positions, and the line is cut into equal ranges,
+// one for each block. A piece (a block's share of a unit) stores its partial in slot unit + block.
+struct PrefixPlan {
+    int32_t *begin;      // [groups + 1] first sequence of each group, clamped
+    int32_t *len;        // [groups] tokens of each prefix, clamped; 0 where the group is empty
+    int32_t *line;       // [groups + 1] first line position of each group's units
+    int32_t *unit;       // [groups + 1] first unit of each group
+    int32_t *own_lens;   // [max_batch] tokens that each sequence holds itself
+    int32_t *win_lens;   // [max_batch, L - 1] valid window slots of each loop
+};
+
+struct PrefixParams {
+    const void* q;                 // [B, L, Qn, Hq, d] bf16
+    const int32_t* seq_lens;       // [B], prefix counted
+    const int32_t* win_lens;       // [B, L - 1] or null: as the caller gave them
+    const int32_t* group_begin;    // as the caller gave them
+    const int32_t* prefix_lens;
+    const int32_t* page_table;     // [groups, max_pages]
+    const float *k_scale, *v_scale;
+    PrefixPlan plan;
+    float* acc;                    // [slots][2 tiles][d / 4][128 rows][4]: unnormalised sums of p * V
+    float* ml;                     // [slots][2 tiles][128 rows][2]: reference (log2 units; -inf: saw no key), sum of p
+    uint32_t* status;
+    int32_t groups, B, L, Qn, Hq, Hkv, G, R, d, w;
+    int32_t max_seq_len, max_prefix_len, page_size, max_pages, num_pool_pages, kbox;
+    int32_t blocks;                // of the prefix kernel
+    float scale_log2;
+    int32_t delta[kMaxLoops];
+};
+
+// What a run needs of the prefixes: filled by the public entry point, completed by the decode step's run.
+struct PrefixRun {
+    PrefixParams pp;
+    CUtensorMap maps[2];           // K, V of the prefixes
+    bool fp8;
+};
+
+size_t prefix_smem(int d, bool fp8);
+cudaError_t prefix_prepare(int d, bool fp8);
+cudaError_t launch_prefix_plan(const PrefixParams& pp, cudaStream_t stream);
+cudaError_t launch_prefix_main(const CUtensorMap maps[2], const PrefixParams& pp, bool fp8, cudaStream_t stream);
+cudaError_t launch_prefix_merge(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream);
+
+// plt_decode_attn_run with shared prefixes in front of the caches: `args` as the caller gave them.
+plt_status decode_run_prefix(plt_decode_attn_t h, const plt_decode_attn_args* args, PrefixRun* prefix, void* cuda_stream);
+// Encodes the map of a cache's rows: [outer][heads][keys][d] with strides in elements, boxes of `box_keys` keys of one head.
+plt_status decode_encode_rows(plt_decode_attn_t h, CUtensorMap* map, const void* base, int es, int d, int64_t keys, int64_t heads,
+                              int64_t outer, int64_t sn, int64_t sh, int64_t so, int box_keys);
+
+// Block of the prefix kernel that owns line position `pos` (T positions in all, C blocks).
+__host__ __device__ inline int prefix_block_of(int64_t pos, int64_t T, int C) { return (int)(((pos + 1) * C - 1) / T); }
+// Blocks that take part: at least kPrefixMinLine positions each.
+constexpr int kPrefixMinLine = 3;
+__host__ __device__ inline int prefix_blocks(int64_t T, int launched) {
+    const int64_t c = T / kPrefixMinLine;
+    return c < 1 ? 1 : c < launched ? (int)c : launched;
+}
+
+}  // namespace plt

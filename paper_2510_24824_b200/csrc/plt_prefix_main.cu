@@ -1,0 +1,689 @@
+// The pass over shared prefixes: the queries of a whole group of sequences against the group's one prefix, on the 5th-generation
+// tensor cores (tcgen05.mma, accumulators in tensor memory), and the plan that it walks.
+//
+// All sequences of a group, all loops, tokens and query heads of a KV head are rows of one matrix product:
+//
+//   S [128 rows x 128 keys] = Q . K_tile^T        A = packed query rows, B = K tile as TMA wrote it (K-major, 128-byte swizzle)
+//   O [128 rows x d]       += P . V_tile          A = probabilities in tensor memory (written over S), B = V tile (MN-major)
+//
+// with an online softmax whose reference maximum is moved only when a score outruns it by more than a few powers of two. A unit
+// is two such tiles of 128 rows, A and B, of one KV head. Where a unit has more than 128 rows, both tiles take every key tile, so
+// that each K/V tile in shared memory serves 256 rows; where it has fewer, A and B are the same rows and take the key tiles in
+// turn, so that one tile's products run beside the other's softmax either way. Blocks are persistent: each takes an equal range
+// of a line on which the units' key tiles lie one behind the other, and leaves unnormalised partials for the merge.
+//
+// Warp roles: warp 0 loads K and V tiles by TMA into a ring (pages: their ids one tile ahead); warp 1 issues the products and
+// owns the tensor memory; warps 2 and 3 turn E4M3 codes into f16 (exact) in a second ring, and idle otherwise; warps 4-7 and
+// 8-11 are the softmax of A and of B (thread = row), load their query rows and store the partials. A partial lies as
+// [d / 4][128 rows][4], so that a warp's store is 512 consecutive bytes.
+//
+// bf16 probabilities carry 8 bits, f16 ones (E4M3 caches) 11; their sum is taken before that rounding, in fp32.
+// Every wait is bounded and reports through the status word.
+#include <cuda_bf16.h>
+
+#include "plt_prefix.h"
+#include "plt_seq_util.cuh"
+
+namespace plt {
+namespace {
+
+template <int D, bool FP8>
+struct PCfg {
+    static constexpr int TILE = kPrefixTile * D * 2;              // a tile of 16-bit elements
+    static constexpr int RING = FP8 ? 3 : D == 64 ? 8 : 5;        // 16-bit tiles
+    static constexpr int RAW = FP8 ? 4 : 0;                       // tiles of codes
+    static constexpr int RAW_TILE = kPrefixTile * D;
+    // mbarriers
+    static constexpr int QFULL = 0, FULL = 2, EMPTY = FULL + RING, RFULL = EMPTY + RING, REMPTY = RFULL + RAW, SFULL = REMPTY + RAW,
+                         PFULL = SFULL + 2, ODONE = PFULL + 2, COUNT = ODONE + 2;
+    static constexpr size_t SMEM = 1024 + 2 * TILE + (size_t)RING * TILE + (size_t)RAW * RAW_TILE + COUNT * 8 + 64;
+};
+
+constexpr int kPThreads = 384;
+
+// Instruction descriptor: fp32 accumulate, A and B both bf16 or both f16, B majorness, N / 8, M / 16.
+__host__ __device__ constexpr uint32_t p_instr_desc(int N, int b_mn_major, bool f16) {
+    return (1u << 4) | (f16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+// ---- the walk over a block's range ------------------------------------------------------------------------------
+struct PPiece {
+    int g, unit, h, m;    // group, unit, KV head, 256-row block of the group
+    int t0, t1;           // key tiles
+    int len, rows;        // tokens of the prefix, packed rows of the group
+    bool wide;            // both tiles have rows of their own
+};
+struct PWalk {
+    int pos, hi, g;
+    __device__ __forceinline__ bool next(const PrefixParams& p, PPiece& pc) {
+        for (;;) {
+            if (pos >= hi) return false;
+            while (p.plan.line[g + 1] <= pos) ++g;
+            pc.g = g;
+            pc.len = p.plan.len[g];
+            pc.rows = (p.plan.begin[g + 1] - p.plan.begin[g]) * p.R;
+            const int per = (pc.len + kPrefixTile - 1) / kPrefixTile + kPrefixLead, nm = (pc.rows + kPrefixRows - 1) / kPrefixRows;
+            const int o = pos - p.plan.line[g], u = o / per, v0 = o - u * per;
+            const int end = min(pos + per - v0, hi), v1 = v0 + end - pos;
+            pos = end;
+            pc.t0 = max(v0 - kPrefixLead, 0);
+            pc.t1 = max(v1 - kPrefixLead, 0);
+            if (pc.t1 <= pc.t0) continue;
+            pc.unit = p.plan.unit[g] + u;
+            pc.h = u / nm;
+            pc.m = u - pc.h * nm;
+            pc.wide = pc.rows - pc.m * kPrefixRows > 128;
+            return true;
+        }
+    }
+};
+__device__ __forceinline__ PWalk walk_of_block(const PrefixParams& p) {
+    PWalk w;
+    const int64_t T = p.plan.line[p.groups];
+    const int C = prefix_blocks(T, p.blocks), c = blockIdx.x;
+    w.pos = w.hi = 0;
+    w.g = 0;
+    if (c < C && T > 0) {
+        w.pos = (int)(T * c / C);
+        w.hi = (int)(T * (c + 1) / C);
+        int lo = 0, hi = p.groups;          // line[lo] <= pos < line[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (p.plan.line[mid] <= w.pos) lo = mid; else hi = mid;
+        }
+        w.g = lo;
+    }
+    return w;
+}
+// Key tiles of a piece that tile x takes: every one, or every second.
+__device__ __forceinline__ int tiles_of(const PPiece& pc, int x) {
+    const int n = pc.t1 - pc.t0;
+    return pc.wide ? n : (n + 1 - x) >> 1;
+}
+
+template <int RING>
+struct Ring {
+    int slot = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void advance() {
+        if (++slot == RING) {
+            slot = 0;
+            parity ^= 1u;
+        }
+    }
+};
+
+// ---- softmax on 32 columns of a row ---------------------------------------------------------------------------------
+template <bool FULL, bool FP8>
+__device__ __forceinline__ void p_chunk(const uint32_t (&r)[32], int c, int lim, float2 sc2, float2 nm2, uint32_t* pk, float2& sum2,
+                                        uint32_t& pmax) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+        float2 t = __ffma2_rn(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), sc2, nm2);
+        if (!FULL) {
+            if (c * 32 + i >= lim) t.x = -INFINITY;
+            if (c * 32 + i + 1 >= lim) t.y = -INFINITY;
+        }
+        const float2 pr = make_float2(fast_exp2(t.x), fast_exp2(t.y));
+        sum2 = __fadd2_rn(sum2, pr);
+        const uint32_t h = FP8 ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);
+        pk[i / 2] = h;
+        asm("max.u16x2 %0, %0, %1;" : "+r"(pmax) : "r"(h));      // patterns of numbers that are not negative order like integers
+    }
+}
+// Largest pattern that needs no new reference: 2^8 in bf16; with f16 references lie 2^8 below the maximum, and 2^14 is the limit.
+template <bool FP8>
+constexpr uint32_t kBigPattern = FP8 ? 0x7400u : 0x4380u;
+template <bool FP8>
+constexpr float kBelow = FP8 ? 8.f : 0.f;
+
+template <bool FP8>
+__device__ __forceinline__ void p_pass(uint32_t tS, int lim, bool full, float scale, float mref, uint32_t (&pk)[64], float& lsum,
+                                       uint32_t& pbig) {
+    const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-mref, -mref);
+    float2 sum2 = make_float2(0.f, 0.f);
+    uint32_t pmax = 0;
+    uint32_t ra[32], rb[32];
+    tmem_ld32(tS, ra);
+    tmem_wait_ld();
+    tmem_ld32(tS + 32, rb);
+    if (full) p_chunk<true, FP8>(ra, 0, lim, sc2, nm2, &pk[0], sum2, pmax); else p_chunk<false, FP8>(ra, 0, lim, sc2, nm2, &pk[0], sum2, pmax);
+    tmem_wait_ld();
+    tmem_ld32(tS + 64, ra);
+    if (full) p_chunk<true, FP8>(rb, 1, lim, sc2, nm2, &pk[16], sum2, pmax); else p_chunk<false, FP8>(rb, 1, lim, sc2, nm2, &pk[16], sum2, pmax);
+    tmem_wait_ld();
+    tmem_ld32(tS + 96, rb);
+    if (full) p_chunk<true, FP8>(ra, 2, lim, sc2, nm2, &pk[32], sum2, pmax); else p_chunk<false, FP8>(ra, 2, lim, sc2, nm2, &pk[32], sum2, pmax);
+    tmem_wait_ld();
+    if (full) p_chunk<true, FP8>(rb, 3, lim, sc2, nm2, &pk[48], sum2, pmax); else p_chunk<false, FP8>(rb, 3, lim, sc2, nm2, &pk[48], sum2, pmax);
+    lsum = sum2.x + sum2.y;
+    pbig = max(pmax & 0xffffu, pmax >> 16);
+}
+__device__ __forceinline__ float p_row_max(uint32_t tS, int lim) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        uint32_t r[32];
+        tmem_ld32(tS + c * 32, r);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (c * 32 + i < lim) mx = fmaxf(mx, __uint_as_float(r[i]));
+    }
+    return mx;
+}
+template <int D>
+__device__ __forceinline__ void p_scale_o(uint32_t tO, float f) {
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+        uint32_t r[32];
+        tmem_ld32(tO + c * 32, r);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+        tmem_st32(tO + c * 32, r);
+    }
+    tmem_wait_st();
+}
+
+template <int D, bool FP8>
+__global__ void __launch_bounds__(kPThreads, 1)
+plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PrefixParams p) {
+    using C = PCfg<D, FP8>;
+    constexpr int HALVES = D / 64;
+    extern __shared__ uint8_t prefix_smem_raw[];
+    uint8_t* smem = (uint8_t*)(((uintptr_t)prefix_smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* q_smem = smem;                                        // [2][tile]
+    uint8_t* ring = smem + 2 * C::TILE;                            // [RING][tile]
+    uint8_t* raw = ring + (size_t)C::RING * C::TILE;               // [RAW][tile of codes]
+    uint64_t* bars = (uint64_t*)(raw + (size_t)C::RAW * C::RAW_TILE);
+    int32_t* s_ctl = (int32_t*)(bars + C::COUNT);                  // [0] abort flag, [1] tensor-memory base, [2] loads issued
+    volatile int* abort_flag = (volatile int*)s_ctl;
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+
+    if (tid == 0) {
+        s_ctl[0] = 0;
+        s_ctl[2] = 0;
+        for (int s = 0; s < C::RING; ++s) {
+            mbar_init(&bars[C::FULL + s], FP8 ? 2 : 1);
+            mbar_init(&bars[C::EMPTY + s], 1);
+        }
+        for (int s = 0; s < C::RAW; ++s) {
+            mbar_init(&bars[C::RFULL + s], 1);
+            mbar_init(&bars[C::REMPTY + s], 2);
+        }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(&bars[C::QFULL + x], 4);
+            mbar_init(&bars[C::SFULL + x], 1);
+            mbar_init(&bars[C::PFULL + x], 4);
+            mbar_init(&bars[C::ODONE + x], 1);
+        }
+        mbar_fence_init();
+    }
+    if (wid == 1) tmem_alloc((uint32_t*)&s_ctl[1], 512);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = (uint32_t)s_ctl[1];
+    // columns: S_A 0..127 (P_A over 0..63), S_B 128..255, O_A from 256, O_B from 384
+    // The plan (and whatever the caller's kernels before it wrote) is complete from here on; the kernel behind this one reads
+    // the plan's lengths before its own wait, hence is not let go earlier.
+    grid_dependency_wait();
+    grid_launch_dependents();
+    PWalk walk = walk_of_block(p);
+    PPiece pc;
+    bool ok = true;
+
+    if (wid == 0) {
+        // =========================== TMA producer ===========================================================
+        constexpr int NRING = FP8 ? C::RAW : C::RING;
+        constexpr int TILE_BYTES = FP8 ? C::RAW_TILE : C::TILE;
+        constexpr int HB = kPrefixTile * 128;                      // bytes of a 128-byte wide half
+        uint8_t* const to = FP8 ? raw : ring;
+        uint64_t* const full = bars + (FP8 ? C::RFULL : C::FULL);
+        uint64_t* const empty = bars + (FP8 ? C::REMPTY : C::EMPTY);
+        const uint64_t keep = l2_evict_first_policy();
+        const int per_tile = kPrefixTile / p.kbox;
+        Ring<NRING> rg;
+        uint32_t issued = 0, flags = 0;
+        if (lane == 0) {
+            tma_prefetch_desc(&tmK);
+            tma_prefetch_desc(&tmV);
+        }
+        while (ok && walk.next(p, pc)) {
+            // lane j holds the page of the tile's j-th box, read one tile ahead
+            auto page_of = [&](int t) {
+                const int key = t * kPrefixTile + lane * p.kbox;
+                if (p.page_size == 0 || lane >= per_tile || key >= pc.len) return 0;
+                int page = p.page_table[(int64_t)pc.g * p.max_pages + key / p.page_size];
+                if (page < 0 || page >= p.num_pool_pages) {
+                    flags |= kDevPageIdClamped;
+                    page = page < 0 ? 0 : p.num_pool_pages - 1;
+                }
+                return page;
+            };
+            int next_page = page_of(pc.t0);
+            for (int t = pc.t0; t < pc.t1 && ok; ++t) {
+                const int page = next_page;
+                if (t + 1 < pc.t1) next_page = page_of(t + 1);
+                const int boxes = min(per_tile, (pc.len - t * kPrefixTile + p.kbox - 1) / p.kbox);
+                for (int which = 0; which < 2; ++which) {
+                    if (issued >= (uint32_t)NRING) ok = seq_wait(&empty[rg.slot], rg.parity ^ 1u, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    uint8_t* dst = to + (size_t)rg.slot * TILE_BYTES;
+                    if (lane == 0) mbar_expect_tx(&full[rg.slot], (uint32_t)(boxes * p.kbox) * (TILE_BYTES / kPrefixTile));
+                    for (int j = 0; j < boxes; ++j) {
+                        const int pg = __shfl_sync(0xffffffffu, page, j);
+                        const int key = t * kPrefixTile + j * p.kbox;
+                        const int row = p.page_size > 0 ? key % p.page_size : key, outer = p.page_size > 0 ? pg : pc.g;
+                        if (lane == 0)
+#pragma unroll
+                            for (int hf = 0; hf < (FP8 ? 1 : HALVES); ++hf)
+                                tma_load_4d(dst + hf * HB + j * p.kbox * 128, which == 0 ? &tmK : &tmV, &full[rg.slot], hf * 64, row, pc.h, outer, keep);
+                    }
+                    __syncwarp();
+                    ++issued;
+                    rg.advance();
+                }
+            }
+        }
+        if (lane == 0) s_ctl[2] = (int32_t)issued;
+        if (flags) atomicOr(p.status, flags);
+    } else if (wid == 1) {
+        // =========================== product issue (whole warp walks, lane 0 issues) =====================
+        constexpr uint32_t idesc_qk = p_instr_desc(128, 0, FP8), idesc_pv = p_instr_desc(D, 1, FP8);
+        constexpr int HB = kPrefixTile * 128;
+        const uint32_t q_a = smem_u32(q_smem), ring_a = smem_u32(ring);
+        uint32_t base = 0;                    // ring tiles before this piece: K of its i-th key tile is base + 2 i, V the next
+        uint32_t q_parity[2] = {0, 0}, p_parity[2] = {0, 0};
+        while (ok && walk.next(p, pc)) {
+            const int n = pc.t1 - pc.t0;
+            auto wait_tile = [&](uint32_t cnt) {
+                bool y = seq_wait(&bars[C::FULL + cnt % C::RING], (cnt / C::RING) & 1u, abort_flag);
+                ok = __all_sync(0xffffffffu, y);
+            };
+            // tile x's query rows have been loaded (a tile without a key tile in this piece has none)
+            auto wait_q = [&](int x) {
+                ok = seq_wait(&bars[C::QFULL + x], q_parity[x], abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                q_parity[x] ^= 1u;
+            };
+            // S_x = Q_x . K(i)^T. The K tile is free once the last tile that takes it has been issued.
+            auto issue_s = [&](int i, int x) {
+                const uint32_t cnt = base + 2u * (uint32_t)i;
+                wait_tile(cnt);
+                if (!ok) return;
+                tc_fence_after_sync();
+                if (lane == 0) {
+                    const uint32_t ka = ring_a + (cnt % C::RING) * C::TILE, qa = q_a + (uint32_t)x * C::TILE;
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk)
+                        umma_bf16(tmem_base + x * 128, seq_smem_desc(qa + (kk >> 2) * HB + (kk & 3) * 32, 16, 1024),
+                                  seq_smem_desc(ka + (kk >> 2) * HB + (kk & 3) * 32, 16, 1024), idesc_qk, kk == 0 ? 0u : 1u);
+                    umma_commit(&bars[C::SFULL + x]);
+                    if (!pc.wide || x == 1) umma_commit(&bars[C::EMPTY + cnt % C::RING]);
+                }
+                __syncwarp();
+            };
+            auto finish = [&](int i, int x, bool last) {       // O_x += P_x . V(i)
+                ok = seq_wait(&bars[C::PFULL + x], p_parity[x], abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                p_parity[x] ^= 1u;
+                if (!ok) return;
+                const uint32_t cnt = base + 2u * (uint32_t)i + 1u;
+                wait_tile(cnt);
+                if (!ok) return;
+                const uint32_t slot = cnt % C::RING;
+                // Rows of the V tile behind the prefix may hold anything: zero them, so that a probability of 0 times garbage
+                // is 0. Done by the first tile that uses it (E4M3: by the warps that convert).
+                const int held = pc.len - (pc.t0 + i) * kPrefixTile;
+                if (!FP8 && held < kPrefixTile && (!pc.wide || x == 0)) {
+                    uint8_t* v = ring + (size_t)slot * C::TILE;
+                    for (int idx = lane; idx < (kPrefixTile - held) * (D / 8); idx += 32) {
+                        const int row = held + idx / (D / 8), ch = idx % (D / 8);
+                        *(uint4*)(v + (ch >> 3) * HB + row * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                }
+                tc_fence_after_sync();
+                if (lane == 0) {
+                    const uint32_t va = ring_a + slot * C::TILE;
+#pragma unroll
+                    for (int kk = 0; kk < kPrefixTile / 16; ++kk)
+                        umma_bf16_ts(tmem_base + 256 + x * 128, tmem_base + x * 128 + kk * 8, seq_smem_desc(va + kk * 2048, HB, 1024), idesc_pv,
+                                     (i > (pc.wide ? 0 : x) || kk > 0) ? 1u : 0u);
+                    if (!pc.wide || x == 1) umma_commit(&bars[C::EMPTY + slot]);
+                    if (last) umma_commit(&bars[C::ODONE + x]);
+                }
+                __syncwarp();
+            };
+            wait_q(0);
+            if (ok) issue_s(0, 0);
+            if (ok && (pc.wide || n > 1)) wait_q(1);
+            if (pc.wide) {
+                if (ok) issue_s(0, 1);
+                for (int i = 0; i < n && ok; ++i)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (ok) finish(i, x, i + 1 == n);
+                        if (ok && i + 1 < n) issue_s(i + 1, x);
+                    }
+            } else {
+                if (ok && n > 1) issue_s(1, 1);
+                for (int i = 0; i < n && ok; ++i) {
+                    finish(i, i & 1, i + 2 >= n);
+                    if (ok && i + 2 < n) issue_s(i + 2, i & 1);
+                }
+            }
+            base += 2u * (uint32_t)n;
+        }
+    } else if (wid < 4) {
+        // =========================== E4M3 codes to f16 =======================================================
+        if constexpr (FP8) {
+            constexpr int HB = kPrefixTile * 128;
+            Ring<C::RAW> src;
+            Ring<C::RING> dst;
+            uint32_t done = 0;
+            const int t64 = tid - 64;
+            while (ok && walk.next(p, pc))
+                for (int t = pc.t0; t < pc.t1 && ok; ++t)
+                    for (int which = 0; which < 2 && ok; ++which) {
+                        ok = seq_wait(&bars[C::RFULL + src.slot], src.parity, abort_flag);
+                        if (ok && done >= (uint32_t)C::RING) ok = seq_wait(&bars[C::EMPTY + dst.slot], dst.parity ^ 1u, abort_flag);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        const uint8_t* a = raw + (size_t)src.slot * C::RAW_TILE;
+                        uint8_t* o = ring + (size_t)dst.slot * C::TILE;
+                        const int held = pc.len - t * kPrefixTile;       // rows from here on are zeroed
+#pragma unroll 2
+                        for (int k = 0; k < 16; ++k) {
+                            const int row = k * 8 + (t64 >> 3), c = t64 & 7;
+                            uint4 v = *(const uint4*)(a + row * 128 + ((c ^ (row & 7)) << 4));
+                            if (row >= held) v = make_uint4(0, 0, 0, 0);
+                            const uint4 lo = make_uint4(e4m3x2_to_f16x2(v.x & 0xffffu), e4m3x2_to_f16x2(v.x >> 16), e4m3x2_to_f16x2(v.y & 0xffffu),
+                                                        e4m3x2_to_f16x2(v.y >> 16));
+                            const uint4 hi = make_uint4(e4m3x2_to_f16x2(v.z & 0xffffu), e4m3x2_to_f16x2(v.z >> 16), e4m3x2_to_f16x2(v.w & 0xffffu),
+                                                        e4m3x2_to_f16x2(v.w >> 16));
+                            uint8_t* half = o + (c >> 2) * HB + row * 128;
+                            const int c0 = (2 * (c & 3)) ^ (row & 7), c1 = (2 * (c & 3) + 1) ^ (row & 7);
+                            // the two halves' threads store their pieces in opposite order: no two in one bank
+                            const bool swap = c >= 4;
+                            *(uint4*)(half + ((swap ? c1 : c0) << 4)) = swap ? hi : lo;
+                            *(uint4*)(half + ((swap ? c0 : c1) << 4)) = swap ? lo : hi;
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            mbar_arrive(&bars[C::FULL + dst.slot]);
+                            mbar_arrive(&bars[C::REMPTY + src.slot]);
+                        }
+                        ++done;
+                        src.advance();
+                        dst.advance();
+                    }
+        }
+    } else {
+        // =========================== softmax, query rows and partials ======================================
+        constexpr int HB = kPrefixTile * 128;
+        const int x = (wid - 4) >> 2;                      // 0: tile A, 1: tile B
+        const int wq = wid & 3, row = wq * 32 + lane;      // lane quarter of tensor memory; row of the tile
+        const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
+        const uint32_t tS = tmem_base + lane_off + x * 128, tO = tmem_base + lane_off + 256 + x * 128;
+        uint32_t s_parity = 0, o_parity = 0;
+        while (ok && walk.next(p, pc)) {
+            // ---- this row's query, and how many tokens of the prefix it sees ------------------------------------
+            const int lr = pc.m * kPrefixRows + (pc.wide ? x * 128 : 0) + row;
+            const int mine = tiles_of(pc, x), step = pc.wide ? 1 : 2;
+            int sees = 0;
+            if (mine > 0) {
+                uint8_t* q = q_smem + x * C::TILE;
+                if (lr < pc.rows) {
+                    const int b = p.plan.begin[pc.g] + lr / p.R, r = lr % p.R, lq = r / p.G, l = lq / p.Qn;
+                    const int cut = (int)min((int64_t)p.seq_lens[b], (int64_t)pc.len + p.max_seq_len) - p.delta[l] - (p.Qn - 1 - lq % p.Qn);
+                    sees = max(0, min(pc.len, cut));
+                    const uint4* src = (const uint4*)((const __nv_bfloat16*)p.q + (((int64_t)b * p.L * p.Qn + lq) * p.Hq + pc.h * p.G + (r - lq * p.G)) * D);
+#pragma unroll 4
+                    for (int c = 0; c < D / 8; ++c) {
+                        uint4 v = src[c];
+                        if (FP8) {
+                            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) w[i] = pack_f16x2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+                            v = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                        *(uint4*)(q + (c >> 3) * HB + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+                    }
+                } else {
+#pragma unroll 4
+                    for (int c = 0; c < D / 8; ++c) *(uint4*)(q + (c >> 3) * HB + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+                }
+                fence_proxy_async_smem();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars[C::QFULL + x]);
+            }
+            const float scale = FP8 ? p.scale_log2 * p.k_scale[pc.h] : p.scale_log2;
+            float mref = kSeqNoMax, sum = 0.f;
+            for (int i = 0; i < mine; ++i) {
+                ok = seq_wait(&bars[C::SFULL + x], s_parity, abort_flag);
+                ok = __all_sync(0xffffffffu, ok);      // the tensor-memory accesses below are collective over the warp
+                s_parity ^= 1u;
+                if (!ok) break;
+                tc_fence_after_sync();
+                const int t = pc.t0 + (pc.wide ? 0 : x) + i * step;
+                const int lim = sees - t * kPrefixTile;    // keys [0, lim) of the tile are visible to this row
+                const bool full = __all_sync(0xffffffffu, lim >= kPrefixTile);
+                uint32_t pk[64], pbig = 0xffffu;
+                float lsum = 0.f;
+                if (i > 0) p_pass<FP8>(tS, lim, full, scale, mref, pk, lsum, pbig);
+                if (__any_sync(0xffffffffu, i == 0 || (lim > 0 && pbig > kBigPattern<FP8>))) {
+                    // the tile's true maximum, rescale of this row of O (every product into it has completed: the commit behind
+                    // S_FULL covers them), and the probabilities against the new reference
+                    const float mx = p_row_max(tS, lim) * scale;
+                    const float m_new = fmaxf(mref, mx - kBelow<FP8>);
+                    const float alpha = fast_exp2(mref - m_new);
+                    mref = m_new;
+                    sum *= alpha;
+                    if (i > 0) p_scale_o<D>(tO, alpha);
+                    p_pass<FP8>(tS, lim, full, scale, mref, pk, lsum, pbig);
+                }
+                sum += lsum;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) tmem_st32(tS + c * 32, &pk[c * 32]);
+                tmem_wait_st();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars[C::PFULL + x]);
+            }
+            if (!ok) break;
+            // ---- the partial ---------------------------------------------------------------------------------------
+            const int64_t slot = (int64_t)pc.unit + blockIdx.x;
+            const bool saw = mine > 0 && mref > kSeqNoMax;
+            *(float2*)(p.ml + ((slot * 2 + x) * 128 + row) * 2) = make_float2(saw ? mref : -INFINITY, saw ? sum : 0.f);
+            if (mine > 0) {
+                ok = seq_wait(&bars[C::ODONE + x], o_parity, abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                o_parity ^= 1u;
+                if (!ok) break;
+                tc_fence_after_sync();
+                const float f = FP8 ? p.v_scale[pc.h] : 1.f;
+                float* out = p.acc + (slot * 2 + x) * (128 * D) + row * 4;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t r[32];
+                    tmem_ld32(tO + c * 32, r);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        *(float4*)(out + (c * 8 + k) * 512) = make_float4(__uint_as_float(r[4 * k]) * f, __uint_as_float(r[4 * k + 1]) * f,
+                                                                          __uint_as_float(r[4 * k + 2]) * f, __uint_as_float(r[4 * k + 3]) * f);
+                }
+            }
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (tid == 0 && s_ctl[0] != 0) {
+        atomicOr(p.status, kDevWaitTimeout);
+        // give every copy that was issued a bounded chance to land before the block retires
+        constexpr int NRING = FP8 ? C::RAW : C::RING;
+        const uint32_t issued = (uint32_t)s_ctl[2], outstanding = issued < (uint32_t)NRING ? issued : (uint32_t)NRING;
+        for (uint32_t k = 0; k < outstanding; ++k) {
+            const uint32_t cnt = issued - 1 - k;
+            mbar_wait_bounded(&bars[(FP8 ? C::RFULL : C::FULL) + cnt % NRING], (cnt / NRING) & 1u, kSeqWaitNs);
+        }
+    }
+    __syncthreads();
+    if (wid == 1) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem_base, 512);
+    }
+}
+
+// ---- the plan -------------------------------------------------------------------------------------------------------
+// One block: clamped groups and lengths, the line of their units, and what each sequence holds itself.
+constexpr int kPlanThreads = 512;
+
+__global__ void __launch_bounds__(kPlanThreads) plt_prefix_plan(const __grid_constant__ PrefixParams p) {
+    __shared__ int32_t s_begin[kMaxGroups + 1], s_len[kMaxGroups], s_line[kMaxGroups + 1], s_unit[kMaxGroups + 1];
+    grid_launch_dependents();
+    const int tid = threadIdx.x, lane = tid & 31;
+    uint32_t flags = 0;
+    for (int g = tid; g <= p.groups; g += kPlanThreads) s_begin[g] = p.groups > 0 ? p.group_begin[g] : 0;
+    for (int g = tid; g < p.groups; g += kPlanThreads) {
+        int n = p.prefix_lens[g];
+        if (n < 0 || n > p.max_prefix_len) {
+            flags |= kDevGroupClamped;
+            n = n < 0 ? 0 : p.max_prefix_len;
+        }
+        s_len[g] = n;
+    }
+    __syncthreads();
+    if (tid < 32) {
+        // first sequences: running maximum of what the caller gave, within [0, B]; then the line and the units
+        int last = 0, line = 0, unit = 0;
+        for (int g0 = 0; g0 <= p.groups; g0 += 32) {
+            const int g = g0 + lane;
+            const int given = g <= p.groups ? s_begin[g] : 0;
+            int v = min(max(given, 0), p.B);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, v, o);
+                if (lane >= o) v = max(v, y);
+            }
+            v = max(v, last);
+            last = __shfl_sync(0xffffffffu, v, 31);
+            if (g <= p.groups) {
+                if (v != given) flags |= kDevGroupClamped;
+                s_begin[g] = v;
+            }
+        }
+        __syncwarp();
+        for (int g0 = 0; g0 < p.groups; g0 += 32) {
+            const int g = g0 + lane;
+            int units = 0, positions = 0;
+            if (g < p.groups) {
+                const int rows = (s_begin[g + 1] - s_begin[g]) * p.R;
+                if (rows == 0) s_len[g] = 0;
+                const int tiles = (s_len[g] + kPrefixTile - 1) / kPrefixTile;
+                units = tiles > 0 ? p.Hkv * ((rows + kPrefixRows - 1) / kPrefixRows) : 0;
+                positions = units * (tiles + kPrefixLead);
+            }
+            int u = units, q = positions;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int a = __shfl_up_sync(0xffffffffu, u, o), c = __shfl_up_sync(0xffffffffu, q, o);
+                if (lane >= o) {
+                    u += a;
+                    q += c;
+                }
+            }
+            if (g < p.groups) {
+                s_unit[g] = unit + u - units;
+                s_line[g] = line + q - positions;
+            }
+            unit += __shfl_sync(0xffffffffu, u, 31);
+            line += __shfl_sync(0xffffffffu, q, 31);
+        }
+        if (lane == 0) {
+            s_unit[p.groups] = unit;
+            s_line[p.groups] = line;
+        }
+    }
+    __syncthreads();
+    for (int g = tid; g <= p.groups; g += kPlanThreads) {
+        p.plan.begin[g] = s_begin[g];
+        p.plan.line[g] = s_line[g];
+        p.plan.unit[g] = s_unit[g];
+        if (g < p.groups) p.plan.len[g] = s_len[g];
+    }
+    for (int b = tid; b < p.B; b += kPlanThreads) {
+        // the group of sequence b, if any
+        int len = 0;
+        if (p.groups > 0 && b >= s_begin[0] && b < s_begin[p.groups]) {
+            int lo = 0, hi = p.groups;             // begin[lo] <= b < begin[hi]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (s_begin[mid] <= b) lo = mid; else hi = mid;
+            }
+            len = s_len[lo];
+        }
+        int n = p.seq_lens[b];
+        if (n < 0 || n > (int64_t)len + p.max_seq_len) {
+            flags |= kDevSeqLenClamped;
+            n = n < 0 ? 0 : len + p.max_seq_len;
+        }
+        p.plan.own_lens[b] = max(0, n - len);
+        for (int l = 1; l < p.L; ++l) {
+            const int cut = max(0, n - p.delta[l]);
+            int wl = min(cut, p.w);
+            if (p.win_lens != nullptr && cut > 0) {
+                wl = p.win_lens[b * (p.L - 1) + l - 1];
+                if (wl < 0 || wl > p.w) {
+                    flags |= kDevWinLenClamped;
+                    wl = wl < 0 ? 0 : p.w;
+                }
+            }
+            p.plan.win_lens[b * (p.L - 1) + l - 1] = wl;
+        }
+    }
+    if (flags) atomicOr(p.status, flags);
+}
+
+template <int D, bool FP8>
+cudaError_t launch_one(const CUtensorMap maps[2], const PrefixParams& pp, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)pp.blocks);
+    cfg.blockDim = dim3(kPThreads);
+    cfg.dynamicSmemBytes = PCfg<D, FP8>::SMEM;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, plt_prefix_main<D, FP8>, maps[0], maps[1], pp);
+}
+
+}  // namespace
+
+size_t prefix_smem(int d, bool fp8) { return fp8 ? PCfg<128, true>::SMEM : d == 128 ? PCfg<128, false>::SMEM : PCfg<64, false>::SMEM; }
+
+cudaError_t prefix_prepare(int d, bool fp8) {
+    return allow_max_dynamic_smem(fp8 ? (const void*)plt_prefix_main<128, true>
+                                      : d == 128 ? (const void*)plt_prefix_main<128, false> : (const void*)plt_prefix_main<64, false>);
+}
+
+cudaError_t launch_prefix_plan(const PrefixParams& pp, cudaStream_t stream) {
+    plt_prefix_plan<<<1, kPlanThreads, 0, stream>>>(pp);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_prefix_main(const CUtensorMap maps[2], const PrefixParams& pp, bool fp8, cudaStream_t stream) {
+    if (fp8) return launch_one<128, true>(maps, pp, stream);
+    return pp.d == 128 ? launch_one<128, false>(maps, pp, stream) : launch_one<64, false>(maps, pp, stream);
+}
+
+}  // namespace plt
