@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kVerifyThreads = 256;
 constexpr int kMinChunk = 2048, kMaxChunk = 16384;   // elements of a chunk: multiples of 8 * kVerifyThreads
+constexpr int kOneWave = 592;                         // blocks that run at once (4 of 256 threads on each of 148 SMs)
 constexpr int kMaxDrafts = 64;
 
 thread_local char g_verify_error[512] = "";
@@ -28,8 +29,7 @@ thread_local char g_verify_error[512] = "";
 
 struct plt_draft_verify : HandleBase {
     plt_draft_verify_config cfg;
-    int chunk, chunks;
-    double* sums = nullptr;      // [max_batch, chunks]
+    double* sums = nullptr;      // [batch, chunks] of a call
     uint32_t* arrived = nullptr; // [max_batch] blocks of a sequence that have left their sum; 0 between calls
 };
 
@@ -66,10 +66,10 @@ struct Row {
     const T* q;       // or null
     int without;      // index whose weight is 0, or -1
     int V;
-    // finite and above 0, or 0 (an infinite entry counts as nothing, in p or as the difference's result)
+    // a - b where that is finite and above 0, else 0. The test is made in fp32, where it is exact: 64-bit units are few.
     __device__ __forceinline__ double weight(float a, float b) const {
-        const double w = (double)a - (double)b;
-        return w > 0.0 && w <= 3.4028234663852886e38 ? w : 0.0;
+        const bool counts = a > b && a <= 3.402823466e38f && b >= -3.402823466e38f;
+        return (double)(counts ? a : 0.f) - (double)(counts ? b : 0.f);
     }
     __device__ __forceinline__ double at(int i) const {
         if (i == without) return 0.0;
@@ -113,9 +113,8 @@ __device__ __forceinline__ double warp_sum(double x) {
     return x;
 }
 
-// Inclusive running sum over the block's threads; s_warp: one double for each warp. Ends with a barrier passed, so that
-// s_warp may be used again after the next one.
-__device__ __forceinline__ double block_running_sum(double x, double* s_warp) {
+// Inclusive running sum over the block's threads, and the sum of all; s_warp: one double for each warp.
+__device__ __forceinline__ double block_running_sum(double x, double* s_warp, double& total) {
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -126,7 +125,12 @@ __device__ __forceinline__ double block_running_sum(double x, double* s_warp) {
     if (lane == 31) s_warp[wid] = x;
     __syncthreads();
     double base = 0.0;
-    for (int w = 0; w < wid; ++w) base += s_warp[w];
+    total = 0.0;
+#pragma unroll
+    for (int w = 0; w < kVerifyThreads / 32; ++w) {
+        if (w == wid) base = total;
+        total += s_warp[w];
+    }
     return base + x;
 }
 
@@ -142,28 +146,29 @@ __device__ __forceinline__ int first_thread(bool yes, int* s_first) {
     return *s_first;
 }
 
-// Walks `n` numbers (value(i), i < n, none below 0) to the first whose running sum, from `before` on, exceeds `limit`.
-// Returns its index, or the last with a value above 0 where none does (-1: none has); `before` becomes the sum in front of it.
-// Each thread takes a run of consecutive numbers. All threads of the block call it and get the same answer. Only numbers
-// above 0 are candidates: two running sums of the same numbers may differ by a rounding.
+// Walks `n` numbers (value(i), i < n, none below 0) to the first whose running sum exceeds r times their total. Returns its
+// index, or the last with a value above 0 where none does (-1: none has), `before`, the sum in front of it, and `total`. Each
+// thread takes a run of consecutive numbers. All threads of the block call it and get the same answer. Only numbers above 0 are
+// candidates: two running sums of the same numbers may differ by a rounding.
 template <typename F>
-__device__ int walk(int n, F value, double& before, double limit, double* s_warp, int* s_first, double* s_base) {
+__device__ int walk(int n, F value, double& before, double& total, double r, double* s_warp, int* s_first, double* s_base) {
     const int per = (n + kVerifyThreads - 1) / kVerifyThreads;
     const int lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
     double own = 0.0;
     for (int i = lo; i < hi; ++i) own += value(i);
-    const double upto = block_running_sum(own, s_warp);
-    int t = first_thread(own > 0.0 && before + upto > limit, s_first);
+    const double upto = block_running_sum(own, s_warp, total);
+    const double limit = r * total;
+    int t = first_thread(own > 0.0 && upto > limit, s_first);
     if (t == kVerifyThreads) {
         t = last_thread(own > 0.0, s_first);
         if (t < 0) return -1;
     }
     __syncthreads();
     if ((int)threadIdx.x == t) {
-        double run = before + (upto - own), base = run;
+        double run = upto - own, base = run;
         int found = lo;
         for (int i = lo; i < hi; ++i) {
-            const double v = value(i);
+            const double v = hi - lo == 1 ? own : value(i);
             if (v > 0.0) {
                 found = i;
                 base = run;
@@ -222,6 +227,7 @@ __device__ int walk_row(const Row<T>& row, int first, int last, double before, d
         bool done = false;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
+            if (s >= per || done) break;
             double upto = own[s];
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -230,7 +236,7 @@ __device__ int walk_row(const Row<T>& row, int first, int last, double before, d
             }
             const uint32_t any = __ballot_sync(0xffffffffu, own[s] > 0.0);
             const uint32_t past = __ballot_sync(0xffffffffu, own[s] > 0.0 && base + upto > limit);
-            if (!done && any != 0) {
+            if (any != 0) {
                 const int l = past != 0 ? __ffs(past) - 1 : 31 - __clz(any);
                 pick = s * 32 + l;
                 at_pick = base + __shfl_sync(0xffffffffu, upto - own[s], l);
@@ -258,7 +264,7 @@ __device__ int walk_row(const Row<T>& row, int first, int last, double before, d
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kVerifyThreads) plt_draft_verify_kernel(const __grid_constant__ VerifyParams p) {
+__global__ void __launch_bounds__(kVerifyThreads, 4) plt_draft_verify_kernel(const __grid_constant__ VerifyParams p) {
     __shared__ double s_warp[kVerifyThreads / 32];
     __shared__ double s_base;
     __shared__ int s_first, s_n, s_len;
@@ -319,7 +325,7 @@ __global__ void __launch_bounds__(kVerifyThreads) plt_draft_verify_kernel(const 
     const int c0 = (int)blockIdx.x * p.chunk - lead;          // may be below 0
     double sum = 0.0;
     if constexpr (VEC) {
-        constexpr int U = 4;
+        constexpr int U = 16 / N;         // vectors in flight: 16 elements of each row
         for (int i0 = c0 + tid * N; i0 < min(c0 + p.chunk, p.V); i0 += kVerifyThreads * N * U) {
             float a[U][N], q[U][N];
 #pragma unroll
@@ -381,35 +387,18 @@ __global__ void __launch_bounds__(kVerifyThreads) plt_draft_verify_kernel(const 
     // ---- the sequence's last block: the token --------------------------------------------------------------------
     __threadfence();
     const double* sums = p.sums + (int64_t)b * p.chunks;
-    double part = 0.0;
-    for (int i = tid; i < p.chunks; i += kVerifyThreads) part += __ldcg(sums + i);
-    part = block_running_sum(part, s_warp);
-    __syncthreads();
-    if (tid == kVerifyThreads - 1) s_base = part;
-    __syncthreads();
-    double total = s_base;
-    __syncthreads();
     const double r = (double)p.sample_u[b];
     int token = -1;
-    double before = 0.0;
+    double before = 0.0, total = 0.0;
+    const int c = walk(p.chunks, [&](int i) { return __ldcg(sums + i); }, before, total, r, s_warp, &s_first, &s_base);
     if (total > 0.0) {
-        const int c = walk(p.chunks, [&](int i) { return __ldcg(sums + i); }, before, r * total, s_warp, &s_first, &s_base);
         const int first = max(c * p.chunk - lead, 0), last = min((c + 1) * p.chunk - lead, p.V);
         token = walk_row(row, first, last, before, r * total, s_warp, &s_first);
     } else if (cut) {
         // p lies nowhere above q: the whole of p
         row.q = nullptr;
         row.without = -1;
-        const int per = (p.V + kVerifyThreads - 1) / kVerifyThreads;
-        double own = 0.0;
-        for (int i = min(tid * per, p.V); i < min((tid + 1) * per, p.V); ++i) own += row.at(i);
-        own = block_running_sum(own, s_warp);
-        __syncthreads();
-        if (tid == kVerifyThreads - 1) s_base = own;
-        __syncthreads();
-        total = s_base;
-        __syncthreads();
-        if (total > 0.0) token = walk(p.V, [&](int i) { return row.at(i); }, before, r * total, s_warp, &s_first, &s_base);
+        token = walk(p.V, [&](int i) { return row.at(i); }, before, total, r, s_warp, &s_first, &s_base);
     }
     for (int j = tid; j <= p.K; j += kVerifyThreads)
         p.tokens[(int64_t)b * (p.K + 1) + j] = j < n ? p.draft_tokens[(int64_t)b * p.K + j] : j == n ? token : -1;
@@ -437,18 +426,22 @@ plt_status check_config(const plt_draft_verify_config* c) {
     return PLT_OK;
 }
 
-// Elements of a chunk: as long as kMaxChunk where the batch alone fills the device, shorter where it does not.
-int chunk_of(const plt_draft_verify_config* c) {
-    int chunk = kMaxChunk;
-    while (chunk > kMinChunk && (int64_t)c->max_batch * (c->vocab / chunk) < 592) chunk >>= 1;
+// Chunks of a row: of a length that lets all blocks of the batch run at once, or the longest. A row may start up to 7 elements
+// behind a place of the 16-byte grid (`lead`).
+int chunk_of(int batch, int vocab, int lead) {
+    int chunk = kMinChunk;
+    while (chunk < kMaxChunk && (int64_t)batch * ((vocab + lead + chunk - 1) / chunk) > kOneWave) chunk <<= 1;
     return chunk;
 }
 
-// Chunks of a row that starts at any place of the 16-byte grid.
-int chunks_of(const plt_draft_verify_config* c, int chunk) { return (c->vocab + 7 + chunk - 1) / chunk; }
+// Sums that any batch up to the largest leaves.
+size_t sums_of(const plt_draft_verify_config* c) {
+    const size_t most = (size_t)c->max_batch * ((c->vocab + 7 + kMaxChunk - 1) / kMaxChunk);
+    return most > kOneWave ? most : kOneWave;
+}
 
 size_t workspace_of(const plt_draft_verify_config* c) {
-    return (size_t)c->max_batch * (8u * (size_t)chunks_of(c, chunk_of(c)) + 4u) + 256;
+    return 8u * sums_of(c) + 4u * (size_t)c->max_batch + 256;
 }
 
 }  // namespace
@@ -480,8 +473,6 @@ PLT_API plt_status plt_draft_verify_create(const plt_draft_verify_config* config
     if (!h) return verify_fail(nullptr, PLT_ERR_OUT_OF_MEMORY, "host allocation failed");
     h->cfg = *config;
     h->device = config->device;
-    h->chunk = chunk_of(config);
-    h->chunks = chunks_of(config, h->chunk);
     const size_t bytes = workspace_of(config);
     void* ws = nullptr;
     if (cudaMalloc(&ws, bytes) != cudaSuccess) {
@@ -491,7 +482,7 @@ PLT_API plt_status plt_draft_verify_create(const plt_draft_verify_config* config
     }
     h->status = (uint32_t*)ws;
     h->sums = (double*)((char*)ws + 256);
-    h->arrived = (uint32_t*)(h->sums + (size_t)config->max_batch * h->chunks);
+    h->arrived = (uint32_t*)(h->sums + sums_of(config));
     cudaError_t e = cudaMemset(ws, 0, bytes);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();   // another stream may run first
     if (e != cudaSuccess) {
@@ -540,12 +531,16 @@ PLT_API plt_status plt_draft_verify_run(plt_draft_verify_t h, const plt_draft_ve
     p.draft_tokens = a->draft_tokens; p.draft_lens = a->draft_lens; p.accept_u = a->accept_u; p.sample_u = a->sample_u;
     p.tokens = a->tokens; p.num_accepted = a->num_accepted; p.seq_lens = a->seq_lens; p.new_lens = a->new_lens;
     p.sums = h->sums; p.arrived = h->arrived; p.status = h->status;
-    p.K = c.max_drafts; p.V = c.vocab; p.chunk = h->chunk; p.chunks = h->chunks;
+    p.K = c.max_drafts; p.V = c.vocab;
     // 16-byte loads where the rows of p and q that one sequence needs lie alike on the 16-byte grid: always without q
     // (chunks follow p's rows), else where both bases are aligned and all strides are whole vectors.
     const int unit = 16 / es;
     const bool vec = !a->draft_probs || (!misaligned(a->target_probs, 16) && !misaligned(a->draft_probs, 16) && p.target_b % unit == 0 &&
                                          p.target_j % unit == 0 && p.draft_b % unit == 0 && p.draft_j % unit == 0);
+    const bool on_grid = !misaligned(a->target_probs, 16) && p.target_b % unit == 0 && p.target_j % unit == 0;
+    const int lead = vec && !on_grid ? unit - 1 : 0;
+    p.chunk = chunk_of(a->batch, c.vocab, lead);
+    p.chunks = (c.vocab + lead + p.chunk - 1) / p.chunk;
     DeviceScope scope(h->device);
     if (scope.err != cudaSuccess) return handle_fail(h, g_verify_error, PLT_ERR_CUDA, "cudaSetDevice: %s", cudaGetErrorString(scope.err));
     const dim3 grid((unsigned)p.chunks, (unsigned)a->batch);

@@ -124,9 +124,9 @@ struct Lane {
     }
 };
 
-// Norm (gain: this thread's 16 factors) and rotation (cs: the token's cosines and sines) of a row, in place.
+// Norm (gain: the row's factors) and rotation (cs: the token's cosines and sines) of a row, in place.
 template <int D>
-__device__ __forceinline__ void norm_and_turn(float (&x)[16], const Lane<D>& ln, bool norm, const float (&gain)[16], float eps,
+__device__ __forceinline__ void norm_and_turn(float (&x)[16], const Lane<D>& ln, bool norm, const float* gain, float eps,
                                               const float2* cs) {
     if (norm) {
         float ss = 0.f;
@@ -136,7 +136,13 @@ __device__ __forceinline__ void norm_and_turn(float (&x)[16], const Lane<D>& ln,
         for (int o = D / 32; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         const float inv = 1.f / sqrtf(ss * (1.f / D) + eps);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] *= inv * gain[i];
+        for (int i = 0; i < 4; ++i) {
+            const float4 g = *(const float4*)(gain + (i < 2 ? ln.o0 : ln.o1) + 4 * (i & 1));
+            x[4 * i] *= inv * g.x;
+            x[4 * i + 1] *= inv * g.y;
+            x[4 * i + 2] *= inv * g.z;
+            x[4 * i + 3] *= inv * g.w;
+        }
     }
     if (ln.turning) {
         float4 t4[4];
@@ -160,12 +166,13 @@ __device__ __forceinline__ void norm_and_turn(float (&x)[16], const Lane<D>& ln,
 
 // SEQ: rows of a prompt (TB of one loop of a sequence to a block), else one token of a step to a block.
 template <typename T, bool FP8, int D, bool SEQ>
-__global__ void __launch_bounds__(kRopeThreads) plt_rope_kernel(const __grid_constant__ RopeParams p) {
+__global__ void __launch_bounds__(kRopeThreads, SEQ ? 4 : 2) plt_rope_kernel(const __grid_constant__ RopeParams p) {
     constexpr int TB = SEQ ? kSeqTokens : 1;
     constexpr int TPR = D / 16, RPB = kRopeThreads / TPR;      // threads of a row, rows of a pass
     using TD = typename std::conditional<FP8, uint8_t, T>::type;
     __shared__ Token s_tok[TB];
     __shared__ __align__(16) float2 s_cs[TB][kMaxPairs];
+    __shared__ __align__(16) float s_gain[2][D];
     if (!SEQ) grid_launch_dependents();   // the attention's blocks may be set up meanwhile; they wait for this grid
 
     const int tid = threadIdx.x;
@@ -206,6 +213,10 @@ __global__ void __launch_bounds__(kRopeThreads) plt_rope_kernel(const __grid_con
     if (SEQ && t0 >= n) {
         if (flags && tid == 0) atomicOr(p.status, flags);
         return;
+    }
+    if (tid < 2 * D) {
+        const float* gain = tid < D ? p.q_gain : p.k_gain;
+        s_gain[tid / D][tid % D] = gain != nullptr ? gain[tid % D] : 1.f;
     }
     if (tid < TB) {
         Token tk;
@@ -250,12 +261,9 @@ __global__ void __launch_bounds__(kRopeThreads) plt_rope_kernel(const __grid_con
 
     const Lane<D> ln(p);
     const int r_in = tid / TPR;
-    float gain[16];
 
     // ---- queries -----------------------------------------------------------------------------------------------
     const bool qnorm = p.q_gain != nullptr;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) gain[i] = qnorm ? p.q_gain[(i < 8 ? ln.o0 + i : ln.o1 + i - 8)] : 1.f;
     {
         constexpr int U = sizeof(T) == 2 ? 2 : 1;      // rows whose loads are in flight together
         const int rows = TB * p.Hq;
@@ -291,7 +299,7 @@ __global__ void __launch_bounds__(kRopeThreads) plt_rope_kernel(const __grid_con
             for (int u = 0; u < U; ++u) {
                 const int r = r0 + u * RPB + r_in;
                 const int tk = SEQ ? min(r / p.Hq, TB - 1) : 0;
-                norm_and_turn<D>(x[u], ln, qnorm, gain, p.eps, s_cs[tk]);
+                norm_and_turn<D>(x[u], ln, qnorm, s_gain[0], p.eps, s_cs[tk]);
                 if (SEQ ? live[u] : at[u] >= 0) {
                     if (!live[u])
 #pragma unroll
@@ -316,8 +324,6 @@ __global__ void __launch_bounds__(kRopeThreads) plt_rope_kernel(const __grid_con
 
     // ---- keys, then values ---------------------------------------------------------------------------------------
     const bool knorm = p.k_gain != nullptr;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) gain[i] = knorm ? p.k_gain[(i < 8 ? ln.o0 + i : ln.o1 + i - 8)] : 1.f;
     const int rows = TB * p.Hkv;
     const int64_t head_stride = !SEQ && l > 0 ? D : p.kv_stride_h;
     TD* const k_to = (TD*)(!SEQ && l > 0 ? p.k_win : p.k_cache);
@@ -350,7 +356,7 @@ __global__ void __launch_bounds__(kRopeThreads) plt_rope_kernel(const __grid_con
             load8(vsrc + ln.o0, y);
             load8(vsrc + ln.o1, y + 8);
         }
-        norm_and_turn<D>(x, ln, knorm, gain, p.eps, s_cs[tk]);
+        norm_and_turn<D>(x, ln, knorm, s_gain[1], p.eps, s_cs[tk]);
         if (SEQ && live) {
             T* const out = (T*)(l == 0 ? p.k_out : p.k_loc_out);
             if (out != nullptr) {
