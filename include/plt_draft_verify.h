@@ -77,8 +77,8 @@ plt_status plt_draft_verify_create(const plt_draft_verify_config* config, plt_dr
 /* Device bytes plt_draft_verify_create would allocate for this configuration (no device needed). */
 plt_status plt_draft_verify_workspace_bytes(const plt_draft_verify_config* config, size_t* out_bytes);
 
-/* Enqueues the verification on `cuda_stream`: ONE kernel, which reads one row of p and (after a refusal) one of q for each
- * sequence. */
+/* Enqueues the verification on `cuda_stream`: two kernels (three for a large batch), which read one row of p and (after a
+ * refusal) one of q for each sequence. */
 plt_status plt_draft_verify_run(plt_draft_verify_t handle, const plt_draft_verify_args* args, void* cuda_stream);
 
 /* Synchronises `cuda_stream`, reads the device status word and clears it (PLT_DEV_* bits), as plt_decode_attn_check. */

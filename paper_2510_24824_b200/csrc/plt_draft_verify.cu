@@ -1,10 +1,12 @@
 // Draft verification: how many of a sequence's drafted tokens stand, and the token behind them by inversion of the
 // remaining distribution's running sum.
 //
-// One launch. A block takes one chunk of one sequence's vocabulary. It finds the number n of drafts that stand by itself (a
-// warp reads the K pairs of probabilities), sums the chunk's weights in 64 bits and leaves the sum in the workspace; the
-// sequence's last block to arrive walks the chunk sums to the chunk in which the running sum passes r * total, and that chunk
-// (still in L2) to the token. The weights are never written. Bound by reading one row of p and one of q.
+// Two or three launches, each set up while the one before it ends. (1) A warp for each sequence finds the number n of drafts that
+// stand. (2) A warp for each chunk of 8 vectors a lane sums the chunk's weights in 64 bits, all its loads in flight at once, and
+// leaves the sum; warps do not wait for one another. (3) A block for each sequence walks the sums to the chunk in which the
+// running sum passes r * total, and that chunk (still in L2) to the token. The weights are never written. Where the chunks of
+// the batch fit on the device at once, latency counts and (2) does the work of (1) itself. Bound by reading one row of p and, after
+// a refusal, one of q.
 #include "../../include/plt_draft_verify.h"
 
 #include <cuda_bf16.h>
@@ -13,14 +15,15 @@
 #include <new>
 
 #include "plt_handle.h"
+#include "plt_ptx.cuh"
 
 using namespace plt;
 
 namespace {
 
 constexpr int kVerifyThreads = 256;
-constexpr int kMinChunk = 2048, kMaxChunk = 16384;   // elements of a chunk: multiples of 8 * kVerifyThreads
-constexpr int kOneWave = 592;                         // blocks that run at once (4 of 256 threads on each of 148 SMs)
+constexpr int kVecs = 8;                // vectors of 16 bytes that a lane takes of a row's chunk
+constexpr int kAtOnce = 148 * 24;       // warps that run at once
 constexpr int kMaxDrafts = 64;
 
 thread_local char g_verify_error[512] = "";
@@ -30,7 +33,7 @@ thread_local char g_verify_error[512] = "";
 struct plt_draft_verify : HandleBase {
     plt_draft_verify_config cfg;
     double* sums = nullptr;      // [batch, chunks] of a call
-    uint32_t* arrived = nullptr; // [max_batch] blocks of a sequence that have left their sum; 0 between calls
+    int2* stand = nullptr;       // [batch] drafts that stand, drafts there were
 };
 
 namespace {
@@ -48,9 +51,9 @@ struct VerifyParams {
     const int32_t* seq_lens;
     int32_t* new_lens;
     double* sums;
-    uint32_t* arrived;
+    int2* stand;
     uint32_t* status;
-    int32_t K, V, chunk, chunks;
+    int32_t B, K, V, chunks;
 };
 
 template <typename T>
@@ -65,7 +68,6 @@ struct Row {
     const T* p;
     const T* q;       // or null
     int without;      // index whose weight is 0, or -1
-    int V;
     // a - b where that is finite and above 0, else 0. The test is made in fp32, where it is exact: 64-bit units are few.
     __device__ __forceinline__ double weight(float a, float b) const {
         const bool counts = a > b && a <= 3.402823466e38f && b >= -3.402823466e38f;
@@ -184,156 +186,99 @@ __device__ int walk(int n, F value, double& before, double& total, double r, dou
     return *s_first;
 }
 
-// The same over the weights [first, last) of a row, at most kMaxChunk of them, with loads that lie together: a warp takes an
-// eighth, its lanes N neighbouring weights at a time.
+// (drafts that stand, drafts there were) of sequence b, by a whole warp.
 template <typename T>
-__device__ int walk_row(const Row<T>& row, int first, int last, double before, double limit, double* s_warp, int* s_first) {
-    constexpr int N = kVec<T>, STEPS = kMaxChunk / (kVerifyThreads * N);
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const int per = (last - first + kVerifyThreads * N - 1) / (kVerifyThreads * N);   // steps of a warp, at most STEPS
-    const int lo = first + wid * per * 32 * N + lane * N;
-    double own[STEPS], sum = 0.0;
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-        own[s] = 0.0;
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const int i = lo + s * 32 * N + k;
-            if (s < per && i < last) own[s] += row.at(i);
-        }
-        sum += own[s];
-    }
-    sum = warp_sum(sum);
-    __syncthreads();
-    if (lane == 0) s_warp[wid] = sum;
-    __syncthreads();
-    int warp = -1;
-    double base = before;
-#pragma unroll
-    for (int w = 0; w < kVerifyThreads / 32; ++w) {
-        const double v = s_warp[w];
-        if (v > 0.0) {
-            if (warp >= 0) base += s_warp[warp];
-            warp = w;
-            if (base + v > limit) break;
+__device__ __forceinline__ int2 count_standing(const VerifyParams& p, int b, bool report) {
+    const int lane = threadIdx.x & 31;
+    uint32_t flags = 0;
+    int len = p.K;
+    if (p.draft_lens != nullptr) {
+        len = p.draft_lens[b];
+        if (len < 0 || len > p.K) {
+            flags |= kDevSeqLenClamped;
+            len = len < 0 ? 0 : p.K;
         }
     }
-    if (threadIdx.x == 0) *s_first = -1;
-    __syncthreads();
-    if (wid == warp) {
-        // the step, then the lane, then the weight; `pick` is the last candidate seen where none passes the limit
-        int pick = -1;
-        double at_pick = 0.0;
-        bool done = false;
+    int n = len;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            if (s >= per || done) break;
-            double upto = own[s];
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double y = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += y;
+    for (int h = 0; h < kMaxDrafts / 32; ++h) {
+        const int j = h * 32 + lane;
+        bool refused = false;
+        if (j < len) {
+            const int x = p.draft_tokens[(int64_t)b * p.K + j];
+            const float u = p.accept_u[(int64_t)b * p.K + j];
+            refused = true;
+            if (x < 0 || x >= p.V) {
+                flags |= kDevTokenRange;
+            } else {
+                const float pj = widen(((const T*)p.target)[b * p.target_b + j * p.target_j + x]);
+                const float qj = p.draft != nullptr ? widen(((const T*)p.draft)[b * p.draft_b + j * p.draft_j + x]) : 1.f;
+                refused = !((double)u * (double)qj < (double)pj);
             }
-            const uint32_t any = __ballot_sync(0xffffffffu, own[s] > 0.0);
-            const uint32_t past = __ballot_sync(0xffffffffu, own[s] > 0.0 && base + upto > limit);
-            if (any != 0) {
-                const int l = past != 0 ? __ffs(past) - 1 : 31 - __clz(any);
-                pick = s * 32 + l;
-                at_pick = base + __shfl_sync(0xffffffffu, upto - own[s], l);
-                done = past != 0;
-            }
-            base += __shfl_sync(0xffffffffu, upto, 31);
         }
-        if (pick >= 0 && lane == (pick & 31)) {
-            const int i0 = first + wid * per * 32 * N + (pick >> 5) * 32 * N + lane * N;
-            int found = -1;
-            double run = at_pick;
-            for (int k = 0; k < N && i0 + k < last; ++k) {
-                const double v = row.at(i0 + k);
-                if (v > 0.0) {
-                    found = i0 + k;
-                    run += v;
-                    if (run > limit) break;
-                }
-            }
-            *s_first = found;
-        }
+        const uint32_t m = __ballot_sync(0xffffffffu, refused);
+        if (m != 0) n = min(n, h * 32 + __ffs(m) - 1);
     }
-    __syncthreads();
-    return *s_first;
+    if (report && flags) atomicOr(p.status, flags);
+    return make_int2(n, len);
 }
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kVerifyThreads, 4) plt_draft_verify_kernel(const __grid_constant__ VerifyParams p) {
-    __shared__ double s_warp[kVerifyThreads / 32];
-    __shared__ double s_base;
-    __shared__ int s_first, s_n, s_len;
-    __shared__ bool s_last;
-    const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-
-    // ---- how many drafts stand ---------------------------------------------------------------------------------
-    if (wid == 0) {
-        uint32_t flags = 0;
-        int len = p.K;
-        if (p.draft_lens != nullptr) {
-            len = p.draft_lens[b];
-            if (len < 0 || len > p.K) {
-                flags |= kDevSeqLenClamped;
-                len = len < 0 ? 0 : p.K;
-            }
-        }
-        int n = len;
-#pragma unroll
-        for (int h = 0; h < kMaxDrafts / 32; ++h) {
-            const int j = h * 32 + lane;
-            bool refused = false;
-            if (j < len) {
-                const int x = p.draft_tokens[(int64_t)b * p.K + j];
-                const float u = p.accept_u[(int64_t)b * p.K + j];
-                refused = true;
-                if (x < 0 || x >= p.V) {
-                    flags |= kDevTokenRange;
-                } else {
-                    const float pj = widen(((const T*)p.target)[b * p.target_b + j * p.target_j + x]);
-                    const float qj = p.draft != nullptr ? widen(((const T*)p.draft)[b * p.draft_b + j * p.draft_j + x]) : 1.f;
-                    refused = !((double)u * (double)qj < (double)pj);
-                }
-            }
-            const uint32_t m = __ballot_sync(0xffffffffu, refused);
-            if (m != 0) n = min(n, h * 32 + __ffs(m) - 1);
-        }
-        if (lane == 0) {
-            s_n = n;
-            s_len = len;
-        }
-        if (blockIdx.x == 0 && flags) atomicOr(p.status, flags);
-    }
-    __syncthreads();
-    const int n = s_n;
-    const bool cut = n < s_len;
+// The row of weights that decides sequence b's next token.
+template <typename T>
+__device__ __forceinline__ Row<T> row_of(const VerifyParams& p, int b, int2 stand) {
+    const bool cut = stand.x < stand.y;
     Row<T> row;
-    row.p = (const T*)p.target + b * p.target_b + n * p.target_j;
-    row.q = cut && p.draft != nullptr ? (const T*)p.draft + b * p.draft_b + n * p.draft_j : nullptr;
-    row.without = cut && p.draft == nullptr ? p.draft_tokens[(int64_t)b * p.K + n] : -1;
-    row.V = p.V;
+    row.p = (const T*)p.target + b * p.target_b + stand.x * p.target_j;
+    row.q = cut && p.draft != nullptr ? (const T*)p.draft + b * p.draft_b + stand.x * p.draft_j : nullptr;
+    row.without = cut && p.draft == nullptr ? p.draft_tokens[(int64_t)b * p.K + stand.x] : -1;
+    return row;
+}
 
-    // ---- the chunk's sum ----------------------------------------------------------------------------------------
-    // With VEC, chunks are laid on the 16-byte grid of the row of p (the row of q lies alike): chunk 0 starts up to
-    // kVec - 1 elements in front of the row. Each of a thread's sums takes the elements in a fixed order.
+// Elements of a chunk, and elements that the 16-byte grid puts in front of a row (chunk 0 starts there).
+template <typename T>
+constexpr int kChunk = 32 * kVecs * kVec<T>;
+template <typename T, bool VEC>
+__device__ __forceinline__ int lead_of(const Row<T>& row) {
+    return VEC ? (int)(((uintptr_t)row.p & 15) / sizeof(T)) : 0;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kVerifyThreads) plt_draft_verify_count(const __grid_constant__ VerifyParams p) {
+    grid_launch_dependents();
+    const int b = blockIdx.x * (kVerifyThreads / 32) + (threadIdx.x >> 5);
+    if (b >= p.B) return;
+    const int2 s = count_standing<T>(p, b, true);
+    if ((threadIdx.x & 31) == 0) p.stand[b] = s;
+}
+
+template <typename T, bool VEC, bool COUNT>
+__global__ void __launch_bounds__(kVerifyThreads, 3) plt_draft_verify_sums(const __grid_constant__ VerifyParams p) {
     constexpr int N = kVec<T>;
-    const int lead = VEC ? (int)(((uintptr_t)row.p & 15) / sizeof(T)) : 0;
-    const int c0 = (int)blockIdx.x * p.chunk - lead;          // may be below 0
+    grid_launch_dependents();
+    const int b = blockIdx.y, lane = threadIdx.x & 31, chunk = blockIdx.x * (kVerifyThreads / 32) + (threadIdx.x >> 5);
+    if (chunk >= p.chunks) return;
+    int2 stand;
+    if (COUNT) {
+        stand = count_standing<T>(p, b, chunk == 0);
+        if (chunk == 0 && lane == 0) p.stand[b] = stand;
+    } else {
+        grid_dependency_wait();
+        stand = p.stand[b];
+    }
+    const Row<T> row = row_of<T>(p, b, stand);
+    const int c0 = chunk * kChunk<T> - lead_of<T, VEC>(row);      // may be below 0
     double sum = 0.0;
     if constexpr (VEC) {
-        constexpr int U = 16 / N;         // vectors in flight: 16 elements of each row
-        for (int i0 = c0 + tid * N; i0 < min(c0 + p.chunk, p.V); i0 += kVerifyThreads * N * U) {
+        // the row of q lies on the 16-byte grid as the row of p does
+        constexpr int U = sizeof(T) == 4 ? kVecs : kVecs / 2;     // vectors in flight: 32 elements of each row
+#pragma unroll
+        for (int v0 = 0; v0 < kVecs; v0 += U) {
             float a[U][N], q[U][N];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int i = i0 + u * kVerifyThreads * N;
+                const int i = c0 + ((v0 + u) * 32 + lane) * N;
 #pragma unroll
                 for (int k = 0; k < N; ++k) a[u][k] = q[u][k] = 0.f;
-                if (u * kVerifyThreads * N >= p.chunk) continue;     // the chunk's end (the same for the whole block)
                 if (i >= 0 && i + N <= p.V) {
                     load_vec16<T>(row.p + i, a[u]);
                     if (row.q != nullptr) load_vec16<T>(row.q + i, q[u]);
@@ -345,24 +290,22 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) plt_draft_verify_kernel(con
                             if (row.q != nullptr) q[u][k] = widen(row.q[i + k]);
                         }
                 }
-                if (row.without >= i && row.without < i + N)
-#pragma unroll
-                    for (int k = 0; k < N; ++k)
-                        if (i + k == row.without) a[u][k] = 0.f;
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u) {
+                const int i = c0 + ((v0 + u) * 32 + lane) * N;
 #pragma unroll
-                for (int k = 0; k < N; ++k) sum += row.weight(a[u][k], q[u][k]);
+                for (int k = 0; k < N; ++k) sum += i + k == row.without ? 0.0 : row.weight(a[u][k], q[u][k]);
+            }
         }
     } else {
         constexpr int U = 16;
-        for (int i0 = c0 + tid; i0 < min(c0 + p.chunk, p.V); i0 += kVerifyThreads * U) {
+        for (int v0 = 0; v0 < kChunk<T> / 32; v0 += U) {
             float a[U], q[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int i = i0 + u * kVerifyThreads;
-                const bool in = i < min(c0 + p.chunk, p.V) && i != row.without;
+                const int i = c0 + (v0 + u) * 32 + lane;
+                const bool in = i < p.V && i != row.without;
                 a[u] = in ? widen(row.p[i]) : 0.f;
                 q[u] = in && row.q != nullptr ? widen(row.q[i]) : 0.f;
             }
@@ -371,43 +314,93 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) plt_draft_verify_kernel(con
         }
     }
     sum = warp_sum(sum);
-    if (lane == 0) s_warp[wid] = sum;
-    __syncthreads();
-    if (tid == 0) {
-        double total = 0.0;
-#pragma unroll
-        for (int w = 0; w < kVerifyThreads / 32; ++w) total += s_warp[w];
-        p.sums[(int64_t)b * p.chunks + blockIdx.x] = total;
-        __threadfence();
-        s_last = atomicAdd(&p.arrived[b], 1u) == (uint32_t)(p.chunks - 1);
-    }
-    __syncthreads();
-    if (!s_last) return;
+    if (lane == 0) p.sums[(int64_t)b * p.chunks + chunk] = sum;
+}
 
-    // ---- the sequence's last block: the token --------------------------------------------------------------------
-    __threadfence();
-    const double* sums = p.sums + (int64_t)b * p.chunks;
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kVerifyThreads) plt_draft_verify_pick(const __grid_constant__ VerifyParams p) {
+    constexpr int N = kVec<T>;
+    static_assert(kChunk<T> == kVerifyThreads * N, "a thread takes one vector of the chunk");
+    __shared__ double s_warp[kVerifyThreads / 32];
+    __shared__ double s_base;
+    __shared__ int s_pick;
+    const int b = blockIdx.x, tid = threadIdx.x;
     const double r = (double)p.sample_u[b];
+    grid_dependency_wait();
+    const int2 stand = p.stand[b];
+    const double* sums = p.sums + (int64_t)b * p.chunks;
     int token = -1;
     double before = 0.0, total = 0.0;
-    const int c = walk(p.chunks, [&](int i) { return __ldcg(sums + i); }, before, total, r, s_warp, &s_first, &s_base);
+    const int c = walk(p.chunks, [&](int i) { return sums[i]; }, before, total, r, s_warp, &s_pick, &s_base);
+    Row<T> row = row_of<T>(p, b, stand);
     if (total > 0.0) {
-        const int first = max(c * p.chunk - lead, 0), last = min((c + 1) * p.chunk - lead, p.V);
-        token = walk_row(row, first, last, before, r * total, s_warp, &s_first);
-    } else if (cut) {
+        const int first = c * kChunk<T> - lead_of<T, VEC>(row) + tid * N;
+        double w[N], own = 0.0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            w[k] = first + k >= 0 && first + k < p.V ? row.at(first + k) : 0.0;
+            own += w[k];
+        }
+        double chunk_total;
+        const double upto = before + block_running_sum(own, s_warp, chunk_total), limit = r * total;
+        int t = first_thread(own > 0.0 && upto > limit, &s_pick);
+        if (t == kVerifyThreads) t = last_thread(own > 0.0, &s_pick);
+        __syncthreads();
+        if (tid == t) {
+            double run = upto - own;
+            int found = -1;
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (w[k] > 0.0 && (found < 0 || !(run > limit))) {
+                    found = first + k;
+                    run += w[k];
+                }
+            s_pick = found;
+        }
+        __syncthreads();
+        token = s_pick;
+    } else if (stand.x < stand.y) {
         // p lies nowhere above q: the whole of p
         row.q = nullptr;
         row.without = -1;
-        token = walk(p.V, [&](int i) { return row.at(i); }, before, total, r, s_warp, &s_first, &s_base);
+        token = walk(p.V, [&](int i) { return row.at(i); }, before, total, r, s_warp, &s_pick, &s_base);
     }
     for (int j = tid; j <= p.K; j += kVerifyThreads)
-        p.tokens[(int64_t)b * (p.K + 1) + j] = j < n ? p.draft_tokens[(int64_t)b * p.K + j] : j == n ? token : -1;
+        p.tokens[(int64_t)b * (p.K + 1) + j] = j < stand.x ? p.draft_tokens[(int64_t)b * p.K + j] : j == stand.x ? token : -1;
     if (tid == 0) {
-        p.num_accepted[b] = n;
-        if (p.new_lens != nullptr) p.new_lens[b] = max(0, p.seq_lens[b] - (p.K - n));
+        p.num_accepted[b] = stand.x;
+        if (p.new_lens != nullptr) p.new_lens[b] = max(0, p.seq_lens[b] - (p.K - stand.x));
         if (token < 0) atomicOr(p.status, kDevNoProbability);
-        p.arrived[b] = 0;
     }
+}
+
+template <typename F>
+cudaError_t launch(F fn, dim3 grid, bool overlap, const VerifyParams& p, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kVerifyThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = overlap ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, fn, p);
+}
+
+template <typename T, bool VEC>
+cudaError_t launch_all(const VerifyParams& p, cudaStream_t stream) {
+    constexpr int W = kVerifyThreads / 32;
+    const dim3 grid((unsigned)((p.chunks + W - 1) / W), (unsigned)p.B);
+    cudaError_t e;
+    if ((int64_t)p.chunks * p.B <= kAtOnce) {
+        e = launch(plt_draft_verify_sums<T, VEC, true>, grid, false, p, stream);
+    } else {
+        e = launch(plt_draft_verify_count<T>, dim3((unsigned)((p.B + W - 1) / W)), false, p, stream);
+        if (e == cudaSuccess) e = launch(plt_draft_verify_sums<T, VEC, false>, grid, true, p, stream);
+    }
+    if (e == cudaSuccess) e = launch(plt_draft_verify_pick<T, VEC>, dim3((unsigned)p.B), true, p, stream);
+    return e;
 }
 
 plt_status verify_fail(plt_draft_verify_t h, plt_status code, const char* what) {
@@ -426,22 +419,14 @@ plt_status check_config(const plt_draft_verify_config* c) {
     return PLT_OK;
 }
 
-// Chunks of a row: of a length that lets all blocks of the batch run at once, or the longest. A row may start up to 7 elements
-// behind a place of the 16-byte grid (`lead`).
-int chunk_of(int batch, int vocab, int lead) {
-    int chunk = kMinChunk;
-    while (chunk < kMaxChunk && (int64_t)batch * ((vocab + lead + chunk - 1) / chunk) > kOneWave) chunk <<= 1;
-    return chunk;
-}
-
-// Sums that any batch up to the largest leaves.
-size_t sums_of(const plt_draft_verify_config* c) {
-    const size_t most = (size_t)c->max_batch * ((c->vocab + 7 + kMaxChunk - 1) / kMaxChunk);
-    return most > kOneWave ? most : kOneWave;
+// Chunks of a row that starts up to `lead` elements behind a place of the 16-byte grid.
+int chunks_of(const plt_draft_verify_config* c, int lead) {
+    const int chunk = c->dtype == PLT_F32 ? kChunk<float> : kChunk<__nv_bfloat16>;
+    return (c->vocab + lead + chunk - 1) / chunk;
 }
 
 size_t workspace_of(const plt_draft_verify_config* c) {
-    return 8u * sums_of(c) + 4u * (size_t)c->max_batch + 256;
+    return (size_t)c->max_batch * (8u * (size_t)chunks_of(c, 7) + sizeof(int2)) + 256;
 }
 
 }  // namespace
@@ -482,7 +467,7 @@ PLT_API plt_status plt_draft_verify_create(const plt_draft_verify_config* config
     }
     h->status = (uint32_t*)ws;
     h->sums = (double*)((char*)ws + 256);
-    h->arrived = (uint32_t*)(h->sums + sums_of(config));
+    h->stand = (int2*)(h->sums + (size_t)config->max_batch * chunks_of(config, 7));
     cudaError_t e = cudaMemset(ws, 0, bytes);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();   // another stream may run first
     if (e != cudaSuccess) {
@@ -530,8 +515,8 @@ PLT_API plt_status plt_draft_verify_run(plt_draft_verify_t h, const plt_draft_ve
     p.target = a->target_probs; p.draft = a->draft_probs;
     p.draft_tokens = a->draft_tokens; p.draft_lens = a->draft_lens; p.accept_u = a->accept_u; p.sample_u = a->sample_u;
     p.tokens = a->tokens; p.num_accepted = a->num_accepted; p.seq_lens = a->seq_lens; p.new_lens = a->new_lens;
-    p.sums = h->sums; p.arrived = h->arrived; p.status = h->status;
-    p.K = c.max_drafts; p.V = c.vocab;
+    p.sums = h->sums; p.stand = h->stand; p.status = h->status;
+    p.B = a->batch; p.K = c.max_drafts; p.V = c.vocab;
     // 16-byte loads where the rows of p and q that one sequence needs lie alike on the 16-byte grid: always without q
     // (chunks follow p's rows), else where both bases are aligned and all strides are whole vectors.
     const int unit = 16 / es;
@@ -539,21 +524,14 @@ PLT_API plt_status plt_draft_verify_run(plt_draft_verify_t h, const plt_draft_ve
                                          p.target_j % unit == 0 && p.draft_b % unit == 0 && p.draft_j % unit == 0);
     const bool on_grid = !misaligned(a->target_probs, 16) && p.target_b % unit == 0 && p.target_j % unit == 0;
     const int lead = vec && !on_grid ? unit - 1 : 0;
-    p.chunk = chunk_of(a->batch, c.vocab, lead);
-    p.chunks = (c.vocab + lead + p.chunk - 1) / p.chunk;
+    p.chunks = chunks_of(&c, lead);
     DeviceScope scope(h->device);
     if (scope.err != cudaSuccess) return handle_fail(h, g_verify_error, PLT_ERR_CUDA, "cudaSetDevice: %s", cudaGetErrorString(scope.err));
-    const dim3 grid((unsigned)p.chunks, (unsigned)a->batch);
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    if (c.dtype == PLT_F32) {
-        if (vec) plt_draft_verify_kernel<float, true><<<grid, kVerifyThreads, 0, stream>>>(p);
-        else plt_draft_verify_kernel<float, false><<<grid, kVerifyThreads, 0, stream>>>(p);
-    } else {
-        if (vec) plt_draft_verify_kernel<__nv_bfloat16, true><<<grid, kVerifyThreads, 0, stream>>>(p);
-        else plt_draft_verify_kernel<__nv_bfloat16, false><<<grid, kVerifyThreads, 0, stream>>>(p);
-    }
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return handle_fail(h, g_verify_error, PLT_ERR_CUDA, "launching the kernel: %s", cudaGetErrorString(e));
+    cudaError_t e;
+    if (c.dtype == PLT_F32) e = vec ? launch_all<float, true>(p, stream) : launch_all<float, false>(p, stream);
+    else e = vec ? launch_all<__nv_bfloat16, true>(p, stream) : launch_all<__nv_bfloat16, false>(p, stream);
+    if (e != cudaSuccess) return handle_fail(h, g_verify_error, PLT_ERR_CUDA, "launching the kernels: %s", cudaGetErrorString(e));
     return PLT_OK;
 }
 

@@ -13,9 +13,10 @@
 // of a line on which the units' key tiles lie one behind the other, and leaves unnormalised partials for the merge.
 //
 // Warp roles: warp 0 loads K and V tiles by TMA into a ring (pages: their ids one tile ahead); warp 1 issues the products and
-// owns the tensor memory; warps 2 and 3 turn E4M3 codes into f16 (exact) in a second ring, and idle otherwise; warps 4-7 and
-// 8-11 are the softmax of A and of B (thread = row), load their query rows and store the partials. A partial lies as
-// [d / 4][128 rows][4], so that a warp's store is 512 consecutive bytes.
+// owns the tensor memory; warps 2 and 3 turn E4M3 codes into f16 (exact) in a second ring, and idle otherwise; warps 4-11 and
+// 12-19 are the softmax of A and of B, load their query rows and store the partials. Two threads share a row, half the keys of
+// a tile each: they vote, warp by warp, on whether the reference has to move. A partial lies as [d / 4][128 rows][4], so that a
+// warp's store is 512 consecutive bytes.
 //
 // bf16 probabilities carry 8 bits, f16 ones (E4M3 caches) 11; their sum is taken before that rounding, in fp32.
 // Every wait is bounded and reports through the status word.
@@ -27,6 +28,8 @@
 namespace plt {
 namespace {
 
+constexpr int kNearGroups = 32;      // plans of up to this many groups are kept in shared memory
+
 template <int D, bool FP8>
 struct PCfg {
     static constexpr int TILE = kPrefixTile * D * 2;              // a tile of 16-bit elements
@@ -36,10 +39,11 @@ struct PCfg {
     // mbarriers
     static constexpr int QFULL = 0, FULL = 2, EMPTY = FULL + RING, RFULL = EMPTY + RING, REMPTY = RFULL + RAW, SFULL = REMPTY + RAW,
                          PFULL = SFULL + 2, ODONE = PFULL + 2, COUNT = ODONE + 2;
-    static constexpr size_t SMEM = 1024 + 2 * TILE + (size_t)RING * TILE + (size_t)RAW * RAW_TILE + COUNT * 8 + 64;
+    // tiles, barriers, control words, a word for each row (what the threads of a row tell each other), the plan
+    static constexpr size_t SMEM = 1024 + 2 * TILE + (size_t)RING * TILE + (size_t)RAW * RAW_TILE + COUNT * 8 + 64 + 1024 + 4 * (kNearGroups + 1) * 4;
 };
 
-constexpr int kPThreads = 384;
+constexpr int kPThreads = 640;
 
 // Instruction descriptor: fp32 accumulate, A and B both bf16 or both f16, B majorness, N / 8, M / 16.
 __host__ __device__ constexpr uint32_t p_instr_desc(int N, int b_mn_major, bool f16) {
@@ -53,23 +57,26 @@ struct PPiece {
     int len, rows;        // tokens of the prefix, packed rows of the group
     bool wide;            // both tiles have rows of their own
 };
+struct PlanView {
+    const int32_t *begin, *len, *line, *unit;
+};
 struct PWalk {
     int pos, hi, g;
-    __device__ __forceinline__ bool next(const PrefixParams& p, PPiece& pc) {
+    __device__ __forceinline__ bool next(const PrefixParams& p, const PlanView& plan, PPiece& pc) {
         for (;;) {
             if (pos >= hi) return false;
-            while (p.plan.line[g + 1] <= pos) ++g;
+            while (plan.line[g + 1] <= pos) ++g;
             pc.g = g;
-            pc.len = p.plan.len[g];
-            pc.rows = (p.plan.begin[g + 1] - p.plan.begin[g]) * p.R;
+            pc.len = plan.len[g];
+            pc.rows = (plan.begin[g + 1] - plan.begin[g]) * p.R;
             const int per = (pc.len + kPrefixTile - 1) / kPrefixTile + kPrefixLead, nm = (pc.rows + kPrefixRows - 1) / kPrefixRows;
-            const int o = pos - p.plan.line[g], u = o / per, v0 = o - u * per;
+            const int o = pos - plan.line[g], u = o / per, v0 = o - u * per;
             const int end = min(pos + per - v0, hi), v1 = v0 + end - pos;
             pos = end;
             pc.t0 = max(v0 - kPrefixLead, 0);
             pc.t1 = max(v1 - kPrefixLead, 0);
             if (pc.t1 <= pc.t0) continue;
-            pc.unit = p.plan.unit[g] + u;
+            pc.unit = plan.unit[g] + u;
             pc.h = u / nm;
             pc.m = u - pc.h * nm;
             pc.wide = pc.rows - pc.m * kPrefixRows > 128;
@@ -77,9 +84,9 @@ struct PWalk {
         }
     }
 };
-__device__ __forceinline__ PWalk walk_of_block(const PrefixParams& p) {
+__device__ __forceinline__ PWalk walk_of_block(const PrefixParams& p, const PlanView& plan) {
     PWalk w;
-    const int64_t T = p.plan.line[p.groups];
+    const int64_t T = plan.line[p.groups];
     const int C = prefix_blocks(T, p.blocks), c = blockIdx.x;
     w.pos = w.hi = 0;
     w.g = 0;
@@ -89,7 +96,7 @@ __device__ __forceinline__ PWalk walk_of_block(const PrefixParams& p) {
         int lo = 0, hi = p.groups;          // line[lo] <= pos < line[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (p.plan.line[mid] <= w.pos) lo = mid; else hi = mid;
+            if (plan.line[mid] <= w.pos) lo = mid; else hi = mid;
         }
         w.g = lo;
     }
@@ -113,75 +120,56 @@ struct Ring {
     }
 };
 
-// ---- softmax on 32 columns of a row ---------------------------------------------------------------------------------
-template <bool FULL, bool FP8>
-__device__ __forceinline__ void p_chunk(const uint32_t (&r)[32], int c, int lim, float2 sc2, float2 nm2, uint32_t* pk, float2& sum2,
-                                        uint32_t& pmax) {
-#pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-        float2 t = __ffma2_rn(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), sc2, nm2);
-        if (!FULL) {
-            if (c * 32 + i >= lim) t.x = -INFINITY;
-            if (c * 32 + i + 1 >= lim) t.y = -INFINITY;
-        }
-        const float2 pr = make_float2(fast_exp2(t.x), fast_exp2(t.y));
-        sum2 = __fadd2_rn(sum2, pr);
-        const uint32_t h = FP8 ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);
-        pk[i / 2] = h;
-        asm("max.u16x2 %0, %0, %1;" : "+r"(pmax) : "r"(h));      // patterns of numbers that are not negative order like integers
-    }
-}
-// Largest pattern that needs no new reference: 2^8 in bf16; with f16 references lie 2^8 below the maximum, and 2^14 is the limit.
+// ---- softmax on a thread's 64 scores of a row --------------------------------------------------------------------------
+// Powers of two above the reference that a score may reach before the reference moves. With f16 probabilities references lie 8
+// below the maximum, so that the small ones do not fall under f16's range: up to 2^14 stays far from its end.
 template <bool FP8>
-constexpr uint32_t kBigPattern = FP8 ? 0x7400u : 0x4380u;
+constexpr float kAbove = FP8 ? 14.f : 8.f;
 template <bool FP8>
 constexpr float kBelow = FP8 ? 8.f : 0.f;
 
-template <bool FP8>
-__device__ __forceinline__ void p_pass(uint32_t tS, int lim, bool full, float scale, float mref, uint32_t (&pk)[64], float& lsum,
-                                       uint32_t& pbig) {
-    const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-mref, -mref);
-    float2 sum2 = make_float2(0.f, 0.f);
-    uint32_t pmax = 0;
-    uint32_t ra[32], rb[32];
-    tmem_ld32(tS, ra);
-    tmem_wait_ld();
-    tmem_ld32(tS + 32, rb);
-    if (full) p_chunk<true, FP8>(ra, 0, lim, sc2, nm2, &pk[0], sum2, pmax); else p_chunk<false, FP8>(ra, 0, lim, sc2, nm2, &pk[0], sum2, pmax);
-    tmem_wait_ld();
-    tmem_ld32(tS + 64, ra);
-    if (full) p_chunk<true, FP8>(rb, 1, lim, sc2, nm2, &pk[16], sum2, pmax); else p_chunk<false, FP8>(rb, 1, lim, sc2, nm2, &pk[16], sum2, pmax);
-    tmem_wait_ld();
-    tmem_ld32(tS + 96, rb);
-    if (full) p_chunk<true, FP8>(ra, 2, lim, sc2, nm2, &pk[32], sum2, pmax); else p_chunk<false, FP8>(ra, 2, lim, sc2, nm2, &pk[32], sum2, pmax);
-    tmem_wait_ld();
-    if (full) p_chunk<true, FP8>(rb, 3, lim, sc2, nm2, &pk[48], sum2, pmax); else p_chunk<false, FP8>(rb, 3, lim, sc2, nm2, &pk[48], sum2, pmax);
-    lsum = sum2.x + sum2.y;
-    pbig = max(pmax & 0xffffu, pmax >> 16);
-}
-__device__ __forceinline__ float p_row_max(uint32_t tS, int lim) {
-    float mx = -INFINITY;
+// Largest of 32 scores, those before `lim` where not all count.
+__device__ __forceinline__ float p_max(const uint32_t (&r)[32], bool full, int lim) {
+    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (full) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        uint32_t r[32];
-        tmem_ld32(tS + c * 32, r);
-        tmem_wait_ld();
+        for (int i = 0; i < 32; i += 8)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m[j] = fmaxf(fmaxf(m[j], __uint_as_float(r[i + 2 * j])), __uint_as_float(r[i + 2 * j + 1]));
+    } else {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-            if (c * 32 + i < lim) mx = fmaxf(mx, __uint_as_float(r[i]));
+            if (i < lim) m[i & 3] = fmaxf(m[i & 3], __uint_as_float(r[i]));
     }
-    return mx;
+    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
-template <int D>
-__device__ __forceinline__ void p_scale_o(uint32_t tO, float f) {
+
+// 32 scores -> probabilities, packed 16 bits wide, and their sum.
+template <bool FP8>
+__device__ __forceinline__ void p_chunk(uint32_t (&r)[32], bool full, int lim, float2 sc2, float2 nm2, uint32_t (&pk)[16], float2& sum2) {
+    if (!full)
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
-        uint32_t r[32];
-        tmem_ld32(tO + c * 32, r);
+        for (int i = 0; i < 32; ++i)
+            if (i >= lim) r[i] = 0xff800000u;              // -inf
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+        const float2 t = __ffma2_rn(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), sc2, nm2);
+        const float2 pr = make_float2(fast_exp2(t.x), fast_exp2(t.y));
+        sum2 = __fadd2_rn(sum2, pr);
+        pk[i / 2] = FP8 ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);
+    }
+}
+// Multiplies N columns of this thread's row of O by f; rolled, since a thread has 32 scores in registers meanwhile.
+template <int N>
+__device__ __forceinline__ void p_scale_o(uint32_t tO, float f) {
+#pragma unroll 1
+    for (int c = 0; c < N / 16; ++c) {
+        uint32_t r[16];
+        tmem_ld16(tO + c * 16, r);
         tmem_wait_ld();
 #pragma unroll
-        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
-        tmem_st32(tO + c * 32, r);
+        for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+        tmem_st16(tO + c * 16, r);
     }
     tmem_wait_st();
 }
@@ -198,6 +186,8 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     uint8_t* raw = ring + (size_t)C::RING * C::TILE;               // [RAW][tile of codes]
     uint64_t* bars = (uint64_t*)(raw + (size_t)C::RAW * C::RAW_TILE);
     int32_t* s_ctl = (int32_t*)(bars + C::COUNT);                  // [0] abort flag, [1] tensor-memory base, [2] loads issued
+    float* s_row = (float*)(s_ctl + 16);                           // [2 tiles][128 rows]
+    int32_t* s_plan = (int32_t*)(s_row + 256);                     // begin, len, line, unit: [kNearGroups + 1] each
     volatile int* abort_flag = (volatile int*)s_ctl;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
 
@@ -213,9 +203,9 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             mbar_init(&bars[C::REMPTY + s], 2);
         }
         for (int x = 0; x < 2; ++x) {
-            mbar_init(&bars[C::QFULL + x], 4);
+            mbar_init(&bars[C::QFULL + x], 8);
             mbar_init(&bars[C::SFULL + x], 1);
-            mbar_init(&bars[C::PFULL + x], 4);
+            mbar_init(&bars[C::PFULL + x], 8);
             mbar_init(&bars[C::ODONE + x], 1);
         }
         mbar_fence_init();
@@ -225,12 +215,24 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = (uint32_t)s_ctl[1];
-    // columns: S_A 0..127 (P_A over 0..63), S_B 128..255, O_A from 256, O_B from 384
+    // columns: S_A 0..127 (P_A over the first 16 of every 32, whose scores have been read by then), S_B 128..255, O_A from
+    // 256, O_B from 384
     // The plan (and whatever the caller's kernels before it wrote) is complete from here on; the kernel behind this one reads
     // the plan's lengths before its own wait, hence is not let go earlier.
     grid_dependency_wait();
     grid_launch_dependents();
-    PWalk walk = walk_of_block(p);
+    PlanView plan = {p.plan.begin, p.plan.len, p.plan.line, p.plan.unit};
+    if (p.groups <= kNearGroups) {
+        constexpr int W = kNearGroups + 1;
+        if (tid < 4 * W) {
+            const int which = tid / W, g = tid - which * W;
+            const int32_t* from = which == 0 ? plan.begin : which == 1 ? plan.len : which == 2 ? plan.line : plan.unit;
+            if (g < p.groups + (which != 1)) s_plan[tid] = from[g];
+        }
+        plan = {s_plan, s_plan + W, s_plan + 2 * W, s_plan + 3 * W};
+        __syncthreads();
+    }
+    PWalk walk = walk_of_block(p, plan);
     PPiece pc;
     bool ok = true;
 
@@ -250,7 +252,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             tma_prefetch_desc(&tmK);
             tma_prefetch_desc(&tmV);
         }
-        while (ok && walk.next(p, pc)) {
+        while (ok && walk.next(p, plan, pc)) {
             // lane j holds the page of the tile's j-th box, read one tile ahead
             auto page_of = [&](int t) {
                 const int key = t * kPrefixTile + lane * p.kbox;
@@ -297,7 +299,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         const uint32_t q_a = smem_u32(q_smem), ring_a = smem_u32(ring);
         uint32_t base = 0;                    // ring tiles before this piece: K of its i-th key tile is base + 2 i, V the next
         uint32_t q_parity[2] = {0, 0}, p_parity[2] = {0, 0};
-        while (ok && walk.next(p, pc)) {
+        while (ok && walk.next(p, plan, pc)) {
             const int n = pc.t1 - pc.t0;
             auto wait_tile = [&](uint32_t cnt) {
                 bool y = seq_wait(&bars[C::FULL + cnt % C::RING], (cnt / C::RING) & 1u, abort_flag);
@@ -352,7 +354,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                     const uint32_t va = ring_a + slot * C::TILE;
 #pragma unroll
                     for (int kk = 0; kk < kPrefixTile / 16; ++kk)
-                        umma_bf16_ts(tmem_base + 256 + x * 128, tmem_base + x * 128 + kk * 8, seq_smem_desc(va + kk * 2048, HB, 1024), idesc_pv,
+                        umma_bf16_ts(tmem_base + 256 + x * 128, tmem_base + x * 128 + (kk >> 1) * 32 + (kk & 1) * 8, seq_smem_desc(va + kk * 2048, HB, 1024), idesc_pv,
                                      (i > (pc.wide ? 0 : x) || kk > 0) ? 1u : 0u);
                     if (!pc.wide || x == 1) umma_commit(&bars[C::EMPTY + slot]);
                     if (last) umma_commit(&bars[C::ODONE + x]);
@@ -387,7 +389,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             Ring<C::RING> dst;
             uint32_t done = 0;
             const int t64 = tid - 64;
-            while (ok && walk.next(p, pc))
+            while (ok && walk.next(p, plan, pc))
                 for (int t = pc.t0; t < pc.t1 && ok; ++t)
                     for (int which = 0; which < 2 && ok; ++which) {
                         ok = seq_wait(&bars[C::RFULL + src.slot], src.parity, abort_flag);
@@ -427,37 +429,41 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     } else {
         // =========================== softmax, query rows and partials ======================================
         constexpr int HB = kPrefixTile * 128;
-        const int x = (wid - 4) >> 2;                      // 0: tile A, 1: tile B
+        constexpr int PART = D / 2;                        // columns of O, and elements of the query row, that a thread takes
+        const int x = (wid - 4) >> 3, half = ((wid - 4) >> 2) & 1;
         const int wq = wid & 3, row = wq * 32 + lane;      // lane quarter of tensor memory; row of the tile
+        const int pair = 1 + x * 4 + wq;                   // named barrier of the two warps that share rows
         const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
-        const uint32_t tS = tmem_base + lane_off + x * 128, tO = tmem_base + lane_off + 256 + x * 128;
+        const uint32_t tS = tmem_base + lane_off + x * 128 + half * 64, tO = tmem_base + lane_off + 256 + x * 128 + half * PART;
+        float* const told = s_row + x * 128 + row;
         uint32_t s_parity = 0, o_parity = 0;
-        while (ok && walk.next(p, pc)) {
+        while (ok && walk.next(p, plan, pc)) {
             // ---- this row's query, and how many tokens of the prefix it sees ------------------------------------
             const int lr = pc.m * kPrefixRows + (pc.wide ? x * 128 : 0) + row;
             const int mine = tiles_of(pc, x), step = pc.wide ? 1 : 2;
             int sees = 0;
             if (mine > 0) {
                 uint8_t* q = q_smem + x * C::TILE;
-                if (lr < pc.rows) {
-                    const int b = p.plan.begin[pc.g] + lr / p.R, r = lr % p.R, lq = r / p.G, l = lq / p.Qn;
-                    const int cut = (int)min((int64_t)p.seq_lens[b], (int64_t)pc.len + p.max_seq_len) - p.delta[l] - (p.Qn - 1 - lq % p.Qn);
-                    sees = max(0, min(pc.len, cut));
-                    const uint4* src = (const uint4*)((const __nv_bfloat16*)p.q + (((int64_t)b * p.L * p.Qn + lq) * p.Hq + pc.h * p.G + (r - lq * p.G)) * D);
-#pragma unroll 4
-                    for (int c = 0; c < D / 8; ++c) {
-                        uint4 v = src[c];
-                        if (FP8) {
-                            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                const bool in = lr < pc.rows;
+                const int b = in ? plan.begin[pc.g] + lr / p.R : 0, r = in ? lr % p.R : 0, lq = r / p.G;
+                const uint4* src = (const uint4*)((const __nv_bfloat16*)p.q + (((int64_t)b * p.L * p.Qn + lq) * p.Hq + pc.h * p.G + (r - lq * p.G)) * D + half * PART);
+                uint4 v[PART / 8];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) w[i] = pack_f16x2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
-                            v = make_uint4(w[0], w[1], w[2], w[3]);
-                        }
-                        *(uint4*)(q + (c >> 3) * HB + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+                for (int c = 0; c < PART / 8; ++c) v[c] = in ? src[c] : make_uint4(0, 0, 0, 0);
+                if (in) {
+                    const int cut = (int)min((int64_t)p.seq_lens[b], (int64_t)pc.len + p.max_seq_len) - p.delta[lq / p.Qn] - (p.Qn - 1 - lq % p.Qn);
+                    sees = max(0, min(pc.len, cut));
+                }
+#pragma unroll
+                for (int c = 0; c < PART / 8; ++c) {
+                    if (FP8) {
+                        uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = pack_f16x2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+                        v[c] = make_uint4(w[0], w[1], w[2], w[3]);
                     }
-                } else {
-#pragma unroll 4
-                    for (int c = 0; c < D / 8; ++c) *(uint4*)(q + (c >> 3) * HB + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+                    const int ch = half * (PART / 8) + c;
+                    *(uint4*)(q + (ch >> 3) * HB + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = v[c];
                 }
                 fence_proxy_async_smem();
                 tc_fence_before_sync();
@@ -473,25 +479,38 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 if (!ok) break;
                 tc_fence_after_sync();
                 const int t = pc.t0 + (pc.wide ? 0 : x) + i * step;
-                const int lim = sees - t * kPrefixTile;    // keys [0, lim) of the tile are visible to this row
-                const bool full = __all_sync(0xffffffffu, lim >= kPrefixTile);
-                uint32_t pk[64], pbig = 0xffffu;
-                float lsum = 0.f;
-                if (i > 0) p_pass<FP8>(tS, lim, full, scale, mref, pk, lsum, pbig);
-                if (__any_sync(0xffffffffu, i == 0 || (lim > 0 && pbig > kBigPattern<FP8>))) {
-                    // the tile's true maximum, rescale of this row of O (every product into it has completed: the commit behind
-                    // S_FULL covers them), and the probabilities against the new reference
-                    const float mx = p_row_max(tS, lim) * scale;
-                    const float m_new = fmaxf(mref, mx - kBelow<FP8>);
-                    const float alpha = fast_exp2(mref - m_new);
-                    mref = m_new;
+                const int lim = sees - t * kPrefixTile - half * 64;    // this thread's keys [0, lim) are visible to the row
+                const bool full = __all_sync(0xffffffffu, lim >= 64);
+                uint32_t r[32];
+                tmem_ld32(tS, r);
+                tmem_wait_ld();
+                float top = p_max(r, full, lim);
+                tmem_ld32(tS + 32, r);                     // stay in registers for their probabilities
+                tmem_wait_ld();
+                top = fmaxf(top, p_max(r, full, lim - 32)) * scale;
+                if (named_barrier_or(pair, 64, i == 0 || top > mref + kAbove<FP8>)) {
+                    // the row's maximum over both threads, and O against the new reference (every product into it has completed:
+                    // the commit behind S_FULL covers them)
+                    if (half == 1) *told = top;
+                    named_barrier_sync(pair, 64);
+                    const float m_new = half == 0 ? fmaxf(mref, fmaxf(top, *told) - kBelow<FP8>) : 0.f;
+                    if (half == 0) *told = m_new;
+                    named_barrier_sync(pair, 64);
+                    const float m = *told, alpha = fast_exp2(mref - m);
+                    mref = m;
                     sum *= alpha;
-                    if (i > 0) p_scale_o<D>(tO, alpha);
-                    p_pass<FP8>(tS, lim, full, scale, mref, pk, lsum, pbig);
+                    if (i > 0) p_scale_o<PART>(tO, alpha);
                 }
-                sum += lsum;
-#pragma unroll
-                for (int c = 0; c < 2; ++c) tmem_st32(tS + c * 32, &pk[c * 32]);
+                const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-mref, -mref);
+                float2 sum2 = make_float2(0.f, 0.f);
+                uint32_t pk[16];
+                p_chunk<FP8>(r, full, lim - 32, sc2, nm2, pk, sum2);
+                tmem_ld32(tS, r);
+                tmem_st16(tS + 32, pk);
+                tmem_wait_ld();
+                p_chunk<FP8>(r, full, lim, sc2, nm2, pk, sum2);
+                tmem_st16(tS, pk);
+                sum += sum2.x + sum2.y;
                 tmem_wait_st();
                 tc_fence_before_sync();
                 __syncwarp();
@@ -500,8 +519,13 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             if (!ok) break;
             // ---- the partial ---------------------------------------------------------------------------------------
             const int64_t slot = (int64_t)pc.unit + blockIdx.x;
-            const bool saw = mine > 0 && mref > kSeqNoMax;
-            *(float2*)(p.ml + ((slot * 2 + x) * 128 + row) * 2) = make_float2(saw ? mref : -INFINITY, saw ? sum : 0.f);
+            if (half == 1) *told = sum;
+            named_barrier_sync(pair, 64);
+            if (half == 0) {
+                const bool saw = mine > 0 && mref > kSeqNoMax;
+                *(float2*)(p.ml + ((slot * 2 + x) * 128 + row) * 2) = make_float2(saw ? mref : -INFINITY, saw ? sum + *told : 0.f);
+            }
+            named_barrier_sync(pair, 64);
             if (mine > 0) {
                 ok = seq_wait(&bars[C::ODONE + x], o_parity, abort_flag);
                 ok = __all_sync(0xffffffffu, ok);
@@ -509,9 +533,9 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 if (!ok) break;
                 tc_fence_after_sync();
                 const float f = FP8 ? p.v_scale[pc.h] : 1.f;
-                float* out = p.acc + (slot * 2 + x) * (128 * D) + row * 4;
+                float* out = p.acc + (slot * 2 + x) * (128 * D) + half * (PART / 4) * 512 + row * 4;
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
+                for (int c = 0; c < PART / 32; ++c) {
                     uint32_t r[32];
                     tmem_ld32(tO + c * 32, r);
                     tmem_wait_ld();

@@ -1,7 +1,8 @@
 // Merge of a decode step with shared prefixes: for every row the partials of its group's prefix and of its own cache are joined
-// by their references into one softmax, the window's likewise, and the gate mixes the two (Eq. 2). A thread holds 16 of a row's
+// by their references into one softmax, the window's likewise, and the gate mixes the two (Eq. 2). A thread holds 8 of a row's
 // elements and a warp 32 neighbouring rows, so that the prefix's partials, which lie [d / 4][128 rows][4], are read 512 bytes at
-// a time. Everything up to the store is fp32. Bound by reading the partials (from L2) and by latency.
+// a time; the loads of four partials are in flight together. Everything up to the store is fp32. Bound by reading the partials
+// (from L2) and by latency.
 #include <cuda_bf16.h>
 
 #include "plt_prefix.h"
@@ -10,17 +11,52 @@
 namespace plt {
 namespace {
 
-// Adds f times 16 elements that lie in four pieces of four, `step` floats apart.
-__device__ __forceinline__ void add16(float (&y)[16], const float* src, int64_t step, float f) {
-    float4 v[4];
+constexpr int kMergeBatch = 4;
+
+// Joins `n` partials of a row into y, top and sum: part(k, ml, acc, step) says where partial k's (reference, sum) and its
+// elements (two pieces of four, `step` floats apart) lie.
+template <typename F>
+__device__ __forceinline__ void join(int n, F part, float (&y)[8], float& top, float& sum) {
+    for (int k0 = 0; k0 < n; k0 += kMergeBatch) {
+        float2 ml[kMergeBatch];
+        float4 v[kMergeBatch][2];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = *(const float4*)(src + k * step);
+        for (int u = 0; u < kMergeBatch; ++u) {
+            ml[u] = make_float2(-INFINITY, 0.f);
+            v[u][0] = v[u][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (k0 + u < n) {
+                const float2* m;
+                const float* acc;
+                int step;
+                part(k0 + u, m, acc, step);
+                ml[u] = *m;
+                v[u][0] = *(const float4*)acc;
+                v[u][1] = *(const float4*)(acc + step);
+            }
+        }
+        float m = top;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        y[4 * k] = fmaf(v[k].x, f, y[4 * k]);
-        y[4 * k + 1] = fmaf(v[k].y, f, y[4 * k + 1]);
-        y[4 * k + 2] = fmaf(v[k].z, f, y[4 * k + 2]);
-        y[4 * k + 3] = fmaf(v[k].w, f, y[4 * k + 3]);
+        for (int u = 0; u < kMergeBatch; ++u) m = fmaxf(m, ml[u].x);
+        if (m == -INFINITY) continue;            // nothing seen yet
+        const float old = exp2f(top - m);
+        top = m;
+        sum *= old;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] *= old;
+#pragma unroll
+        for (int u = 0; u < kMergeBatch; ++u) {
+            if (ml[u].x == -INFINITY) continue;  // saw no key: what lies there was not written
+            const float f = exp2f(ml[u].x - m);
+            sum = fmaf(ml[u].y, f, sum);
+            y[0] = fmaf(v[u][0].x, f, y[0]);
+            y[1] = fmaf(v[u][0].y, f, y[1]);
+            y[2] = fmaf(v[u][0].z, f, y[2]);
+            y[3] = fmaf(v[u][0].w, f, y[3]);
+            y[4] = fmaf(v[u][1].x, f, y[4]);
+            y[5] = fmaf(v[u][1].y, f, y[5]);
+            y[6] = fmaf(v[u][1].z, f, y[6]);
+            y[7] = fmaf(v[u][1].w, f, y[7]);
+        }
     }
 }
 
@@ -39,9 +75,9 @@ __device__ __forceinline__ Own own_pieces(const Params& p, int item, int hl, int
 }
 
 template <int D>
-__global__ void __launch_bounds__(D * 2) plt_prefix_merge(const __grid_constant__ Params p, const __grid_constant__ PrefixParams pp) {
+__global__ void __launch_bounds__(D * 4) plt_prefix_merge(const __grid_constant__ Params p, const __grid_constant__ PrefixParams pp) {
     grid_launch_dependents();
-    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;       // elements 16 part .. 16 part + 15
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;       // elements 8 part .. 8 part + 7
     const int h = blockIdx.y;
     const int64_t id = (int64_t)blockIdx.x * 32 + lane;
     const bool in = id < (int64_t)p.B * p.R;
@@ -92,60 +128,36 @@ __global__ void __launch_bounds__(D * 2) plt_prefix_merge(const __grid_constant_
     if (in && cut > 0 && wl > 0) ow = own_pieces(p, item_index(p, b, hg, 1), hl, r);
 
     // ---- one softmax over the prefix and the own keys ---------------------------------------------------------------
-    float top = -INFINITY;
-    for (int c = c0; c <= c1; ++c)
-        for (int x = x0; x <= x1; ++x) top = fmaxf(top, pp.ml[(((unit + c) * 2 + x) * 128 + row) * 2]);
-    for (int i = 0; i < og.n; ++i) top = fmaxf(top, p.part_ml[(og.row0 + i * og.step) * 2]);
-    float y[16], sum = 0.f;
+    float y[8], z[8], top = -INFINITY, sum = 0.f, top_w = -INFINITY, sum_w = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) y[i] = 0.f;
-    if (top > -INFINITY) {
-        for (int c = c0; c <= c1; ++c)
-            for (int x = x0; x <= x1; ++x) {
-                const int64_t at = ((unit + c) * 2 + x) * 128;
-                const float2 ml = *(const float2*)(pp.ml + (at + row) * 2);
-                if (ml.x == -INFINITY) continue;      // saw no key: its sums were not written
-                const float f = exp2f(ml.x - top);
-                sum = fmaf(ml.y, f, sum);
-                add16(y, pp.acc + at * D + part * 4 * 512 + row * 4, 512, f);
-            }
-        for (int i = 0; i < og.n; ++i) {
-            const int64_t at = og.row0 + i * og.step;
-            const float2 ml = *(const float2*)(p.part_ml + at * 2);
-            if (ml.x == -INFINITY) continue;
-            const float f = exp2f(ml.x - top);
-            sum = fmaf(ml.y, f, sum);
-            add16(y, p.part_acc + at * D + part * 16, 4, f);
+    for (int i = 0; i < 8; ++i) y[i] = z[i] = 0.f;
+    const int tiles = x1 - x0 + 1, shared = (c1 - c0 + 1) * tiles;
+    join(shared + og.n, [&](int k, const float2*& m, const float*& acc, int& step) {
+        if (k < shared) {
+            const int64_t at = ((unit + c0 + k / tiles) * 2 + x0 + k % tiles) * 128;
+            m = (const float2*)(pp.ml + (at + row) * 2);
+            acc = pp.acc + at * D + part * 2 * 512 + row * 4;
+            step = 512;
+        } else {
+            const int64_t at = og.row0 + (k - shared) * og.step;
+            m = (const float2*)(p.part_ml + at * 2);
+            acc = p.part_acc + at * D + part * 8;
+            step = 4;
         }
-    }
-    const float ig = sum > 0.f ? (1.f - gate) / sum : 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) y[i] *= ig;
+    }, y, top, sum);
     // ---- the window -----------------------------------------------------------------------------------------------------
-    if (ow.n > 0) {
-        top = -INFINITY;
-        sum = 0.f;
-        for (int i = 0; i < ow.n; ++i) top = fmaxf(top, p.part_ml[(ow.row0 + i * ow.step) * 2]);
-        if (top > -INFINITY) {
-            for (int i = 0; i < ow.n; ++i) {
-                const float2 ml = *(const float2*)(p.part_ml + (ow.row0 + i * ow.step) * 2);
-                sum += ml.y * exp2f(ml.x - top);
-            }
-            const float il = sum > 0.f ? gate / sum : 0.f;
-            for (int i = 0; i < ow.n; ++i) {
-                const int64_t at = ow.row0 + i * ow.step;
-                const float m = p.part_ml[at * 2];
-                if (m > -INFINITY) add16(y, p.part_acc + at * D + part * 16, 4, exp2f(m - top) * il);
-            }
-        }
-    }
-    if (!in) return;
-    if (cut == 0)
+    join(ow.n, [&](int k, const float2*& m, const float*& acc, int& step) {
+        const int64_t at = ow.row0 + k * ow.step;
+        m = (const float2*)(p.part_ml + at * 2);
+        acc = p.part_acc + at * D + part * 8;
+        step = 4;
+    }, z, top_w, sum_w);
+    const float ig = sum > 0.f ? (1.f - gate) / sum : 0.f, il = sum_w > 0.f ? gate / sum_w : 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = 0.f;
-    uint4* dst = (uint4*)((__nv_bfloat16*)p.out + (((int64_t)b * p.L * p.Qn + lq) * p.Hq + head) * D + part * 16);
-    dst[0] = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-    dst[1] = make_uint4(pack_bf16x2(y[8], y[9]), pack_bf16x2(y[10], y[11]), pack_bf16x2(y[12], y[13]), pack_bf16x2(y[14], y[15]));
+    for (int i = 0; i < 8; ++i) y[i] = cut > 0 ? fmaf(z[i], il, y[i] * ig) : 0.f;
+    if (!in) return;
+    uint4* dst = (uint4*)((__nv_bfloat16*)p.out + (((int64_t)b * p.L * p.Qn + lq) * p.Hq + head) * D + part * 8);
+    *dst = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
 }
 
 }  // namespace
@@ -153,7 +165,7 @@ __global__ void __launch_bounds__(D * 2) plt_prefix_merge(const __grid_constant_
 cudaError_t launch_prefix_merge(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(((int64_t)p.B * p.R + 31) / 32), (unsigned)p.Hkv);
-    cfg.blockDim = dim3((unsigned)p.d * 2);
+    cfg.blockDim = dim3((unsigned)p.d * 4);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

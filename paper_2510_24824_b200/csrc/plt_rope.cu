@@ -137,7 +137,7 @@ __device__ __forceinline__ void norm_and_turn(float (&x)[16], const Lane<D>& ln,
         const float inv = 1.f / sqrtf(ss * (1.f / D) + eps);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float4 g = *(const float4*)(gain + (i < 2 ? ln.o0 : ln.o1) + 4 * (i & 1));
+            const float4 g = *((const float4*)gain + i * (D / 16) + ln.t);
             x[4 * i] *= inv * g.x;
             x[4 * i + 1] *= inv * g.y;
             x[4 * i + 2] *= inv * g.z;
@@ -147,7 +147,7 @@ __device__ __forceinline__ void norm_and_turn(float (&x)[16], const Lane<D>& ln,
     if (ln.turning) {
         float4 t4[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t4[i] = *((const float4*)(cs + ln.t * 8) + i);
+        for (int i = 0; i < 4; ++i) t4[i] = *((const float4*)cs + i * (D / 16) + ln.t);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float c = (i & 1) ? t4[i / 2].z : t4[i / 2].x, s = (i & 1) ? t4[i / 2].w : t4[i / 2].y;
@@ -216,7 +216,11 @@ __global__ void __launch_bounds__(kRopeThreads, SEQ ? 4 : 2) plt_rope_kernel(con
     }
     if (tid < 2 * D) {
         const float* gain = tid < D ? p.q_gain : p.k_gain;
-        s_gain[tid / D][tid % D] = gain != nullptr ? gain[tid % D] : 1.f;
+        // element e of a thread's 16 (pieces at o0 and o1): [e / 4][thread][e % 4]
+        const int i = tid % D, e = i / (TPR * 4) * 4 + i % 4, owner = i / 4 % TPR;
+        const bool halves = owner < p.rd / 16 && !p.interleaved;
+        const int o = e < 8 ? (halves ? owner : 2 * owner) * 8 + e : (halves ? owner + p.rd / 16 : 2 * owner + 1) * 8 + e - 8;
+        s_gain[tid / D][i] = gain != nullptr ? gain[o] : 1.f;
     }
     if (tid < TB) {
         Token tk;
@@ -255,7 +259,9 @@ __global__ void __launch_bounds__(kRopeThreads, SEQ ? 4 : 2) plt_rope_kernel(con
         float s, c;
         sincospif((float)(int32_t)((uint32_t)x - ((uint32_t)quarter << 30)) * 4.656612873077393e-10f, &s, &c);   // 2^-31: half turns
         const float cc = (quarter & 1) ? -s : c, ss = (quarter & 1) ? c : s;
-        s_cs[tk][f] = (quarter & 2) ? make_float2(-cc * p.factor, -ss * p.factor) : make_float2(cc * p.factor, ss * p.factor);
+        // pair k of a thread's 8: [k / 2][thread][k % 2], so that neighbouring threads read neighbouring words
+        float2* const to = &s_cs[tk][((f % 8) / 2 * TPR + f / 8) * 2 + f % 2];
+        *to = (quarter & 2) ? make_float2(-cc * p.factor, -ss * p.factor) : make_float2(cc * p.factor, ss * p.factor);
     }
     __syncthreads();
 
