@@ -108,6 +108,22 @@ __device__ __forceinline__ int tiles_of(const PPiece& pc, int x) {
     return pc.wide ? n : (n + 1 - x) >> 1;
 }
 
+// True in one thread of a converged warp, always the same. The compiler sees that a branch on it holds a single thread, and
+// issues the products one behind the other; behind `lane == 0` it cannot know, and each took twice as long to issue.
+__device__ __forceinline__ bool one_thread() {
+    uint32_t y;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(y));
+    return y != 0;
+}
+
+// A value that all lanes of a converged warp hold alike, in a form that the compiler keeps in uniform registers.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+// umma_commit on a barrier's shared-memory address.
+__device__ __forceinline__ void commit_to(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
 template <int RING>
 struct Ring {
     int slot = 0;
@@ -144,6 +160,24 @@ __device__ __forceinline__ float p_max(const uint32_t (&r)[32], bool full, int l
     return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 
+// 2^t of two numbers on the multiply-add units, which the special-function unit (four results a cycle for each scheduler) leaves
+// idle: t = n + f with n the nearest integer (Cody and Waite's split; n falls out of an addition of 1.5 * 2^23), 2^f on
+// [-1/2, 1/2] by the cubic of least largest relative error (found by Lawson's iteration; 2^-13.7, a fiftieth of what rounding a
+// probability to 8 bits costs), n added to the exponent. Below 2^-125 it stays there, which is 0 beside any probability of 1.
+__device__ __forceinline__ float2 exp2_by_fma(float2 t) {
+    const float2 magic = make_float2(12582912.f, 12582912.f), minus = make_float2(-12582912.f, -12582912.f);
+    t.x = fmaxf(t.x, -125.f);
+    t.y = fmaxf(t.y, -125.f);
+    const float2 z = __fadd2_rn(t, magic);
+    const float2 n = __fadd2_rn(z, minus);
+    const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), t);
+    float2 e = __ffma2_rn(f, make_float2(0.05517167f, 0.05517167f), make_float2(0.24261113f, 0.24261113f));
+    e = __ffma2_rn(f, e, make_float2(0.69326097f, 0.69326097f));
+    e = __ffma2_rn(f, e, make_float2(0.99992806f, 0.99992806f));
+    return make_float2(__uint_as_float(__float_as_uint(e.x) + (__float_as_uint(z.x) << 23)),
+                       __uint_as_float(__float_as_uint(e.y) + (__float_as_uint(z.y) << 23)));
+}
+
 // 32 scores -> probabilities, packed 16 bits wide, and their sum.
 template <bool FP8>
 __device__ __forceinline__ void p_chunk(uint32_t (&r)[32], bool full, int lim, float2 sc2, float2 nm2, uint32_t (&pk)[16], float2& sum2) {
@@ -154,7 +188,7 @@ __device__ __forceinline__ void p_chunk(uint32_t (&r)[32], bool full, int lim, f
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
         const float2 t = __ffma2_rn(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), sc2, nm2);
-        const float2 pr = make_float2(fast_exp2(t.x), fast_exp2(t.y));
+        const float2 pr = (i & 2) != 0 && (i & 4) != 0 ? exp2_by_fma(t) : make_float2(fast_exp2(t.x), fast_exp2(t.y));
         sum2 = __fadd2_rn(sum2, pr);
         pk[i / 2] = FP8 ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);
     }
@@ -293,10 +327,10 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         if (lane == 0) s_ctl[2] = (int32_t)issued;
         if (flags) atomicOr(p.status, flags);
     } else if (wid == 1) {
-        // =========================== product issue (whole warp walks, lane 0 issues) =====================
+        // =========================== product issue (whole warp walks, one thread issues) =====================
         constexpr uint32_t idesc_qk = p_instr_desc(128, 0, FP8), idesc_pv = p_instr_desc(D, 1, FP8);
         constexpr int HB = kPrefixTile * 128;
-        const uint32_t q_a = smem_u32(q_smem), ring_a = smem_u32(ring);
+        const uint32_t q_a = smem_u32(q_smem), ring_a = smem_u32(ring), bars_a = smem_u32(bars);
         uint32_t base = 0;                    // ring tiles before this piece: K of its i-th key tile is base + 2 i, V the next
         uint32_t q_parity[2] = {0, 0}, p_parity[2] = {0, 0};
         while (ok && walk.next(p, plan, pc)) {
@@ -311,20 +345,24 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 ok = __all_sync(0xffffffffu, ok);
                 q_parity[x] ^= 1u;
             };
-            // S_x = Q_x . K(i)^T. The K tile is free once the last tile that takes it has been issued.
+            // S_x = Q_x . K(i)^T. The K tile is free once the last tile that takes it has been issued. (The first tile of a wide
+            // piece has waited for K and V when the second comes.)
             auto issue_s = [&](int i, int x) {
-                const uint32_t cnt = base + 2u * (uint32_t)i;
-                wait_tile(cnt);
+                const uint32_t cnt = base + 2u * (uint32_t)i, slot = cnt % C::RING;
+                if (!pc.wide || x == 0) wait_tile(cnt);
                 if (!ok) return;
                 tc_fence_after_sync();
-                if (lane == 0) {
-                    const uint32_t ka = ring_a + (cnt % C::RING) * C::TILE, qa = q_a + (uint32_t)x * C::TILE;
+                const uint64_t k0 = uniform(seq_smem_desc(ring_a + slot * C::TILE, 16, 1024)), q0 = uniform(seq_smem_desc(q_a + (uint32_t)x * C::TILE, 16, 1024));
+                const uint32_t to = uniform(tmem_base + x * 128), free_bar = uniform(bars_a + 8u * (C::EMPTY + slot)), full_bar = uniform(bars_a + 8u * (C::SFULL + x));
+                const bool last_use = !pc.wide || x == 1;
+                if (one_thread()) {
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk)
-                        umma_bf16(tmem_base + x * 128, seq_smem_desc(qa + (kk >> 2) * HB + (kk & 3) * 32, 16, 1024),
-                                  seq_smem_desc(ka + (kk >> 2) * HB + (kk & 3) * 32, 16, 1024), idesc_qk, kk == 0 ? 0u : 1u);
-                    umma_commit(&bars[C::SFULL + x]);
-                    if (!pc.wide || x == 1) umma_commit(&bars[C::EMPTY + cnt % C::RING]);
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint64_t off = (uint64_t)(((kk >> 2) * HB + (kk & 3) * 32) >> 4);
+                        umma_bf16(to, q0 + off, k0 + off, idesc_qk, kk == 0 ? 0u : 1u);
+                    }
+                    commit_to(full_bar);
+                    if (last_use) commit_to(free_bar);
                 }
                 __syncwarp();
             };
@@ -333,10 +371,9 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 ok = __all_sync(0xffffffffu, ok);
                 p_parity[x] ^= 1u;
                 if (!ok) return;
-                const uint32_t cnt = base + 2u * (uint32_t)i + 1u;
-                wait_tile(cnt);
+                const uint32_t cnt = base + 2u * (uint32_t)i + 1u, slot = cnt % C::RING;
+                if (!pc.wide || x == 0) wait_tile(cnt);
                 if (!ok) return;
-                const uint32_t slot = cnt % C::RING;
                 // Rows of the V tile behind the prefix may hold anything: zero them, so that a probability of 0 times garbage
                 // is 0. Done by the first tile that uses it (E4M3: by the warps that convert).
                 const int held = pc.len - (pc.t0 + i) * kPrefixTile;
@@ -350,14 +387,16 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                     __syncwarp();
                 }
                 tc_fence_after_sync();
-                if (lane == 0) {
-                    const uint32_t va = ring_a + slot * C::TILE;
+                const uint64_t v0 = uniform(seq_smem_desc(ring_a + slot * C::TILE, HB, 1024));
+                const uint32_t from = uniform(tmem_base + x * 128), to = from + 256u, more = uniform(i > (pc.wide ? 0 : x) ? 1u : 0u);
+                const uint32_t free_bar = uniform(bars_a + 8u * (C::EMPTY + slot)), done_bar = uniform(bars_a + 8u * (C::ODONE + x));
+                const bool last_use = !pc.wide || x == 1;
+                if (one_thread()) {
 #pragma unroll
                     for (int kk = 0; kk < kPrefixTile / 16; ++kk)
-                        umma_bf16_ts(tmem_base + 256 + x * 128, tmem_base + x * 128 + (kk >> 1) * 32 + (kk & 1) * 8, seq_smem_desc(va + kk * 2048, HB, 1024), idesc_pv,
-                                     (i > (pc.wide ? 0 : x) || kk > 0) ? 1u : 0u);
-                    if (!pc.wide || x == 1) umma_commit(&bars[C::EMPTY + slot]);
-                    if (last) umma_commit(&bars[C::ODONE + x]);
+                        umma_bf16_ts(to, from + (kk >> 1) * 32 + (kk & 1) * 8, v0 + (uint64_t)(kk * 2048 >> 4), idesc_pv, kk > 0 ? 1u : more);
+                    if (last_use) commit_to(free_bar);
+                    if (last) commit_to(done_bar);
                 }
                 __syncwarp();
             };

@@ -12,6 +12,7 @@ namespace plt {
 namespace {
 
 constexpr int kMergeBatch = 4;
+constexpr int kMergeParts = 4;       // warps of a block: 8 elements each of the same 32 rows
 
 // Joins `n` partials of a row into y, top and sum: part(k, ml, acc, step) says where partial k's (reference, sum) and its
 // elements (two pieces of four, `step` floats apart) lie.
@@ -75,9 +76,9 @@ __device__ __forceinline__ Own own_pieces(const Params& p, int item, int hl, int
 }
 
 template <int D>
-__global__ void __launch_bounds__(D * 4) plt_prefix_merge(const __grid_constant__ Params p, const __grid_constant__ PrefixParams pp) {
+__global__ void __launch_bounds__(kMergeParts * 32, 6) plt_prefix_merge(const __grid_constant__ Params p, const __grid_constant__ PrefixParams pp) {
     grid_launch_dependents();
-    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;       // elements 8 part .. 8 part + 7
+    const int lane = threadIdx.x & 31, part = blockIdx.z * kMergeParts + (threadIdx.x >> 5);   // elements 8 part .. 8 part + 7
     const int h = blockIdx.y;
     const int64_t id = (int64_t)blockIdx.x * 32 + lane;
     const bool in = id < (int64_t)p.B * p.R;
@@ -132,18 +133,17 @@ __global__ void __launch_bounds__(D * 4) plt_prefix_merge(const __grid_constant_
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = z[i] = 0.f;
     const int tiles = x1 - x0 + 1, shared = (c1 - c0 + 1) * tiles;
-    join(shared + og.n, [&](int k, const float2*& m, const float*& acc, int& step) {
-        if (k < shared) {
-            const int64_t at = ((unit + c0 + k / tiles) * 2 + x0 + k % tiles) * 128;
-            m = (const float2*)(pp.ml + (at + row) * 2);
-            acc = pp.acc + at * D + part * 2 * 512 + row * 4;
-            step = 512;
-        } else {
-            const int64_t at = og.row0 + (k - shared) * og.step;
-            m = (const float2*)(p.part_ml + at * 2);
-            acc = p.part_acc + at * D + part * 8;
-            step = 4;
-        }
+    join(shared, [&](int k, const float2*& m, const float*& acc, int& step) {
+        const int64_t at = ((unit + c0 + (tiles == 2 ? k >> 1 : k)) * 2 + x0 + (tiles == 2 ? k & 1 : 0)) * 128;
+        m = (const float2*)(pp.ml + (at + row) * 2);
+        acc = pp.acc + at * D + part * 2 * 512 + row * 4;
+        step = 512;
+    }, y, top, sum);
+    join(og.n, [&](int k, const float2*& m, const float*& acc, int& step) {
+        const int64_t at = og.row0 + k * og.step;
+        m = (const float2*)(p.part_ml + at * 2);
+        acc = p.part_acc + at * D + part * 8;
+        step = 4;
     }, y, top, sum);
     // ---- the window -----------------------------------------------------------------------------------------------------
     join(ow.n, [&](int k, const float2*& m, const float*& acc, int& step) {
@@ -164,8 +164,8 @@ __global__ void __launch_bounds__(D * 4) plt_prefix_merge(const __grid_constant_
 
 cudaError_t launch_prefix_merge(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(((int64_t)p.B * p.R + 31) / 32), (unsigned)p.Hkv);
-    cfg.blockDim = dim3((unsigned)p.d * 4);
+    cfg.gridDim = dim3((unsigned)(((int64_t)p.B * p.R + 31) / 32), (unsigned)p.Hkv, (unsigned)(p.d / (8 * kMergeParts)));
+    cfg.blockDim = dim3(kMergeParts * 32);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
