@@ -54,6 +54,8 @@ struct Params {
                                // packed row i is i >> 1 and its half i & 1
     int32_t win_free;          // 1: win_lens holds for loops that see no key of the shared cache too (the keys in front of it
                                // lie in a prefix of their own)
+    int32_t late_wait;         // 1: the kernel before this one has nothing for it and let it go once it might start (the warp-level
+                               // main kernel then waits for that one's end at its own end, so that the kernel behind sees both)
     float scale_log2;          // sm_scale * log2(e)
     int32_t delta[kMaxLoops];  // per-loop causal offset
 };

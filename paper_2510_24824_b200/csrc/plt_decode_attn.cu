@@ -651,6 +651,12 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
                 s = encode_rows(h, &prefix->maps[1], a->v_cache, es, c.d, c.page_size, c.Hkv, a->num_pool_pages, sn, sh, sb, pp.kbox, 1);
             if (s != PLT_OK) return s;
         }
+        if (pp.q_tma && pp.groups > 0) {
+            // query rows: the heads of a KV head of 128 / G neighbouring tokens
+            const int64_t tokens = (int64_t)a->batch * c.L * h->Qn;
+            const plt_status s = encode_rows(h, &prefix->maps[2], a->q, 2, c.d, c.Hq, tokens, 1, c.d, (int64_t)c.Hq * c.d, tokens * c.Hq * c.d, h->G, 128 / h->G);
+            if (s != PLT_OK) return s;
+        }
         e = launch_prefix_plan(pp, stream);
         if (e != cudaSuccess) return cuda_fail(h, "launching the plan kernel", e);
         if (pp.groups > 0) {
@@ -660,6 +666,7 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
         p.seq_lens = pp.plan.own_lens;
         p.win_lens = pp.plan.win_lens;
         p.win_free = 1;
+        p.late_wait = pp.groups > 0 && h->bf16 && !h->umma;
     }
     if (step) {
         Params pre = p;

@@ -377,7 +377,7 @@ plt_decode_main_bf16(const __grid_constant__ CUtensorMap tmK, const __grid_const
     // to overlap the end of the kernel before it in the stream (the pre-step kernel, or the merge kernel of the step
     // before, which still reads the partials): caches, windows and query rows are read, and the workspace is written,
     // only from here on.
-    grid_dependency_wait();
+    if (!p.late_wait) grid_dependency_wait();
     // The merge kernel may be set up from now on (it reads the gate logits, which the pre-step may have written, before
     // its own wait, hence not earlier); it waits for this grid to complete before it reads the partials.
     grid_launch_dependents();
@@ -745,6 +745,7 @@ plt_decode_main_bf16(const __grid_constant__ CUtensorMap tmK, const __grid_const
         }
     }
     __syncthreads();
+    if (p.late_wait) grid_dependency_wait();
 }
 
 }  // namespace plt

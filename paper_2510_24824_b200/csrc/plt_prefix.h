@@ -9,14 +9,18 @@ constexpr int kPrefixRows = 256;      // packed query rows of a unit: two tiles 
 constexpr int kPrefixTile = 128;      // keys of a tile
 constexpr int kPrefixLead = 2;        // line positions that stand for starting and finishing a unit's piece, in tiles
 
-// The plan that the plan kernel leaves for the others. A unit is (group, KV head, 256 packed rows); the units of a group lie
-// one after the other on a line of key tiles, each preceded by kPrefixLead positions, and the line is cut into equal ranges,
-// one for each block. A piece (a block's share of a unit) stores its partial in slot unit + block.
+// The plan of a call. A unit is (group, KV head, 256 packed rows); its key tiles are cut into pieces, one block each.
+//   - Where all units can be cut into as many pieces as there are blocks (one each) without much loss, every unit of a group has
+//     the same number of nearly equal pieces of at most `*chunk` tiles, and piece i is block i's and leaves its partial in slot i.
+//   - Else (*chunk = 0) the units lie one after the other on a line of key tiles, each preceded by kPrefixLead positions, and the
+//     line is cut into equal ranges, one for each block, which may hold several pieces; slot unit + block.
 struct PrefixPlan {
     int32_t *begin;      // [groups + 1] first sequence of each group, clamped
     int32_t *len;        // [groups] tokens of each prefix, clamped; 0 where the group is empty
     int32_t *line;       // [groups + 1] first line position of each group's units
     int32_t *unit;       // [groups + 1] first unit of each group
+    int32_t *piece;      // [groups + 1] first piece of each group's units (*chunk > 0)
+    int32_t *chunk;      // one word
     int32_t *own_lens;   // [max_batch] tokens that each sequence holds itself
     int32_t *win_lens;   // [max_batch, L - 1] valid window slots of each loop
 };
@@ -36,6 +40,7 @@ struct PrefixParams {
     int32_t groups, B, L, Qn, Hq, Hkv, G, R, d, w;
     int32_t max_seq_len, max_prefix_len, page_size, max_pages, num_pool_pages, kbox;
     int32_t blocks;                // of the prefix kernel
+    int32_t q_tma;                 // 1: query rows by TMA (the heads of a KV head divide 128)
     float scale_log2;
     int32_t delta[kMaxLoops];
 };
@@ -43,14 +48,14 @@ struct PrefixParams {
 // What a run needs of the prefixes: filled by the public entry point, completed by the decode step's run.
 struct PrefixRun {
     PrefixParams pp;
-    CUtensorMap maps[2];           // K, V of the prefixes
+    CUtensorMap maps[3];           // K, V of the prefixes, q
     bool fp8;
 };
 
 size_t prefix_smem(int d, bool fp8);
 cudaError_t prefix_prepare(int d, bool fp8);
 cudaError_t launch_prefix_plan(const PrefixParams& pp, cudaStream_t stream);
-cudaError_t launch_prefix_main(const CUtensorMap maps[2], const PrefixParams& pp, bool fp8, cudaStream_t stream);
+cudaError_t launch_prefix_main(const CUtensorMap maps[3], const PrefixParams& pp, bool fp8, cudaStream_t stream);
 cudaError_t launch_prefix_merge(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream);
 
 // plt_decode_attn_run with shared prefixes in front of the caches: `args` as the caller gave them.
@@ -59,13 +64,14 @@ plt_status decode_run_prefix(plt_decode_attn_t h, const plt_decode_attn_args* ar
 plt_status decode_encode_rows(plt_decode_attn_t h, CUtensorMap* map, const void* base, int es, int d, int64_t keys, int64_t heads,
                               int64_t outer, int64_t sn, int64_t sh, int64_t so, int box_keys);
 
-// Block of the prefix kernel that owns line position `pos` (T positions in all, C blocks).
-__host__ __device__ inline int prefix_block_of(int64_t pos, int64_t T, int C) { return (int)(((pos + 1) * C - 1) / T); }
-// Blocks that take part: at least kPrefixMinLine positions each.
+// Blocks that take part in a line of T positions: at least kPrefixMinLine positions each.
 constexpr int kPrefixMinLine = 3;
-__host__ __device__ inline int prefix_blocks(int64_t T, int launched) {
-    const int64_t c = T / kPrefixMinLine;
-    return c < 1 ? 1 : c < launched ? (int)c : launched;
+__host__ __device__ inline int prefix_blocks(int T, int launched) {
+    const int c = T / kPrefixMinLine;
+    return c < 1 ? 1 : c < launched ? c : launched;
 }
+// First position of block c's range (T c / C, without its product) and the block that owns position `pos`.
+__host__ __device__ inline int prefix_range(int T, int c, int C) { return T / C * c + T % C * c / C; }
+__host__ __device__ inline int prefix_block_of(int pos, int T, int C) { return (int)((((int64_t)pos + 1) * C - 1) / T); }
 
 }  // namespace plt

@@ -61,7 +61,7 @@ int64_t units_of(const plt_prefix_attn_config* c, int R) {
 int rows_of(const plt_prefix_attn_config* c) { return c->L * (c->q_len > 1 ? c->q_len : 1) * (c->Hq / c->Hkv); }
 
 size_t plan_bytes(const plt_prefix_attn_config* c) {
-    return 256 + 4 * ((size_t)4 * (c->max_groups + 1) + (size_t)c->max_batch * c->L);
+    return 256 + 4 * ((size_t)5 * (c->max_groups + 1) + 1 + (size_t)c->max_batch * c->L);
 }
 size_t workspace_of(const plt_prefix_attn_config* c, int blocks) {
     const size_t slots = (size_t)units_of(c, rows_of(c)) + blocks;
@@ -147,6 +147,8 @@ PLT_API plt_status plt_prefix_attn_create(const plt_prefix_attn_config* config, 
     h->plan.len = at; at += groups;
     h->plan.line = at; at += groups;
     h->plan.unit = at; at += groups;
+    h->plan.piece = at; at += groups;
+    h->plan.chunk = at; at += 1;
     h->plan.own_lens = at; at += config->max_batch;
     h->plan.win_lens = at;
     h->acc = (float*)(ws + ((plan_bytes(config) + 255) & ~(size_t)255));
@@ -210,6 +212,7 @@ PLT_API plt_status plt_prefix_attn_run(plt_prefix_attn_t h, const plt_decode_att
     p.group_begin = x->group_begin; p.prefix_lens = x->prefix_lens; p.page_table = x->page_table;
     p.plan = h->plan; p.acc = h->acc; p.ml = h->ml; p.status = h->status;
     p.groups = x->num_groups; p.max_prefix_len = c.max_prefix_len; p.max_pages = x->max_pages; p.blocks = h->blocks;
+    p.q_tma = 128 % h->G == 0;
     // keys of a TMA box: all of a tile, or as many as both tile and page are made of
     p.kbox = kPrefixTile;
     while (c.page_size > 0 && c.page_size % p.kbox != 0) p.kbox >>= 1;

@@ -28,7 +28,7 @@
 namespace plt {
 namespace {
 
-constexpr int kNearGroups = 32;      // plans of up to this many groups are kept in shared memory
+constexpr int kNearGroups = 31;      // plans of up to this many groups are made by a warp, in every block by itself
 
 template <int D, bool FP8>
 struct PCfg {
@@ -37,10 +37,10 @@ struct PCfg {
     static constexpr int RAW = FP8 ? 4 : 0;                       // tiles of codes
     static constexpr int RAW_TILE = kPrefixTile * D;
     // mbarriers
-    static constexpr int QFULL = 0, FULL = 2, EMPTY = FULL + RING, RFULL = EMPTY + RING, REMPTY = RFULL + RAW, SFULL = REMPTY + RAW,
+    static constexpr int QFULL = 0, QRAW = 2, FULL = 4, EMPTY = FULL + RING, RFULL = EMPTY + RING, REMPTY = RFULL + RAW, SFULL = REMPTY + RAW,
                          PFULL = SFULL + 2, ODONE = PFULL + 2, COUNT = ODONE + 2;
     // tiles, barriers, control words, a word for each row (what the threads of a row tell each other), the plan
-    static constexpr size_t SMEM = 1024 + 2 * TILE + (size_t)RING * TILE + (size_t)RAW * RAW_TILE + COUNT * 8 + 64 + 1024 + 4 * (kNearGroups + 1) * 4;
+    static constexpr size_t SMEM = 1024 + 2 * TILE + (size_t)RING * TILE + (size_t)RAW * RAW_TILE + COUNT * 8 + 64 + 1024 + (5 * (kNearGroups + 1) + 4) * 4;
 };
 
 constexpr int kPThreads = 640;
@@ -52,56 +52,140 @@ __host__ __device__ constexpr uint32_t p_instr_desc(int N, int b_mn_major, bool 
 
 // ---- the walk over a block's range ------------------------------------------------------------------------------
 struct PPiece {
-    int g, unit, h, m;    // group, unit, KV head, 256-row block of the group
+    int g, slot, h, m;    // group, slot of the partial, KV head, 256-row block of the group
     int t0, t1;           // key tiles
     int len, rows;        // tokens of the prefix, packed rows of the group
     bool wide;            // both tiles have rows of their own
 };
-struct PlanView {
-    const int32_t *begin, *len, *line, *unit;
-};
 struct PWalk {
-    int pos, hi, g;
-    __device__ __forceinline__ bool next(const PrefixParams& p, const PlanView& plan, PPiece& pc) {
+    int pos, hi, g;       // of the line; with chunks: piece pos = hi - 1, or none
+    __device__ __forceinline__ void fill(const PrefixParams& p, const PrefixPlan& plan, int u, int nm, PPiece& pc) {
+        pc.h = u / nm;
+        pc.m = u - pc.h * nm;
+        pc.wide = pc.rows - pc.m * kPrefixRows > 128;
+    }
+    __device__ __forceinline__ bool next(const PrefixParams& p, const PrefixPlan& plan, PPiece& pc) {
         for (;;) {
             if (pos >= hi) return false;
-            while (plan.line[g + 1] <= pos) ++g;
+            const int chunk = *plan.chunk;
+            if (chunk == 0)
+                while (plan.line[g + 1] <= pos) ++g;
             pc.g = g;
             pc.len = plan.len[g];
             pc.rows = (plan.begin[g + 1] - plan.begin[g]) * p.R;
-            const int per = (pc.len + kPrefixTile - 1) / kPrefixTile + kPrefixLead, nm = (pc.rows + kPrefixRows - 1) / kPrefixRows;
-            const int o = pos - plan.line[g], u = o / per, v0 = o - u * per;
+            const int tiles = (pc.len + kPrefixTile - 1) / kPrefixTile, nm = (pc.rows + kPrefixRows - 1) / kPrefixRows;
+            if (chunk > 0) {
+                const int n = (tiles + chunk - 1) / chunk, o = pos - plan.piece[g], u = o / n, k = o - u * n;
+                pc.slot = pos;
+                pc.t0 = tiles * k / n;
+                pc.t1 = tiles * (k + 1) / n;
+                pos = hi;
+                fill(p, plan, u, nm, pc);
+                return true;
+            }
+            const int per = tiles + kPrefixLead, o = pos - plan.line[g], u = o / per, v0 = o - u * per;
             const int end = min(pos + per - v0, hi), v1 = v0 + end - pos;
             pos = end;
             pc.t0 = max(v0 - kPrefixLead, 0);
             pc.t1 = max(v1 - kPrefixLead, 0);
             if (pc.t1 <= pc.t0) continue;
-            pc.unit = plan.unit[g] + u;
-            pc.h = u / nm;
-            pc.m = u - pc.h * nm;
-            pc.wide = pc.rows - pc.m * kPrefixRows > 128;
+            pc.slot = plan.unit[g] + u + (int)blockIdx.x;
+            fill(p, plan, u, nm, pc);
             return true;
         }
     }
 };
-__device__ __forceinline__ PWalk walk_of_block(const PrefixParams& p, const PlanView& plan) {
+__device__ __forceinline__ PWalk walk_of_block(const PrefixParams& p, const PrefixPlan& plan) {
     PWalk w;
-    const int64_t T = plan.line[p.groups];
-    const int C = prefix_blocks(T, p.blocks), c = blockIdx.x;
-    w.pos = w.hi = 0;
-    w.g = 0;
-    if (c < C && T > 0) {
-        w.pos = (int)(T * c / C);
-        w.hi = (int)(T * (c + 1) / C);
-        int lo = 0, hi = p.groups;          // line[lo] <= pos < line[hi]
+    const int c = blockIdx.x;
+    const int32_t* first = plan.line;       // of each group, on the scale that pos counts
+    w.pos = w.hi = w.g = 0;
+    if (*plan.chunk > 0) {
+        first = plan.piece;
+        if (c < first[p.groups]) {
+            w.pos = c;
+            w.hi = c + 1;
+        }
+    } else {
+        const int T = first[p.groups], C = prefix_blocks(T, p.blocks);
+        if (c < C && T > 0) {
+            w.pos = prefix_range(T, c, C);
+            w.hi = prefix_range(T, c + 1, C);
+        }
+    }
+    if (w.pos < w.hi) {
+        int lo = 0, hi = p.groups;          // first[lo] <= pos < first[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (plan.line[mid] <= w.pos) lo = mid; else hi = mid;
+            if (first[mid] <= w.pos) lo = mid; else hi = mid;
         }
         w.g = lo;
     }
     return w;
 }
+
+// ---- making the plan ----------------------------------------------------------------------------------------------
+__device__ __forceinline__ int warp_scan(int x, int lane) {     // inclusive
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
+
+// The plan of up to kNearGroups groups, by one warp: lane g is group g. Everything but the sequences' lengths goes to `to`.
+__device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const PrefixPlan& to, int lane, uint32_t& flags) {
+    const int given = lane <= p.groups && p.groups > 0 ? p.group_begin[lane] : 0;
+    int len = lane < p.groups ? p.prefix_lens[lane] : 0;
+    if (len < 0 || len > p.max_prefix_len) {
+        flags |= kDevGroupClamped;
+        len = len < 0 ? 0 : p.max_prefix_len;
+    }
+    // first sequences: the largest given so far, within [0, B]
+    int begin = min(max(given, 0), p.B);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, begin, o);
+        if (lane >= o) begin = max(begin, y);
+    }
+    if (lane <= p.groups && begin != given) flags |= kDevGroupClamped;
+    const int next = __shfl_down_sync(0xffffffffu, begin, 1);
+    const int rows = lane < p.groups ? (next - begin) * p.R : 0;
+    if (rows == 0) len = 0;
+    const int tiles = (len + kPrefixTile - 1) / kPrefixTile;
+    const int units = tiles > 0 ? p.Hkv * ((rows + kPrefixRows - 1) / kPrefixRows) : 0;
+    const int positions = units * (tiles + kPrefixLead);
+    const int unit = warp_scan(units, lane), line = warp_scan(positions, lane);
+    const int all_units = __shfl_sync(0xffffffffu, unit, 31), all = __shfl_sync(0xffffffffu, line, 31) - all_units * kPrefixLead;
+    // The shortest chunk that lets every piece have a block, tried in steps of an eighth from the average on; not more than a
+    // tenth and a tile above what the line's ranges hold.
+    int chunk = 0, piece = 0;
+    if (all_units > 0 && all_units <= p.blocks) {
+        const int least = (all + p.blocks - 1) / p.blocks, step = (least + 7) / 8;
+        const int most = (all + all_units * kPrefixLead) / p.blocks * 11 / 10 + 1;
+        for (int s = least; s <= max(most, least); s += step) {
+            const int n = warp_scan(tiles > 0 ? units * ((tiles + s - 1) / s) : 0, lane);
+            if (__shfl_sync(0xffffffffu, n, 31) <= p.blocks) {
+                chunk = s;
+                piece = n;
+                break;
+            }
+        }
+    }
+    if (lane < p.groups) {
+        to.len[lane] = len;
+        to.line[lane + 1] = line;
+        to.unit[lane + 1] = unit;
+        to.piece[lane + 1] = piece;
+    }
+    if (lane <= p.groups) to.begin[lane] = begin;
+    if (lane == 0) {
+        to.line[0] = to.unit[0] = to.piece[0] = 0;
+        *to.chunk = chunk;
+    }
+}
+
 // Key tiles of a piece that tile x takes: every one, or every second.
 __device__ __forceinline__ int tiles_of(const PPiece& pc, int x) {
     const int n = pc.t1 - pc.t0;
@@ -210,7 +294,8 @@ __device__ __forceinline__ void p_scale_o(uint32_t tO, float f) {
 
 template <int D, bool FP8>
 __global__ void __launch_bounds__(kPThreads, 1)
-plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PrefixParams p) {
+plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmQ,
+                const __grid_constant__ PrefixParams p) {
     using C = PCfg<D, FP8>;
     constexpr int HALVES = D / 64;
     extern __shared__ uint8_t prefix_smem_raw[];
@@ -221,13 +306,13 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     uint64_t* bars = (uint64_t*)(raw + (size_t)C::RAW * C::RAW_TILE);
     int32_t* s_ctl = (int32_t*)(bars + C::COUNT);                  // [0] abort flag, [1] tensor-memory base, [2] loads issued
     float* s_row = (float*)(s_ctl + 16);                           // [2 tiles][128 rows]
-    int32_t* s_plan = (int32_t*)(s_row + 256);                     // begin, len, line, unit: [kNearGroups + 1] each
+    int32_t* s_plan = (int32_t*)(s_row + 256);                     // begin, len, line, unit, piece: [kNearGroups + 1] each; chunk
     volatile int* abort_flag = (volatile int*)s_ctl;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
 
     if (tid == 0) {
         s_ctl[0] = 0;
-        s_ctl[2] = 0;
+        s_ctl[2] = s_ctl[3] = s_ctl[4] = 0;
         for (int s = 0; s < C::RING; ++s) {
             mbar_init(&bars[C::FULL + s], FP8 ? 2 : 1);
             mbar_init(&bars[C::EMPTY + s], 1);
@@ -237,7 +322,8 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             mbar_init(&bars[C::REMPTY + s], 2);
         }
         for (int x = 0; x < 2; ++x) {
-            mbar_init(&bars[C::QFULL + x], 8);
+            mbar_init(&bars[C::QFULL + x], p.q_tma && !FP8 ? 1 : 8);
+            mbar_init(&bars[C::QRAW + x], 1);
             mbar_init(&bars[C::SFULL + x], 1);
             mbar_init(&bars[C::PFULL + x], 8);
             mbar_init(&bars[C::ODONE + x], 1);
@@ -245,26 +331,34 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         mbar_fence_init();
     }
     if (wid == 1) tmem_alloc((uint32_t*)&s_ctl[1], 512);
+    // What the kernels before the plan kernel wrote is there (the plan kernel is an ordinary launch, and this one starts behind
+    // its start); of the plan kernel itself only the plan of many groups is needed.
+    const bool near = p.groups <= kNearGroups;
+    PrefixPlan plan = p.plan;
+    if (near) {
+        constexpr int W = kNearGroups + 1;
+        plan.begin = s_plan;
+        plan.len = s_plan + W;
+        plan.line = s_plan + 2 * W;
+        plan.unit = s_plan + 3 * W;
+        plan.piece = s_plan + 4 * W;
+        plan.chunk = s_plan + 5 * W;
+        uint32_t reported = 0;                // by the plan kernel
+        if (wid == 2) plan_by_warp(p, plan, lane, reported);
+    } else {
+        grid_dependency_wait();
+    }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = (uint32_t)s_ctl[1];
     // columns: S_A 0..127 (P_A over the first 16 of every 32, whose scores have been read by then), S_B 128..255, O_A from
     // 256, O_B from 384
-    // The plan (and whatever the caller's kernels before it wrote) is complete from here on; the kernel behind this one reads
-    // the plan's lengths before its own wait, hence is not let go earlier.
-    grid_dependency_wait();
-    grid_launch_dependents();
-    PlanView plan = {p.plan.begin, p.plan.len, p.plan.line, p.plan.unit};
-    if (p.groups <= kNearGroups) {
-        constexpr int W = kNearGroups + 1;
-        if (tid < 4 * W) {
-            const int which = tid / W, g = tid - which * W;
-            const int32_t* from = which == 0 ? plan.begin : which == 1 ? plan.len : which == 2 ? plan.line : plan.unit;
-            if (g < p.groups + (which != 1)) s_plan[tid] = from[g];
-        }
-        plan = {s_plan, s_plan + W, s_plan + 2 * W, s_plan + 3 * W};
-        __syncthreads();
+    if (wid == 3) {
+        // The kernel behind this one reads the plan's lengths, and writes what the step before read, without a wait of its own:
+        // it is let go once the plan kernel has ended.
+        grid_dependency_wait();
+        grid_launch_dependents();
     }
     PWalk walk = walk_of_block(p, plan);
     PPiece pc;
@@ -278,14 +372,39 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         uint8_t* const to = FP8 ? raw : ring;
         uint64_t* const full = bars + (FP8 ? C::RFULL : C::FULL);
         uint64_t* const empty = bars + (FP8 ? C::REMPTY : C::EMPTY);
-        const uint64_t keep = l2_evict_first_policy();
+        const uint64_t keep = l2_evict_first_policy(), keep_q = keep;
         const int per_tile = kPrefixTile / p.kbox;
         Ring<NRING> rg;
-        uint32_t issued = 0, flags = 0;
+        uint32_t issued = 0, flags = 0, q_bars = 0;
+        uint32_t o_parity[2] = {0, 0};
+        bool again = false;                                        // not the block's first piece
         if (lane == 0) {
+            if (p.q_tma) tma_prefetch_desc(&tmQ);
             tma_prefetch_desc(&tmK);
             tma_prefetch_desc(&tmV);
         }
+        // The tiles' query rows, behind the last product that reads the ones before. 128 / G tokens of the G heads: rows behind
+        // the group's belong to the next one or to nobody, and nobody reads their results.
+        auto load_q = [&]() {
+            for (int x = 0; x < 2 && ok; ++x) {
+                if (tiles_of(pc, x) == 0) continue;
+                if ((q_bars >> x) & 1u) {
+                    ok = seq_wait(&bars[C::ODONE + x], o_parity[x], abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                    o_parity[x] ^= 1u;
+                }
+                q_bars |= 1u << x;
+                if (ok && lane == 0) {
+                    uint64_t* bar = &bars[(FP8 ? C::QRAW : C::QFULL) + x];
+                    mbar_expect_tx(bar, C::TILE);
+                    ++s_ctl[3 + x];
+                    const int token = plan.begin[pc.g] * p.L * p.Qn + (pc.m * kPrefixRows + (pc.wide ? x * 128 : 0)) / p.G;
+#pragma unroll
+                    for (int hf = 0; hf < HALVES; ++hf) tma_load_4d(q_smem + x * C::TILE + hf * HB, &tmQ, bar, hf * 64, pc.h * p.G, token, 0, keep_q);
+                }
+                __syncwarp();
+            }
+        };
         while (ok && walk.next(p, plan, pc)) {
             // lane j holds the page of the tile's j-th box, read one tile ahead
             auto page_of = [&](int t) {
@@ -299,6 +418,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 return page;
             };
             int next_page = page_of(pc.t0);
+            if (p.q_tma && !again) load_q();
             for (int t = pc.t0; t < pc.t1 && ok; ++t) {
                 const int page = next_page;
                 if (t + 1 < pc.t1) next_page = page_of(t + 1);
@@ -322,7 +442,9 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                     ++issued;
                     rg.advance();
                 }
+                if (p.q_tma && again && ok && t == pc.t0) load_q();     // the first tiles are on their way meanwhile
             }
+            again = true;
         }
         if (lane == 0) s_ctl[2] = (int32_t)issued;
         if (flags) atomicOr(p.status, flags);
@@ -438,7 +560,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                         const uint8_t* a = raw + (size_t)src.slot * C::RAW_TILE;
                         uint8_t* o = ring + (size_t)dst.slot * C::TILE;
                         const int held = pc.len - t * kPrefixTile;       // rows from here on are zeroed
-#pragma unroll 2
+#pragma unroll 4
                         for (int k = 0; k < 16; ++k) {
                             const int row = k * 8 + (t64 >> 3), c = t64 & 7;
                             uint4 v = *(const uint4*)(a + row * 128 + ((c ^ (row & 7)) << 4));
@@ -475,7 +597,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
         const uint32_t tS = tmem_base + lane_off + x * 128 + half * 64, tO = tmem_base + lane_off + 256 + x * 128 + half * PART;
         float* const told = s_row + x * 128 + row;
-        uint32_t s_parity = 0, o_parity = 0;
+        uint32_t s_parity = 0, o_parity = 0, r_parity = 0;
         while (ok && walk.next(p, plan, pc)) {
             // ---- this row's query, and how many tokens of the prefix it sees ------------------------------------
             const int lr = pc.m * kPrefixRows + (pc.wide ? x * 128 : 0) + row;
@@ -485,29 +607,39 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 uint8_t* q = q_smem + x * C::TILE;
                 const bool in = lr < pc.rows;
                 const int b = in ? plan.begin[pc.g] + lr / p.R : 0, r = in ? lr % p.R : 0, lq = r / p.G;
-                const uint4* src = (const uint4*)((const __nv_bfloat16*)p.q + (((int64_t)b * p.L * p.Qn + lq) * p.Hq + pc.h * p.G + (r - lq * p.G)) * D + half * PART);
-                uint4 v[PART / 8];
-#pragma unroll
-                for (int c = 0; c < PART / 8; ++c) v[c] = in ? src[c] : make_uint4(0, 0, 0, 0);
-                if (in) {
-                    const int cut = (int)min((int64_t)p.seq_lens[b], (int64_t)pc.len + p.max_seq_len) - p.delta[lq / p.Qn] - (p.Qn - 1 - lq % p.Qn);
-                    sees = max(0, min(pc.len, cut));
-                }
-#pragma unroll
-                for (int c = 0; c < PART / 8; ++c) {
-                    if (FP8) {
-                        uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) w[i] = pack_f16x2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
-                        v[c] = make_uint4(w[0], w[1], w[2], w[3]);
+                const int n = in ? p.seq_lens[b] : 0;
+                if (FP8 || !p.q_tma) {
+                    uint4 v[PART / 8];
+                    if (p.q_tma) {       // bf16 rows that TMA wrote become f16 in place
+                        ok = seq_wait(&bars[C::QRAW + x], r_parity, abort_flag);
+                        ok = __all_sync(0xffffffffu, ok);
+                        r_parity ^= 1u;
+                        if (!ok) break;
                     }
-                    const int ch = half * (PART / 8) + c;
-                    *(uint4*)(q + (ch >> 3) * HB + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = v[c];
+                    const uint4* src = (const uint4*)((const __nv_bfloat16*)p.q + (((int64_t)b * p.L * p.Qn + lq) * p.Hq + pc.h * p.G + (r - lq * p.G)) * D + half * PART);
+#pragma unroll
+                    for (int c = 0; c < PART / 8; ++c) {
+                        const int ch = half * (PART / 8) + c;
+                        if (p.q_tma) v[c] = *(const uint4*)(q + (ch >> 3) * HB + row * 128 + (((ch & 7) ^ (row & 7)) << 4));
+                        else v[c] = in ? src[c] : make_uint4(0, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int c = 0; c < PART / 8; ++c) {
+                        if (FP8) {
+                            uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) w[i] = pack_f16x2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+                            v[c] = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                        const int ch = half * (PART / 8) + c;
+                        *(uint4*)(q + (ch >> 3) * HB + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = v[c];
+                    }
+                    fence_proxy_async_smem();
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars[C::QFULL + x]);
                 }
-                fence_proxy_async_smem();
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars[C::QFULL + x]);
+                if (in) sees = max(0, min(pc.len, (int)min((int64_t)n, (int64_t)pc.len + p.max_seq_len) - p.delta[lq / p.Qn] - (p.Qn - 1 - lq % p.Qn)));
             }
             const float scale = FP8 ? p.scale_log2 * p.k_scale[pc.h] : p.scale_log2;
             float mref = kSeqNoMax, sum = 0.f;
@@ -557,7 +689,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             }
             if (!ok) break;
             // ---- the partial ---------------------------------------------------------------------------------------
-            const int64_t slot = (int64_t)pc.unit + blockIdx.x;
+            const int64_t slot = pc.slot;
             if (half == 1) *told = sum;
             named_barrier_sync(pair, 64);
             if (half == 0) {
@@ -597,6 +729,9 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             const uint32_t cnt = issued - 1 - k;
             mbar_wait_bounded(&bars[(FP8 ? C::RFULL : C::FULL) + cnt % NRING], (cnt / NRING) & 1u, kSeqWaitNs);
         }
+        if (p.q_tma)        // the last query tiles: s_ctl[3 + x] counts the ones asked for
+            for (int x = 0; x < 2; ++x)
+                if (s_ctl[3 + x] > 0) mbar_wait_bounded(&bars[(FP8 ? C::QRAW : C::QFULL) + x], (uint32_t)(s_ctl[3 + x] - 1) & 1u, kSeqWaitNs);
     }
     __syncthreads();
     if (wid == 1) {
@@ -610,69 +745,75 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
 constexpr int kPlanThreads = 512;
 
 __global__ void __launch_bounds__(kPlanThreads) plt_prefix_plan(const __grid_constant__ PrefixParams p) {
-    __shared__ int32_t s_begin[kMaxGroups + 1], s_len[kMaxGroups], s_line[kMaxGroups + 1], s_unit[kMaxGroups + 1];
+    __shared__ int32_t s_begin[kMaxGroups + 1], s_len[kMaxGroups], s_line[kMaxGroups + 1], s_unit[kMaxGroups + 1], s_piece[kMaxGroups + 1], s_chunk;
     grid_launch_dependents();
     const int tid = threadIdx.x, lane = tid & 31;
     uint32_t flags = 0;
-    for (int g = tid; g <= p.groups; g += kPlanThreads) s_begin[g] = p.groups > 0 ? p.group_begin[g] : 0;
-    for (int g = tid; g < p.groups; g += kPlanThreads) {
-        int n = p.prefix_lens[g];
-        if (n < 0 || n > p.max_prefix_len) {
-            flags |= kDevGroupClamped;
-            n = n < 0 ? 0 : p.max_prefix_len;
+    if (p.groups <= kNearGroups) {
+        PrefixPlan to = p.plan;
+        to.begin = s_begin;
+        to.len = s_len;
+        to.line = s_line;
+        to.unit = s_unit;
+        to.piece = s_piece;
+        to.chunk = &s_chunk;
+        if (tid < 32) plan_by_warp(p, to, lane, flags);
+    } else {
+        for (int g = tid; g <= p.groups; g += kPlanThreads) s_begin[g] = p.group_begin[g];
+        for (int g = tid; g < p.groups; g += kPlanThreads) {
+            int n = p.prefix_lens[g];
+            if (n < 0 || n > p.max_prefix_len) {
+                flags |= kDevGroupClamped;
+                n = n < 0 ? 0 : p.max_prefix_len;
+            }
+            s_len[g] = n;
         }
-        s_len[g] = n;
-    }
-    __syncthreads();
-    if (tid < 32) {
-        // first sequences: running maximum of what the caller gave, within [0, B]; then the line and the units
-        int last = 0, line = 0, unit = 0;
-        for (int g0 = 0; g0 <= p.groups; g0 += 32) {
-            const int g = g0 + lane;
-            const int given = g <= p.groups ? s_begin[g] : 0;
-            int v = min(max(given, 0), p.B);
+        __syncthreads();
+        if (tid < 32) {
+            // first sequences: running maximum of what the caller gave, within [0, B]; then the line and the units
+            int last = 0, line = 0, unit = 0;
+            for (int g0 = 0; g0 <= p.groups; g0 += 32) {
+                const int g = g0 + lane;
+                const int given = g <= p.groups ? s_begin[g] : 0;
+                int v = min(max(given, 0), p.B);
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, v, o);
-                if (lane >= o) v = max(v, y);
-            }
-            v = max(v, last);
-            last = __shfl_sync(0xffffffffu, v, 31);
-            if (g <= p.groups) {
-                if (v != given) flags |= kDevGroupClamped;
-                s_begin[g] = v;
-            }
-        }
-        __syncwarp();
-        for (int g0 = 0; g0 < p.groups; g0 += 32) {
-            const int g = g0 + lane;
-            int units = 0, positions = 0;
-            if (g < p.groups) {
-                const int rows = (s_begin[g + 1] - s_begin[g]) * p.R;
-                if (rows == 0) s_len[g] = 0;
-                const int tiles = (s_len[g] + kPrefixTile - 1) / kPrefixTile;
-                units = tiles > 0 ? p.Hkv * ((rows + kPrefixRows - 1) / kPrefixRows) : 0;
-                positions = units * (tiles + kPrefixLead);
-            }
-            int u = units, q = positions;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int a = __shfl_up_sync(0xffffffffu, u, o), c = __shfl_up_sync(0xffffffffu, q, o);
-                if (lane >= o) {
-                    u += a;
-                    q += c;
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, v, o);
+                    if (lane >= o) v = max(v, y);
+                }
+                v = max(v, last);
+                last = __shfl_sync(0xffffffffu, v, 31);
+                if (g <= p.groups) {
+                    if (v != given) flags |= kDevGroupClamped;
+                    s_begin[g] = v;
                 }
             }
-            if (g < p.groups) {
-                s_unit[g] = unit + u - units;
-                s_line[g] = line + q - positions;
+            __syncwarp();
+            for (int g0 = 0; g0 < p.groups; g0 += 32) {
+                const int g = g0 + lane;
+                int units = 0, positions = 0;
+                if (g < p.groups) {
+                    const int rows = (s_begin[g + 1] - s_begin[g]) * p.R;
+                    if (rows == 0) s_len[g] = 0;
+                    const int tiles = (s_len[g] + kPrefixTile - 1) / kPrefixTile;
+                    units = tiles > 0 ? p.Hkv * ((rows + kPrefixRows - 1) / kPrefixRows) : 0;
+                    positions = units * (tiles + kPrefixLead);
+                }
+                const int u = warp_scan(units, lane), q = warp_scan(positions, lane);
+                if (g < p.groups) {
+                    s_unit[g] = unit + u - units;
+                    s_line[g] = line + q - positions;
+                    s_piece[g] = 0;
+                }
+                unit += __shfl_sync(0xffffffffu, u, 31);
+                line += __shfl_sync(0xffffffffu, q, 31);
             }
-            unit += __shfl_sync(0xffffffffu, u, 31);
-            line += __shfl_sync(0xffffffffu, q, 31);
-        }
-        if (lane == 0) {
-            s_unit[p.groups] = unit;
-            s_line[p.groups] = line;
+            if (lane == 0) {
+                s_unit[p.groups] = unit;
+                s_line[p.groups] = line;
+                s_piece[p.groups] = 0;
+                s_chunk = 0;
+            }
         }
     }
     __syncthreads();
@@ -680,8 +821,10 @@ __global__ void __launch_bounds__(kPlanThreads) plt_prefix_plan(const __grid_con
         p.plan.begin[g] = s_begin[g];
         p.plan.line[g] = s_line[g];
         p.plan.unit[g] = s_unit[g];
+        p.plan.piece[g] = s_piece[g];
         if (g < p.groups) p.plan.len[g] = s_len[g];
     }
+    if (tid == 0) *p.plan.chunk = s_chunk;
     for (int b = tid; b < p.B; b += kPlanThreads) {
         // the group of sequence b, if any
         int len = 0;
@@ -716,7 +859,7 @@ __global__ void __launch_bounds__(kPlanThreads) plt_prefix_plan(const __grid_con
 }
 
 template <int D, bool FP8>
-cudaError_t launch_one(const CUtensorMap maps[2], const PrefixParams& pp, cudaStream_t stream) {
+cudaError_t launch_one(const CUtensorMap maps[3], const PrefixParams& pp, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)pp.blocks);
     cfg.blockDim = dim3(kPThreads);
@@ -727,7 +870,7 @@ cudaError_t launch_one(const CUtensorMap maps[2], const PrefixParams& pp, cudaSt
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, plt_prefix_main<D, FP8>, maps[0], maps[1], pp);
+    return cudaLaunchKernelEx(&cfg, plt_prefix_main<D, FP8>, maps[0], maps[1], maps[2], pp);
 }
 
 }  // namespace
@@ -744,7 +887,7 @@ cudaError_t launch_prefix_plan(const PrefixParams& pp, cudaStream_t stream) {
     return cudaGetLastError();
 }
 
-cudaError_t launch_prefix_main(const CUtensorMap maps[2], const PrefixParams& pp, bool fp8, cudaStream_t stream) {
+cudaError_t launch_prefix_main(const CUtensorMap maps[3], const PrefixParams& pp, bool fp8, cudaStream_t stream) {
     if (fp8) return launch_one<128, true>(maps, pp, stream);
     return pp.d == 128 ? launch_one<128, false>(maps, pp, stream) : launch_one<64, false>(maps, pp, stream);
 }

@@ -104,22 +104,26 @@ __global__ void __launch_bounds__(kMergeParts * 32, 6) plt_prefix_merge(const __
     float gate = 0.f;
     if (l > 0) gate = 1.f / (1.f + expf(-p.gate_logits[(((int64_t)b * (p.L - 1) + (l - 1)) * p.Qn + (lq - l * p.Qn)) * p.Hq + head]));
 
-    // the prefix's pieces for this row: blocks c0 .. c1, tile x0 (and x1)
-    int64_t unit = 0;
-    int c0 = 0, c1 = -1, x0 = 0, x1 = 0, row = 0;
+    // the prefix's partials for this row: slots s0 .. s0 + ns - 1, tile x0 (or both)
+    int64_t s0 = 0;
+    int ns = 0, x0 = 0, row = 0;
+    bool both = false;
     if (in && sees > 0) {
         const int rows = (plan.begin[group + 1] - plan.begin[group]) * p.R, nm = (rows + kPrefixRows - 1) / kPrefixRows;
-        const int tiles = (len + kPrefixTile - 1) / kPrefixTile, per = tiles + kPrefixLead;
-        const int lr = (b - plan.begin[group]) * p.R + r, m = lr / kPrefixRows;
-        const int64_t T = plan.line[pp.groups], first = plan.line[group] + (int64_t)(h * nm + m) * per + kPrefixLead;
-        const int C = prefix_blocks(T, pp.blocks);
-        c0 = prefix_block_of(first, T, C);
-        c1 = prefix_block_of(first + tiles - 1, T, C);
-        unit = plan.unit[group] + h * nm + m;
+        const int tiles = (len + kPrefixTile - 1) / kPrefixTile, chunk = *plan.chunk;
+        const int lr = (b - plan.begin[group]) * p.R + r, m = lr / kPrefixRows, u = h * nm + m;
+        if (chunk > 0) {
+            ns = (tiles + chunk - 1) / chunk;
+            s0 = plan.piece[group] + (int64_t)u * ns;
+        } else {
+            const int T = plan.line[pp.groups], first = plan.line[group] + u * (tiles + kPrefixLead) + kPrefixLead;
+            const int C = prefix_blocks(T, pp.blocks), c0 = prefix_block_of(first, T, C);
+            ns = prefix_block_of(first + tiles - 1, T, C) - c0 + 1;
+            s0 = (int64_t)plan.unit[group] + u + c0;
+        }
         row = lr & 127;
-        const bool wide = rows - m * kPrefixRows > 128;
-        x0 = wide ? (lr >> 7) & 1 : 0;
-        x1 = wide ? x0 : 1;
+        both = rows - m * kPrefixRows <= 128;
+        x0 = both ? 0 : (lr >> 7) & 1;
     }
     const int hg = h / p.hpc, hl = h - hg * p.hpc;
 
@@ -132,9 +136,8 @@ __global__ void __launch_bounds__(kMergeParts * 32, 6) plt_prefix_merge(const __
     float y[8], z[8], top = -INFINITY, sum = 0.f, top_w = -INFINITY, sum_w = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = z[i] = 0.f;
-    const int tiles = x1 - x0 + 1, shared = (c1 - c0 + 1) * tiles;
-    join(shared, [&](int k, const float2*& m, const float*& acc, int& step) {
-        const int64_t at = ((unit + c0 + (tiles == 2 ? k >> 1 : k)) * 2 + x0 + (tiles == 2 ? k & 1 : 0)) * 128;
+    join(both ? 2 * ns : ns, [&](int k, const float2*& m, const float*& acc, int& step) {
+        const int64_t at = (both ? s0 * 2 + k : (s0 + k) * 2 + x0) * 128;
         m = (const float2*)(pp.ml + (at + row) * 2);
         acc = pp.acc + at * D + part * 2 * 512 + row * 4;
         step = 512;
