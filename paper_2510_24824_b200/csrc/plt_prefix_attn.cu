@@ -100,7 +100,7 @@ PLT_API plt_status plt_prefix_attn_create(const plt_prefix_attn_config* config, 
     if (s != PLT_OK) return from_decode(nullptr, s);
     const int R = rows_of(config);
     if ((double)units_of(config, R) * ((double)config->max_prefix_len / kPrefixTile + 1 + kPrefixLead) >= 2147483647.0 ||
-        (double)config->max_batch * R >= 2147483647.0)
+        (double)config->max_batch * R * config->Hkv >= 1073741824.0)
         return prefix_fail(nullptr, PLT_ERR_UNSUPPORTED, "max_batch * max_prefix_len too large for the tile plan");
     DeviceScope scope(config->device);
     if (scope.err != cudaSuccess) {

@@ -1,8 +1,11 @@
 // Merge of a decode step with shared prefixes: for every row the partials of its group's prefix and of its own cache are joined
-// by their references into one softmax, the window's likewise, and the gate mixes the two (Eq. 2). A thread holds 8 of a row's
-// elements and a warp 32 neighbouring rows, so that the prefix's partials, which lie [d / 4][128 rows][4], are read 512 bytes at
-// a time; the loads of four partials are in flight together. Everything up to the store is fp32. Bound by reading the partials
-// (from L2) and by latency.
+// by their references into one softmax, the window's likewise, and the gate mixes the two (Eq. 2). A block has 32 neighbouring rows
+// of a KV head; what there is to know of them is found out once, by its first warp (with every thread for itself that took longer
+// than the joining). A thread then holds 8 of a row's elements and a warp all 32 rows, so that the prefix's partials, which lie
+// [d / 4][128 rows][4], are read 512 bytes at a time, those of four partials together. Where there are not many rows, four warps
+// work on each at the same time (two take the prefix's partials in turn, one the own cache's, one the window's) and meet in shared
+// memory. Everything up to the store is fp32, in an order that the plan and the batch alone decide. Bound by latency and by
+// reading the partials (from L2).
 #include <cuda_bf16.h>
 
 #include "plt_prefix.h"
@@ -11,12 +14,12 @@
 namespace plt {
 namespace {
 
-constexpr int kMergeBatch = 4;
-constexpr int kMergeParts = 4;       // warps of a block: 8 elements each of the same 32 rows
+// Warps of a block that hold 8 elements each of the same 32 rows. Split: four times as many threads.
+__host__ __device__ constexpr int merge_parts(bool split) { return split ? 4 : 8; }
 
 // Joins `n` partials of a row into y, top and sum: part(k, ml, acc, step) says where partial k's (reference, sum) and its
 // elements (two pieces of four, `step` floats apart) lie.
-template <typename F>
+template <int kMergeBatch, typename F>
 __device__ __forceinline__ void join(int n, F part, float (&y)[8], float& top, float& sum) {
     for (int k0 = 0; k0 < n; k0 += kMergeBatch) {
         float2 ml[kMergeBatch];
@@ -61,121 +64,202 @@ __device__ __forceinline__ void join(int n, F part, float (&y)[8], float& top, f
     }
 }
 
-// The pieces of one item of the split-KV kernel for one row.
-struct Own {
-    int64_t row0, step;   // row of the first piece's partial, rows between pieces
+// What a block knows of each of its rows.
+struct RowInfo {
+    int64_t part[32];      // prefix: 128-row tile where the row's partials start
+    float gate[32];
+    int32_t n[32];         // prefix partials
+    int32_t step[32];      // 128-row tiles from one to the next, and below that the row in the tile: step * 128 + row
+    int32_t own[32];       // item of the own cache, or -1: no key
+    int32_t window[32];    // item of the window, or -1
+    int32_t at[32];        // the row among an item's
+    int32_t out[32];       // row of the output, or -1: none; bit 30: the row has no token
+};
+
+// The partials of one item of the split-KV kernel for one row: the first one's row, and how many.
+struct Item {
+    int64_t row;
     int n;
 };
-__device__ __forceinline__ Own own_pieces(const Params& p, int item, int hl, int r) {
-    const int2 c = *(const int2*)(p.item_blocks + 2 * item);
-    Own o;
-    o.row0 = (slot_of(item, c.x) * p.hpc + hl) * p.R + r;
-    o.step = (int64_t)p.hpc * p.R;
-    o.n = c.y - c.x + 1;
-    return o;
+__device__ __forceinline__ Item item_of(const Params& p, int item, int at) {
+    const int2 c = item >= 0 ? *(const int2*)(p.item_blocks + 2 * item) : make_int2(0, -1);
+    return {slot_of(max(item, 0), c.x) * p.hpc * p.R + at, c.y - c.x + 1};
 }
 
-template <int D>
-__global__ void __launch_bounds__(kMergeParts * 32, 6) plt_prefix_merge(const __grid_constant__ Params p, const __grid_constant__ PrefixParams pp) {
+template <int D, bool SPLIT>
+__global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) plt_prefix_merge(const __grid_constant__ Params p, const __grid_constant__ PrefixParams pp) {
+    constexpr int PARTS = merge_parts(SPLIT), BATCH = SPLIT ? 2 : 4;
+    __shared__ RowInfo s;
+    __shared__ float s_join[SPLIT ? 3 : 1][10][SPLIT ? PARTS * 32 : 1];       // (reference, sum, 8 elements) of the other warps
     grid_launch_dependents();
-    const int lane = threadIdx.x & 31, part = blockIdx.z * kMergeParts + (threadIdx.x >> 5);   // elements 8 part .. 8 part + 7
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, share = SPLIT ? wid / PARTS : 0;
+    const int part = blockIdx.z * PARTS + wid % PARTS;                        // elements 8 part .. 8 part + 7
     const int h = blockIdx.y;
-    const int64_t id = (int64_t)blockIdx.x * 32 + lane;
-    const bool in = id < (int64_t)p.B * p.R;
-    const int b = in ? (int)(id / p.R) : 0, r = in ? (int)(id - (int64_t)b * p.R) : 0;
-    const int lq = r / p.G, l = lq / p.Qn, newer = p.Qn - 1 - lq % p.Qn, head = h * p.G + (r - lq * p.G);
-
-    // what the caller passed and the plan, complete since before the main kernel let this one go
-    int group = -1, len = 0;
-    const PrefixPlan& plan = pp.plan;
-    if (pp.groups > 0 && b >= plan.begin[0] && b < plan.begin[pp.groups]) {
-        int lo = 0, hi = pp.groups;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (plan.begin[mid] <= b) lo = mid; else hi = mid;
+    if (wid == 0) {
+        // what the caller passed and the plan, complete since before the main kernel let this one go
+        const int id = blockIdx.x * 32 + lane;
+        const bool in = id < p.B * p.R;
+        const int b = in ? id / p.R : 0;
+        const int r = in ? id - b * p.R : 0;
+        const int lq = r / p.G, l = lq / p.Qn, newer = p.Qn - 1 - (lq - l * p.Qn), head = h * p.G + (r - lq * p.G);
+        const PrefixPlan& plan = pp.plan;
+        int group = -1, len = 0, begin = 0, end = 0;
+        if (pp.groups > 0) {
+            begin = plan.begin[0];
+            end = plan.begin[pp.groups];
+            if (b >= begin && b < end) {
+                int lo = 0, hi = pp.groups;
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1, at = plan.begin[mid];
+                    if (at <= b) {
+                        lo = mid;
+                        begin = at;
+                    } else {
+                        hi = mid;
+                        end = at;
+                    }
+                }
+                group = lo;
+                len = plan.len[lo];
+            }
         }
-        group = lo;
-        len = plan.len[lo];
-    }
-    const int n = (int)min((int64_t)pp.seq_lens[b], (int64_t)len + p.max_seq_len);
-    const int cut = max(0, n - p.delta[l] - newer), sees = min(cut, len);
-    const int own_cut = max(0, plan.own_lens[b] - p.delta[l] - newer);
-    const int wl = l > 0 ? plan.win_lens[b * (p.L - 1) + l - 1] : 0;
-    float gate = 0.f;
-    if (l > 0) gate = 1.f / (1.f + expf(-p.gate_logits[(((int64_t)b * (p.L - 1) + (l - 1)) * p.Qn + (lq - l * p.Qn)) * p.Hq + head]));
-
-    // the prefix's partials for this row: slots s0 .. s0 + ns - 1, tile x0 (or both)
-    int64_t s0 = 0;
-    int ns = 0, x0 = 0, row = 0;
-    bool both = false;
-    if (in && sees > 0) {
-        const int rows = (plan.begin[group + 1] - plan.begin[group]) * p.R, nm = (rows + kPrefixRows - 1) / kPrefixRows;
-        const int tiles = (len + kPrefixTile - 1) / kPrefixTile, chunk = *plan.chunk;
-        const int lr = (b - plan.begin[group]) * p.R + r, m = lr / kPrefixRows, u = h * nm + m;
-        if (chunk > 0) {
-            ns = (tiles + chunk - 1) / chunk;
-            s0 = plan.piece[group] + (int64_t)u * ns;
-        } else {
-            const int T = plan.line[pp.groups], first = plan.line[group] + u * (tiles + kPrefixLead) + kPrefixLead;
-            const int C = prefix_blocks(T, pp.blocks), c0 = prefix_block_of(first, T, C);
-            ns = prefix_block_of(first + tiles - 1, T, C) - c0 + 1;
-            s0 = (int64_t)plan.unit[group] + u + c0;
+        const int n = (int)min((int64_t)pp.seq_lens[b], (int64_t)len + p.max_seq_len);
+        const int cut = max(0, n - p.delta[l] - newer), sees = min(cut, len);
+        const int wl = l > 0 ? plan.win_lens[b * (p.L - 1) + l - 1] : 0;
+        const bool has_own = in && plan.own_lens[b] - p.delta[l] - newer > 0, has_window = in && cut > 0 && wl > 0;
+        float gate = 0.f;
+        if (l > 0) gate = 1.f / (1.f + expf(-p.gate_logits[(((int64_t)b * (p.L - 1) + (l - 1)) * p.Qn + (lq - l * p.Qn)) * p.Hq + head]));
+        int64_t tile = 0;
+        int count = 0, step = 1, row = 0;
+        if (in && sees > 0) {
+            const int rows = (end - begin) * p.R, nm = (rows + kPrefixRows - 1) / kPrefixRows;
+            const int tiles = (len + kPrefixTile - 1) / kPrefixTile, chunk = *plan.chunk;
+            const int lr = (b - begin) * p.R + r, m = lr / kPrefixRows, u = h * nm + m;
+            if (chunk > 0) {
+                count = (tiles + chunk - 1) / chunk;
+                tile = plan.piece[group] + (int64_t)u * count;
+            } else {
+                const int T = plan.line[pp.groups], first = plan.line[group] + u * (tiles + kPrefixLead) + kPrefixLead;
+                const int C = prefix_blocks(T, pp.blocks), c0 = prefix_block_of(first, T, C);
+                count = prefix_block_of(first + tiles - 1, T, C) - c0 + 1;
+                tile = (int64_t)plan.unit[group] + u + c0;
+            }
+            // a unit of more than 128 rows has one tile for each half of them, else both tiles are partials of the same rows
+            row = lr & 127;
+            tile *= 2;
+            if (rows - m * kPrefixRows > 128) {
+                tile += (lr >> 7) & 1;
+                step = 2;
+            } else {
+                count *= 2;
+            }
         }
-        row = lr & 127;
-        both = rows - m * kPrefixRows <= 128;
-        x0 = both ? 0 : (lr >> 7) & 1;
+        s.part[lane] = tile;
+        s.n[lane] = count;
+        s.step[lane] = step * 128 + row;
+        s.gate[lane] = gate;
+        s.out[lane] = in ? ((b * p.L * p.Qn + lq) * p.Hq + head) | (cut > 0 ? 0 : 1 << 30) : -1;
+        const int hg = h / p.hpc, item = item_index(p, b, hg, 0);
+        s.own[lane] = has_own ? item : -1;
+        s.window[lane] = has_window ? item + 1 : -1;
+        s.at[lane] = (h - hg * p.hpc) * p.R + r;
     }
-    const int hg = h / p.hpc, hl = h - hg * p.hpc;
-
+    __syncthreads();
     grid_dependency_wait();
-    Own og = {0, 0, 0}, ow = {0, 0, 0};
-    if (in && own_cut > 0) og = own_pieces(p, item_index(p, b, hg, 0), hl, r);
-    if (in && cut > 0 && wl > 0) ow = own_pieces(p, item_index(p, b, hg, 1), hl, r);
 
-    // ---- one softmax over the prefix and the own keys ---------------------------------------------------------------
+    // ---- one softmax over the prefix and the own keys, and the window's ---------------------------------------------------
+    const bool does_own = !SPLIT || share == 2, does_window = !SPLIT || share == 3;
+    const Item own = item_of(p, does_own ? s.own[lane] : -1, s.at[lane]), window = item_of(p, does_window ? s.window[lane] : -1, s.at[lane]);
     float y[8], z[8], top = -INFINITY, sum = 0.f, top_w = -INFINITY, sum_w = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = z[i] = 0.f;
-    join(both ? 2 * ns : ns, [&](int k, const float2*& m, const float*& acc, int& step) {
-        const int64_t at = (both ? s0 * 2 + k : (s0 + k) * 2 + x0) * 128;
-        m = (const float2*)(pp.ml + (at + row) * 2);
-        acc = pp.acc + at * D + part * 2 * 512 + row * 4;
-        step = 512;
-    }, y, top, sum);
-    join(og.n, [&](int k, const float2*& m, const float*& acc, int& step) {
-        const int64_t at = og.row0 + k * og.step;
-        m = (const float2*)(p.part_ml + at * 2);
-        acc = p.part_acc + at * D + part * 8;
-        step = 4;
-    }, y, top, sum);
-    // ---- the window -----------------------------------------------------------------------------------------------------
-    join(ow.n, [&](int k, const float2*& m, const float*& acc, int& step) {
-        const int64_t at = ow.row0 + k * ow.step;
-        m = (const float2*)(p.part_ml + at * 2);
-        acc = p.part_acc + at * D + part * 8;
-        step = 4;
-    }, z, top_w, sum_w);
-    const float ig = sum > 0.f ? (1.f - gate) / sum : 0.f, il = sum_w > 0.f ? gate / sum_w : 0.f;
+    if (!SPLIT || share < 2) {
+        constexpr int EVERY = SPLIT ? 2 : 1;
+        const int step = s.step[lane] >> 7, row = s.step[lane] & 127;
+        const int64_t tile = s.part[lane] + share * step;
+        join<BATCH>((s.n[lane] - share + EVERY - 1) / EVERY, [&](int k, const float2*& m, const float*& acc, int& apart) {
+            const int64_t at = (tile + k * EVERY * step) * 128;
+            m = (const float2*)(pp.ml + (at + row) * 2);
+            acc = pp.acc + at * D + part * 2 * 512 + row * 4;
+            apart = 512;
+        }, y, top, sum);
+    }
+    const int64_t next = (int64_t)p.hpc * p.R;               // rows between the partials of one item
+    auto of_item = [&](const Item& it) {
+        return [=, &p](int k, const float2*& m, const float*& acc, int& apart) {
+            const int64_t at = it.row + k * next;
+            m = (const float2*)(p.part_ml + at * 2);
+            acc = p.part_acc + at * D + part * 8;
+            apart = 4;
+        };
+    };
+    if (does_own) join<BATCH>(own.n, of_item(own), y, top, sum);
+    if (does_window) {
+        join<1>(window.n, of_item(window), z, top_w, sum_w);
+        const float f = sum_w > 0.f ? s.gate[lane] / sum_w : 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = cut > 0 ? fmaf(z[i], il, y[i] * ig) : 0.f;
-    if (!in) return;
-    uint4* dst = (uint4*)((__nv_bfloat16*)p.out + (((int64_t)b * p.L * p.Qn + lq) * p.Hq + head) * D + part * 8);
+        for (int i = 0; i < 8; ++i) z[i] *= f;
+    }
+    if (SPLIT) {
+        const int t = (wid % PARTS) * 32 + lane;
+        if (share > 0) {
+            s_join[share - 1][0][t] = top;
+            s_join[share - 1][1][t] = sum;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s_join[share - 1][2 + i][t] = share == 3 ? z[i] : y[i];
+        }
+        __syncthreads();
+        if (share > 0) return;
+        const float all = fmaxf(top, fmaxf(s_join[0][0][t], s_join[1][0][t]));
+        if (all > -INFINITY) {
+            // 0 for one that saw nothing
+            const float f = exp2f(top - all), f1 = exp2f(s_join[0][0][t] - all), f2 = exp2f(s_join[1][0][t] - all);
+            sum = fmaf(sum, f, fmaf(s_join[0][1][t], f1, s_join[1][1][t] * f2));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = fmaf(y[i], f, fmaf(s_join[0][2 + i][t], f1, s_join[1][2 + i][t] * f2));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = s_join[2][2 + i][t];
+    }
+    const int out = s.out[lane];
+    if (out < 0) return;
+    const float ig = sum > 0.f ? (1.f - s.gate[lane]) / sum : 0.f;
+    const bool token = (out >> 30 & 1) == 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = token ? fmaf(y[i], ig, z[i]) : 0.f;
+    uint4* dst = (uint4*)((__nv_bfloat16*)p.out + (int64_t)(out & ~(1 << 30)) * D + part * 8);
     *dst = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
 }
 
 }  // namespace
 
-cudaError_t launch_prefix_merge(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream) {
+namespace {
+
+template <int D, bool SPLIT>
+cudaError_t launch(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(((int64_t)p.B * p.R + 31) / 32), (unsigned)p.Hkv, (unsigned)(p.d / (8 * kMergeParts)));
-    cfg.blockDim = dim3(kMergeParts * 32);
+    cfg.gridDim = dim3((unsigned)((p.B * p.R + 31) / 32), (unsigned)p.Hkv, (unsigned)(D / (8 * merge_parts(SPLIT))));
+    cfg.blockDim = dim3(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = overlap ? 1 : 0;
-    return p.d == 128 ? cudaLaunchKernelEx(&cfg, plt_prefix_merge<128>, p, pp) : cudaLaunchKernelEx(&cfg, plt_prefix_merge<64>, p, pp);
+    return cudaLaunchKernelEx(&cfg, plt_prefix_merge<D, SPLIT>, p, pp);
+}
+
+template <int D>
+cudaError_t launch_for(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream) {
+    // Four warps to a row as long as all run at once (32 on each multiprocessor).
+    const int64_t warps = (int64_t)(p.B * p.R + 31) / 32 * p.Hkv * (D / 8);
+    return warps * 4 <= 148 * 32 ? launch<D, true>(p, pp, overlap, stream) : launch<D, false>(p, pp, overlap, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_prefix_merge(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream) {
+    return p.d == 128 ? launch_for<128>(p, pp, overlap, stream) : launch_for<64>(p, pp, overlap, stream);
 }
 
 }  // namespace plt
