@@ -13,7 +13,7 @@
 // of a line on which the units' key tiles lie one behind the other, and leaves unnormalised partials for the merge.
 //
 // Warp roles: warp 0 loads K and V tiles by TMA into a ring (pages: their ids one tile ahead); warp 1 issues the products and
-// owns the tensor memory; warps 2 and 3 turn E4M3 codes into f16 (exact) in a second ring, and idle otherwise; warps 4-11 and
+// owns the tensor memory; warps 2, 3, 20 and 21 turn E4M3 codes into f16 (exact) in a second ring; warps 4-11 and
 // 12-19 are the softmax of A and of B, load their query rows and store the partials. Two threads share a row, half the keys of
 // a tile each: they vote, warp by warp, on whether the reference has to move. A partial lies as [d / 4][128 rows][4], so that a
 // warp's store is 512 consecutive bytes.
@@ -43,7 +43,8 @@ struct PCfg {
     static constexpr size_t SMEM = 1024 + 2 * TILE + (size_t)RING * TILE + (size_t)RAW * RAW_TILE + COUNT * 8 + 64 + 1024 + (5 * (kNearGroups + 1) + 4) * 4;
 };
 
-constexpr int kPThreads = 640;
+template <bool FP8>
+constexpr int kPThreads = FP8 ? 704 : 640;
 
 // Instruction descriptor: fp32 accumulate, A and B both bf16 or both f16, B majorness, N / 8, M / 16.
 __host__ __device__ constexpr uint32_t p_instr_desc(int N, int b_mn_major, bool f16) {
@@ -293,7 +294,7 @@ __device__ __forceinline__ void p_scale_o(uint32_t tO, float f) {
 }
 
 template <int D, bool FP8>
-__global__ void __launch_bounds__(kPThreads, 1)
+__global__ void __launch_bounds__(kPThreads<FP8>, 1)
 plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmQ,
                 const __grid_constant__ PrefixParams p) {
     using C = PCfg<D, FP8>;
@@ -314,12 +315,12 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         s_ctl[0] = 0;
         s_ctl[2] = s_ctl[3] = s_ctl[4] = 0;
         for (int s = 0; s < C::RING; ++s) {
-            mbar_init(&bars[C::FULL + s], FP8 ? 2 : 1);
+            mbar_init(&bars[C::FULL + s], FP8 ? 4 : 1);
             mbar_init(&bars[C::EMPTY + s], 1);
         }
         for (int s = 0; s < C::RAW; ++s) {
             mbar_init(&bars[C::RFULL + s], 1);
-            mbar_init(&bars[C::REMPTY + s], 2);
+            mbar_init(&bars[C::REMPTY + s], 4);
         }
         for (int x = 0; x < 2; ++x) {
             mbar_init(&bars[C::QFULL + x], p.q_tma && !FP8 ? 1 : 8);
@@ -542,14 +543,14 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             }
             base += 2u * (uint32_t)n;
         }
-    } else if (wid < 4) {
+    } else if (wid < 4 || wid >= 20) {
         // =========================== E4M3 codes to f16 =======================================================
         if constexpr (FP8) {
             constexpr int HB = kPrefixTile * 128;
             Ring<C::RAW> src;
             Ring<C::RING> dst;
             uint32_t done = 0;
-            const int t64 = tid - 64;
+            const int ct = (wid < 4 ? wid - 2 : wid - 18) * 32 + lane;      // of 128
             while (ok && walk.next(p, plan, pc))
                 for (int t = pc.t0; t < pc.t1 && ok; ++t)
                     for (int which = 0; which < 2 && ok; ++which) {
@@ -560,10 +561,17 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                         const uint8_t* a = raw + (size_t)src.slot * C::RAW_TILE;
                         uint8_t* o = ring + (size_t)dst.slot * C::TILE;
                         const int held = pc.len - t * kPrefixTile;       // rows from here on are zeroed
-#pragma unroll 4
-                        for (int k = 0; k < 16; ++k) {
-                            const int row = k * 8 + (t64 >> 3), c = t64 & 7;
-                            uint4 v = *(const uint4*)(a + row * 128 + ((c ^ (row & 7)) << 4));
+                        uint4 codes[8];
+                        const int c = ct & 7;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int row = k * 16 + (ct >> 3);
+                            codes[k] = *(const uint4*)(a + row * 128 + ((c ^ (row & 7)) << 4));
+                        }
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int row = k * 16 + (ct >> 3);
+                            uint4 v = codes[k];
                             if (row >= held) v = make_uint4(0, 0, 0, 0);
                             const uint4 lo = make_uint4(e4m3x2_to_f16x2(v.x & 0xffffu), e4m3x2_to_f16x2(v.x >> 16), e4m3x2_to_f16x2(v.y & 0xffffu),
                                                         e4m3x2_to_f16x2(v.y >> 16));
@@ -862,7 +870,7 @@ template <int D, bool FP8>
 cudaError_t launch_one(const CUtensorMap maps[3], const PrefixParams& pp, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)pp.blocks);
-    cfg.blockDim = dim3(kPThreads);
+    cfg.blockDim = dim3(kPThreads<FP8>);
     cfg.dynamicSmemBytes = PCfg<D, FP8>::SMEM;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
