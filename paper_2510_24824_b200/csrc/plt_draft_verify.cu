@@ -22,8 +22,9 @@ using namespace plt;
 namespace {
 
 constexpr int kVerifyThreads = 256;
-constexpr int kVecs = 8;                // vectors of 16 bytes that a lane takes of a row's chunk
-constexpr int kAtOnce = 148 * 24;       // warps that run at once
+template <typename T>
+constexpr int kVecs = sizeof(T) == 4 ? 4 : 2;   // vectors of 16 bytes that a lane takes of a row's chunk: 16 elements
+constexpr int kAtOnce = 148 * 40;       // warps that run at once
 constexpr int kMaxDrafts = 64;
 
 thread_local char g_verify_error[512] = "";
@@ -68,11 +69,14 @@ struct Row {
     const T* p;
     const T* q;       // or null
     int without;      // index whose weight is 0, or -1
-    // a - b where that is finite and above 0, else 0. The test is made in fp32, where it is exact: 64-bit units are few.
+    // a - b where that is above 0 (and in fp32's range), else 0. The test is made in fp32, where a difference of two numbers that
+    // differ never rounds to 0: 64-bit units are few.
     __device__ __forceinline__ double weight(float a, float b) const {
-        const bool counts = a > b && a <= 3.402823466e38f && b >= -3.402823466e38f;
+        const float d = a - b;
+        const bool counts = d > 0.f && d <= 3.402823466e38f;
         return (double)(counts ? a : 0.f) - (double)(counts ? b : 0.f);
     }
+    __device__ __forceinline__ double weight(float a) const { return (double)(a > 0.f && a <= 3.402823466e38f ? a : 0.f); }
     __device__ __forceinline__ double at(int i) const {
         if (i == without) return 0.0;
         return weight(widen(p[i]), q != nullptr ? widen(q[i]) : 0.f);
@@ -236,7 +240,7 @@ __device__ __forceinline__ Row<T> row_of(const VerifyParams& p, int b, int2 stan
 
 // Elements of a chunk, and elements that the 16-byte grid puts in front of a row (chunk 0 starts there).
 template <typename T>
-constexpr int kChunk = 32 * kVecs * kVec<T>;
+constexpr int kChunk = 32 * kVecs<T> * kVec<T>;
 template <typename T, bool VEC>
 __device__ __forceinline__ int lead_of(const Row<T>& row) {
     return VEC ? (int)(((uintptr_t)row.p & 15) / sizeof(T)) : 0;
@@ -252,7 +256,7 @@ __global__ void __launch_bounds__(kVerifyThreads) plt_draft_verify_count(const _
 }
 
 template <typename T, bool VEC, bool COUNT>
-__global__ void __launch_bounds__(kVerifyThreads, 3) plt_draft_verify_sums(const __grid_constant__ VerifyParams p) {
+__global__ void __launch_bounds__(kVerifyThreads, 5) plt_draft_verify_sums(const __grid_constant__ VerifyParams p) {
     constexpr int N = kVec<T>;
     grid_launch_dependents();
     const int b = blockIdx.y, lane = threadIdx.x & 31, chunk = blockIdx.x * (kVerifyThreads / 32) + (threadIdx.x >> 5);
@@ -270,33 +274,31 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) plt_draft_verify_sums(const
     double sum = 0.0;
     if constexpr (VEC) {
         // the row of q lies on the 16-byte grid as the row of p does
-        constexpr int U = sizeof(T) == 4 ? kVecs : kVecs / 2;     // vectors in flight: 32 elements of each row
+        auto load = [&](const T* from, int i, float (&x)[N]) {
+            if (i >= 0 && i + N <= p.V) {
+                load_vec16<T>(from + i, x);
+            } else {
 #pragma unroll
-        for (int v0 = 0; v0 < kVecs; v0 += U) {
-            float a[U][N], q[U][N];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = c0 + ((v0 + u) * 32 + lane) * N;
-#pragma unroll
-                for (int k = 0; k < N; ++k) a[u][k] = q[u][k] = 0.f;
-                if (i >= 0 && i + N <= p.V) {
-                    load_vec16<T>(row.p + i, a[u]);
-                    if (row.q != nullptr) load_vec16<T>(row.q + i, q[u]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < N; ++k)
-                        if (i + k >= 0 && i + k < p.V) {
-                            a[u][k] = widen(row.p[i + k]);
-                            if (row.q != nullptr) q[u][k] = widen(row.q[i + k]);
-                        }
-                }
+                for (int k = 0; k < N; ++k) x[k] = i + k >= 0 && i + k < p.V ? widen(from[i + k]) : 0.f;
             }
+        };
+        float a[kVecs<T>][N];
+        auto at = [&](int u) { return c0 + (u * 32 + lane) * N; };
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = c0 + ((v0 + u) * 32 + lane) * N;
+        for (int u = 0; u < kVecs<T>; ++u) load(row.p, at(u), a[u]);
+        if (row.q != nullptr) {
+            float q[kVecs<T>][N];
 #pragma unroll
-                for (int k = 0; k < N; ++k) sum += i + k == row.without ? 0.0 : row.weight(a[u][k], q[u][k]);
-            }
+            for (int u = 0; u < kVecs<T>; ++u) load(row.q, at(u), q[u]);
+#pragma unroll
+            for (int u = 0; u < kVecs<T>; ++u)
+#pragma unroll
+                for (int k = 0; k < N; ++k) sum += row.weight(a[u][k], q[u][k]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kVecs<T>; ++u)
+#pragma unroll
+                for (int k = 0; k < N; ++k) sum += at(u) + k == row.without ? 0.0 : row.weight(a[u][k]);
         }
     } else {
         constexpr int U = 16;
@@ -320,7 +322,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) plt_draft_verify_sums(const
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kVerifyThreads) plt_draft_verify_pick(const __grid_constant__ VerifyParams p) {
     constexpr int N = kVec<T>;
-    static_assert(kChunk<T> == kVerifyThreads * N, "a thread takes one vector of the chunk");
+    static_assert(kChunk<T> <= kVerifyThreads * N, "a thread takes one vector of the chunk");
     __shared__ double s_warp[kVerifyThreads / 32];
     __shared__ double s_base;
     __shared__ int s_pick;
@@ -338,7 +340,7 @@ __global__ void __launch_bounds__(kVerifyThreads) plt_draft_verify_pick(const __
         double w[N], own = 0.0;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            w[k] = first + k >= 0 && first + k < p.V ? row.at(first + k) : 0.0;
+            w[k] = tid < 32 * kVecs<T> && first + k >= 0 && first + k < p.V ? row.at(first + k) : 0.0;
             own += w[k];
         }
         double chunk_total;

@@ -1,12 +1,15 @@
 // Norm and rotation of queries and keys, with their way into the caches: a decode step and the rows of a prompt.
 //
-// d / 16 threads hold a head's row, 16 elements each: two 16-byte pieces whose elements are exactly the pairs that turn
-// together (thread t < rotary_dim / 16 has pairs 8 t .. 8 t + 7 in both layouts), so a row is read once, normed by a shuffle
-// over its threads, turned in registers and written once. The cosines and sines of a token are computed once for all its heads.
+// d / 16 threads hold a head's row, 16 elements each: the 8 pairs (a, b) that turn together, a from one 16-byte piece and b from
+// another (halves) or both from the same two (interleaved), so a row is read once, normed by a shuffle over its threads, turned in
+// registers (two pairs to an instruction) and written once. The cosines and sines of a token are computed once for all its heads.
 //
 // An angle p f is taken in turns: f / 2 pi as a 64-bit fraction, multiplied by the position in integers, so that whole turns
 // fall away exactly however far the position lies; the quarter turn is split off in integers too, and what is left (at most
-// an eighth of a turn either way) goes to sincospif. Bound by reading and writing the rows.
+// an eighth of a turn either way) goes to sincospif.
+//
+// Prompts are bound by reading and writing the rows, with the instructions close behind. A step is bound by latency: its rows are
+// asked for before the lengths, the page and the cosines are known.
 #include "../../include/plt_rope.h"
 
 #include <cuda_bf16.h>
@@ -51,26 +54,83 @@ struct RopeParams {
     const int32_t *seq_lens, *start, *prefix_lens, *page_table;
     const uint64_t* turns;
     uint32_t* status;
-    int32_t B, L, Qn, Hq, Hkv, T, w, max_seq_len, page_size, max_pages, num_pool_pages, rd, interleaved;
+    int32_t B, L, Qn, Hq, Hkv, T, w, max_seq_len, page_size, max_pages, num_pool_pages, rd;
+    uint32_t q_reciprocal, k_reciprocal;   // ceil(2^32 / heads), or 0 for one head
     float factor, eps;
     int32_t delta[kMaxLoops];
 };
 
-// 16 elements of a row as fp32: two pieces of 8.
+// ---- a thread's 16 elements of a row ------------------------------------------------------------------------------------
+// As loaded: two pieces of 8 elements.
 template <typename T>
-__device__ __forceinline__ void load8(const T* src, float* x) {
+struct Raw {
+    uint4 v[sizeof(T)];       // sizeof(T) = 2: one 16-byte vector for each piece; 4: two
+};
+template <typename T>
+__device__ __forceinline__ Raw<T> load_raw(const T* row, int o0, int o1) {
+    Raw<T> x;
     if constexpr (sizeof(T) == 2) {
-        const uint4 v = *(const uint4*)src;
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        x.v[0] = *(const uint4*)(row + o0);
+        x.v[1] = *(const uint4*)(row + o1);
+    } else {
+        x.v[0] = *(const uint4*)(row + o0);
+        x.v[1] = *(const uint4*)(row + o0 + 4);
+        x.v[2] = *(const uint4*)(row + o1);
+        x.v[3] = *(const uint4*)(row + o1 + 4);
+    }
+    return x;
+}
+template <typename T>
+__device__ __forceinline__ Raw<T> no_raw() {
+    Raw<T> x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < (int)sizeof(T); ++i) x.v[i] = make_uint4(0, 0, 0, 0);
+    return x;
+}
+
+// As pairs, in fp32: {a[2 i], a[2 i + 1]} and {b[2 i], b[2 i + 1]}.
+struct Pairs {
+    float2 a[4], b[4];
+};
+template <typename T, bool INTER>
+__device__ __forceinline__ Pairs pairs_of(const Raw<T>& x) {
+    float e[16];
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t w[4] = {x.v[i].x, x.v[i].y, x.v[i].z, x.v[i].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                e[8 * i + 2 * k] = __uint_as_float(w[k] << 16);
+                e[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+            }
         }
     } else {
-        const float4 a = *(const float4*)src, b = *((const float4*)src + 1);
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            e[4 * i] = __uint_as_float(x.v[i].x);
+            e[4 * i + 1] = __uint_as_float(x.v[i].y);
+            e[4 * i + 2] = __uint_as_float(x.v[i].z);
+            e[4 * i + 3] = __uint_as_float(x.v[i].w);
+        }
+    }
+    Pairs y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        y.a[i] = INTER ? make_float2(e[4 * i], e[4 * i + 2]) : make_float2(e[2 * i], e[2 * i + 1]);
+        y.b[i] = INTER ? make_float2(e[4 * i + 1], e[4 * i + 3]) : make_float2(e[8 + 2 * i], e[8 + 2 * i + 1]);
+    }
+    return y;
+}
+// Element k of the row's two pieces, in the order of memory.
+template <bool INTER>
+__device__ __forceinline__ void elements_of(const Pairs& y, float (&e)[16]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        e[INTER ? 4 * i : 2 * i] = y.a[i].x;
+        e[INTER ? 4 * i + 2 : 2 * i + 1] = y.a[i].y;
+        e[INTER ? 4 * i + 1 : 8 + 2 * i] = y.b[i].x;
+        e[INTER ? 4 * i + 3 : 8 + 2 * i + 1] = y.b[i].y;
     }
 }
 __device__ __forceinline__ void store8(__nv_bfloat16* dst, const float* x) {
@@ -91,12 +151,17 @@ __device__ __forceinline__ void store8_codes(uint8_t* dst, const float* x, float
     }
     *(uint2*)dst = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
 }
-
-// What a block knows about each of its tokens.
-struct Token {
-    int64_t cell;     // element where head 0 of its row starts in the cache (or window), or -1: not stored
-    int64_t pos;      // its position, or -1: the row has no token
-};
+// A row into the cache (or window): as it is, or as codes.
+template <bool FP8, typename TD>
+__device__ __forceinline__ void store_cached(TD* row, int o0, int o1, const float (&e)[16], float scale) {
+    if constexpr (FP8) {
+        store8_codes(row + o0, e, scale);
+        store8_codes(row + o1, e + 8, scale);
+    } else {
+        store8(row + o0, e);
+        store8(row + o1, e + 8);
+    }
+}
 
 // Where position `slot` of sequence b lies in the shared cache, or -1.
 __device__ __forceinline__ int64_t cache_cell(const RopeParams& p, int b, int64_t slot, uint32_t& flags) {
@@ -109,83 +174,121 @@ __device__ __forceinline__ int64_t cache_cell(const RopeParams& p, int b, int64_
     return (int64_t)page * p.kv_stride_b + (slot % p.page_size) * p.kv_stride_n;
 }
 
-// This thread's 16 elements of a row: the two pieces' offsets, and which of the pairs turn.
-template <int D>
+// Where a thread's pieces lie in its row, and whether its pairs turn.
+template <int D, bool INTER>
 struct Lane {
     int t, o0, o1;
-    bool turning, interleaved;
-    __device__ __forceinline__ Lane(const RopeParams& p) {
-        t = threadIdx.x % (D / 16);
+    bool turning;
+    __device__ __forceinline__ Lane(const RopeParams& p, int thread) {
+        t = thread % (D / 16);
         turning = t < p.rd / 16;
-        interleaved = p.interleaved != 0;
-        const bool halves = turning && !interleaved;
+        const bool halves = turning && !INTER;
         o0 = (halves ? t : 2 * t) * 8;
         o1 = (halves ? t + p.rd / 16 : 2 * t + 1) * 8;
     }
+    // row element of a[e] (e < 8) or b[e - 8]
+    __device__ __forceinline__ int element(int e) const {
+        if (INTER) return o0 + 2 * (e & 7) + (e >> 3);
+        return e < 8 ? o0 + e : o1 + e - 8;
+    }
 };
 
-// Norm (gain: the row's factors) and rotation (cs: the token's cosines and sines) of a row, in place.
+// In shared memory: of each thread of a row, its 8 (cosine, sine) and its 16 gains, in 16-byte words of which neighbouring
+// threads' are neighbours.
 template <int D>
-__device__ __forceinline__ void norm_and_turn(float (&x)[16], const Lane<D>& ln, bool norm, const float* gain, float eps,
-                                              const float2* cs) {
-    if (norm) {
-        float ss = 0.f;
+struct Turns {
+    float4 w[4][D / 16];      // word i: c[2 i], c[2 i + 1], s[2 i], s[2 i + 1]
+};
+template <int D>
+struct Gains {
+    float4 w[4][D / 16];      // words 0, 1: of a; 2, 3: of b
+};
+template <int D, bool INTER>
+__device__ __forceinline__ void fill_gains(const RopeParams& p, Gains<D>& to, const float* gain, int i) {   // i < D
+    const Lane<D, INTER> owner(p, i / 16);
+    ((float*)&to.w[i % 16 / 4][owner.t])[i % 4] = gain != nullptr ? gain[owner.element(i % 16)] : 1.f;
+}
+// Pair f of a token at position `pos`.
+template <int D>
+__device__ __forceinline__ void fill_turn(const RopeParams& p, Turns<D>& to, int64_t pos, int f) {
+    const uint64_t turn = (uint64_t)pos * p.turns[f];                    // whole turns fall off the top
+    const int32_t x = (int32_t)((turn + (1ull << 31)) >> 32);            // 2^-32 turns, nearest
+    const int32_t quarter = (int32_t)((uint32_t)x + (1u << 29)) >> 30;
+    float s, c;
+    sincospif((float)(int32_t)((uint32_t)x - ((uint32_t)quarter << 30)) * 4.656612873077393e-10f, &s, &c);   // 2^-31: half turns
+    const float cc = (quarter & 1) ? -s : c, ss = (quarter & 1) ? c : s, sign = (quarter & 2) ? -p.factor : p.factor;
+    float* w = (float*)&to.w[f % 8 / 2][f / 8];
+    w[f % 2] = cc * sign;
+    w[2 + f % 2] = ss * sign;
+}
+
+__device__ __forceinline__ float2 times(float2 x, float2 y) { return __fmul2_rn(x, y); }
+
+// Sum of squares over a row's threads.
+template <int D>
+__device__ __forceinline__ float row_squares(const Pairs& x) {
+    float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
-#pragma unroll
-        for (int o = D / 32; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        const float inv = 1.f / sqrtf(ss * (1.f / D) + eps);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 g = *((const float4*)gain + i * (D / 16) + ln.t);
-            x[4 * i] *= inv * g.x;
-            x[4 * i + 1] *= inv * g.y;
-            x[4 * i + 2] *= inv * g.z;
-            x[4 * i + 3] *= inv * g.w;
-        }
+    for (int i = 0; i < 4; ++i) {
+        s = __ffma2_rn(x.a[i], x.a[i], s);
+        s = __ffma2_rn(x.b[i], x.b[i], s);
     }
-    if (ln.turning) {
-        float4 t4[4];
+    float ss = s.x + s.y;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t4[i] = *((const float4*)cs + i * (D / 16) + ln.t);
+    for (int o = D / 32; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    return ss;
+}
+// Norm by the row's sum of squares: the reciprocal root is the unit's, with one step of Newton's iteration (below a step of fp32).
+template <int D>
+__device__ __forceinline__ void norm_row(Pairs& x, float squares, float eps, const Gains<D>& g, int t) {
+    const float m = fmaf(squares, 1.f / D, eps);
+    float inv = rsqrtf(m);
+    if (m <= 3.402823466e38f) inv = fmaf(0.5f * inv, fmaf(-m * inv, inv, 1.f), inv);
+    const float2 i2 = make_float2(inv, inv);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float c = (i & 1) ? t4[i / 2].z : t4[i / 2].x, s = (i & 1) ? t4[i / 2].w : t4[i / 2].y;
-            if (ln.interleaved) {
-                const float a = x[2 * i], b = x[2 * i + 1];
-                x[2 * i] = fmaf(a, c, -(b * s));
-                x[2 * i + 1] = fmaf(b, c, a * s);
-            } else {
-                const float a = x[i], b = x[i + 8];
-                x[i] = fmaf(a, c, -(b * s));
-                x[i + 8] = fmaf(b, c, a * s);
-            }
-        }
+    for (int i = 0; i < 2; ++i) {
+        const float4 ga = g.w[i][t], gb = g.w[2 + i][t];
+        x.a[2 * i] = times(x.a[2 * i], times(make_float2(ga.x, ga.y), i2));
+        x.a[2 * i + 1] = times(x.a[2 * i + 1], times(make_float2(ga.z, ga.w), i2));
+        x.b[2 * i] = times(x.b[2 * i], times(make_float2(gb.x, gb.y), i2));
+        x.b[2 * i + 1] = times(x.b[2 * i + 1], times(make_float2(gb.z, gb.w), i2));
+    }
+}
+template <int D>
+__device__ __forceinline__ void turn_row(Pairs& x, const Turns<D>& cs, int t) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 w = cs.w[i][t];
+        const float2 c = make_float2(w.x, w.y), s = make_float2(w.z, w.w), m = make_float2(-w.z, -w.w);
+        const float2 a = x.a[i], b = x.b[i];
+        x.a[i] = __ffma2_rn(a, c, times(b, m));
+        x.b[i] = __ffma2_rn(b, c, times(a, s));
     }
 }
 
-// SEQ: rows of a prompt (TB of one loop of a sequence to a block), else one token of a step to a block.
-template <typename T, bool FP8, int D, bool SEQ>
-__global__ void __launch_bounds__(kRopeThreads, SEQ ? 4 : 2) plt_rope_kernel(const __grid_constant__ RopeParams p) {
-    constexpr int TB = SEQ ? kSeqTokens : 1;
+// ---- a decode step: a block for each token of a loop of a sequence ---------------------------------------------------------
+template <typename T, bool FP8, int D, bool INTER>
+__global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 2 ? 4 : 3) plt_rope_step_kernel(const __grid_constant__ RopeParams p) {
     constexpr int TPR = D / 16, RPB = kRopeThreads / TPR;      // threads of a row, rows of a pass
+    constexpr int U = 2;                                       // passes whose loads are in flight together
     using TD = typename std::conditional<FP8, uint8_t, T>::type;
-    __shared__ Token s_tok[TB];
-    __shared__ __align__(16) float2 s_cs[TB][kMaxPairs];
-    __shared__ __align__(16) float s_gain[2][D];
-    if (!SEQ) grid_launch_dependents();   // the attention's blocks may be set up meanwhile; they wait for this grid
+    __shared__ Turns<D> s_cs;
+    __shared__ Gains<D> s_gain[2];
+    grid_launch_dependents();   // the attention's blocks may be set up meanwhile; they wait for this grid
+    const int tid = threadIdx.x, token = blockIdx.x;
+    const int j = token % p.Qn, l = (token / p.Qn) % p.L, b = token / (p.Qn * p.L);
+    const Lane<D, INTER> ln(p, tid);
+    const int r_in = tid / TPR, rows = p.Hq + 2 * p.Hkv;       // queries, keys, values
+    auto row_at = [&](int r) {
+        if (r < p.Hq) return (const T*)p.q + (int64_t)token * p.q_stride + (int64_t)r * D;
+        r -= p.Hq;
+        if (r < p.Hkv) return (const T*)p.k + (int64_t)token * p.k_stride + (int64_t)r * D;
+        return (const T*)p.v + (int64_t)token * p.v_stride + (int64_t)(r - p.Hkv) * D;
+    };
+    Raw<T> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = r_in + u * RPB < rows ? load_raw(row_at(r_in + u * RPB), ln.o0, ln.o1) : no_raw<T>();
 
-    const int tid = threadIdx.x;
-    int b, l, t0;                       // t0: first row of the prompt, or the token of the step
-    if (SEQ) {
-        b = blockIdx.y / p.L;
-        l = blockIdx.y % p.L;
-        t0 = blockIdx.x * TB;
-    } else {
-        t0 = blockIdx.x % p.Qn;
-        l = (blockIdx.x / p.Qn) % p.L;
-        b = blockIdx.x / (p.Qn * p.L);
-    }
     uint32_t flags = 0;
     int n = p.seq_lens[b];
     int64_t before = p.prefix_lens != nullptr ? p.prefix_lens[b] : 0;
@@ -193,198 +296,189 @@ __global__ void __launch_bounds__(kRopeThreads, SEQ ? 4 : 2) plt_rope_kernel(con
         flags |= kDevGroupClamped;
         before = 0;
     }
-    if (SEQ) {
-        if (n < 0 || n > p.T) {
-            flags |= kDevSeqLenClamped;
-            n = n < 0 ? 0 : p.T;
-        }
-    } else if (n < 0 || n > before + p.max_seq_len) {
+    if (n < 0 || n > before + p.max_seq_len) {
         flags |= kDevSeqLenClamped;
         n = n < 0 ? 0 : (int)min(before + p.max_seq_len, (int64_t)0x7fffffff);
     }
-    int64_t start = 0;
-    if (SEQ && p.start != nullptr) {
-        start = p.start[b];
-        if (start < 0) {
-            flags |= kDevGroupClamped;
-            start = 0;
+    const int64_t pos = (int64_t)n - p.delta[l] - 1 - (p.Qn - 1 - j);
+    int64_t cell = -1;                                         // element of the cache or window where the key's first head starts
+    if (pos >= 0) {
+        if (l > 0) cell = (((int64_t)b * (p.L - 1) + (l - 1)) * p.w + pos % p.w) * p.Hkv * D;
+        else if (pos >= before) cell = cache_cell(p, b, pos - before, flags);
+    }
+    if (flags && tid == 0) atomicOr(p.status, flags);
+    for (int i = tid; i < p.rd / 2; i += kRopeThreads) fill_turn<D>(p, s_cs, pos, i);
+    if (tid < 2 * D) fill_gains<D, INTER>(p, s_gain[tid / D], tid < D ? p.q_gain : p.k_gain, tid % D);
+    __syncthreads();
+
+    const bool qnorm = p.q_gain != nullptr, knorm = p.k_gain != nullptr, gates = l > 0 && p.gate_out != nullptr;
+    const int64_t head_stride = l > 0 ? D : p.kv_stride_h;
+    TD* const k_to = (TD*)(l > 0 ? p.k_win : p.k_cache);
+    TD* const v_to = (TD*)(l > 0 ? p.v_win : p.v_cache);
+    for (int r0 = 0; r0 < rows; r0 += RPB * U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int r = r0 + u * RPB + r_in;
+            Pairs x = pairs_of<T, INTER>(raw[u]);
+            const int next = r + RPB * U;
+            if (r0 + RPB * U < rows) raw[u] = next < rows ? load_raw(row_at(next), ln.o0, ln.o1) : no_raw<T>();
+            const int kind = r < p.Hq ? 0 : r < p.Hq + p.Hkv ? 1 : r < rows ? 2 : 3;
+            if (qnorm || knorm) {
+                const float ss = row_squares<D>(x);
+                if (kind == 0 ? qnorm : kind == 1 && knorm) norm_row<D>(x, ss, p.eps, s_gain[kind & 1], ln.t);
+            }
+            if (kind < 2 && ln.turning) turn_row<D>(x, s_cs, ln.t);
+            float e[16];
+            elements_of<INTER>(x, e);
+            if (kind == 0) {
+                if (pos < 0)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) e[i] = 0.f;
+                T* const out = (T*)p.q_out + ((int64_t)token * p.Hq + r) * D;
+                store8(out + ln.o0, e);
+                store8(out + ln.o1, e + 8);
+            } else if (kind < 3 && cell >= 0) {
+                const int h = r - p.Hq - (kind == 2 ? p.Hkv : 0);
+                store_cached<FP8>((kind == 1 ? k_to : v_to) + cell + (int64_t)h * head_stride, ln.o0, ln.o1, e,
+                                  FP8 ? (kind == 1 ? p.k_scale : p.v_scale)[h] : 1.f);
+            }
+            if (gates) {
+                float dot = 0.f;
+                if (kind == 0 && pos >= 0) {
+                    const float* w = p.w_gate + (int64_t)r * D;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float4 g = *(const float4*)(w + (i < 2 ? ln.o0 : ln.o1) + 4 * (i & 1));
+                        dot = fmaf(g.x, e[4 * i], dot);
+                        dot = fmaf(g.y, e[4 * i + 1], dot);
+                        dot = fmaf(g.z, e[4 * i + 2], dot);
+                        dot = fmaf(g.w, e[4 * i + 3], dot);
+                    }
+                }
+#pragma unroll
+                for (int o = TPR / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                if (ln.t == 0 && kind == 0) p.gate_out[((int64_t)b * (p.L - 1) + (l - 1)) * p.Hq + r] = dot + p.b_gate[r];
+            }
         }
     }
-    if (SEQ && t0 >= n) {
+}
+
+// ---- the rows of a prompt: a block for kSeqTokens rows of a loop of a sequence ------------------------------------------------
+template <typename T, bool FP8, int D, bool INTER>
+__global__ void __launch_bounds__(kRopeThreads, 4) plt_rope_seq_kernel(const __grid_constant__ RopeParams p) {
+    constexpr int TB = kSeqTokens, TPR = D / 16, RPB = kRopeThreads / TPR;
+    using TD = typename std::conditional<FP8, uint8_t, T>::type;
+    __shared__ int64_t s_cell[TB];      // element where head 0 of the token's row starts in the cache, or -1: not stored
+    __shared__ Turns<D> s_cs[TB];
+    __shared__ Gains<D> s_gain[2];
+    const int tid = threadIdx.x, b = blockIdx.y / p.L, l = blockIdx.y % p.L, t0 = blockIdx.x * TB;
+    uint32_t flags = 0;
+    int n = p.seq_lens[b];
+    int64_t before = p.prefix_lens != nullptr ? p.prefix_lens[b] : 0, start = p.start != nullptr ? p.start[b] : 0;
+    if (before < 0 || start < 0) {
+        flags |= kDevGroupClamped;
+        before = max(before, (int64_t)0);
+        start = max(start, (int64_t)0);
+    }
+    if (n < 0 || n > p.T) {
+        flags |= kDevSeqLenClamped;
+        n = n < 0 ? 0 : p.T;
+    }
+    const int64_t first = start + t0 - p.delta[l];             // position of the block's first row
+    const int hi = min(n - t0, TB), lo = first < 0 ? (int)min(-first, (int64_t)TB) : 0;     // its tokens [lo, hi)
+    if (lo >= hi && !(l == 0 && hi > 0)) {
         if (flags && tid == 0) atomicOr(p.status, flags);
         return;
     }
-    if (tid < 2 * D) {
-        const float* gain = tid < D ? p.q_gain : p.k_gain;
-        // element e of a thread's 16 (pieces at o0 and o1): [e / 4][thread][e % 4]
-        const int i = tid % D, e = i / (TPR * 4) * 4 + i % 4, owner = i / 4 % TPR;
-        const bool halves = owner < p.rd / 16 && !p.interleaved;
-        const int o = e < 8 ? (halves ? owner : 2 * owner) * 8 + e : (halves ? owner + p.rd / 16 : 2 * owner + 1) * 8 + e - 8;
-        s_gain[tid / D][i] = gain != nullptr ? gain[o] : 1.f;
-    }
+    const bool cached = l == 0 && p.k_cache != nullptr;
     if (tid < TB) {
-        Token tk;
-        tk.cell = -1;
-        if (SEQ) {
-            const int t = t0 + tid;
-            tk.pos = t < n ? start + t - p.delta[l] : -1;
-            if (l == 0 && t < n && p.k_cache != nullptr) {
-                const int64_t slot = start + t - before;
-                if (slot >= p.max_seq_len) flags |= kDevSeqLenClamped;
-                else if (slot >= 0) tk.cell = cache_cell(p, b, slot, flags);
-            }
-        } else {
-            tk.pos = (int64_t)n - p.delta[l] - 1 - (p.Qn - 1 - t0);
-            if (tk.pos >= 0) {
-                if (l == 0) {
-                    if (tk.pos >= before) tk.cell = cache_cell(p, b, tk.pos - before, flags);
-                } else {
-                    tk.cell = (((int64_t)b * (p.L - 1) + (l - 1)) * p.w + tk.pos % p.w) * p.Hkv * D;
-                }
-            }
+        int64_t cell = -1;
+        if (cached && tid < hi) {
+            const int64_t slot = start + t0 + tid - before;
+            if (slot >= p.max_seq_len) flags |= kDevSeqLenClamped;
+            else if (slot >= 0) cell = cache_cell(p, b, slot, flags);
         }
-        if (tk.pos < 0) tk.pos = -1;
-        s_tok[tid] = tk;
+        s_cell[tid] = cell;
     }
     if (flags) atomicOr(p.status, flags);
-    __syncthreads();
-
-    // cosines and sines of the block's tokens
+    // the first queries are on their way while the tables are made
+    constexpr int U = sizeof(T) == 2 ? 2 : 1;                  // rows whose loads are in flight together
+    const Lane<D, INTER> ln(p, tid);
+    const int r_in = tid / TPR, q_from = lo * p.Hq, q_to = hi * p.Hq;
+    const int64_t q_base = (((int64_t)b * p.L + l) * p.T + t0) * p.Hq * D;
+    const T* const q_in = (const T*)p.q + q_base;
+    Raw<T> raws[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int r = q_from + u * RPB + r_in;
+        raws[u] = r < q_to ? load_raw(q_in + r * D, ln.o0, ln.o1) : no_raw<T>();
+    }
+    if (tid < 2 * D) fill_gains<D, INTER>(p, s_gain[tid / D], tid < D ? p.q_gain : p.k_gain, tid % D);
     const int pairs = p.rd / 2;
     for (int i = tid; i < TB * pairs; i += kRopeThreads) {
-        const int tk = i / pairs, f = i - tk * pairs;
-        const uint64_t turn = (uint64_t)s_tok[tk].pos * p.turns[f];      // whole turns fall off the top
-        const int32_t x = (int32_t)((turn + (1ull << 31)) >> 32);        // 2^-32 turns, nearest
-        const int32_t quarter = (int32_t)((uint32_t)x + (1u << 29)) >> 30;
-        float s, c;
-        sincospif((float)(int32_t)((uint32_t)x - ((uint32_t)quarter << 30)) * 4.656612873077393e-10f, &s, &c);   // 2^-31: half turns
-        const float cc = (quarter & 1) ? -s : c, ss = (quarter & 1) ? c : s;
-        // pair k of a thread's 8: [k / 2][thread][k % 2], so that neighbouring threads read neighbouring words
-        float2* const to = &s_cs[tk][((f % 8) / 2 * TPR + f / 8) * 2 + f % 2];
-        *to = (quarter & 2) ? make_float2(-cc * p.factor, -ss * p.factor) : make_float2(cc * p.factor, ss * p.factor);
+        const int tk = i / pairs;
+        fill_turn<D>(p, s_cs[tk], first + tk, i - tk * pairs);
     }
     __syncthreads();
 
-    const Lane<D> ln(p);
-    const int r_in = tid / TPR;
+    // A tensor's rows of the block lie one behind the other: row r is head r % heads of token r / heads (by a reciprocal; r and
+    // heads are below 2^13 and 2^11).
+    auto token_of = [](int r, uint32_t reciprocal) { return reciprocal == 0 ? r : (int)__umulhi((uint32_t)r, reciprocal); };
 
     // ---- queries -----------------------------------------------------------------------------------------------
-    const bool qnorm = p.q_gain != nullptr;
     {
-        constexpr int U = sizeof(T) == 2 ? 2 : 1;      // rows whose loads are in flight together
-        const int rows = TB * p.Hq;
-        for (int r0 = 0; r0 < rows; r0 += RPB * U) {
-            float x[U][16];
-            int64_t at[U];
-            bool live[U];
+        const bool norm = p.q_gain != nullptr;
+        T* const out = (T*)p.q_out + q_base;
+        for (int r0 = q_from; r0 < q_to; r0 += RPB * U) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int r = r0 + u * RPB + r_in;
-                const int tk = SEQ ? r / p.Hq : 0, h = r - tk * p.Hq;
-                live[u] = r < rows && s_tok[r < rows ? tk : 0].pos >= 0;
-                at[u] = -1;
-                if (SEQ) {
-                    at[u] = ((((int64_t)b * p.L + l) * p.T + t0 + tk) * p.Hq + h) * D;
-                    if (live[u]) {
-                        load8((const T*)p.q + at[u] + ln.o0, x[u]);
-                        load8((const T*)p.q + at[u] + ln.o1, x[u] + 8);
-                    }
-                } else {
-                    if (r < rows) at[u] = ((int64_t)blockIdx.x * p.Hq + h) * D;
-                    if (live[u]) {
-                        const T* src = (const T*)p.q + (int64_t)blockIdx.x * p.q_stride + (int64_t)h * D;
-                        load8(src + ln.o0, x[u]);
-                        load8(src + ln.o1, x[u] + 8);
-                    }
-                }
-                if (!live[u])
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[u][i] = 0.f;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int r = r0 + u * RPB + r_in;
-                const int tk = SEQ ? min(r / p.Hq, TB - 1) : 0;
-                norm_and_turn<D>(x[u], ln, qnorm, s_gain[0], p.eps, s_cs[tk]);
-                if (SEQ ? live[u] : at[u] >= 0) {
-                    if (!live[u])
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) x[u][i] = 0.f;
-                    store8((T*)p.q_out + at[u] + ln.o0, x[u]);
-                    store8((T*)p.q_out + at[u] + ln.o1, x[u] + 8);
-                }
-                if (!SEQ && l > 0 && p.gate_out != nullptr) {
-                    float dot = 0.f;
-                    if (live[u]) {
-                        const float* w = p.w_gate + (int64_t)r * D;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) dot = fmaf(w[i < 8 ? ln.o0 + i : ln.o1 + i - 8], x[u][i], dot);
-                    }
-#pragma unroll
-                    for (int o = TPR / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                    if (ln.t == 0 && r < rows) p.gate_out[((int64_t)b * (p.L - 1) + (l - 1)) * p.Hq + r] = dot + p.b_gate[r];
+                const int r = r0 + u * RPB + r_in, tk = min(token_of(r, p.q_reciprocal), TB - 1);
+                Pairs x = pairs_of<T, INTER>(raws[u]);
+                if (norm) norm_row<D>(x, row_squares<D>(x), p.eps, s_gain[0], ln.t);
+                if (ln.turning) turn_row<D>(x, s_cs[tk], ln.t);
+                if (r < q_to) {
+                    float e[16];
+                    elements_of<INTER>(x, e);
+                    store8(out + r * D + ln.o0, e);
+                    store8(out + r * D + ln.o1, e + 8);
                 }
             }
+            if (r0 + RPB * U < q_to)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int r = r0 + (U + u) * RPB + r_in;
+                    raws[u] = r < q_to ? load_raw(q_in + r * D, ln.o0, ln.o1) : no_raw<T>();
+                }
         }
     }
 
-    // ---- keys, then values ---------------------------------------------------------------------------------------
-    const bool knorm = p.k_gain != nullptr;
-    const int rows = TB * p.Hkv;
-    const int64_t head_stride = !SEQ && l > 0 ? D : p.kv_stride_h;
-    TD* const k_to = (TD*)(!SEQ && l > 0 ? p.k_win : p.k_cache);
-    TD* const v_to = (TD*)(!SEQ && l > 0 ? p.v_win : p.v_cache);
-    const bool values = SEQ ? l == 0 && p.v_cache != nullptr : true;
-    for (int r0 = 0; r0 < rows; r0 += RPB) {
-        const int r = r0 + r_in;
-        const int tk = SEQ ? min(r / p.Hkv, TB - 1) : 0, h = r - tk * p.Hkv;
-        const Token tok = s_tok[tk];
-        const bool live = r < rows && tok.pos >= 0, cached = live && tok.cell >= 0;
-        float x[16], y[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.f;
-        int64_t at = 0;
-        const T *ksrc, *vsrc;
-        if (SEQ) {
-            at = l == 0 ? (((int64_t)b * p.T + t0 + tk) * p.Hkv + h) * D
-                        : ((((int64_t)b * (p.L - 1) + (l - 1)) * p.T + t0 + tk) * p.Hkv + h) * D;
-            ksrc = (const T*)(l == 0 ? p.k : p.k_loc) + at;
-            vsrc = (const T*)p.v + at;
-        } else {
-            ksrc = (const T*)p.k + (int64_t)blockIdx.x * p.k_stride + (int64_t)h * D;
-            vsrc = (const T*)p.v + (int64_t)blockIdx.x * p.v_stride + (int64_t)h * D;
+    // ---- keys, and the first loop's values ------------------------------------------------------------------------
+    const bool norm = p.k_gain != nullptr;
+    const int64_t base = (l == 0 ? (int64_t)b * p.T + t0 : ((int64_t)b * (p.L - 1) + (l - 1)) * p.T + t0) * p.Hkv * D;
+    const T* const k_in = (const T*)(l == 0 ? p.k : p.k_loc) + base;
+    T* const k_out = (T*)(l == 0 ? p.k_out : p.k_loc_out);
+    const int from = (l == 0 ? 0 : lo) * p.Hkv, to = hi * p.Hkv;
+    for (int r0 = from; r0 < to; r0 += RPB) {
+        const int r = r0 + r_in, tk = min(token_of(r, p.k_reciprocal), TB - 1);
+        const Raw<T> raw = r < to ? load_raw(k_in + r * D, ln.o0, ln.o1) : no_raw<T>();
+        const int64_t cell = cached && r < to ? s_cell[tk] : -1;
+        Raw<T> values = no_raw<T>();
+        if (cell >= 0) values = load_raw((const T*)p.v + base + r * D, ln.o0, ln.o1);
+        Pairs x = pairs_of<T, INTER>(raw);
+        if (norm) norm_row<D>(x, row_squares<D>(x), p.eps, s_gain[1], ln.t);
+        if (ln.turning) turn_row<D>(x, s_cs[tk], ln.t);
+        float e[16];
+        elements_of<INTER>(x, e);
+        if (k_out != nullptr && r < to) {
+            store8(k_out + base + r * D + ln.o0, e);
+            store8(k_out + base + r * D + ln.o1, e + 8);
         }
-        if (SEQ ? live : cached) {
-            load8(ksrc + ln.o0, x);
-            load8(ksrc + ln.o1, x + 8);
-        }
-        if (values && cached) {
-            load8(vsrc + ln.o0, y);
-            load8(vsrc + ln.o1, y + 8);
-        }
-        norm_and_turn<D>(x, ln, knorm, s_gain[1], p.eps, s_cs[tk]);
-        if (SEQ && live) {
-            T* const out = (T*)(l == 0 ? p.k_out : p.k_loc_out);
-            if (out != nullptr) {
-                store8(out + at + ln.o0, x);
-                store8(out + at + ln.o1, x + 8);
-            }
-        }
-        if (cached && (!SEQ || l == 0)) {
-            TD* const kd = k_to + tok.cell + (int64_t)h * head_stride;
-            TD* const vd = v_to + tok.cell + (int64_t)h * head_stride;
-            if constexpr (FP8) {
-                const float ks = p.k_scale[h], vs = p.v_scale[h];
-                store8_codes(kd + ln.o0, x, ks);
-                store8_codes(kd + ln.o1, x + 8, ks);
-                store8_codes(vd + ln.o0, y, vs);
-                store8_codes(vd + ln.o1, y + 8, vs);
-            } else {
-                store8(kd + ln.o0, x);
-                store8(kd + ln.o1, x + 8);
-                store8(vd + ln.o0, y);
-                store8(vd + ln.o1, y + 8);
-            }
+        if (cell >= 0) {
+            const int h = r - tk * p.Hkv;
+            const int64_t at = cell + (int64_t)h * p.kv_stride_h;
+            store_cached<FP8>((TD*)p.k_cache + at, ln.o0, ln.o1, e, FP8 ? p.k_scale[h] : 1.f);
+            elements_of<INTER>(pairs_of<T, INTER>(values), e);
+            store_cached<FP8>((TD*)p.v_cache + at, ln.o0, ln.o1, e, FP8 ? p.v_scale[h] : 1.f);
         }
     }
 }
@@ -505,23 +599,35 @@ plt_status common(plt_rope_t h, int32_t batch, const int32_t* page_table, int32_
     p->k_scale = k_scale; p->v_scale = v_scale;
     p->turns = h->turns; p->status = h->status;
     p->B = batch; p->L = c.L; p->Qn = h->Qn; p->Hq = c.Hq; p->Hkv = c.Hkv; p->w = c.w; p->max_seq_len = c.max_seq_len;
-    p->rd = h->rd; p->interleaved = c.layout == PLT_ROPE_INTERLEAVED;
+    p->rd = h->rd;
+    p->q_reciprocal = c.Hq > 1 ? (uint32_t)(((1ull << 32) + c.Hq - 1) / c.Hq) : 0;
+    p->k_reciprocal = c.Hkv > 1 ? (uint32_t)(((1ull << 32) + c.Hkv - 1) / c.Hkv) : 0;
     p->factor = c.attn_factor != 0.f ? c.attn_factor : 1.f;
     p->eps = c.norm_eps;
     for (int l = 0; l < kMaxLoops; ++l) p->delta[l] = h->delta[l];
     return PLT_OK;
 }
 
-template <bool SEQ>
-plt_status launch(plt_rope_t h, const RopeParams& p, dim3 grid, cudaStream_t stream) {
+template <typename T, bool FP8, int D, bool INTER>
+void launch_one(bool seq, const RopeParams& p, dim3 grid, cudaStream_t stream) {
+    if (seq) plt_rope_seq_kernel<T, FP8, D, INTER><<<grid, kRopeThreads, 0, stream>>>(p);
+    else plt_rope_step_kernel<T, FP8, D, INTER><<<grid, kRopeThreads, 0, stream>>>(p);
+}
+
+template <bool INTER>
+void launch_type(const plt_rope_config& c, bool seq, const RopeParams& p, dim3 grid, cudaStream_t stream) {
+    if (c.kv_dtype == PLT_KV_E4M3) launch_one<__nv_bfloat16, true, 128, INTER>(seq, p, grid, stream);
+    else if (c.dtype == PLT_BF16 && c.d == 128) launch_one<__nv_bfloat16, false, 128, INTER>(seq, p, grid, stream);
+    else if (c.dtype == PLT_BF16) launch_one<__nv_bfloat16, false, 64, INTER>(seq, p, grid, stream);
+    else if (c.d == 128) launch_one<float, false, 128, INTER>(seq, p, grid, stream);
+    else launch_one<float, false, 64, INTER>(seq, p, grid, stream);
+}
+
+plt_status launch(plt_rope_t h, bool seq, const RopeParams& p, dim3 grid, cudaStream_t stream) {
     DeviceScope scope(h->device);
     if (scope.err != cudaSuccess) return handle_fail(h, g_rope_error, PLT_ERR_CUDA, "cudaSetDevice: %s", cudaGetErrorString(scope.err));
-    const plt_rope_config& c = h->cfg;
-    if (c.kv_dtype == PLT_KV_E4M3) plt_rope_kernel<__nv_bfloat16, true, 128, SEQ><<<grid, kRopeThreads, 0, stream>>>(p);
-    else if (c.dtype == PLT_BF16 && c.d == 128) plt_rope_kernel<__nv_bfloat16, false, 128, SEQ><<<grid, kRopeThreads, 0, stream>>>(p);
-    else if (c.dtype == PLT_BF16) plt_rope_kernel<__nv_bfloat16, false, 64, SEQ><<<grid, kRopeThreads, 0, stream>>>(p);
-    else if (c.d == 128) plt_rope_kernel<float, false, 128, SEQ><<<grid, kRopeThreads, 0, stream>>>(p);
-    else plt_rope_kernel<float, false, 64, SEQ><<<grid, kRopeThreads, 0, stream>>>(p);
+    if (h->cfg.layout == PLT_ROPE_INTERLEAVED) launch_type<true>(h->cfg, seq, p, grid, stream);
+    else launch_type<false>(h->cfg, seq, p, grid, stream);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return handle_fail(h, g_rope_error, PLT_ERR_CUDA, "launching the kernel: %s", cudaGetErrorString(e));
     return PLT_OK;
@@ -630,7 +736,7 @@ PLT_API plt_status plt_rope_step(plt_rope_t h, const plt_rope_step_args* a, void
     p.q_gain = a->q_gain; p.k_gain = a->k_gain;
     p.w_gate = a->w_gate; p.b_gate = a->b_gate; p.gate_out = c.L > 1 ? a->gate_logits : nullptr;
     p.seq_lens = a->seq_lens; p.prefix_lens = a->prefix_lens;
-    return launch<false>(h, p, dim3((unsigned)rows_total), (cudaStream_t)cuda_stream);
+    return launch(h, false, p, dim3((unsigned)rows_total), (cudaStream_t)cuda_stream);
 }
 
 PLT_API plt_status plt_rope_seq(plt_rope_t h, const plt_rope_seq_args* a, void* cuda_stream) {
@@ -668,7 +774,7 @@ PLT_API plt_status plt_rope_seq(plt_rope_t h, const plt_rope_seq_args* a, void* 
     p.seq_lens = a->seq_lens; p.start = a->start; p.prefix_lens = a->prefix_lens;
     p.T = a->rows;
     const dim3 grid((unsigned)((a->rows + kSeqTokens - 1) / kSeqTokens), (unsigned)(a->batch * c.L));
-    return launch<true>(h, p, grid, (cudaStream_t)cuda_stream);
+    return launch(h, true, p, grid, (cudaStream_t)cuda_stream);
 }
 
 PLT_API plt_status plt_rope_check(plt_rope_t h, void* cuda_stream, uint32_t* out_bits) {
