@@ -56,6 +56,7 @@ struct Params {
                                // lie in a prefix of their own)
     int32_t late_wait;         // 1: the kernel before this one has nothing for it and let it go once it might start (the warp-level
                                // main kernel then waits for that one's end at its own end, so that the kernel behind sees both)
+    const int32_t* block_limit; // or null: blocks of the warp-level main kernel that may take part (a word on the device)
     float scale_log2;          // sm_scale * log2(e)
     int32_t delta[kMaxLoops];  // per-loop causal offset
 };

@@ -644,6 +644,9 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
         pp.B = p.B; pp.L = p.L; pp.Qn = p.Qn; pp.Hq = p.Hq; pp.Hkv = p.Hkv; pp.G = p.G; pp.R = p.R; pp.d = p.d; pp.w = p.w;
         pp.max_seq_len = p.max_seq_len; pp.page_size = p.page_size; pp.num_pool_pages = p.num_pool_pages;
         pp.scale_log2 = p.scale_log2;
+        p.late_wait = pp.groups > 0 && h->bf16 && !h->umma;
+        pp.own_per_sm = p.late_wait ? h->ctas_per_sm : 0;
+        pp.own_items = p.B * (p.Hkv / p.hpc) * (p.L > 1 ? 2 : 1);
         for (int l = 0; l < kMaxLoops; ++l) pp.delta[l] = p.delta[l];
         if (c.page_size > 0 && pp.groups > 0) {
             plt_status s = encode_rows(h, &prefix->maps[0], a->k_cache, es, c.d, c.page_size, c.Hkv, a->num_pool_pages, sn, sh, sb, pp.kbox, 1);
@@ -666,7 +669,7 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
         p.seq_lens = pp.plan.own_lens;
         p.win_lens = pp.plan.win_lens;
         p.win_free = 1;
-        p.late_wait = pp.groups > 0 && h->bf16 && !h->umma;
+        p.block_limit = p.late_wait ? pp.plan.chunk + 2 : nullptr;
     }
     if (step) {
         Params pre = p;

@@ -382,7 +382,7 @@ plt_decode_main_bf16(const __grid_constant__ CUtensorMap tmK, const __grid_const
     // its own wait, hence not earlier); it waits for this grid to complete before it reads the partials.
     grid_launch_dependents();
     const int64_t T = s_prefix[p.B];
-    const int cta = blockIdx.x, nctas = plan_ctas(T, (int)gridDim.x);
+    const int cta = blockIdx.x, nctas = plan_ctas(T, p.block_limit != nullptr ? min((int)gridDim.x, *p.block_limit) : (int)gridDim.x);
     if (cta == 0)
         for (int b = tid; b <= p.B; b += C::NTHREADS) p.prefix[b] = s_prefix[b];
     const bool in_plan = cta < nctas;

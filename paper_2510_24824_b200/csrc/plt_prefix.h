@@ -14,13 +14,15 @@ constexpr int kPrefixLead = 2;        // line positions that stand for starting 
 //     the same number of nearly equal pieces of at most `*chunk` tiles, and piece i is block i's and leaves its partial in slot i.
 //   - Else (*chunk = 0) the units lie one after the other on a line of key tiles, each preceded by kPrefixLead positions, and the
 //     line is cut into equal ranges, one for each block, which may hold several pieces; slot unit + block.
+// Not every block need take part: the pass over the prefixes is bound by the tensor cores and its start, the one over the own caches
+// by memory and its start, so that the plan may leave some multiprocessors to the latter, which then runs at the same time.
 struct PrefixPlan {
     int32_t *begin;      // [groups + 1] first sequence of each group, clamped
     int32_t *len;        // [groups] tokens of each prefix, clamped; 0 where the group is empty
     int32_t *line;       // [groups + 1] first line position of each group's units
     int32_t *unit;       // [groups + 1] first unit of each group
     int32_t *piece;      // [groups + 1] first piece of each group's units (*chunk > 0)
-    int32_t *chunk;      // one word
+    int32_t *chunk;      // three words: tiles of a chunk or 0, blocks that take part, blocks of the pass over the own caches
     int32_t *own_lens;   // [max_batch] tokens that each sequence holds itself
     int32_t *win_lens;   // [max_batch, L - 1] valid window slots of each loop
 };
@@ -40,6 +42,11 @@ struct PrefixParams {
     int32_t groups, B, L, Qn, Hq, Hkv, G, R, d, w;
     int32_t max_seq_len, max_prefix_len, page_size, max_pages, num_pool_pages, kbox;
     int32_t blocks;                // of the prefix kernel
+    int32_t own_per_sm;            // blocks of the pass over the own caches on a multiprocessor; 0: it runs behind this one
+    int32_t own_rate;              // bytes a nanosecond that a multiprocessor streams of the own caches, about
+    int32_t own_items;             // items of the own caches and windows (sequence, heads of a block)
+    int32_t tile_ns;               // time of a key tile of 256 rows, about
+    int32_t token_bytes;           // K and V rows of a token
     int32_t q_tma;                 // 1: query rows by TMA (the heads of a KV head divide 128)
     float scale_log2;
     int32_t delta[kMaxLoops];

@@ -61,7 +61,7 @@ int64_t units_of(const plt_prefix_attn_config* c, int R) {
 int rows_of(const plt_prefix_attn_config* c) { return c->L * (c->q_len > 1 ? c->q_len : 1) * (c->Hq / c->Hkv); }
 
 size_t plan_bytes(const plt_prefix_attn_config* c) {
-    return 256 + 4 * ((size_t)5 * (c->max_groups + 1) + 1 + (size_t)c->max_batch * c->L);
+    return 256 + 4 * ((size_t)5 * (c->max_groups + 1) + 3 + (size_t)c->max_batch * c->L);
 }
 size_t workspace_of(const plt_prefix_attn_config* c, int blocks) {
     const size_t slots = (size_t)units_of(c, rows_of(c)) + blocks;
@@ -148,7 +148,7 @@ PLT_API plt_status plt_prefix_attn_create(const plt_prefix_attn_config* config, 
     h->plan.line = at; at += groups;
     h->plan.unit = at; at += groups;
     h->plan.piece = at; at += groups;
-    h->plan.chunk = at; at += 1;
+    h->plan.chunk = at; at += 3;
     h->plan.own_lens = at; at += config->max_batch;
     h->plan.win_lens = at;
     h->acc = (float*)(ws + ((plan_bytes(config) + 255) & ~(size_t)255));
@@ -213,6 +213,15 @@ PLT_API plt_status plt_prefix_attn_run(plt_prefix_attn_t h, const plt_decode_att
     p.plan = h->plan; p.acc = h->acc; p.ml = h->ml; p.status = h->status;
     p.groups = x->num_groups; p.max_prefix_len = c.max_prefix_len; p.max_pages = x->max_pages; p.blocks = h->blocks;
     p.q_tma = 128 % h->G == 0;
+    // Rates that the plan divides the multiprocessors by, read off batches of 21 to 96 sequences behind 1777 to 8192 tokens with 9 to
+    // 138 multiprocessors left to the own caches: a key tile of 256 rows takes 1.9 us (8-bit caches 3.0); of the own caches a
+    // multiprocessor streams 80 bytes a nanosecond at up to 8 packed rows, and less where its products bound it: 50 at 16 and 24 at 32
+    // (8-bit caches 36 at 16; with heads of 64 58 at 8; the others go on from these). 64 sequences of two loops: 39 us with the
+    // multiprocessors divided, 46 with one pass behind the other.
+    p.tile_ns = fp8 ? 3000 : 1900;
+    p.own_rate = h->R <= 8 ? 80 : h->R <= 16 ? (fp8 ? 36 : 50) : h->R <= 32 ? (fp8 ? 18 : 24) : (fp8 ? 9 : 12);
+    if (c.d == 64) p.own_rate = p.own_rate * 7 / 10;
+    p.token_bytes = 2 * c.Hkv * c.d * es;
     // keys of a TMA box: all of a tile, or as many as both tile and page are made of
     p.kbox = kPrefixTile;
     while (c.page_size > 0 && c.page_size % p.kbox != 0) p.kbox >>= 1;

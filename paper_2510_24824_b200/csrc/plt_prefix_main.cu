@@ -108,7 +108,7 @@ __device__ __forceinline__ PWalk walk_of_block(const PrefixParams& p, const Pref
             w.hi = c + 1;
         }
     } else {
-        const int T = first[p.groups], C = prefix_blocks(T, p.blocks);
+        const int T = first[p.groups], C = prefix_blocks(T, plan.chunk[1]);
         if (c < C && T > 0) {
             w.pos = prefix_range(T, c, C);
             w.hi = prefix_range(T, c + 1, C);
@@ -124,6 +124,11 @@ __device__ __forceinline__ PWalk walk_of_block(const PrefixParams& p, const Pref
     }
     return w;
 }
+
+constexpr int kOwnStartNs = 7000;     // what starting and finishing the pass over the own caches takes, about
+constexpr int kGapNs = 2000;          // what one pass behind the other loses between them, about
+constexpr int kItemNs = 3000;         // what one of its items takes a block at least, about
+constexpr int kMemoryRate = 5500;     // bytes a nanosecond that the device streams, about
 
 // ---- making the plan ----------------------------------------------------------------------------------------------
 __device__ __forceinline__ int warp_scan(int x, int lane) {     // inclusive
@@ -159,15 +164,42 @@ __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const Prefix
     const int positions = units * (tiles + kPrefixLead);
     const int unit = warp_scan(units, lane), line = warp_scan(positions, lane);
     const int all_units = __shfl_sync(0xffffffffu, unit, 31), all = __shfl_sync(0xffffffffu, line, 31) - all_units * kPrefixLead;
+    // How many blocks take part. What both passes take is estimated (in whole numbers: every block and the merge have to come to the
+    // same plan) for sixteen ways of dividing the multiprocessors, a lane each; none for the own caches means one pass behind the
+    // other.
+    int blocks = p.blocks, own_blocks = 0x7fffffff;
+    if (p.own_per_sm > 0 && all_units > 0) {
+        const bool wide = (rows - 1) % kPrefixRows >= 128;      // of a group's units all but the last are; that one may have half the work
+        const int last = tiles > 0 && !wide ? p.Hkv * (tiles / 2) : 0;
+        const int work = __shfl_sync(0xffffffffu, warp_scan(units * tiles - last, lane), 31);
+        int64_t tokens = 0;
+        for (int b = lane; b < p.B; b += 32) tokens += max(p.seq_lens[b], 0);
+        tokens -= (int64_t)(lane < p.groups ? next - begin : 0) * len;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) tokens += __shfl_xor_sync(0xffffffffu, tokens, o);
+        const int64_t bytes = (max(tokens, (int64_t)0) + (int64_t)p.B * (p.L - 1) * p.w) * p.token_bytes;
+        const int left = p.blocks * (lane & 15) / 16, mine = p.blocks - left;
+        const int64_t prefix_ns = (int64_t)((work + mine - 1) / mine) * p.tile_ns;
+        const int n_own = left > 0 ? left : p.blocks;
+        const int64_t own_ns = kOwnStartNs + max(bytes / min(n_own * p.own_rate, kMemoryRate), (int64_t)p.own_items * kItemNs / (n_own * p.own_per_sm));
+        // side by side the longer one counts, and the shorter one a little: it takes its share of memory and of the L2
+        const int64_t ns = left > 0 ? max(prefix_ns, own_ns) + min(prefix_ns, own_ns) / 8 : prefix_ns + own_ns + kGapNs;
+        const uint32_t cost = (uint32_t)min(ns, (int64_t)0x7fffffff), best = __reduce_min_sync(0xffffffffu, cost);
+        const int way = __ffs(__ballot_sync(0xffffffffu, cost == best)) - 1;
+        if (way > 0) {
+            blocks = __shfl_sync(0xffffffffu, mine, way);
+            own_blocks = (p.blocks - blocks) * p.own_per_sm;
+        }
+    }
     // The shortest chunk that lets every piece have a block, tried in steps of an eighth from the average on; not more than a
     // tenth and a tile above what the line's ranges hold.
     int chunk = 0, piece = 0;
-    if (all_units > 0 && all_units <= p.blocks) {
-        const int least = (all + p.blocks - 1) / p.blocks, step = (least + 7) / 8;
-        const int most = (all + all_units * kPrefixLead) / p.blocks * 11 / 10 + 1;
+    if (all_units > 0 && all_units <= blocks) {
+        const int least = (all + blocks - 1) / blocks, step = (least + 7) / 8;
+        const int most = (all + all_units * kPrefixLead) / blocks * 11 / 10 + 1;
         for (int s = least; s <= max(most, least); s += step) {
             const int n = warp_scan(tiles > 0 ? units * ((tiles + s - 1) / s) : 0, lane);
-            if (__shfl_sync(0xffffffffu, n, 31) <= p.blocks) {
+            if (__shfl_sync(0xffffffffu, n, 31) <= blocks) {
                 chunk = s;
                 piece = n;
                 break;
@@ -183,7 +215,9 @@ __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const Prefix
     if (lane <= p.groups) to.begin[lane] = begin;
     if (lane == 0) {
         to.line[0] = to.unit[0] = to.piece[0] = 0;
-        *to.chunk = chunk;
+        to.chunk[0] = chunk;
+        to.chunk[1] = blocks;
+        to.chunk[2] = own_blocks;
     }
 }
 
@@ -753,7 +787,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
 constexpr int kPlanThreads = 512;
 
 __global__ void __launch_bounds__(kPlanThreads) plt_prefix_plan(const __grid_constant__ PrefixParams p) {
-    __shared__ int32_t s_begin[kMaxGroups + 1], s_len[kMaxGroups], s_line[kMaxGroups + 1], s_unit[kMaxGroups + 1], s_piece[kMaxGroups + 1], s_chunk;
+    __shared__ int32_t s_begin[kMaxGroups + 1], s_len[kMaxGroups], s_line[kMaxGroups + 1], s_unit[kMaxGroups + 1], s_piece[kMaxGroups + 1], s_chunk[3];
     grid_launch_dependents();
     const int tid = threadIdx.x, lane = tid & 31;
     uint32_t flags = 0;
@@ -764,7 +798,7 @@ __global__ void __launch_bounds__(kPlanThreads) plt_prefix_plan(const __grid_con
         to.line = s_line;
         to.unit = s_unit;
         to.piece = s_piece;
-        to.chunk = &s_chunk;
+        to.chunk = s_chunk;
         if (tid < 32) plan_by_warp(p, to, lane, flags);
     } else {
         for (int g = tid; g <= p.groups; g += kPlanThreads) s_begin[g] = p.group_begin[g];
@@ -820,7 +854,9 @@ __global__ void __launch_bounds__(kPlanThreads) plt_prefix_plan(const __grid_con
                 s_unit[p.groups] = unit;
                 s_line[p.groups] = line;
                 s_piece[p.groups] = 0;
-                s_chunk = 0;
+                s_chunk[0] = 0;
+                s_chunk[1] = p.blocks;
+                s_chunk[2] = 0x7fffffff;
             }
         }
     }
@@ -832,7 +868,7 @@ __global__ void __launch_bounds__(kPlanThreads) plt_prefix_plan(const __grid_con
         p.plan.piece[g] = s_piece[g];
         if (g < p.groups) p.plan.len[g] = s_len[g];
     }
-    if (tid == 0) *p.plan.chunk = s_chunk;
+    if (tid < 3) p.plan.chunk[tid] = s_chunk[tid];
     for (int b = tid; b < p.B; b += kPlanThreads) {
         // the group of sequence b, if any
         int len = 0;

@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) 
                 tile = plan.piece[group] + (int64_t)u * count;
             } else {
                 const int T = plan.line[pp.groups], first = plan.line[group] + u * (tiles + kPrefixLead) + kPrefixLead;
-                const int C = prefix_blocks(T, pp.blocks), c0 = prefix_block_of(first, T, C);
+                const int C = prefix_blocks(T, plan.chunk[1]), c0 = prefix_block_of(first, T, C);
                 count = prefix_block_of(first + tiles - 1, T, C) - c0 + 1;
                 tile = (int64_t)plan.unit[group] + u + c0;
             }
