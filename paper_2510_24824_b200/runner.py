@@ -490,6 +490,64 @@ class Rope:
             pass
 
 
+class PrefixAttn:
+    """Owns one plt_prefix_attn handle sized for a problem: decode steps of sequences that share prefixes in front of the caches of a
+    DeviceProblem (whose max_seq_len and lengths are the own caches' capacity and the whole sequences' lengths)."""
+
+    def __init__(self, p, max_prefix_len: int, max_groups: int = 1, device_index: int = 0, max_batch: Optional[int] = None, q_len: int = 1,
+                 kernel_path: int = 0, typical_seq_len: int = 0):
+        self.handle = None
+        self.config = B.make_prefix_config(
+            p.dtype, max_batch or max(p.B, 1), p.L, p.Hq, p.Hkv, p.d, p.max_seq_len, p.w, max_prefix_len, max_groups, page_size=p.page_size,
+            sm_scale=p.sm_scale, device=device_index, loop_offset=None if p.loop_offset is None else [int(x) for x in p.loop_offset],
+            kernel_path=kernel_path, kv_dtype=p.kv_dtype, q_len=q_len, typical_seq_len=typical_seq_len)
+        self.handle = B.plt_prefix_attn_create(self.config)
+
+    def prefix_args(self, group_begin, prefix_lens, k_prefix=None, v_prefix=None, page_table=None):
+        """group_begin [groups + 1] and prefix_lens [groups] int32; k_prefix, v_prefix [groups, tokens, Hkv, d] (views whose rows are dense
+        will do), or in pages page_table [groups, pages] int32."""
+        c, groups = self.config, prefix_lens.shape[0]
+        _dense("prefix_lens", prefix_lens, torch.int32, groups, 1)
+        _dense("group_begin", group_begin, torch.int32, groups + 1, 1)
+        if c.page_size:
+            _dense("page_table", page_table, torch.int32, groups, page_table.shape[-1])
+            return B.make_prefix_args(groups, group_begin, prefix_lens, page_table=page_table, max_pages=page_table.shape[-1])
+        want = torch.uint8 if c.kv_dtype == B.PLT_KV_E4M3 else torch.bfloat16
+        for name, t in (("k_prefix", k_prefix), ("v_prefix", v_prefix)):
+            if t.dtype != want or t.dim() != 4 or t.shape[0] < groups or t.shape[1] < c.max_prefix_len or tuple(t.shape[2:]) != (c.Hkv, c.d) or \
+                    t.stride(3) != 1 or t.stride() != k_prefix.stride():
+                raise ValueError(f"{name}: {groups} x {c.max_prefix_len} x {c.Hkv} x {c.d} elements of {want} with dense rows, K and V alike, are "
+                                 f"needed, not {tuple(t.shape)} of {t.dtype} with strides {t.stride()}")
+        # a dimension of one has any stride
+        token = k_prefix.stride(1) if c.max_prefix_len > 1 else c.Hkv * c.d
+        return B.make_prefix_args(groups, group_begin, prefix_lens, k_prefix=k_prefix, v_prefix=v_prefix, strides=(
+            k_prefix.stride(0) if groups > 1 else c.max_prefix_len * token, token, k_prefix.stride(2) if c.Hkv > 1 else c.d))
+
+    def run(self, dp: DeviceProblem, prefix: B.PrefixArgs, stream: Optional[int] = None, out=None):
+        B.plt_prefix_attn_run(self.handle, dp.args(out), prefix, torch.cuda.current_stream().cuda_stream if stream is None else stream)
+        return dp.out if out is None else out
+
+    def check(self, stream: Optional[int] = None) -> int:
+        return B.plt_prefix_attn_check(self.handle, torch.cuda.current_stream().cuda_stream if stream is None else stream)
+
+    def close(self):
+        if self.handle is not None:
+            B.plt_prefix_attn_destroy(self.handle)
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 class DraftVerify:
     """Owns one plt_draft_verify handle: which drafted tokens of a multi-token step stand, and the token behind them.
     Probabilities [B, K + 1, V] and [B, K, V] may be views whose vocabulary is dense; the other tensors are dense."""

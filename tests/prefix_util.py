@@ -10,7 +10,7 @@ class Problem:
     lens: total lengths where they are not prefix + own."""
 
     def __init__(self, seed, own, plens, begin, L=1, Hq=4, Hkv=2, d=128, cap=None, pcap=None, w=16, page=0, q_len=1, kv="", lens=None, offsets=None,
-                 peak=1.5, max_groups=None, max_batch=None, junk=float("nan"), kernel_path=0, strided=False):
+                 peak=1.5, max_groups=None, max_batch=None, junk=float("nan"), kernel_path=0, strided=False, win_lens=None, scale=0.0, own_strided=False):
         g = torch.Generator("cuda").manual_seed(seed)
         rand = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
         self.own, self.plens, self.begin, self.L, self.q_len, self.kv = own, plens, begin, L, q_len, kv
@@ -53,7 +53,7 @@ class Problem:
         self.values = dict(k_own=value(self.k_own, self.k_scale), v_own=value(self.v_own, self.v_scale),
                            pre=[(value(a, self.k_scale)[:p], value(c, self.v_scale)[:p]) for a, c, p in zip(self.k_pre, self.v_pre, plens)],
                            k_win=None if L == 1 else value(self.k_win, self.k_scale), v_win=None if L == 1 else value(self.v_win, self.v_scale))
-        self.w, self.d = w, d
+        self.w, self.d, self.win_lens, self.scale = w, d, win_lens, scale
         dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
         self.seq_lens, self.group_begin, self.prefix_lens = dev(self.lens), dev(begin if groups else [0]), dev(plens if groups else [0])
         self.out = torch.full_like(self.q, float("nan"))
@@ -79,6 +79,12 @@ class Problem:
             shared = dict(page_table=self.ptable, max_pages=pper)
         else:
             self.k_cache, self.v_cache = self.k_own, self.v_own
+            if own_strided:          # [sequences, Hkv, tokens, d + a pad]
+                wide = [torch.zeros(n, Hkv, cap, d + 16, dtype=self.k_own.dtype, device="cuda") for _ in range(2)]
+                for x, y in zip(wide, (self.k_own, self.v_own)):
+                    x[..., :d] = y.transpose(1, 2)
+                self.k_cache, self.v_cache = wide
+                more["kv_strides"] = (wide[0].stride(0), wide[0].stride(2), wide[0].stride(1))
             if groups:
                 kp, vp = torch.stack(self.k_pre), torch.stack(self.v_pre)
                 if strided:      # [groups, Hkv, tokens, d + a pad]
@@ -90,17 +96,20 @@ class Problem:
                 shared.update(k_prefix=kp, v_prefix=vp)
         self.config = B.make_prefix_config("bf16", max_batch or n, L, Hq, Hkv, d, cap, w if L > 1 else 0, max_prefix_len=pcap,
                                            max_groups=max_groups or max(groups, 1), page_size=page, kv_dtype=kv, q_len=q_len, loop_offset=offsets,
-                                           kernel_path=kernel_path)
+                                           kernel_path=kernel_path, sm_scale=scale)
         self.args = B.make_args(n, self.q, self.k_cache, self.v_cache, self.seq_lens, self.out, k_win=self.k_win, v_win=self.v_win,
                                 gate_logits=self.gate, k_scale=self.k_scale, v_scale=self.v_scale, **more)
         self.shared = B.make_prefix_args(groups, self.group_begin, self.prefix_lens, **shared)
+        if win_lens is not None:
+            self.kept_win = dev(win_lens)
+            self.args.win_lens = self.kept_win.data_ptr()
         self.more, self.shared_more = more, shared
 
     def expect(self, lens=None, plens=None, begin=None):
         v = self.values
         pre = v["pre"] if plens is None else [(a[:p], c[:p]) for (a, c), p in zip(v["pre"], plens)]
-        return oracle_prefix.attend(self.q, pre, begin or self.begin, v["k_own"], v["v_own"], lens or self.lens, self.d ** -0.5, self.offsets, self.w,
-                                    v["k_win"], v["v_win"], None, self.gate)
+        return oracle_prefix.attend(self.q, pre, begin or self.begin, v["k_own"], v["v_own"], lens or self.lens, self.scale or self.d ** -0.5, self.offsets, self.w,
+                                    v["k_win"], v["v_win"], self.win_lens, self.gate)
 
     def run(self, handle=None, stream=0):
         own = handle is None

@@ -37,6 +37,15 @@ CASES = [
     dict(own=[4] * 130, plens=[64] * 65, begin=list(range(0, 131, 2))),              # many short groups: pieces of one key tile
     dict(own=[2] * 12, plens=[130] * 12, begin=list(range(13)), Hq=32, Hkv=8),
     dict(own=[8, 9], plens=[200], begin=[0, 2], offsets=[2, 5], L=2),
+    dict(own=[8, 9, 10], plens=[200], begin=[0, 3], L=3, w=9, win_lens=[[0, 9], [3, 1], [9, 0]]),
+    dict(own=[8, 9, 10], plens=[200], begin=[0, 3], scale=0.01),
+    dict(own=[8, 9, 40], plens=[200], begin=[0, 3], own_strided=True, L=2),
+    dict(own=[1000, 3, 700, 900] * 8, plens=[1000, 300], begin=[0, 20, 30], L=2, Hq=32, Hkv=8),      # multiprocessors divided between the passes
+    dict(own=[1000, 3, 700, 900] * 8, plens=[1000, 300], begin=[0, 20, 30], L=2, Hq=32, Hkv=8, kv="e4m3", page=64),
+    dict(own=[300] * 8, plens=[6000], begin=[0, 8], Hq=48, Hkv=8, d=64),                             # 6 heads: query rows without TMA
+    dict(own=[300] * 8, plens=[6000], begin=[0, 8], Hq=24, Hkv=8, kv="e4m3", L=2),
+    dict(own=[2] * 40, plens=[9000] * 40, begin=list(range(41)), Hq=2, Hkv=1),                       # a plan of many groups, several pieces a block
+    dict(own=[2] * 20, plens=[2500] * 20, begin=list(range(21)), Hq=32, Hkv=8),                      # more units than blocks
 ]
 
 
@@ -208,6 +217,35 @@ def test_two_handles_at_once_and_batches_below_the_largest():
     assert (a.out == 7).all()
     B.plt_prefix_attn_destroy(ha)
     B.plt_prefix_attn_destroy(hb)
+
+
+def test_window_lengths_out_of_range_are_clamped_and_flagged():
+    p = Problem(17, [8, 9, 10], [200], [0, 3], L=2, w=9, win_lens=[[-3], [10], [5]])
+    assert p.run() == B.PLT_DEV_WIN_LEN_CLAMPED
+    p.win_lens = [[0], [9], [5]]
+    p.hold()
+
+
+def test_runner_class():
+    from paper_2510_24824_b200.inputs import make_problem, shrunk_workload
+    from paper_2510_24824_b200.runner import DecodeAttn, DeviceProblem, PrefixAttn
+    # a prefix copied in front of every sequence's own keys is the plain step, within both's bounds
+    p = make_problem(shrunk_workload(2))
+    dp, P = DeviceProblem(p), 40
+    dp.k_cache[:, :P], dp.v_cache[:, :P] = dp.k_cache[:1, :P].clone(), dp.v_cache[:1, :P].clone()
+    with DecodeAttn(p) as op:
+        whole = op.run(dp).clone()
+    kp, vp = (x[:1, :P].contiguous() for x in (dp.k_cache, dp.v_cache))
+    dp.k_cache, dp.v_cache = (torch.cat([x[:, P:], x[:, :P]], dim=1).contiguous() for x in (dp.k_cache, dp.v_cache))
+    with PrefixAttn(p, P) as op:
+        out = op.run(dp, op.prefix_args(_dev([0, p.B]), _dev([P]), kp, vp))
+        assert op.check() == 0
+        with pytest.raises(ValueError):
+            op.prefix_args(_dev([0, p.B]), _dev([P]), kp.float(), vp)
+        with pytest.raises(ValueError):
+            op.prefix_args(_dev([0]), _dev([P]), kp, vp)
+    # each is within 2^-8 |ref| + 2^-8 sum p |v| of the true result; |v| stays below 6
+    assert float((out.float() - whole.float()).abs().max()) <= 2 * (2.0 ** -8 + 2.0 ** -8) * 6
 
 
 def test_refusals_of_a_call():
