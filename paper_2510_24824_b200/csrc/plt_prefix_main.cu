@@ -60,7 +60,7 @@ struct PPiece {
 };
 struct PWalk {
     int pos, hi, g;       // of the line; with chunks: piece pos = hi - 1, or none
-    __device__ __forceinline__ void fill(const PrefixParams& p, const PrefixPlan& plan, int u, int nm, PPiece& pc) {
+    __device__ __forceinline__ void fill(int u, int nm, PPiece& pc) {
         pc.h = u / nm;
         pc.m = u - pc.h * nm;
         pc.wide = pc.rows - pc.m * kPrefixRows > 128;
@@ -81,7 +81,7 @@ struct PWalk {
                 pc.t0 = tiles * k / n;
                 pc.t1 = tiles * (k + 1) / n;
                 pos = hi;
-                fill(p, plan, u, nm, pc);
+                fill(u, nm, pc);
                 return true;
             }
             const int per = tiles + kPrefixLead, o = pos - plan.line[g], u = o / per, v0 = o - u * per;
@@ -91,7 +91,7 @@ struct PWalk {
             pc.t1 = max(v1 - kPrefixLead, 0);
             if (pc.t1 <= pc.t0) continue;
             pc.slot = plan.unit[g] + u + (int)blockIdx.x;
-            fill(p, plan, u, nm, pc);
+            fill(u, nm, pc);
             return true;
         }
     }
@@ -282,7 +282,9 @@ __device__ __forceinline__ float p_max(const uint32_t (&r)[32], bool full, int l
 // 2^t of two numbers on the multiply-add units, which the special-function unit (four results a cycle for each scheduler) leaves
 // idle: t = n + f with n the nearest integer (Cody and Waite's split; n falls out of an addition of 1.5 * 2^23), 2^f on
 // [-1/2, 1/2] by the cubic of least largest relative error (found by Lawson's iteration; 2^-13.7, a fiftieth of what rounding a
-// probability to 8 bits costs), n added to the exponent. Below 2^-125 it stays there, which is 0 beside any probability of 1.
+// probability to 8 bits costs), n added to the exponent. At 2^-125 and below, what the cubic gives there is taken off where EXACT0, so
+// that a masked key weighs exactly 0 however large its value is (f16 probabilities lose so small a number anyway).
+template <bool EXACT0>
 __device__ __forceinline__ float2 exp2_by_fma(float2 t) {
     const float2 magic = make_float2(12582912.f, 12582912.f), minus = make_float2(-12582912.f, -12582912.f);
     t.x = fmaxf(t.x, -125.f);
@@ -293,8 +295,9 @@ __device__ __forceinline__ float2 exp2_by_fma(float2 t) {
     float2 e = __ffma2_rn(f, make_float2(0.05517167f, 0.05517167f), make_float2(0.24261113f, 0.24261113f));
     e = __ffma2_rn(f, e, make_float2(0.69326097f, 0.69326097f));
     e = __ffma2_rn(f, e, make_float2(0.99992806f, 0.99992806f));
-    return make_float2(__uint_as_float(__float_as_uint(e.x) + (__float_as_uint(z.x) << 23)),
-                       __uint_as_float(__float_as_uint(e.y) + (__float_as_uint(z.y) << 23)));
+    e = make_float2(__uint_as_float(__float_as_uint(e.x) + (__float_as_uint(z.x) << 23)), __uint_as_float(__float_as_uint(e.y) + (__float_as_uint(z.y) << 23)));
+    constexpr float least = -0.99992806f * 0x1p-125f;
+    return EXACT0 ? __fadd2_rn(e, make_float2(least, least)) : e;
 }
 
 // 32 scores -> probabilities, packed 16 bits wide, and their sum.
@@ -307,7 +310,7 @@ __device__ __forceinline__ void p_chunk(uint32_t (&r)[32], bool full, int lim, f
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
         const float2 t = __ffma2_rn(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), sc2, nm2);
-        const float2 pr = (i & 2) != 0 && (i & 4) != 0 ? exp2_by_fma(t) : make_float2(fast_exp2(t.x), fast_exp2(t.y));
+        const float2 pr = (i & 2) != 0 && (i & 4) != 0 ? exp2_by_fma<!FP8>(t) : make_float2(fast_exp2(t.x), fast_exp2(t.y));
         sum2 = __fadd2_rn(sum2, pr);
         pk[i / 2] = FP8 ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);
     }
@@ -407,7 +410,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         uint8_t* const to = FP8 ? raw : ring;
         uint64_t* const full = bars + (FP8 ? C::RFULL : C::FULL);
         uint64_t* const empty = bars + (FP8 ? C::REMPTY : C::EMPTY);
-        const uint64_t keep = l2_evict_first_policy(), keep_q = keep;
+        const uint64_t keep = l2_evict_first_policy();
         const int per_tile = kPrefixTile / p.kbox;
         Ring<NRING> rg;
         uint32_t issued = 0, flags = 0, q_bars = 0;
@@ -435,7 +438,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                     ++s_ctl[3 + x];
                     const int token = plan.begin[pc.g] * p.L * p.Qn + (pc.m * kPrefixRows + (pc.wide ? x * 128 : 0)) / p.G;
 #pragma unroll
-                    for (int hf = 0; hf < HALVES; ++hf) tma_load_4d(q_smem + x * C::TILE + hf * HB, &tmQ, bar, hf * 64, pc.h * p.G, token, 0, keep_q);
+                    for (int hf = 0; hf < HALVES; ++hf) tma_load_4d(q_smem + x * C::TILE + hf * HB, &tmQ, bar, hf * 64, pc.h * p.G, token, 0, keep);
                 }
                 __syncwarp();
             }
@@ -683,7 +686,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 }
                 if (in) sees = max(0, min(pc.len, (int)min((int64_t)n, (int64_t)pc.len + p.max_seq_len) - p.delta[lq / p.Qn] - (p.Qn - 1 - lq % p.Qn)));
             }
-            const float scale = FP8 ? p.scale_log2 * p.k_scale[pc.h] : p.scale_log2;
+            const float scale = FP8 ? fmaxf(p.scale_log2 * p.k_scale[pc.h], 1e-30f) : p.scale_log2;     // above 0: -inf has to stay that
             float mref = kSeqNoMax, sum = 0.f;
             for (int i = 0; i < mine; ++i) {
                 ok = seq_wait(&bars[C::SFULL + x], s_parity, abort_flag);

@@ -226,6 +226,24 @@ def test_window_lengths_out_of_range_are_clamped_and_flagged():
     p.hold()
 
 
+def test_large_values_behind_a_row_s_last_key_weigh_nothing():
+    """Finite values of 2^126 in the part of the prefix that no row sees: not a trace of them in the output."""
+    p = Problem(18, [0, 0], [300], [0, 2], lens=[200, 131])
+    p.shared_more["v_prefix"][:, 200:300] = 2.0 ** 126
+    assert p.run() == 0
+    p.hold()
+
+
+def test_a_head_whose_codes_have_scale_zero():
+    """Keys of scale 0 are all alike to every query: the mean of the values that a row sees."""
+    p = Problem(19, [0, 0, 0], [200], [0, 3], kv="e4m3", lens=[150, 199, 200])
+    p.k_scale[0] = 0.0
+    for k, _ in p.values["pre"]:
+        k[:, 0] = 0
+    assert p.run() == 0
+    p.hold()
+
+
 def test_runner_class():
     from paper_2510_24824_b200.inputs import make_problem, shrunk_workload
     from paper_2510_24824_b200.runner import DecodeAttn, DeviceProblem, PrefixAttn
