@@ -15,7 +15,7 @@
  * were certain: q_j is 1 at x_j and 0 elsewhere.  Products, differences and sums are held in 64 bits; the order of the sums
  * depends on nothing but the sizes and the tensors' alignment, so results repeat bit for bit.
  *
- * Entries of w that are NaN, infinite or not above 0 count as 0.  Where rounding leaves no v (or r is NaN or not below 1), the
+ * Entries of w that are NaN, not above 0, or infinite as fp32 numbers count as 0.  Where rounding leaves no v (or r is NaN or not below 1), the
  * last v with a weight is taken; a row without any weight gives token -1 and PLT_DEV_NO_PROBABILITY.  A draft outside
  * [0, vocab) is refused and flagged with PLT_DEV_TOKEN_OUT_OF_RANGE.
  *
@@ -50,7 +50,7 @@ typedef struct {
 } plt_draft_verify_config;
 
 /* Per call.  struct_size = sizeof(plt_draft_verify_args).  Probabilities need the alignment of their type; rows and sequences
- * may lie any number of elements apart (the vocabulary itself is dense). */
+ * may lie any number of elements apart, `vocab` at least (the vocabulary itself is dense). */
 typedef struct {
     uint32_t struct_size;
     int32_t batch;                  /* B, 0 <= B <= max_batch */

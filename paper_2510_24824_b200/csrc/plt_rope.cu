@@ -773,7 +773,7 @@ PLT_API plt_status plt_rope_seq(plt_rope_t h, const plt_rope_seq_args* a, void* 
     p.q_gain = a->q_gain; p.k_gain = a->k_gain;
     p.seq_lens = a->seq_lens; p.start = a->start; p.prefix_lens = a->prefix_lens;
     p.T = a->rows;
-    const dim3 grid((unsigned)((a->rows + kSeqTokens - 1) / kSeqTokens), (unsigned)(a->batch * c.L));
+    const dim3 grid((unsigned)(((int64_t)a->rows + kSeqTokens - 1) / kSeqTokens), (unsigned)(a->batch * c.L));
     return launch(h, true, p, grid, (cudaStream_t)cuda_stream);
 }
 

@@ -278,6 +278,52 @@ def test_lengths_and_pages_out_of_range():
     assert torch.equal(c.v_cache[c.table[0].long()].flatten(0, 1), v[0, 0, :32]) and (c.v_cache[c.table[2].long()] == 0).all()
 
 
+def test_replayed_steps_on_other_streams_and_two_handles():
+    """A captured step replayed with other lengths and rows in the same buffers gives what a call does; two handles whose calls
+    run on two streams do not meet."""
+    dev = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    cases = [Case(seed=8 + i, L=2, w=6, layout=layout) for i, layout in enumerate(("half", "interleaved"))]
+    new = [[(c.rand(3, 2, 1, h, c.d)).to(c.act) for h in (c.Hq, c.Hkv, c.Hkv)] for c in cases for _ in range(4)]
+    lens = [dev(1, 9, 30), dev(2, 10, 31), dev(64, 1, 2), dev(0, 33, 17)]
+
+    def state(c):
+        return [x.clone() for x in (c.k_cache, c.v_cache, c.k_win, c.v_win)]
+
+    def call(c, rows, n, to, out, stream=0):
+        B.plt_rope_step(c.op, B.make_rope_step_args(3, *rows, out, to[0], to[1], n, q_gain=c.q_gain, k_gain=c.k_gain, k_win=to[2], v_win=to[3]), stream)
+    want = []
+    for i, c in enumerate(cases):
+        to, outs = state(c), []
+        for s in range(4):
+            outs.append(torch.empty_like(new[0][0]))
+            call(c, new[4 * i + s], lens[s], to, outs[-1])
+        want.append((to, outs))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for i, c in enumerate(cases):       # one captured, one called
+        c.to, c.out, c.rows, c.n = state(c), torch.empty_like(new[0][0]), [x.clone() for x in new[4 * i]], lens[0].clone()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        call(cases[0], cases[0].rows, cases[0].n, cases[0].to, cases[0].out, torch.cuda.current_stream().cuda_stream)
+    got = [[], []]
+    for s in range(4):
+        for i, c in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                for x, y in zip(c.rows, new[4 * i + s]):
+                    x.copy_(y)
+                c.n.copy_(lens[s])
+                if i == 0:
+                    graph.replay()
+                else:
+                    call(c, c.rows, c.n, c.to, c.out, streams[i].cuda_stream)
+                got[i].append(c.out.clone())
+    torch.cuda.synchronize()
+    for i, c in enumerate(cases):
+        assert B.plt_rope_check(c.op) == 0
+        assert all(torch.equal(a, b) for a, b in zip(got[i], want[i][1])) and all(torch.equal(a, b) for a, b in zip(c.to, want[i][0]))
+
+
 def test_refusals_of_a_call():
     c = Case(seed=6, L=2)
     q, k, v = ((c.rand(3, 2, 1, h, c.d)).to(c.act) for h in (c.Hq, c.Hkv, c.Hkv))
