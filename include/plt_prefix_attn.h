@@ -82,9 +82,10 @@ plt_status plt_prefix_attn_create(const plt_prefix_attn_config* config, plt_pref
 /* Device bytes plt_prefix_attn_create would allocate (as plt_decode_attn_workspace_bytes). */
 plt_status plt_prefix_attn_workspace_bytes(const plt_prefix_attn_config* config, size_t* out_bytes);
 
-/* Enqueues one decode step on `cuda_stream`: a small plan kernel, the kernel over the prefixes (tcgen05.mma with the queries of a
- * whole group as its rows), the split-KV kernel over the own caches and windows, and the merge.  seq_lens, win_lens and gate_logits are read under
- * the terms that plt_decode_attn_run states for the kernels after the call; the kernels before it may write anything. */
+/* Enqueues one decode step on `cuda_stream`: the kernel over the prefixes (tcgen05.mma with the queries of a whole group as its
+ * rows), the split-KV kernel over the own caches and windows, which runs beside it, and the merge; before them a small plan kernel
+ * where there are more than 31 groups, or none.  seq_lens, win_lens and gate_logits are read under the terms that
+ * plt_decode_attn_run states for the kernels after the call; the kernels before it may write anything. */
 plt_status plt_prefix_attn_run(plt_prefix_attn_t handle, const plt_decode_attn_args* args, const plt_prefix_args* prefix,
                                void* cuda_stream);
 

@@ -1,5 +1,5 @@
-// C ABI of the decode step with shared prefixes. The own caches and windows go through the decode step's kernels on the lengths
-// that the plan kernel leaves; the prefixes have a kernel of their own (plt_prefix_main.cu), and plt_prefix_merge.cu joins both.
+// C ABI of the decode step with shared prefixes. The prefixes have a kernel of their own (plt_prefix_main.cu), which leaves the plan;
+// the own caches and windows go through the decode step's kernels on the lengths in it, and plt_prefix_merge.cu joins both.
 // Here: argument checks, the workspace and the tensor maps.
 #include "../../include/plt_prefix_attn.h"
 

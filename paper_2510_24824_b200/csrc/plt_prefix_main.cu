@@ -28,7 +28,7 @@
 namespace plt {
 namespace {
 
-constexpr int kNearGroups = 31;      // plans of up to this many groups are made by a warp, in every block by itself
+constexpr int kNearGroups = 31;      // plans of up to this many groups are made by a warp of every block, without a kernel before
 
 template <int D, bool FP8>
 struct PCfg {
@@ -142,8 +142,12 @@ __device__ __forceinline__ int warp_scan(int x, int lane) {     // inclusive
 
 // The plan of up to kNearGroups groups, by one warp: lane g is group g. Everything but the sequences' lengths goes to `to`.
 __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const PrefixPlan& to, int lane, uint32_t& flags) {
-    const int given = lane <= p.groups && p.groups > 0 ? p.group_begin[lane] : 0;
+    const int given = lane <= p.groups ? p.group_begin[lane] : 0;
     int len = lane < p.groups ? p.prefix_lens[lane] : 0;
+    int64_t tokens = 0;
+    if (p.own_per_sm > 0)
+#pragma unroll 4
+        for (int b = lane; b < p.B; b += 32) tokens += max(p.seq_lens[b], 0);
     if (len < 0 || len > p.max_prefix_len) {
         flags |= kDevGroupClamped;
         len = len < 0 ? 0 : p.max_prefix_len;
@@ -164,46 +168,45 @@ __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const Prefix
     const int positions = units * (tiles + kPrefixLead);
     const int unit = warp_scan(units, lane), line = warp_scan(positions, lane);
     const int all_units = __shfl_sync(0xffffffffu, unit, 31), all = __shfl_sync(0xffffffffu, line, 31) - all_units * kPrefixLead;
-    // How many blocks take part. What both passes take is estimated (in whole numbers: every block and the merge have to come to the
-    // same plan) for sixteen ways of dividing the multiprocessors, a lane each; none for the own caches means one pass behind the
+    // How many blocks take part. What both passes take is estimated for sixteen ways of dividing the multiprocessors, a lane each (in
+    // every block by the same instructions, so that all come to the same plan); none for the own caches means one pass behind the
     // other.
     int blocks = p.blocks, own_blocks = 0x7fffffff;
     if (p.own_per_sm > 0 && all_units > 0) {
         const bool wide = (rows - 1) % kPrefixRows >= 128;      // of a group's units all but the last are; that one may have half the work
         const int last = tiles > 0 && !wide ? p.Hkv * (tiles / 2) : 0;
-        const int work = __shfl_sync(0xffffffffu, warp_scan(units * tiles - last, lane), 31);
-        int64_t tokens = 0;
-        for (int b = lane; b < p.B; b += 32) tokens += max(p.seq_lens[b], 0);
+        const int work = __reduce_add_sync(0xffffffffu, units * tiles - last);
         tokens -= (int64_t)(lane < p.groups ? next - begin : 0) * len;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) tokens += __shfl_xor_sync(0xffffffffu, tokens, o);
-        const int64_t bytes = (max(tokens, (int64_t)0) + (int64_t)p.B * (p.L - 1) * p.w) * p.token_bytes;
-        const int left = p.blocks * (lane & 15) / 16, mine = p.blocks - left;
-        const int64_t prefix_ns = (int64_t)((work + mine - 1) / mine) * p.tile_ns;
-        const int n_own = left > 0 ? left : p.blocks;
-        const int64_t own_ns = kOwnStartNs + max(bytes / min(n_own * p.own_rate, kMemoryRate), (int64_t)p.own_items * kItemNs / (n_own * p.own_per_sm));
+        const float held = (float)__reduce_add_sync(0xffffffffu, (int)(tokens >> 24)) * 16777216.f + (float)__reduce_add_sync(0xffffffffu, (int)(tokens & 0xffffff));
+        const float bytes = (fmaxf(held, 0.f) + (float)(p.B * (p.L - 1)) * (float)p.w) * (float)p.token_bytes;
+        const int left = p.blocks * (lane & 15) / 16, mine = p.blocks - left, n_own = left > 0 ? left : p.blocks;
+        const float prefix_ns = (float)((work + mine - 1) / mine) * (float)p.tile_ns;
+        const float own_ns = (float)kOwnStartNs + fmaxf(__fdividef(bytes, (float)min(n_own * p.own_rate, kMemoryRate)),
+                                                        __fdividef((float)p.own_items * (float)kItemNs, (float)(n_own * p.own_per_sm)));
         // side by side the longer one counts, and the shorter one a little: it takes its share of memory and of the L2
-        const int64_t ns = left > 0 ? max(prefix_ns, own_ns) + min(prefix_ns, own_ns) / 8 : prefix_ns + own_ns + kGapNs;
-        const uint32_t cost = (uint32_t)min(ns, (int64_t)0x7fffffff), best = __reduce_min_sync(0xffffffffu, cost);
+        const float ns = left > 0 ? fmaxf(prefix_ns, own_ns) + fminf(prefix_ns, own_ns) * 0.125f : prefix_ns + own_ns + (float)kGapNs;
+        const uint32_t cost = (uint32_t)fminf(ns, 4e9f), best = __reduce_min_sync(0xffffffffu, cost);
         const int way = __ffs(__ballot_sync(0xffffffffu, cost == best)) - 1;
         if (way > 0) {
             blocks = __shfl_sync(0xffffffffu, mine, way);
             own_blocks = (p.blocks - blocks) * p.own_per_sm;
         }
     }
-    // The shortest chunk that lets every piece have a block, tried in steps of an eighth from the average on; not more than a
-    // tenth and a tile above what the line's ranges hold.
+    // The shortest chunk that lets every piece have a block, tried in steps of an eighth from the average on, a lane each; not more
+    // than a tenth and a tile above what the line's ranges hold.
     int chunk = 0, piece = 0;
     if (all_units > 0 && all_units <= blocks) {
-        const int least = (all + blocks - 1) / blocks, step = (least + 7) / 8;
-        const int most = (all + all_units * kPrefixLead) / blocks * 11 / 10 + 1;
-        for (int s = least; s <= max(most, least); s += step) {
-            const int n = warp_scan(tiles > 0 ? units * ((tiles + s - 1) / s) : 0, lane);
-            if (__shfl_sync(0xffffffffu, n, 31) <= blocks) {
-                chunk = s;
-                piece = n;
-                break;
-            }
+        const int least = (all + blocks - 1) / blocks, step = (least + 7) / 8, s = least + lane * step;
+        const int most = max((all + all_units * kPrefixLead) / blocks * 11 / 10 + 1, least);
+        int n = 0;
+        for (int g = 0; g < p.groups; ++g) {
+            const int tg = __shfl_sync(0xffffffffu, tiles, g), ug = __shfl_sync(0xffffffffu, units, g);
+            n += tg > 0 ? ug * ((tg + s - 1) / s) : 0;
+        }
+        const uint32_t fits = __ballot_sync(0xffffffffu, s <= most && n <= blocks);
+        if (fits != 0) {
+            chunk = least + (__ffs(fits) - 1) * step;
+            piece = warp_scan(tiles > 0 ? units * ((tiles + chunk - 1) / chunk) : 0, lane);
         }
     }
     if (lane < p.groups) {
@@ -218,6 +221,49 @@ __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const Prefix
         to.chunk[0] = chunk;
         to.chunk[1] = blocks;
         to.chunk[2] = own_blocks;
+    }
+}
+
+// Leaves the plan `from` (in shared memory) where the kernels behind find it, with what each sequence holds itself. By `threads`
+// threads, whose groups and lengths all have been written.
+__device__ __forceinline__ void leave_plan(const PrefixParams& p, const PrefixPlan& from, int tid, int threads, uint32_t& flags) {
+    for (int g = tid; g <= p.groups; g += threads) {
+        p.plan.begin[g] = from.begin[g];
+        p.plan.line[g] = from.line[g];
+        p.plan.unit[g] = from.unit[g];
+        p.plan.piece[g] = from.piece[g];
+        if (g < p.groups) p.plan.len[g] = from.len[g];
+    }
+    if (tid < 3) p.plan.chunk[tid] = from.chunk[tid];
+    for (int b = tid; b < p.B; b += threads) {
+        // the group of sequence b, if any
+        int len = 0;
+        if (p.groups > 0 && b >= from.begin[0] && b < from.begin[p.groups]) {
+            int lo = 0, hi = p.groups;             // begin[lo] <= b < begin[hi]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (from.begin[mid] <= b) lo = mid; else hi = mid;
+            }
+            len = from.len[lo];
+        }
+        int n = p.seq_lens[b];
+        if (n < 0 || n > (int64_t)len + p.max_seq_len) {
+            flags |= kDevSeqLenClamped;
+            n = n < 0 ? 0 : len + p.max_seq_len;
+        }
+        p.plan.own_lens[b] = max(0, n - len);
+        for (int l = 1; l < p.L; ++l) {
+            const int cut = max(0, n - p.delta[l]);
+            int wl = min(cut, p.w);
+            if (p.win_lens != nullptr && cut > 0) {
+                wl = p.win_lens[b * (p.L - 1) + l - 1];
+                if (wl < 0 || wl > p.w) {
+                    flags |= kDevWinLenClamped;
+                    wl = wl < 0 ? 0 : p.w;
+                }
+            }
+            p.plan.win_lens[b * (p.L - 1) + l - 1] = wl;
+        }
     }
 }
 
@@ -369,10 +415,11 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         mbar_fence_init();
     }
     if (wid == 1) tmem_alloc((uint32_t*)&s_ctl[1], 512);
-    // What the kernels before the plan kernel wrote is there (the plan kernel is an ordinary launch, and this one starts behind
-    // its start); of the plan kernel itself only the plan of many groups is needed.
-    const bool near = p.groups <= kNearGroups;
+    // Few groups: this kernel is an ordinary launch, each block makes the plan for itself, and the last one leaves it for the kernels
+    // behind. Many: it starts behind the plan kernel's start and waits for its end.
+    const bool near = p.groups <= kNearGroups, leaves = near && blockIdx.x + 1 == gridDim.x;
     PrefixPlan plan = p.plan;
+    uint32_t reported = 0;
     if (near) {
         constexpr int W = kNearGroups + 1;
         plan.begin = s_plan;
@@ -381,10 +428,11 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         plan.unit = s_plan + 3 * W;
         plan.piece = s_plan + 4 * W;
         plan.chunk = s_plan + 5 * W;
-        uint32_t reported = 0;                // by the plan kernel
+        if (!leaves) grid_launch_dependents();
         if (wid == 2) plan_by_warp(p, plan, lane, reported);
     } else {
         grid_dependency_wait();
+        grid_launch_dependents();
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -392,11 +440,16 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     const uint32_t tmem_base = (uint32_t)s_ctl[1];
     // columns: S_A 0..127 (P_A over the first 16 of every 32, whose scores have been read by then), S_B 128..255, O_A from
     // 256, O_B from 384
-    if (wid == 3) {
-        // The kernel behind this one reads the plan's lengths, and writes what the step before read, without a wait of its own:
-        // it is let go once the plan kernel has ended.
-        grid_dependency_wait();
-        grid_launch_dependents();
+    if (leaves) {
+        // The kernel behind this one reads the plan without a wait of its own: it is let go once the plan has been written. (The
+        // warps of the softmax have nothing to do yet.)
+        if (wid >= 4 && wid < 20) {
+            leave_plan(p, plan, tid - 128, 512, reported);
+            __threadfence();
+            named_barrier_sync(9, 512);
+            if (tid == 128) grid_launch_dependents();
+        }
+        if (reported) atomicOr(p.status, reported);
     }
     PWalk walk = walk_of_block(p, plan);
     PPiece pc;
@@ -785,7 +838,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     }
 }
 
-// ---- the plan -------------------------------------------------------------------------------------------------------
+// ---- the plan of many groups, or of none ---------------------------------------------------------------------------------
 // One block: clamped groups and lengths, the line of their units, and what each sequence holds itself.
 constexpr int kPlanThreads = 512;
 
@@ -794,114 +847,74 @@ __global__ void __launch_bounds__(kPlanThreads) plt_prefix_plan(const __grid_con
     grid_launch_dependents();
     const int tid = threadIdx.x, lane = tid & 31;
     uint32_t flags = 0;
-    if (p.groups <= kNearGroups) {
-        PrefixPlan to = p.plan;
-        to.begin = s_begin;
-        to.len = s_len;
-        to.line = s_line;
-        to.unit = s_unit;
-        to.piece = s_piece;
-        to.chunk = s_chunk;
-        if (tid < 32) plan_by_warp(p, to, lane, flags);
-    } else {
-        for (int g = tid; g <= p.groups; g += kPlanThreads) s_begin[g] = p.group_begin[g];
-        for (int g = tid; g < p.groups; g += kPlanThreads) {
-            int n = p.prefix_lens[g];
-            if (n < 0 || n > p.max_prefix_len) {
-                flags |= kDevGroupClamped;
-                n = n < 0 ? 0 : p.max_prefix_len;
-            }
-            s_len[g] = n;
+    for (int g = tid; g <= p.groups && p.groups > 0; g += kPlanThreads) s_begin[g] = p.group_begin[g];
+    for (int g = tid; g < p.groups; g += kPlanThreads) {
+        int n = p.prefix_lens[g];
+        if (n < 0 || n > p.max_prefix_len) {
+            flags |= kDevGroupClamped;
+            n = n < 0 ? 0 : p.max_prefix_len;
         }
-        __syncthreads();
-        if (tid < 32) {
-            // first sequences: running maximum of what the caller gave, within [0, B]; then the line and the units
-            int last = 0, line = 0, unit = 0;
-            for (int g0 = 0; g0 <= p.groups; g0 += 32) {
-                const int g = g0 + lane;
-                const int given = g <= p.groups ? s_begin[g] : 0;
-                int v = min(max(given, 0), p.B);
+        s_len[g] = n;
+    }
+    if (tid == 0 && p.groups == 0) s_begin[0] = 0;
+    __syncthreads();
+    if (tid < 32) {
+        // first sequences: running maximum of what the caller gave, within [0, B]; then the line and the units
+        int last = 0, line = 0, unit = 0;
+        for (int g0 = 0; g0 <= p.groups; g0 += 32) {
+            const int g = g0 + lane;
+            const int given = g <= p.groups ? s_begin[g] : 0;
+            int v = min(max(given, 0), p.B);
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int y = __shfl_up_sync(0xffffffffu, v, o);
-                    if (lane >= o) v = max(v, y);
-                }
-                v = max(v, last);
-                last = __shfl_sync(0xffffffffu, v, 31);
-                if (g <= p.groups) {
-                    if (v != given) flags |= kDevGroupClamped;
-                    s_begin[g] = v;
-                }
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, v, o);
+                if (lane >= o) v = max(v, y);
             }
-            __syncwarp();
-            for (int g0 = 0; g0 < p.groups; g0 += 32) {
-                const int g = g0 + lane;
-                int units = 0, positions = 0;
-                if (g < p.groups) {
-                    const int rows = (s_begin[g + 1] - s_begin[g]) * p.R;
-                    if (rows == 0) s_len[g] = 0;
-                    const int tiles = (s_len[g] + kPrefixTile - 1) / kPrefixTile;
-                    units = tiles > 0 ? p.Hkv * ((rows + kPrefixRows - 1) / kPrefixRows) : 0;
-                    positions = units * (tiles + kPrefixLead);
-                }
-                const int u = warp_scan(units, lane), q = warp_scan(positions, lane);
-                if (g < p.groups) {
-                    s_unit[g] = unit + u - units;
-                    s_line[g] = line + q - positions;
-                    s_piece[g] = 0;
-                }
-                unit += __shfl_sync(0xffffffffu, u, 31);
-                line += __shfl_sync(0xffffffffu, q, 31);
+            v = max(v, last);
+            last = __shfl_sync(0xffffffffu, v, 31);
+            if (g <= p.groups) {
+                if (v != given) flags |= kDevGroupClamped;
+                s_begin[g] = v;
             }
-            if (lane == 0) {
-                s_unit[p.groups] = unit;
-                s_line[p.groups] = line;
-                s_piece[p.groups] = 0;
-                s_chunk[0] = 0;
-                s_chunk[1] = p.blocks;
-                s_chunk[2] = 0x7fffffff;
+        }
+        __syncwarp();
+        for (int g0 = 0; g0 < p.groups; g0 += 32) {
+            const int g = g0 + lane;
+            int units = 0, positions = 0;
+            if (g < p.groups) {
+                const int rows = (s_begin[g + 1] - s_begin[g]) * p.R;
+                if (rows == 0) s_len[g] = 0;
+                const int tiles = (s_len[g] + kPrefixTile - 1) / kPrefixTile;
+                units = tiles > 0 ? p.Hkv * ((rows + kPrefixRows - 1) / kPrefixRows) : 0;
+                positions = units * (tiles + kPrefixLead);
             }
+            const int u = warp_scan(units, lane), q = warp_scan(positions, lane);
+            if (g < p.groups) {
+                s_unit[g] = unit + u - units;
+                s_line[g] = line + q - positions;
+                s_piece[g] = 0;
+            }
+            unit += __shfl_sync(0xffffffffu, u, 31);
+            line += __shfl_sync(0xffffffffu, q, 31);
+        }
+        if (lane == 0) {
+            s_unit[p.groups] = unit;
+            s_line[p.groups] = line;
+            s_piece[p.groups] = 0;
+            s_chunk[0] = 0;
+            s_chunk[1] = p.blocks;
+            s_chunk[2] = 0x7fffffff;
         }
     }
     __syncthreads();
-    for (int g = tid; g <= p.groups; g += kPlanThreads) {
-        p.plan.begin[g] = s_begin[g];
-        p.plan.line[g] = s_line[g];
-        p.plan.unit[g] = s_unit[g];
-        p.plan.piece[g] = s_piece[g];
-        if (g < p.groups) p.plan.len[g] = s_len[g];
-    }
-    if (tid < 3) p.plan.chunk[tid] = s_chunk[tid];
-    for (int b = tid; b < p.B; b += kPlanThreads) {
-        // the group of sequence b, if any
-        int len = 0;
-        if (p.groups > 0 && b >= s_begin[0] && b < s_begin[p.groups]) {
-            int lo = 0, hi = p.groups;             // begin[lo] <= b < begin[hi]
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (s_begin[mid] <= b) lo = mid; else hi = mid;
-            }
-            len = s_len[lo];
-        }
-        int n = p.seq_lens[b];
-        if (n < 0 || n > (int64_t)len + p.max_seq_len) {
-            flags |= kDevSeqLenClamped;
-            n = n < 0 ? 0 : len + p.max_seq_len;
-        }
-        p.plan.own_lens[b] = max(0, n - len);
-        for (int l = 1; l < p.L; ++l) {
-            const int cut = max(0, n - p.delta[l]);
-            int wl = min(cut, p.w);
-            if (p.win_lens != nullptr && cut > 0) {
-                wl = p.win_lens[b * (p.L - 1) + l - 1];
-                if (wl < 0 || wl > p.w) {
-                    flags |= kDevWinLenClamped;
-                    wl = wl < 0 ? 0 : p.w;
-                }
-            }
-            p.plan.win_lens[b * (p.L - 1) + l - 1] = wl;
-        }
-    }
+    PrefixPlan from = p.plan;
+    from.begin = s_begin;
+    from.len = s_len;
+    from.line = s_line;
+    from.unit = s_unit;
+    from.piece = s_piece;
+    from.chunk = s_chunk;
+    leave_plan(p, from, tid, kPlanThreads, flags);
     if (flags) atomicOr(p.status, flags);
 }
 
@@ -916,7 +929,7 @@ cudaError_t launch_one(const CUtensorMap maps[3], const PrefixParams& pp, cudaSt
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = pp.groups <= kNearGroups ? 0 : 1;
     return cudaLaunchKernelEx(&cfg, plt_prefix_main<D, FP8>, maps[0], maps[1], maps[2], pp);
 }
 
@@ -930,6 +943,7 @@ cudaError_t prefix_prepare(int d, bool fp8) {
 }
 
 cudaError_t launch_prefix_plan(const PrefixParams& pp, cudaStream_t stream) {
+    if (pp.groups > 0 && pp.groups <= kNearGroups) return cudaSuccess;       // the prefix kernel makes it
     plt_prefix_plan<<<1, kPlanThreads, 0, stream>>>(pp);
     return cudaGetLastError();
 }
