@@ -9,14 +9,19 @@
 // with an online softmax whose reference maximum is moved only when a score outruns it by more than a few powers of two. A unit
 // is two such tiles of 128 rows, A and B, of one KV head. Where a unit has more than 128 rows, both tiles take every key tile, so
 // that each K/V tile in shared memory serves 256 rows; where it has fewer, A and B are the same rows and take the key tiles in
-// turn, so that one tile's products run beside the other's softmax either way. Blocks are persistent: each takes an equal range
-// of a line on which the units' key tiles lie one behind the other, and leaves unnormalised partials for the merge.
+// turn. Blocks are persistent: each takes an equal range of a line on which the units' key tiles lie one behind the other, and
+// leaves unnormalised partials for the merge.
 //
-// Warp roles: warp 0 loads K and V tiles by TMA into a ring (pages: their ids one tile ahead); warp 1 issues the products and
-// owns the tensor memory; warps 2, 3, 20 and 21 turn E4M3 codes into f16 (exact) in a second ring; warps 4-11 and
-// 12-19 are the softmax of A and of B, load their query rows and store the partials. Two threads share a row, half the keys of
-// a tile each: they vote, warp by warp, on whether the reference has to move. A partial lies as [d / 4][128 rows][4], so that a
-// warp's store is 512 consecutive bytes.
+// A tile's scores come in two halves of 64 keys, each with tensor memory and barriers of its own: while the warps work on one, the
+// products of the other (P . V of these keys, then the next key tile's scores) run. With whole tiles a tile's softmax and its
+// products took turns, 4600 cycles for a wide key tile of which the products alone are 2050; halves make the scores' products dearer
+// (64 columns take 49 cycles for 16 elements of depth, 128 take 64: the rows of Q are read from shared memory for each) and the whole
+// shorter: 128 sequences behind 32768 tokens 154 -> 144 us. A and B have an issuing warp each, since the issue of a half costs about
+// as much in waits and commits as its products take.
+//
+// Warp roles: warp 0 loads K and V tiles by TMA into a ring (pages: their ids one tile ahead); warps 1 and 3 issue the products, warp
+// 1 owns the tensor memory; warp 2 makes the plan; warps 2, 20, 21 and 22 turn E4M3 codes into f16 (exact) in a second ring; warps
+// 4-11 and 12-19 are the softmax of A and of B, load their query rows and store the partials. A partial lies as [d / 4][128 rows][4].
 //
 // bf16 probabilities carry 8 bits, f16 ones (E4M3 caches) 11; their sum is taken before that rounding, in fp32.
 // Every wait is bounded and reports through the status word.
@@ -37,14 +42,15 @@ struct PCfg {
     static constexpr int RAW = FP8 ? 4 : 0;                       // tiles of codes
     static constexpr int RAW_TILE = kPrefixTile * D;
     // mbarriers
+    // (S, P and PV: of tile x and half h at 2 x + h)
     static constexpr int QFULL = 0, QRAW = 2, FULL = 4, EMPTY = FULL + RING, RFULL = EMPTY + RING, REMPTY = RFULL + RAW, SFULL = REMPTY + RAW,
-                         PFULL = SFULL + 2, ODONE = PFULL + 2, COUNT = ODONE + 2;
-    // tiles, barriers, control words, a word for each row (what the threads of a row tell each other), the plan
-    static constexpr size_t SMEM = 1024 + 2 * TILE + (size_t)RING * TILE + (size_t)RAW * RAW_TILE + COUNT * 8 + 64 + 1024 + (5 * (kNearGroups + 1) + 4) * 4;
+                         PFULL = SFULL + 4, PVDONE = PFULL + 4, ODONE = PVDONE + 4, COUNT = ODONE + 2;
+    // tiles, barriers, control words, the plan
+    static constexpr size_t SMEM = 1024 + 2 * TILE + (size_t)RING * TILE + (size_t)RAW * RAW_TILE + COUNT * 8 + 64 + (5 * (kNearGroups + 1) + 4) * 4;
 };
 
 template <bool FP8>
-constexpr int kPThreads = FP8 ? 704 : 640;
+constexpr int kPThreads = FP8 ? 736 : 640;
 
 // Instruction descriptor: fp32 accumulate, A and B both bf16 or both f16, B majorness, N / 8, M / 16.
 __host__ __device__ constexpr uint32_t p_instr_desc(int N, int b_mn_major, bool f16) {
@@ -301,7 +307,11 @@ struct Ring {
     }
 };
 
-// ---- softmax on a thread's 64 scores of a row --------------------------------------------------------------------------
+// ---- softmax ----------------------------------------------------------------------------------------------------------
+// A warp takes 16 rows and the 64 keys of a half tile, four threads to a row, as the fragments of a tensor-memory load of 16 lanes lie:
+// a thread has rows r and r + 8 (r = lane / 4 of the 16) and of each 8 keys the two at 2 (lane % 4): scores 4 g + {0, 1} are row r's at
+// keys 8 g + 2 (lane % 4) + {0, 1}, 4 g + {2, 3} row r + 8's. A row's threads tell each other by shuffles; no warp waits for another.
+//
 // Powers of two above the reference that a score may reach before the reference moves. With f16 probabilities references lie 8
 // below the maximum, so that the small ones do not fall under f16's range: up to 2^14 stays far from its end.
 template <bool FP8>
@@ -309,20 +319,55 @@ constexpr float kAbove = FP8 ? 14.f : 8.f;
 template <bool FP8>
 constexpr float kBelow = FP8 ? 8.f : 0.f;
 
-// Largest of 32 scores, those before `lim` where not all count.
-__device__ __forceinline__ float p_max(const uint32_t (&r)[32], bool full, int lim) {
-    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    if (full) {
+// 64 columns of 16 lanes, as above.
+__device__ __forceinline__ void tmem_ld_rows16(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+        "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+          "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+// 32 packed columns of 16 lanes: words 2 g + {0, 1} are rows r's and r + 8's pair of column 4 g + lane % 4.
+__device__ __forceinline__ void tmem_st_pairs16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr), "r"(r[0]),
+                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+                 "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+// 16 columns of 16 lanes, to be scaled: row r's by f0, row r + 8's by f1.
+__device__ __forceinline__ void tmem_scale_rows16(uint32_t taddr, float f0, float f1) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
+    tmem_wait_ld();
 #pragma unroll
-        for (int i = 0; i < 32; i += 8)
+    for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * ((i & 2) != 0 ? f1 : f0));
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+
+// Scores behind a row's last key become -inf; lim0, lim1: keys from the thread's first one to the end of its two rows.
+__device__ __forceinline__ void p_mask(uint32_t (&r)[32], int lim0, int lim1) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) m[j] = fmaxf(fmaxf(m[j], __uint_as_float(r[i + 2 * j])), __uint_as_float(r[i + 2 * j + 1]));
-    } else {
+    for (int i = 0; i < 32; ++i)
+        if (8 * (i >> 2) + (i & 1) >= ((i & 2) != 0 ? lim1 : lim0)) r[i] = 0xff800000u;
+}
+// Largest score of row r (k = 0) or r + 8 (k = 2) in the whole row.
+template <int K>
+__device__ __forceinline__ float p_max(const uint32_t (&r)[32]) {
+    float m[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < lim) m[i & 3] = fmaxf(m[i & 3], __uint_as_float(r[i]));
-    }
-    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+    for (int g = 0; g < 8; ++g) m[g & 1] = fmaxf(fmaxf(m[g & 1], __uint_as_float(r[4 * g + K])), __uint_as_float(r[4 * g + K + 1]));
+    float y = fmaxf(m[0], m[1]);
+    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 1));
+    return fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 2));
 }
 
 // 2^t of two numbers on the multiply-add units, which the special-function unit (four results a cycle for each scheduler) leaves
@@ -346,34 +391,20 @@ __device__ __forceinline__ float2 exp2_by_fma(float2 t) {
     return EXACT0 ? __fadd2_rn(e, make_float2(least, least)) : e;
 }
 
-// 32 scores -> probabilities, packed 16 bits wide, and their sum.
+// Scores -> probabilities, packed 16 bits wide, and their sums.
 template <bool FP8>
-__device__ __forceinline__ void p_chunk(uint32_t (&r)[32], bool full, int lim, float2 sc2, float2 nm2, uint32_t (&pk)[16], float2& sum2) {
-    if (!full)
+__device__ __forceinline__ void p_half(const uint32_t (&r)[32], float scale, float m0, float m1, uint32_t (&pk)[16], float2& sum0, float2& sum1) {
+    const float2 sc2 = make_float2(scale, scale), nm0 = make_float2(-m0, -m0), nm1 = make_float2(-m1, -m1);
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i >= lim) r[i] = 0xff800000u;              // -inf
+    for (int g = 0; g < 8; ++g)
 #pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-        const float2 t = __ffma2_rn(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), sc2, nm2);
-        const float2 pr = (i & 2) != 0 && (i & 4) != 0 ? exp2_by_fma<!FP8>(t) : make_float2(fast_exp2(t.x), fast_exp2(t.y));
-        sum2 = __fadd2_rn(sum2, pr);
-        pk[i / 2] = FP8 ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);
-    }
-}
-// Multiplies N columns of this thread's row of O by f; rolled, since a thread has 32 scores in registers meanwhile.
-template <int N>
-__device__ __forceinline__ void p_scale_o(uint32_t tO, float f) {
-#pragma unroll 1
-    for (int c = 0; c < N / 16; ++c) {
-        uint32_t r[16];
-        tmem_ld16(tO + c * 16, r);
-        tmem_wait_ld();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
-        tmem_st16(tO + c * 16, r);
-    }
-    tmem_wait_st();
+        for (int k = 0; k < 2; ++k) {
+            const float2 t = __ffma2_rn(make_float2(__uint_as_float(r[4 * g + 2 * k]), __uint_as_float(r[4 * g + 2 * k + 1])), sc2, k == 0 ? nm0 : nm1);
+            const float2 pr = (g & 1) != 0 && k == 1 ? exp2_by_fma<!FP8>(t) : make_float2(fast_exp2(t.x), fast_exp2(t.y));
+            float2& s = k == 0 ? sum0 : sum1;
+            s = __fadd2_rn(s, pr);
+            pk[2 * g + k] = FP8 ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);
+        }
 }
 
 template <int D, bool FP8>
@@ -389,8 +420,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     uint8_t* raw = ring + (size_t)C::RING * C::TILE;               // [RAW][tile of codes]
     uint64_t* bars = (uint64_t*)(raw + (size_t)C::RAW * C::RAW_TILE);
     int32_t* s_ctl = (int32_t*)(bars + C::COUNT);                  // [0] abort flag, [1] tensor-memory base, [2] loads issued
-    float* s_row = (float*)(s_ctl + 16);                           // [2 tiles][128 rows]
-    int32_t* s_plan = (int32_t*)(s_row + 256);                     // begin, len, line, unit, piece: [kNearGroups + 1] each; chunk
+    int32_t* s_plan = s_ctl + 16;                                  // begin, len, line, unit, piece: [kNearGroups + 1] each; chunk
     volatile int* abort_flag = (volatile int*)s_ctl;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
 
@@ -399,7 +429,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         s_ctl[2] = s_ctl[3] = s_ctl[4] = 0;
         for (int s = 0; s < C::RING; ++s) {
             mbar_init(&bars[C::FULL + s], FP8 ? 4 : 1);
-            mbar_init(&bars[C::EMPTY + s], 1);
+            mbar_init(&bars[C::EMPTY + s], 2);
         }
         for (int s = 0; s < C::RAW; ++s) {
             mbar_init(&bars[C::RFULL + s], 1);
@@ -408,9 +438,12 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         for (int x = 0; x < 2; ++x) {
             mbar_init(&bars[C::QFULL + x], p.q_tma && !FP8 ? 1 : 8);
             mbar_init(&bars[C::QRAW + x], 1);
-            mbar_init(&bars[C::SFULL + x], 1);
-            mbar_init(&bars[C::PFULL + x], 8);
             mbar_init(&bars[C::ODONE + x], 1);
+        }
+        for (int s = 0; s < 4; ++s) {
+            mbar_init(&bars[C::SFULL + s], 1);
+            mbar_init(&bars[C::PFULL + s], 8);
+            mbar_init(&bars[C::PVDONE + s], 1);
         }
         mbar_fence_init();
     }
@@ -438,7 +471,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = (uint32_t)s_ctl[1];
-    // columns: S_A 0..127 (P_A over the first 16 of every 32, whose scores have been read by then), S_B 128..255, O_A from
+    // columns: S_A 0..127 in halves of 64 (its P over the first 32 of each, once the scores have been read), S_B 128..255, O_A from
     // 256, O_B from 384
     if (leaves) {
         // The kernel behind this one reads the plan without a wait of its own: it is let go once the plan has been written. (The
@@ -539,35 +572,29 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         }
         if (lane == 0) s_ctl[2] = (int32_t)issued;
         if (flags) atomicOr(p.status, flags);
-    } else if (wid == 1) {
-        // =========================== product issue (whole warp walks, one thread issues) =====================
-        constexpr uint32_t idesc_qk = p_instr_desc(128, 0, FP8), idesc_pv = p_instr_desc(D, 1, FP8);
+    } else if (wid == 1 || wid == 3) {
+        // =========================== product issue (whole warps walk, one thread issues) =====================
+        // A wide piece's tile A is warp 1's and its tile B warp 3's; a narrow piece is warp 1's.
+        constexpr uint32_t idesc_qk = p_instr_desc(64, 0, FP8), idesc_pv = p_instr_desc(D, 1, FP8);
         constexpr int HB = kPrefixTile * 128;
         const uint32_t q_a = smem_u32(q_smem), ring_a = smem_u32(ring), bars_a = smem_u32(bars);
         uint32_t base = 0;                    // ring tiles before this piece: K of its i-th key tile is base + 2 i, V the next
-        uint32_t q_parity[2] = {0, 0}, p_parity[2] = {0, 0};
+        uint32_t q_parity[2] = {0, 0}, p_parity[2] = {0, 0}, o_parity[2] = {0, 0};
         while (ok && walk.next(p, plan, pc)) {
             const int n = pc.t1 - pc.t0;
-            auto wait_tile = [&](uint32_t cnt) {
-                bool y = seq_wait(&bars[C::FULL + cnt % C::RING], (cnt / C::RING) & 1u, abort_flag);
+            auto wait_for = [&](int bar, uint32_t parity) {
+                const bool y = seq_wait(&bars[bar], parity, abort_flag);
                 ok = __all_sync(0xffffffffu, y);
             };
-            // tile x's query rows have been loaded (a tile without a key tile in this piece has none)
-            auto wait_q = [&](int x) {
-                ok = seq_wait(&bars[C::QFULL + x], q_parity[x], abort_flag);
-                ok = __all_sync(0xffffffffu, ok);
-                q_parity[x] ^= 1u;
-            };
-            // S_x = Q_x . K(i)^T. The K tile is free once the last tile that takes it has been issued. (The first tile of a wide
-            // piece has waited for K and V when the second comes.)
-            auto issue_s = [&](int i, int x) {
+            // S_x,h = Q_x . K(i)[64 h ..]^T. The K tile is free once the second half of the last tile that takes it has been issued
+            // (two arrivals: one of each tile, or both of the one).
+            auto issue_s = [&](int i, int x, int h) {
                 const uint32_t cnt = base + 2u * (uint32_t)i, slot = cnt % C::RING;
-                if (!pc.wide || x == 0) wait_tile(cnt);
+                if (h == 0) wait_for(C::FULL + slot, (cnt / C::RING) & 1u);
                 if (!ok) return;
                 tc_fence_after_sync();
-                const uint64_t k0 = uniform(seq_smem_desc(ring_a + slot * C::TILE, 16, 1024)), q0 = uniform(seq_smem_desc(q_a + (uint32_t)x * C::TILE, 16, 1024));
-                const uint32_t to = uniform(tmem_base + x * 128), free_bar = uniform(bars_a + 8u * (C::EMPTY + slot)), full_bar = uniform(bars_a + 8u * (C::SFULL + x));
-                const bool last_use = !pc.wide || x == 1;
+                const uint64_t k0 = uniform(seq_smem_desc(ring_a + slot * C::TILE + h * 8192, 16, 1024)), q0 = uniform(seq_smem_desc(q_a + (uint32_t)x * C::TILE, 16, 1024));
+                const uint32_t to = uniform(tmem_base + x * 128 + h * 64), free_bar = uniform(bars_a + 8u * (C::EMPTY + slot)), full_bar = uniform(bars_a + 8u * (C::SFULL + 2 * x + h));
                 if (one_thread()) {
 #pragma unroll
                     for (int kk = 0; kk < D / 16; ++kk) {
@@ -575,22 +602,23 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                         umma_bf16(to, q0 + off, k0 + off, idesc_qk, kk == 0 ? 0u : 1u);
                     }
                     commit_to(full_bar);
-                    if (last_use) commit_to(free_bar);
+                    if (h == 1) {
+                        commit_to(free_bar);
+                        if (!pc.wide) commit_to(free_bar);
+                    }
                 }
                 __syncwarp();
             };
-            auto finish = [&](int i, int x, bool last) {       // O_x += P_x . V(i)
-                ok = seq_wait(&bars[C::PFULL + x], p_parity[x], abort_flag);
-                ok = __all_sync(0xffffffffu, ok);
-                p_parity[x] ^= 1u;
+            auto finish = [&](int i, int x, int h, bool first, bool last) {       // O_x += P_x,h . V(i)[64 h ..]
+                wait_for(C::PFULL + 2 * x + h, p_parity[x]);
                 if (!ok) return;
                 const uint32_t cnt = base + 2u * (uint32_t)i + 1u, slot = cnt % C::RING;
-                if (!pc.wide || x == 0) wait_tile(cnt);
+                if (h == 0) wait_for(C::FULL + slot, (cnt / C::RING) & 1u);
                 if (!ok) return;
                 // Rows of the V tile behind the prefix may hold anything: zero them, so that a probability of 0 times garbage
-                // is 0. Done by the first tile that uses it (E4M3: by the warps that convert).
+                // is 0. (Of a wide piece by both warps, each for its own products. E4M3: by the warps that convert.)
                 const int held = pc.len - (pc.t0 + i) * kPrefixTile;
-                if (!FP8 && held < kPrefixTile && (!pc.wide || x == 0)) {
+                if (!FP8 && held < kPrefixTile && h == 0) {
                     uint8_t* v = ring + (size_t)slot * C::TILE;
                     for (int idx = lane; idx < (kPrefixTile - held) * (D / 8); idx += 32) {
                         const int row = held + idx / (D / 8), ch = idx % (D / 8);
@@ -600,47 +628,68 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                     __syncwarp();
                 }
                 tc_fence_after_sync();
-                const uint64_t v0 = uniform(seq_smem_desc(ring_a + slot * C::TILE, HB, 1024));
-                const uint32_t from = uniform(tmem_base + x * 128), to = from + 256u, more = uniform(i > (pc.wide ? 0 : x) ? 1u : 0u);
-                const uint32_t free_bar = uniform(bars_a + 8u * (C::EMPTY + slot)), done_bar = uniform(bars_a + 8u * (C::ODONE + x));
-                const bool last_use = !pc.wide || x == 1;
+                const uint64_t v0 = uniform(seq_smem_desc(ring_a + slot * C::TILE + h * 8192, HB, 1024));
+                const uint32_t from = uniform(tmem_base + x * 128 + h * 64), to = uniform(tmem_base + x * 128 + 256), more = uniform(first ? 0u : 1u);
+                const uint32_t free_bar = uniform(bars_a + 8u * (C::EMPTY + slot)), done_bar = uniform(bars_a + 8u * (C::PVDONE + 2 * x + h)), all_bar = uniform(bars_a + 8u * (C::ODONE + x));
                 if (one_thread()) {
 #pragma unroll
-                    for (int kk = 0; kk < kPrefixTile / 16; ++kk)
-                        umma_bf16_ts(to, from + (kk >> 1) * 32 + (kk & 1) * 8, v0 + (uint64_t)(kk * 2048 >> 4), idesc_pv, kk > 0 ? 1u : more);
-                    if (last_use) commit_to(free_bar);
-                    if (last) commit_to(done_bar);
+                    for (int kk = 0; kk < 4; ++kk) umma_bf16_ts(to, from + kk * 8, v0 + (uint64_t)(kk * 2048 >> 4), idesc_pv, kk > 0 ? 1u : more);
+                    commit_to(done_bar);
+                    if (h == 1) {
+                        commit_to(free_bar);
+                        if (!pc.wide) commit_to(free_bar);
+                        if (last) commit_to(all_bar);
+                    }
                 }
                 __syncwarp();
+                if (h == 1) p_parity[x] ^= 1u;
             };
-            wait_q(0);
-            if (ok) issue_s(0, 0);
-            if (ok && (pc.wide || n > 1)) wait_q(1);
+            auto start = [&](int i, int x) {       // its query rows have been loaded (a tile without a key tile in this piece has none)
+                wait_for(C::QFULL + x, q_parity[x]);
+                if (ok) issue_s(i, x, 0);
+                if (ok) issue_s(i, x, 1);
+            };
+            // Where the ring is short, K two tiles on waits for the V tile that is about to be used: its scores come behind both halves.
+            auto step = [&](int i, int x, int by) {
+                const bool next = i + by < n;
+                finish(i, x, 0, i < by, false);
+                if (ok && next && (C::RING > 3 || by == 1)) issue_s(i + by, x, 0);
+                if (ok) finish(i, x, 1, false, !next);
+                if (ok && next && C::RING <= 3 && by == 2) issue_s(i + by, x, 0);
+                if (ok && next) issue_s(i + by, x, 1);
+            };
             if (pc.wide) {
-                if (ok) issue_s(0, 1);
-                for (int i = 0; i < n && ok; ++i)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        if (ok) finish(i, x, i + 1 == n);
-                        if (ok && i + 1 < n) issue_s(i + 1, x);
-                    }
+                const int x = wid >> 1;
+                start(0, x);
+                for (int i = 0; i < n && ok; ++i) step(i, x, 1);
+                if (n & 1) p_parity[x ^ 1] ^= 1u;
+            } else if (wid == 1) {
+                start(0, 0);
+                if (ok && n > 1) start(1, 1);
+                for (int i = 0; i < n && ok; ++i) step(i, i & 1, 2);
             } else {
-                if (ok && n > 1) issue_s(1, 1);
-                for (int i = 0; i < n && ok; ++i) {
-                    finish(i, i & 1, i + 2 >= n);
-                    if (ok && i + 2 < n) issue_s(i + 2, i & 1);
-                }
+                if (tiles_of(pc, 0) & 1) p_parity[0] ^= 1u;
+                if (tiles_of(pc, 1) & 1) p_parity[1] ^= 1u;
             }
+            q_parity[0] ^= 1u;
+            if (tiles_of(pc, 1) > 0) q_parity[1] ^= 1u;
             base += 2u * (uint32_t)n;
+            // Warp 3 does not see the tiles of a narrow piece land, and a barrier's parity says nothing about the phase before the last:
+            // it goes on behind the piece's last products.
+            for (int x = 0; wid == 3 && x < 2 && ok; ++x)
+                if (tiles_of(pc, x) > 0) {
+                    wait_for(C::ODONE + x, o_parity[x]);
+                    o_parity[x] ^= 1u;
+                }
         }
-    } else if (wid < 4 || wid >= 20) {
+    } else if (wid == 2 || wid >= 20) {
         // =========================== E4M3 codes to f16 =======================================================
         if constexpr (FP8) {
             constexpr int HB = kPrefixTile * 128;
             Ring<C::RAW> src;
             Ring<C::RING> dst;
             uint32_t done = 0;
-            const int ct = (wid < 4 ? wid - 2 : wid - 18) * 32 + lane;      // of 128
+            const int ct = (wid == 2 ? 0 : wid - 19) * 32 + lane;      // of 128
             while (ok && walk.next(p, plan, pc))
                 for (int t = pc.t0; t < pc.t1 && ok; ++t)
                     for (int which = 0; which < 2 && ok; ++which) {
@@ -688,25 +737,29 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     } else {
         // =========================== softmax, query rows and partials ======================================
         constexpr int HB = kPrefixTile * 128;
-        constexpr int PART = D / 2;                        // columns of O, and elements of the query row, that a thread takes
+        constexpr int PART = D / 2;                        // elements of a query row that a thread loads
         const int x = (wid - 4) >> 3, half = ((wid - 4) >> 2) & 1;
-        const int wq = wid & 3, row = wq * 32 + lane;      // lane quarter of tensor memory; row of the tile
-        const int pair = 1 + x * 4 + wq;                   // named barrier of the two warps that share rows
-        const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
-        const uint32_t tS = tmem_base + lane_off + x * 128 + half * 64, tO = tmem_base + lane_off + 256 + x * 128 + half * PART;
-        float* const told = s_row + x * 128 + row;
+        const int wq = wid & 3, row = wq * 32 + lane;      // lane quarter of tensor memory; row of the tile whose query it loads
+        const int row0 = wq * 32 + half * 16 + (lane >> 2);        // rows whose scores it has: this one and 8 on
+        const uint32_t lane_off = (uint32_t)(wq * 32 + half * 16) << 16;
+        const uint32_t tS = tmem_base + lane_off + x * 128, tO = tmem_base + lane_off + 256 + x * 128;
         uint32_t s_parity = 0, o_parity = 0, r_parity = 0;
         while (ok && walk.next(p, plan, pc)) {
-            // ---- this row's query, and how many tokens of the prefix it sees ------------------------------------
-            const int lr = pc.m * kPrefixRows + (pc.wide ? x * 128 : 0) + row;
+            // ---- a row's query, and how many tokens of the prefix the two rows see -----------------------------------
+            const int first_row = pc.m * kPrefixRows + (pc.wide ? x * 128 : 0);
             const int mine = tiles_of(pc, x), step = pc.wide ? 1 : 2;
-            int sees = 0;
+            auto sees_of = [&](int lr) {
+                if (lr >= pc.rows) return 0;
+                const int lq = lr % p.R / p.G, n = p.seq_lens[plan.begin[pc.g] + lr / p.R];
+                return max(0, min(pc.len, (int)min((int64_t)n, (int64_t)pc.len + p.max_seq_len) - p.delta[lq / p.Qn] - (p.Qn - 1 - lq % p.Qn)));
+            };
+            int sees0 = 0, sees1 = 0;
             if (mine > 0) {
                 uint8_t* q = q_smem + x * C::TILE;
-                const bool in = lr < pc.rows;
-                const int b = in ? plan.begin[pc.g] + lr / p.R : 0, r = in ? lr % p.R : 0, lq = r / p.G;
-                const int n = in ? p.seq_lens[b] : 0;
                 if (FP8 || !p.q_tma) {
+                    const int lr = first_row + row;
+                    const bool in = lr < pc.rows;
+                    const int b = in ? plan.begin[pc.g] + lr / p.R : 0, r = in ? lr % p.R : 0, lq = r / p.G;
                     uint4 v[PART / 8];
                     if (p.q_tma) {       // bf16 rows that TMA wrote become f16 in place
                         ok = seq_wait(&bars[C::QRAW + x], r_parity, abort_flag);
@@ -737,64 +790,71 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bars[C::QFULL + x]);
                 }
-                if (in) sees = max(0, min(pc.len, (int)min((int64_t)n, (int64_t)pc.len + p.max_seq_len) - p.delta[lq / p.Qn] - (p.Qn - 1 - lq % p.Qn)));
+                sees0 = sees_of(first_row + row0);
+                sees1 = sees_of(first_row + row0 + 8);
             }
             const float scale = FP8 ? fmaxf(p.scale_log2 * p.k_scale[pc.h], 1e-30f) : p.scale_log2;     // above 0: -inf has to stay that
-            float mref = kSeqNoMax, sum = 0.f;
+            float m0 = kSeqNoMax, m1 = kSeqNoMax;
+            float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
             for (int i = 0; i < mine; ++i) {
-                ok = seq_wait(&bars[C::SFULL + x], s_parity, abort_flag);
-                ok = __all_sync(0xffffffffu, ok);      // the tensor-memory accesses below are collective over the warp
-                s_parity ^= 1u;
-                if (!ok) break;
-                tc_fence_after_sync();
                 const int t = pc.t0 + (pc.wide ? 0 : x) + i * step;
-                const int lim = sees - t * kPrefixTile - half * 64;    // this thread's keys [0, lim) are visible to the row
-                const bool full = __all_sync(0xffffffffu, lim >= 64);
-                uint32_t r[32];
-                tmem_ld32(tS, r);
-                tmem_wait_ld();
-                float top = p_max(r, full, lim);
-                tmem_ld32(tS + 32, r);                     // stay in registers for their probabilities
-                tmem_wait_ld();
-                top = fmaxf(top, p_max(r, full, lim - 32)) * scale;
-                if (named_barrier_or(pair, 64, i == 0 || top > mref + kAbove<FP8>)) {
-                    // the row's maximum over both threads, and O against the new reference (every product into it has completed:
-                    // the commit behind S_FULL covers them)
-                    if (half == 1) *told = top;
-                    named_barrier_sync(pair, 64);
-                    const float m_new = half == 0 ? fmaxf(mref, fmaxf(top, *told) - kBelow<FP8>) : 0.f;
-                    if (half == 0) *told = m_new;
-                    named_barrier_sync(pair, 64);
-                    const float m = *told, alpha = fast_exp2(mref - m);
-                    mref = m;
-                    sum *= alpha;
-                    if (i > 0) p_scale_o<PART>(tO, alpha);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    ok = seq_wait(&bars[C::SFULL + 2 * x + h], s_parity, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);      // the tensor-memory accesses below are collective over the warp
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    uint32_t r[32];
+                    tmem_ld_rows16(tS + h * 64, r);
+                    const int key = t * kPrefixTile + h * 64, lim0 = sees0 - key, lim1 = sees1 - key;      // keys that the rows see
+                    const bool full = __all_sync(0xffffffffu, min(lim0, lim1) >= 64);
+                    tmem_wait_ld();
+                    if (!full) p_mask(r, lim0 - 2 * (lane & 3), lim1 - 2 * (lane & 3));
+                    const float top0 = p_max<0>(r) * scale, top1 = p_max<2>(r) * scale;
+                    const bool first = i == 0 && h == 0;
+                    if (__any_sync(0xffffffffu, first || top0 > m0 + kAbove<FP8> || top1 > m1 + kAbove<FP8>)) {
+                        const float n0 = fmaxf(m0, top0 - kBelow<FP8>), n1 = fmaxf(m1, top1 - kBelow<FP8>);
+                        const float f0 = fast_exp2(m0 - n0), f1 = fast_exp2(m1 - n1);
+                        m0 = n0;
+                        m1 = n1;
+                        sum0 = make_float2(sum0.x * f0, sum0.y * f0);
+                        sum1 = make_float2(sum1.x * f1, sum1.y * f1);
+                        if (!first) {
+                            // O against the new reference, once the product of the half before has completed. (The one before that
+                            // on the same barrier has: this warp has seen scores that were issued behind it.)
+                            ok = seq_wait(&bars[C::PVDONE + 2 * x + (h ^ 1)], s_parity ^ (uint32_t)(h ^ 1), abort_flag);
+                            ok = __all_sync(0xffffffffu, ok);
+                            if (!ok) break;
+                            tc_fence_after_sync();
+#pragma unroll 1
+                            for (int c = 0; c < D / 16; ++c) tmem_scale_rows16(tO + c * 16, f0, f1);
+                        }
+                    }
+                    uint32_t pk[16];
+                    p_half<FP8>(r, scale, m0, m1, pk, sum0, sum1);
+                    tmem_st_pairs16(tS + h * 64, pk);
+                    tmem_wait_st();
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars[C::PFULL + 2 * x + h]);
                 }
-                const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-mref, -mref);
-                float2 sum2 = make_float2(0.f, 0.f);
-                uint32_t pk[16];
-                p_chunk<FP8>(r, full, lim - 32, sc2, nm2, pk, sum2);
-                tmem_ld32(tS, r);
-                tmem_st16(tS + 32, pk);
-                tmem_wait_ld();
-                p_chunk<FP8>(r, full, lim, sc2, nm2, pk, sum2);
-                tmem_st16(tS, pk);
-                sum += sum2.x + sum2.y;
-                tmem_wait_st();
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars[C::PFULL + x]);
+                if (!ok) break;
+                s_parity ^= 1u;
             }
             if (!ok) break;
             // ---- the partial ---------------------------------------------------------------------------------------
             const int64_t slot = pc.slot;
-            if (half == 1) *told = sum;
-            named_barrier_sync(pair, 64);
-            if (half == 0) {
-                const bool saw = mine > 0 && mref > kSeqNoMax;
-                *(float2*)(p.ml + ((slot * 2 + x) * 128 + row) * 2) = make_float2(saw ? mref : -INFINITY, saw ? sum + *told : 0.f);
+            float s0 = sum0.x + sum0.y, s1 = sum1.x + sum1.y;
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) {
+                s0 += __shfl_xor_sync(0xffffffffu, s0, o);
+                s1 += __shfl_xor_sync(0xffffffffu, s1, o);
             }
-            named_barrier_sync(pair, 64);
+            if ((lane & 3) < 2) {
+                const float m = (lane & 1) != 0 ? m1 : m0;
+                const bool saw = mine > 0 && m > kSeqNoMax;
+                *(float2*)(p.ml + ((slot * 2 + x) * 128 + row0 + 8 * (lane & 1)) * 2) = make_float2(saw ? m : -INFINITY, !saw ? 0.f : (lane & 1) != 0 ? s1 : s0);
+            }
             if (mine > 0) {
                 ok = seq_wait(&bars[C::ODONE + x], o_parity, abort_flag);
                 ok = __all_sync(0xffffffffu, ok);
@@ -802,16 +862,17 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 if (!ok) break;
                 tc_fence_after_sync();
                 const float f = FP8 ? p.v_scale[pc.h] : 1.f;
-                float* out = p.acc + (slot * 2 + x) * (128 * D) + half * (PART / 4) * 512 + row * 4;
-#pragma unroll
-                for (int c = 0; c < PART / 32; ++c) {
+                float* out = p.acc + (slot * 2 + x) * (128 * D) + ((lane & 3) >> 1) * 512 + row0 * 4 + 2 * (lane & 1);
+#pragma unroll 1
+                for (int c = 0; c < D / 64; ++c) {
                     uint32_t r[32];
-                    tmem_ld32(tO + c * 32, r);
+                    tmem_ld_rows16(tO + c * 64, r);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        *(float4*)(out + (c * 8 + k) * 512) = make_float4(__uint_as_float(r[4 * k]) * f, __uint_as_float(r[4 * k + 1]) * f,
-                                                                          __uint_as_float(r[4 * k + 2]) * f, __uint_as_float(r[4 * k + 3]) * f);
+                    for (int g = 0; g < 8; ++g)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+                            *(float2*)(out + (c * 16 + g * 2) * 512 + 32 * k) = make_float2(__uint_as_float(r[4 * g + 2 * k]) * f, __uint_as_float(r[4 * g + 2 * k + 1]) * f);
                 }
             }
         }
