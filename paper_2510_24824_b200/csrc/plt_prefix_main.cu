@@ -359,13 +359,16 @@ __device__ __forceinline__ void p_mask(uint32_t (&r)[32], int lim0, int lim1) {
     for (int i = 0; i < 32; ++i)
         if (8 * (i >> 2) + (i & 1) >= ((i & 2) != 0 ? lim1 : lim0)) r[i] = 0xff800000u;
 }
-// Largest score of row r (k = 0) or r + 8 (k = 2) in the whole row.
+// Largest of a thread's scores of row r (K = 0) or r + 8 (K = 2).
 template <int K>
 __device__ __forceinline__ float p_max(const uint32_t (&r)[32]) {
     float m[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int g = 0; g < 8; ++g) m[g & 1] = fmaxf(fmaxf(m[g & 1], __uint_as_float(r[4 * g + K])), __uint_as_float(r[4 * g + K + 1]));
-    float y = fmaxf(m[0], m[1]);
+    return fmaxf(m[0], m[1]);
+}
+// Largest of a row's four threads.
+__device__ __forceinline__ float row_max(float y) {
     y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 1));
     return fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 2));
 }
@@ -796,24 +799,24 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             const float scale = FP8 ? fmaxf(p.scale_log2 * p.k_scale[pc.h], 1e-30f) : p.scale_log2;     // above 0: -inf has to stay that
             float m0 = kSeqNoMax, m1 = kSeqNoMax;
             float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+            const int all_see = __reduce_min_sync(0xffffffffu, min(sees0, sees1));
             for (int i = 0; i < mine; ++i) {
                 const int t = pc.t0 + (pc.wide ? 0 : x) + i * step;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
+                    const bool first = i == 0 && h == 0;
                     ok = seq_wait(&bars[C::SFULL + 2 * x + h], s_parity, abort_flag);
                     ok = __all_sync(0xffffffffu, ok);      // the tensor-memory accesses below are collective over the warp
                     if (!ok) break;
                     tc_fence_after_sync();
                     uint32_t r[32];
                     tmem_ld_rows16(tS + h * 64, r);
-                    const int key = t * kPrefixTile + h * 64, lim0 = sees0 - key, lim1 = sees1 - key;      // keys that the rows see
-                    const bool full = __all_sync(0xffffffffu, min(lim0, lim1) >= 64);
+                    const int key = t * kPrefixTile + h * 64;
                     tmem_wait_ld();
-                    if (!full) p_mask(r, lim0 - 2 * (lane & 3), lim1 - 2 * (lane & 3));
+                    if (key + 64 > all_see) p_mask(r, sees0 - key - 2 * (lane & 3), sees1 - key - 2 * (lane & 3));
                     const float top0 = p_max<0>(r) * scale, top1 = p_max<2>(r) * scale;
-                    const bool first = i == 0 && h == 0;
                     if (__any_sync(0xffffffffu, first || top0 > m0 + kAbove<FP8> || top1 > m1 + kAbove<FP8>)) {
-                        const float n0 = fmaxf(m0, top0 - kBelow<FP8>), n1 = fmaxf(m1, top1 - kBelow<FP8>);
+                        const float n0 = fmaxf(m0, row_max(top0) - kBelow<FP8>), n1 = fmaxf(m1, row_max(top1) - kBelow<FP8>);
                         const float f0 = fast_exp2(m0 - n0), f1 = fast_exp2(m1 - n1);
                         m0 = n0;
                         m1 = n1;
