@@ -403,7 +403,7 @@ __device__ __forceinline__ void p_half(const uint32_t (&r)[32], float scale, flo
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const float2 t = __ffma2_rn(make_float2(__uint_as_float(r[4 * g + 2 * k]), __uint_as_float(r[4 * g + 2 * k + 1])), sc2, k == 0 ? nm0 : nm1);
-            const float2 pr = (g & 1) != 0 && k == 1 ? exp2_by_fma<!FP8>(t) : make_float2(fast_exp2(t.x), fast_exp2(t.y));
+            const float2 pr = (g & 3) == 3 && k == 1 ? exp2_by_fma<!FP8>(t) : make_float2(fast_exp2(t.x), fast_exp2(t.y));
             float2& s = k == 0 ? sum0 : sum1;
             s = __fadd2_rn(s, pr);
             pk[2 * g + k] = FP8 ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);

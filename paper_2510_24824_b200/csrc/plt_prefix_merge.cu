@@ -2,7 +2,7 @@
 // by their references into one softmax, the window's likewise, and the gate mixes the two (Eq. 2). A block has 32 neighbouring rows
 // of a KV head; what there is to know of them is found out once, by its first warp (with every thread for itself that took longer
 // than the joining). A thread then holds 8 of a row's elements and a warp all 32 rows, so that the prefix's partials, which lie
-// [d / 4][128 rows][4], are read 512 bytes at a time, those of four partials together. Where there are not many rows, four warps
+// [d / 4][128 rows][4], are read 512 bytes at a time, those of four partials and the first of the own cache and of the window together. Where there are not many rows, four warps
 // work on each at the same time (two take the prefix's partials in turn, one the own cache's, one the window's) and meet in shared
 // memory. Everything up to the store is fp32, in an order that the plan and the batch alone decide. Bound by latency and by
 // reading the partials (from L2).
@@ -17,15 +17,17 @@ namespace {
 // Warps of a block that hold 8 elements each of the same 32 rows. Split: four times as many threads.
 __host__ __device__ constexpr int merge_parts(bool split) { return split ? 4 : 8; }
 
-// Joins `n` partials of a row into y, top and sum: part(k, ml, acc, step) says where partial k's (reference, sum) and its
-// elements (two pieces of four, `step` floats apart) lie.
-template <int kMergeBatch, typename F>
-__device__ __forceinline__ void join(int n, F part, float (&y)[8], float& top, float& sum) {
-    for (int k0 = 0; k0 < n; k0 += kMergeBatch) {
-        float2 ml[kMergeBatch];
-        float4 v[kMergeBatch][2];
+// N partials of a row, on their way: (reference, sum) and 8 elements each.
+template <int N>
+struct Parts {
+    float2 ml[N];
+    float4 v[N][2];
+    // Partials k0 .. of `n`: part(k, ml, acc, step) says where partial k's (reference, sum) and its elements (two pieces of four,
+    // `step` floats apart) lie.
+    template <typename F>
+    __device__ __forceinline__ void load(int k0, int n, F part) {
 #pragma unroll
-        for (int u = 0; u < kMergeBatch; ++u) {
+        for (int u = 0; u < N; ++u) {
             ml[u] = make_float2(-INFINITY, 0.f);
             v[u][0] = v[u][1] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (k0 + u < n) {
@@ -38,17 +40,20 @@ __device__ __forceinline__ void join(int n, F part, float (&y)[8], float& top, f
                 v[u][1] = *(const float4*)(acc + step);
             }
         }
+    }
+    // Joins them into y, top and sum.
+    __device__ __forceinline__ void join(float (&y)[8], float& top, float& sum) const {
         float m = top;
 #pragma unroll
-        for (int u = 0; u < kMergeBatch; ++u) m = fmaxf(m, ml[u].x);
-        if (m == -INFINITY) continue;            // nothing seen yet
+        for (int u = 0; u < N; ++u) m = fmaxf(m, ml[u].x);
+        if (m == -INFINITY) return;              // nothing seen yet
         const float old = exp2f(top - m);
         top = m;
         sum *= old;
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] *= old;
 #pragma unroll
-        for (int u = 0; u < kMergeBatch; ++u) {
+        for (int u = 0; u < N; ++u) {
             if (ml[u].x == -INFINITY) continue;  // saw no key: what lies there was not written
             const float f = exp2f(ml[u].x - m);
             sum = fmaf(ml[u].y, f, sum);
@@ -61,6 +66,15 @@ __device__ __forceinline__ void join(int n, F part, float (&y)[8], float& top, f
             y[6] = fmaf(v[u][1].z, f, y[6]);
             y[7] = fmaf(v[u][1].w, f, y[7]);
         }
+    }
+};
+// Joins the partials behind the `have` that have been joined.
+template <int N, typename F>
+__device__ __forceinline__ void join_rest(int have, int n, F part, float (&y)[8], float& top, float& sum) {
+    for (int k = have; k < n; k += N) {
+        Parts<N> more;
+        more.load(k, n, part);
+        more.join(y, top, sum);
     }
 }
 
@@ -88,7 +102,7 @@ __device__ __forceinline__ Item item_of(const Params& p, int item, int at) {
 
 template <int D, bool SPLIT>
 __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) plt_prefix_merge(const __grid_constant__ Params p, const __grid_constant__ PrefixParams pp) {
-    constexpr int PARTS = merge_parts(SPLIT), BATCH = SPLIT ? 2 : 4;
+    constexpr int PARTS = merge_parts(SPLIT);
     __shared__ RowInfo s;
     __shared__ float s_join[SPLIT ? 3 : 1][10][SPLIT ? PARTS * 32 : 1];       // (reference, sum, 8 elements) of the other warps
     grid_launch_dependents();
@@ -173,17 +187,16 @@ __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) 
     float y[8], z[8], top = -INFINITY, sum = 0.f, top_w = -INFINITY, sum_w = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = z[i] = 0.f;
-    if (!SPLIT || share < 2) {
-        constexpr int EVERY = SPLIT ? 2 : 1;
-        const int step = s.step[lane] >> 7, row = s.step[lane] & 127;
-        const int64_t tile = s.part[lane] + share * step;
-        join<BATCH>((s.n[lane] - share + EVERY - 1) / EVERY, [&](int k, const float2*& m, const float*& acc, int& apart) {
-            const int64_t at = (tile + k * EVERY * step) * 128;
-            m = (const float2*)(pp.ml + (at + row) * 2);
-            acc = pp.acc + at * D + part * 2 * 512 + row * 4;
-            apart = 512;
-        }, y, top, sum);
-    }
+    constexpr int EVERY = SPLIT ? 2 : 1;
+    const int prefix_step = s.step[lane] >> 7, row = s.step[lane] & 127;
+    const int64_t tile = s.part[lane] + share * prefix_step;
+    const int n_prefix = !SPLIT || share < 2 ? (s.n[lane] - share + EVERY - 1) / EVERY : 0;
+    auto of_prefix = [&](int k, const float2*& m, const float*& acc, int& apart) {
+        const int64_t at = (tile + k * EVERY * prefix_step) * 128;
+        m = (const float2*)(pp.ml + (at + row) * 2);
+        acc = pp.acc + at * D + part * 2 * 512 + row * 4;
+        apart = 512;
+    };
     const int64_t next = (int64_t)p.hpc * p.R;               // rows between the partials of one item
     auto of_item = [&](const Item& it) {
         return [=, &p](int k, const float2*& m, const float*& acc, int& apart) {
@@ -193,9 +206,25 @@ __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) 
             apart = 4;
         };
     };
-    if (does_own) join<BATCH>(own.n, of_item(own), y, top, sum);
+    if constexpr (SPLIT) {
+        if (share < 2) join_rest<2>(0, n_prefix, of_prefix, y, top, sum);
+        if (does_own) join_rest<2>(0, own.n, of_item(own), y, top, sum);
+        if (does_window) join_rest<1>(0, window.n, of_item(window), z, top_w, sum_w);
+    } else {
+        // the first partials of all three are on their way together
+        Parts<4> of_p;
+        Parts<1> of_o, of_w;
+        of_p.load(0, n_prefix, of_prefix);
+        of_o.load(0, own.n, of_item(own));
+        of_w.load(0, window.n, of_item(window));
+        of_p.join(y, top, sum);
+        join_rest<4>(4, n_prefix, of_prefix, y, top, sum);
+        of_o.join(y, top, sum);
+        join_rest<4>(1, own.n, of_item(own), y, top, sum);
+        of_w.join(z, top_w, sum_w);
+        join_rest<1>(1, window.n, of_item(window), z, top_w, sum_w);
+    }
     if (does_window) {
-        join<1>(window.n, of_item(window), z, top_w, sum_w);
         const float f = sum_w > 0.f ? s.gate[lane] / sum_w : 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] *= f;
