@@ -19,8 +19,8 @@
 // shorter: 128 sequences behind 32768 tokens 154 -> 144 us. A and B have an issuing warp each, since the issue of a half costs about
 // as much in waits and commits as its products take.
 //
-// Warp roles: warp 0 loads K and V tiles by TMA into a ring (pages: their ids one tile ahead); warps 1 and 3 issue the products, warp
-// 1 owns the tensor memory; warp 2 makes the plan; warps 2, 20, 21 and 22 turn E4M3 codes into f16 (exact) in a second ring; warps
+// Warp roles: warp 0 loads K and V tiles by TMA into a ring (pages: their ids one tile ahead); warps 1 and 3 load query tiles and issue
+// the products, warp 1 owns the tensor memory; warp 2 makes the plan; warps 2, 20, 21 and 22 turn E4M3 codes into f16 (exact) in a second ring; warps
 // 4-11 and 12-19 are the softmax of A and of B, load their query rows and store the partials. A partial lies as [d / 4][128 rows][4].
 //
 // bf16 probabilities carry 8 bits, f16 ones (E4M3 caches) 11; their sum is taken before that rounding, in fp32.
@@ -57,6 +57,10 @@ __host__ __device__ constexpr uint32_t p_instr_desc(int N, int b_mn_major, bool 
     return (1u << 4) | (f16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
+// a / b for 0 <= a < 2^21 and b > 0: (a + 1/2) / b is at least 1 / 2 b away from a whole number, and off by less than 2^-22 of itself.
+// (A division of whole numbers is a long piece of code, which a launch finds outside the instruction caches.)
+__device__ __forceinline__ int small_div(int a, int b) { return (int)__fdividef((float)a + 0.5f, (float)b); }
+
 // ---- the walk over a block's range ------------------------------------------------------------------------------
 struct PPiece {
     int g, slot, h, m;    // group, slot of the partial, KV head, 256-row block of the group
@@ -66,10 +70,10 @@ struct PPiece {
 };
 struct PWalk {
     int pos, hi, g;       // of the line; with chunks: piece pos = hi - 1, or none
-    __device__ __forceinline__ void fill(int u, int nm, PPiece& pc) {
-        pc.h = u / nm;
-        pc.m = u - pc.h * nm;
-        pc.wide = pc.rows - pc.m * kPrefixRows > 128;
+    __device__ __forceinline__ static void fill(int h, int m, PPiece& pc) {
+        pc.h = h;
+        pc.m = m;
+        pc.wide = pc.rows - m * kPrefixRows > 128;
     }
     __device__ __forceinline__ bool next(const PrefixParams& p, const PrefixPlan& plan, PPiece& pc) {
         for (;;) {
@@ -82,12 +86,15 @@ struct PWalk {
             pc.rows = (plan.begin[g + 1] - plan.begin[g]) * p.R;
             const int tiles = (pc.len + kPrefixTile - 1) / kPrefixTile, nm = (pc.rows + kPrefixRows - 1) / kPrefixRows;
             if (chunk > 0) {
-                const int n = (tiles + chunk - 1) / chunk, o = pos - plan.piece[g], u = o / n, k = o - u * n;
+                // piece k of n: `each` tiles, one more in the first ones
+                const int n = small_div(tiles + chunk - 1, chunk), o = pos - plan.piece[g], u = small_div(o, n), k = o - u * n;
+                const int each = small_div(tiles, n), more = tiles - each * n;
                 pc.slot = pos;
-                pc.t0 = tiles * k / n;
-                pc.t1 = tiles * (k + 1) / n;
+                pc.t0 = k * each + min(k, more);
+                pc.t1 = pc.t0 + each + (k < more ? 1 : 0);
                 pos = hi;
-                fill(u, nm, pc);
+                const int h = small_div(u, nm);
+                fill(h, u - h * nm, pc);
                 return true;
             }
             const int per = tiles + kPrefixLead, o = pos - plan.line[g], u = o / per, v0 = o - u * per;
@@ -97,7 +104,7 @@ struct PWalk {
             pc.t1 = max(v1 - kPrefixLead, 0);
             if (pc.t1 <= pc.t0) continue;
             pc.slot = plan.unit[g] + u + (int)blockIdx.x;
-            fill(u, nm, pc);
+            fill(u / nm, u % nm, pc);
             return true;
         }
     }
@@ -186,7 +193,7 @@ __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const Prefix
         const float held = (float)__reduce_add_sync(0xffffffffu, (int)(tokens >> 24)) * 16777216.f + (float)__reduce_add_sync(0xffffffffu, (int)(tokens & 0xffffff));
         const float bytes = (fmaxf(held, 0.f) + (float)(p.B * (p.L - 1)) * (float)p.w) * (float)p.token_bytes;
         const int left = p.blocks * (lane & 15) / 16, mine = p.blocks - left, n_own = left > 0 ? left : p.blocks;
-        const float prefix_ns = (float)((work + mine - 1) / mine) * (float)p.tile_ns;
+        const float prefix_ns = ceilf(__fdividef((float)work, (float)mine)) * (float)p.tile_ns;
         const float own_ns = (float)kOwnStartNs + fmaxf(__fdividef(bytes, (float)min(n_own * p.own_rate, kMemoryRate)),
                                                         __fdividef((float)p.own_items * (float)kItemNs, (float)(n_own * p.own_per_sm)));
         // side by side the longer one counts, and the shorter one a little: it takes its share of memory and of the L2
@@ -207,12 +214,12 @@ __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const Prefix
         int n = 0;
         for (int g = 0; g < p.groups; ++g) {
             const int tg = __shfl_sync(0xffffffffu, tiles, g), ug = __shfl_sync(0xffffffffu, units, g);
-            n += tg > 0 ? ug * ((tg + s - 1) / s) : 0;
+            n += tg > 0 ? ug * small_div(tg + s - 1, s) : 0;
         }
         const uint32_t fits = __ballot_sync(0xffffffffu, s <= most && n <= blocks);
         if (fits != 0) {
             chunk = least + (__ffs(fits) - 1) * step;
-            piece = warp_scan(tiles > 0 ? units * ((tiles + chunk - 1) / chunk) : 0, lane);
+            piece = warp_scan(tiles > 0 ? units * small_div(tiles + chunk - 1, chunk) : 0, lane);
         }
     }
     if (lane < p.groups) {
@@ -428,6 +435,9 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
 
     if (tid == 0) {
+        tma_prefetch_desc(&tmK);
+        tma_prefetch_desc(&tmV);
+        if (p.q_tma) tma_prefetch_desc(&tmQ);
         s_ctl[0] = 0;
         s_ctl[2] = s_ctl[3] = s_ctl[4] = 0;
         for (int s = 0; s < C::RING; ++s) {
@@ -500,38 +510,9 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         uint64_t* const full = bars + (FP8 ? C::RFULL : C::FULL);
         uint64_t* const empty = bars + (FP8 ? C::REMPTY : C::EMPTY);
         const uint64_t keep = l2_evict_first_policy();
-        const int per_tile = kPrefixTile / p.kbox;
+        const int box_bits = 31 - __clz(p.kbox), per_tile = kPrefixTile >> box_bits;     // boxes are of a power of two keys
         Ring<NRING> rg;
-        uint32_t issued = 0, flags = 0, q_bars = 0;
-        uint32_t o_parity[2] = {0, 0};
-        bool again = false;                                        // not the block's first piece
-        if (lane == 0) {
-            if (p.q_tma) tma_prefetch_desc(&tmQ);
-            tma_prefetch_desc(&tmK);
-            tma_prefetch_desc(&tmV);
-        }
-        // The tiles' query rows, behind the last product that reads the ones before. 128 / G tokens of the G heads: rows behind
-        // the group's belong to the next one or to nobody, and nobody reads their results.
-        auto load_q = [&]() {
-            for (int x = 0; x < 2 && ok; ++x) {
-                if (tiles_of(pc, x) == 0) continue;
-                if ((q_bars >> x) & 1u) {
-                    ok = seq_wait(&bars[C::ODONE + x], o_parity[x], abort_flag);
-                    ok = __all_sync(0xffffffffu, ok);
-                    o_parity[x] ^= 1u;
-                }
-                q_bars |= 1u << x;
-                if (ok && lane == 0) {
-                    uint64_t* bar = &bars[(FP8 ? C::QRAW : C::QFULL) + x];
-                    mbar_expect_tx(bar, C::TILE);
-                    ++s_ctl[3 + x];
-                    const int token = plan.begin[pc.g] * p.L * p.Qn + (pc.m * kPrefixRows + (pc.wide ? x * 128 : 0)) / p.G;
-#pragma unroll
-                    for (int hf = 0; hf < HALVES; ++hf) tma_load_4d(q_smem + x * C::TILE + hf * HB, &tmQ, bar, hf * 64, pc.h * p.G, token, 0, keep);
-                }
-                __syncwarp();
-            }
-        };
+        uint32_t issued = 0, flags = 0;
         while (ok && walk.next(p, plan, pc)) {
             // lane j holds the page of the tile's j-th box, read one tile ahead
             auto page_of = [&](int t) {
@@ -545,11 +526,10 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 return page;
             };
             int next_page = page_of(pc.t0);
-            if (p.q_tma && !again) load_q();
             for (int t = pc.t0; t < pc.t1 && ok; ++t) {
                 const int page = next_page;
                 if (t + 1 < pc.t1) next_page = page_of(t + 1);
-                const int boxes = min(per_tile, (pc.len - t * kPrefixTile + p.kbox - 1) / p.kbox);
+                const int boxes = min(per_tile, (pc.len - t * kPrefixTile + p.kbox - 1) >> box_bits);
                 for (int which = 0; which < 2; ++which) {
                     if (issued >= (uint32_t)NRING) ok = seq_wait(&empty[rg.slot], rg.parity ^ 1u, abort_flag);
                     ok = __all_sync(0xffffffffu, ok);
@@ -569,9 +549,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                     ++issued;
                     rg.advance();
                 }
-                if (p.q_tma && again && ok && t == pc.t0) load_q();     // the first tiles are on their way meanwhile
             }
-            again = true;
         }
         if (lane == 0) s_ctl[2] = (int32_t)issued;
         if (flags) atomicOr(p.status, flags);
@@ -581,6 +559,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         constexpr uint32_t idesc_qk = p_instr_desc(64, 0, FP8), idesc_pv = p_instr_desc(D, 1, FP8);
         constexpr int HB = kPrefixTile * 128;
         const uint32_t q_a = smem_u32(q_smem), ring_a = smem_u32(ring), bars_a = smem_u32(bars);
+        const uint64_t keep = l2_evict_first_policy();
         uint32_t base = 0;                    // ring tiles before this piece: K of its i-th key tile is base + 2 i, V the next
         uint32_t q_parity[2] = {0, 0}, p_parity[2] = {0, 0}, o_parity[2] = {0, 0};
         while (ok && walk.next(p, plan, pc)) {
@@ -647,7 +626,22 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 __syncwarp();
                 if (h == 1) p_parity[x] ^= 1u;
             };
-            auto start = [&](int i, int x) {       // its query rows have been loaded (a tile without a key tile in this piece has none)
+            // Tile x's query rows by TMA, behind the last product that reads the ones before (a tile without a key tile in this piece
+            // has none). 128 / G tokens of the G heads: rows behind the group's belong to the next one or to nobody, and nobody reads
+            // their results.
+            auto load_q = [&](int x) {
+                if (!p.q_tma) return;
+                if (one_thread()) {
+                    uint64_t* bar = &bars[(FP8 ? C::QRAW : C::QFULL) + x];
+                    mbar_expect_tx(bar, C::TILE);
+                    ++s_ctl[3 + x];
+                    const int token = plan.begin[pc.g] * p.L * p.Qn + ((pc.m * kPrefixRows + (pc.wide ? x * 128 : 0)) >> (31 - __clz(p.G)));     // G is a power of two
+#pragma unroll
+                    for (int hf = 0; hf < HALVES; ++hf) tma_load_4d(q_smem + x * C::TILE + hf * HB, &tmQ, bar, hf * 64, pc.h * p.G, token, 0, keep);
+                }
+                __syncwarp();
+            };
+            auto start = [&](int i, int x) {
                 wait_for(C::QFULL + x, q_parity[x]);
                 if (ok) issue_s(i, x, 0);
                 if (ok) issue_s(i, x, 1);
@@ -663,10 +657,13 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             };
             if (pc.wide) {
                 const int x = wid >> 1;
+                load_q(x);
                 start(0, x);
                 for (int i = 0; i < n && ok; ++i) step(i, x, 1);
                 if (n & 1) p_parity[x ^ 1] ^= 1u;
             } else if (wid == 1) {
+                load_q(0);
+                if (n > 1) load_q(1);
                 start(0, 0);
                 if (ok && n > 1) start(1, 1);
                 for (int i = 0; i < n && ok; ++i) step(i, i & 1, 2);
@@ -677,9 +674,9 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             q_parity[0] ^= 1u;
             if (tiles_of(pc, 1) > 0) q_parity[1] ^= 1u;
             base += 2u * (uint32_t)n;
-            // Warp 3 does not see the tiles of a narrow piece land, and a barrier's parity says nothing about the phase before the last:
-            // it goes on behind the piece's last products.
-            for (int x = 0; wid == 3 && x < 2 && ok; ++x)
+            // On behind the piece's last products: then the query tiles are free, and all of the piece's ring tiles have landed, which
+            // warp 3 does not see of a narrow piece (a barrier's parity says nothing about the phase before the last).
+            for (int x = 0; x < 2 && ok; ++x)
                 if (tiles_of(pc, x) > 0) {
                     wait_for(C::ODONE + x, o_parity[x]);
                     o_parity[x] ^= 1u;
@@ -753,8 +750,8 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             const int mine = tiles_of(pc, x), step = pc.wide ? 1 : 2;
             auto sees_of = [&](int lr) {
                 if (lr >= pc.rows) return 0;
-                const int lq = lr % p.R / p.G, n = p.seq_lens[plan.begin[pc.g] + lr / p.R];
-                return max(0, min(pc.len, (int)min((int64_t)n, (int64_t)pc.len + p.max_seq_len) - p.delta[lq / p.Qn] - (p.Qn - 1 - lq % p.Qn)));
+                const int b = small_div(lr, p.R), lq = small_div(lr - b * p.R, p.G), l = small_div(lq, p.Qn), n = p.seq_lens[plan.begin[pc.g] + b];
+                return max(0, min(pc.len, (int)min((int64_t)n, (int64_t)pc.len + p.max_seq_len) - p.delta[l] - (p.Qn - 1 - (lq - l * p.Qn))));
             };
             int sees0 = 0, sees1 = 0;
             if (mine > 0) {
@@ -762,7 +759,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 if (FP8 || !p.q_tma) {
                     const int lr = first_row + row;
                     const bool in = lr < pc.rows;
-                    const int b = in ? plan.begin[pc.g] + lr / p.R : 0, r = in ? lr % p.R : 0, lq = r / p.G;
+                    const int bg = in ? small_div(lr, p.R) : 0, b = in ? plan.begin[pc.g] + bg : 0, r = in ? lr - bg * p.R : 0, lq = small_div(r, p.G);
                     uint4 v[PART / 8];
                     if (p.q_tma) {       // bf16 rows that TMA wrote become f16 in place
                         ok = seq_wait(&bars[C::QRAW + x], r_parity, abort_flag);
