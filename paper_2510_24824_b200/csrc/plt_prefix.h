@@ -71,6 +71,10 @@ plt_status decode_run_prefix(plt_decode_attn_t h, const plt_decode_attn_args* ar
 plt_status decode_encode_rows(plt_decode_attn_t h, CUtensorMap* map, const void* base, int es, int d, int64_t keys, int64_t heads,
                               int64_t outer, int64_t sn, int64_t sh, int64_t so, int box_keys);
 
+// a / b for 0 <= a < 2^21 and b > 0: (a + 1/2) / b is at least 1 / 2 b away from a whole number, and off by less than 2^-22 of itself.
+// (A division of whole numbers is a long piece of code, which a launch finds outside the instruction caches.)
+__device__ __forceinline__ int small_div(int a, int b) { return (int)__fdividef((float)a + 0.5f, (float)b); }
+
 // Blocks that take part in a line of T positions: at least kPrefixMinLine positions each.
 constexpr int kPrefixMinLine = 3;
 __host__ __device__ inline int prefix_blocks(int T, int launched) {

@@ -57,10 +57,6 @@ __host__ __device__ constexpr uint32_t p_instr_desc(int N, int b_mn_major, bool 
     return (1u << 4) | (f16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
-// a / b for 0 <= a < 2^21 and b > 0: (a + 1/2) / b is at least 1 / 2 b away from a whole number, and off by less than 2^-22 of itself.
-// (A division of whole numbers is a long piece of code, which a launch finds outside the instruction caches.)
-__device__ __forceinline__ int small_div(int a, int b) { return (int)__fdividef((float)a + 0.5f, (float)b); }
-
 // ---- the walk over a block's range ------------------------------------------------------------------------------
 struct PPiece {
     int g, slot, h, m;    // group, slot of the partial, KV head, 256-row block of the group
@@ -153,8 +149,12 @@ __device__ __forceinline__ int warp_scan(int x, int lane) {     // inclusive
     return x;
 }
 
-// The plan of up to kNearGroups groups, by one warp: lane g is group g. Everything but the sequences' lengths goes to `to`.
-__device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const PrefixPlan& to, int lane, uint32_t& flags) {
+constexpr int kLeavers = 512;        // threads of the last block that leave the sequences' lengths: the softmax's
+constexpr int kBarLeft = 9, kBarGroups = 10;     // named barriers: the plan has been left; the groups and lengths are known
+
+// The plan of up to kNearGroups groups, by one warp: lane g is group g. Everything but the sequences' lengths goes to `to`; where
+// `leaves`, the threads that leave those are let go as soon as groups and lengths are known.
+__device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const PrefixPlan& to, int lane, bool leaves, uint32_t& flags) {
     const int given = lane <= p.groups ? p.group_begin[lane] : 0;
     int len = lane < p.groups ? p.prefix_lens[lane] : 0;
     int64_t tokens = 0;
@@ -176,6 +176,9 @@ __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const Prefix
     const int next = __shfl_down_sync(0xffffffffu, begin, 1);
     const int rows = lane < p.groups ? (next - begin) * p.R : 0;
     if (rows == 0) len = 0;
+    if (lane < p.groups) to.len[lane] = len;
+    if (lane <= p.groups) to.begin[lane] = begin;
+    if (leaves) named_barrier_sync(kBarGroups, kLeavers + 32);
     const int tiles = (len + kPrefixTile - 1) / kPrefixTile;
     const int units = tiles > 0 ? p.Hkv * ((rows + kPrefixRows - 1) / kPrefixRows) : 0;
     const int positions = units * (tiles + kPrefixLead);
@@ -223,12 +226,10 @@ __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const Prefix
         }
     }
     if (lane < p.groups) {
-        to.len[lane] = len;
         to.line[lane + 1] = line;
         to.unit[lane + 1] = unit;
         to.piece[lane + 1] = piece;
     }
-    if (lane <= p.groups) to.begin[lane] = begin;
     if (lane == 0) {
         to.line[0] = to.unit[0] = to.piece[0] = 0;
         to.chunk[0] = chunk;
@@ -237,9 +238,8 @@ __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const Prefix
     }
 }
 
-// Leaves the plan `from` (in shared memory) where the kernels behind find it, with what each sequence holds itself. By `threads`
-// threads, whose groups and lengths all have been written.
-__device__ __forceinline__ void leave_plan(const PrefixParams& p, const PrefixPlan& from, int tid, int threads, uint32_t& flags) {
+// Leaves the plan `from` (in shared memory) where the kernels behind find it: here all but the lengths.
+__device__ __forceinline__ void leave_plan(const PrefixParams& p, const PrefixPlan& from, int tid, int threads) {
     for (int g = tid; g <= p.groups; g += threads) {
         p.plan.begin[g] = from.begin[g];
         p.plan.line[g] = from.line[g];
@@ -248,6 +248,9 @@ __device__ __forceinline__ void leave_plan(const PrefixParams& p, const PrefixPl
         if (g < p.groups) p.plan.len[g] = from.len[g];
     }
     if (tid < 3) p.plan.chunk[tid] = from.chunk[tid];
+}
+// And what each sequence holds itself; `ahead` is the length of sequence `tid`.
+__device__ __forceinline__ void leave_lens(const PrefixParams& p, const PrefixPlan& from, int tid, int threads, int ahead, uint32_t& flags) {
     for (int b = tid; b < p.B; b += threads) {
         // the group of sequence b, if any
         int len = 0;
@@ -259,7 +262,7 @@ __device__ __forceinline__ void leave_plan(const PrefixParams& p, const PrefixPl
             }
             len = from.len[lo];
         }
-        int n = p.seq_lens[b];
+        int n = b == tid ? ahead : p.seq_lens[b];
         if (n < 0 || n > (int64_t)len + p.max_seq_len) {
             flags |= kDevSeqLenClamped;
             n = n < 0 ? 0 : len + p.max_seq_len;
@@ -475,7 +478,12 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         plan.piece = s_plan + 4 * W;
         plan.chunk = s_plan + 5 * W;
         if (!leaves) grid_launch_dependents();
-        if (wid == 2) plan_by_warp(p, plan, lane, reported);
+        if (wid == 2) plan_by_warp(p, plan, lane, leaves, reported);
+        if (leaves && wid >= 4 && wid < 20) {      // the warps of the softmax, which have nothing to do yet
+            const int ahead = tid - 128 < p.B ? p.seq_lens[tid - 128] : 0;
+            named_barrier_sync(kBarGroups, kLeavers + 32);
+            leave_lens(p, plan, tid - 128, kLeavers, ahead, reported);
+        }
     } else {
         grid_dependency_wait();
         grid_launch_dependents();
@@ -487,12 +495,11 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     // columns: S_A 0..127 in halves of 64 (its P over the first 32 of each, once the scores have been read), S_B 128..255, O_A from
     // 256, O_B from 384
     if (leaves) {
-        // The kernel behind this one reads the plan without a wait of its own: it is let go once the plan has been written. (The
-        // warps of the softmax have nothing to do yet.)
+        // The kernel behind this one reads the plan without a wait of its own: it is let go once the plan has been written.
         if (wid >= 4 && wid < 20) {
-            leave_plan(p, plan, tid - 128, 512, reported);
+            leave_plan(p, plan, tid - 128, kLeavers);
             __threadfence();
-            named_barrier_sync(9, 512);
+            named_barrier_sync(kBarLeft, kLeavers);
             if (tid == 128) grid_launch_dependents();
         }
         if (reported) atomicOr(p.status, reported);
@@ -975,7 +982,8 @@ __global__ void __launch_bounds__(kPlanThreads) plt_prefix_plan(const __grid_con
     from.unit = s_unit;
     from.piece = s_piece;
     from.chunk = s_chunk;
-    leave_plan(p, from, tid, kPlanThreads, flags);
+    leave_plan(p, from, tid, kPlanThreads);
+    leave_lens(p, from, tid, kPlanThreads, tid < p.B ? p.seq_lens[tid] : 0, flags);
     if (flags) atomicOr(p.status, flags);
 }
 

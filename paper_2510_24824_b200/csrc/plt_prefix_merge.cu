@@ -113,9 +113,9 @@ __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) 
         // what the caller passed and the plan, complete since before the main kernel let this one go
         const int id = blockIdx.x * 32 + lane;
         const bool in = id < p.B * p.R;
-        const int b = in ? id / p.R : 0;
+        const int b = in ? small_div(id, p.R) : 0;
         const int r = in ? id - b * p.R : 0;
-        const int lq = r / p.G, l = lq / p.Qn, newer = p.Qn - 1 - (lq - l * p.Qn), head = h * p.G + (r - lq * p.G);
+        const int lq = small_div(r, p.G), l = small_div(lq, p.Qn), newer = p.Qn - 1 - (lq - l * p.Qn), head = h * p.G + (r - lq * p.G);
         const PrefixPlan& plan = pp.plan;
         int group = -1, len = 0, begin = 0, end = 0;
         if (pp.groups > 0) {
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) 
             const int tiles = (len + kPrefixTile - 1) / kPrefixTile, chunk = *plan.chunk;
             const int lr = (b - begin) * p.R + r, m = lr / kPrefixRows, u = h * nm + m;
             if (chunk > 0) {
-                count = (tiles + chunk - 1) / chunk;
+                count = small_div(tiles + chunk - 1, chunk);
                 tile = plan.piece[group] + (int64_t)u * count;
             } else {
                 const int T = plan.line[pp.groups], first = plan.line[group] + u * (tiles + kPrefixLead) + kPrefixLead;
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) 
         s.step[lane] = step * 128 + row;
         s.gate[lane] = gate;
         s.out[lane] = in ? ((b * p.L * p.Qn + lq) * p.Hq + head) | (cut > 0 ? 0 : 1 << 30) : -1;
-        const int hg = h / p.hpc, item = item_index(p, b, hg, 0);
+        const int hg = small_div(h, p.hpc), item = item_index(p, b, hg, 0);
         s.own[lane] = has_own ? item : -1;
         s.window[lane] = has_window ? item + 1 : -1;
         s.at[lane] = (h - hg * p.hpc) * p.R + r;
