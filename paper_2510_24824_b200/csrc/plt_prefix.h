@@ -14,6 +14,8 @@ constexpr int kPrefixLead = 2;        // line positions that stand for starting 
 //     the same number of nearly equal pieces of at most `*chunk` tiles, and piece i is block i's and leaves its partial in slot i.
 //   - Else (*chunk = 0) the units lie one after the other on a line of key tiles, each preceded by kPrefixLead positions, and the
 //     line is cut into equal ranges, one for each block, which may hold several pieces; slot unit + block.
+// The line for all calls measured 18.0 us against 15.9 (two users), 26.4 against 20.0 (21 sequences of drafts), 33.4 against 33.0 (64
+// sequences of two loops), 150 against 139 (128 of them behind 32768 tokens), and 40.4 against 41.2 for three groups of 8-bit caches.
 // Not every block need take part: the pass over the prefixes is bound by the tensor cores and its start, the one over the own caches
 // by memory and its start, so that the plan may leave some multiprocessors to the latter, which then runs at the same time.
 struct PrefixPlan {

