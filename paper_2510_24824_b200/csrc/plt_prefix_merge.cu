@@ -2,10 +2,10 @@
 // by their references into one softmax, the window's likewise, and the gate mixes the two (Eq. 2). A block has 32 neighbouring rows
 // of a KV head; what there is to know of them is found out once, by its first warp (with every thread for itself that took longer
 // than the joining). A thread then holds 8 of a row's elements and a warp all 32 rows, so that the prefix's partials, which lie
-// [d / 4][128 rows][4], are read 512 bytes at a time, those of four partials and the first of the own cache and of the window together. Where there are not many rows, four warps
-// work on each at the same time (two take the prefix's partials in turn, one the own cache's, one the window's) and meet in shared
-// memory. Everything up to the store is fp32, in an order that the plan and the batch alone decide. Bound by latency and by
-// reading the partials (from L2).
+// [d / 4][128 rows][4], are read 512 bytes at a time, those of four partials and the first of the own cache and of the window
+// together. Where there are not many rows, four or sixteen warps work on each at the same time (two or fourteen take the prefix's
+// partials in turn, one the own cache's, one the window's) and meet in shared memory. Everything up to the store is fp32, in an order
+// that the plan and the batch alone decide. Bound by latency and by reading the partials (from L2): 3 to 5 us behind the last of them.
 #include <cuda_bf16.h>
 
 #include "plt_prefix.h"
@@ -14,8 +14,8 @@
 namespace plt {
 namespace {
 
-// Warps of a block that hold 8 elements each of the same 32 rows. Split: four times as many threads.
-__host__ __device__ constexpr int merge_parts(bool split) { return split ? 4 : 8; }
+// Warps of a block that hold 8 elements each of the same 32 rows, and warps that share one such piece (1: none).
+__host__ __device__ constexpr int merge_parts(int shares) { return shares == 1 ? 8 : shares == 4 ? 4 : 1; }
 
 // N partials of a row, on their way: (reference, sum) and 8 elements each.
 template <int N>
@@ -100,11 +100,12 @@ __device__ __forceinline__ Item item_of(const Params& p, int item, int at) {
     return {slot_of(max(item, 0), c.x) * p.hpc * p.R + at, c.y - c.x + 1};
 }
 
-template <int D, bool SPLIT>
-__global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) plt_prefix_merge(const __grid_constant__ Params p, const __grid_constant__ PrefixParams pp) {
-    constexpr int PARTS = merge_parts(SPLIT);
+template <int D, int SHARES>
+__global__ void __launch_bounds__(merge_parts(SHARES) * SHARES * 32, 2) plt_prefix_merge(const __grid_constant__ Params p, const __grid_constant__ PrefixParams pp) {
+    constexpr bool SPLIT = SHARES > 1;
+    constexpr int PARTS = merge_parts(SHARES), OWN = SHARES - 2, WINDOW = SHARES - 1;      // shares 0 .. OWN - 1: the prefix's partials
     __shared__ RowInfo s;
-    __shared__ float s_join[SPLIT ? 3 : 1][10][SPLIT ? PARTS * 32 : 1];       // (reference, sum, 8 elements) of the other warps
+    __shared__ float s_join[SPLIT ? SHARES - 1 : 1][10][SPLIT ? PARTS * 32 : 1];       // (reference, sum, 8 elements) of the other warps
     grid_launch_dependents();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, share = SPLIT ? wid / PARTS : 0;
     const int part = blockIdx.z * PARTS + wid % PARTS;                        // elements 8 part .. 8 part + 7
@@ -164,6 +165,8 @@ __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) 
             if (rows - m * kPrefixRows > 128) {
                 tile += (lr >> 7) & 1;
                 step = 2;
+            } else if (chunk > 0 && count == tiles) {
+                step = 2;              // pieces of one key tile each: the first tile's
             } else {
                 count *= 2;
             }
@@ -182,15 +185,15 @@ __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) 
     grid_dependency_wait();
 
     // ---- one softmax over the prefix and the own keys, and the window's ---------------------------------------------------
-    const bool does_own = !SPLIT || share == 2, does_window = !SPLIT || share == 3;
+    const bool does_own = !SPLIT || share == OWN, does_window = !SPLIT || share == WINDOW;
     const Item own = item_of(p, does_own ? s.own[lane] : -1, s.at[lane]), window = item_of(p, does_window ? s.window[lane] : -1, s.at[lane]);
     float y[8], z[8], top = -INFINITY, sum = 0.f, top_w = -INFINITY, sum_w = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = z[i] = 0.f;
-    constexpr int EVERY = SPLIT ? 2 : 1;
+    constexpr int EVERY = SPLIT ? OWN : 1;
     const int prefix_step = s.step[lane] >> 7, row = s.step[lane] & 127;
     const int64_t tile = s.part[lane] + share * prefix_step;
-    const int n_prefix = !SPLIT || share < 2 ? (s.n[lane] - share + EVERY - 1) / EVERY : 0;
+    const int n_prefix = !SPLIT || share < OWN ? (s.n[lane] - share + EVERY - 1) / EVERY : 0;
     auto of_prefix = [&](int k, const float2*& m, const float*& acc, int& apart) {
         const int64_t at = (tile + k * EVERY * prefix_step) * 128;
         m = (const float2*)(pp.ml + (at + row) * 2);
@@ -207,7 +210,7 @@ __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) 
         };
     };
     if constexpr (SPLIT) {
-        if (share < 2) join_rest<2>(0, n_prefix, of_prefix, y, top, sum);
+        if (share < OWN) join_rest<2>(0, n_prefix, of_prefix, y, top, sum);
         if (does_own) join_rest<2>(0, own.n, of_item(own), y, top, sum);
         if (does_window) join_rest<1>(0, window.n, of_item(window), z, top_w, sum_w);
     } else {
@@ -235,20 +238,28 @@ __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) 
             s_join[share - 1][0][t] = top;
             s_join[share - 1][1][t] = sum;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s_join[share - 1][2 + i][t] = share == 3 ? z[i] : y[i];
+            for (int i = 0; i < 8; ++i) s_join[share - 1][2 + i][t] = share == WINDOW ? z[i] : y[i];
         }
         __syncthreads();
         if (share > 0) return;
-        const float all = fmaxf(top, fmaxf(s_join[0][0][t], s_join[1][0][t]));
-        if (all > -INFINITY) {
-            // 0 for one that saw nothing
-            const float f = exp2f(top - all), f1 = exp2f(s_join[0][0][t] - all), f2 = exp2f(s_join[1][0][t] - all);
-            sum = fmaf(sum, f, fmaf(s_join[0][1][t], f1, s_join[1][1][t] * f2));
+        float all = top;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = fmaf(y[i], f, fmaf(s_join[0][2 + i][t], f1, s_join[1][2 + i][t] * f2));
+        for (int o = 0; o < OWN; ++o) all = fmaxf(all, s_join[o][0][t]);
+        if (all > -INFINITY) {
+            const float own_f = exp2f(top - all);      // 0 for one that saw nothing
+            sum *= own_f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] *= own_f;
+#pragma unroll
+            for (int o = 0; o < OWN; ++o) {
+                const float f = exp2f(s_join[o][0][t] - all);
+                sum = fmaf(s_join[o][1][t], f, sum);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = fmaf(s_join[o][2 + i][t], f, y[i]);
+            }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = s_join[2][2 + i][t];
+        for (int i = 0; i < 8; ++i) z[i] = s_join[WINDOW - 1][2 + i][t];
     }
     const int out = s.out[lane];
     if (out < 0) return;
@@ -264,27 +275,31 @@ __global__ void __launch_bounds__(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32, 2) 
 
 namespace {
 
-template <int D, bool SPLIT>
+template <int D, int SHARES>
 cudaError_t launch(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((p.B * p.R + 31) / 32), (unsigned)p.Hkv, (unsigned)(D / (8 * merge_parts(SPLIT))));
-    cfg.blockDim = dim3(merge_parts(SPLIT) * (SPLIT ? 4 : 1) * 32);
+    cfg.gridDim = dim3((unsigned)((p.B * p.R + 31) / 32), (unsigned)p.Hkv, (unsigned)(D / (8 * merge_parts(SHARES))));
+    cfg.blockDim = dim3(merge_parts(SHARES) * SHARES * 32);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = overlap ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, plt_prefix_merge<D, SPLIT>, p, pp);
+    return cudaLaunchKernelEx(&cfg, plt_prefix_merge<D, SHARES>, p, pp);
 }
 
 template <int D>
 cudaError_t launch_for(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream) {
     // Four warps to a row as long as all run at once (32 on each multiprocessor): the step of two users 15.9 us against 16.6, drafts of
     // 21 sequences 20.0 against 20.7, 16 sequences 19.2 against 21.4, 32 of two loops 25.1 against 26.1; where they do not, 64 of two
-    // loops 36.2 against 33.0, 128 of them 142.8 against 138.6.
+    // loops 36.2 against 33.0, 128 of them 142.8 against 138.6. Sixteen where few units of long prefixes may have been cut into many
+    // pieces (one sequence behind 12615 tokens of one KV head 19.3 us against 28.0, 6 behind two prefixes of 32705 29.5 against 34.7;
+    // short prefixes lose half a microsecond).
     const int64_t warps = (int64_t)(p.B * p.R + 31) / 32 * p.Hkv * (D / 8);
-    return warps * 4 <= 148 * 32 ? launch<D, true>(p, pp, overlap, stream) : launch<D, false>(p, pp, overlap, stream);
+    const int pieces = min(pp.blocks / p.Hkv, (pp.max_prefix_len + kPrefixTile - 1) / kPrefixTile);      // of a unit, at most
+    if (warps * 16 <= 148 * 32 && pieces > 8) return launch<D, 16>(p, pp, overlap, stream);
+    return warps * 4 <= 148 * 32 ? launch<D, 4>(p, pp, overlap, stream) : launch<D, 1>(p, pp, overlap, stream);
 }
 
 }  // namespace

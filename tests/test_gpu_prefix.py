@@ -46,6 +46,10 @@ CASES = [
     dict(own=[300] * 8, plens=[6000], begin=[0, 8], Hq=24, Hkv=8, kv="e4m3", L=2),
     dict(own=[2] * 40, plens=[9000] * 40, begin=list(range(41)), Hq=2, Hkv=1),                       # a plan of many groups, several pieces a block
     dict(own=[2] * 20, plens=[2500] * 20, begin=list(range(21)), Hq=32, Hkv=8),                      # more units than blocks
+    dict(own=[900], plens=[12615], begin=[0, 1], Hq=3, Hkv=1, kv="e4m3", q_len=2, page=32),          # pieces of a tile each, many to a row
+    dict(own=[6, 0, 3], plens=[20000, 3000], begin=[0, 1, 3], Hq=4, Hkv=2, d=64, L=2, w=9),          # several tiles each, many to a row
+    dict(own=[5], plens=[128 * 9], begin=[0, 1], Hq=8, Hkv=1),                                       # at the borders of the merge's forms
+    dict(own=[5], plens=[128 * 8], begin=[0, 1], Hq=8, Hkv=1),
 ]
 
 
