@@ -140,7 +140,8 @@ __device__ __forceinline__ PWalk walk_of_block(const PrefixParams& p, const Pref
 }
 
 constexpr int kOwnStartNs = 7000;     // what starting and finishing the pass over the own caches takes, about
-constexpr int kGapNs = 2000;          // what one pass behind the other loses between them, about
+constexpr int kGapNs = 8000;          // what one pass behind the other loses between them, about (with less, large batches of 8-bit caches with
+                                      // 16 packed rows took 71 us one behind the other instead of 61 side by side)
 constexpr int kItemNs = 3000;         // what one of its items takes a block at least, about
 constexpr int kMemoryRate = 5500;     // bytes a nanosecond that the device streams, about
 
