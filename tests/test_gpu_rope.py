@@ -222,6 +222,40 @@ def test_prompt_in_parts_and_step_by_step_give_the_same_bits():
         assert torch.equal(a, caches[0][0]) and torch.equal(b, caches[0][1])
 
 
+@pytest.mark.parametrize("kw", [dict(Hq=1, Hkv=1), dict(Hq=3, Hkv=1, d=64, L=2, w=9, layout="interleaved"), dict(Hq=4, Hkv=2, dtype="f32", d=64, page=32),
+                                dict(Hq=2, Hkv=2, kv="e4m3", page=48)], ids=str)
+def test_blocks_of_many_tokens_give_the_same_bits(kw):
+    """Many short rows go in larger blocks: every sequence of such a call gives what a call of its own gives, and nothing else is
+    written."""
+    n, T = 60, 260
+    c = Case(seed=9, B_=n, cap=288, **kw)
+    lens = [(37 * b) % (T + 1) for b in range(n)]
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    q, ks, vs = (c.rand(n, c.L, T, c.Hq, c.d) * 1.5).to(c.act), (c.rand(n, T, c.Hkv, c.d) * 1.5).to(c.act), c.rand(n, T, c.Hkv, c.d).to(c.act)
+    kl = (c.rand(n, c.L - 1, T, c.Hkv, c.d) * 1.5).to(c.act) if c.L > 1 else None
+
+    def call(rows, caches):
+        outs = [torch.full_like(x[rows], 7.0) if x is not None else None for x in (q, ks, kl)]
+        pages = dict(c.pages, page_table=c.table[rows].contiguous()) if c.page else {}
+        B.plt_rope_seq(c.op, B.make_rope_seq_args(len(lens[rows]), T, q[rows], ks[rows], dev(lens[rows]), outs[0], k_share_out=outs[1],
+                                                  k_loc=None if kl is None else kl[rows], k_loc_out=outs[2], q_gain=c.q_gain, k_gain=c.k_gain, start=dev([5] * len(lens[rows])),
+                                                  v_share=vs[rows], k_cache=caches[0] if c.page else caches[0][rows], v_cache=caches[1] if c.page else caches[1][rows],
+                                                  **pages, **c.scales))
+        return outs
+    caches = [[x.clone() for x in (c.k_cache, c.v_cache)] for _ in range(2)]
+    whole = call(slice(0, n), caches[0])
+    parts = [call(slice(b, b + 1), caches[1]) for b in range(n)]
+    torch.cuda.synchronize()
+    assert B.plt_rope_check(c.op) == 0
+    for i, x in enumerate(whole):
+        if x is not None:
+            assert torch.equal(x.view(torch.uint8), torch.cat([o[i] for o in parts]).view(torch.uint8))
+    for a, b in zip(*caches):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    y, err = c.row(q[1, 0, 36], 41, c.q_gain)
+    c.stored(whole[0][1, 0, 36], y, err, c.act)
+
+
 def test_no_turn_and_no_norm_is_the_plain_pre_step():
     """With frequencies of 0 and no gains, rope_step and run do what plt_decode_attn_step does."""
     from paper_2510_24824_b200.inputs import make_problem, shrunk_workload
