@@ -609,12 +609,16 @@ plt_status common(plt_rope_t h, int32_t batch, const int32_t* page_table, int32_
     return PLT_OK;
 }
 
-// Whether a prompt goes in blocks of 32 tokens instead of 8: where a token's queries and keys are so few bytes that a block's start
-// counts, and the larger blocks still fill the device. 32 ragged prompts of up to 4096 rows of bf16: 1 + 1 heads of 64 17.9 us against
-// 45.3, 3 + 1 of 128 27.5 against 51.7, 8 + 2 of 128 44.1 against 54.8, 8 + 8 of 128 79.6 against 76.7; one prompt of 1000 rows of 3 + 1
-// heads of 128 6.0 against 4.3.
-bool large_blocks(const RopeParams& p, int row_bytes) {
-    return (p.Hq + p.Hkv) * row_bytes <= 2560 && (int64_t)p.B * p.L * ((p.T + 31LL) / 32) >= 3 * 148;
+// Tokens of a block of a prompt.
+//   - 32 where a token's queries and keys are so few bytes that a block's start counts, and the larger blocks still fill the device: 32
+//     ragged prompts of up to 4096 rows of bf16 1 + 1 heads of 64 17.9 us against 45.3 with 8, 3 + 1 of 128 27.5 against 51.7, 8 + 2 of
+//     128 44.1 against 54.8, 8 + 8 of 128 79.6 against 76.7; one prompt of 1000 rows of 3 + 1 heads of 128 6.0 against 4.3.
+//   - 2 where blocks of 8 are few, since a block walks over its heads: one prompt of 60 rows, 32 + 8 heads of 128 in bf16 3.9 us against
+//     7.3 with 8, of 300 rows 4.5 against 7.5; 1000 rows of 16 + 4 heads 6.3 against 5.3.
+int tokens_of_block(const RopeParams& p, int row_bytes) {
+    const int64_t prompts = (int64_t)p.B * p.L;
+    if (prompts * ((p.T + 7LL) / 8) <= 64) return 2;
+    return (p.Hq + p.Hkv) * row_bytes <= 2560 && prompts * ((p.T + 31LL) / 32) >= 3 * 148 ? 32 : 8;
 }
 
 // A prompt's rows in blocks of TB tokens.
@@ -626,9 +630,14 @@ void launch_seq(const RopeParams& p, cudaStream_t stream) {
 
 template <typename T, bool FP8, int D, bool INTER>
 void launch_one(bool seq, const RopeParams& p, cudaStream_t stream) {
-    if (!seq) plt_rope_step_kernel<T, FP8, D, INTER><<<p.B * p.L * p.Qn, kRopeThreads, 0, stream>>>(p);
-    else if (large_blocks(p, D * (int)sizeof(T))) launch_seq<T, FP8, D, INTER, 32>(p, stream);
-    else launch_seq<T, FP8, D, INTER, 8>(p, stream);
+    if (!seq) {
+        plt_rope_step_kernel<T, FP8, D, INTER><<<p.B * p.L * p.Qn, kRopeThreads, 0, stream>>>(p);
+        return;
+    }
+    const int tokens = tokens_of_block(p, D * (int)sizeof(T));
+    if (tokens == 32) launch_seq<T, FP8, D, INTER, 32>(p, stream);
+    else if (tokens == 8) launch_seq<T, FP8, D, INTER, 8>(p, stream);
+    else launch_seq<T, FP8, D, INTER, 2>(p, stream);
 }
 
 template <bool INTER>

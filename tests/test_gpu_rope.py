@@ -224,11 +224,12 @@ def test_prompt_in_parts_and_step_by_step_give_the_same_bits():
 
 @pytest.mark.parametrize("kw", [dict(Hq=1, Hkv=1), dict(Hq=3, Hkv=1, d=64, L=2, w=9, layout="interleaved"), dict(Hq=4, Hkv=2, dtype="f32", d=64, page=32),
                                 dict(Hq=2, Hkv=2, kv="e4m3", page=48)], ids=str)
-def test_blocks_of_many_tokens_give_the_same_bits(kw):
-    """Many short rows go in larger blocks: every sequence of such a call gives what a call of its own gives, and nothing else is
-    written."""
-    n, T = 60, 260
-    c = Case(seed=9, B_=n, cap=288, **kw)
+@pytest.mark.parametrize("T", [260, 700])
+def test_blocks_of_many_tokens_give_the_same_bits(kw, T):
+    """A large call goes in larger blocks than a small one: every sequence of it gives what a call of its own gives, and nothing else
+    is written."""
+    n = 60
+    c = Case(seed=9, B_=n, cap=720, **kw)
     lens = [(37 * b) % (T + 1) for b in range(n)]
     dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
     q, ks, vs = (c.rand(n, c.L, T, c.Hq, c.d) * 1.5).to(c.act), (c.rand(n, T, c.Hkv, c.d) * 1.5).to(c.act), c.rand(n, T, c.Hkv, c.d).to(c.act)
