@@ -223,6 +223,17 @@ def test_two_handles_at_once_and_batches_below_the_largest():
     B.plt_prefix_attn_destroy(hb)
 
 
+def test_a_batch_of_none_writes_nothing():
+    p = Problem(20, [5, 6], [200], [0, 2])
+    h = B.plt_prefix_attn_create(p.config)
+    B.plt_prefix_attn_run(h, B.make_args(0, p.q, p.k_cache, p.v_cache, p.seq_lens, p.out), p.shared)
+    torch.cuda.synchronize()
+    assert torch.isnan(p.out.float()).all() and B.plt_prefix_attn_check(h) == 0
+    assert p.run(handle=h) == 0
+    p.hold()
+    B.plt_prefix_attn_destroy(h)
+
+
 def test_window_lengths_out_of_range_are_clamped_and_flagged():
     p = Problem(17, [8, 9, 10], [200], [0, 3], L=2, w=9, win_lens=[[-3], [10], [5]])
     assert p.run() == B.PLT_DEV_WIN_LEN_CLAMPED
