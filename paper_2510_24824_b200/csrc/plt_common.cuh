@@ -54,9 +54,10 @@ struct Params {
                                // packed row i is i >> 1 and its half i & 1
     int32_t win_free;          // 1: win_lens holds for loops that see no key of the shared cache too (the keys in front of it
                                // lie in a prefix of their own)
-    int32_t late_wait;         // 1: the kernel before this one has nothing for it and let it go once it might start (the warp-level
-                               // main kernel then waits for that one's end at its own end, so that the kernel behind sees both)
-    const int32_t* block_limit; // or null: blocks of the warp-level main kernel that may take part (a word on the device)
+    const uint32_t* handed;    // or null. A word that the kernel before this one releases once it has written seq_lens, win_lens and
+                               // block_limit, before it lets this one go. The warp-level main kernel acquires it, needs nothing
+                               // else of that kernel, and waits for its end only at its own end, so that the kernel behind sees both
+    const int32_t* block_limit; // blocks of the warp-level main kernel that may take part (a word on the device); with `handed`
     float scale_log2;          // sm_scale * log2(e)
     int32_t delta[kMaxLoops];  // per-loop causal offset
 };

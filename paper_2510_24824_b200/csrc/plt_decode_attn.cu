@@ -644,8 +644,8 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
         pp.B = p.B; pp.L = p.L; pp.Qn = p.Qn; pp.Hq = p.Hq; pp.Hkv = p.Hkv; pp.G = p.G; pp.R = p.R; pp.d = p.d; pp.w = p.w;
         pp.max_seq_len = p.max_seq_len; pp.page_size = p.page_size; pp.num_pool_pages = p.num_pool_pages;
         pp.scale_log2 = p.scale_log2;
-        p.late_wait = pp.groups > 0 && h->bf16 && !h->umma;
-        pp.own_per_sm = p.late_wait ? h->ctas_per_sm : 0;
+        const bool beside = pp.groups > 0 && h->bf16 && !h->umma;      // the pass over the own caches runs beside the prefixes'
+        pp.own_per_sm = beside ? h->ctas_per_sm : 0;
         pp.own_items = p.B * (p.Hkv / p.hpc) * (p.L > 1 ? 2 : 1);
         for (int l = 0; l < kMaxLoops; ++l) pp.delta[l] = p.delta[l];
         if (c.page_size > 0 && pp.groups > 0) {
@@ -669,7 +669,10 @@ plt_status run_impl(plt_decode_attn_t h, const plt_decode_attn_args* a, void* cu
         p.seq_lens = pp.plan.own_lens;
         p.win_lens = pp.plan.win_lens;
         p.win_free = 1;
-        p.block_limit = p.late_wait ? pp.plan.chunk + 2 : nullptr;
+        if (beside) {
+            p.handed = pp.plan.ready;
+            p.block_limit = pp.plan.chunk + 2;
+        }
     }
     if (step) {
         Params pre = p;

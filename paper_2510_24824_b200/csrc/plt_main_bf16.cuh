@@ -372,17 +372,21 @@ plt_decode_main_bf16(const __grid_constant__ CUtensorMap tmK, const __grid_const
         }
         mbar_fence_init();
     }
+    if (p.handed != nullptr) {       // by a thread that has nothing else to do before the barrier
+        if (tid == 32 && !acquire_word(p.handed, kWaitLimitNs)) flags |= kDevWaitTimeout;
+        __syncthreads();
+    }
     build_prefix(p, s_prefix, flags, s_lens);  // contains __syncthreads
     // Everything above reads only what the caller passed (lengths) and writes only shared memory. This grid is launched
     // to overlap the end of the kernel before it in the stream (the pre-step kernel, or the merge kernel of the step
     // before, which still reads the partials): caches, windows and query rows are read, and the workspace is written,
     // only from here on.
-    if (!p.late_wait) grid_dependency_wait();
+    if (p.handed == nullptr) grid_dependency_wait();
     // The merge kernel may be set up from now on (it reads the gate logits, which the pre-step may have written, before
     // its own wait, hence not earlier); it waits for this grid to complete before it reads the partials.
     grid_launch_dependents();
     const int64_t T = s_prefix[p.B];
-    const int cta = blockIdx.x, nctas = plan_ctas(T, p.block_limit != nullptr ? min((int)gridDim.x, *p.block_limit) : (int)gridDim.x);
+    const int cta = blockIdx.x, nctas = plan_ctas(T, p.handed != nullptr ? min((int)gridDim.x, max(*p.block_limit, 1)) : (int)gridDim.x);
     if (cta == 0)
         for (int b = tid; b <= p.B; b += C::NTHREADS) p.prefix[b] = s_prefix[b];
     const bool in_plan = cta < nctas;
@@ -745,7 +749,7 @@ plt_decode_main_bf16(const __grid_constant__ CUtensorMap tmK, const __grid_const
         }
     }
     __syncthreads();
-    if (p.late_wait) grid_dependency_wait();
+    if (p.handed != nullptr) grid_dependency_wait();
 }
 
 }  // namespace plt

@@ -18,7 +18,13 @@ constexpr int kPrefixLead = 2;        // line positions that stand for starting 
 // sequences of two loops), 150 against 139 (128 of them behind 32768 tokens), and 40.4 against 41.2 for three groups of 8-bit caches.
 // Not every block need take part: the pass over the prefixes is bound by the tensor cores and its start, the one over the own caches
 // by memory and its start, so that the plan may leave some multiprocessors to the latter, which then runs at the same time.
+//
+// The plan reaches the kernels behind by release and acquire: its writer releases `ready[0]`, the pass over the own caches and the merge
+// acquire it before they read a word of the plan. (griddepcontrol.launch_dependents only lets them start: it makes nothing visible,
+// and a griddepcontrol.wait would have them wait for the prefixes' products.) The merge's last block to pass by, counted in ready[1],
+// sets both words back behind its griddepcontrol.wait, so that every call finds them 0.
 struct PrefixPlan {
+    uint32_t *ready;     // two words
     int32_t *begin;      // [groups + 1] first sequence of each group, clamped
     int32_t *len;        // [groups] tokens of each prefix, clamped; 0 where the group is empty
     int32_t *line;       // [groups + 1] first line position of each group's units

@@ -141,6 +141,7 @@ PLT_API plt_status plt_prefix_attn_create(const plt_prefix_attn_config* config, 
         return handle_fail(nullptr, g_prefix_error, PLT_ERR_OUT_OF_MEMORY, "cudaMalloc of %zu workspace bytes failed", bytes);
     }
     h->status = (uint32_t*)ws;
+    h->plan.ready = h->status + 1;
     int32_t* at = (int32_t*)(ws + 256);
     const int groups = config->max_groups + 1;
     h->plan.begin = at; at += groups;
@@ -153,7 +154,7 @@ PLT_API plt_status plt_prefix_attn_create(const plt_prefix_attn_config* config, 
     h->plan.win_lens = at;
     h->acc = (float*)(ws + ((plan_bytes(config) + 255) & ~(size_t)255));
     h->ml = h->acc + ((size_t)units_of(config, R) + sms) * kPrefixRows * config->d;
-    e = cudaMemset(ws, 0, 256);
+    e = cudaMemset(ws, 0, plan_bytes(config));
     if (e == cudaSuccess) e = cudaDeviceSynchronize();   // another stream may run first
     if (e != cudaSuccess) {
         cudaFree(ws);

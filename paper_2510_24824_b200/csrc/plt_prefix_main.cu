@@ -503,12 +503,14 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     // columns: S_A 0..127 in halves of 64 (its P over the first 32 of each, once the scores have been read), S_B 128..255, O_A from
     // 256, O_B from 384
     if (leaves) {
-        // The kernel behind this one reads the plan without a wait of its own: it is let go once the plan has been written.
+        // The kernels behind acquire the plan: this one is let go once it has been released.
         if (wid >= 4 && wid < 20) {
             leave_plan(p, plan, tid - 128, kLeavers);
-            __threadfence();
             named_barrier_sync(kBarLeft, kLeavers);
-            if (tid == 128) grid_launch_dependents();
+            if (tid == 128) {
+                release_word(p.plan.ready);
+                grid_launch_dependents();
+            }
         }
         if (reported) atomicOr(p.status, reported);
     }
@@ -993,6 +995,8 @@ __global__ void __launch_bounds__(kPlanThreads) plt_prefix_plan(const __grid_con
     leave_plan(p, from, tid, kPlanThreads);
     leave_lens(p, from, tid, kPlanThreads, tid < p.B ? p.seq_lens[tid] : 0, flags);
     if (flags) atomicOr(p.status, flags);
+    __syncthreads();
+    if (tid == 0) release_word(p.plan.ready);
 }
 
 template <int D, bool FP8>

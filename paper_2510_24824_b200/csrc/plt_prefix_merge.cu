@@ -14,6 +14,8 @@
 namespace plt {
 namespace {
 
+constexpr uint64_t kMergeWaitNs = 1000000000ull;
+
 // Warps of a block that hold 8 elements each of the same 32 rows, and warps that share one such piece (1: none).
 __host__ __device__ constexpr int merge_parts(int shares) { return shares == 1 ? 8 : shares == 4 ? 4 : 1; }
 
@@ -110,8 +112,11 @@ __global__ void __launch_bounds__(merge_parts(SHARES) * SHARES * 32, 2) plt_pref
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, share = SPLIT ? wid / PARTS : 0;
     const int part = blockIdx.z * PARTS + wid % PARTS;                        // elements 8 part .. 8 part + 7
     const int h = blockIdx.y;
+    bool last = false;
     if (wid == 0) {
-        // what the caller passed and the plan, complete since before the main kernel let this one go
+        // what the caller passed, and the plan, while the main kernel drains
+        if (!acquire_word(pp.plan.ready, kMergeWaitNs)) atomicOr(pp.status, kDevWaitTimeout);
+        if (lane == 0) last = atomicAdd(pp.plan.ready + 1, 1u) + 1 == gridDim.x * gridDim.y * gridDim.z;
         const int id = blockIdx.x * 32 + lane;
         const bool in = id < p.B * p.R;
         const int b = in ? small_div(id, p.R) : 0;
@@ -183,6 +188,7 @@ __global__ void __launch_bounds__(merge_parts(SHARES) * SHARES * 32, 2) plt_pref
     }
     __syncthreads();
     grid_dependency_wait();
+    if (last) pp.plan.ready[0] = pp.plan.ready[1] = 0;      // every block of the main kernel and of this one has acquired the plan
 
     // ---- one softmax over the prefix and the own keys, and the window's ---------------------------------------------------
     const bool does_own = !SPLIT || share == OWN, does_window = !SPLIT || share == WINDOW;

@@ -76,6 +76,23 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint64_t* bar, uint32_t parity
     return true;
 }
 
+// A word in device memory by which one thread of a grid lets threads of another see what its block has written (and
+// synchronised on): release and acquire at device scope. The reader waits for it to become 1, for at most ~limit_ns, and
+// returns false when it gave up.
+__device__ __forceinline__ void release_word(uint32_t* word) {
+    asm volatile("st.release.gpu.global.u32 [%0], 1;" ::"l"(word) : "memory");
+}
+__device__ __forceinline__ bool acquire_word(const uint32_t* word, uint64_t limit_ns) {
+    uint64_t t0 = 0;
+    for (uint32_t spins = 0;; ++spins) {
+        uint32_t x;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(x) : "l"(word) : "memory");
+        if (x == 1u) return true;
+        if (spins == 0) t0 = global_timer_ns();
+        else if ((spins & 0x3fu) == 0 && global_timer_ns() - t0 > limit_ns) return false;
+    }
+}
+
 // ---- TMA (tiled; every block issues its own loads) ----------------------------------------------
 __device__ __forceinline__ void tma_prefetch_desc(const CUtensorMap* m) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
