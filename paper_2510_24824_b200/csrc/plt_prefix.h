@@ -83,6 +83,13 @@ plt_status decode_encode_rows(plt_decode_attn_t h, CUtensorMap* map, const void*
 // (A division of whole numbers is a long piece of code, which a launch finds outside the instruction caches.)
 __device__ __forceinline__ int small_div(int a, int b) { return (int)__fdividef((float)a + 0.5f, (float)b); }
 
+// Keys (prefix and own) that a row sees of a sequence whose length was given as `given`, `capacity` at most: its loop lies delta
+// behind, `newer` tokens of the step are younger. No difference leaves 32 bits, whatever lengths and offsets are.
+__device__ __forceinline__ int row_sees(int given, int64_t capacity, int delta, int newer) {
+    const int n = (int)min((int64_t)max(given, 0), capacity);
+    return max(max(n - delta, 0) - newer, 0);
+}
+
 // Blocks that take part in a line of T positions: at least kPrefixMinLine positions each.
 constexpr int kPrefixMinLine = 3;
 __host__ __device__ inline int prefix_blocks(int T, int launched) {

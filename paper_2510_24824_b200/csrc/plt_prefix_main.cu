@@ -767,8 +767,8 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             const int mine = tiles_of(pc, x), step = pc.wide ? 1 : 2;
             auto sees_of = [&](int lr) {
                 if (lr >= pc.rows) return 0;
-                const int b = small_div(lr, p.R), lq = small_div(lr - b * p.R, p.G), l = small_div(lq, p.Qn), n = p.seq_lens[plan.begin[pc.g] + b];
-                return max(0, min(pc.len, (int)min((int64_t)n, (int64_t)pc.len + p.max_seq_len) - p.delta[l] - (p.Qn - 1 - (lq - l * p.Qn))));
+                const int b = small_div(lr, p.R), lq = small_div(lr - b * p.R, p.G), l = small_div(lq, p.Qn);
+                return min(pc.len, row_sees(p.seq_lens[plan.begin[pc.g] + b], (int64_t)pc.len + p.max_seq_len, p.delta[l], p.Qn - 1 - (lq - l * p.Qn)));
             };
             int sees0 = 0, sees1 = 0;
             if (mine > 0) {

@@ -143,10 +143,9 @@ __global__ void __launch_bounds__(merge_parts(SHARES) * SHARES * 32, 2) plt_pref
                 len = plan.len[lo];
             }
         }
-        const int n = (int)min((int64_t)pp.seq_lens[b], (int64_t)len + p.max_seq_len);
-        const int cut = max(0, n - p.delta[l] - newer), sees = min(cut, len);
+        const int cut = row_sees(pp.seq_lens[b], (int64_t)len + p.max_seq_len, p.delta[l], newer), sees = min(cut, len);
         const int wl = l > 0 ? plan.win_lens[b * (p.L - 1) + l - 1] : 0;
-        const bool has_own = in && plan.own_lens[b] - p.delta[l] - newer > 0, has_window = in && cut > 0 && wl > 0;
+        const bool has_own = in && plan.own_lens[b] - p.delta[l] > newer, has_window = in && cut > 0 && wl > 0;
         float gate = 0.f;
         if (l > 0) gate = 1.f / (1.f + expf(-p.gate_logits[(((int64_t)b * (p.L - 1) + (l - 1)) * p.Qn + (lq - l * p.Qn)) * p.Hq + head]));
         int64_t tile = 0;
