@@ -868,8 +868,9 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 s1 += __shfl_xor_sync(0xffffffffu, s1, o);
             }
             if ((lane & 3) < 2) {
+                // by the count of keys, not by the reference, which scores that are not numbers leave alone
                 const float m = (lane & 1) != 0 ? m1 : m0;
-                const bool saw = mine > 0 && m > kSeqNoMax;
+                const bool saw = mine > 0 && ((lane & 1) != 0 ? sees1 : sees0) > (pc.t0 + (pc.wide ? 0 : x)) * kPrefixTile;
                 *(float2*)(p.ml + ((slot * 2 + x) * 128 + row0 + 8 * (lane & 1)) * 2) = make_float2(saw ? m : -INFINITY, !saw ? 0.f : (lane & 1) != 0 ? s1 : s0);
             }
             if (mine > 0) {

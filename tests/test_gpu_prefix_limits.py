@@ -1,5 +1,6 @@
 """Shared prefixes on the GPU: the ends of what the arguments may be."""
 import pytest
+import torch
 
 from paper_2510_24824_b200 import binding as B
 from prefix_util import Problem
@@ -25,3 +26,21 @@ def test_offsets_that_no_length_reaches():
         assert p.run() == 0
         assert (p.out[:, 1] == 0).all()
         p.hold()
+
+
+# ---- queries that are not numbers ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kv", ["", "e4m3"])
+@pytest.mark.parametrize("n", [30, 700])
+def test_a_query_that_is_not_a_number_gives_none(kv, n):
+    """Its own row alone: softmax of scores that are not numbers is none either, wherever the keys lie."""
+    p = Problem(42, [0, 3, 0, 4], [n], [0, 4], kv=kv, Hq=8, Hkv=2)
+    ref = p.expect()
+    p.q[2, 0, 0, 5] = float("nan")
+    p.q[1, 0, 0, 2, 7] = float("nan")
+    assert p.run() == 0
+    assert torch.isnan(p.out[2, 0, 0, 5]).all() and torch.isnan(p.out[1, 0, 0, 2]).all()
+    bad = torch.zeros(p.out.shape, dtype=torch.bool, device="cuda")
+    bad[2, 0, 0, 5] = bad[1, 0, 0, 2] = True
+    assert torch.isfinite(p.out[~bad]).all()
+    p.out = torch.where(bad, ref[0].to(p.out.dtype), p.out)
+    p.hold(ref)
