@@ -28,7 +28,15 @@
 // the products, warp 1 owns the tensor memory; warp 2 makes the plan; warps 2, 20, 21 and 22 turn E4M3 codes into f16 (exact) in a second ring; warps
 // 4-11 and 12-19 are the softmax of A and of B, load their query rows and store the partials. A partial lies as [d / 4][128 rows][4].
 //
-// bf16 probabilities carry 8 bits, f16 ones (E4M3 caches) 11; their sum is taken before that rounding, in fp32.
+// bf16 probabilities carry 8 bits, f16 ones (E4M3 caches) 11; their sum is taken before that rounding, in fp32. Where one key holds a
+// large share of a row's weight, 8 bits show in the output (rows with a few dominant keys and large V came to 1.96 times the
+// framework's bound of 2e-2), so there bf16 probabilities are multiplied with V in two terms, p = hi + lo, hi = bf16(p), lo = bf16(p -
+// hi), as in the decode step's kernel. Scores above a limit, a share of the row's sum when it was last taken, send a warp the longer
+// way, with the vote that lets a reference move: it takes the sum anew and, where a probability is above the share of it, leaves lo
+// behind hi in tensor memory and sets a flag, by which the issuing warp adds a second product on the lanes of the warps that did (the
+// others' lanes are masked off). That way costs 36.5 us instead of 34.0 (64 sequences of two loops behind 4096 tokens), 149.5 instead
+// of 142 (128 behind 32768), 16.1 instead of 15.6 (two users): the first halves of a piece take it, and scores outrun the limit now
+// and then until the sum has grown.
 // Every wait is bounded and reports through the status word.
 #include <cuda_bf16.h>
 
@@ -50,8 +58,8 @@ struct PCfg {
     // (S, P and PV: of tile x and half h at 2 x + h)
     static constexpr int QFULL = 0, QRAW = 2, FULL = 4, EMPTY = FULL + RING, RFULL = EMPTY + RING, REMPTY = RFULL + RAW, SFULL = REMPTY + RAW,
                          PFULL = SFULL + 4, PVDONE = PFULL + 4, ODONE = PVDONE + 4, COUNT = ODONE + 2;
-    // tiles, barriers, control words, the plan
-    static constexpr size_t SMEM = 1024 + 2 * TILE + (size_t)RING * TILE + (size_t)RAW * RAW_TILE + COUNT * 8 + 64 + (5 * (kNearGroups + 1) + 4) * 4;
+    // tiles, barriers, control words, the plan, the softmax's flags
+    static constexpr size_t SMEM = 1024 + 2 * TILE + (size_t)RING * TILE + (size_t)RAW * RAW_TILE + COUNT * 8 + 64 + (5 * (kNearGroups + 1) + 4 + 8) * 4;
 };
 
 template <bool FP8>
@@ -335,6 +343,10 @@ template <bool FP8>
 constexpr float kAbove = FP8 ? 14.f : 8.f;
 template <bool FP8>
 constexpr float kBelow = FP8 ? 8.f : 0.f;
+// Share of a row's sum, as 2^-kShareBits, from which on a bf16 probability has a second term. The largest error on sharply peaked
+// rows is 0.88 of the bound (the result's rounding) for shares of 1/4, 0.35 and 1/2, and 1.43 for 0.66; 64 sequences of two loops behind
+// 4096 tokens take 37.0, 36.5, 36.1 and 35.7 us.
+constexpr float kShareBits = 1.5f;
 
 // 64 columns of 16 lanes, as above.
 __device__ __forceinline__ void tmem_ld_rows16(uint32_t taddr, uint32_t (&r)[32]) {
@@ -355,6 +367,21 @@ __device__ __forceinline__ void tmem_st_pairs16(uint32_t taddr, const uint32_t (
                  "r"(r[13]), "r"(r[14]), "r"(r[15])
                  : "memory");
 }
+// Sum over a row's four threads.
+__device__ __forceinline__ float row_sum(float y) {
+    y += __shfl_xor_sync(0xffffffffu, y, 1);
+    return y + __shfl_xor_sync(0xffffffffu, y, 2);
+}
+// D[tmem] += A[tmem] * B[smem] on the lanes whose bits in `off` are 0 (bit i of word w: lane 32 w + i).
+__device__ __forceinline__ void umma_bf16_ts_lanes(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint4 off) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.eq.b32 p, 0, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%4, %5, %6, %7}, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(off.x), "r"(off.y), "r"(off.z), "r"(off.w)
+        : "memory");
+}
+
 // 16 columns of 16 lanes, to be scaled: row r's by f0, row r + 8's by f1.
 __device__ __forceinline__ void tmem_scale_rows16(uint32_t taddr, float f0, float f1) {
     uint32_t r[8];
@@ -412,9 +439,9 @@ __device__ __forceinline__ float2 exp2_by_fma(float2 t) {
     return EXACT0 ? __fadd2_rn(e, make_float2(least, least)) : e;
 }
 
-// Scores -> probabilities, packed 16 bits wide, and their sums.
-template <bool FP8>
-__device__ __forceinline__ void p_half(const uint32_t (&r)[32], float scale, float m0, float m1, uint32_t (&pk)[16], float2& sum0, float2& sum1) {
+// Scores -> probabilities, packed 16 bits wide, and their sums. KEEP: in fp32 they take the scores' place.
+template <bool FP8, bool KEEP>
+__device__ __forceinline__ void p_half(uint32_t (&r)[32], float scale, float m0, float m1, uint32_t (&pk)[16], float2& sum0, float2& sum1) {
     const float2 sc2 = make_float2(scale, scale), nm0 = make_float2(-m0, -m0), nm1 = make_float2(-m1, -m1);
 #pragma unroll
     for (int g = 0; g < 8; ++g)
@@ -425,7 +452,17 @@ __device__ __forceinline__ void p_half(const uint32_t (&r)[32], float scale, flo
             float2& s = k == 0 ? sum0 : sum1;
             s = __fadd2_rn(s, pr);
             pk[2 * g + k] = FP8 ? pack_f16x2(pr.x, pr.y) : pack_bf16x2(pr.x, pr.y);
+            if (KEEP) {
+                r[4 * g + 2 * k] = __float_as_uint(pr.x);
+                r[4 * g + 2 * k + 1] = __float_as_uint(pr.y);
+            }
         }
+}
+// What rounding the probabilities p to bf16 (pk) dropped, in the place of the first half of p.
+__device__ __forceinline__ void p_second(uint32_t (&p)[32], const uint32_t (&pk)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        p[i] = pack_bf16x2(__uint_as_float(p[2 * i]) - __uint_as_float(pk[i] << 16), __uint_as_float(p[2 * i + 1]) - __uint_as_float(pk[i] & 0xffff0000u));
 }
 
 template <int D, bool FP8>
@@ -442,6 +479,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     uint64_t* bars = (uint64_t*)(raw + (size_t)C::RAW * C::RAW_TILE);
     int32_t* s_ctl = (int32_t*)(bars + C::COUNT);                  // [0] abort flag, [1] tensor-memory base, [2] loads issued
     int32_t* s_plan = s_ctl + 16;                                  // begin, len, line, unit, piece: [kNearGroups + 1] each; chunk
+    volatile uint8_t* s_lo = (uint8_t*)(s_plan + 5 * (kNearGroups + 1) + 4);       // [tile][half][warp]: 1: the warp has left second terms
     volatile int* abort_flag = (volatile int*)s_ctl;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
 
@@ -472,6 +510,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         mbar_fence_init();
     }
     if (wid == 1) tmem_alloc((uint32_t*)&s_ctl[1], 512);
+    if (wid == 3) s_lo[lane] = 0;
     // Few groups: this kernel is an ordinary launch, each block makes the plan for itself, and the last one leaves it for the kernels
     // behind. Many: it starts behind the plan kernel's start and waits for its end.
     const bool near = p.groups <= kNearGroups, leaves = near && blockIdx.x + 1 == gridDim.x;
@@ -633,6 +672,18 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 if (one_thread()) {
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) umma_bf16_ts(to, from + kk * 8, v0 + (uint64_t)(kk * 2048 >> 4), idesc_pv, kk > 0 ? 1u : more);
+                    // the flags are read while these products run
+                    uint32_t low = 0, high = 0;        // of the warps with the lower and the upper 16 lanes of each quarter, a byte each
+                    if (!FP8) {
+                        low = *(volatile uint32_t*)(s_lo + (2 * x + h) * 8);
+                        high = *(volatile uint32_t*)(s_lo + (2 * x + h) * 8 + 4);
+                    }
+                    if ((low | high) != 0) {
+                        auto off = [&](int quarter) { return ~((low >> (8 * quarter) & 1u) * 0xffffu | (high >> (8 * quarter) & 1u) * 0xffff0000u); };
+                        const uint4 mask = make_uint4(off(0), off(1), off(2), off(3));
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk) umma_bf16_ts_lanes(to, from + 32 + kk * 8, v0 + (uint64_t)(kk * 2048 >> 4), idesc_pv, mask);
+                    }
                     commit_to(done_bar);
                     if (h == 1) {
                         commit_to(free_bar);
@@ -760,7 +811,7 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         const int row0 = wq * 32 + half * 16 + (lane >> 2);        // rows whose scores it has: this one and 8 on
         const uint32_t lane_off = (uint32_t)(wq * 32 + half * 16) << 16;
         const uint32_t tS = tmem_base + lane_off + x * 128, tO = tmem_base + lane_off + 256 + x * 128;
-        uint32_t s_parity = 0, o_parity = 0, r_parity = 0;
+        uint32_t s_parity = 0, o_parity = 0, r_parity = 0, told = 0;       // told: bit h: the flag of half h is set
         while (ok && walk.next(p, plan, pc)) {
             // ---- a row's query, and how many tokens of the prefix the two rows see -----------------------------------
             const int first_row = pc.m * kPrefixRows + (pc.wide ? x * 128 : 0);
@@ -811,17 +862,16 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                 sees1 = sees_of(first_row + row0 + 8);
             }
             const float scale = FP8 ? fmaxf(p.scale_log2 * p.k_scale[pc.h], 1e-30f) : p.scale_log2;     // above 0: -inf has to stay that
-            float m0 = kSeqNoMax, m1 = kSeqNoMax;
+            float m0 = kSeqNoMax, m1 = kSeqNoMax, most0 = 0.f, most1 = 0.f;      // most (bf16): scores above it take a longer way
             float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
             const int all_see = __reduce_min_sync(0xffffffffu, min(sees0, sees1));
             for (int i = 0; i < mine; ++i) {
                 const int t = pc.t0 + (pc.wide ? 0 : x) + i * step;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                auto half_tile = [&](int h) {
                     const bool first = i == 0 && h == 0;
                     ok = seq_wait(&bars[C::SFULL + 2 * x + h], s_parity, abort_flag);
                     ok = __all_sync(0xffffffffu, ok);      // the tensor-memory accesses below are collective over the warp
-                    if (!ok) break;
+                    if (!ok) return;
                     tc_fence_after_sync();
                     uint32_t r[32];
                     tmem_ld_rows16(tS + h * 64, r);
@@ -829,31 +879,57 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                     tmem_wait_ld();
                     if (key + 64 > all_see) p_mask(r, sees0 - key - 2 * (lane & 3), sees1 - key - 2 * (lane & 3));
                     const float top0 = p_max<0>(r) * scale, top1 = p_max<2>(r) * scale;
-                    if (__any_sync(0xffffffffu, first || top0 > m0 + kAbove<FP8> || top1 > m1 + kAbove<FP8>)) {
-                        const float n0 = fmaxf(m0, row_max(top0) - kBelow<FP8>), n1 = fmaxf(m1, row_max(top1) - kBelow<FP8>);
-                        const float f0 = fast_exp2(m0 - n0), f1 = fast_exp2(m1 - n1);
-                        m0 = n0;
-                        m1 = n1;
-                        sum0 = make_float2(sum0.x * f0, sum0.y * f0);
-                        sum1 = make_float2(sum1.x * f1, sum1.y * f1);
-                        if (!first) {
-                            // O against the new reference, once the product of the half before has completed. (The one before that
-                            // on the same barrier has: this warp has seen scores that were issued behind it.)
-                            ok = seq_wait(&bars[C::PVDONE + 2 * x + (h ^ 1)], s_parity ^ (uint32_t)(h ^ 1), abort_flag);
-                            ok = __all_sync(0xffffffffu, ok);
-                            if (!ok) break;
-                            tc_fence_after_sync();
+                    uint32_t pk[16];
+                    const bool high = first || top0 > (FP8 ? m0 + kAbove<FP8> : most0) || top1 > (FP8 ? m1 + kAbove<FP8> : most1);
+                    const bool slow = __any_sync(0xffffffffu, high || (!FP8 && (told >> h & 1u) != 0));
+                    if (slow) {
+                        if (FP8 || __any_sync(0xffffffffu, first || top0 > m0 + kAbove<FP8> || top1 > m1 + kAbove<FP8>)) {
+                            const float n0 = fmaxf(m0, row_max(top0) - kBelow<FP8>), n1 = fmaxf(m1, row_max(top1) - kBelow<FP8>);
+                            const float f0 = fast_exp2(m0 - n0), f1 = fast_exp2(m1 - n1);
+                            m0 = n0;
+                            m1 = n1;
+                            sum0 = make_float2(sum0.x * f0, sum0.y * f0);
+                            sum1 = make_float2(sum1.x * f1, sum1.y * f1);
+                            if (!first) {
+                                // O against the new reference, once the product of the half before has completed. (The one before that
+                                // on the same barrier has: this warp has seen scores that were issued behind it.)
+                                ok = seq_wait(&bars[C::PVDONE + 2 * x + (h ^ 1)], s_parity ^ (uint32_t)(h ^ 1), abort_flag);
+                                ok = __all_sync(0xffffffffu, ok);
+                                if (!ok) return;
+                                tc_fence_after_sync();
 #pragma unroll 1
-                            for (int c = 0; c < D / 16; ++c) tmem_scale_rows16(tO + c * 16, f0, f1);
+                                for (int c = 0; c < D / 16; ++c) tmem_scale_rows16(tO + c * 16, f0, f1);
+                            }
+                        }
+                        if (!FP8) {
+                            p_half<FP8, true>(r, scale, m0, m1, pk, sum0, sum1);
+                            const float all0 = row_sum(sum0.x + sum0.y) * exp2f(-kShareBits), all1 = row_sum(sum1.x + sum1.y) * exp2f(-kShareBits);
+                            const bool second = __any_sync(0xffffffffu, fast_exp2(top0 - m0) > all0 || fast_exp2(top1 - m1) > all1);
+                            most0 = m0 + fminf(__log2f(all0), kAbove<FP8>);
+                            most1 = m1 + fminf(__log2f(all1), kAbove<FP8>);
+                            if (second) {
+                                p_second(r, pk);
+                                tmem_st_pairs16(tS + h * 64 + 32, (const uint32_t(&)[16])r);
+                            }
+                            told = (told & ~(1u << h)) | (uint32_t)second << h;
+                            if (lane == 0) s_lo[(2 * x + h) * 8 + half * 4 + wq] = second;
                         }
                     }
-                    uint32_t pk[16];
-                    p_half<FP8>(r, scale, m0, m1, pk, sum0, sum1);
+                    if (FP8 || !slow) p_half<FP8, false>(r, scale, m0, m1, pk, sum0, sum1);
                     tmem_st_pairs16(tS + h * 64, pk);
                     tmem_wait_st();
                     tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bars[C::PFULL + 2 * x + h]);
+                };
+                // halves one behind the other in the code only where it is short enough: with second terms a copy for each took 149.0 us
+                // against 148.7 (128 sequences behind 32768 tokens), 37.1 against 36.5 (64 behind 4096); 8-bit caches 42.4 against 44.1
+                if constexpr (FP8) {
+                    half_tile(0);
+                    if (ok) half_tile(1);
+                } else {
+#pragma unroll 1
+                    for (int h = 0; h < 2 && ok; ++h) half_tile(h);
                 }
                 if (!ok) break;
                 s_parity ^= 1u;
