@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(kVerifyThreads) plt_draft_verify_pick(const __
         p.tokens[(int64_t)b * (p.K + 1) + j] = j < stand.x ? p.draft_tokens[(int64_t)b * p.K + j] : j == stand.x ? token : -1;
     if (tid == 0) {
         p.num_accepted[b] = stand.x;
-        if (p.new_lens != nullptr) p.new_lens[b] = max(0, p.seq_lens[b] - (p.K - stand.x));
+        if (p.new_lens != nullptr) p.new_lens[b] = max(0, max(p.seq_lens[b], 0) - (p.K - stand.x));
         if (token < 0) atomicOr(p.status, kDevNoProbability);
     }
 }
