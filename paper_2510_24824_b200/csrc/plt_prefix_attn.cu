@@ -54,11 +54,21 @@ plt_status decode_config(const plt_prefix_attn_config* c, plt_decode_attn_config
     return PLT_OK;
 }
 
-// Units of a full batch: every group may end inside one. (The configuration has passed the decode step's checks.)
+// Units of a full batch: every group that has a sequence may end inside one. (The configuration has passed the decode step's checks.)
 int64_t units_of(const plt_prefix_attn_config* c, int R) {
-    return (int64_t)c->Hkv * (((int64_t)c->max_batch * R + kPrefixRows - 1) / kPrefixRows + c->max_groups);
+    const int groups = c->max_groups < c->max_batch ? c->max_groups : c->max_batch;
+    return (int64_t)c->Hkv * (((int64_t)c->max_batch * R + kPrefixRows - 1) / kPrefixRows + groups);
 }
 int rows_of(const plt_prefix_attn_config* c) { return c->L * (c->q_len > 1 ? c->q_len : 1) * (c->Hq / c->Hkv); }
+
+// The line of all units' key tiles and the rows of the output have to fit the kernels' whole numbers.
+plt_status check_plan(const plt_prefix_attn_config* c) {
+    const int R = rows_of(c);
+    if ((double)units_of(c, R) * ((double)c->max_prefix_len / kPrefixTile + 1 + kPrefixLead) >= 2147483647.0 ||
+        (double)c->max_batch * R * c->Hkv >= 1073741824.0)
+        return prefix_fail(nullptr, PLT_ERR_UNSUPPORTED, "max_batch * max_prefix_len too large for the tile plan");
+    return PLT_OK;
+}
 
 size_t plan_bytes(const plt_prefix_attn_config* c) {
     return 256 + 4 * ((size_t)5 * (c->max_groups + 1) + 3 + (size_t)c->max_batch * c->L);
@@ -81,6 +91,8 @@ PLT_API plt_status plt_prefix_attn_workspace_bytes(const plt_prefix_attn_config*
     size_t own = 0;
     s = plt_decode_attn_workspace_bytes(&d, &own);
     if (s != PLT_OK) return from_decode(nullptr, s);
+    s = check_plan(config);
+    if (s != PLT_OK) return s;
     int sms = 148;
     cudaDeviceProp prop;
     if (cudaGetDeviceProperties(&prop, config->device) == cudaSuccess) sms = prop.multiProcessorCount;
@@ -99,9 +111,8 @@ PLT_API plt_status plt_prefix_attn_create(const plt_prefix_attn_config* config, 
     s = plt_decode_attn_workspace_bytes(&d, &own);      // all of the decode step's checks, without a device
     if (s != PLT_OK) return from_decode(nullptr, s);
     const int R = rows_of(config);
-    if ((double)units_of(config, R) * ((double)config->max_prefix_len / kPrefixTile + 1 + kPrefixLead) >= 2147483647.0 ||
-        (double)config->max_batch * R * config->Hkv >= 1073741824.0)
-        return prefix_fail(nullptr, PLT_ERR_UNSUPPORTED, "max_batch * max_prefix_len too large for the tile plan");
+    s = check_plan(config);
+    if (s != PLT_OK) return s;
     DeviceScope scope(config->device);
     if (scope.err != cudaSuccess) {
         (void)cudaGetLastError();
