@@ -499,6 +499,8 @@ def plt_seq_attn_destroy(handle) -> None:
 # ---- differential attention (plt_diff_attn.h) ---------------------------------------------------------------------
 def _offsets(c, loop_offset: Optional[Sequence[int]]) -> None:
     if loop_offset is not None:
+        if len(loop_offset) < c.L:
+            raise ValueError(f"loop_offset: {c.L} entries are needed, not {len(loop_offset)}")
         arr = (ctypes.c_int32 * len(loop_offset))(*[int(x) for x in loop_offset])
         c._keep = arr
         c.loop_offset = ctypes.cast(arr, ctypes.POINTER(ctypes.c_int32))
@@ -767,6 +769,8 @@ def make_rope_config(dtype, max_batch: int, L: int, Hq: int, Hkv: int, d: int, m
     c.theta, c.factor, c.low, c.high = theta, factor, low, high
     _offsets(c, loop_offset)
     if inv_freq is not None:
+        if len(inv_freq) < (rotary_dim or d) // 2:
+            raise ValueError(f"inv_freq: {(rotary_dim or d) // 2} entries are needed, not {len(inv_freq)}")
         c._keep_freq = (ctypes.c_double * len(inv_freq))(*[float(x) for x in inv_freq])
         c.inv_freq = ctypes.cast(c._keep_freq, ctypes.POINTER(ctypes.c_double))
     return c
