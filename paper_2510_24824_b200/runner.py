@@ -427,9 +427,19 @@ class Rope:
                 dtype, lead, per = want[name]
                 _dense(name, t.view(1, -1) if name.endswith("gain") and t.is_contiguous() else t, dtype, lead, per)
 
+    def _caches(self, dp: DeviceProblem, n: int, kv_strides=(0, 0, 0)):
+        """Refuses caches that n sequences of this handle would be written past the end of, or elsewhere than they lie."""
+        p, c = dp.problem, self.config
+        has, needs = (p.L, p.Hkv, p.d, p.w if p.L > 1 else 0, p.page_size), (c.L, c.Hkv, c.d, c.w if c.L > 1 else 0, c.page_size)
+        dense = not c.page_size and not any(kv_strides)
+        if p.B < n or p.max_seq_len < c.max_seq_len or (dense and p.max_seq_len != c.max_seq_len) or has != needs:
+            raise ValueError(f"caches of {n} sequences of {c.max_seq_len} tokens and (L, Hkv, d, w, page_size) = {needs} are needed, not of "
+                             f"{p.B} of {p.max_seq_len} and {has}")
+
     def step_args(self, dp: DeviceProblem, q, k_new, v_new, q_out=None, q_gain=None, k_gain=None, prefix_lens=None, w_gate=None,
                   b_gate=None, gate_logits=None, kv_strides=(0, 0, 0)):
         p, c = dp.problem, self.config
+        self._caches(dp, p.B, kv_strides)
         q_out = dp.q if q_out is None else q_out
         strides = [self._rows(name, t, p.B, h) for name, t, h in (("q", q, c.Hq), ("k_new", k_new, c.Hkv), ("v_new", v_new, c.Hkv))]
         _dense("q_out", q_out, self._act(), p.B, c.L * max(1, c.q_len) * c.Hq * c.d)
@@ -461,6 +471,8 @@ class Rope:
             if t is not None:
                 _dense(name, t, self._act(), n, per)
         self._small(n, q_gain=q_gain, k_gain=k_gain, seq_lens=seq_lens, start=start, prefix_lens=prefix_lens)
+        if dp is not None:
+            self._caches(dp, n, kv_strides)
         cache = {} if dp is None else dict(
             k_cache=dp.k_cache, v_cache=dp.v_cache, page_table=dp.page_table, max_pages=dp.problem.max_pages,
             num_pool_pages=dp.problem.num_pool_pages, k_scale=dp.k_scale, v_scale=dp.v_scale, kv_strides=kv_strides)
