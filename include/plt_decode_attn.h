@@ -86,6 +86,8 @@ typedef enum {
 #define PLT_DEV_PAGE_ID_CLAMPED 2u  /* a page id was outside [0, num_pool_pages) */
 #define PLT_DEV_WAIT_TIMEOUT 4u     /* a bounded wait inside a kernel ran out; the output is not valid */
 #define PLT_DEV_WIN_LEN_CLAMPED 8u  /* a win_lens entry was outside [0, w] */
+#define PLT_DEV_GROUP_CLAMPED 128u  /* plt_prefix_attn.h: a group_begin entry was below the one before or above the batch, or a prefix
+                                       length outside [0, max_prefix_len]; plt_rope.h: a prefix length or a start below 0 */
 
 /*
  * Fixed at create.  struct_size = sizeof(plt_decode_attn_config) (versioning).

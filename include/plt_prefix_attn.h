@@ -29,10 +29,6 @@ extern "C" {
 
 typedef struct plt_prefix_attn* plt_prefix_attn_t; /* opaque; owned by the library */
 
-/* A further bit of the device status word. */
-#define PLT_DEV_GROUP_CLAMPED 128u /* a group_begin entry was below the one before or above the batch, or a prefix length outside
-                                      [0, max_prefix_len] */
-
 /*
  * Fixed at create.  struct_size = sizeof(plt_prefix_attn_config).  Fields that plt_decode_attn_config has too mean the same and
  * have the same limits.  dtype is PLT_BF16 (the prefix's products run on the tensor cores).

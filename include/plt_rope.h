@@ -101,9 +101,9 @@ typedef struct {
     void* v_cache;
     int64_t kv_stride_b, kv_stride_n, kv_stride_h;
     const int32_t* seq_lens;       /* [B] tokens of each sequence, the prefix and this step's counted; values outside
-                                      [0, prefix + max_seq_len] are clamped and flagged */
+                                      [0, prefix + max_seq_len] are clamped and flagged (PLT_DEV_SEQ_LEN_CLAMPED) */
     const int32_t* prefix_lens;    /* [B] tokens in front of this cache's first one, or NULL: 0; values below 0 are clamped and
-                                      flagged */
+                                      flagged (PLT_DEV_GROUP_CLAMPED) */
     const int32_t* page_table;
     int32_t max_pages, num_pool_pages;
     void* k_win;                   /* [B, L-1, w, Hkv, d]; both are written (NULL allowed when L == 1) */
@@ -137,8 +137,10 @@ typedef struct {
     void* k_loc_out;
     const float* q_gain;
     const float* k_gain;
-    const int32_t* seq_lens;       /* [B] rows of each sequence; values outside [0, T] are clamped and flagged */
-    const int32_t* start;          /* [B] position of row 0, or NULL: 0; values below 0 are clamped and flagged */
+    const int32_t* seq_lens;       /* [B] rows of each sequence; values outside [0, T] are clamped and flagged
+                                      (PLT_DEV_SEQ_LEN_CLAMPED) */
+    const int32_t* start;          /* [B] position of row 0, or NULL: 0; values below 0 are clamped and flagged
+                                      (PLT_DEV_GROUP_CLAMPED) */
     const int32_t* prefix_lens;    /* as above */
     void* k_cache;                 /* as above, or NULL (with v_cache) */
     void* v_cache;

@@ -58,7 +58,7 @@ inline plt_status handle_check(HandleBase* h, char* none, cudaStream_t stream, u
                        (bits & kDevWinLenClamped) ? " win_lens entry out of range (clamped)" : "",
                        (bits & kDevTokenRange) ? " drafted token out of range (refused)" : "",
                        (bits & kDevNoProbability) ? " a row without probabilities" : "",
-                       (bits & kDevGroupClamped) ? " a group's bounds or prefix length out of range (clamped)" : "");
+                       (bits & kDevGroupClamped) ? " a group's bounds, a prefix length or a start out of range (clamped)" : "");
 }
 
 inline bool misaligned(const void* p, uintptr_t unit) { return ((uintptr_t)p & (unit - 1)) != 0; }

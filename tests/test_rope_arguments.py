@@ -1,10 +1,15 @@
 """CPU checks of what the binding and the runner make of a rotation's arguments (no compute call is made)."""
+import subprocess
+from pathlib import Path
+
 import pytest
 import torch
 
 from paper_2510_24824_b200 import binding as B
 from paper_2510_24824_b200.inputs import make_problem
 from paper_2510_24824_b200.runner import DeviceProblem, Rope
+
+ROOT = Path(__file__).resolve().parents[1]
 
 
 def test_lists_that_are_too_short_are_refused_before_c_reads_them():
@@ -39,3 +44,12 @@ def test_caches_that_a_handle_would_write_past_are_refused():
     o._caches(longer, 2, (96 * 4 * 128, 4 * 128, 128))
     o._caches(dp, 2)
     o._caches(dp, 1)
+
+
+def test_the_header_names_every_bit_that_a_check_can_return(tmp_path):
+    bits = ["PLT_DEV_SEQ_LEN_CLAMPED", "PLT_DEV_PAGE_ID_CLAMPED", "PLT_DEV_GROUP_CLAMPED"]
+    (tmp_path / "bits.c").write_text(f'#include "{ROOT}/include/plt_rope.h"\n#include <stdio.h>\nint main(void) {{\n' +
+                                     "".join(f'    printf("%u\\n", {b});\n' for b in bits) + "    return 0;\n}\n")
+    subprocess.run(["gcc", "-std=c11", "-Wall", "-Werror", "-o", str(tmp_path / "bits"), str(tmp_path / "bits.c")], check=True)
+    out = subprocess.run([str(tmp_path / "bits")], capture_output=True, text=True, check=True).stdout.split()
+    assert [int(x) for x in out] == [getattr(B, b) for b in bits]
