@@ -26,10 +26,10 @@ namespace {
 constexpr int kVerifyThreads = 256;
 template <typename T>
 constexpr int kVecs = sizeof(T) == 4 ? 4 : 2;   // vectors of 16 bytes that a lane takes of a row's chunk: 16 elements
-// Chunks up to which the sums' warps count the drafts that stand themselves (about as many as the device holds warps), instead of a
-// kernel before them: 64 chunks 5.5 us against 6.3, 4096 7.2 against 8.2, 8192 9.9 against 10.4; 16384 16.5 against 16.2, 65536 44.6
-// against 39.4.
-constexpr int kAtOnce = 148 * 64;
+// Chunks of a multiprocessor up to which the sums' warps count the drafts that stand themselves (about as many as it holds warps),
+// instead of a kernel before them: 64 chunks in all 5.5 us against 6.3, 4096 7.2 against 8.2, 8192 9.9 against 10.4; 16384 16.5 against
+// 16.2, 65536 44.6 against 39.4.
+constexpr int kAtOnce = 64;
 constexpr int kMaxDrafts = 64;
 
 thread_local char g_verify_error[512] = "";
@@ -40,6 +40,7 @@ struct plt_draft_verify : HandleBase {
     plt_draft_verify_config cfg;
     double* sums = nullptr;      // [batch, chunks] of a call
     int2* stand = nullptr;       // [batch] drafts that stand, drafts there were
+    int sms = 0;
 };
 
 namespace {
@@ -396,11 +397,11 @@ cudaError_t launch(F fn, dim3 grid, bool overlap, const VerifyParams& p, cudaStr
 }
 
 template <typename T, bool VEC>
-cudaError_t launch_all(const VerifyParams& p, cudaStream_t stream) {
+cudaError_t launch_all(const VerifyParams& p, int sms, cudaStream_t stream) {
     constexpr int W = kVerifyThreads / 32;
     const dim3 grid((unsigned)((p.chunks + W - 1) / W), (unsigned)p.B);
     cudaError_t e;
-    if ((int64_t)p.chunks * p.B <= kAtOnce) {
+    if ((int64_t)p.chunks * p.B <= (int64_t)kAtOnce * sms) {
         e = launch(plt_draft_verify_sums<T, VEC, true>, grid, false, p, stream);
     } else {
         e = launch(plt_draft_verify_count<T>, dim3((unsigned)((p.B + W - 1) / W)), false, p, stream);
@@ -459,12 +460,14 @@ PLT_API plt_status plt_draft_verify_create(const plt_draft_verify_config* config
         (void)cudaGetLastError();
         return handle_fail(nullptr, g_verify_error, PLT_ERR_CUDA, "cudaSetDevice: %s", cudaGetErrorString(scope.err));
     }
-    s = check_device(config->device, g_verify_error, nullptr);
+    int sms = 0;
+    s = check_device(config->device, g_verify_error, &sms);
     if (s != PLT_OK) return s;
     plt_draft_verify* h = new (std::nothrow) plt_draft_verify();
     if (!h) return verify_fail(nullptr, PLT_ERR_OUT_OF_MEMORY, "host allocation failed");
     h->cfg = *config;
     h->device = config->device;
+    h->sms = sms;
     const size_t bytes = workspace_of(config);
     void* ws = nullptr;
     if (cudaMalloc(&ws, bytes) != cudaSuccess) {
@@ -537,8 +540,8 @@ PLT_API plt_status plt_draft_verify_run(plt_draft_verify_t h, const plt_draft_ve
     if (scope.err != cudaSuccess) return handle_fail(h, g_verify_error, PLT_ERR_CUDA, "cudaSetDevice: %s", cudaGetErrorString(scope.err));
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     cudaError_t e;
-    if (c.dtype == PLT_F32) e = vec ? launch_all<float, true>(p, stream) : launch_all<float, false>(p, stream);
-    else e = vec ? launch_all<__nv_bfloat16, true>(p, stream) : launch_all<__nv_bfloat16, false>(p, stream);
+    if (c.dtype == PLT_F32) e = vec ? launch_all<float, true>(p, h->sms, stream) : launch_all<float, false>(p, h->sms, stream);
+    else e = vec ? launch_all<__nv_bfloat16, true>(p, h->sms, stream) : launch_all<__nv_bfloat16, false>(p, h->sms, stream);
     if (e != cudaSuccess) return handle_fail(h, g_verify_error, PLT_ERR_CUDA, "launching the kernels: %s", cudaGetErrorString(e));
     return PLT_OK;
 }

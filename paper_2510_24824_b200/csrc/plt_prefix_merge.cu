@@ -303,8 +303,8 @@ cudaError_t launch_for(const Params& p, const PrefixParams& pp, bool overlap, cu
     // short prefixes lose half a microsecond).
     const int64_t warps = (int64_t)(p.B * p.R + 31) / 32 * p.Hkv * (D / 8);
     const int pieces = min(pp.blocks / p.Hkv, (pp.max_prefix_len + kPrefixTile - 1) / kPrefixTile);      // of a unit, at most
-    if (warps * 16 <= 148 * 32 && pieces > 8) return launch<D, 16>(p, pp, overlap, stream);
-    return warps * 4 <= 148 * 32 ? launch<D, 4>(p, pp, overlap, stream) : launch<D, 1>(p, pp, overlap, stream);
+    if (warps * 16 <= pp.blocks * 32 && pieces > 8) return launch<D, 16>(p, pp, overlap, stream);
+    return warps * 4 <= pp.blocks * 32 ? launch<D, 4>(p, pp, overlap, stream) : launch<D, 1>(p, pp, overlap, stream);
 }
 
 }  // namespace

@@ -39,6 +39,7 @@ struct plt_rope : HandleBase {
     plt_rope_config cfg;
     int32_t delta[kMaxLoops];
     int rd, Qn;
+    int sms = 0;
     uint64_t* turns = nullptr;        // [rd / 2] fractions of a turn per position, in units of 2^-64
 };
 
@@ -615,10 +616,10 @@ plt_status common(plt_rope_t h, int32_t batch, const int32_t* page_table, int32_
 //     128 44.1 against 54.8, 8 + 8 of 128 79.6 against 76.7; one prompt of 1000 rows of 3 + 1 heads of 128 6.0 against 4.3.
 //   - 2 where blocks of 8 are few, since a block walks over its heads: one prompt of 60 rows, 32 + 8 heads of 128 in bf16 3.9 us against
 //     7.3 with 8, of 300 rows 4.5 against 7.5; 1000 rows of 16 + 4 heads 6.3 against 5.3.
-int tokens_of_block(const RopeParams& p, int row_bytes) {
+int tokens_of_block(const RopeParams& p, int row_bytes, int sms) {
     const int64_t prompts = (int64_t)p.B * p.L;
     if (prompts * ((p.T + 7LL) / 8) <= 64) return 2;
-    return (p.Hq + p.Hkv) * row_bytes <= 2560 && prompts * ((p.T + 31LL) / 32) >= 3 * 148 ? 32 : 8;
+    return (p.Hq + p.Hkv) * row_bytes <= 2560 && prompts * ((p.T + 31LL) / 32) >= 3 * sms ? 32 : 8;
 }
 
 // A prompt's rows in blocks of TB tokens.
@@ -629,31 +630,31 @@ void launch_seq(const RopeParams& p, cudaStream_t stream) {
 }
 
 template <typename T, bool FP8, int D, bool INTER>
-void launch_one(bool seq, const RopeParams& p, cudaStream_t stream) {
+void launch_one(bool seq, const RopeParams& p, int sms, cudaStream_t stream) {
     if (!seq) {
         plt_rope_step_kernel<T, FP8, D, INTER><<<p.B * p.L * p.Qn, kRopeThreads, 0, stream>>>(p);
         return;
     }
-    const int tokens = tokens_of_block(p, D * (int)sizeof(T));
+    const int tokens = tokens_of_block(p, D * (int)sizeof(T), sms);
     if (tokens == 32) launch_seq<T, FP8, D, INTER, 32>(p, stream);
     else if (tokens == 8) launch_seq<T, FP8, D, INTER, 8>(p, stream);
     else launch_seq<T, FP8, D, INTER, 2>(p, stream);
 }
 
 template <bool INTER>
-void launch_type(const plt_rope_config& c, bool seq, const RopeParams& p, cudaStream_t stream) {
-    if (c.kv_dtype == PLT_KV_E4M3) launch_one<__nv_bfloat16, true, 128, INTER>(seq, p, stream);
-    else if (c.dtype == PLT_BF16 && c.d == 128) launch_one<__nv_bfloat16, false, 128, INTER>(seq, p, stream);
-    else if (c.dtype == PLT_BF16) launch_one<__nv_bfloat16, false, 64, INTER>(seq, p, stream);
-    else if (c.d == 128) launch_one<float, false, 128, INTER>(seq, p, stream);
-    else launch_one<float, false, 64, INTER>(seq, p, stream);
+void launch_type(const plt_rope_config& c, bool seq, const RopeParams& p, int sms, cudaStream_t stream) {
+    if (c.kv_dtype == PLT_KV_E4M3) launch_one<__nv_bfloat16, true, 128, INTER>(seq, p, sms, stream);
+    else if (c.dtype == PLT_BF16 && c.d == 128) launch_one<__nv_bfloat16, false, 128, INTER>(seq, p, sms, stream);
+    else if (c.dtype == PLT_BF16) launch_one<__nv_bfloat16, false, 64, INTER>(seq, p, sms, stream);
+    else if (c.d == 128) launch_one<float, false, 128, INTER>(seq, p, sms, stream);
+    else launch_one<float, false, 64, INTER>(seq, p, sms, stream);
 }
 
 plt_status launch(plt_rope_t h, bool seq, const RopeParams& p, cudaStream_t stream) {
     DeviceScope scope(h->device);
     if (scope.err != cudaSuccess) return handle_fail(h, g_rope_error, PLT_ERR_CUDA, "cudaSetDevice: %s", cudaGetErrorString(scope.err));
-    if (h->cfg.layout == PLT_ROPE_INTERLEAVED) launch_type<true>(h->cfg, seq, p, stream);
-    else launch_type<false>(h->cfg, seq, p, stream);
+    if (h->cfg.layout == PLT_ROPE_INTERLEAVED) launch_type<true>(h->cfg, seq, p, h->sms, stream);
+    else launch_type<false>(h->cfg, seq, p, h->sms, stream);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return handle_fail(h, g_rope_error, PLT_ERR_CUDA, "launching the kernel: %s", cudaGetErrorString(e));
     return PLT_OK;
@@ -691,7 +692,8 @@ PLT_API plt_status plt_rope_create(const plt_rope_config* config, plt_rope_t* ou
         (void)cudaGetLastError();
         return handle_fail(nullptr, g_rope_error, PLT_ERR_CUDA, "cudaSetDevice: %s", cudaGetErrorString(scope.err));
     }
-    s = check_device(config->device, g_rope_error, nullptr);
+    int sms = 0;
+    s = check_device(config->device, g_rope_error, &sms);
     if (s != PLT_OK) return s;
     plt_rope* h = new (std::nothrow) plt_rope();
     if (!h) return rope_fail(nullptr, PLT_ERR_OUT_OF_MEMORY, "host allocation failed");
@@ -700,6 +702,7 @@ PLT_API plt_status plt_rope_create(const plt_rope_config* config, plt_rope_t* ou
     h->cfg.inv_freq = nullptr;
     h->device = config->device;
     h->rd = rd;
+    h->sms = sms;
     h->Qn = config->q_len > 1 ? config->q_len : 1;
     for (int l = 0; l < kMaxLoops; ++l) h->delta[l] = config->loop_offset && l < config->L ? config->loop_offset[l] : l;
     void* ws = nullptr;
