@@ -34,7 +34,7 @@
 // hi), as in the decode step's kernel. Scores above a limit, a share of the row's sum when it was last taken, send a warp the longer
 // way, with the vote that lets a reference move: it takes the sum anew and, where a probability is above the share of it, leaves lo
 // behind hi in tensor memory and sets a flag, by which the issuing warp adds a second product on the lanes of the warps that did (the
-// others' lanes are masked off). That way costs 36.5 us instead of 34.0 (64 sequences of two loops behind 4096 tokens), 149.5 instead
+// others' lanes are masked off). That way costs 36.2 us instead of 34.0 (64 sequences of two loops behind 4096 tokens), 146 instead
 // of 142 (128 behind 32768), 16.1 instead of 15.6 (two users): the first halves of a piece take it, and scores outrun the limit now
 // and then until the sum has grown.
 // Every wait is bounded and reports through the status word.
@@ -879,7 +879,6 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                     tmem_wait_ld();
                     if (key + 64 > all_see) p_mask(r, sees0 - key - 2 * (lane & 3), sees1 - key - 2 * (lane & 3));
                     const float top0 = p_max<0>(r) * scale, top1 = p_max<2>(r) * scale;
-                    uint32_t pk[16];
                     const bool high = first || top0 > (FP8 ? m0 + kAbove<FP8> : most0) || top1 > (FP8 ? m1 + kAbove<FP8> : most1);
                     const bool slow = __any_sync(0xffffffffu, high || (!FP8 && (told >> h & 1u) != 0));
                     if (slow) {
@@ -902,7 +901,9 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                             }
                         }
                         if (!FP8) {
+                            uint32_t pk[16];          // (registers that both ways shared took 148.0 us instead of 145.5)
                             p_half<FP8, true>(r, scale, m0, m1, pk, sum0, sum1);
+                            tmem_st_pairs16(tS + h * 64, pk);
                             const float all0 = row_sum(sum0.x + sum0.y) * exp2f(-kShareBits), all1 = row_sum(sum1.x + sum1.y) * exp2f(-kShareBits);
                             const bool second = __any_sync(0xffffffffu, fast_exp2(top0 - m0) > all0 || fast_exp2(top1 - m1) > all1);
                             most0 = m0 + fminf(__log2f(all0), kAbove<FP8>);
@@ -915,15 +916,18 @@ plt_prefix_main(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
                             if (lane == 0) s_lo[(2 * x + h) * 8 + half * 4 + wq] = second;
                         }
                     }
-                    if (FP8 || !slow) p_half<FP8, false>(r, scale, m0, m1, pk, sum0, sum1);
-                    tmem_st_pairs16(tS + h * 64, pk);
+                    if (FP8 || !slow) {
+                        uint32_t pk[16];
+                        p_half<FP8, false>(r, scale, m0, m1, pk, sum0, sum1);
+                        tmem_st_pairs16(tS + h * 64, pk);
+                    }
                     tmem_wait_st();
                     tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bars[C::PFULL + 2 * x + h]);
                 };
-                // halves one behind the other in the code only where it is short enough: with second terms a copy for each took 149.0 us
-                // against 148.7 (128 sequences behind 32768 tokens), 37.1 against 36.5 (64 behind 4096); 8-bit caches 42.4 against 44.1
+                // a copy of the code for each half only where it is short enough: with second terms copies took 146.4 us against 145.5 (128
+                // sequences behind 32768 tokens) and 36.9 against 36.2 (64 behind 4096); 8-bit caches 42.4 against 44.1
                 if constexpr (FP8) {
                     half_tile(0);
                     if (ok) half_tile(1);
