@@ -67,7 +67,6 @@ struct PrefixRun {
     bool fp8;
 };
 
-size_t prefix_smem(int d, bool fp8);
 cudaError_t prefix_prepare(int d, bool fp8);
 cudaError_t launch_prefix_plan(const PrefixParams& pp, cudaStream_t stream);
 cudaError_t launch_prefix_main(const CUtensorMap maps[3], const PrefixParams& pp, bool fp8, cudaStream_t stream);

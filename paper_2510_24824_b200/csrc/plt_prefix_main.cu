@@ -1097,8 +1097,6 @@ cudaError_t launch_one(const CUtensorMap maps[3], const PrefixParams& pp, cudaSt
 
 }  // namespace
 
-size_t prefix_smem(int d, bool fp8) { return fp8 ? PCfg<128, true>::SMEM : d == 128 ? PCfg<128, false>::SMEM : PCfg<64, false>::SMEM; }
-
 cudaError_t prefix_prepare(int d, bool fp8) {
     return allow_max_dynamic_smem(fp8 ? (const void*)plt_prefix_main<128, true>
                                       : d == 128 ? (const void*)plt_prefix_main<128, false> : (const void*)plt_prefix_main<64, false>);
