@@ -11,7 +11,8 @@
  * Everything else is plt_decode_attn_run's: seq_lens count the prefix, loop l's token j sees
  * cut = max(0, seq_lens[b] - delta_l - (q_len - 1 - j)) positions, which may end inside the prefix; loops 2..L mix in their windows
  * by the gate; one softmax runs over prefix and own keys; rows without a token are zero.  Sequences behind the last group have
- * no prefix.
+ * no prefix.  bf16 probabilities that hold a large share of a row's weight meet the values in two terms on the prefix too, so that
+ * results keep the decode step's bounds wherever a token lies.
  *
  * All tensor pointers are DEVICE pointers owned by the caller.  No exception crosses this boundary; errors are plt_status
  * codes.  There is no CPU fallback.  The device of a handle is made current for the length of each call; the stream must

@@ -20,8 +20,8 @@
  *                         first = max(floor(c(high)), 0), last = min(ceil(c(low)), rotary_dim - 1),
  *                         c(t) = rotary_dim log(original_len / (2 pi t)) / (2 log theta)
  *
- * or from the caller (inv_freq).  Angles are taken modulo a turn in 64-bit integers, to 2^-32 of a turn at any position, and
- * rounded to fp32 then; norm, rotation and gates are held in fp32 (a row to be normed has to have a sum of squares below 2^128),
+ * or from the caller (inv_freq).  Angles are taken modulo a turn in 64-bit integers, to 2^-32 of a turn at any position (for
+ * frequencies of up to a turn a position; faster ones lose in proportion), and rounded to fp32 then; norm, rotation and gates are held in fp32 (a row to be normed has to have a sum of squares below 2^128),
  * and each result is rounded once, to the type it is stored in (E4M3: the code nearest to value / scale[head]).
  *
  * All tensor pointers are DEVICE pointers owned by the caller unless a comment says "host".  No exception crosses this

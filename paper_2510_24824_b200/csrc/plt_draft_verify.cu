@@ -7,8 +7,8 @@
 // running sum passes r * total, and that chunk (still in L2) to the token. The weights are never written. Where there are few
 // chunks, latency counts and (2) does the work of (1) itself.
 //
-// Bound by reading one row of p and, after a refusal, one of q: 256 sequences of 131072 fp32 take 42.4 us, 268 MB of p and q at 6.3
-// TB/s (kernels alone 39.4). One sequence of 32768 takes 5.5 us, which is two dependent launches; 48 copied drafts of 50257 bf16 7.8.
+// Bound by reading one row of p and, after a refusal, one of q: 256 sequences of 131072 fp32 take 42 us (39.5 in a graph), 189 MB of p
+// and q, which the copy rate would take 29.2 for: two more starts, and additions in 64 bits. One sequence of 32768 takes 5.5 us, which is two dependent launches; 48 copied drafts of 50257 bf16 7.8.
 #include "../../include/plt_draft_verify.h"
 
 #include <cuda_bf16.h>

@@ -14,12 +14,12 @@ constexpr int kPrefixLead = 2;        // line positions that stand for starting 
 //     the same number of nearly equal pieces of at most `*chunk` tiles, and piece i is block i's and leaves its partial in slot i.
 //   - Else (*chunk = 0) the units lie one after the other on a line of key tiles, each preceded by kPrefixLead positions, and the
 //     line is cut into equal ranges, one for each block, which may hold several pieces; slot unit + block.
-// The line for all calls measured 18.0 us against 15.9 (two users), 26.4 against 20.0 (21 sequences of drafts), 33.4 against 33.0 (64
-// sequences of two loops), 150 against 139 (128 of them behind 32768 tokens), and 40.4 against 41.2 for three groups of 8-bit caches.
+// The line for all calls measured 19.0 us against 15.7 (two users), 28.3 against 21.9 (21 sequences of drafts), 36.9 against 36.2 (64
+// sequences of two loops), 157 against 146 (128 of them behind 32768 tokens), and 41.4 against 42.8 for three groups of 8-bit caches.
 // Not every block need take part: the pass over the prefixes is bound by the tensor cores and its start, the one over the own caches
 // by memory and its start, so that the plan may leave some multiprocessors to the latter, which then runs at the same time.
 //
-// The plan reaches the kernels behind by release and acquire: its writer releases `ready[0]`, the pass over the own caches and the merge
+// The plan reaches the kernels behind by release and acquire (0.3 to 1 us a call): its writer releases `ready[0]`, the pass over the own caches and the merge
 // acquire it before they read a word of the plan. (griddepcontrol.launch_dependents only lets them start: it makes nothing visible,
 // and a griddepcontrol.wait would have them wait for the prefixes' products.) The merge's last block to pass by, counted in ready[1],
 // sets both words back behind its griddepcontrol.wait, so that every call finds them 0.

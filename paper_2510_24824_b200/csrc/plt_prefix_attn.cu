@@ -224,16 +224,17 @@ PLT_API plt_status plt_prefix_attn_run(plt_prefix_attn_t h, const plt_decode_att
     p.group_begin = x->group_begin; p.prefix_lens = x->prefix_lens; p.page_table = x->page_table;
     p.plan = h->plan; p.acc = h->acc; p.ml = h->ml; p.status = h->status;
     p.groups = x->num_groups; p.max_prefix_len = c.max_prefix_len; p.max_pages = x->max_pages; p.blocks = h->blocks;
-    // Query rows by TMA where whole tokens make up a tile; by the softmax's threads two users take 16.4 us instead of 15.9, 64 sequences
-    // of two loops 35.8 instead of 33.0.
+    // Query rows by TMA where whole tokens make up a tile; by the softmax's threads two users take 16.1 us instead of 15.7, 64 sequences
+    // of two loops 39.5 instead of 36.2.
     p.q_tma = 128 % h->G == 0;
     // Rates that the plan divides the multiprocessors by, read off batches of 21 to 96 sequences behind 1777 to 8192 tokens with 9 to
     // 138 multiprocessors left to the own caches: a key tile of 256 rows takes 1.9 us (8-bit caches 3.0) with the pass's start; of the
     // own caches a multiprocessor streams 80 bytes a nanosecond at up to 8 packed rows, and less where its products bound it: 50 at 16
     // and 24 at 32 (8-bit caches 36 at 16; with heads of 64 58 at 8; the others go on from these). Tiles of 1.5 us give the same times
-    // within 1 %, of 1.3 us drafts lose (32 us instead of 20). With the multiprocessors divided and with one pass behind the other: 64
-    // sequences of two loops 33.0 and 40.7 us, groups of 8-bit caches 41.2 and 49.1, drafts 20.0 and 25.8, 128 sequences behind 32768
-    // tokens 139 and 158.
+    // within 1 %, of 1.3 us drafts lose (32 us instead of 20, both before probabilities had second terms; tiles of 2.1 us give the same times, of
+    // 2.3 us the long prefixes lose, 208 instead of 149). With the multiprocessors divided and with one pass behind the other: 64
+    // sequences of two loops 36.2 and 43.6 us, groups of 8-bit caches 42.8 and 49.2, drafts 21.9 and 27.2, 128 sequences behind 32768
+    // tokens 146 and 164.
     p.tile_ns = fp8 ? 3000 : 1900;
     p.own_rate = h->R <= 8 ? 80 : h->R <= 16 ? (fp8 ? 36 : 50) : h->R <= 32 ? (fp8 ? 18 : 24) : (fp8 ? 9 : 12);
     if (c.d == 64) p.own_rate = p.own_rate * 7 / 10;

@@ -9,8 +9,9 @@
 // with an online softmax whose reference maximum is moved only when a score outruns it by more than a few powers of two. A unit
 // is two such tiles of 128 rows, A and B, of one KV head. Where a unit has more than 128 rows, both tiles take every key tile, so
 // that each K/V tile in shared memory serves 256 rows; where it has fewer, A and B are the same rows and take the key tiles in
-// turn. Blocks are persistent: each takes an equal range of a line on which the units' key tiles lie one behind the other, and
-// leaves unnormalised partials for the merge.
+// turn. Blocks are persistent, and leave unnormalised partials for the merge. Where the units can be cut into about as many equal
+// pieces as there are blocks, each takes one piece; else each takes an equal range of a line on which the units' key tiles lie one behind
+// the other.
 //
 // A tile's scores come in two halves of 64 keys, each with tensor memory and barriers of its own: while the warps work on one, the
 // products of the other (P . V of these keys, then the next key tile's scores) run. With whole tiles a tile's softmax and its
@@ -20,8 +21,8 @@
 // as much in waits and commits as its products take.
 //
 // What bounds it: on long prefixes the 16 warps of the softmax, always busy with a latency chain of loads, maximum, exponentials and
-// stores, next to the products (2600 cycles of some 3500 for a wide key tile), under the power limit: 1.09 PFLOP/s (128 sequences of
-// two loops behind 32768 tokens, 126 us). On short ones the start: the plan, and code that a launch finds outside the instruction
+// stores, next to the products (2600 cycles of some 3500 for a wide key tile), under the power limit: 1.04 PFLOP/s (128 sequences of
+// two loops behind 32768 tokens, 133 us). On short ones the start: the plan, and code that a launch finds outside the instruction
 // caches, so that what lies between the launch and the first product is kept short: 3 us of plan, 4 to the first scores.
 //
 // Warp roles: warp 0 loads K and V tiles by TMA into a ring (pages: their ids one tile ahead); warps 1 and 3 load query tiles and issue
@@ -201,7 +202,7 @@ __device__ __forceinline__ void plan_by_warp(const PrefixParams& p, const Prefix
     // How many blocks take part. What both passes take is estimated for sixteen ways of dividing the multiprocessors, a lane each (in
     // every block by the same instructions, so that all come to the same plan); none for the own caches means one pass behind the
     // other. Where the prefixes have so few tiles that half of the blocks stay idle, those are the own caches' anyway, and the
-    // estimate (0.9 us, before the pass over the own caches can start) is left out.
+    // estimate (1.1 us, before the pass over the own caches can start) is left out.
     int blocks = p.blocks, own_blocks = 0x7fffffff;
     if (p.own_per_sm > 0 && all * 2 > p.blocks) {
         const bool wide = (rows - 1) % kPrefixRows >= 128;      // of a group's units all but the last are; that one may have half the work

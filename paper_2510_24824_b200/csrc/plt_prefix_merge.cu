@@ -296,11 +296,11 @@ cudaError_t launch(const Params& p, const PrefixParams& pp, bool overlap, cudaSt
 
 template <int D>
 cudaError_t launch_for(const Params& p, const PrefixParams& pp, bool overlap, cudaStream_t stream) {
-    // Four warps to a row as long as all run at once (32 on each multiprocessor): the step of two users 15.9 us against 16.6, drafts of
-    // 21 sequences 20.0 against 20.7, 16 sequences 19.2 against 21.4, 32 of two loops 25.1 against 26.1; where they do not, 64 of two
-    // loops 36.2 against 33.0, 128 of them 142.8 against 138.6. Sixteen where few units of long prefixes may have been cut into many
-    // pieces (one sequence behind 12615 tokens of one KV head 19.3 us against 28.0, 6 behind two prefixes of 32705 29.5 against 34.7;
-    // short prefixes lose half a microsecond).
+    // Four warps to a row as long as all run at once (32 on each multiprocessor): the step of two users 15.7 us against 16.4, drafts of
+    // 21 sequences 21.9 against 22.7, 32 sequences of two loops 27.7 against 28.3; where they do not, 64 of two loops 40.2 against 36.2,
+    // 128 of them 153 against 146. Sixteen where few units of long prefixes may have been cut into many pieces (one sequence of 2 heads
+    // behind 12615 tokens 21.8 us against 29.0, 6 of 4 heads behind two prefixes of 32705 31.5 against 37.2; short prefixes lose half a
+    // microsecond).
     const int64_t warps = (int64_t)(p.B * p.R + 31) / 32 * p.Hkv * (D / 8);
     const int pieces = min(pp.blocks / p.Hkv, (pp.max_prefix_len + kPrefixTile - 1) / kPrefixTile);      // of a unit, at most
     if (warps * 16 <= pp.blocks * 32 && pieces > 8) return launch<D, 16>(p, pp, overlap, stream);
